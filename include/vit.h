@@ -46,7 +46,8 @@ enum {
   VIT_ERR_NO_DEVICE = -7,   /* no sm_100 device / driver available */
   VIT_ERR_TOO_LARGE = -8,   /* problem exceeds the fixed scratch of an allocation-free entry point,
                                or the partitioner's tables do not fit in host memory */
-  VIT_ERR_INFEASIBLE = -9   /* the partitioner found no assignment that fits the devices' memory */
+  VIT_ERR_INFEASIBLE = -9,  /* the partitioner found no assignment that fits the devices' memory */
+  VIT_ERR_OFFSETS = -10     /* device status word: a packed sequence's offsets were out of order or range */
 };
 
 enum { VIT_BF16 = 0, VIT_FP32 = 1 };
@@ -295,6 +296,89 @@ int vit_op_linear_ln(vit_handle* h, int M, int N, int K, const void* a, const fl
  * out_h = softmax_rows(Q_h K_h^T / sqrt(d)) V_h. */
 int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int d,
                      const void* qkv, void* out, void* stream);
+
+/* ---- packed images: position rotation, query/key norm, attention and their gradients ---------
+ * A batch of images of different sizes is one buffer of tokens, image after image.  These operations
+ * serve such a layer between its QKV product and its output product, in inference and fine-tuning.
+ * Rows have strides of their own (`ld...`, in elements), so that queries, keys and values can be read
+ * from, and their gradients written to, the column blocks of one [rows, (heads + 2 kv_heads) * d] buffer.
+ * Common rules, checked before anything is launched: pointers 16-byte aligned; d a multiple of 16, at
+ * most 128; a stride at least as wide as its heads and a multiple of 8; no output may overlap an input
+ * or another output unless stated (column blocks of one buffer with the same stride do not overlap).
+ * Sums, norms and softmax statistics are fp32; bf16 results are rounded once.
+ * Results do not depend on the schedule: the same call gives the same bits. */
+
+/* Rotary positions on one to four axes (row and column of a patch, frame of a video).  Pair i of a head
+ * (0 <= i < n, n = sum of pairs[a]) belongs to the axis whose section it lies in: the first pairs[0]
+ * pairs to axis 0, the next pairs[1] to axis 1, and so on.  It is turned by the angle
+ * positions[axis * rows + row] * freqs[i] (radians; the product is taken in 64 bits, so that far
+ * positions keep their angle).  Channels from 2 n on are passed on as they are. */
+typedef struct vit_rope {
+  int32_t axes;               /* 1 ... 4 */
+  int32_t pairs[4];           /* pairs of channels of each axis, >= 0; 2 n <= d */
+  int32_t interleaved;        /* pair i is the channels (2 i, 2 i + 1) if not 0, else (i, n + i) */
+  const int32_t* positions;   /* dev [axes][rows] */
+  const float* freqs;         /* dev [n] */
+} vit_rope;
+
+/* y = x with every head's pairs turned; inverse != 0 turns them back, which is also the gradient.
+ *   x, y: activations [rows, heads * d] with strides ldx, ldy; x == y with ldx == ldy is allowed. */
+int vit_op_rope_axes(vit_handle* h, int dtype, int rows, int heads, int d, const vit_rope* rope, int inverse,
+                     const void* x, int64_t ldx, void* y, int64_t ldy, void* stream);
+
+/* Norm of queries and keys, then the rotation: every head becomes gain * x / sqrt(mean(x^2) + eps), turned.
+ *   x, y: activations [rows, (q_heads + k_heads) * d]: query heads first, then key heads;
+ *   x == y with ldx == ldy is allowed.  q_gain, k_gain: dev fp32 [d].  rope: NULL for no rotation. */
+int vit_op_qk_norm_rope(vit_handle* h, int dtype, int rows, int q_heads, int k_heads, int d, const float* q_gain,
+                        const float* k_gain, float eps, const vit_rope* rope, const void* x, int64_t ldx, void* y,
+                        int64_t ldy, void* stream);
+
+/* Bytes of scratch for vit_op_qk_norm_rope_backward; 0 if an argument is invalid. */
+size_t vit_qk_norm_rope_backward_bytes(int rows, int q_heads, int k_heads, int d);
+
+/* Gradients of vit_op_qk_norm_rope: dx from x (its input) and dy, and the sums over rows and heads
+ * dq_gain, dk_gain (dev fp32 [d], overwritten; zero for no rows).  dx == x or dx == dy with the same
+ * stride is allowed. */
+int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads, int k_heads, int d,
+                                 const float* q_gain, const float* k_gain, float eps, const vit_rope* rope,
+                                 const void* x, int64_t ldx, const void* dy, int64_t lddy, void* dx, int64_t lddx,
+                                 float* dq_gain, float* dk_gain, void* ws, size_t ws_bytes, void* stream);
+
+/* Softmax attention of packed sequences: the queries of sequence i are rows q_offsets[i] ... q_offsets[i+1] - 1
+ * of q, its keys and values rows k_offsets[i] ... k_offsets[i+1] - 1 of k and v (self-attention passes the same
+ * offsets twice; attention pooling has one query per image).  heads is a multiple of kv_heads; query head j
+ * reads key head j / (heads / kv_heads).
+ * The offsets are read on the device.  A sequence whose offsets are out of order, reach outside the buffers or
+ * make it longer than max_q / max_k is skipped, its rows are left as they were, and vit_check_status reports
+ * VIT_ERR_OFFSETS.  Rows that no sequence covers are left as they were. */
+typedef struct vit_attention_problem {
+  int32_t sequences, heads, kv_heads, d;
+  int32_t q_rows, max_q;      /* rows of q; bound on the length of a sequence's queries */
+  int32_t k_rows, max_k;      /* rows of k and v; bound on the length of its keys */
+  const int32_t* q_offsets;   /* dev [sequences + 1] */
+  const int32_t* k_offsets;   /* dev [sequences + 1] */
+  float scale;                /* of the scores, usually 1 / sqrt(d); finite and positive */
+} vit_attention_problem;
+
+/* Bytes of scratch for vit_op_attention_packed (backward == 0) or its gradients; 0 if none is needed or an
+ * argument is invalid. */
+size_t vit_attention_packed_bytes(int dtype, const vit_attention_problem* problem, int backward);
+
+/* out[r, j] = softmax(scale q[r, j] . k^T) v over the row's sequence, and lse[j * q_rows + r] = log of the sum
+ * of exp(scale q[r, j] . k), which the gradients need.  A query without keys gives out = 0, lse = -infinity.
+ *   q, out: activations [q_rows, heads * d]; k, v: [k_rows, kv_heads * d]; lse: dev fp32 [heads][q_rows]. */
+int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_problem* problem, const void* q, int64_t ldq,
+                            const void* k, int64_t ldk, const void* v, int64_t ldv, void* out, int64_t ldo, float* lse,
+                            void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients of vit_op_attention_packed from its operands, its two results and dout.  The probabilities are
+ * computed again from lse.  dk and dv of a key head are summed over the query heads that share it.
+ *   dq: activations [q_rows, heads * d]; dk, dv: [k_rows, kv_heads * d]. */
+int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attention_problem* problem, const void* q,
+                                     int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                     const void* out, int64_t ldo, const float* lse, const void* dout, int64_t lddo,
+                                     void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* ws,
+                                     size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,6 +20,7 @@ VIT_ERR_INVALID_ARG, VIT_ERR_RANGE, VIT_ERR_CONFIG, VIT_ERR_WORKSPACE = -1, -2, 
 VIT_ERR_CUDA, VIT_ERR_TIMEOUT, VIT_ERR_NO_DEVICE = -5, -6, -7
 VIT_ERR_TOO_LARGE = -8
 VIT_ERR_INFEASIBLE = -9
+VIT_ERR_OFFSETS = -10
 VIT_HEAD_STATIC_MAX_FLOATS = 512 * 1024
 VIT_BF16, VIT_FP32 = 0, 1
 VIT_TILING_AUTO, VIT_TILING_128x128, VIT_TILING_128x256, VIT_TILING_PAIR_256x256 = 0, 1, 2, 3
@@ -30,7 +31,9 @@ EXPORTS = [
     "vit_run_pipeline_host", "vit_run_pipeline_grouped", "vit_check_status", "vit_launch_count", "vit_status_string",
     "vit_op_layernorm", "vit_op_linear", "vit_op_linear_tiled", "vit_op_attention", "vit_op_rowstats", "vit_op_linear_ln", "vit_profile_enable",
     "vit_profile_collect", "vit_head_static", "vit_partition", "vit_partition_categories",
-    "vit_debug_wait_probe",
+    "vit_debug_wait_probe", "vit_op_rope_axes", "vit_op_qk_norm_rope", "vit_qk_norm_rope_backward_bytes",
+    "vit_op_qk_norm_rope_backward", "vit_attention_packed_bytes", "vit_op_attention_packed",
+    "vit_op_attention_packed_backward",
 ]
 PROF_CLASSES = ["layernorm", "qkv", "attention", "outproj", "fc1", "fc2", "embed", "head", "op"]
 
@@ -48,6 +51,21 @@ class VitPartitionProblem(Structure):
     _fields_ = [
         ("layers", c_int32), ("devices", c_int32), ("layer_time", c_void_p), ("out_bytes", c_void_p),
         ("layer_mem", c_void_p), ("device_mem", c_void_p), ("bandwidth", c_void_p),
+    ]
+
+
+class VitRope(Structure):
+    _fields_ = [
+        ("axes", c_int32), ("pairs", c_int32 * 4), ("interleaved", c_int32), ("positions", c_void_p),
+        ("freqs", c_void_p),
+    ]
+
+
+class VitAttentionProblem(Structure):
+    _fields_ = [
+        ("sequences", c_int32), ("heads", c_int32), ("kv_heads", c_int32), ("d", c_int32), ("q_rows", c_int32),
+        ("max_q", c_int32), ("k_rows", c_int32), ("max_k", c_int32), ("q_offsets", c_void_p),
+        ("k_offsets", c_void_p), ("scale", c_float),
     ]
 
 
@@ -111,6 +129,27 @@ def lib():
                                    c_int, c_void_p, c_int, c_void_p]
     L.vit_op_attention.restype = c_int
     L.vit_op_attention.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]
+    i64, pf = ctypes.c_int64, c_void_p
+    L.vit_op_rope_axes.restype = c_int
+    L.vit_op_rope_axes.argtypes = [c_void_p, c_int, c_int, c_int, c_int, P(VitRope), c_int, c_void_p, i64, c_void_p, i64,
+                                   c_void_p]
+    L.vit_op_qk_norm_rope.restype = c_int
+    L.vit_op_qk_norm_rope.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int, pf, pf, c_float, P(VitRope), c_void_p,
+                                      i64, c_void_p, i64, c_void_p]
+    L.vit_qk_norm_rope_backward_bytes.restype = c_size_t
+    L.vit_qk_norm_rope_backward_bytes.argtypes = [c_int, c_int, c_int, c_int]
+    L.vit_op_qk_norm_rope_backward.restype = c_int
+    L.vit_op_qk_norm_rope_backward.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int, pf, pf, c_float, P(VitRope),
+                                               c_void_p, i64, c_void_p, i64, c_void_p, i64, pf, pf, c_void_p, c_size_t,
+                                               c_void_p]
+    L.vit_attention_packed_bytes.restype = c_size_t
+    L.vit_attention_packed_bytes.argtypes = [c_int, P(VitAttentionProblem), c_int]
+    L.vit_op_attention_packed.restype = c_int
+    L.vit_op_attention_packed.argtypes = [c_void_p, c_int, P(VitAttentionProblem)] + [c_void_p, i64] * 4 + [
+        pf, c_void_p, c_size_t, c_void_p]
+    L.vit_op_attention_packed_backward.restype = c_int
+    L.vit_op_attention_packed_backward.argtypes = [c_void_p, c_int, P(VitAttentionProblem)] + [c_void_p, i64] * 4 + [
+        pf] + [c_void_p, i64] * 4 + [c_void_p, c_size_t, c_void_p]
     L.vit_head_static.restype = c_int
     L.vit_head_static.argtypes = [c_void_p, c_int, c_void_p, c_void_p, c_void_p]
     L.vit_partition.restype = c_int
@@ -312,6 +351,63 @@ def vit_op_linear_ln(h, M, N, K, a, stats, wg, c1, c0, gelu, out, tiling=0, stre
 
 def vit_op_attention(h, dtype, images, T, heads, d, qkv, out, stream=0):
     _check(lib().vit_op_attention(h, dtype, images, T, heads, d, qkv, out, stream), "vit_op_attention")
+
+
+def make_rope(axis_pairs, freqs, positions, interleaved=False) -> VitRope:
+    """Rotary positions: channel pairs per axis (1 to 4 axes), device pointers of the pairs' fp32 frequencies and of
+    the int32 positions [axes][rows]."""
+    n = len(axis_pairs)
+    if not 1 <= n <= 4:
+        raise ValueError("one to four axes")
+    return VitRope(n, (c_int32 * 4)(*axis_pairs), 1 if interleaved else 0, positions, freqs)
+
+
+def make_attention_problem(sequences, heads, kv_heads, d, q_rows, max_q, q_offsets, k_rows, max_k, k_offsets,
+                           scale) -> VitAttentionProblem:
+    """Packed sequences: device pointers of int32 offsets [sequences + 1], bounds on the sequences' lengths."""
+    return VitAttentionProblem(sequences, heads, kv_heads, d, q_rows, max_q, k_rows, max_k, q_offsets, k_offsets, scale)
+
+
+def _ref(struct):
+    return byref(struct) if struct is not None else None
+
+
+def vit_op_rope_axes(h, dtype, rows, heads, d, rope, inverse, x, ldx, y, ldy, stream=0):
+    _check(lib().vit_op_rope_axes(h, dtype, rows, heads, d, _ref(rope), 1 if inverse else 0, x, ldx, y, ldy, stream),
+           "vit_op_rope_axes")
+
+
+def vit_op_qk_norm_rope(h, dtype, rows, q_heads, k_heads, d, q_gain, k_gain, eps, rope, x, ldx, y, ldy, stream=0):
+    """`rope` may be None: norm and gain without a rotation."""
+    _check(lib().vit_op_qk_norm_rope(h, dtype, rows, q_heads, k_heads, d, q_gain, k_gain, eps, _ref(rope), x, ldx, y,
+                                     ldy, stream), "vit_op_qk_norm_rope")
+
+
+def vit_qk_norm_rope_backward_bytes(rows, q_heads, k_heads, d) -> int:
+    return lib().vit_qk_norm_rope_backward_bytes(rows, q_heads, k_heads, d)
+
+
+def vit_op_qk_norm_rope_backward(h, dtype, rows, q_heads, k_heads, d, q_gain, k_gain, eps, rope, x, ldx, dy, lddy, dx,
+                                 lddx, dq_gain, dk_gain, ws, ws_bytes, stream=0):
+    _check(lib().vit_op_qk_norm_rope_backward(h, dtype, rows, q_heads, k_heads, d, q_gain, k_gain, eps, _ref(rope), x,
+                                              ldx, dy, lddy, dx, lddx, dq_gain, dk_gain, ws, ws_bytes, stream),
+           "vit_op_qk_norm_rope_backward")
+
+
+def vit_attention_packed_bytes(dtype, problem, backward) -> int:
+    return lib().vit_attention_packed_bytes(dtype, _ref(problem), 1 if backward else 0)
+
+
+def vit_op_attention_packed(h, dtype, problem, q, ldq, k, ldk, v, ldv, out, ldo, lse, ws, ws_bytes, stream=0):
+    _check(lib().vit_op_attention_packed(h, dtype, _ref(problem), q, ldq, k, ldk, v, ldv, out, ldo, lse, ws, ws_bytes,
+                                         stream), "vit_op_attention_packed")
+
+
+def vit_op_attention_packed_backward(h, dtype, problem, q, ldq, k, ldk, v, ldv, out, ldo, lse, dout, lddo, dq, lddq, dk,
+                                     lddk, dv, lddv, ws, ws_bytes, stream=0):
+    _check(lib().vit_op_attention_packed_backward(h, dtype, _ref(problem), q, ldq, k, ldk, v, ldv, out, ldo, lse, dout,
+                                                  lddo, dq, lddq, dk, lddk, dv, lddv, ws, ws_bytes, stream),
+           "vit_op_attention_packed_backward")
 
 
 # ---- convenience object: owns a handle and torch-allocated buffers --------------------------------

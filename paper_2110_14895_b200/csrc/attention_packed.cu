@@ -1,0 +1,379 @@
+// Attention over packed sequences of any lengths, forward and backward, on the fp32 pipes.
+//
+//   s = scale q k^T, lse = log sum exp s, out = exp(s - lse) v                       (forward)
+//   p = exp(s - lse), delta = rowsum(dout * out), ds = p (dout v^T - delta)
+//   dv = p^T dout, dk = scale ds^T q, dq = scale ds k                                 (backward)
+//
+// A block of 256 threads works on 64 x 64 scores at a time, 4 x 4 of them to a thread; operands are
+// converted to fp32 in shared memory, rows behind the end of a sequence are zero there.  The backward
+// pass is two kernels, one that keeps a tile of keys and walks over the queries (dk, dv) and one that
+// keeps a tile of queries and walks over the keys (dq): seven products instead of five, but every
+// gradient is summed by one block in a fixed order, so that results do not depend on the schedule.
+#include "vit_internal.h"
+#include "attention_packed.cuh"
+
+namespace vit {
+
+namespace {
+
+constexpr int BT = 64;              // rows and columns of a tile of scores
+constexpr int THREADS = 256;
+constexpr int PS = BT + 4;          // row stride of a tile of probabilities
+
+__device__ __forceinline__ float4 load4(const float* a) { return *reinterpret_cast<const float4*>(a); }
+__device__ __forceinline__ float4 load4(const bf16* a) {
+  const uint2 u = *reinterpret_cast<const uint2*>(a);
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+__device__ __forceinline__ void store1(float* a, float v) { *a = v; }
+__device__ __forceinline__ void store1(bf16* a, float v) { *a = __float2bfloat16_rn(v); }
+
+// rows [row0, row0 + 64) of one head as fp32 [64][DP + 4]; rows >= end and columns >= d are zero
+template <typename T, int DP>
+__device__ __forceinline__ void load_tile(float* dst, const T* base, int64_t ld, int64_t row0, int rows, int d) {
+  for (int i = threadIdx.x; i < BT * (DP / 4); i += THREADS) {
+    const int r = i / (DP / 4), c = (i % (DP / 4)) * 4;
+    const float4 v = r < rows && c < d ? load4(base + (row0 + r) * ld + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+    *reinterpret_cast<float4*>(dst + r * (DP + 4) + c) = v;
+  }
+}
+
+// acc[i][j] = a[ty * 4 + i] . b[tx + 16 j] over the head's channels
+template <int DP>
+__device__ __forceinline__ void scores(float (&acc)[4][4], const float* a, const float* b, int tx, int ty) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+  for (int c = 0; c < DP; c += 4) {
+    float4 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = load4(a + (ty * 4 + i) * (DP + 4) + c);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = load4(b + (tx + 16 * j) * (DP + 4) + c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        acc[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, acc[i][j]))));
+  }
+}
+
+// acc[i][cc] += sum over t of w[t][ty * 4 + i] * x[t][tx + 16 cc]      (w transposed: rows are the summed index)
+template <int DP>
+__device__ __forceinline__ void accumulate_t(float (&acc)[4][DP / 16], const float* w, const float* x, int tx, int ty) {
+#pragma unroll 2
+  for (int t = 0; t < BT; ++t) {
+    const float4 p = load4(w + t * PS + ty * 4);
+#pragma unroll
+    for (int cc = 0; cc < DP / 16; ++cc) {
+      const float v = x[t * (DP + 4) + tx + 16 * cc];
+      acc[0][cc] = fmaf(p.x, v, acc[0][cc]);
+      acc[1][cc] = fmaf(p.y, v, acc[1][cc]);
+      acc[2][cc] = fmaf(p.z, v, acc[2][cc]);
+      acc[3][cc] = fmaf(p.w, v, acc[3][cc]);
+    }
+  }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS)
+packed_forward_kernel(const PackedCall c) {
+  extern __shared__ __align__(16) float sm[];
+  float* qs = sm;                               // [64][DP + 4]
+  float* ks = qs + BT * (DP + 4);               // keys, then values
+  float* ps = ks + BT * (DP + 4);               // [key][query]: probabilities, transposed
+  const int tiles = (c.p.max_q + BT - 1) / BT;
+  const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
+  SeqRange r;
+  if (!seq_range(c.p, seq, r, c.dev_status)) return;
+  const int q0 = tile * BT;
+  if (q0 >= r.q_len) return;
+  const int q_here = min(BT, r.q_len - q0), d = c.p.d;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int kv = head / (c.p.heads / c.p.kv_heads);
+  const T* q = static_cast<const T*>(c.q) + (int64_t)head * d;
+  const T* k = static_cast<const T*>(c.k) + (int64_t)kv * d;
+  const T* v = static_cast<const T*>(c.v) + (int64_t)kv * d;
+  const float sl2 = c.p.scale * 1.4426950408889634f;
+
+  load_tile<T, DP>(qs, q, c.ldq, (int64_t)r.q_begin + q0, q_here, d);
+  float m[4], l[4], o[4][DP / 16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int cc = 0; cc < DP / 16; ++cc) o[i][cc] = 0.f;
+  }
+  for (int k0 = 0; k0 < r.k_len; k0 += BT) {
+    const int k_here = min(BT, r.k_len - k0);
+    load_tile<T, DP>(ks, k, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
+    __syncthreads();
+    float s[4][4];
+    scores<DP>(s, qs, ks, tx, ty);
+    __syncthreads();
+    load_tile<T, DP>(ks, v, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float top = m[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = tx + 16 * j < k_here ? s[i][j] * sl2 : -INFINITY;
+        top = fmaxf(top, s[i][j]);
+      }
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+      const float ref = top == -INFINITY ? 0.f : top;      // a row of minus infinities keeps probabilities of zero
+      const float keep = exp2f(m[i] - ref);
+      m[i] = top;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = exp2f(s[i][j] - ref);
+        sum += s[i][j];
+        ps[(tx + 16 * j) * PS + ty * 4 + i] = s[i][j];
+      }
+      l[i] = l[i] * keep + sum;                            // this lane's part of the row sum
+#pragma unroll
+      for (int cc = 0; cc < DP / 16; ++cc) o[i][cc] *= keep;
+    }
+    __syncthreads();
+    accumulate_t<DP>(o, ps, ks, tx, ty);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
+    const int row = ty * 4 + i;
+    if (row >= q_here) continue;
+    const int64_t at = (int64_t)r.q_begin + q0 + row;
+    const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];     // no keys: zero
+    T* out = static_cast<T*>(c.out) + at * c.ldo + (int64_t)head * d;
+#pragma unroll
+    for (int cc = 0; cc < DP / 16; ++cc)
+      if (tx + 16 * cc < d) store1(out + tx + 16 * cc, o[i][cc] * inv);
+    if (tx == 0) c.lse[(int64_t)head * c.p.q_rows + at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718055994531f;
+  }
+}
+
+// delta[head][row] = sum over the head's channels of dout * out: one warp per row and head
+template <typename T>
+__global__ void __launch_bounds__(THREADS)
+packed_delta_kernel(const PackedCall c) {
+  const int64_t item = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const int covered = c.p.q_offsets[c.p.sequences];      // rows behind the last sequence are not looked at
+  const int64_t row = item / c.p.heads;
+  const int head = (int)(item % c.p.heads);
+  if (row >= c.p.q_rows || row >= covered) return;
+  float sum = 0.f;
+  if (lane * 4 < c.p.d) {
+    const int64_t col = (int64_t)head * c.p.d + lane * 4;
+    const float4 a = load4(static_cast<const T*>(c.out) + row * c.ldo + col);
+    const float4 b = load4(static_cast<const T*>(c.dout) + row * c.lddo + col);
+    sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w)));
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+  if (lane == 0) c.delta[(int64_t)head * c.p.q_rows + row] = sum;
+}
+
+// p and ds of a tile: s = q k^T, dp = dout v^T; rows beyond q_here and keys beyond k_here give zero
+__device__ __forceinline__ void grad_scores(float (&s)[4][4], float (&dp)[4][4], const float* lse2, const float* delta, float sl2,
+                                            int q_here, int k_here, int tx, int ty) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = ty * 4 + i;
+    const float ls = lse2[row], de = delta[row];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool there = row < q_here && tx + 16 * j < k_here;
+      const float p = there ? exp2f(fmaf(s[i][j], sl2, -ls)) : 0.f;
+      dp[i][j] = there ? p * (dp[i][j] - de) : 0.f;
+      s[i][j] = p;
+    }
+  }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS)
+packed_dkdv_kernel(const PackedCall c) {
+  extern __shared__ __align__(16) float sm[];
+  constexpr int TILE = BT * (DP + 4);
+  float *ks = sm, *vs = ks + TILE, *qs = vs + TILE, *os = qs + TILE, *ps = os + TILE, *ds = ps + BT * PS;   // ps, ds: [query][key]
+  float *lse2 = ds + BT * PS, *delta = lse2 + BT;
+  const int tiles = (c.p.max_k + BT - 1) / BT;
+  const int tile = blockIdx.x % tiles, kv = blockIdx.x / tiles % c.p.kv_heads, seq = blockIdx.x / tiles / c.p.kv_heads;
+  SeqRange r;
+  if (!seq_range(c.p, seq, r, c.dev_status)) return;
+  const int k0 = tile * BT;
+  if (k0 >= r.k_len) return;
+  const int k_here = min(BT, r.k_len - k0), d = c.p.d, group = c.p.heads / c.p.kv_heads;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const float sl2 = c.p.scale * 1.4426950408889634f;
+  load_tile<T, DP>(ks, static_cast<const T*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
+  load_tile<T, DP>(vs, static_cast<const T*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
+  float dk[4][DP / 16], dv[4][DP / 16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int cc = 0; cc < DP / 16; ++cc) dk[i][cc] = dv[i][cc] = 0.f;
+  for (int head = kv * group; head < (kv + 1) * group; ++head) {
+    for (int q0 = 0; q0 < r.q_len; q0 += BT) {
+      const int q_here = min(BT, r.q_len - q0);
+      const int64_t at = (int64_t)r.q_begin + q0;
+      load_tile<T, DP>(qs, static_cast<const T*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
+      load_tile<T, DP>(os, static_cast<const T*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
+      if (threadIdx.x < BT) {
+        const bool there = (int)threadIdx.x < q_here;
+        const int64_t i = (int64_t)head * c.p.q_rows + at + threadIdx.x;
+        lse2[threadIdx.x] = there ? c.lse[i] * 1.4426950408889634f : 0.f;
+        delta[threadIdx.x] = there ? c.delta[i] : 0.f;
+      }
+      __syncthreads();
+      float s[4][4], dp[4][4];
+      scores<DP>(s, qs, ks, tx, ty);
+      scores<DP>(dp, os, vs, tx, ty);
+      grad_scores(s, dp, lse2, delta, sl2, q_here, k_here, tx, ty);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          ps[(ty * 4 + i) * PS + tx + 16 * j] = s[i][j];
+          ds[(ty * 4 + i) * PS + tx + 16 * j] = dp[i][j];
+        }
+      __syncthreads();
+      accumulate_t<DP>(dv, ps, os, tx, ty);
+      accumulate_t<DP>(dk, ds, qs, tx, ty);
+      __syncthreads();
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = ty * 4 + i;
+    if (row >= k_here) continue;
+    const int64_t at = (int64_t)r.k_begin + k0 + row;
+    T* gk = static_cast<T*>(c.dk) + at * c.lddk + (int64_t)kv * d;
+    T* gv = static_cast<T*>(c.dv) + at * c.lddv + (int64_t)kv * d;
+#pragma unroll
+    for (int cc = 0; cc < DP / 16; ++cc)
+      if (tx + 16 * cc < d) {
+        store1(gk + tx + 16 * cc, dk[i][cc] * c.p.scale);
+        store1(gv + tx + 16 * cc, dv[i][cc]);
+      }
+  }
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(THREADS)
+packed_dq_kernel(const PackedCall c) {
+  extern __shared__ __align__(16) float sm[];
+  constexpr int TILE = BT * (DP + 4);
+  float *qs = sm, *os = qs + TILE, *ks = os + TILE, *vs = ks + TILE, *ds = vs + TILE;       // ds: [key][query]
+  float *lse2 = ds + BT * PS, *delta = lse2 + BT;
+  const int tiles = (c.p.max_q + BT - 1) / BT;
+  const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
+  SeqRange r;
+  if (!seq_range(c.p, seq, r, c.dev_status)) return;
+  const int q0 = tile * BT;
+  if (q0 >= r.q_len) return;
+  const int q_here = min(BT, r.q_len - q0), d = c.p.d, kv = head / (c.p.heads / c.p.kv_heads);
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const float sl2 = c.p.scale * 1.4426950408889634f;
+  const int64_t at = (int64_t)r.q_begin + q0;
+  load_tile<T, DP>(qs, static_cast<const T*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
+  load_tile<T, DP>(os, static_cast<const T*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
+  if (threadIdx.x < BT) {
+    const bool there = (int)threadIdx.x < q_here;
+    const int64_t i = (int64_t)head * c.p.q_rows + at + threadIdx.x;
+    lse2[threadIdx.x] = there ? c.lse[i] * 1.4426950408889634f : 0.f;
+    delta[threadIdx.x] = there ? c.delta[i] : 0.f;
+  }
+  float dq[4][DP / 16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int cc = 0; cc < DP / 16; ++cc) dq[i][cc] = 0.f;
+  for (int k0 = 0; k0 < r.k_len; k0 += BT) {
+    const int k_here = min(BT, r.k_len - k0);
+    load_tile<T, DP>(ks, static_cast<const T*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
+    load_tile<T, DP>(vs, static_cast<const T*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
+    __syncthreads();
+    float s[4][4], dp[4][4];
+    scores<DP>(s, qs, ks, tx, ty);
+    scores<DP>(dp, os, vs, tx, ty);
+    grad_scores(s, dp, lse2, delta, sl2, q_here, k_here, tx, ty);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ds[(tx + 16 * j) * PS + ty * 4 + i] = dp[i][j];
+    __syncthreads();
+    accumulate_t<DP>(dq, ds, ks, tx, ty);
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = ty * 4 + i;
+    if (row >= q_here) continue;
+    T* g = static_cast<T*>(c.dq) + (at + row) * c.lddq + (int64_t)head * d;
+#pragma unroll
+    for (int cc = 0; cc < DP / 16; ++cc)
+      if (tx + 16 * cc < d) store1(g + tx + 16 * cc, dq[i][cc] * c.p.scale);
+  }
+}
+
+enum Which { FORWARD, DKDV, DQ };
+
+template <typename T, int DP>
+cudaError_t launch_variant(const PackedCall& c, Which w, cudaStream_t s) {
+  constexpr size_t tile = (size_t)BT * (DP + 4) * 4, prob = (size_t)BT * PS * 4;
+  if (w == FORWARD) {
+    static PerDeviceFlag done;
+    const size_t smem = 2 * tile + prob;
+    if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_kernel<T, DP>, (int)smem)) return e;
+    packed_forward_kernel<T, DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
+  } else if (w == DKDV) {
+    static PerDeviceFlag done;
+    const size_t smem = 4 * tile + 2 * prob + 2 * BT * 4;
+    if (cudaError_t e = ensure_dynamic_smem(done, packed_dkdv_kernel<T, DP>, (int)smem)) return e;
+    packed_dkdv_kernel<T, DP><<<c.p.sequences * c.p.kv_heads * ((c.p.max_k + BT - 1) / BT), THREADS, smem, s>>>(c);
+  } else {
+    static PerDeviceFlag done;
+    const size_t smem = 4 * tile + prob + 2 * BT * 4;
+    if (cudaError_t e = ensure_dynamic_smem(done, packed_dq_kernel<T, DP>, (int)smem)) return e;
+    packed_dq_kernel<T, DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
+  }
+  return cudaGetLastError();
+}
+template <typename T>
+cudaError_t launch_width(const PackedCall& c, Which w, cudaStream_t s) {
+  if (c.p.d <= 32) return launch_variant<T, 32>(c, w, s);
+  if (c.p.d <= 64) return launch_variant<T, 64>(c, w, s);
+  if (c.p.d <= 96) return launch_variant<T, 96>(c, w, s);
+  return launch_variant<T, 128>(c, w, s);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) { return launch_width<float>(c, FORWARD, s); }
+cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s) { return launch_width<bf16>(c, FORWARD, s); }
+
+cudaError_t launch_attention_delta(const PackedCall& c, bool act_bf16, cudaStream_t s) {
+  const int64_t items = (int64_t)c.p.q_rows * c.p.heads;
+  const unsigned blocks = (unsigned)((items + THREADS / 32 - 1) / (THREADS / 32));
+  if (act_bf16) packed_delta_kernel<bf16><<<blocks, THREADS, 0, s>>>(c);
+  else packed_delta_kernel<float><<<blocks, THREADS, 0, s>>>(c);
+  return cudaGetLastError();
+}
+cudaError_t launch_attention_packed_dkdv(const PackedCall& c, bool act_bf16, cudaStream_t s) {
+  return act_bf16 ? launch_width<bf16>(c, DKDV, s) : launch_width<float>(c, DKDV, s);
+}
+cudaError_t launch_attention_packed_dq(const PackedCall& c, bool act_bf16, cudaStream_t s) {
+  return act_bf16 ? launch_width<bf16>(c, DQ, s) : launch_width<float>(c, DQ, s);
+}
+
+}  // namespace vit

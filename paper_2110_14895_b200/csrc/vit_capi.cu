@@ -223,6 +223,58 @@ int run_pipeline(vit_handle* h, const int32_t* stage_layers, int n_stages, int b
   return VIT_OK;
 }
 
+// ---- packed operations: a buffer of rows with a stride, seen as bytes
+struct Block { const void* p; int64_t rows, width, ld; size_t es; };   // width, ld in elements
+
+bool block_ok(const Block& b) {
+  if (b.ld < b.width || b.ld % 8) return false;
+  if (b.rows <= 0) return true;                       // nothing is read or written there
+  return b.p && !misaligned(b.p) && b.ld <= INT64_MAX / 16 / b.rows;
+}
+bool blocks_overlap(const Block& a, const Block& b) {
+  if (a.rows <= 0 || b.rows <= 0 || a.width <= 0 || b.width <= 0) return false;
+  const uint64_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  const uint64_t a1 = a0 + ((a.rows - 1) * a.ld + a.width) * a.es, b1 = b0 + ((b.rows - 1) * b.ld + b.width) * b.es;
+  if (a1 <= b0 || b1 <= a0) return false;
+  if (a.ld != b.ld || a.es != b.es) return true;
+  // the same stride: column blocks of one buffer
+  const uint64_t pitch = (uint64_t)a.ld * a.es;
+  const uint64_t off = b0 >= a0 ? (b0 - a0) % pitch : (pitch - (a0 - b0) % pitch) % pitch;   // of b's columns behind a's
+  return !(off >= a.width * a.es && off + b.width * b.es <= pitch);
+}
+bool same_block(const Block& a, const Block& b) { return a.p == b.p && a.ld == b.ld; }
+
+size_t element_bytes(int dtype) { return dtype == VIT_BF16 ? 2 : 4; }
+
+bool head_ok(int dtype, int d) { return (dtype == VIT_BF16 || dtype == VIT_FP32) && d >= 16 && d <= 128 && d % 16 == 0; }
+
+bool rope_ok(const vit_rope* r, int d) {
+  if (r->axes < 1 || r->axes > 4) return false;
+  int64_t n = 0;
+  for (int a = 0; a < r->axes; ++a) {
+    if (r->pairs[a] < 0) return false;
+    n += r->pairs[a];
+  }
+  return 2 * n <= d && r->positions && r->freqs && !misaligned(r->positions) && !misaligned(r->freqs);
+}
+
+bool attention_problem_ok(int dtype, const vit_attention_problem* p) {
+  if (!p || !head_ok(dtype, p->d) || p->sequences < 0 || p->heads < 1 || p->kv_heads < 1 || p->heads % p->kv_heads) return false;
+  if (p->q_rows < 0 || p->k_rows < 0 || p->max_q < 0 || p->max_k < 0 || !p->q_offsets || !p->k_offsets) return false;
+  if ((reinterpret_cast<uintptr_t>(p->q_offsets) | reinterpret_cast<uintptr_t>(p->k_offsets)) & 3) return false;
+  if ((int64_t)p->heads * p->d > INT32_MAX) return false;
+  return p->scale > 0.f && p->scale <= 3.402823466e38f;
+}
+// blocks of the launches: one per sequence, head and tile of at least 64 rows
+bool attention_fits(const vit_attention_problem* p) {
+  const int64_t longest = p->max_q > p->max_k ? p->max_q : p->max_k;
+  const int64_t per = (int64_t)p->heads * ((longest + 63) / 64 + 1);
+  return p->sequences == 0 || per <= INT32_MAX / p->sequences;
+}
+size_t attention_packed_ws(int dtype, const vit_attention_problem& p, bool backward) {
+  return backward ? align_up((size_t)p.heads * p.q_rows * sizeof(float), 256) : 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -614,6 +666,7 @@ const char* vit_status_string(int status) {
     case VIT_ERR_CUDA: return "CUDA call or kernel launch failed";
     case VIT_ERR_TIMEOUT: return "a bounded wait inside a kernel expired";
     case VIT_ERR_NO_DEVICE: return "no usable sm_100 device";
+    case VIT_ERR_OFFSETS: return "offsets of a packed sequence out of order, out of range or longer than the call's bound";
     case VIT_ERR_INFEASIBLE: return "no partition fits the devices' memory";
     case VIT_ERR_TOO_LARGE: return "problem larger than the fixed scratch of this allocation-free entry point";
   }
@@ -697,6 +750,145 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
   } else {
     return VIT_ERR_INVALID_ARG;
   }
+  return VIT_OK;
+}
+
+int vit_op_rope_axes(vit_handle* h, int dtype, int rows, int heads, int d, const vit_rope* rope, int inverse,
+                     const void* x, int64_t ldx, void* y, int64_t ldy, void* stream) {
+  if (!h || rows < 0 || heads < 1 || !head_ok(dtype, d) || !rope || !rope_ok(rope, d) || !on_own_device(h)) return VIT_ERR_INVALID_ARG;
+  const size_t es = element_bytes(dtype);
+  const Block bx{x, rows, (int64_t)heads * d, ldx, es}, by{y, rows, (int64_t)heads * d, ldy, es};
+  if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by))) return VIT_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  RopeNormCall c{};
+  c.act_bf16 = dtype == VIT_BF16; c.inverse = inverse != 0; c.rows = rows; c.heads = heads; c.q_heads = heads; c.d = d; c.rope = rope;
+  c.x = x; c.ldx = ldx; c.y = y; c.ldy = ldy;
+  VIT_LAUNCH(h, VIT_PROF_OP, launch_rope_norm(c, s));
+  return VIT_OK;
+}
+
+int vit_op_qk_norm_rope(vit_handle* h, int dtype, int rows, int q_heads, int k_heads, int d, const float* q_gain,
+                        const float* k_gain, float eps, const vit_rope* rope, const void* x, int64_t ldx, void* y,
+                        int64_t ldy, void* stream) {
+  if (!h || rows < 0 || q_heads < 0 || k_heads < 0 || (int64_t)q_heads + k_heads < 1 || (int64_t)q_heads + k_heads > INT32_MAX ||
+      !head_ok(dtype, d) || !q_gain || !k_gain || misaligned(q_gain) || misaligned(k_gain) || !(eps >= 0.f) ||
+      (rope && !rope_ok(rope, d)) || !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
+  const size_t es = element_bytes(dtype);
+  const int64_t width = ((int64_t)q_heads + k_heads) * d;
+  const Block bx{x, rows, width, ldx, es}, by{y, rows, width, ldy, es};
+  if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by))) return VIT_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  RopeNormCall c{};
+  c.act_bf16 = dtype == VIT_BF16; c.rows = rows; c.heads = q_heads + k_heads; c.q_heads = q_heads; c.d = d; c.rope = rope;
+  c.q_gain = q_gain; c.k_gain = k_gain; c.eps = eps; c.x = x; c.ldx = ldx; c.y = y; c.ldy = ldy;
+  VIT_LAUNCH(h, VIT_PROF_OP, launch_rope_norm(c, s));
+  return VIT_OK;
+}
+
+size_t vit_qk_norm_rope_backward_bytes(int rows, int q_heads, int k_heads, int d) {
+  if (rows < 0 || q_heads < 0 || k_heads < 0 || !head_ok(VIT_BF16, d)) return 0;
+  return qk_norm_rope_backward_bytes(d);
+}
+
+int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads, int k_heads, int d,
+                                 const float* q_gain, const float* k_gain, float eps, const vit_rope* rope,
+                                 const void* x, int64_t ldx, const void* dy, int64_t lddy, void* dx, int64_t lddx,
+                                 float* dq_gain, float* dk_gain, void* ws, size_t ws_bytes, void* stream) {
+  if (!h || rows < 0 || q_heads < 0 || k_heads < 0 || (int64_t)q_heads + k_heads < 1 || (int64_t)q_heads + k_heads > INT32_MAX ||
+      !head_ok(dtype, d) || !q_gain || !k_gain || misaligned(q_gain) || misaligned(k_gain) || !(eps >= 0.f) ||
+      (rope && !rope_ok(rope, d)) || !dq_gain || !dk_gain || misaligned(dq_gain) || misaligned(dk_gain) || !ws || misaligned(ws) ||
+      !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
+  const size_t es = element_bytes(dtype), need = qk_norm_rope_backward_bytes(d);
+  const int64_t width = ((int64_t)q_heads + k_heads) * d;
+  const Block bx{x, rows, width, ldx, es}, bdy{dy, rows, width, lddy, es}, bdx{dx, rows, width, lddx, es};
+  const Block bgq{dq_gain, 1, d, d, 4}, bgk{dk_gain, 1, d, d, 4}, bws{ws, 1, (int64_t)need, (int64_t)need, 1};
+  if (!block_ok(bx) || !block_ok(bdy) || !block_ok(bdx)) return VIT_ERR_INVALID_ARG;
+  if ((!same_block(bx, bdx) && blocks_overlap(bx, bdx)) || (!same_block(bdy, bdx) && blocks_overlap(bdy, bdx)) ||
+      blocks_overlap(bgq, bgk))
+    return VIT_ERR_INVALID_ARG;
+  for (const Block* b : {&bx, &bdy, &bdx, &bgq, &bgk})
+    if (blocks_overlap(*b, bws) || (b != &bgq && blocks_overlap(*b, bgq)) || (b != &bgk && blocks_overlap(*b, bgk)))
+      return VIT_ERR_INVALID_ARG;
+  if (ws_bytes < need) return VIT_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  RopeNormCall c{};
+  c.act_bf16 = dtype == VIT_BF16; c.rows = rows; c.heads = q_heads + k_heads; c.q_heads = q_heads; c.d = d; c.rope = rope;
+  c.q_gain = q_gain; c.k_gain = k_gain; c.eps = eps; c.x = x; c.ldx = ldx; c.dy = dy; c.lddy = lddy; c.y = dx; c.ldy = lddx;
+  c.partial = static_cast<float*>(ws);
+  if (rows > 0) VIT_LAUNCH(h, VIT_PROF_OP, launch_rope_norm(c, s));
+  VIT_LAUNCH(h, VIT_PROF_OP, launch_gain_grad(c, dq_gain, dk_gain, s));
+  return VIT_OK;
+}
+
+size_t vit_attention_packed_bytes(int dtype, const vit_attention_problem* problem, int backward) {
+  if (!attention_problem_ok(dtype, problem) || !attention_fits(problem)) return 0;
+  return attention_packed_ws(dtype, *problem, backward != 0);
+}
+
+int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_problem* problem, const void* q, int64_t ldq,
+                            const void* k, int64_t ldk, const void* v, int64_t ldv, void* out, int64_t ldo, float* lse,
+                            void* ws, size_t ws_bytes, void* stream) {
+  if (!h || !attention_problem_ok(dtype, problem) || (problem->q_rows > 0 && (!lse || misaligned(lse))) || !on_own_device(h)) return VIT_ERR_INVALID_ARG;
+  if (!attention_fits(problem)) return VIT_ERR_TOO_LARGE;
+  const vit_attention_problem& p = *problem;
+  const size_t es = element_bytes(dtype), need = attention_packed_ws(dtype, p, false);
+  const int64_t wq = (int64_t)p.heads * p.d, wk = (int64_t)p.kv_heads * p.d;
+  const Block bq{q, p.q_rows, wq, ldq, es}, bk{k, p.k_rows, wk, ldk, es}, bv{v, p.k_rows, wk, ldv, es}, bo{out, p.q_rows, wq, ldo, es};
+  const Block bl{lse, p.heads, p.q_rows, p.q_rows, 4}, bws{ws, 1, (int64_t)need, (int64_t)need, 1};
+  if (!block_ok(bq) || !block_ok(bk) || !block_ok(bv) || !block_ok(bo) || (need && (!ws || misaligned(ws)))) return VIT_ERR_INVALID_ARG;
+  for (const Block* b : {&bq, &bk, &bv, &bo, &bl})
+    if ((b != &bo && blocks_overlap(*b, bo)) || (b != &bl && blocks_overlap(*b, bl)) || blocks_overlap(*b, bws)) return VIT_ERR_INVALID_ARG;
+  if (ws_bytes < need) return VIT_ERR_WORKSPACE;
+  if (p.sequences == 0 || p.q_rows == 0 || p.max_q == 0) return VIT_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  PackedCall c{};
+  c.p = p; c.q = q; c.ldq = ldq; c.k = k; c.ldk = ldk; c.v = v; c.ldv = ldv; c.out = out; c.ldo = ldo; c.lse = lse;
+  c.dev_status = h->dev_status;
+  if (dtype == VIT_BF16) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_bf16(c, s));
+  else VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_f32(c, s));
+  return VIT_OK;
+}
+
+int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attention_problem* problem, const void* q,
+                                     int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                                     const void* out, int64_t ldo, const float* lse, const void* dout, int64_t lddo,
+                                     void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* ws,
+                                     size_t ws_bytes, void* stream) {
+  if (!h || !attention_problem_ok(dtype, problem) || (problem->q_rows > 0 && (!lse || misaligned(lse))) || !on_own_device(h)) return VIT_ERR_INVALID_ARG;
+  if (!attention_fits(problem)) return VIT_ERR_TOO_LARGE;
+  const vit_attention_problem& p = *problem;
+  const size_t es = element_bytes(dtype), need = attention_packed_ws(dtype, p, true);
+  const int64_t wq = (int64_t)p.heads * p.d, wk = (int64_t)p.kv_heads * p.d;
+  const Block in[] = {{q, p.q_rows, wq, ldq, es}, {k, p.k_rows, wk, ldk, es}, {v, p.k_rows, wk, ldv, es},
+                      {out, p.q_rows, wq, ldo, es}, {dout, p.q_rows, wq, lddo, es}, {lse, p.heads, p.q_rows, p.q_rows, 4}};
+  const Block to[] = {{dq, p.q_rows, wq, lddq, es}, {dk, p.k_rows, wk, lddk, es}, {dv, p.k_rows, wk, lddv, es},
+                      {ws, 1, (int64_t)need, (int64_t)need, 1}};
+  for (int i = 0; i < 5; ++i)
+    if (!block_ok(in[i])) return VIT_ERR_INVALID_ARG;
+  for (int i = 0; i < 3; ++i)
+    if (!block_ok(to[i])) return VIT_ERR_INVALID_ARG;
+  if (need && (!ws || misaligned(ws))) return VIT_ERR_INVALID_ARG;
+  for (int i = 0; i < 4; ++i) {
+    for (const Block& b : in)
+      if (blocks_overlap(to[i], b)) return VIT_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (blocks_overlap(to[i], to[j])) return VIT_ERR_INVALID_ARG;
+  }
+  if (ws_bytes < need) return VIT_ERR_WORKSPACE;
+  if (p.sequences == 0) return VIT_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  PackedCall c{};
+  c.p = p; c.q = q; c.ldq = ldq; c.k = k; c.ldk = ldk; c.v = v; c.ldv = ldv; c.out = const_cast<void*>(out); c.ldo = ldo;
+  c.lse = const_cast<float*>(lse); c.dout = dout; c.lddo = lddo;
+  c.dq = dq; c.lddq = lddq; c.dk = dk; c.lddk = lddk; c.dv = dv; c.lddv = lddv;
+  c.delta = static_cast<float*>(ws);
+  c.dev_status = h->dev_status;
+  const bool b16 = dtype == VIT_BF16;
+  if (p.q_rows > 0 && p.max_q > 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta(c, b16, s));
+  if (p.k_rows > 0 && p.max_k > 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dkdv(c, b16, s));
+  if (p.q_rows > 0 && p.max_q > 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dq(c, b16, s));
   return VIT_OK;
 }
 

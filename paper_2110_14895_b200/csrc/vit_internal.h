@@ -156,6 +156,41 @@ cudaError_t launch_head_static(const void* tokens, const float* g, const float* 
                                float* logits, int images, int T,
                                int H, int classes, bool act_bf16, cudaStream_t s);
 
+// rotation of channel pairs by the rows' positions (rope_norm.cu); with gains behind the norm of each
+// head; with dy the gradients of that: y = dx, partial = the blocks' shares of the gains' gradients
+struct RopeNormCall {
+  bool act_bf16, inverse;
+  int rows, heads, q_heads, d;
+  const vit_rope* rope;                // nullptr: no rotation
+  const float *q_gain, *k_gain;
+  float eps;
+  const void* x;  int64_t ldx;
+  const void* dy; int64_t lddy;
+  void* y;        int64_t ldy;
+  float* partial;
+};
+size_t qk_norm_rope_backward_bytes(int d);
+cudaError_t launch_rope_norm(const RopeNormCall& c, cudaStream_t s);
+cudaError_t launch_gain_grad(const RopeNormCall& c, float* dq_gain, float* dk_gain, cudaStream_t s);
+
+// attention over packed sequences (attention_packed.cu) and its gradients
+struct PackedCall {
+  vit_attention_problem p;
+  const void *q, *k, *v;  int64_t ldq, ldk, ldv;
+  void* out;              int64_t ldo;      // read by the backward pass
+  float* lse;                               // [heads][q_rows]; read by the backward pass
+  const void* dout;       int64_t lddo;
+  void *dq, *dk, *dv;     int64_t lddq, lddk, lddv;
+  float* delta;                             // backward: [heads][q_rows] rowsum(dout * out)
+  int* dev_status;
+};
+cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s);
+cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s);
+// the three kernels of the backward pass
+cudaError_t launch_attention_delta(const PackedCall& c, bool act_bf16, cudaStream_t s);
+cudaError_t launch_attention_packed_dkdv(const PackedCall& c, bool act_bf16, cudaStream_t s);
+cudaError_t launch_attention_packed_dq(const PackedCall& c, bool act_bf16, cudaStream_t s);
+
 cudaError_t launch_wait_probe(long long limit_cycles, int* dev_status, cudaStream_t s);
 // *snapshot = atomic exchange of *status with 0, on stream s
 cudaError_t launch_status_take(int* status, int* snapshot, cudaStream_t s);
