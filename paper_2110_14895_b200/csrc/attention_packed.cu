@@ -1,11 +1,12 @@
-// Attention over packed sequences of any lengths, forward and backward, on the fp32 pipes.
+// Attention over packed sequences of any lengths in fp32, forward and backward, on the fp32 pipes; the
+// tensor-core kernels of the bf16 mode are in attention_packed_tc.cu.
 //
 //   s = scale q k^T, lse = log sum exp s, out = exp(s - lse) v                       (forward)
 //   p = exp(s - lse), delta = rowsum(dout * out), ds = p (dout v^T - delta)
 //   dv = p^T dout, dk = scale ds^T q, dq = scale ds k                                 (backward)
 //
 // A block of 256 threads works on 64 x 64 scores at a time, 4 x 4 of them to a thread; operands are
-// converted to fp32 in shared memory, rows behind the end of a sequence are zero there.  The backward
+// staged in shared memory, rows behind the end of a sequence are zero there.  The backward
 // pass is two kernels, one that keeps a tile of keys and walks over the queries (dk, dv) and one that
 // keeps a tile of queries and walks over the keys (dq): seven products instead of five, but every
 // gradient is summed by one block in a fixed order, so that results do not depend on the schedule.
@@ -26,12 +27,10 @@ __device__ __forceinline__ float4 load4(const bf16* a) {
   return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
                      __uint_as_float(u.y & 0xffff0000u));
 }
-__device__ __forceinline__ void store1(float* a, float v) { *a = v; }
-__device__ __forceinline__ void store1(bf16* a, float v) { *a = __float2bfloat16_rn(v); }
 
 // rows [row0, row0 + 64) of one head as fp32 [64][DP + 4]; rows >= end and columns >= d are zero
-template <typename T, int DP>
-__device__ __forceinline__ void load_tile(float* dst, const T* base, int64_t ld, int64_t row0, int rows, int d) {
+template <int DP>
+__device__ __forceinline__ void load_tile(float* dst, const float* base, int64_t ld, int64_t row0, int rows, int d) {
   for (int i = threadIdx.x; i < BT * (DP / 4); i += THREADS) {
     const int r = i / (DP / 4), c = (i % (DP / 4)) * 4;
     const float4 v = r < rows && c < d ? load4(base + (row0 + r) * ld + c) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -78,7 +77,7 @@ __device__ __forceinline__ void accumulate_t(float (&acc)[4][DP / 16], const flo
   }
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(THREADS)
 packed_forward_kernel(const PackedCall c) {
   extern __shared__ __align__(16) float sm[];
@@ -94,12 +93,12 @@ packed_forward_kernel(const PackedCall c) {
   const int q_here = min(BT, r.q_len - q0), d = c.p.d;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int kv = head / (c.p.heads / c.p.kv_heads);
-  const T* q = static_cast<const T*>(c.q) + (int64_t)head * d;
-  const T* k = static_cast<const T*>(c.k) + (int64_t)kv * d;
-  const T* v = static_cast<const T*>(c.v) + (int64_t)kv * d;
+  const float* q = static_cast<const float*>(c.q) + (int64_t)head * d;
+  const float* k = static_cast<const float*>(c.k) + (int64_t)kv * d;
+  const float* v = static_cast<const float*>(c.v) + (int64_t)kv * d;
   const float sl2 = c.p.scale * 1.4426950408889634f;
 
-  load_tile<T, DP>(qs, q, c.ldq, (int64_t)r.q_begin + q0, q_here, d);
+  load_tile<DP>(qs, q, c.ldq, (int64_t)r.q_begin + q0, q_here, d);
   float m[4], l[4], o[4][DP / 16];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -110,12 +109,12 @@ packed_forward_kernel(const PackedCall c) {
   }
   for (int k0 = 0; k0 < r.k_len; k0 += BT) {
     const int k_here = min(BT, r.k_len - k0);
-    load_tile<T, DP>(ks, k, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
+    load_tile<DP>(ks, k, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
     __syncthreads();
     float s[4][4];
     scores<DP>(s, qs, ks, tx, ty);
     __syncthreads();
-    load_tile<T, DP>(ks, v, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
+    load_tile<DP>(ks, v, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float top = m[i];
@@ -152,15 +151,15 @@ packed_forward_kernel(const PackedCall c) {
     if (row >= q_here) continue;
     const int64_t at = (int64_t)r.q_begin + q0 + row;
     const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];     // no keys: zero
-    T* out = static_cast<T*>(c.out) + at * c.ldo + (int64_t)head * d;
+    float* out = static_cast<float*>(c.out) + at * c.ldo + (int64_t)head * d;
 #pragma unroll
     for (int cc = 0; cc < DP / 16; ++cc)
-      if (tx + 16 * cc < d) store1(out + tx + 16 * cc, o[i][cc] * inv);
+      if (tx + 16 * cc < d) out[tx + 16 * cc] = o[i][cc] * inv;
     if (tx == 0) c.lse[(int64_t)head * c.p.q_rows + at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718055994531f;
   }
 }
 
-// delta[head][row] = sum over the head's channels of dout * out: one warp per row and head
+// (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head
 template <typename T>
 __global__ void __launch_bounds__(THREADS)
 packed_delta_kernel(const PackedCall c) {
@@ -179,7 +178,8 @@ packed_delta_kernel(const PackedCall c) {
   }
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-  if (lane == 0) c.delta[(int64_t)head * c.p.q_rows + row] = sum;
+  const int64_t at = (int64_t)head * c.p.q_rows + row;
+  if (lane == 0) c.delta[at] = make_float2(c.lse[at] * 1.4426950408889634f, sum);
 }
 
 // p and ds of a tile: s = q k^T, dp = dout v^T; rows beyond q_here and keys beyond k_here give zero
@@ -199,7 +199,7 @@ __device__ __forceinline__ void grad_scores(float (&s)[4][4], float (&dp)[4][4],
   }
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(THREADS)
 packed_dkdv_kernel(const PackedCall c) {
   extern __shared__ __align__(16) float sm[];
@@ -215,8 +215,8 @@ packed_dkdv_kernel(const PackedCall c) {
   const int k_here = min(BT, r.k_len - k0), d = c.p.d, group = c.p.heads / c.p.kv_heads;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const float sl2 = c.p.scale * 1.4426950408889634f;
-  load_tile<T, DP>(ks, static_cast<const T*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
-  load_tile<T, DP>(vs, static_cast<const T*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
+  load_tile<DP>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
+  load_tile<DP>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
   float dk[4][DP / 16], dv[4][DP / 16];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -226,13 +226,14 @@ packed_dkdv_kernel(const PackedCall c) {
     for (int q0 = 0; q0 < r.q_len; q0 += BT) {
       const int q_here = min(BT, r.q_len - q0);
       const int64_t at = (int64_t)r.q_begin + q0;
-      load_tile<T, DP>(qs, static_cast<const T*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
-      load_tile<T, DP>(os, static_cast<const T*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
+      load_tile<DP>(qs, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
+      load_tile<DP>(os, static_cast<const float*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
       if (threadIdx.x < BT) {
         const bool there = (int)threadIdx.x < q_here;
         const int64_t i = (int64_t)head * c.p.q_rows + at + threadIdx.x;
-        lse2[threadIdx.x] = there ? c.lse[i] * 1.4426950408889634f : 0.f;
-        delta[threadIdx.x] = there ? c.delta[i] : 0.f;
+        const float2 v = there ? c.delta[i] : make_float2(0.f, 0.f);
+        lse2[threadIdx.x] = v.x;
+        delta[threadIdx.x] = v.y;
       }
       __syncthreads();
       float s[4][4], dp[4][4];
@@ -257,18 +258,18 @@ packed_dkdv_kernel(const PackedCall c) {
     const int row = ty * 4 + i;
     if (row >= k_here) continue;
     const int64_t at = (int64_t)r.k_begin + k0 + row;
-    T* gk = static_cast<T*>(c.dk) + at * c.lddk + (int64_t)kv * d;
-    T* gv = static_cast<T*>(c.dv) + at * c.lddv + (int64_t)kv * d;
+    float* gk = static_cast<float*>(c.dk) + at * c.lddk + (int64_t)kv * d;
+    float* gv = static_cast<float*>(c.dv) + at * c.lddv + (int64_t)kv * d;
 #pragma unroll
     for (int cc = 0; cc < DP / 16; ++cc)
       if (tx + 16 * cc < d) {
-        store1(gk + tx + 16 * cc, dk[i][cc] * c.p.scale);
-        store1(gv + tx + 16 * cc, dv[i][cc]);
+        gk[tx + 16 * cc] = dk[i][cc] * c.p.scale;
+        gv[tx + 16 * cc] = dv[i][cc];
       }
   }
 }
 
-template <typename T, int DP>
+template <int DP>
 __global__ void __launch_bounds__(THREADS)
 packed_dq_kernel(const PackedCall c) {
   extern __shared__ __align__(16) float sm[];
@@ -285,13 +286,14 @@ packed_dq_kernel(const PackedCall c) {
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const float sl2 = c.p.scale * 1.4426950408889634f;
   const int64_t at = (int64_t)r.q_begin + q0;
-  load_tile<T, DP>(qs, static_cast<const T*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
-  load_tile<T, DP>(os, static_cast<const T*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
+  load_tile<DP>(qs, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
+  load_tile<DP>(os, static_cast<const float*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
   if (threadIdx.x < BT) {
     const bool there = (int)threadIdx.x < q_here;
     const int64_t i = (int64_t)head * c.p.q_rows + at + threadIdx.x;
-    lse2[threadIdx.x] = there ? c.lse[i] * 1.4426950408889634f : 0.f;
-    delta[threadIdx.x] = there ? c.delta[i] : 0.f;
+    const float2 v = there ? c.delta[i] : make_float2(0.f, 0.f);
+    lse2[threadIdx.x] = v.x;
+    delta[threadIdx.x] = v.y;
   }
   float dq[4][DP / 16];
 #pragma unroll
@@ -300,8 +302,8 @@ packed_dq_kernel(const PackedCall c) {
     for (int cc = 0; cc < DP / 16; ++cc) dq[i][cc] = 0.f;
   for (int k0 = 0; k0 < r.k_len; k0 += BT) {
     const int k_here = min(BT, r.k_len - k0);
-    load_tile<T, DP>(ks, static_cast<const T*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
-    load_tile<T, DP>(vs, static_cast<const T*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
+    load_tile<DP>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
+    load_tile<DP>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
     __syncthreads();
     float s[4][4], dp[4][4];
     scores<DP>(s, qs, ks, tx, ty);
@@ -319,48 +321,46 @@ packed_dq_kernel(const PackedCall c) {
   for (int i = 0; i < 4; ++i) {
     const int row = ty * 4 + i;
     if (row >= q_here) continue;
-    T* g = static_cast<T*>(c.dq) + (at + row) * c.lddq + (int64_t)head * d;
+    float* g = static_cast<float*>(c.dq) + (at + row) * c.lddq + (int64_t)head * d;
 #pragma unroll
     for (int cc = 0; cc < DP / 16; ++cc)
-      if (tx + 16 * cc < d) store1(g + tx + 16 * cc, dq[i][cc] * c.p.scale);
+      if (tx + 16 * cc < d) g[tx + 16 * cc] = dq[i][cc] * c.p.scale;
   }
 }
 
 enum Which { FORWARD, DKDV, DQ };
 
-template <typename T, int DP>
+template <int DP>
 cudaError_t launch_variant(const PackedCall& c, Which w, cudaStream_t s) {
   constexpr size_t tile = (size_t)BT * (DP + 4) * 4, prob = (size_t)BT * PS * 4;
   if (w == FORWARD) {
     static PerDeviceFlag done;
     const size_t smem = 2 * tile + prob;
-    if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_kernel<T, DP>, (int)smem)) return e;
-    packed_forward_kernel<T, DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
+    if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_kernel<DP>, (int)smem)) return e;
+    packed_forward_kernel<DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
   } else if (w == DKDV) {
     static PerDeviceFlag done;
     const size_t smem = 4 * tile + 2 * prob + 2 * BT * 4;
-    if (cudaError_t e = ensure_dynamic_smem(done, packed_dkdv_kernel<T, DP>, (int)smem)) return e;
-    packed_dkdv_kernel<T, DP><<<c.p.sequences * c.p.kv_heads * ((c.p.max_k + BT - 1) / BT), THREADS, smem, s>>>(c);
+    if (cudaError_t e = ensure_dynamic_smem(done, packed_dkdv_kernel<DP>, (int)smem)) return e;
+    packed_dkdv_kernel<DP><<<c.p.sequences * c.p.kv_heads * ((c.p.max_k + BT - 1) / BT), THREADS, smem, s>>>(c);
   } else {
     static PerDeviceFlag done;
     const size_t smem = 4 * tile + prob + 2 * BT * 4;
-    if (cudaError_t e = ensure_dynamic_smem(done, packed_dq_kernel<T, DP>, (int)smem)) return e;
-    packed_dq_kernel<T, DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
+    if (cudaError_t e = ensure_dynamic_smem(done, packed_dq_kernel<DP>, (int)smem)) return e;
+    packed_dq_kernel<DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
   }
   return cudaGetLastError();
 }
-template <typename T>
 cudaError_t launch_width(const PackedCall& c, Which w, cudaStream_t s) {
-  if (c.p.d <= 32) return launch_variant<T, 32>(c, w, s);
-  if (c.p.d <= 64) return launch_variant<T, 64>(c, w, s);
-  if (c.p.d <= 96) return launch_variant<T, 96>(c, w, s);
-  return launch_variant<T, 128>(c, w, s);
+  if (c.p.d <= 32) return launch_variant<32>(c, w, s);
+  if (c.p.d <= 64) return launch_variant<64>(c, w, s);
+  if (c.p.d <= 96) return launch_variant<96>(c, w, s);
+  return launch_variant<128>(c, w, s);
 }
 
 }  // namespace
 
-cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) { return launch_width<float>(c, FORWARD, s); }
-cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s) { return launch_width<bf16>(c, FORWARD, s); }
+cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, FORWARD, s); }
 
 cudaError_t launch_attention_delta(const PackedCall& c, bool act_bf16, cudaStream_t s) {
   const int64_t items = (int64_t)c.p.q_rows * c.p.heads;
@@ -370,10 +370,10 @@ cudaError_t launch_attention_delta(const PackedCall& c, bool act_bf16, cudaStrea
   return cudaGetLastError();
 }
 cudaError_t launch_attention_packed_dkdv(const PackedCall& c, bool act_bf16, cudaStream_t s) {
-  return act_bf16 ? launch_width<bf16>(c, DKDV, s) : launch_width<float>(c, DKDV, s);
+  return act_bf16 ? launch_attention_packed_dkdv_bf16(c, s) : launch_width(c, DKDV, s);
 }
 cudaError_t launch_attention_packed_dq(const PackedCall& c, bool act_bf16, cudaStream_t s) {
-  return act_bf16 ? launch_width<bf16>(c, DQ, s) : launch_width<float>(c, DQ, s);
+  return act_bf16 ? launch_attention_packed_dq_bf16(c, s) : launch_width(c, DQ, s);
 }
 
 }  // namespace vit

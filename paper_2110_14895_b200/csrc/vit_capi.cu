@@ -272,7 +272,7 @@ bool attention_fits(const vit_attention_problem* p) {
   return p->sequences == 0 || per <= INT32_MAX / p->sequences;
 }
 size_t attention_packed_ws(int dtype, const vit_attention_problem& p, bool backward) {
-  return backward ? align_up((size_t)p.heads * p.q_rows * sizeof(float), 256) : 0;
+  return backward ? align_up((size_t)p.heads * p.q_rows * sizeof(float2), 256) : 0;
 }
 
 }  // namespace
@@ -883,7 +883,7 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
   c.p = p; c.q = q; c.ldq = ldq; c.k = k; c.ldk = ldk; c.v = v; c.ldv = ldv; c.out = const_cast<void*>(out); c.ldo = ldo;
   c.lse = const_cast<float*>(lse); c.dout = dout; c.lddo = lddo;
   c.dq = dq; c.lddq = lddq; c.dk = dk; c.lddk = lddk; c.dv = dv; c.lddv = lddv;
-  c.delta = static_cast<float*>(ws);
+  c.delta = static_cast<float2*>(ws);
   c.dev_status = h->dev_status;
   const bool b16 = dtype == VIT_BF16;
   if (p.q_rows > 0 && p.max_q > 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta(c, b16, s));

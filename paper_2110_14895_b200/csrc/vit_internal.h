@@ -181,11 +181,13 @@ struct PackedCall {
   float* lse;                               // [heads][q_rows]; read by the backward pass
   const void* dout;       int64_t lddo;
   void *dq, *dk, *dv;     int64_t lddq, lddk, lddv;
-  float* delta;                             // backward: [heads][q_rows] rowsum(dout * out)
+  float2* delta;                            // backward: [heads][q_rows] (lse log2(e), rowsum(dout * out))
   int* dev_status;
 };
 cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s);
+cudaError_t launch_attention_packed_dkdv_bf16(const PackedCall& c, cudaStream_t s);
+cudaError_t launch_attention_packed_dq_bf16(const PackedCall& c, cudaStream_t s);
 // the three kernels of the backward pass
 cudaError_t launch_attention_delta(const PackedCall& c, bool act_bf16, cudaStream_t s);
 cudaError_t launch_attention_packed_dkdv(const PackedCall& c, bool act_bf16, cudaStream_t s);
