@@ -57,6 +57,20 @@ __device__ __forceinline__ void store_16_bf16(bf16* dst, const uint32_t (&o)[16]
 __device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag) {
   return __all_sync(0xffffffffu, mbar_wait(bar, (uint32_t)parity, abort_flag));
 }
+// the same without letting the hardware suspend the warp: for the one warp that issues the products, which
+// otherwise takes a few hundred cycles to come back
+__device__ __forceinline__ bool warp_spin(uint32_t bar, int parity, volatile int* abort_flag) {
+  const long long t0 = clock64();
+  for (;;) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(done) : "r"(bar), "r"((uint32_t)parity) : "memory");
+    if (__all_sync(0xffffffffu, done)) return true;
+    const bool late = clock64() - t0 > WAIT_LIMIT_CYCLES;
+    if (late) *abort_flag = 1;
+    if (__any_sync(0xffffffffu, late || *abort_flag)) return false;
+  }
+}
 // rows [from, rows) of a tile of `slabs` slabs become zero; one warp, then visible to the tensor core
 __device__ __forceinline__ void zero_rows(uint32_t tile, int rows, int slabs, int from, int lane) {
   for (int s = 0; s < slabs; ++s)
@@ -66,19 +80,34 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, int rows, int slabs, in
   __syncwarp();
 }
 
+// One lane of the warp, chosen by the hardware.  The products are issued behind this and not behind
+// `lane == 0`: their operands then stay in uniform registers (110 -> about 20 cycles to issue one).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(one));
+  return one != 0;
+}
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
+
 // S[128 x n] = X[128 rows] . Y[n rows]^T over the head's channels, both operands as slabs of 64 channels
-__device__ __forceinline__ void issue_scores(uint32_t d_tmem, uint32_t x, int x_rows, uint32_t y, int y_rows, int n, int ksteps) {
+template <int SLABS, int X_ROWS, int Y_ROWS>
+__device__ __forceinline__ void issue_scores(uint32_t d_tmem, uint32_t x, uint32_t y, int n, int ksteps) {
   const uint32_t id = idesc(n, false);
-  for (int k = 0; k < ksteps; ++k)
-    umma_bf16(d_tmem, desc_sw128(x + (uint32_t)((k >> 2) * x_rows * 128)) + (uint64_t)(2 * (k & 3)),
-              desc_sw128(y + (uint32_t)((k >> 2) * y_rows * 128)) + (uint64_t)(2 * (k & 3)), id, k > 0 ? 1u : 0u);
+  const uint64_t xd = desc_sw128(x), yd = desc_sw128(y);
+#pragma unroll
+  for (int k = 0; k < 4 * SLABS; ++k)
+    if (k < ksteps)
+      umma_bf16(d_tmem, xd + (uint64_t)((k >> 2) * (X_ROWS * 8) + 2 * (k & 3)), yd + (uint64_t)((k >> 2) * (Y_ROWS * 8) + 2 * (k & 3)), id,
+                k > 0 ? 1u : 0u);
 }
 // D[128 x d] (+)= P[128 x 16 ksteps] . Y[16 ksteps rows x d], P packed in tensor memory
-__device__ __forceinline__ void issue_weighted(uint32_t d_tmem, uint32_t p_tmem, uint32_t y, int y_rows, int d, int ksteps, bool first) {
+template <int Y_ROWS>
+__device__ __forceinline__ void issue_weighted(uint32_t d_tmem, uint32_t p_tmem, uint32_t y, int d, int ksteps, bool first) {
   const uint32_t id = idesc(d, true);
-  for (int k = 0; k < ksteps; ++k)
-    umma_bf16_ts(d_tmem, p_tmem + (uint32_t)(8 * k), desc_sw128(y + (uint32_t)(k * 2048), (uint32_t)(y_rows * 128)), id,
-                 first && k == 0 ? 0u : 1u);
+  const uint64_t yd = desc_sw128(y, Y_ROWS * 128);
+#pragma unroll
+  for (int k = 0; k < Y_ROWS / 16; ++k)
+    if (k < ksteps) umma_bf16_ts(d_tmem, p_tmem + (uint32_t)(8 * k), yd + (uint64_t)(k * 128), id, first && k == 0 ? 0u : 1u);
 }
 
 // ============================================================================================ forward
@@ -111,7 +140,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
   const int q0 = tile * RT;
   if (q0 >= r.q_len) return;
   const int d = c.p.d, kv = head / (c.p.heads / c.p.kv_heads);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int row = q0 + (warp & 3) * 32 + lane;                   // softmax warps: this thread's query
   const int64_t at = (int64_t)r.q_begin + row;
   const int n_tiles = (r.k_len + RT - 1) / RT;
@@ -138,7 +167,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = uniform(*tmem_slot);
 
   if (warp == 5) {
     // ------------------------------------------------------------------ TMA producer
@@ -171,31 +200,33 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     }
   } else if (warp == 4) {
     // ------------------------------------------------------------------ MMA issuer (the whole warp keeps step)
-    bool ok = warp_wait(bar(F_Q), 0, abort_flag);
+    bool ok = warp_spin(bar(F_Q), 0, abort_flag);
     for (int j = 0; j < n_tiles && ok; ++j) {
       const int st = j % L::STAGES, ph = (j / L::STAGES) & 1;
       const int here = min(RT, r.k_len - j * RT), n16 = (here + 15) / 16;
       const uint32_t ks = sb + L::OFF_K + st * L::TILE, vs = sb + L::OFF_V + st * L::TILE;
-      if (!warp_wait(bar(F_KFULL + st), ph, abort_flag)) { ok = false; break; }
+      if (!warp_spin(bar(F_KFULL + st), ph, abort_flag)) { ok = false; break; }
       __syncwarp();
-      if (lane == 0) {
+      if (elect_one()) {
         // the scores overwrite P of tile j - 1: its product was issued before, by this thread
-        issue_scores(tmem, sb, RT, ks, RT, 16 * n16, d / 16);
+        issue_scores<SLABS, RT, RT>(tmem, sb, ks, 16 * n16, d / 16);
         umma_commit(bar(F_S));
         umma_commit(bar(F_KFREE + st));
       }
-      if (!warp_wait(bar(F_VFULL + st), ph, abort_flag)) { ok = false; break; }
+      __syncwarp();                                            // lanes that poll would hold up the one that issues
+      if (!warp_spin(bar(F_VFULL + st), ph, abort_flag)) { ok = false; break; }
       __syncwarp();
       // rows of V behind the last key meet probabilities of zero: make them zero too, whatever lies there
       if (here < 16 * n16) zero_rows(vs, RT, SLABS, here, lane);
-      if (!warp_wait(bar(F_P), j & 1, abort_flag)) { ok = false; break; }
+      if (!warp_spin(bar(F_P), j & 1, abort_flag)) { ok = false; break; }
       __syncwarp();
-      if (lane == 0) {
+      if (elect_one()) {
         tc_fence_after();
-        issue_weighted(tmem + O_COL, tmem, vs, RT, d, n16, j == 0);
+        issue_weighted<RT>(tmem + O_COL, tmem, vs, d, n16, j == 0);
         umma_commit(bar(F_VFREE + st));
         if (j == n_tiles - 1) umma_commit(bar(F_O));
       }
+      __syncwarp();
     }
     __syncwarp();
     if (*abort_flag && lane == 0) {
@@ -340,7 +371,7 @@ struct BackwardMaps { CUtensorMap x1, x2, y1, y2; };
 constexpr int CT = 64;                                 // rows of a Y tile = columns of a tile of scores
 template <int SLABS, bool DKDV, int NB>
 struct BackwardCfg {
-  static constexpr int STAGES = NB + (SLABS == 1 ? 2 : 1);
+  static constexpr int STAGES = NB + 2;
   static constexpr int THREADS = NB * 128 + 64;
   static constexpr uint32_t XTILE = SLABS * RT * 128, YTILE = SLABS * CT * 128;
   static constexpr uint32_t OFF_Y = 2 * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // float2 [STAGES][64]: -lse2, -delta of the columns
@@ -369,7 +400,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   const int x0 = tile * RT;
   if (x0 >= x_len) return;
   const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   const int y_tiles = (y_len + CT - 1) / CT;
   const int n = DKDV ? group * y_tiles : y_tiles;      // tiles in all, head after head
   const int row = x0 + (warp & 3) * 32 + lane;         // score warps: this thread's row of X
@@ -400,7 +431,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
+  const uint32_t tmem = uniform(*tmem_slot);
 
   if (warp == TMA_WARP) {
     // ------------------------------------------------------------------ producer (the whole warp keeps step)
@@ -453,13 +484,13 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     }
   } else if (warp == MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuer (the whole warp keeps step)
-    bool ok = warp_wait(bar(B_X), 0, abort_flag);
+    bool ok = warp_spin(bar(B_X), 0, abort_flag);
     for (int t = 0; t < n + NB - 1 && ok; ++t) {
       if (t < n) {
         const int st = t % L::STAGES, b = t % NB;
         const int here = min(CT, y_len - (DKDV ? t % y_tiles : t) * CT), n16 = (here + 15) / 16;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE;
-        if (!warp_wait(bar(B_FULL + st), (t / L::STAGES) & 1, abort_flag)) { ok = false; break; }
+        if (!warp_spin(bar(B_FULL + st), (t / L::STAGES) & 1, abort_flag)) { ok = false; break; }
         __syncwarp();
         // rows of Y behind the end of the sequence become zero, whatever lies there: they meet weights of
         // zero in the second products, and give scores of zero in the first
@@ -467,28 +498,30 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
           zero_rows(y, CT, SLABS, here, lane);
           zero_rows(y + L::YTILE, CT, SLABS, here, lane);
         }
-        if (lane == 0) {
+        if (elect_one()) {
           // S and dP overwrite P and dS of tile t - NB: their products were issued before, by this thread
           const uint32_t s_col = tmem + (uint32_t)(b * 2 * CT);
-          issue_scores(s_col, sb, RT, y, CT, 16 * n16, d / 16);
-          issue_scores(s_col + CT, sb + L::XTILE, RT, y + L::YTILE, CT, 16 * n16, d / 16);
+          issue_scores<SLABS, RT, CT>(s_col, sb, y, 16 * n16, d / 16);
+          issue_scores<SLABS, RT, CT>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
           umma_commit(bar(B_S + b));
         }
+        __syncwarp();                                          // lanes that poll would hold up the one that issues
       }
       const int u = t - (NB - 1);
       if (u >= 0) {
         const int st = u % L::STAGES, b = u % NB;
         const int here = min(CT, y_len - (DKDV ? u % y_tiles : u) * CT), n16 = (here + 15) / 16;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + (uint32_t)(b * 2 * CT);
-        if (!warp_wait(bar(B_P + b), (u / NB) & 1, abort_flag)) { ok = false; break; }
+        if (!warp_spin(bar(B_P + b), (u / NB) & 1, abort_flag)) { ok = false; break; }
         __syncwarp();
-        if (lane == 0) {
+        if (elect_one()) {
           tc_fence_after();
-          if (DKDV) issue_weighted(tmem + L::ACC1, s_col, y + L::YTILE, CT, d, n16, u == 0);
-          issue_weighted(tmem + L::ACC2, s_col + CT, y, CT, d, n16, u == 0);
+          if (DKDV) issue_weighted<CT>(tmem + L::ACC1, s_col, y + L::YTILE, d, n16, u == 0);
+          issue_weighted<CT>(tmem + L::ACC2, s_col + CT, y, d, n16, u == 0);
           umma_commit(bar(B_FREE + st));
           if (u == n - 1) umma_commit(bar(B_ACC));
         }
+        __syncwarp();
       }
     }
     __syncwarp();

@@ -19,7 +19,8 @@ class _Shape:
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--op", required=True, choices=["linear", "linear_ln", "attention", "layernorm", "rowstats"])
+    ap.add_argument("--op", required=True, choices=["linear", "linear_ln", "attention", "layernorm", "rowstats", "rope_axes", "qk_norm_rope",
+                                                   "qk_norm_rope_backward", "attention_packed", "attention_packed_backward"])
     ap.add_argument("--M", type=int, default=32896)
     ap.add_argument("--N", type=int, default=1280)
     ap.add_argument("--K", type=int, default=1280)
@@ -70,6 +71,47 @@ def main():
         run = lambda: vit.vit_op_attention(h, vit.VIT_BF16, a.images, a.T, a.heads, a.d, qkv.data_ptr(), out.data_ptr())
         work = 4.0 * a.images * a.T * a.T * H
         unit = "TFLOP/s"
+    elif a.op.startswith("attention_packed"):
+        # --images sequences of T tokens each, in the column blocks of one QKV buffer
+        rows, H = a.images * a.T, a.heads * a.d
+        qkv = torch.randn(rows, 3 * H, device="cuda").to(bf)
+        dout = torch.randn(rows, H, device="cuda").to(bf)
+        out, dqkv = torch.empty_like(dout), torch.empty_like(qkv)
+        lse = torch.empty(a.heads, rows, device="cuda")
+        off = (torch.arange(a.images + 1, device="cuda") * a.T).to(torch.int32)
+        p = vit.make_attention_problem(a.images, a.heads, a.heads, a.d, rows, a.T, off.data_ptr(), rows, a.T, off.data_ptr(), a.d ** -0.5)
+        n = max(vit.vit_attention_packed_bytes(vit.VIT_BF16, p, b) for b in (False, True))
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        q, dq = qkv.data_ptr(), dqkv.data_ptr()
+        fwd = lambda: vit.vit_op_attention_packed(h, vit.VIT_BF16, p, q, 3 * H, q + 2 * H, 3 * H, q + 4 * H, 3 * H, out.data_ptr(), H,
+                                                  lse.data_ptr(), ws.data_ptr(), n)
+        bwd = lambda: vit.vit_op_attention_packed_backward(
+            h, vit.VIT_BF16, p, q, 3 * H, q + 2 * H, 3 * H, q + 4 * H, 3 * H, out.data_ptr(), H, lse.data_ptr(), dout.data_ptr(), H, dq,
+            3 * H, dq + 2 * H, 3 * H, dq + 4 * H, 3 * H, ws.data_ptr(), n)
+        fwd()
+        backward = a.op.endswith("backward")
+        run = bwd if backward else fwd
+        work = (10.0 if backward else 4.0) * a.images * a.T * a.T * H
+        unit = "TFLOP/s"
+    elif a.op in ("rope_axes", "qk_norm_rope", "qk_norm_rope_backward"):
+        # --M rows, query and key heads of a QKV buffer, two position axes
+        H = 2 * a.heads * a.d
+        x = torch.randn(a.M, 3 * a.heads * a.d, device="cuda").to(bf)
+        dy, y = torch.randn(a.M, H, device="cuda").to(bf), torch.empty(a.M, H, device="cuda", dtype=bf)
+        g, dg = torch.ones(2, a.d, device="cuda"), torch.empty(2, a.d, device="cuda")
+        freqs = (100.0 ** (-torch.arange(a.d // 2, device="cuda") / (a.d // 2))).float()
+        pos = torch.randint(0, 64, (2, a.M), device="cuda").to(torch.int32)
+        rope = vit.make_rope((a.d // 4, a.d // 2 - a.d // 4), freqs.data_ptr(), pos.data_ptr())
+        n = vit.vit_qk_norm_rope_backward_bytes(a.M, a.heads, a.heads, a.d)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        common = (h, vit.VIT_BF16, a.M, a.heads, a.heads, a.d, g[0].data_ptr(), g[1].data_ptr(), 1e-6, rope, x.data_ptr(), x.stride(0))
+        run = {"rope_axes": lambda: vit.vit_op_rope_axes(h, vit.VIT_BF16, a.M, 2 * a.heads, a.d, rope, 0, x.data_ptr(), x.stride(0),
+                                                         y.data_ptr(), H),
+               "qk_norm_rope": lambda: vit.vit_op_qk_norm_rope(*common, y.data_ptr(), H),
+               "qk_norm_rope_backward": lambda: vit.vit_op_qk_norm_rope_backward(*common, dy.data_ptr(), H, y.data_ptr(), H,
+                                                                                 dg[0].data_ptr(), dg[1].data_ptr(), ws.data_ptr(), n)}[a.op]
+        work = a.M * H * 2 * (3.0 if a.op.endswith("backward") else 2.0) / 1e-3   # bytes, scaled so the print below reads GB/s
+        unit = "GB/s"
     else:
         x = torch.randn(a.M, a.N, device="cuda").to(bf)
         y = torch.empty_like(x)
