@@ -22,11 +22,6 @@ constexpr int THREADS = 256;
 constexpr int PS = BT + 4;          // row stride of a tile of probabilities
 
 __device__ __forceinline__ float4 load4(const float* a) { return *reinterpret_cast<const float4*>(a); }
-__device__ __forceinline__ float4 load4(const bf16* a) {
-  const uint2 u = *reinterpret_cast<const uint2*>(a);
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
-}
 
 // rows [row0, row0 + 64) of one head as fp32 [64][DP + 4]; rows >= end and columns >= d are zero
 template <int DP>
@@ -160,7 +155,6 @@ packed_forward_kernel(const PackedCall c) {
 }
 
 // (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head
-template <typename T>
 __global__ void __launch_bounds__(THREADS)
 packed_delta_kernel(const PackedCall c) {
   const int64_t item = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
@@ -172,8 +166,8 @@ packed_delta_kernel(const PackedCall c) {
   float sum = 0.f;
   if (lane * 4 < c.p.d) {
     const int64_t col = (int64_t)head * c.p.d + lane * 4;
-    const float4 a = load4(static_cast<const T*>(c.out) + row * c.ldo + col);
-    const float4 b = load4(static_cast<const T*>(c.dout) + row * c.lddo + col);
+    const float4 a = load4(static_cast<const float*>(c.out) + row * c.ldo + col);
+    const float4 b = load4(static_cast<const float*>(c.dout) + row * c.lddo + col);
     sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w)));
   }
 #pragma unroll
@@ -362,18 +356,12 @@ cudaError_t launch_width(const PackedCall& c, Which w, cudaStream_t s) {
 
 cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, FORWARD, s); }
 
-cudaError_t launch_attention_delta(const PackedCall& c, bool act_bf16, cudaStream_t s) {
+cudaError_t launch_attention_delta_f32(const PackedCall& c, cudaStream_t s) {
   const int64_t items = (int64_t)c.p.q_rows * c.p.heads;
-  const unsigned blocks = (unsigned)((items + THREADS / 32 - 1) / (THREADS / 32));
-  if (act_bf16) packed_delta_kernel<bf16><<<blocks, THREADS, 0, s>>>(c);
-  else packed_delta_kernel<float><<<blocks, THREADS, 0, s>>>(c);
+  packed_delta_kernel<<<(unsigned)((items + THREADS / 32 - 1) / (THREADS / 32)), THREADS, 0, s>>>(c);
   return cudaGetLastError();
 }
-cudaError_t launch_attention_packed_dkdv(const PackedCall& c, bool act_bf16, cudaStream_t s) {
-  return act_bf16 ? launch_attention_packed_dkdv_bf16(c, s) : launch_width(c, DKDV, s);
-}
-cudaError_t launch_attention_packed_dq(const PackedCall& c, bool act_bf16, cudaStream_t s) {
-  return act_bf16 ? launch_attention_packed_dq_bf16(c, s) : launch_width(c, DQ, s);
-}
+cudaError_t launch_attention_packed_dkdv_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, DKDV, s); }
+cudaError_t launch_attention_packed_dq_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, DQ, s); }
 
 }  // namespace vit

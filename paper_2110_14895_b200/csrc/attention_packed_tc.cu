@@ -8,6 +8,12 @@
 // and are the A operand of the second products, so that nothing of the score matrix leaves the SM.  One
 // thread owns one row of a tile of scores.
 //
+// Persistent blocks, one per SM, walk over the work with a static schedule; the operands of the next piece
+// are fetched while the last one is finished.  A tile of queries (or of whatever stays) is held in tensor
+// memory too where it fits, as the A operand of the scores: with both operands in shared memory a product
+// of 128 x 64 x 16 reads 6 KB there in the 32 cycles that it takes, more than the 128 bytes a cycle that
+// shared memory gives, and holds up everything else that goes through it.
+//
 // Every mbarrier wait is bounded; on expiry the block raises the device status word, lets the copies and
 // products in flight finish (bounded), frees tensor memory and leaves.
 #include "vit_internal.h"
@@ -23,6 +29,7 @@ namespace {
 using namespace ptx;
 
 constexpr int RT = 128;                                // rows of a tile of scores = lanes of tensor memory
+constexpr int CT = 64;                                 // columns of a tile of scores
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 constexpr long long DRAIN_LIMIT_CYCLES = 1ll << 24;    // teardown after a failed wait: ~10 ms
 
@@ -54,18 +61,22 @@ __device__ __forceinline__ void store_16_bf16(bf16* dst, const uint32_t (&o)[16]
   *reinterpret_cast<uint4*>(dst + 8) = make_uint4(w[4], w[5], w[6], w[7]);
 }
 // a bounded wait of a whole warp: all lanes leave with the same answer
-__device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag) {
-  return __all_sync(0xffffffffu, mbar_wait(bar, (uint32_t)parity, abort_flag));
+__device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag, long long limit = WAIT_LIMIT_CYCLES) {
+  return __all_sync(0xffffffffu, mbar_wait_limit(bar, (uint32_t)parity, abort_flag, limit));
 }
-// the same without letting the hardware suspend the warp: for the one warp that issues the products, which
-// otherwise takes a few hundred cycles to come back
+// the same without letting the hardware suspend the warp: for the warps that issue the products, which
+// otherwise take a few hundred cycles to come back
+__device__ __forceinline__ bool mbar_test(uint32_t bar, int parity) {
+  uint32_t done;
+  asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(done) : "r"(bar), "r"((uint32_t)parity) : "memory");
+  return done != 0;
+}
 __device__ __forceinline__ bool warp_spin(uint32_t bar, int parity, volatile int* abort_flag) {
+  if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
   const long long t0 = clock64();
   for (;;) {
-    uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
-                 : "=r"(done) : "r"(bar), "r"((uint32_t)parity) : "memory");
-    if (__all_sync(0xffffffffu, done)) return true;
+    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
     const bool late = clock64() - t0 > WAIT_LIMIT_CYCLES;
     if (late) *abort_flag = 1;
     if (__any_sync(0xffffffffu, late || *abort_flag)) return false;
@@ -89,69 +100,100 @@ __device__ __forceinline__ bool elect_one() {
 }
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 
-// S[128 x n] = X[128 rows] . Y[n rows]^T over the head's channels, both operands as slabs of 64 channels
-template <int SLABS, int X_ROWS, int Y_ROWS>
-__device__ __forceinline__ void issue_scores(uint32_t d_tmem, uint32_t x, uint32_t y, int n, int ksteps) {
+// S[128 x n] = X[128 rows] . Y[n rows]^T over the head's channels; X in tensor memory (packed pairs) or in
+// shared memory, as slabs of 64 channels like Y
+template <int SLABS>
+__device__ __forceinline__ void issue_scores_ts(uint32_t d_tmem, uint32_t x_tmem, uint32_t y, int n, int ksteps) {
+  const uint32_t id = idesc(n, false);
+  const uint64_t yd = desc_sw128(y);
+#pragma unroll
+  for (int k = 0; k < 4 * SLABS; ++k)
+    if (k < ksteps) umma_bf16_ts(d_tmem, x_tmem + (uint32_t)(8 * k), yd + (uint64_t)((k >> 2) * (CT * 8) + 2 * (k & 3)), id, k > 0 ? 1u : 0u);
+}
+template <int SLABS>
+__device__ __forceinline__ void issue_scores_ss(uint32_t d_tmem, uint32_t x, uint32_t y, int n, int ksteps) {
   const uint32_t id = idesc(n, false);
   const uint64_t xd = desc_sw128(x), yd = desc_sw128(y);
 #pragma unroll
   for (int k = 0; k < 4 * SLABS; ++k)
     if (k < ksteps)
-      umma_bf16(d_tmem, xd + (uint64_t)((k >> 2) * (X_ROWS * 8) + 2 * (k & 3)), yd + (uint64_t)((k >> 2) * (Y_ROWS * 8) + 2 * (k & 3)), id,
+      umma_bf16(d_tmem, xd + (uint64_t)((k >> 2) * (RT * 8) + 2 * (k & 3)), yd + (uint64_t)((k >> 2) * (CT * 8) + 2 * (k & 3)), id,
                 k > 0 ? 1u : 0u);
 }
 // D[128 x d] (+)= P[128 x 16 ksteps] . Y[16 ksteps rows x d], P packed in tensor memory
-template <int Y_ROWS>
 __device__ __forceinline__ void issue_weighted(uint32_t d_tmem, uint32_t p_tmem, uint32_t y, int d, int ksteps, bool first) {
   const uint32_t id = idesc(d, true);
-  const uint64_t yd = desc_sw128(y, Y_ROWS * 128);
+  const uint64_t yd = desc_sw128(y, CT * 128);
 #pragma unroll
-  for (int k = 0; k < Y_ROWS / 16; ++k)
+  for (int k = 0; k < CT / 16; ++k)
     if (k < ksteps) umma_bf16_ts(d_tmem, p_tmem + (uint32_t)(8 * k), yd + (uint64_t)(k * 128), id, first && k == 0 ? 0u : 1u);
+}
+// A row of d channels from global memory into tensor memory, 16 channels (8 columns) at a time; rows that are
+// not there become zero.  `each` sees the words on their way.
+template <typename Each>
+__device__ __forceinline__ void row_to_tmem(uint32_t taddr, const bf16* src, int d, bool there, Each each) {
+#pragma unroll 2
+  for (int g = 0; g < d / 16; ++g) {
+    uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+    if (there) {
+      a = reinterpret_cast<const uint4*>(src)[2 * g];
+      b = reinterpret_cast<const uint4*>(src)[2 * g + 1];
+    }
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    tmem_st8(taddr + (uint32_t)(8 * g), w);
+    each(g, w);
+  }
+}
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float acc) {
+  acc = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), acc);
+  return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), acc);
+}
+
+// A piece of work: `span` rows of one head of one sequence.
+struct Piece { int head, x0; SeqRange r; };
+// The first piece from number i on (in steps of the grid) whose rows exist; i = total if there is none.
+__device__ __forceinline__ int find_piece(const PackedCall& c, int i, int total, int tiles, int heads, int span, bool of_keys, Piece& w) {
+  for (; i < total; i += (int)gridDim.x) {
+    const int seq = i / tiles / heads;
+    w.head = i / tiles % heads;
+    w.x0 = i % tiles * span;
+    if (seq_range(c.p, seq, w.r, c.dev_status) && w.x0 < (of_keys ? w.r.k_len : w.r.q_len)) return i;
+  }
+  return total;
 }
 
 // ============================================================================================ forward
-// One block per (sequence, head, 128 queries): warps 0-3 softmax, warp 4 MMA, warp 5 TMA.  Two blocks share
-// an SM (256 columns of tensor memory each): while one is in its exp2 phase the tensor core works for the
-// other.  Keys come in tiles of 128.  The accumulator is rescaled only when a row's maximum has grown by
-// more than 2^8 since the last time (probabilities stay below 2^8, the row sum in fp32).
+// A piece is 256 queries of a head: warps 0-3 and 4-7 hold 128 of them each and share the keys, which come
+// in tiles of 64; warps 8 and 9 issue the products of one warpgroup each, warp 10 the copies.  Each warpgroup has two tiles of scores, so
+// that the next one is ready when it has finished its exp2 phase.  The accumulator is rescaled only when a
+// row's maximum has grown by more than 2^8 since the last time (probabilities stay below 2^8, the row sum
+// in fp32): it rarely is after the first tile, and only then does a warpgroup wait for its last product.
 struct ForwardMaps { CUtensorMap q, k, v; };
 
-template <int SLABS>
-struct ForwardSmem {
-  static constexpr int STAGES = SLABS == 1 ? 2 : 1;
-  static constexpr uint32_t TILE = SLABS * RT * 128;
-  static constexpr uint32_t OFF_K = TILE, OFF_V = OFF_K + STAGES * TILE, OFF_BARS = OFF_V + STAGES * TILE;
-  static constexpr uint32_t BYTES = OFF_BARS + 256 + 1024;
+template <int SLABS, bool XT>
+struct ForwardCfg {
+  static constexpr int STAGES = SLABS == 1 ? 6 : 4;
+  static constexpr uint32_t TILE = SLABS * CT * 128, QTILE = SLABS * RT * 128;
+  static constexpr uint32_t OFF_K = XT ? 0 : 2 * QTILE, OFF_V = OFF_K + STAGES * TILE, OFF_BARS = OFF_V + STAGES * TILE;
+  static constexpr uint32_t BYTES = OFF_BARS + 512 + 1024;
+  static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
-constexpr int FWD_THREADS = 192;
-constexpr uint32_t FWD_TMEM = 256, O_COL = 128;
-enum FwdBar : int { F_Q = 0, F_KFULL, F_KFREE = F_KFULL + 2, F_VFULL = F_KFREE + 2, F_VFREE = F_VFULL + 2, F_S = F_VFREE + 2, F_P, F_O, F_DRAIN, F_BARS };
+constexpr int TC_THREADS = 352, MMA_WARP = 8 /* two */, TMA_WARP = 10;
+constexpr uint32_t TMEM_ALL = 512;
+// columns of a warpgroup (256): two tiles of scores, the accumulator (d), the queries (d / 2)
+constexpr uint32_t F_WG = 256, F_O = 2 * CT;
+enum FwdBar : int {
+  F_KFULL = 0, F_KFREE = F_KFULL + 6, F_VFULL = F_KFREE + 6, F_VFREE = F_VFULL + 6, F_Q = F_VFREE + 6 /* [wg], or [0] for both */,
+  F_QFREE = F_Q + 2, F_S = F_QFREE + 1 /* [wg][tile parity] */, F_P = F_S + 4, F_PV = F_P + 4, F_DRAIN = F_PV + 4 /* [MMA warp] */, F_BARS = F_DRAIN + 2
+};
 
-template <int SLABS>
-__global__ void __launch_bounds__(FWD_THREADS, 2)
-packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedCall c) {
-  using L = ForwardSmem<SLABS>;
+template <int SLABS, bool XT>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedCall c, int total, int tiles) {
+  using L = ForwardCfg<SLABS, XT>;
   extern __shared__ uint8_t smem_raw[];
-  const int tiles = (c.p.max_q + RT - 1) / RT;
-  const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
-  SeqRange r;
-  if (!seq_range(c.p, seq, r, c.dev_status)) return;
-  const int q0 = tile * RT;
-  if (q0 >= r.q_len) return;
-  const int d = c.p.d, kv = head / (c.p.heads / c.p.kv_heads);
+  const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const int row = q0 + (warp & 3) * 32 + lane;                   // softmax warps: this thread's query
-  const int64_t at = (int64_t)r.q_begin + row;
-  const int n_tiles = (r.k_len + RT - 1) / RT;
-  if (n_tiles == 0) {                                            // no keys
-    if (warp < 4 && row < r.q_len) {
-      bf16* out = static_cast<bf16*>(c.out) + at * c.ldo + (int64_t)head * d;
-      for (int i = 0; i < d; i += 8) *reinterpret_cast<uint4*>(out + i) = make_uint4(0u, 0u, 0u, 0u);
-      c.lse[(int64_t)head * c.p.q_rows + at] = -INFINITY;
-    }
-    return;
-  }
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t sb = smem_u32(smem);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BARS);
@@ -160,444 +202,247 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
-    for (int i = 0; i < F_BARS; ++i) mbar_init(bar(i), i == F_P ? 4 : 1);
+    for (int i = 0; i < F_BARS; ++i) {
+      const bool stage_free = (i >= F_KFREE && i < F_KFREE + 6) || (i >= F_VFREE && i < F_VFREE + 6) || i == F_QFREE;   // by both MMA warps
+      const bool by_warps = (i >= F_P && i < F_P + 4) || (XT && (i == F_Q || i == F_Q + 1));
+      mbar_init(bar(i), stage_free ? 2 : by_warps ? 4 : 1);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 4) tmem_alloc(smem_u32(tmem_slot), FWD_TMEM);
+  if (warp == MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
+  Piece w;
 
-  if (warp == 5) {
+  if (warp == TMA_WARP) {
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0) {
-      mbar_arrive_expect_tx(bar(F_Q), L::TILE);
-      for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + s * RT * 128, &maps.q, 64 * s, head, r.q_begin + q0, bar(F_Q));
-      int armed = 0;
+      int t = 0, pieces = 0, armed_k = 0, armed_v = 0;           // tiles and pieces so far
       bool ok = true;
-      for (int j = 0; j < n_tiles && ok; ++j) {
-        const int st = j % L::STAGES, ph = (j / L::STAGES) & 1;
-        const int krow = r.k_begin + j * RT;
-        if (!mbar_wait(bar(F_KFREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
-        mbar_arrive_expect_tx(bar(F_KFULL + st), L::TILE);
-        for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_K + st * L::TILE + s * RT * 128, &maps.k, 64 * s, kv, krow, bar(F_KFULL + st));
-        armed = 2 * j + 1;
-        if (!mbar_wait(bar(F_VFREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
-        mbar_arrive_expect_tx(bar(F_VFULL + st), L::TILE);
-        for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_V + st * L::TILE + s * RT * 128, &maps.v, 64 * s, kv, krow, bar(F_VFULL + st));
-        armed = 2 * j + 2;
+      for (int i = find_piece(c, blockIdx.x, total, tiles, c.p.heads, 2 * RT, false, w); i < total && ok;
+           i = find_piece(c, i + gridDim.x, total, tiles, c.p.heads, 2 * RT, false, w)) {
+        const int n = (w.r.k_len + CT - 1) / CT, kv = w.head / group;
+        if (n == 0) continue;
+        if (!XT) {
+          if (!mbar_wait(bar(F_QFREE), (pieces & 1) ^ 1, abort_flag)) break;
+          mbar_arrive_expect_tx(bar(F_Q), 2 * L::QTILE);
+          for (int s = 0; s < 2 * SLABS; ++s)                    // both tiles; rows behind the sequence are not used
+            tma_load_3d(sb + s * RT * 128, &maps.q, 64 * (s % SLABS), w.head, w.r.q_begin + w.x0 + s / SLABS * RT, bar(F_Q));
+          ++pieces;
+        }
+        for (int j = 0; j < n; ++j, ++t) {
+          const int st = t % L::STAGES, ph = (t / L::STAGES) & 1, krow = w.r.k_begin + j * CT;
+          if (!mbar_wait(bar(F_KFREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
+          mbar_arrive_expect_tx(bar(F_KFULL + st), L::TILE);
+          armed_k = t + 1;
+          for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_K + st * L::TILE + s * CT * 128, &maps.k, 64 * s, kv, krow, bar(F_KFULL + st));
+          if (!mbar_wait(bar(F_VFREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
+          mbar_arrive_expect_tx(bar(F_VFULL + st), L::TILE);
+          armed_v = t + 1;
+          for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_V + st * L::TILE + s * CT * 128, &maps.v, 64 * s, kv, krow, bar(F_VFULL + st));
+        }
       }
       if (*abort_flag) {
         // a wait gave up somewhere: let the copies that were started land before the block leaves
         volatile int never = 0;
-        mbar_wait_limit(bar(F_Q), 0, &never, DRAIN_LIMIT_CYCLES);
-        for (int i = armed > 2 * L::STAGES ? armed - 2 * L::STAGES : 0; i < armed; ++i) {
-          const int j = i >> 1, st = j % L::STAGES;
-          mbar_wait_limit(bar((i & 1 ? F_VFULL : F_KFULL) + st), (j / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
-        }
+        if (!XT && pieces) mbar_wait_limit(bar(F_Q), (pieces - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
+        for (int i = armed_k > L::STAGES ? armed_k - L::STAGES : 0; i < armed_k; ++i)
+          mbar_wait_limit(bar(F_KFULL + i % L::STAGES), (i / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
+        for (int i = armed_v > L::STAGES ? armed_v - L::STAGES : 0; i < armed_v; ++i)
+          mbar_wait_limit(bar(F_VFULL + i % L::STAGES), (i / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
       }
     }
-  } else if (warp == 4) {
-    // ------------------------------------------------------------------ MMA issuer (the whole warp keeps step)
-    bool ok = warp_spin(bar(F_Q), 0, abort_flag);
-    for (int j = 0; j < n_tiles && ok; ++j) {
-      const int st = j % L::STAGES, ph = (j / L::STAGES) & 1;
-      const int here = min(RT, r.k_len - j * RT), n16 = (here + 15) / 16;
-      const uint32_t ks = sb + L::OFF_K + st * L::TILE, vs = sb + L::OFF_V + st * L::TILE;
-      if (!warp_spin(bar(F_KFULL + st), ph, abort_flag)) { ok = false; break; }
-      __syncwarp();
-      if (elect_one()) {
-        // the scores overwrite P of tile j - 1: its product was issued before, by this thread
-        issue_scores<SLABS, RT, RT>(tmem, sb, ks, 16 * n16, d / 16);
-        umma_commit(bar(F_S));
-        umma_commit(bar(F_KFREE + st));
+  } else if (warp >= MMA_WARP) {
+    // ------------------------------------------------------------------ MMA issuers, one per warpgroup (the whole warp keeps step)
+    const int h = warp - MMA_WARP;
+    const uint32_t base = tmem + h * F_WG;
+    int t0 = 0, g = 0, seen = 0;                                 // tiles of keys so far, those of this warpgroup, pieces
+    bool ok = true;
+    for (int i = find_piece(c, blockIdx.x, total, tiles, c.p.heads, 2 * RT, false, w); i < total && ok;
+         i = find_piece(c, i + gridDim.x, total, tiles, c.p.heads, 2 * RT, false, w)) {
+      const int n = (w.r.k_len + CT - 1) / CT;
+      if (n == 0) continue;
+      const bool mine = w.x0 + h * RT < w.r.q_len;               // else the stages are passed on only
+      for (int j = 0; j <= n; ++j) {
+        if (j < n) {
+          const int st = (t0 + j) % L::STAGES, n16 = (min(CT, w.r.k_len - j * CT) + 15) / 16, b = (g + j) & 1;
+          const uint32_t ks = sb + L::OFF_K + st * L::TILE;
+          if (!warp_spin(bar(F_KFULL + st), ((t0 + j) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
+          if (j == 0 && (mine || !XT) && !warp_spin(bar(F_Q + (XT ? h : 0)), seen & 1, abort_flag)) { ok = false; break; }
+          if (elect_one()) {
+            if (mine) {
+              // the scores overwrite P of tile j - 2: its product was issued before, by this warp
+              tc_fence_after();
+              if (XT) issue_scores_ts<SLABS>(base + b * CT, base + F_O + d, ks, 16 * n16, d / 16);
+              else issue_scores_ss<SLABS>(base + b * CT, sb + h * L::QTILE, ks, 16 * n16, d / 16);
+              umma_commit(bar(F_S + 2 * h + b));
+            }
+            umma_commit(bar(F_KFREE + st));
+            if (!XT && j == n - 1) umma_commit(bar(F_QFREE));
+          }
+          __syncwarp();                                          // lanes that poll would hold up the one that issues
+        }
+        if (j > 0) {
+          const int jj = j - 1, st = (t0 + jj) % L::STAGES, here = min(CT, w.r.k_len - jj * CT), n16 = (here + 15) / 16, b = (g + jj) & 1;
+          const uint32_t vs = sb + L::OFF_V + st * L::TILE;
+          if (!warp_spin(bar(F_VFULL + st), ((t0 + jj) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
+          // rows of V behind the last key meet probabilities of zero: make them zero too, whatever lies there
+          // (both warps write the same zeros; neither reads before its own are there)
+          if (mine && here < 16 * n16) zero_rows(vs, CT, SLABS, here, lane);
+          if (mine && !warp_spin(bar(F_P + 2 * h + b), ((g + jj) >> 1) & 1, abort_flag)) { ok = false; break; }
+          if (elect_one()) {
+            if (mine) {
+              tc_fence_after();
+              issue_weighted(base + F_O, base + b * CT, vs, d, n16, jj == 0);
+              umma_commit(bar(F_PV + 2 * h + b));
+            }
+            umma_commit(bar(F_VFREE + st));
+          }
+          __syncwarp();
+        }
       }
-      __syncwarp();                                            // lanes that poll would hold up the one that issues
-      if (!warp_spin(bar(F_VFULL + st), ph, abort_flag)) { ok = false; break; }
-      __syncwarp();
-      // rows of V behind the last key meet probabilities of zero: make them zero too, whatever lies there
-      if (here < 16 * n16) zero_rows(vs, RT, SLABS, here, lane);
-      if (!warp_spin(bar(F_P), j & 1, abort_flag)) { ok = false; break; }
-      __syncwarp();
-      if (elect_one()) {
-        tc_fence_after();
-        issue_weighted<RT>(tmem + O_COL, tmem, vs, d, n16, j == 0);
-        umma_commit(bar(F_VFREE + st));
-        if (j == n_tiles - 1) umma_commit(bar(F_O));
-      }
-      __syncwarp();
+      t0 += n;
+      if (mine || !XT) ++seen;
+      if (mine) g += n;
     }
     __syncwarp();
     if (*abort_flag && lane == 0) {
       volatile int never = 0;
-      umma_commit(bar(F_DRAIN));
-      mbar_wait_limit(bar(F_DRAIN), 0, &never, DRAIN_LIMIT_CYCLES);
+      umma_commit(bar(F_DRAIN + h));
+      mbar_wait_limit(bar(F_DRAIN + h), 0, &never, DRAIN_LIMIT_CYCLES);
     }
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
-    const uint32_t taddr = tmem + ((uint32_t)(warp * 32) << 16);
-    const float sl2 = c.p.scale * LOG2E;
-    const bool warp_active = q0 + warp * 32 < r.q_len;
-    float m = -INFINITY, l = 0.f;                       // row maximum in use (raw scores), row sum
-    bool ok = true;
-    for (int j = 0; j < n_tiles && ok; ++j) {
-      const int here = min(RT, r.k_len - j * RT);
-      const int nch = (here + 31) / 32;
-      if (!warp_wait(bar(F_S), j & 1, abort_flag)) { ok = false; break; }
-      tc_fence_after();
-      if (warp_active) {
-        uint32_t x[2][32];
-        float top = -INFINITY;
-        // pass 1: row maximum
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          if (i >= nch) break;
-          tmem_ld32(taddr + (uint32_t)(32 * i), x[0]);
-          tmem_ld32(taddr + (uint32_t)(32 * (i + 1)), x[1]);
-          tmem_ld_wait_for(x[0]);
-          tmem_ld_wait_for(x[1]);
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const int left = here - 32 * (i + h);
-            if (left >= 32) {
-              float m2[2] = {top, top};
-#pragma unroll
-              for (int e = 0; e < 32; e += 4) {
-                asm("max.f32 %0, %0, %1, %2;" : "+f"(m2[0]) : "f"(__uint_as_float(x[h][e])), "f"(__uint_as_float(x[h][e + 1])));
-                asm("max.f32 %0, %0, %1, %2;" : "+f"(m2[1]) : "f"(__uint_as_float(x[h][e + 2])), "f"(__uint_as_float(x[h][e + 3])));
-              }
-              top = fmaxf(m2[0], m2[1]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (e < left) top = fmaxf(top, __uint_as_float(x[h][e]));
-            }
-          }
-        }
-        const bool grow = (top - m) * sl2 > 8.f;         // false for NaN and for -infinity over -infinity
-        if (__any_sync(0xffffffffu, grow)) {
-          const float factor = grow ? (m == -INFINITY ? 0.f : ex2_approx((m - top) * sl2)) : 1.f;
-          if (grow) m = top;
-          l *= factor;
-          if (j > 0) {                                   // the products of tile j - 1 are complete: this tile's scores are
-            for (int g = 0; g < d / 16; ++g) {
-              uint32_t o[16];
-              tmem_ld16(taddr + O_COL + (uint32_t)(16 * g), o);
-              tmem_ld_wait();
-#pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
-              tmem_st16(taddr + O_COL + (uint32_t)(16 * g), o);
-            }
-          }
-        }
-        // pass 2: p = exp2((s - m) sl2), row sum, P (bf16 pairs) over columns this thread has read
-        const float nm = m == -INFINITY ? 0.f : -m * sl2;
-        const float2 sl2v = make_float2(sl2, sl2), nmv = make_float2(nm, nm);
-        float2 l2 = make_float2(0.f, 0.f);
-        tmem_ld32(taddr, x[0]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (i >= nch) break;
-          tmem_ld_wait_for(x[i & 1]);
-          if (i + 1 < 4 && i + 1 < nch) tmem_ld32(taddr + (uint32_t)(32 * (i + 1)), x[(i + 1) & 1]);
-          const uint32_t (&s)[32] = x[i & 1];
-          uint32_t pk[16];
-          const int left = here - 32 * i;
-          if (left >= 32) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float2 y = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), sl2v, nmv);
-              const float2 p = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-              l2 = __fadd2_rn(l2, p);
-              pk[e] = pack_bf16(p.x, p.y);
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float p0 = 2 * e < left ? ex2_approx(fmaf(__uint_as_float(s[2 * e]), sl2, nm)) : 0.f;
-              const float p1 = 2 * e + 1 < left ? ex2_approx(fmaf(__uint_as_float(s[2 * e + 1]), sl2, nm)) : 0.f;
-              l2.x += p0;
-              l2.y += p1;
-              pk[e] = pack_bf16(p0, p1);
-            }
-          }
-          tmem_st16(taddr + (uint32_t)(16 * i), pk);
-        }
-        l += l2.x + l2.y;
-        tmem_st_wait();
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar(F_P));
-    }
-    if (ok && warp_wait(bar(F_O), 0, abort_flag)) {
-      tc_fence_after();
-      if (warp_active) {
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        bf16* out = static_cast<bf16*>(c.out) + at * c.ldo + (int64_t)head * d;
-        for (int g = 0; g < d / 16; ++g) {
-          uint32_t o[16];
-          tmem_ld16(taddr + O_COL + (uint32_t)(16 * g), o);
-          tmem_ld_wait();
-          if (row < r.q_len) store_16_bf16(out + 16 * g, o, inv);
-        }
-        if (row < r.q_len) c.lse[(int64_t)head * c.p.q_rows + at] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
-      }
-    }
-  }
-  // ---------------------------------------------------------------------- teardown
-  __syncwarp();
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  if (threadIdx.x == 0 && *abort_flag) atomicExch(c.dev_status, (int)VIT_ERR_TIMEOUT);
-  if (warp == 4) {
-    __syncwarp();
-    tmem_dealloc(tmem, FWD_TMEM);
-  }
-}
-
-// ============================================================================================ backward
-// Two kernels of one form.  A block keeps a tile of 128 rows X1, X2 and walks over tiles of 64 rows Y1, Y2:
-//   S = X1 Y1^T, dP = X2 Y2^T;  P = exp2(S sl2 - lse2), dS = P (dP - delta)
-//   DKDV: X = K, V; Y = Q, dout of every query head that shares the key head (scores transposed);
-//         dv += P Y2, dk += dS Y1
-//   DQ:   X = Q, dout; Y = K, V;  dq += dS Y1
-// NB warpgroups take the tiles in turn, each with its own columns of tensor memory for S and dP, so that
-// the tensor core works for one while the others are in their exp2 phase; the MMA warp runs NB - 1 tiles ahead.
-struct BackwardMaps { CUtensorMap x1, x2, y1, y2; };
-
-constexpr int CT = 64;                                 // rows of a Y tile = columns of a tile of scores
-template <int SLABS, bool DKDV, int NB>
-struct BackwardCfg {
-  static constexpr int STAGES = NB + 2;
-  static constexpr int THREADS = NB * 128 + 64;
-  static constexpr uint32_t XTILE = SLABS * RT * 128, YTILE = SLABS * CT * 128;
-  static constexpr uint32_t OFF_Y = 2 * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // float2 [STAGES][64]: -lse2, -delta of the columns
-  static constexpr uint32_t OFF_BARS = OFF_COL + STAGES * CT * 8;
-  static constexpr uint32_t BYTES = OFF_BARS + 512 + 1024;
-  static constexpr uint32_t ACC = 64 * SLABS;          // columns of one accumulator
-  static constexpr uint32_t USED = NB * 2 * CT + (DKDV ? 2 : 1) * ACC;
-  static constexpr uint32_t TMEM = USED <= 256 ? 256 : 512;
-  static constexpr uint32_t ACC1 = NB * 2 * CT, ACC2 = ACC1 + (DKDV ? ACC : 0);        // dv; dk or dq
-  static_assert(USED <= 512 && BYTES <= 227 * 1024, "fits an SM");
-};
-enum BwdBar : int { B_X = 0, B_FULL, B_FREE = B_FULL + 5, B_S = B_FREE + 5, B_P = B_S + 4, B_ACC = B_P + 4, B_DRAIN, B_BARS };
-
-template <int SLABS, bool DKDV, int NB>
-__global__ void __launch_bounds__(NB * 128 + 64, NB == 1 ? 2 : 1)
-packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c) {
-  using L = BackwardCfg<SLABS, DKDV, NB>;
-  extern __shared__ uint8_t smem_raw[];
-  const int max_x = DKDV ? c.p.max_k : c.p.max_q, x_heads = DKDV ? c.p.kv_heads : c.p.heads;
-  const int tiles = (max_x + RT - 1) / RT;
-  const int tile = blockIdx.x % tiles, xh = blockIdx.x / tiles % x_heads, seq = blockIdx.x / tiles / x_heads;
-  SeqRange r;
-  if (!seq_range(c.p, seq, r, c.dev_status)) return;
-  const int x_begin = DKDV ? r.k_begin : r.q_begin, x_len = DKDV ? r.k_len : r.q_len;
-  const int y_begin = DKDV ? r.q_begin : r.k_begin, y_len = DKDV ? r.q_len : r.k_len;
-  const int x0 = tile * RT;
-  if (x0 >= x_len) return;
-  const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
-  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
-  const int y_tiles = (y_len + CT - 1) / CT;
-  const int n = DKDV ? group * y_tiles : y_tiles;      // tiles in all, head after head
-  const int row = x0 + (warp & 3) * 32 + lane;         // score warps: this thread's row of X
-  const int64_t at = (int64_t)x_begin + row;
-  bf16* g1 = DKDV ? static_cast<bf16*>(c.dv) + at * c.lddv + (int64_t)xh * d : nullptr;
-  bf16* g2 = DKDV ? static_cast<bf16*>(c.dk) + at * c.lddk + (int64_t)xh * d : static_cast<bf16*>(c.dq) + at * c.lddq + (int64_t)xh * d;
-  if (n == 0) {                                        // nothing attends or is attended to: zero
-    if (warp < 4 && row < x_len)
-      for (int i = 0; i < d; i += 8) {
-        *reinterpret_cast<uint4*>(g2 + i) = make_uint4(0u, 0u, 0u, 0u);
-        if (DKDV) *reinterpret_cast<uint4*>(g1 + i) = make_uint4(0u, 0u, 0u, 0u);
-      }
-    return;
-  }
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sb = smem_u32(smem);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BARS);
-  auto bar = [&](int i) { return smem_u32(&bars[i]); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(&bars[B_BARS]);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  constexpr int MMA_WARP = NB * 4, TMA_WARP = MMA_WARP + 1;
-  if (threadIdx.x == 0) {
-    *abort_flag = 0;
-    for (int i = 0; i < B_BARS; ++i) mbar_init(bar(i), i >= B_P && i < B_P + 4 ? 4 : 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  if (warp == MMA_WARP) tmem_alloc(smem_u32(tmem_slot), L::TMEM);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = uniform(*tmem_slot);
-
-  if (warp == TMA_WARP) {
-    // ------------------------------------------------------------------ producer (the whole warp keeps step)
-    if (lane == 0) {
-      mbar_arrive_expect_tx(bar(B_X), 2 * L::XTILE);
-      for (int s = 0; s < SLABS; ++s) {
-        tma_load_3d(sb + s * RT * 128, &maps.x1, 64 * s, xh, x_begin + x0, bar(B_X));
-        tma_load_3d(sb + L::XTILE + s * RT * 128, &maps.x2, 64 * s, xh, x_begin + x0, bar(B_X));
-      }
-    }
-    int armed = 0;
-    for (int t = 0; t < n; ++t) {
-      const int st = t % L::STAGES, ph = (t / L::STAGES) & 1;
-      const int yh = DKDV ? xh * group + t / y_tiles : xh / group;
-      const int y0 = (DKDV ? t % y_tiles : t) * CT;
-      const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE;
-      // DKDV: the numbers of the tile's columns travel with it, negated; beyond the sequence
-      // P = exp2(0 - infinity) = 0 and dS = 0.  They are in flight while this warp waits for the stage.
-      float2 v[2];
-      if (DKDV) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          v[i] = make_float2(INFINITY, 0.f);
-          if (y0 + 32 * i + lane < y_len) v[i] = c.delta[(int64_t)yh * c.p.q_rows + y_begin + y0 + 32 * i + lane];
-        }
-      }
-      if (!warp_wait(bar(B_FREE + st), ph ^ 1, abort_flag)) break;
-      if (DKDV) {
-        float2* col = reinterpret_cast<float2*>(smem + L::OFF_COL) + st * CT;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) col[32 * i + lane] = make_float2(-v[i].x, -v[i].y);
-        __syncwarp();
-      }
-      armed = t + 1;
-      if (lane == 0) {
-        mbar_arrive_expect_tx(bar(B_FULL + st), 2 * L::YTILE);
-        for (int s = 0; s < SLABS; ++s) {
-          tma_load_3d(y + s * CT * 128, &maps.y1, 64 * s, yh, y_begin + y0, bar(B_FULL + st));
-          tma_load_3d(y + L::YTILE + s * CT * 128, &maps.y2, 64 * s, yh, y_begin + y0, bar(B_FULL + st));
-        }
-      }
-    }
-    __syncwarp();
-    if (*abort_flag && lane == 0) {
-      // a wait gave up somewhere: let the copies that were started land before the block leaves
-      volatile int never = 0;
-      mbar_wait_limit(bar(B_X), 0, &never, DRAIN_LIMIT_CYCLES);
-      for (int t = armed > L::STAGES ? armed - L::STAGES : 0; t < armed; ++t)
-        mbar_wait_limit(bar(B_FULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
-    }
-  } else if (warp == MMA_WARP) {
-    // ------------------------------------------------------------------ MMA issuer (the whole warp keeps step)
-    bool ok = warp_spin(bar(B_X), 0, abort_flag);
-    for (int t = 0; t < n + NB - 1 && ok; ++t) {
-      if (t < n) {
-        const int st = t % L::STAGES, b = t % NB;
-        const int here = min(CT, y_len - (DKDV ? t % y_tiles : t) * CT), n16 = (here + 15) / 16;
-        const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE;
-        if (!warp_spin(bar(B_FULL + st), (t / L::STAGES) & 1, abort_flag)) { ok = false; break; }
-        __syncwarp();
-        // rows of Y behind the end of the sequence become zero, whatever lies there: they meet weights of
-        // zero in the second products, and give scores of zero in the first
-        if (here < 16 * n16) {
-          zero_rows(y, CT, SLABS, here, lane);
-          zero_rows(y + L::YTILE, CT, SLABS, here, lane);
-        }
-        if (elect_one()) {
-          // S and dP overwrite P and dS of tile t - NB: their products were issued before, by this thread
-          const uint32_t s_col = tmem + (uint32_t)(b * 2 * CT);
-          issue_scores<SLABS, RT, CT>(s_col, sb, y, 16 * n16, d / 16);
-          issue_scores<SLABS, RT, CT>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
-          umma_commit(bar(B_S + b));
-        }
-        __syncwarp();                                          // lanes that poll would hold up the one that issues
-      }
-      const int u = t - (NB - 1);
-      if (u >= 0) {
-        const int st = u % L::STAGES, b = u % NB;
-        const int here = min(CT, y_len - (DKDV ? u % y_tiles : u) * CT), n16 = (here + 15) / 16;
-        const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + (uint32_t)(b * 2 * CT);
-        if (!warp_spin(bar(B_P + b), (u / NB) & 1, abort_flag)) { ok = false; break; }
-        __syncwarp();
-        if (elect_one()) {
-          tc_fence_after();
-          if (DKDV) issue_weighted<CT>(tmem + L::ACC1, s_col, y + L::YTILE, d, n16, u == 0);
-          issue_weighted<CT>(tmem + L::ACC2, s_col + CT, y, d, n16, u == 0);
-          umma_commit(bar(B_FREE + st));
-          if (u == n - 1) umma_commit(bar(B_ACC));
-        }
-        __syncwarp();
-      }
-    }
-    __syncwarp();
-    if (*abort_flag && lane == 0) {
-      volatile int never = 0;
-      umma_commit(bar(B_DRAIN));
-      mbar_wait_limit(bar(B_DRAIN), 0, &never, DRAIN_LIMIT_CYCLES);
-    }
-  } else {
-    // ------------------------------------------------------------------ probabilities and their gradients
-    const int wg = warp >> 2;
-    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t taddr = lanes + (uint32_t)(wg * 2 * CT);
+    const int wg = warp >> 2, in_tile = (warp & 3) * 32 + lane;
+    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * F_WG;
     const float sl2 = c.p.scale * LOG2E;
     const float2 sl2v = make_float2(sl2, sl2);
-    const bool warp_active = x0 + (warp & 3) * 32 < x_len;
-    float2 mine = make_float2(0.f, 0.f);                 // DQ: of this thread's row
-    if (!DKDV && row < x_len) mine = c.delta[(int64_t)xh * c.p.q_rows + at];
-    const float2 nls = make_float2(-mine.x, -mine.x), nde = make_float2(-mine.y, -mine.y);
-    bool ok = true;
-    for (int t = wg; t < n && ok; t += NB) {
-      const int here = min(CT, y_len - (DKDV ? t % y_tiles : t) * CT), nch = (here + 31) / 32;
-      const int st = t % L::STAGES;
-      const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2);   // two columns each
-      if (DKDV && !warp_wait(bar(B_FULL + st), (t / L::STAGES) & 1, abort_flag)) { ok = false; break; }
-      if (!warp_wait(bar(B_S + wg), (t / NB) & 1, abort_flag)) { ok = false; break; }
-      tc_fence_after();
-      if (warp_active) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (i >= nch) break;
-          uint32_t s[32], g[32];
-          tmem_ld32(taddr + (uint32_t)(32 * i), s);
-          tmem_ld32(taddr + (uint32_t)(CT + 32 * i), g);
-          tmem_ld_wait_for(s);
-          tmem_ld_wait_for(g);
-          uint32_t pk[16], dk[16];
-          const int left = here - 32 * i;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            float2 a = nls, b = nde;
-            if (DKDV) {
-              const float4 v = col[16 * i + e];
-              a = make_float2(v.x, v.z);
-              b = make_float2(v.y, v.w);
-            }
-            const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1])), sl2v, a);
-            float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-            if (!DKDV && left < 32) {                      // keys behind the end
-              if (2 * e >= left) p.x = 0.f;
-              if (2 * e + 1 >= left) p.y = 0.f;
-            }
-            const float2 y = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(g[2 * e]), __uint_as_float(g[2 * e + 1])), b));
-            if (DKDV) pk[e] = pack_bf16(p.x, p.y);
-            dk[e] = pack_bf16(y.x, y.y);
-          }
-          if (DKDV) tmem_st16(taddr + (uint32_t)(16 * i), pk);
-          tmem_st16(taddr + (uint32_t)(CT + 16 * i), dk);
+    // the next piece that has keys and rows for this warpgroup; queries without keys are finished on the way
+    auto next = [&](int i) {
+      for (i = find_piece(c, i, total, tiles, c.p.heads, 2 * RT, false, w); i < total;
+           i = find_piece(c, i + gridDim.x, total, tiles, c.p.heads, 2 * RT, false, w)) {
+        if (w.x0 + wg * RT >= w.r.q_len) continue;
+        if (w.r.k_len > 0) break;
+        const int row = w.x0 + wg * RT + in_tile;
+        if (row < w.r.q_len) {
+          const int64_t at = (int64_t)w.r.q_begin + row;
+          bf16* out = static_cast<bf16*>(c.out) + at * c.ldo + (int64_t)w.head * d;
+          for (int e = 0; e < d; e += 8) *reinterpret_cast<uint4*>(out + e) = make_uint4(0u, 0u, 0u, 0u);
+          c.lse[(int64_t)w.head * c.p.q_rows + at] = -INFINITY;
         }
-        tmem_st_wait();
       }
+      return i;
+    };
+    // this thread's query of piece w into tensor memory (the scores that used the last one are complete)
+    auto load_query = [&] {
+      const int row = w.x0 + wg * RT + in_tile;
+      row_to_tmem(taddr + F_O + d, static_cast<const bf16*>(c.q) + ((int64_t)w.r.q_begin + row) * c.ldq + (int64_t)w.head * d, d,
+                  row < w.r.q_len, [](int, const uint32_t(&)[8]) {});
+      tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_P + wg));
-    }
-    if (ok && warp_wait(bar(B_ACC), 0, abort_flag)) {
+      if (lane == 0) mbar_arrive(bar(F_Q + wg));
+    };
+    int g = 0;                                                   // tiles of this warpgroup so far
+    bool ok = true;
+    int i = next(blockIdx.x);
+    if (XT && i < total) load_query();
+    while (i < total && ok) {
+      const Piece now = w;
+      const int n = (now.r.k_len + CT - 1) / CT, row = now.x0 + wg * RT + in_tile;
+      const bool warp_active = now.x0 + wg * RT + (warp & 3) * 32 < now.r.q_len;
+      float m = -INFINITY, l = 0.f;                              // row maximum in use (raw scores), row sum
+      for (int j = 0; j < n; ++j, ++g) {
+        const int b = g & 1, here = min(CT, now.r.k_len - j * CT);
+        const uint32_t s_col = taddr + b * CT;
+        // a warpgroup without rows in the pieces before this one waits for all of them: what bounds the wait is
+        // the limit of the warps that are at work
+        if (!warp_wait(bar(F_S + 2 * wg + b), (g >> 1) & 1, abort_flag, j == 0 ? WAIT_LIMIT_CYCLES << 8 : WAIT_LIMIT_CYCLES)) { ok = false; break; }
+        tc_fence_after();
+        if (warp_active) {
+          uint32_t x[2][32];
+          tmem_ld32(s_col, x[0]);
+          tmem_ld32(s_col + 32, x[1]);
+          tmem_ld_wait_for(x[0]);
+          tmem_ld_wait_for(x[1]);
+          if (here < CT) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (32 * h + e >= here) x[h][e] = 0xff800000u;   // keys behind the end: minus infinity
+          }
+          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              asm("max.f32 %0, %0, %1, %2;" : "+f"(m4[2 * h]) : "f"(__uint_as_float(x[h][e])), "f"(__uint_as_float(x[h][e + 1])));
+              asm("max.f32 %0, %0, %1, %2;" : "+f"(m4[2 * h + 1]) : "f"(__uint_as_float(x[h][e + 2])), "f"(__uint_as_float(x[h][e + 3])));
+            }
+          }
+          const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+          const bool grow = (top - m) * sl2 > 8.f;               // false for NaN and for -infinity over -infinity
+          if (__any_sync(0xffffffffu, grow)) {
+            const float factor = grow ? (m == -INFINITY ? 0.f : ex2_approx((m - top) * sl2)) : 1.f;
+            if (grow) m = top;
+            l *= factor;
+            if (j > 0) {
+              if (!warp_wait(bar(F_PV + 2 * wg + (b ^ 1)), ((g - 1) >> 1) & 1, abort_flag)) { ok = false; break; }
+              tc_fence_after();
+              for (int e = 0; e < d / 16; ++e) {
+                uint32_t o[16];
+                tmem_ld16(taddr + F_O + (uint32_t)(16 * e), o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int f = 0; f < 16; ++f) o[f] = __float_as_uint(__uint_as_float(o[f]) * factor);
+                tmem_st16(taddr + F_O + (uint32_t)(16 * e), o);
+              }
+            }
+          }
+          // p = exp2((s - m) sl2), row sum, P (bf16 pairs) over the scores
+          const float nm = m == -INFINITY ? 0.f : -m * sl2;
+          const float2 nmv = make_float2(nm, nm);
+          float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[h][2 * e]), __uint_as_float(x[h][2 * e + 1])), sl2v, nmv);
+              const float2 p = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+              l2[e & 1] = __fadd2_rn(l2[e & 1], p);
+              pk[e] = pack_bf16(p.x, p.y);
+            }
+            tmem_st16(s_col + (uint32_t)(16 * h), pk);
+          }
+          l2[0] = __fadd2_rn(l2[0], l2[1]);
+          l += l2[0].x + l2[0].y;
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(F_P + 2 * wg + b));
+      }
+      if (!ok) break;
+      i = next(i + gridDim.x);
+      if (XT && i < total) load_query();
+      if (!warp_wait(bar(F_PV + 2 * wg + ((g - 1) & 1)), ((g - 1) >> 1) & 1, abort_flag)) { ok = false; break; }
       tc_fence_after();
       if (warp_active) {
-        for (int i = wg; i < d / 16 * (DKDV ? 2 : 1); i += NB) {
-          const bool second = i >= d / 16;
-          const int cc = 16 * (second ? i - d / 16 : i);
+        const int64_t at = (int64_t)now.r.q_begin + row;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        bf16* out = static_cast<bf16*>(c.out) + at * c.ldo + (int64_t)now.head * d;
+#pragma unroll 2
+        for (int e = 0; e < d / 16; ++e) {
           uint32_t o[16];
-          tmem_ld16(lanes + (second ? L::ACC1 : L::ACC2) + (uint32_t)cc, o);
+          tmem_ld16(taddr + F_O + (uint32_t)(16 * e), o);
           tmem_ld_wait();
-          if (row < x_len) store_16_bf16((second ? g1 : g2) + cc, o, second ? 1.f : c.p.scale);
+          if (row < now.r.q_len) store_16_bf16(out + 16 * e, o, inv);
         }
+        if (row < now.r.q_len) c.lse[(int64_t)now.head * c.p.q_rows + at] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
       }
     }
   }
@@ -609,7 +454,365 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (threadIdx.x == 0 && *abort_flag) atomicExch(c.dev_status, (int)VIT_ERR_TIMEOUT);
   if (warp == MMA_WARP) {
     __syncwarp();
-    tmem_dealloc(tmem, L::TMEM);
+    tmem_dealloc(tmem, TMEM_ALL);
+  }
+}
+
+// ============================================================================================ backward
+// Two kernels of one form.  A piece is a tile of 128 rows X1, X2 of a head, which stays, and tiles of 64 rows
+// Y1, Y2 go by:
+//   S = X1 Y1^T, dP = X2 Y2^T;  P = exp2(S sl2 - lse2), dS = P (dP - delta)
+//   DQ:   X = Q, dout; Y = K, V;  dq += dS Y1.  It comes first and also writes lse2 and delta of its rows.
+//   DKDV: X = K, V; Y = Q, dout of every query head that shares the key head (scores transposed);
+//         dv += P Y2, dk += dS Y1
+// Seven products instead of the five of a single pass, but every gradient is summed in one place in a fixed
+// order.  Two warpgroups take the tiles in turn, each with its own columns of tensor memory for S and dP:
+// while one is in its exp2 phase the tensor core works for the other.  X is in tensor memory (XT) where it
+// fits beside the accumulators: always for DQ, up to d = 80 for DKDV.
+struct BackwardMaps { CUtensorMap x1, x2, y1, y2; };
+
+template <int SLABS, bool DKDV, bool XT>
+struct BackwardCfg {
+  static constexpr int STAGES = SLABS == 1 ? 6 : XT ? 5 : 4;
+  static constexpr uint32_t XTILE = SLABS * RT * 128, YTILE = SLABS * CT * 128;
+  static constexpr uint32_t OFF_Y = XT ? 0 : 2 * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // DKDV: float2 [STAGES][64] -lse2, -delta of the columns
+  static constexpr uint32_t OFF_ROW = OFF_COL + STAGES * CT * 8;                                // DQ: float2 [2][128] of the rows
+  static constexpr uint32_t OFF_BARS = OFF_ROW + 2 * RT * 8;
+  static constexpr uint32_t BYTES = OFF_BARS + 512 + 1024;
+  static_assert(BYTES <= 227 * 1024, "fits an SM");
+};
+// columns: S and dP of the two warpgroups, then the accumulators (d each), then X1 and X2 (d / 2 each)
+constexpr uint32_t B_WG = 2 * CT, B_COLS = 2 * B_WG;
+enum BwdBar : int {
+  B_FULL = 0, B_FREE = B_FULL + 6, B_X = B_FREE + 6, B_XFREE, B_S, B_P = B_S + 2, B_SFREE = B_P + 2, B_ACC = B_SFREE + 2, B_ACCFREE,
+  B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 2
+};
+
+template <int SLABS, bool DKDV, bool XT>
+__global__ void __launch_bounds__(TC_THREADS, 1)
+packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, int total, int tiles) {
+  using L = BackwardCfg<SLABS, DKDV, XT>;
+  extern __shared__ uint8_t smem_raw[];
+  const int d = c.p.d, group = c.p.heads / c.p.kv_heads, x_heads = DKDV ? c.p.kv_heads : c.p.heads;
+  const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t sb = smem_u32(smem);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BARS);
+  auto bar = [&](int i) { return smem_u32(&bars[i]); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(&bars[B_BARS]);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  if (threadIdx.x == 0) {
+    *abort_flag = 0;
+    for (int i = 0; i < B_BARS; ++i)
+      mbar_init(bar(i), i == B_P || i == B_P + 1 ? 4 : i == B_ACCFREE || (XT && i == B_X) ? 8 : 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = uniform(*tmem_slot);
+  const uint32_t acc2 = B_COLS, acc1 = B_COLS + d, x1_col = B_COLS + (DKDV ? 2 : 1) * d, x2_col = x1_col + d / 2;   // dk or dq; dv
+  Piece w;
+  auto find = [&](int i) { return find_piece(c, i, total, tiles, x_heads, RT, DKDV, w); };
+  // tiles of Y that a piece walks over, head after head
+  auto y_tiles_of = [&](const Piece& p) { return ((DKDV ? p.r.q_len : p.r.k_len) + CT - 1) / CT; };
+
+  if (warp == TMA_WARP) {
+    // ------------------------------------------------------------------ producer (the whole warp keeps step)
+    int t0 = 0, pieces = 0, armed = 0;
+    bool ok = true;
+    for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
+      const int y_tiles = y_tiles_of(w), n = DKDV ? group * y_tiles : y_tiles;
+      const int y_begin = DKDV ? w.r.q_begin : w.r.k_begin, y_len = DKDV ? w.r.q_len : w.r.k_len;
+      if (n == 0) continue;
+      if (!XT) {
+        if (!warp_wait(bar(B_XFREE), (pieces & 1) ^ 1, abort_flag)) break;
+        if (lane == 0) {
+          const int row = (DKDV ? w.r.k_begin : w.r.q_begin) + w.x0;
+          mbar_arrive_expect_tx(bar(B_X), 2 * L::XTILE);
+          for (int s = 0; s < SLABS; ++s) {
+            tma_load_3d(sb + s * RT * 128, &maps.x1, 64 * s, w.head, row, bar(B_X));
+            tma_load_3d(sb + L::XTILE + s * RT * 128, &maps.x2, 64 * s, w.head, row, bar(B_X));
+          }
+        }
+        ++pieces;
+      }
+      int yt = 0, yh = DKDV ? w.head * group : w.head / group;
+      for (int t = t0; t < t0 + n; ++t) {
+        const int st = t % L::STAGES, ph = (t / L::STAGES) & 1, y0 = yt * CT;
+        const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE;
+        // DKDV: the numbers of the tile's columns travel with it, negated; beyond the sequence
+        // P = exp2(0 - infinity) = 0 and dS = 0.  They are in flight while this warp waits for the stage.
+        float2 v[2];
+        if (DKDV) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            v[e] = make_float2(INFINITY, 0.f);
+            if (y0 + 32 * e + lane < y_len) v[e] = c.delta[(int64_t)yh * c.p.q_rows + y_begin + y0 + 32 * e + lane];
+          }
+        }
+        if (!warp_wait(bar(B_FREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
+        if (DKDV) {
+          float2* col = reinterpret_cast<float2*>(smem + L::OFF_COL) + st * CT;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) col[32 * e + lane] = make_float2(-v[e].x, -v[e].y);
+          __syncwarp();
+        }
+        armed = t + 1;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar(B_FULL + st), 2 * L::YTILE);
+          for (int s = 0; s < SLABS; ++s) {
+            tma_load_3d(y + s * CT * 128, &maps.y1, 64 * s, yh, y_begin + y0, bar(B_FULL + st));
+            tma_load_3d(y + L::YTILE + s * CT * 128, &maps.y2, 64 * s, yh, y_begin + y0, bar(B_FULL + st));
+          }
+        }
+        if (++yt == y_tiles) { yt = 0; ++yh; }
+      }
+      t0 += n;
+    }
+    __syncwarp();
+    if (*abort_flag && lane == 0) {
+      // a wait gave up somewhere: let the copies that were started land before the block leaves
+      volatile int never = 0;
+      if (!XT && pieces) mbar_wait_limit(bar(B_X), (pieces - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
+      for (int t = armed > L::STAGES ? armed - L::STAGES : 0; t < armed; ++t)
+        mbar_wait_limit(bar(B_FULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
+    }
+  } else if (warp >= MMA_WARP) {
+    // ------------------------------------------------------------------ MMA issuers (whole warps keep step): one of the
+    // scores, one of the second products
+    const bool scores = warp == MMA_WARP;
+    int t0 = 0, pieces = 0;
+    uint32_t phase = 0;                                          // bit b: parity of the next wait for warpgroup b's columns
+    bool ok = true;
+    for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
+      const int y_tiles = y_tiles_of(w), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
+      if (n == 0) continue;
+      if (scores && !warp_spin(bar(B_X), pieces & 1, abort_flag)) break;
+      const int last = y_len - (y_tiles - 1) * CT;               // rows of a head's last tile
+      int yt = 0;                                                // tile of its head
+      for (int t = 0; t < n; ++t) {
+        const int st = (t0 + t) % L::STAGES, b = t & 1, here = yt == y_tiles - 1 ? last : CT, n16 = (here + 15) / 16;
+        const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + b * B_WG;
+        if (++yt == y_tiles) yt = 0;
+        if (scores) {
+          if (!warp_spin(bar(B_FULL + st), ((t0 + t) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
+          // rows of Y behind the end of the sequence become zero, whatever lies there: they meet weights of
+          // zero in the second products, and give scores of zero in the first
+          if (here < 16 * n16) {
+            zero_rows(y, CT, SLABS, here, lane);
+            zero_rows(y + L::YTILE, CT, SLABS, here, lane);
+          }
+          // S and dP overwrite P and dS of tile t - 2, once their products are complete
+          if (!warp_spin(bar(B_SFREE + b), (phase >> b & 1) ^ 1, abort_flag)) { ok = false; break; }
+          phase ^= 1u << b;
+          if (elect_one()) {
+            tc_fence_after();
+            if (XT) {
+              issue_scores_ts<SLABS>(s_col, tmem + x1_col, y, 16 * n16, d / 16);
+              issue_scores_ts<SLABS>(s_col + CT, tmem + x2_col, y + L::YTILE, 16 * n16, d / 16);
+            } else {
+              issue_scores_ss<SLABS>(s_col, sb, y, 16 * n16, d / 16);
+              issue_scores_ss<SLABS>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
+            }
+            umma_commit(bar(B_S + b));
+            if (t == n - 1) umma_commit(bar(B_XFREE));
+          }
+        } else {
+          if (!warp_spin(bar(B_P + b), phase >> b & 1, abort_flag)) { ok = false; break; }
+          phase ^= 1u << b;
+          // the accumulators of the last piece have been read
+          if (t == 0 && !warp_spin(bar(B_ACCFREE), (pieces & 1) ^ 1, abort_flag)) { ok = false; break; }
+          if (elect_one()) {
+            tc_fence_after();
+            if (DKDV) issue_weighted(tmem + acc1, s_col, y + L::YTILE, d, n16, t == 0);
+            issue_weighted(tmem + acc2, s_col + CT, y, d, n16, t == 0);
+            umma_commit(bar(B_SFREE + b));
+            umma_commit(bar(B_FREE + st));
+            if (t == n - 1) umma_commit(bar(B_ACC));
+          }
+        }
+        __syncwarp();                                            // lanes that poll would hold up the one that issues
+      }
+      t0 += n;
+      ++pieces;
+    }
+    __syncwarp();
+    if (*abort_flag && lane == 0) {
+      volatile int never = 0;
+      umma_commit(bar(B_DRAIN + warp - MMA_WARP));
+      mbar_wait_limit(bar(B_DRAIN + warp - MMA_WARP), 0, &never, DRAIN_LIMIT_CYCLES);
+    }
+  } else {
+    // ------------------------------------------------------------------ probabilities and their gradients
+    const int wg = warp >> 2, in_tile = (warp & 3) * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t taddr = lanes + wg * B_WG;
+    const float sl2 = c.p.scale * LOG2E;
+    const float2 sl2v = make_float2(sl2, sl2);
+    int pieces = 0, t0 = 0;
+    uint32_t s_phase = 0;
+    bool ok = true;
+    auto grad1 = [&](const Piece& p, int64_t at) { return static_cast<bf16*>(c.dv) + at * c.lddv + (int64_t)p.head * d; };
+    auto grad2 = [&](const Piece& p, int64_t at) {
+      return DKDV ? static_cast<bf16*>(c.dk) + at * c.lddk + (int64_t)p.head * d : static_cast<bf16*>(c.dq) + at * c.lddq + (int64_t)p.head * d;
+    };
+    // the next piece with something to walk over; rows that nothing meets get gradients of zero on the way
+    auto next = [&](int i) {
+      for (i = find(i); i < total; i = find(i + gridDim.x)) {
+        if (y_tiles_of(w) > 0) break;
+        const int row = w.x0 + in_tile;
+        const int64_t at = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row;
+        if (wg == 0 && row < (DKDV ? w.r.k_len : w.r.q_len))
+          for (int e = 0; e < d; e += 8) {
+            *reinterpret_cast<uint4*>(grad2(w, at) + e) = make_uint4(0u, 0u, 0u, 0u);
+            if (DKDV) *reinterpret_cast<uint4*>(grad1(w, at) + e) = make_uint4(0u, 0u, 0u, 0u);
+          }
+      }
+      return i;
+    };
+    // this thread's row of X1 (first warpgroup) or X2 (second) of piece w into tensor memory; the second
+    // warpgroup of DQ holds dout and takes its product with out on the way
+    auto load_x = [&] {
+      const int row = w.x0 + in_tile;
+      const bool there = row < (DKDV ? w.r.k_len : w.r.q_len);
+      const int64_t at = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row;
+      const bf16* src = wg == 0 ? static_cast<const bf16*>(DKDV ? c.k : c.q) + at * (DKDV ? c.ldk : c.ldq)
+                                : static_cast<const bf16*>(DKDV ? c.v : c.dout) + at * (DKDV ? c.ldv : c.lddo);
+      src += (int64_t)w.head * d;
+      const uint32_t to = lanes + (wg == 0 ? x1_col : x2_col);
+      if (DKDV || wg == 0) {
+        row_to_tmem(to, src, d, there, [](int, const uint32_t(&)[8]) {});
+      } else {
+        const uint4* o = reinterpret_cast<const uint4*>(static_cast<const bf16*>(c.out) + at * c.ldo + (int64_t)w.head * d);
+        const float lse = there ? c.lse[(int64_t)w.head * c.p.q_rows + at] : 0.f;
+        float delta = 0.f;
+        row_to_tmem(to, src, d, there, [&](int g, const uint32_t(&v)[8]) {
+          if (!there) return;
+          const uint4 a = o[2 * g], b = o[2 * g + 1];
+          const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e) delta = dot2(u[e], v[e], delta);
+        });
+        const float2 mine = make_float2(lse * LOG2E, delta);
+        reinterpret_cast<float2*>(smem + L::OFF_ROW)[(pieces & 1) * RT + in_tile] = mine;
+        if (there) c.delta[(int64_t)w.head * c.p.q_rows + at] = mine;
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_X));
+    };
+    int i = next(blockIdx.x);
+    if (XT && i < total) load_x();
+    while (i < total) {
+      const Piece now = w;
+      const int y_tiles = y_tiles_of(now), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? now.r.q_len : now.r.k_len;
+      const int x_len = DKDV ? now.r.k_len : now.r.q_len, row = now.x0 + in_tile;
+      const bool warp_active = now.x0 + (warp & 3) * 32 < x_len;
+      float2 nls = make_float2(0.f, 0.f), nde = nls;             // DQ: of this thread's row
+      if (!DKDV) {
+        if (!warp_wait(bar(B_X), pieces & 1, abort_flag)) break;
+        const float2 mine = reinterpret_cast<const float2*>(smem + L::OFF_ROW)[(pieces & 1) * RT + in_tile];
+        nls = make_float2(-mine.x, -mine.x);
+        nde = make_float2(-mine.y, -mine.y);
+      }
+      int yt = wg % y_tiles;                                     // DKDV: tile of its head
+      for (int t = wg; t < n; t += 2) {
+        const int here = (DKDV ? yt : t) == y_tiles - 1 ? y_len - (y_tiles - 1) * CT : CT, nch = (here + 31) / 32;
+        const int st = (t0 + t) % L::STAGES;
+        const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2);   // two columns each
+        if (DKDV) {
+          yt = (yt + 2) % y_tiles;
+          if (!warp_wait(bar(B_FULL + st), ((t0 + t) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
+        }
+        if (!warp_wait(bar(B_S + wg), s_phase, abort_flag)) { ok = false; break; }
+        s_phase ^= 1;
+        tc_fence_after();
+        if (warp_active) {
+          uint32_t s[2][32], g[2][32];
+          tmem_ld32(taddr, s[0]);
+          tmem_ld32(taddr + CT, g[0]);
+          tmem_ld_wait_for(s[0]);
+          tmem_ld_wait_for(g[0]);
+          if (nch > 1) {
+            tmem_ld32(taddr + 32, s[1]);
+            tmem_ld32(taddr + CT + 32, g[1]);
+          }
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (h >= nch) break;
+            if (h == 1) {
+              tmem_ld_wait_for(s[1]);
+              tmem_ld_wait_for(g[1]);
+            }
+            uint32_t pk[16], dk[16];
+            const int left = here - 32 * h;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float2 a = nls, b = nde;
+              if (DKDV) {
+                const float4 v = col[16 * h + e];
+                a = make_float2(v.x, v.z);
+                b = make_float2(v.y, v.w);
+              }
+              const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[h][2 * e]), __uint_as_float(s[h][2 * e + 1])), sl2v, a);
+              float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+              if (!DKDV && left < 32) {                          // keys behind the end
+                if (2 * e >= left) p.x = 0.f;
+                if (2 * e + 1 >= left) p.y = 0.f;
+              }
+              const float2 y = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(g[h][2 * e]), __uint_as_float(g[h][2 * e + 1])), b));
+              if (DKDV) pk[e] = pack_bf16(p.x, p.y);
+              dk[e] = pack_bf16(y.x, y.y);
+            }
+            if (DKDV) tmem_st16(taddr + (uint32_t)(16 * h), pk);
+            tmem_st16(taddr + (uint32_t)(CT + 16 * h), dk);
+          }
+          tmem_st_wait();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(B_P + wg));
+      }
+      if (!ok) break;
+      t0 += n;
+      ++pieces;
+      i = next(i + gridDim.x);
+      if (XT && i < total) {
+        // every score of the last piece is complete: its X may be overwritten
+        if (!warp_wait(bar(B_XFREE), (pieces - 1) & 1, abort_flag)) break;
+        tc_fence_after();
+        load_x();
+      }
+      if (!warp_wait(bar(B_ACC), (pieces - 1) & 1, abort_flag)) break;
+      tc_fence_after();
+      if (warp_active) {
+        const int64_t at = (int64_t)(DKDV ? now.r.k_begin : now.r.q_begin) + row;
+        for (int e = wg; e < d / 16 * (DKDV ? 2 : 1); e += 2) {
+          const bool second = e >= d / 16;
+          const int cc = 16 * (second ? e - d / 16 : e);
+          uint32_t o[16];
+          tmem_ld16(lanes + (second ? acc1 : acc2) + (uint32_t)cc, o);
+          tmem_ld_wait();
+          if (row < x_len) store_16_bf16((second ? grad1(now, at) : grad2(now, at)) + cc, o, second ? 1.f : c.p.scale);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(B_ACCFREE));
+    }
+  }
+  // ---------------------------------------------------------------------- teardown
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (threadIdx.x == 0 && *abort_flag) atomicExch(c.dev_status, (int)VIT_ERR_TIMEOUT);
+  if (warp == MMA_WARP) {
+    __syncwarp();
+    tmem_dealloc(tmem, TMEM_ALL);
   }
 }
 
@@ -640,27 +843,29 @@ bool encode_heads(CUtensorMap* tm, const void* base, int64_t rows, int heads, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int SLABS>
+template <int SLABS, bool XT>
 cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
-  using L = ForwardSmem<SLABS>;
+  using L = ForwardCfg<SLABS, XT>;
   ForwardMaps m;
   if (!encode_heads(&m.q, c.q, c.p.q_rows, c.p.heads, c.p.d, c.ldq, RT)) return cudaErrorInvalidValue;
   if (c.p.k_rows > 0) {
-    if (!encode_heads(&m.k, c.k, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldk, RT)) return cudaErrorInvalidValue;
-    if (!encode_heads(&m.v, c.v, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldv, RT)) return cudaErrorInvalidValue;
+    if (!encode_heads(&m.k, c.k, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldk, CT)) return cudaErrorInvalidValue;
+    if (!encode_heads(&m.v, c.v, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldv, CT)) return cudaErrorInvalidValue;
   } else {
     m.k = m.v = m.q;                                   // no keys at all: never used
   }
   static PerDeviceFlag done;
-  if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_tc_kernel<SLABS>, (int)L::BYTES)) return e;
-  const int tiles = (c.p.max_q + RT - 1) / RT;
-  packed_forward_tc_kernel<SLABS><<<c.p.sequences * c.p.heads * tiles, FWD_THREADS, L::BYTES, s>>>(m, c);
+  if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_tc_kernel<SLABS, XT>, (int)L::BYTES)) return e;
+  const int sms = current_device_sm_count();
+  if (sms < 1) return cudaErrorInvalidDevice;
+  const int tiles = (c.p.max_q + 2 * RT - 1) / (2 * RT), total = c.p.sequences * c.p.heads * tiles;
+  packed_forward_tc_kernel<SLABS, XT><<<total < sms ? total : sms, TC_THREADS, L::BYTES, s>>>(m, c, total, tiles);
   return cudaGetLastError();
 }
 
-template <int SLABS, bool DKDV, int NB>
+template <int SLABS, bool DKDV, bool XT>
 cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
-  using L = BackwardCfg<SLABS, DKDV, NB>;
+  using L = BackwardCfg<SLABS, DKDV, XT>;
   BackwardMaps m;
   const void *x1 = DKDV ? c.k : c.q, *x2 = DKDV ? c.v : c.dout, *y1 = DKDV ? c.q : c.k, *y2 = DKDV ? c.dout : c.v;
   const int64_t lx1 = DKDV ? c.ldk : c.ldq, lx2 = DKDV ? c.ldv : c.lddo, ly1 = DKDV ? c.ldq : c.ldk, ly2 = DKDV ? c.lddo : c.ldv;
@@ -673,22 +878,28 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
     m.y1 = m.y2 = m.x1;
   }
   static PerDeviceFlag done;
-  if (cudaError_t e = ensure_dynamic_smem(done, packed_backward_tc_kernel<SLABS, DKDV, NB>, (int)L::BYTES)) return e;
-  const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT;
-  packed_backward_tc_kernel<SLABS, DKDV, NB><<<c.p.sequences * xh * tiles, L::THREADS, L::BYTES, s>>>(m, c);
+  if (cudaError_t e = ensure_dynamic_smem(done, packed_backward_tc_kernel<SLABS, DKDV, XT>, (int)L::BYTES)) return e;
+  const int sms = current_device_sm_count();
+  if (sms < 1) return cudaErrorInvalidDevice;
+  const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT, total = c.p.sequences * xh * tiles;
+  packed_backward_tc_kernel<SLABS, DKDV, XT><<<total < sms ? total : sms, TC_THREADS, L::BYTES, s>>>(m, c, total, tiles);
   return cudaGetLastError();
 }
 
 }  // namespace
 
+// Columns of tensor memory decide where a piece's rows are held: 2 x 64 + d + d / 2 of a warpgroup's 256 in
+// the forward pass, 256 + 2 d + d of 512 for dk and dv, 256 + d + d for dq.
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s) {
-  return c.p.d <= 64 ? launch_forward<1>(c, s) : launch_forward<2>(c, s);
+  if (c.p.d <= 64) return launch_forward<1, true>(c, s);
+  return c.p.d <= 80 ? launch_forward<2, true>(c, s) : launch_forward<2, false>(c, s);
 }
 cudaError_t launch_attention_packed_dkdv_bf16(const PackedCall& c, cudaStream_t s) {
-  return c.p.d <= 64 ? launch_backward<1, true, 1>(c, s) : launch_backward<2, true, 2>(c, s);
+  if (c.p.d <= 64) return launch_backward<1, true, true>(c, s);
+  return c.p.d <= 80 ? launch_backward<2, true, true>(c, s) : launch_backward<2, true, false>(c, s);
 }
 cudaError_t launch_attention_packed_dq_bf16(const PackedCall& c, cudaStream_t s) {
-  return c.p.d <= 64 ? launch_backward<1, false, 1>(c, s) : launch_backward<2, false, 2>(c, s);
+  return c.p.d <= 64 ? launch_backward<1, false, true>(c, s) : launch_backward<2, false, true>(c, s);
 }
 
 }  // namespace vit

@@ -886,9 +886,11 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
   c.delta = static_cast<float2*>(ws);
   c.dev_status = h->dev_status;
   const bool b16 = dtype == VIT_BF16;
-  if (p.q_rows > 0 && p.max_q > 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta(c, b16, s));
-  if (p.k_rows > 0 && p.max_k > 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dkdv(c, b16, s));
-  if (p.q_rows > 0 && p.max_q > 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dq(c, b16, s));
+  const bool queries = p.q_rows > 0 && p.max_q > 0, keys = p.k_rows > 0 && p.max_k > 0;
+  // dq comes first: in bf16 mode its kernel also leaves lse and delta of every row for the other one
+  if (!b16 && queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta_f32(c, s));
+  if (queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, b16 ? launch_attention_packed_dq_bf16(c, s) : launch_attention_packed_dq_f32(c, s));
+  if (keys) VIT_LAUNCH(h, VIT_PROF_ATTENTION, b16 ? launch_attention_packed_dkdv_bf16(c, s) : launch_attention_packed_dkdv_f32(c, s));
   return VIT_OK;
 }
 

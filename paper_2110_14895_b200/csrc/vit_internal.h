@@ -186,12 +186,12 @@ struct PackedCall {
 };
 cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s);
-cudaError_t launch_attention_packed_dkdv_bf16(const PackedCall& c, cudaStream_t s);
+// the kernels of the backward pass, in this order; delta is part of dq in bf16 mode
+cudaError_t launch_attention_delta_f32(const PackedCall& c, cudaStream_t s);
+cudaError_t launch_attention_packed_dq_f32(const PackedCall& c, cudaStream_t s);
+cudaError_t launch_attention_packed_dkdv_f32(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_dq_bf16(const PackedCall& c, cudaStream_t s);
-// the three kernels of the backward pass
-cudaError_t launch_attention_delta(const PackedCall& c, bool act_bf16, cudaStream_t s);
-cudaError_t launch_attention_packed_dkdv(const PackedCall& c, bool act_bf16, cudaStream_t s);
-cudaError_t launch_attention_packed_dq(const PackedCall& c, bool act_bf16, cudaStream_t s);
+cudaError_t launch_attention_packed_dkdv_bf16(const PackedCall& c, cudaStream_t s);
 
 cudaError_t launch_wait_probe(long long limit_cycles, int* dev_status, cudaStream_t s);
 // *snapshot = atomic exchange of *status with 0, on stream s
