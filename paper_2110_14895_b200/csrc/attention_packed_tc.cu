@@ -32,6 +32,7 @@ constexpr int RT = 128;                                // rows of a tile of scor
 constexpr int CT = 64;                                 // columns of a tile of scores
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
 constexpr long long DRAIN_LIMIT_CYCLES = 1ll << 24;    // teardown after a failed wait: ~10 ms
+constexpr long long LONG_WAIT_CYCLES = WAIT_LIMIT_CYCLES << 8;   // for other pieces, whose own waits are bounded
 
 // Shared-memory matrix descriptor of a 128-byte-swizzled slab (rows of 128 bytes, groups of 8 rows 1024
 // bytes apart).  lbo: distance of the slabs of 64 columns, for an operand whose rows are the summed index
@@ -128,36 +129,70 @@ __device__ __forceinline__ void issue_weighted(uint32_t d_tmem, uint32_t p_tmem,
   for (int k = 0; k < CT / 16; ++k)
     if (k < ksteps) umma_bf16_ts(d_tmem, p_tmem + (uint32_t)(8 * k), yd + (uint64_t)(k * 128), id, first && k == 0 ? 0u : 1u);
 }
-// A row of d channels from global memory into tensor memory, 16 channels (8 columns) at a time; rows that are
-// not there become zero.  `each` sees the words on their way.
-template <typename Each>
-__device__ __forceinline__ void row_to_tmem(uint32_t taddr, const bf16* src, int d, bool there, Each each) {
-#pragma unroll 2
-  for (int g = 0; g < d / 16; ++g) {
-    uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-    if (there) {
-      a = reinterpret_cast<const uint4*>(src)[2 * g];
-      b = reinterpret_cast<const uint4*>(src)[2 * g + 1];
+// The 16 channels 16 g ... of a row of a swizzled tile of 128 rows in shared memory
+__device__ __forceinline__ void read_16(uint32_t (&w)[8], uint32_t tile, int row, int g) {
+  const uint32_t at = tile + (uint32_t)((g >> 2) * RT * 128 + row * 128);
+  const int c = 2 * (g & 3), x = row & 7;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at + (uint32_t)((c ^ x) << 4)));
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "r"(at + (uint32_t)(((c + 1) ^ x) << 4)));
+}
+// A row of a tile from shared memory into tensor memory.  Rows behind the end of a sequence bring whatever lies
+// there: every row of a product depends on its own row of this operand only.
+template <int SLABS>
+__device__ __forceinline__ void row_to_tmem(uint32_t taddr, uint32_t tile, int row, int d) {
+#pragma unroll
+  for (int g = 0; g < 4 * SLABS; ++g)
+    if (g < d / 16) {
+      uint32_t w[8];
+      read_16(w, tile, row, g);
+      tmem_st8(taddr + (uint32_t)(8 * g), w);
     }
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    tmem_st8(taddr + (uint32_t)(8 * g), w);
-    each(g, w);
-  }
 }
 __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float acc) {
   acc = fmaf(__uint_as_float(a << 16), __uint_as_float(b << 16), acc);
   return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), acc);
 }
 
+// 64 accumulator columns of a row (those below d) times a factor to global memory: all loads, one wait, the stores
+__device__ __forceinline__ void store_row(bf16* dst, uint32_t taddr, int left, float by, bool there) {
+  uint32_t o[4][16];
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (16 * e < left) tmem_ld16(taddr + (uint32_t)(16 * e), o[e]);
+  tmem_ld_wait();
+#pragma unroll
+  for (int e = 0; e < 4; ++e) asm volatile("" : "+r"(o[e][0]), "+r"(o[e][1]), "+r"(o[e][2]), "+r"(o[e][3]), "+r"(o[e][4]), "+r"(o[e][5]),
+      "+r"(o[e][6]), "+r"(o[e][7]), "+r"(o[e][8]), "+r"(o[e][9]), "+r"(o[e][10]), "+r"(o[e][11]), "+r"(o[e][12]), "+r"(o[e][13]),
+      "+r"(o[e][14]), "+r"(o[e][15]));                           // nothing reads them before the wait
+  if (!there) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (16 * e < left) store_16_bf16(dst + 16 * e, o[e], by);
+}
+
+// The sequences' offsets are kept in shared memory where they fit: every role of a block looks at them for every piece.
+constexpr int MAX_STAGED = 1024;
+constexpr uint32_t OFFSETS_BYTES = 2 * (MAX_STAGED + 1) * 4 + 8;
+__device__ __forceinline__ void stage_offsets(vit_attention_problem& p, int32_t* to) {
+  if (p.sequences > MAX_STAGED) return;
+  for (int i = threadIdx.x; i <= p.sequences; i += (int)blockDim.x) {
+    to[i] = p.q_offsets[i];
+    to[MAX_STAGED + 1 + i] = p.k_offsets[i];
+  }
+  p.q_offsets = to;
+  p.k_offsets = to + MAX_STAGED + 1;
+}
+
 // A piece of work: `span` rows of one head of one sequence.
 struct Piece { int head, x0; SeqRange r; };
 // The first piece from number i on (in steps of the grid) whose rows exist; i = total if there is none.
-__device__ __forceinline__ int find_piece(const PackedCall& c, int i, int total, int tiles, int heads, int span, bool of_keys, Piece& w) {
+__device__ __forceinline__ int find_piece(const vit_attention_problem& p, int* status, int i, int total, int tiles, int heads, int span,
+                                          bool of_keys, Piece& w) {
   for (; i < total; i += (int)gridDim.x) {
-    const int seq = i / tiles / heads;
-    w.head = i / tiles % heads;
-    w.x0 = i % tiles * span;
-    if (seq_range(c.p, seq, w.r, c.dev_status) && w.x0 < (of_keys ? w.r.k_len : w.r.q_len)) return i;
+    const unsigned hs = (unsigned)i / (unsigned)tiles, seq = hs / (unsigned)heads;
+    w.head = (int)(hs - seq * (unsigned)heads);
+    w.x0 = (int)((unsigned)i - hs * (unsigned)tiles) * span;
+    if (seq_range(p, (int)seq, w.r, status) && w.x0 < (of_keys ? w.r.k_len : w.r.q_len)) return i;
   }
   return total;
 }
@@ -174,17 +209,21 @@ template <int SLABS, bool XT>
 struct ForwardCfg {
   static constexpr int STAGES = SLABS == 1 ? 6 : 4;
   static constexpr uint32_t TILE = SLABS * CT * 128, QTILE = SLABS * RT * 128;
-  static constexpr uint32_t OFF_K = XT ? 0 : 2 * QTILE, OFF_V = OFF_K + STAGES * TILE, OFF_BARS = OFF_V + STAGES * TILE;
-  static constexpr uint32_t BYTES = OFF_BARS + 512 + 1024;
+  static constexpr uint32_t OFF_K = 2 * QTILE, OFF_V = OFF_K + STAGES * TILE, OFF_BARS = OFF_V + STAGES * TILE, OFF_SEQ = OFF_BARS + 512;
+  static constexpr uint32_t BYTES = OFF_SEQ + OFFSETS_BYTES + 1024;
   static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
-constexpr int TC_THREADS = 352, MMA_WARP = 8 /* two */, TMA_WARP = 10;
+constexpr int TC_THREADS = 384, MMA_WARP = 8 /* two */, TMA_WARP = 10;   // warp 11 only hands its registers on
+// 168 registers a thread at launch (384 x 168 = 64512): the score warps take 200, the other four warps keep 96
+// (256 x 200 + 128 x 96 = 63488)
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 200;"); }
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 96;"); }
 constexpr uint32_t TMEM_ALL = 512;
 // columns of a warpgroup (256): two tiles of scores, the accumulator (d), the queries (d / 2)
 constexpr uint32_t F_WG = 256, F_O = 2 * CT;
 enum FwdBar : int {
-  F_KFULL = 0, F_KFREE = F_KFULL + 6, F_VFULL = F_KFREE + 6, F_VFREE = F_VFULL + 6, F_Q = F_VFREE + 6 /* [wg], or [0] for both */,
-  F_QFREE = F_Q + 2, F_S = F_QFREE + 1 /* [wg][tile parity] */, F_P = F_S + 4, F_PV = F_P + 4, F_DRAIN = F_PV + 4 /* [MMA warp] */, F_BARS = F_DRAIN + 2
+  F_KFULL = 0, F_KFREE = F_KFULL + 6, F_VFULL = F_KFREE + 6, F_VFREE = F_VFULL + 6, F_QFULL = F_VFREE + 6 /* [wg] shared memory */,
+  F_QFREE = F_QFULL + 2, F_Q = F_QFREE + 2 /* [wg] tensor memory */, F_S = F_Q + 2 /* [wg][tile parity] */, F_P = F_S + 4, F_PV = F_P + 4, F_DRAIN = F_PV + 4 /* [MMA warp] */, F_BARS = F_DRAIN + 2
 };
 
 template <int SLABS, bool XT>
@@ -203,36 +242,42 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < F_BARS; ++i) {
-      const bool stage_free = (i >= F_KFREE && i < F_KFREE + 6) || (i >= F_VFREE && i < F_VFREE + 6) || i == F_QFREE;   // by both MMA warps
-      const bool by_warps = (i >= F_P && i < F_P + 4) || (XT && (i == F_Q || i == F_Q + 1));
+      const bool stage_free = (i >= F_KFREE && i < F_KFREE + 6) || (i >= F_VFREE && i < F_VFREE + 6);   // by both MMA warps
+      const bool by_warps = (i >= F_P && i < F_P + 4) || i == F_Q || i == F_Q + 1 || (XT && (i == F_QFREE || i == F_QFREE + 1));
       mbar_init(bar(i), stage_free ? 2 : by_warps ? 4 : 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
+  vit_attention_problem p = c.p;
+  stage_offsets(p, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
   Piece w;
+  auto find = [&](int i) { return find_piece(p, c.dev_status, i, total, tiles, p.heads, 2 * RT, false, w); };
 
-  if (warp == TMA_WARP) {
+  if (warp >= MMA_WARP) give_registers();
+  else take_registers();
+  if (warp > TMA_WARP) {
+  } else if (warp == TMA_WARP) {
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0) {
-      int t = 0, pieces = 0, armed_k = 0, armed_v = 0;           // tiles and pieces so far
+      int t = 0, q_tiles[2] = {0, 0}, armed_k = 0, armed_v = 0;   // tiles of keys and of queries so far
       bool ok = true;
-      for (int i = find_piece(c, blockIdx.x, total, tiles, c.p.heads, 2 * RT, false, w); i < total && ok;
-           i = find_piece(c, i + gridDim.x, total, tiles, c.p.heads, 2 * RT, false, w)) {
+      for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
         const int n = (w.r.k_len + CT - 1) / CT, kv = w.head / group;
         if (n == 0) continue;
-        if (!XT) {
-          if (!mbar_wait(bar(F_QFREE), (pieces & 1) ^ 1, abort_flag)) break;
-          mbar_arrive_expect_tx(bar(F_Q), 2 * L::QTILE);
-          for (int s = 0; s < 2 * SLABS; ++s)                    // both tiles; rows behind the sequence are not used
-            tma_load_3d(sb + s * RT * 128, &maps.q, 64 * (s % SLABS), w.head, w.r.q_begin + w.x0 + s / SLABS * RT, bar(F_Q));
-          ++pieces;
+        for (int h = 0; h < 2 && ok; ++h) {
+          if (w.x0 + h * RT >= w.r.q_len) break;
+          if (!mbar_wait_limit(bar(F_QFREE + h), (q_tiles[h] & 1) ^ 1, abort_flag, LONG_WAIT_CYCLES)) { ok = false; break; }
+          mbar_arrive_expect_tx(bar(F_QFULL + h), L::QTILE);
+          ++q_tiles[h];
+          for (int s = 0; s < SLABS; ++s)
+            tma_load_3d(sb + h * L::QTILE + s * RT * 128, &maps.q, 64 * s, w.head, w.r.q_begin + w.x0 + h * RT, bar(F_QFULL + h));
         }
-        for (int j = 0; j < n; ++j, ++t) {
+        for (int j = 0; j < n && ok; ++j, ++t) {
           const int st = t % L::STAGES, ph = (t / L::STAGES) & 1, krow = w.r.k_begin + j * CT;
           if (!mbar_wait(bar(F_KFREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
           mbar_arrive_expect_tx(bar(F_KFULL + st), L::TILE);
@@ -247,7 +292,8 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       if (*abort_flag) {
         // a wait gave up somewhere: let the copies that were started land before the block leaves
         volatile int never = 0;
-        if (!XT && pieces) mbar_wait_limit(bar(F_Q), (pieces - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
+        for (int h = 0; h < 2; ++h)
+          if (q_tiles[h]) mbar_wait_limit(bar(F_QFULL + h), (q_tiles[h] - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
         for (int i = armed_k > L::STAGES ? armed_k - L::STAGES : 0; i < armed_k; ++i)
           mbar_wait_limit(bar(F_KFULL + i % L::STAGES), (i / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
         for (int i = armed_v > L::STAGES ? armed_v - L::STAGES : 0; i < armed_v; ++i)
@@ -260,8 +306,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     const uint32_t base = tmem + h * F_WG;
     int t0 = 0, g = 0, seen = 0;                                 // tiles of keys so far, those of this warpgroup, pieces
     bool ok = true;
-    for (int i = find_piece(c, blockIdx.x, total, tiles, c.p.heads, 2 * RT, false, w); i < total && ok;
-         i = find_piece(c, i + gridDim.x, total, tiles, c.p.heads, 2 * RT, false, w)) {
+    for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
       const int n = (w.r.k_len + CT - 1) / CT;
       if (n == 0) continue;
       const bool mine = w.x0 + h * RT < w.r.q_len;               // else the stages are passed on only
@@ -270,7 +315,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
           const int st = (t0 + j) % L::STAGES, n16 = (min(CT, w.r.k_len - j * CT) + 15) / 16, b = (g + j) & 1;
           const uint32_t ks = sb + L::OFF_K + st * L::TILE;
           if (!warp_spin(bar(F_KFULL + st), ((t0 + j) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
-          if (j == 0 && (mine || !XT) && !warp_spin(bar(F_Q + (XT ? h : 0)), seen & 1, abort_flag)) { ok = false; break; }
+          if (j == 0 && mine && !warp_spin(bar((XT ? F_Q : F_QFULL) + h), seen & 1, abort_flag)) { ok = false; break; }
           if (elect_one()) {
             if (mine) {
               // the scores overwrite P of tile j - 2: its product was issued before, by this warp
@@ -278,9 +323,9 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
               if (XT) issue_scores_ts<SLABS>(base + b * CT, base + F_O + d, ks, 16 * n16, d / 16);
               else issue_scores_ss<SLABS>(base + b * CT, sb + h * L::QTILE, ks, 16 * n16, d / 16);
               umma_commit(bar(F_S + 2 * h + b));
+              if (!XT && j == n - 1) umma_commit(bar(F_QFREE + h));
             }
             umma_commit(bar(F_KFREE + st));
-            if (!XT && j == n - 1) umma_commit(bar(F_QFREE));
           }
           __syncwarp();                                          // lanes that poll would hold up the one that issues
         }
@@ -304,8 +349,10 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
         }
       }
       t0 += n;
-      if (mine || !XT) ++seen;
-      if (mine) g += n;
+      if (mine) {
+        ++seen;
+        g += n;
+      }
     }
     __syncwarp();
     if (*abort_flag && lane == 0) {
@@ -321,8 +368,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     const float2 sl2v = make_float2(sl2, sl2);
     // the next piece that has keys and rows for this warpgroup; queries without keys are finished on the way
     auto next = [&](int i) {
-      for (i = find_piece(c, i, total, tiles, c.p.heads, 2 * RT, false, w); i < total;
-           i = find_piece(c, i + gridDim.x, total, tiles, c.p.heads, 2 * RT, false, w)) {
+      for (i = find(i); i < total; i = find(i + gridDim.x)) {
         if (w.x0 + wg * RT >= w.r.q_len) continue;
         if (w.r.k_len > 0) break;
         const int row = w.x0 + wg * RT + in_tile;
@@ -335,20 +381,23 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       }
       return i;
     };
-    // this thread's query of piece w into tensor memory (the scores that used the last one are complete)
+    int g = 0, seen = 0;                                         // tiles and pieces of this warpgroup so far
+    // this thread's query of the next piece into tensor memory (the scores that used the last one are complete)
     auto load_query = [&] {
-      const int row = w.x0 + wg * RT + in_tile;
-      row_to_tmem(taddr + F_O + d, static_cast<const bf16*>(c.q) + ((int64_t)w.r.q_begin + row) * c.ldq + (int64_t)w.head * d, d,
-                  row < w.r.q_len, [](int, const uint32_t(&)[8]) {});
+      if (!warp_wait(bar(F_QFULL + wg), seen & 1, abort_flag, LONG_WAIT_CYCLES)) return false;
+      ++seen;
+      row_to_tmem<SLABS>(taddr + F_O + d, sb + wg * L::QTILE, in_tile, d);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(F_Q + wg));
+      if (lane == 0) {
+        mbar_arrive(bar(F_Q + wg));
+        mbar_arrive(bar(F_QFREE + wg));
+      }
+      return true;
     };
-    int g = 0;                                                   // tiles of this warpgroup so far
-    bool ok = true;
     int i = next(blockIdx.x);
-    if (XT && i < total) load_query();
+    bool ok = !XT || i >= total || load_query();
     while (i < total && ok) {
       const Piece now = w;
       const int n = (now.r.k_len + CT - 1) / CT, row = now.x0 + wg * RT + in_tile;
@@ -359,7 +408,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
         const uint32_t s_col = taddr + b * CT;
         // a warpgroup without rows in the pieces before this one waits for all of them: what bounds the wait is
         // the limit of the warps that are at work
-        if (!warp_wait(bar(F_S + 2 * wg + b), (g >> 1) & 1, abort_flag, j == 0 ? WAIT_LIMIT_CYCLES << 8 : WAIT_LIMIT_CYCLES)) { ok = false; break; }
+        if (!warp_wait(bar(F_S + 2 * wg + b), (g >> 1) & 1, abort_flag, j == 0 ? LONG_WAIT_CYCLES : WAIT_LIMIT_CYCLES)) { ok = false; break; }
         tc_fence_after();
         if (warp_active) {
           uint32_t x[2][32];
@@ -428,21 +477,17 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       }
       if (!ok) break;
       i = next(i + gridDim.x);
-      if (XT && i < total) load_query();
-      if (!warp_wait(bar(F_PV + 2 * wg + ((g - 1) & 1)), ((g - 1) >> 1) & 1, abort_flag)) { ok = false; break; }
+      if (XT && i < total && !load_query()) break;
+      if (!warp_wait(bar(F_PV + 2 * wg + ((g - 1) & 1)), ((g - 1) >> 1) & 1, abort_flag)) break;
       tc_fence_after();
       if (warp_active) {
+        const bool there = row < now.r.q_len;
         const int64_t at = (int64_t)now.r.q_begin + row;
         const float inv = l == 0.f ? 0.f : 1.0f / l;
         bf16* out = static_cast<bf16*>(c.out) + at * c.ldo + (int64_t)now.head * d;
-#pragma unroll 2
-        for (int e = 0; e < d / 16; ++e) {
-          uint32_t o[16];
-          tmem_ld16(taddr + F_O + (uint32_t)(16 * e), o);
-          tmem_ld_wait();
-          if (row < now.r.q_len) store_16_bf16(out + 16 * e, o, inv);
-        }
-        if (row < now.r.q_len) c.lse[(int64_t)now.head * c.p.q_rows + at] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
+#pragma unroll
+        for (int s = 0; s < SLABS; ++s) store_row(out + 64 * s, taddr + F_O + 64 * s, d - 64 * s, inv, there);
+        if (there) c.lse[(int64_t)now.head * c.p.q_rows + at] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
       }
     }
   }
@@ -469,22 +514,23 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
 // order.  Two warpgroups take the tiles in turn, each with its own columns of tensor memory for S and dP:
 // while one is in its exp2 phase the tensor core works for the other.  X is in tensor memory (XT) where it
 // fits beside the accumulators: always for DQ, up to d = 80 for DKDV.
-struct BackwardMaps { CUtensorMap x1, x2, y1, y2; };
+struct BackwardMaps { CUtensorMap x1, x2, x3, y1, y2; };
 
 template <int SLABS, bool DKDV, bool XT>
 struct BackwardCfg {
-  static constexpr int STAGES = SLABS == 1 ? 6 : XT ? 5 : 4;
+  static constexpr int XS = DKDV ? 2 : 3;              // tiles of X in shared memory; DQ: out, for delta
+  static constexpr int STAGES = SLABS == 1 ? 6 : DKDV ? 4 : 3;
   static constexpr uint32_t XTILE = SLABS * RT * 128, YTILE = SLABS * CT * 128;
-  static constexpr uint32_t OFF_Y = XT ? 0 : 2 * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // DKDV: float2 [STAGES][64] -lse2, -delta of the columns
-  static constexpr uint32_t OFF_ROW = OFF_COL + STAGES * CT * 8;                                // DQ: float2 [2][128] of the rows
-  static constexpr uint32_t OFF_BARS = OFF_ROW + 2 * RT * 8;
-  static constexpr uint32_t BYTES = OFF_BARS + 512 + 1024;
+  static constexpr uint32_t OFF_Y = XS * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // DKDV: float [STAGES][2][64] -lse2, -delta of the columns
+  static constexpr uint32_t OFF_ROW = OFF_COL + (DKDV ? STAGES * CT * 8 : 0);           // DQ: float2 [2][128] of the rows
+  static constexpr uint32_t OFF_BARS = OFF_ROW + (DKDV ? 0 : 2 * RT * 8), OFF_SEQ = OFF_BARS + 512;
+  static constexpr uint32_t BYTES = OFF_SEQ + OFFSETS_BYTES + 1024;
   static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
 // columns: S and dP of the two warpgroups, then the accumulators (d each), then X1 and X2 (d / 2 each)
 constexpr uint32_t B_WG = 2 * CT, B_COLS = 2 * B_WG;
 enum BwdBar : int {
-  B_FULL = 0, B_FREE = B_FULL + 6, B_X = B_FREE + 6, B_XFREE, B_S, B_P = B_S + 2, B_SFREE = B_P + 2, B_ACC = B_SFREE + 2, B_ACCFREE,
+  B_FULL = 0, B_FREE = B_FULL + 6, B_XS = B_FREE + 6 /* X in shared memory */, B_XSFREE, B_X /* in tensor memory */, B_XFREE, B_S, B_P = B_S + 2, B_SFREE = B_P + 2, B_ACC = B_SFREE + 2, B_ACCFREE,
   B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 2
 };
 
@@ -504,21 +550,26 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < B_BARS; ++i)
-      mbar_init(bar(i), i == B_P || i == B_P + 1 ? 4 : i == B_ACCFREE || (XT && i == B_X) ? 8 : 1);
+      mbar_init(bar(i), i == B_P || i == B_P + 1 ? 4 : i == B_ACCFREE || i == B_X || (XT && i == B_XSFREE) ? 8 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
+  vit_attention_problem p = c.p;
+  stage_offsets(p, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
   const uint32_t acc2 = B_COLS, acc1 = B_COLS + d, x1_col = B_COLS + (DKDV ? 2 : 1) * d, x2_col = x1_col + d / 2;   // dk or dq; dv
   Piece w;
-  auto find = [&](int i) { return find_piece(c, i, total, tiles, x_heads, RT, DKDV, w); };
+  auto find = [&](int i) { return find_piece(p, c.dev_status, i, total, tiles, x_heads, RT, DKDV, w); };
   // tiles of Y that a piece walks over, head after head
   auto y_tiles_of = [&](const Piece& p) { return ((DKDV ? p.r.q_len : p.r.k_len) + CT - 1) / CT; };
 
-  if (warp == TMA_WARP) {
+  if (warp >= MMA_WARP) give_registers();
+  else take_registers();
+  if (warp > TMA_WARP) {
+  } else if (warp == TMA_WARP) {
     // ------------------------------------------------------------------ producer (the whole warp keeps step)
     int t0 = 0, pieces = 0, armed = 0;
     bool ok = true;
@@ -526,18 +577,17 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       const int y_tiles = y_tiles_of(w), n = DKDV ? group * y_tiles : y_tiles;
       const int y_begin = DKDV ? w.r.q_begin : w.r.k_begin, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
-      if (!XT) {
-        if (!warp_wait(bar(B_XFREE), (pieces & 1) ^ 1, abort_flag)) break;
-        if (lane == 0) {
-          const int row = (DKDV ? w.r.k_begin : w.r.q_begin) + w.x0;
-          mbar_arrive_expect_tx(bar(B_X), 2 * L::XTILE);
-          for (int s = 0; s < SLABS; ++s) {
-            tma_load_3d(sb + s * RT * 128, &maps.x1, 64 * s, w.head, row, bar(B_X));
-            tma_load_3d(sb + L::XTILE + s * RT * 128, &maps.x2, 64 * s, w.head, row, bar(B_X));
-          }
+      if (!warp_wait(bar(B_XSFREE), (pieces & 1) ^ 1, abort_flag)) break;
+      if (lane == 0) {
+        const int row = (DKDV ? w.r.k_begin : w.r.q_begin) + w.x0;
+        mbar_arrive_expect_tx(bar(B_XS), L::XS * L::XTILE);
+        for (int s = 0; s < SLABS; ++s) {
+          tma_load_3d(sb + s * RT * 128, &maps.x1, 64 * s, w.head, row, bar(B_XS));
+          tma_load_3d(sb + L::XTILE + s * RT * 128, &maps.x2, 64 * s, w.head, row, bar(B_XS));
+          if (!DKDV) tma_load_3d(sb + 2 * L::XTILE + s * RT * 128, &maps.x3, 64 * s, w.head, row, bar(B_XS));
         }
-        ++pieces;
       }
+      ++pieces;
       int yt = 0, yh = DKDV ? w.head * group : w.head / group;
       for (int t = t0; t < t0 + n; ++t) {
         const int st = t % L::STAGES, ph = (t / L::STAGES) & 1, y0 = yt * CT;
@@ -554,9 +604,12 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         }
         if (!warp_wait(bar(B_FREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
         if (DKDV) {
-          float2* col = reinterpret_cast<float2*>(smem + L::OFF_COL) + st * CT;
+          float* col = reinterpret_cast<float*>(smem + L::OFF_COL) + st * 2 * CT;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) col[32 * e + lane] = make_float2(-v[e].x, -v[e].y);
+          for (int e = 0; e < 2; ++e) {
+            col[32 * e + lane] = -v[e].x;
+            col[CT + 32 * e + lane] = -v[e].y;
+          }
           __syncwarp();
         }
         armed = t + 1;
@@ -575,7 +628,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     if (*abort_flag && lane == 0) {
       // a wait gave up somewhere: let the copies that were started land before the block leaves
       volatile int never = 0;
-      if (!XT && pieces) mbar_wait_limit(bar(B_X), (pieces - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
+      if (pieces) mbar_wait_limit(bar(B_XS), (pieces - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
       for (int t = armed > L::STAGES ? armed - L::STAGES : 0; t < armed; ++t)
         mbar_wait_limit(bar(B_FULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
     }
@@ -589,7 +642,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
       const int y_tiles = y_tiles_of(w), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
-      if (scores && !warp_spin(bar(B_X), pieces & 1, abort_flag)) break;
+      if (scores && !warp_spin(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
       const int last = y_len - (y_tiles - 1) * CT;               // rows of a head's last tile
       int yt = 0;                                                // tile of its head
       for (int t = 0; t < n; ++t) {
@@ -617,7 +670,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
               issue_scores_ss<SLABS>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
             }
             umma_commit(bar(B_S + b));
-            if (t == n - 1) umma_commit(bar(B_XFREE));
+            if (t == n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE));
           }
         } else {
           if (!warp_spin(bar(B_P + b), phase >> b & 1, abort_flag)) { ok = false; break; }
@@ -673,40 +726,41 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       return i;
     };
     // this thread's row of X1 (first warpgroup) or X2 (second) of piece w into tensor memory; the second
-    // warpgroup of DQ holds dout and takes its product with out on the way
+    // warpgroup of DQ has dout and takes its product with out on the way
     auto load_x = [&] {
-      const int row = w.x0 + in_tile;
-      const bool there = row < (DKDV ? w.r.k_len : w.r.q_len);
-      const int64_t at = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row;
-      const bf16* src = wg == 0 ? static_cast<const bf16*>(DKDV ? c.k : c.q) + at * (DKDV ? c.ldk : c.ldq)
-                                : static_cast<const bf16*>(DKDV ? c.v : c.dout) + at * (DKDV ? c.ldv : c.lddo);
-      src += (int64_t)w.head * d;
-      const uint32_t to = lanes + (wg == 0 ? x1_col : x2_col);
-      if (DKDV || wg == 0) {
-        row_to_tmem(to, src, d, there, [](int, const uint32_t(&)[8]) {});
-      } else {
-        const uint4* o = reinterpret_cast<const uint4*>(static_cast<const bf16*>(c.out) + at * c.ldo + (int64_t)w.head * d);
-        const float lse = there ? c.lse[(int64_t)w.head * c.p.q_rows + at] : 0.f;
+      if (!warp_wait(bar(B_XS), pieces & 1, abort_flag)) return false;
+      row_to_tmem<SLABS>(lanes + (wg == 0 ? x1_col : x2_col), sb + wg * L::XTILE, in_tile, d);
+      if (!DKDV && wg == 1) {
+        const int row = w.x0 + in_tile;
+        const int64_t i = (int64_t)w.head * c.p.q_rows + w.r.q_begin + row;
+        const bool there = row < w.r.q_len;
+        const float lse = there ? c.lse[i] : 0.f;
         float delta = 0.f;
-        row_to_tmem(to, src, d, there, [&](int g, const uint32_t(&v)[8]) {
-          if (!there) return;
-          const uint4 a = o[2 * g], b = o[2 * g + 1];
-          const uint32_t u[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) delta = dot2(u[e], v[e], delta);
-        });
+        for (int g = 0; g < 4 * SLABS; ++g)
+          if (g < d / 16) {
+            uint32_t u[8], v[8];
+            read_16(u, sb + L::XTILE, in_tile, g);
+            read_16(v, sb + 2 * L::XTILE, in_tile, g);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = dot2(u[e], v[e], delta);
+          }
         const float2 mine = make_float2(lse * LOG2E, delta);
         reinterpret_cast<float2*>(smem + L::OFF_ROW)[(pieces & 1) * RT + in_tile] = mine;
-        if (there) c.delta[(int64_t)w.head * c.p.q_rows + at] = mine;
+        if (there) c.delta[i] = mine;
       }
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(B_X));
+      if (lane == 0) {
+        mbar_arrive(bar(B_X));
+        mbar_arrive(bar(B_XSFREE));
+      }
+      return true;
     };
     int i = next(blockIdx.x);
-    if (XT && i < total) load_x();
-    while (i < total) {
+    ok = !XT || i >= total || load_x();
+    while (i < total && ok) {
       const Piece now = w;
       const int y_tiles = y_tiles_of(now), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? now.r.q_len : now.r.k_len;
       const int x_len = DKDV ? now.r.k_len : now.r.q_len, row = now.x0 + in_tile;
@@ -722,7 +776,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       for (int t = wg; t < n; t += 2) {
         const int here = (DKDV ? yt : t) == y_tiles - 1 ? y_len - (y_tiles - 1) * CT : CT, nch = (here + 31) / 32;
         const int st = (t0 + t) % L::STAGES;
-        const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2);   // two columns each
+        const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2);   // four columns each: -lse2, then -delta
         if (DKDV) {
           yt = (yt + 2) % y_tiles;
           if (!warp_wait(bar(B_FULL + st), ((t0 + t) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
@@ -750,22 +804,26 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
             uint32_t pk[16], dk[16];
             const int left = here - 32 * h;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float2 a = nls, b = nde;
+            for (int q = 0; q < 8; ++q) {
+              float4 a4 = make_float4(nls.x, nls.x, nls.x, nls.x), b4 = make_float4(nde.x, nde.x, nde.x, nde.x);
               if (DKDV) {
-                const float4 v = col[16 * h + e];
-                a = make_float2(v.x, v.z);
-                b = make_float2(v.y, v.w);
+                a4 = col[8 * h + q];
+                b4 = col[CT / 4 + 8 * h + q];
               }
-              const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[h][2 * e]), __uint_as_float(s[h][2 * e + 1])), sl2v, a);
-              float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-              if (!DKDV && left < 32) {                          // keys behind the end
-                if (2 * e >= left) p.x = 0.f;
-                if (2 * e + 1 >= left) p.y = 0.f;
+#pragma unroll
+              for (int f = 0; f < 2; ++f) {
+                const int e = 2 * q + f;
+                const float2 a = f ? make_float2(a4.z, a4.w) : make_float2(a4.x, a4.y), b = f ? make_float2(b4.z, b4.w) : make_float2(b4.x, b4.y);
+                const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[h][2 * e]), __uint_as_float(s[h][2 * e + 1])), sl2v, a);
+                float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                if (!DKDV && left < 32) {                        // keys behind the end
+                  if (2 * e >= left) p.x = 0.f;
+                  if (2 * e + 1 >= left) p.y = 0.f;
+                }
+                const float2 y = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(g[h][2 * e]), __uint_as_float(g[h][2 * e + 1])), b));
+                if (DKDV) pk[e] = pack_bf16(p.x, p.y);
+                dk[e] = pack_bf16(y.x, y.y);
               }
-              const float2 y = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(g[h][2 * e]), __uint_as_float(g[h][2 * e + 1])), b));
-              if (DKDV) pk[e] = pack_bf16(p.x, p.y);
-              dk[e] = pack_bf16(y.x, y.y);
             }
             if (DKDV) tmem_st16(taddr + (uint32_t)(16 * h), pk);
             tmem_st16(taddr + (uint32_t)(CT + 16 * h), dk);
@@ -784,19 +842,21 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         // every score of the last piece is complete: its X may be overwritten
         if (!warp_wait(bar(B_XFREE), (pieces - 1) & 1, abort_flag)) break;
         tc_fence_after();
-        load_x();
+        if (!load_x()) break;
       }
       if (!warp_wait(bar(B_ACC), (pieces - 1) & 1, abort_flag)) break;
       tc_fence_after();
       if (warp_active) {
         const int64_t at = (int64_t)(DKDV ? now.r.k_begin : now.r.q_begin) + row;
-        for (int e = wg; e < d / 16 * (DKDV ? 2 : 1); e += 2) {
-          const bool second = e >= d / 16;
-          const int cc = 16 * (second ? e - d / 16 : e);
-          uint32_t o[16];
-          tmem_ld16(lanes + (second ? acc1 : acc2) + (uint32_t)cc, o);
-          tmem_ld_wait();
-          if (row < x_len) store_16_bf16((second ? grad1(now, at) : grad2(now, at)) + cc, o, second ? 1.f : c.p.scale);
+        const bool there = row < x_len;
+        // DKDV: dk by the first warpgroup, dv by the second; DQ: halves of the head
+        if (DKDV) {
+          bf16* to = wg == 0 ? grad2(now, at) : grad1(now, at);
+#pragma unroll
+          for (int s = 0; s < SLABS; ++s) store_row(to + 64 * s, lanes + (wg == 0 ? acc2 : acc1) + 64 * s, d - 64 * s, wg == 0 ? c.p.scale : 1.f, there);
+        } else {
+          const int half = d / 32 * 16, from = wg == 0 ? 0 : half;
+          store_row(grad2(now, at) + from, lanes + acc2 + from, wg == 0 ? half : d - half, c.p.scale, there);
         }
       }
       tc_fence_before();
@@ -877,6 +937,8 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
   } else {
     m.y1 = m.y2 = m.x1;
   }
+  if (DKDV) m.x3 = m.x1;
+  else if (!encode_heads(&m.x3, c.out, xr, xh, c.p.d, c.ldo, RT)) return cudaErrorInvalidValue;
   static PerDeviceFlag done;
   if (cudaError_t e = ensure_dynamic_smem(done, packed_backward_tc_kernel<SLABS, DKDV, XT>, (int)L::BYTES)) return e;
   const int sms = current_device_sm_count();
