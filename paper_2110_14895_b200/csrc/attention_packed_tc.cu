@@ -54,13 +54,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
       "l"(reinterpret_cast<uint64_t>(tm)), "r"(c), "r"(head), "r"(row), "r"(bar)
       : "memory");
 }
-__device__ __forceinline__ void store_16_bf16(bf16* dst, const uint32_t (&o)[16], float by) {   // 32 bytes, one sector
-  uint32_t w[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = pack_bf16(__uint_as_float(o[2 * i]) * by, __uint_as_float(o[2 * i + 1]) * by);
-  *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-  *reinterpret_cast<uint4*>(dst + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-}
 // a bounded wait of a whole warp: all lanes leave with the same answer
 __device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag, long long limit = WAIT_LIMIT_CYCLES) {
   return __all_sync(0xffffffffu, mbar_wait_limit(bar, (uint32_t)parity, abort_flag, limit));
@@ -92,6 +85,16 @@ __device__ __forceinline__ void zero_rows(uint32_t tile, int rows, int slabs, in
   __syncwarp();
 }
 
+// waits for tensor-memory loads and names their registers, so that nothing reads them before
+__device__ __forceinline__ void tmem_ld_wait_16(uint32_t (&r)[16], uint32_t (&t)[16]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                 "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(t[0]), "+r"(t[1]), "+r"(t[2]),
+                 "+r"(t[3]), "+r"(t[4]), "+r"(t[5]), "+r"(t[6]), "+r"(t[7]), "+r"(t[8]), "+r"(t[9]), "+r"(t[10]), "+r"(t[11]),
+                 "+r"(t[12]), "+r"(t[13]), "+r"(t[14]), "+r"(t[15])
+               :
+               : "memory");
+}
 // One lane of the warp, chosen by the hardware.  The products are issued behind this and not behind
 // `lane == 0`: their operands then stay in uniform registers (110 -> about 20 cycles to issue one).
 __device__ __forceinline__ bool elect_one() {
@@ -102,31 +105,33 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xffffffffu, v, 0); }
 
 // S[128 x n] = X[128 rows] . Y[n rows]^T over the head's channels; X in tensor memory (packed pairs) or in
-// shared memory, as slabs of 64 channels like Y
-template <int SLABS>
+// shared memory, as slabs of 64 channels like Y (whose tiles have Y_ROWS rows)
+template <int SLABS, int Y_ROWS>
 __device__ __forceinline__ void issue_scores_ts(uint32_t d_tmem, uint32_t x_tmem, uint32_t y, int n, int ksteps) {
   const uint32_t id = idesc(n, false);
   const uint64_t yd = desc_sw128(y);
 #pragma unroll
   for (int k = 0; k < 4 * SLABS; ++k)
-    if (k < ksteps) umma_bf16_ts(d_tmem, x_tmem + (uint32_t)(8 * k), yd + (uint64_t)((k >> 2) * (CT * 8) + 2 * (k & 3)), id, k > 0 ? 1u : 0u);
+    if (k < ksteps) umma_bf16_ts(d_tmem, x_tmem + (uint32_t)(8 * k), yd + (uint64_t)((k >> 2) * (Y_ROWS * 8) + 2 * (k & 3)), id, k > 0 ? 1u : 0u);
 }
-template <int SLABS>
+template <int SLABS, int Y_ROWS>
 __device__ __forceinline__ void issue_scores_ss(uint32_t d_tmem, uint32_t x, uint32_t y, int n, int ksteps) {
   const uint32_t id = idesc(n, false);
   const uint64_t xd = desc_sw128(x), yd = desc_sw128(y);
 #pragma unroll
   for (int k = 0; k < 4 * SLABS; ++k)
     if (k < ksteps)
-      umma_bf16(d_tmem, xd + (uint64_t)((k >> 2) * (RT * 8) + 2 * (k & 3)), yd + (uint64_t)((k >> 2) * (CT * 8) + 2 * (k & 3)), id,
+      umma_bf16(d_tmem, xd + (uint64_t)((k >> 2) * (RT * 8) + 2 * (k & 3)), yd + (uint64_t)((k >> 2) * (Y_ROWS * 8) + 2 * (k & 3)), id,
                 k > 0 ? 1u : 0u);
 }
-// D[128 x d] (+)= P[128 x 16 ksteps] . Y[16 ksteps rows x d], P packed in tensor memory
+// D[128 x d] (+)= P[128 x 64] . Y[64 rows x d], `ksteps` of the four steps of 16 rows; P packed in tensor memory;
+// y: the first of the 64 rows in a tile of Y_ROWS
+template <int Y_ROWS>
 __device__ __forceinline__ void issue_weighted(uint32_t d_tmem, uint32_t p_tmem, uint32_t y, int d, int ksteps, bool first) {
   const uint32_t id = idesc(d, true);
-  const uint64_t yd = desc_sw128(y, CT * 128);
+  const uint64_t yd = desc_sw128(y, Y_ROWS * 128);
 #pragma unroll
-  for (int k = 0; k < CT / 16; ++k)
+  for (int k = 0; k < 4; ++k)
     if (k < ksteps) umma_bf16_ts(d_tmem, p_tmem + (uint32_t)(8 * k), yd + (uint64_t)(k * 128), id, first && k == 0 ? 0u : 1u);
 }
 // The 16 channels 16 g ... of a row of a swizzled tile of 128 rows in shared memory
@@ -153,22 +158,54 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float acc) {
   return fmaf(__uint_as_float(a & 0xffff0000u), __uint_as_float(b & 0xffff0000u), acc);
 }
 
-// 64 accumulator columns of a row (those below d) times a factor to global memory: all loads, one wait, the stores
-__device__ __forceinline__ void store_row(bf16* dst, uint32_t taddr, int left, float by, bool there) {
-  uint32_t o[4][16];
+// The accumulator rows of a warp (32 rows, columns [0, cols)) times a factor per row to global memory.  A row
+// belongs to a lane, and lanes that wrote their rows themselves would touch 32 lines with every store: the
+// rows go through 2 KB of shared memory, 32 columns at a time, and leave as 64 bytes each of eight rows.
+// stage: this warp's 2 KB; rows: how many of the 32 exist; dst: row 0, its columns; ld in elements.
+__device__ __forceinline__ void store_rows(bf16* dst, int64_t ld, uint32_t taddr, int cols, float by, int rows, uint32_t stage, int lane) {
+  for (int c = 0; c < cols; c += 32) {
+    uint32_t o[2][16];
+    tmem_ld16(taddr + (uint32_t)c, o[0]);
+    if (c + 16 < cols) tmem_ld16(taddr + (uint32_t)(c + 16), o[1]);
+    tmem_ld_wait_16(o[0], o[1]);
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (16 * e < left) tmem_ld16(taddr + (uint32_t)(16 * e), o[e]);
-  tmem_ld_wait();
+    for (int q = 0; q < 4; ++q) {
+      uint32_t w[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) asm volatile("" : "+r"(o[e][0]), "+r"(o[e][1]), "+r"(o[e][2]), "+r"(o[e][3]), "+r"(o[e][4]), "+r"(o[e][5]),
-      "+r"(o[e][6]), "+r"(o[e][7]), "+r"(o[e][8]), "+r"(o[e][9]), "+r"(o[e][10]), "+r"(o[e][11]), "+r"(o[e][12]), "+r"(o[e][13]),
-      "+r"(o[e][14]), "+r"(o[e][15]));                           // nothing reads them before the wait
-  if (!there) return;
+      for (int e = 0; e < 4; ++e)
+        w[e] = pack_bf16(__uint_as_float(o[q >> 1][8 * (q & 1) + 2 * e]) * by, __uint_as_float(o[q >> 1][8 * (q & 1) + 2 * e + 1]) * by);
+      // 16-byte piece q of this lane's row, turned by the row so that eight lanes meet different banks
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + (uint32_t)(lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4))), "r"(w[0]),
+                   "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    }
+    __syncwarp();
+    const int q = lane & 3;
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (16 * e < left) store_16_bf16(dst + 16 * e, o[e], by);
+    for (int e = 0; e < 4; ++e) {
+      const int r = 8 * e + (lane >> 2);
+      uint4 v;
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                   : "r"(stage + (uint32_t)(r * 64 + ((q ^ ((r >> 1) & 3)) << 4))));
+      if (r < rows && c + 8 * q < cols) *reinterpret_cast<uint4*>(dst + r * ld + c + 8 * q) = v;
+    }
+    __syncwarp();
+  }
 }
+
+// Division by a number that is the same for the whole launch: q = (t + ((n - t) >> 1)) >> shift with
+// t = high word of n * mul (Granlund and Montgomery's method for 32 bits)
+struct Divisor { uint32_t d, mul, shift; };
+Divisor divisor(uint32_t d) {
+  uint32_t l = 0;
+  while (l < 32 && ((uint64_t)1 << l) < d) ++l;
+  return Divisor{d, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1), l > 0 ? l - 1 : 0};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor& v) {
+  if (v.d == 1) return n;
+  const uint32_t t = __umulhi(n, v.mul);
+  return (t + ((n - t) >> 1)) >> v.shift;
+}
+struct Pieces { int total; Divisor tiles, heads; };             // of a launch: number, tiles of a sequence, heads
 
 // The sequences' offsets are kept in shared memory where they fit: every role of a block looks at them for every piece.
 constexpr int MAX_STAGED = 1024;
@@ -185,173 +222,211 @@ __device__ __forceinline__ void stage_offsets(vit_attention_problem& p, int32_t*
 
 // A piece of work: `span` rows of one head of one sequence.
 struct Piece { int head, x0; SeqRange r; };
-// The first piece from number i on (in steps of the grid) whose rows exist; i = total if there is none.
-__device__ __forceinline__ int find_piece(const vit_attention_problem& p, int* status, int i, int total, int tiles, int heads, int span,
-                                          bool of_keys, Piece& w) {
-  for (; i < total; i += (int)gridDim.x) {
-    const unsigned hs = (unsigned)i / (unsigned)tiles, seq = hs / (unsigned)heads;
-    w.head = (int)(hs - seq * (unsigned)heads);
-    w.x0 = (int)((unsigned)i - hs * (unsigned)tiles) * span;
-    if (seq_range(p, (int)seq, w.r, status) && w.x0 < (of_keys ? w.r.k_len : w.r.q_len)) return i;
+// The first piece from number i on (in steps of the grid) whose rows exist; i >= total if there is none.
+__device__ __forceinline__ int find_piece(const vit_attention_problem& p, int* status, int i, const Pieces& all, int span, bool of_keys, Piece& w) {
+  for (; i < all.total; i += (int)gridDim.x) {
+    const uint32_t hs = divide((uint32_t)i, all.tiles), seq = divide(hs, all.heads);
+    w.head = (int)(hs - seq * all.heads.d);
+    w.x0 = (int)((uint32_t)i - hs * all.tiles.d) * span;
+    if (seq_range(p, (int)seq, w.r, status) && w.x0 < (of_keys ? w.r.k_len : w.r.q_len)) break;
   }
-  return total;
+  return i;
 }
+// Place in a ring of stages and the parity of its present round
+template <int N>
+struct Ring {
+  int at = 0, parity = 0;
+  __device__ __forceinline__ void step() {
+    if (++at == N) {
+      at = 0;
+      parity ^= 1;
+    }
+  }
+};
 
 // ============================================================================================ forward
 // A piece is 256 queries of a head: warps 0-3 and 4-7 hold 128 of them each and share the keys, which come
-// in tiles of 64; warps 8 and 9 issue the products of one warpgroup each, warp 10 the copies.  Each warpgroup has two tiles of scores, so
-// that the next one is ready when it has finished its exp2 phase.  The accumulator is rescaled only when a
-// row's maximum has grown by more than 2^8 since the last time (probabilities stay below 2^8, the row sum
-// in fp32): it rarely is after the first tile, and only then does a warpgroup wait for its last product.
+// in tiles of 128; warps 8 and 9 issue the products of one warpgroup each, warp 10 the copies.  The scores of
+// a warpgroup's next tile come only after its last probabilities were used: the two warpgroups fall into step
+// so that one runs its exponentials while the tensor core works for the other (a warp of each shares a
+// scheduler and its exp2 unit, 8 cycles for 32 of them, which bounds the kernel up to d = 128: 1024 cycles for
+// 2 x 128 x 64 scores).  The accumulator is rescaled only when a row's maximum has grown by more than 2^8
+// since the last time (probabilities stay below 2^8, the row sum in fp32): rarely after the first tile.
 struct ForwardMaps { CUtensorMap q, k, v; };
+constexpr int F_MMA_WARP = 8 /* two */, F_TMA_WARP = 10, F_THREADS = 352;
+constexpr uint32_t TMEM_ALL = 512;
 
-template <int SLABS, bool XT>
+template <int SLABS>
 struct ForwardCfg {
-  static constexpr int STAGES = SLABS == 1 ? 6 : 4;
-  static constexpr uint32_t TILE = SLABS * CT * 128, QTILE = SLABS * RT * 128;
-  static constexpr uint32_t OFF_K = 2 * QTILE, OFF_V = OFF_K + STAGES * TILE, OFF_BARS = OFF_V + STAGES * TILE, OFF_SEQ = OFF_BARS + 512;
+  static constexpr int STAGES = SLABS == 1 ? 3 : 2;
+  static constexpr uint32_t TILE = SLABS * RT * 128;             // of queries, keys or values
+  static constexpr uint32_t OFF_K = 2 * TILE, OFF_V = OFF_K + STAGES * TILE, OFF_OUT = OFF_V + STAGES * TILE;
+  static constexpr uint32_t OFF_BARS = OFF_OUT + 8 * 2048, OFF_SEQ = OFF_BARS + 512;
   static constexpr uint32_t BYTES = OFF_SEQ + OFFSETS_BYTES + 1024;
   static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
-constexpr int TC_THREADS = 384, MMA_WARP = 8 /* two */, TMA_WARP = 10;   // warp 11 only hands its registers on
-// 168 registers a thread at launch (384 x 168 = 64512): the score warps take 200, the other four warps keep 96
-// (256 x 200 + 128 x 96 = 63488)
-__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 200;"); }
-__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 96;"); }
-constexpr uint32_t TMEM_ALL = 512;
-// columns of a warpgroup (256): two tiles of scores, the accumulator (d), the queries (d / 2)
-constexpr uint32_t F_WG = 256, F_O = 2 * CT;
+// Columns of a warpgroup (256): scores (128), the accumulator (d), the queries (d / 2) where they fit (XT).
+// Probabilities of keys [0, 64) lie in [0, 32), of keys [64, 128) in [64, 96).
+constexpr uint32_t F_WG = 256, F_O = RT;
 enum FwdBar : int {
-  F_KFULL = 0, F_KFREE = F_KFULL + 6, F_VFULL = F_KFREE + 6, F_VFREE = F_VFULL + 6, F_QFULL = F_VFREE + 6 /* [wg] shared memory */,
-  F_QFREE = F_QFULL + 2, F_Q = F_QFREE + 2 /* [wg] tensor memory */, F_S = F_Q + 2 /* [wg][tile parity] */, F_P = F_S + 4, F_PV = F_P + 4, F_DRAIN = F_PV + 4 /* [MMA warp] */, F_BARS = F_DRAIN + 2
+  F_KFULL = 0, F_KFREE = F_KFULL + 3, F_VFULL = F_KFREE + 3, F_VFREE = F_VFULL + 3, F_QFULL = F_VFREE + 3 /* [wg] shared memory */,
+  F_QFREE = F_QFULL + 2, F_Q = F_QFREE + 2 /* [wg] tensor memory */, F_S = F_Q + 2 /* [wg] */, F_P = F_S + 2 /* [wg][half] */,
+  F_PV = F_P + 4 /* [wg] */, F_DRAIN = F_PV + 2 /* [MMA warp] */, F_BARS = F_DRAIN + 2
 };
 
+// Row sums and packed probabilities of 32 scores
+__device__ __forceinline__ void exp_32(const uint32_t (&x)[32], float2 sl2v, float2 nmv, float2 (&l2)[2], uint32_t (&pk)[16]) {
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[2 * e]), __uint_as_float(x[2 * e + 1])), sl2v, nmv);
+    const float2 p = make_float2(ex2_approx(y.x), ex2_approx(y.y));
+    l2[e & 1] = __fadd2_rn(l2[e & 1], p);
+    pk[e] = pack_bf16(p.x, p.y);
+  }
+}
+__device__ __forceinline__ float max_32(const uint32_t (&x)[32], float top) {
+  float m[2] = {top, -INFINITY};
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) {
+    asm("max.f32 %0, %0, %1, %2;" : "+f"(m[0]) : "f"(__uint_as_float(x[e])), "f"(__uint_as_float(x[e + 1])));
+    asm("max.f32 %0, %0, %1, %2;" : "+f"(m[1]) : "f"(__uint_as_float(x[e + 2])), "f"(__uint_as_float(x[e + 3])));
+  }
+  return fmaxf(m[0], m[1]);
+}
+// keys behind the end: minus infinity
+__device__ __forceinline__ void mask_32(uint32_t (&x)[32], int left) {
+  if (left < 32) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e >= left) x[e] = 0xff800000u;
+  }
+}
+
 template <int SLABS, bool XT>
-__global__ void __launch_bounds__(TC_THREADS, 1)
-packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedCall c, int total, int tiles) {
-  using L = ForwardCfg<SLABS, XT>;
+__global__ void __launch_bounds__(F_THREADS, 1)
+packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedCall c, const Pieces all) {
+  using L = ForwardCfg<SLABS>;
   extern __shared__ uint8_t smem_raw[];
   const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sb = smem_u32(smem);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BARS);
-  auto bar = [&](int i) { return smem_u32(&bars[i]); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(&bars[F_BARS]);
+  const uint32_t sb = smem_u32(smem), bars = sb + L::OFF_BARS;
+  auto bar = [&](int i) { return bars + (uint32_t)(8 * i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_BARS + 8 * F_BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < F_BARS; ++i) {
-      const bool stage_free = (i >= F_KFREE && i < F_KFREE + 6) || (i >= F_VFREE && i < F_VFREE + 6);   // by both MMA warps
+      const bool stage_free = (i >= F_KFREE && i < F_KFREE + 3) || (i >= F_VFREE && i < F_VFREE + 3);   // by both MMA warps
       const bool by_warps = (i >= F_P && i < F_P + 4) || i == F_Q || i == F_Q + 1 || (XT && (i == F_QFREE || i == F_QFREE + 1));
       mbar_init(bar(i), stage_free ? 2 : by_warps ? 4 : 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
+  if (warp == F_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
   vit_attention_problem p = c.p;
   stage_offsets(p, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
+  auto find = [&](int i, Piece& w) { return find_piece(p, c.dev_status, i, all, 2 * RT, false, w); };
   Piece w;
-  auto find = [&](int i) { return find_piece(p, c.dev_status, i, total, tiles, p.heads, 2 * RT, false, w); };
 
-  if (warp >= MMA_WARP) give_registers();
-  else take_registers();
-  if (warp > TMA_WARP) {
-  } else if (warp == TMA_WARP) {
+  if (warp == F_TMA_WARP) {
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0) {
-      int t = 0, q_tiles[2] = {0, 0}, armed_k = 0, armed_v = 0;   // tiles of keys and of queries so far
+      Ring<L::STAGES> ring;
+      int q0 = 0, q1 = 0, n_all = 0;                             // tiles of queries of each warpgroup, of keys so far
       bool ok = true;
-      for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
-        const int n = (w.r.k_len + CT - 1) / CT, kv = w.head / group;
+      for (int i = find(blockIdx.x, w); i < all.total && ok; i = find(i + gridDim.x, w)) {
+        const int n = (w.r.k_len + RT - 1) / RT, kv = group == 1 ? w.head : w.head / group;
         if (n == 0) continue;
-        for (int h = 0; h < 2 && ok; ++h) {
-          if (w.x0 + h * RT >= w.r.q_len) break;
-          if (!mbar_wait_limit(bar(F_QFREE + h), (q_tiles[h] & 1) ^ 1, abort_flag, LONG_WAIT_CYCLES)) { ok = false; break; }
-          mbar_arrive_expect_tx(bar(F_QFULL + h), L::QTILE);
-          ++q_tiles[h];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          int& q = h ? q1 : q0;
+          if (w.x0 + h * RT >= w.r.q_len || !ok) continue;
+          if (!mbar_wait_limit(bar(F_QFREE + h), (q & 1) ^ 1, abort_flag, LONG_WAIT_CYCLES)) { ok = false; continue; }
+          mbar_arrive_expect_tx(bar(F_QFULL + h), L::TILE);
+          ++q;
           for (int s = 0; s < SLABS; ++s)
-            tma_load_3d(sb + h * L::QTILE + s * RT * 128, &maps.q, 64 * s, w.head, w.r.q_begin + w.x0 + h * RT, bar(F_QFULL + h));
+            tma_load_3d(sb + h * L::TILE + s * RT * 128, &maps.q, 64 * s, w.head, w.r.q_begin + w.x0 + h * RT, bar(F_QFULL + h));
         }
-        for (int j = 0; j < n && ok; ++j, ++t) {
-          const int st = t % L::STAGES, ph = (t / L::STAGES) & 1, krow = w.r.k_begin + j * CT;
-          if (!mbar_wait(bar(F_KFREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
+        for (int j = 0; j < n && ok; ++j, ring.step()) {
+          const int st = ring.at, krow = w.r.k_begin + j * RT;
+          if (!mbar_wait(bar(F_KFREE + st), ring.parity ^ 1, abort_flag)) { ok = false; break; }
           mbar_arrive_expect_tx(bar(F_KFULL + st), L::TILE);
-          armed_k = t + 1;
-          for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_K + st * L::TILE + s * CT * 128, &maps.k, 64 * s, kv, krow, bar(F_KFULL + st));
-          if (!mbar_wait(bar(F_VFREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
+          for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_K + st * L::TILE + s * RT * 128, &maps.k, 64 * s, kv, krow, bar(F_KFULL + st));
+          if (!mbar_wait(bar(F_VFREE + st), ring.parity ^ 1, abort_flag)) { ok = false; break; }
           mbar_arrive_expect_tx(bar(F_VFULL + st), L::TILE);
-          armed_v = t + 1;
-          for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_V + st * L::TILE + s * CT * 128, &maps.v, 64 * s, kv, krow, bar(F_VFULL + st));
+          for (int s = 0; s < SLABS; ++s) tma_load_3d(sb + L::OFF_V + st * L::TILE + s * RT * 128, &maps.v, 64 * s, kv, krow, bar(F_VFULL + st));
+          ++n_all;
         }
       }
       if (*abort_flag) {
         // a wait gave up somewhere: let the copies that were started land before the block leaves
         volatile int never = 0;
-        for (int h = 0; h < 2; ++h)
-          if (q_tiles[h]) mbar_wait_limit(bar(F_QFULL + h), (q_tiles[h] - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
-        for (int i = armed_k > L::STAGES ? armed_k - L::STAGES : 0; i < armed_k; ++i)
-          mbar_wait_limit(bar(F_KFULL + i % L::STAGES), (i / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
-        for (int i = armed_v > L::STAGES ? armed_v - L::STAGES : 0; i < armed_v; ++i)
-          mbar_wait_limit(bar(F_VFULL + i % L::STAGES), (i / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
+        if (q0) mbar_wait_limit(bar(F_QFULL), (q0 - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
+        if (q1) mbar_wait_limit(bar(F_QFULL + 1), (q1 - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
+        // (one tile of keys more than of values may be under way)
+        for (int t = n_all > L::STAGES ? n_all - L::STAGES : 0; t <= n_all; ++t) {
+          if (t < n_all || !ok) mbar_wait_limit(bar(F_KFULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
+          if (t < n_all) mbar_wait_limit(bar(F_VFULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
+        }
       }
     }
-  } else if (warp >= MMA_WARP) {
+  } else if (warp >= F_MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuers, one per warpgroup (the whole warp keeps step)
-    const int h = warp - MMA_WARP;
-    const uint32_t base = tmem + h * F_WG;
-    int t0 = 0, g = 0, seen = 0;                                 // tiles of keys so far, those of this warpgroup, pieces
+    const int h = warp - F_MMA_WARP;
+    const uint32_t base = tmem + h * F_WG, q_smem = sb + h * L::TILE;
+    Ring<L::STAGES> ring;
+    int seen = 0, turn = 0;                                      // parities: pieces and tiles of this warpgroup so far
     bool ok = true;
-    for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
-      const int n = (w.r.k_len + CT - 1) / CT;
+    for (int i = find(blockIdx.x, w); i < all.total && ok; i = find(i + gridDim.x, w)) {
+      const int n = (w.r.k_len + RT - 1) / RT;
       if (n == 0) continue;
       const bool mine = w.x0 + h * RT < w.r.q_len;               // else the stages are passed on only
-      for (int j = 0; j <= n; ++j) {
-        if (j < n) {
-          const int st = (t0 + j) % L::STAGES, n16 = (min(CT, w.r.k_len - j * CT) + 15) / 16, b = (g + j) & 1;
-          const uint32_t ks = sb + L::OFF_K + st * L::TILE;
-          if (!warp_spin(bar(F_KFULL + st), ((t0 + j) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
-          if (j == 0 && mine && !warp_spin(bar((XT ? F_Q : F_QFULL) + h), seen & 1, abort_flag)) { ok = false; break; }
-          if (elect_one()) {
-            if (mine) {
-              // the scores overwrite P of tile j - 2: its product was issued before, by this warp
-              tc_fence_after();
-              if (XT) issue_scores_ts<SLABS>(base + b * CT, base + F_O + d, ks, 16 * n16, d / 16);
-              else issue_scores_ss<SLABS>(base + b * CT, sb + h * L::QTILE, ks, 16 * n16, d / 16);
-              umma_commit(bar(F_S + 2 * h + b));
-              if (!XT && j == n - 1) umma_commit(bar(F_QFREE + h));
-            }
-            umma_commit(bar(F_KFREE + st));
+      if (mine) {
+        if (!warp_spin(bar((XT ? F_Q : F_QFULL) + h), seen, abort_flag)) break;
+        seen ^= 1;
+      }
+      for (int j = 0; j < n; ++j, ring.step()) {
+        const int st = ring.at, here = min(RT, w.r.k_len - j * RT), n16 = (here + 15) / 16;
+        const uint32_t ks = sb + L::OFF_K + st * L::TILE, vs = sb + L::OFF_V + st * L::TILE;
+        if (!warp_spin(bar(F_KFULL + st), ring.parity, abort_flag)) { ok = false; break; }
+        if (elect_one()) {
+          if (mine) {
+            // the scores overwrite P of the last tile: its product was issued before, by this warp
+            tc_fence_after();
+            if (XT) issue_scores_ts<SLABS, RT>(base, base + F_O + d, ks, 16 * n16, d / 16);
+            else issue_scores_ss<SLABS, RT>(base, q_smem, ks, 16 * n16, d / 16);
+            umma_commit(bar(F_S + h));
+            if (!XT && j == n - 1) umma_commit(bar(F_QFREE + h));
           }
-          __syncwarp();                                          // lanes that poll would hold up the one that issues
+          umma_commit(bar(F_KFREE + st));
         }
-        if (j > 0) {
-          const int jj = j - 1, st = (t0 + jj) % L::STAGES, here = min(CT, w.r.k_len - jj * CT), n16 = (here + 15) / 16, b = (g + jj) & 1;
-          const uint32_t vs = sb + L::OFF_V + st * L::TILE;
-          if (!warp_spin(bar(F_VFULL + st), ((t0 + jj) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
-          // rows of V behind the last key meet probabilities of zero: make them zero too, whatever lies there
-          // (both warps write the same zeros; neither reads before its own are there)
-          if (mine && here < 16 * n16) zero_rows(vs, CT, SLABS, here, lane);
-          if (mine && !warp_spin(bar(F_P + 2 * h + b), ((g + jj) >> 1) & 1, abort_flag)) { ok = false; break; }
+        __syncwarp();                                            // lanes that poll would hold up the one that issues
+        if (!warp_spin(bar(F_VFULL + st), ring.parity, abort_flag)) { ok = false; break; }
+        // rows of V behind the last key meet probabilities of zero: make them zero too, whatever lies there
+        // (both warps write the same zeros; neither reads before its own are there)
+        if (mine && here < 16 * n16) zero_rows(vs, RT, SLABS, here, lane);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (!mine || 4 * half >= n16) break;
+          if (!warp_spin(bar(F_P + 2 * h + half), turn, abort_flag)) { ok = false; break; }
           if (elect_one()) {
-            if (mine) {
-              tc_fence_after();
-              issue_weighted(base + F_O, base + b * CT, vs, d, n16, jj == 0);
-              umma_commit(bar(F_PV + 2 * h + b));
-            }
-            umma_commit(bar(F_VFREE + st));
+            tc_fence_after();
+            issue_weighted<RT>(base + F_O, base + 64 * half, vs + half * 64 * 128, d, n16 - 4 * half, j == 0 && half == 0);
           }
           __syncwarp();
         }
-      }
-      t0 += n;
-      if (mine) {
-        ++seen;
-        g += n;
+        if (!ok) break;
+        if (mine) turn ^= 1;
+        if (elect_one()) {
+          if (mine) umma_commit(bar(F_PV + h));
+          umma_commit(bar(F_VFREE + st));
+        }
+        __syncwarp();
       }
     }
     __syncwarp();
@@ -362,16 +437,16 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     }
   } else {
     // ------------------------------------------------------------------ softmax and epilogue
-    const int wg = warp >> 2, in_tile = (warp & 3) * 32 + lane;
-    const uint32_t taddr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + wg * F_WG;
+    const int wg = warp >> 2, quarter = warp & 3;
+    const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + wg * F_WG;
     const float sl2 = c.p.scale * LOG2E;
     const float2 sl2v = make_float2(sl2, sl2);
     // the next piece that has keys and rows for this warpgroup; queries without keys are finished on the way
     auto next = [&](int i) {
-      for (i = find(i); i < total; i = find(i + gridDim.x)) {
+      for (i = find(i, w); i < all.total; i = find(i + gridDim.x, w)) {
         if (w.x0 + wg * RT >= w.r.q_len) continue;
         if (w.r.k_len > 0) break;
-        const int row = w.x0 + wg * RT + in_tile;
+        const int row = w.x0 + wg * RT + quarter * 32 + lane;
         if (row < w.r.q_len) {
           const int64_t at = (int64_t)w.r.q_begin + row;
           bf16* out = static_cast<bf16*>(c.out) + at * c.ldo + (int64_t)w.head * d;
@@ -381,12 +456,12 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       }
       return i;
     };
-    int g = 0, seen = 0;                                         // tiles and pieces of this warpgroup so far
+    int turn = 0, seen = 0;                                      // parities: tiles and pieces of this warpgroup so far
     // this thread's query of the next piece into tensor memory (the scores that used the last one are complete)
     auto load_query = [&] {
-      if (!warp_wait(bar(F_QFULL + wg), seen & 1, abort_flag, LONG_WAIT_CYCLES)) return false;
-      ++seen;
-      row_to_tmem<SLABS>(taddr + F_O + d, sb + wg * L::QTILE, in_tile, d);
+      if (!warp_wait(bar(F_QFULL + wg), seen, abort_flag, LONG_WAIT_CYCLES)) return false;
+      seen ^= 1;
+      row_to_tmem<SLABS>(taddr + F_O + d, sb + wg * L::TILE, quarter * 32 + lane, d);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -397,50 +472,49 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       return true;
     };
     int i = next(blockIdx.x);
-    bool ok = !XT || i >= total || load_query();
-    while (i < total && ok) {
-      const Piece now = w;
-      const int n = (now.r.k_len + CT - 1) / CT, row = now.x0 + wg * RT + in_tile;
-      const bool warp_active = now.x0 + wg * RT + (warp & 3) * 32 < now.r.q_len;
+    bool ok = !XT || i >= all.total || load_query();
+    while (i < all.total && ok) {
+      const int head = w.head, k_len = w.r.k_len, row0 = w.x0 + wg * RT + quarter * 32;
+      const int rows = min(32, w.r.q_len - row0);                // of this warp that exist; none if not positive
+      const int64_t at0 = (int64_t)w.r.q_begin + row0;
+      i = next(i + gridDim.x);                                   // looked up while the first scores are computed
       float m = -INFINITY, l = 0.f;                              // row maximum in use (raw scores), row sum
-      for (int j = 0; j < n; ++j, ++g) {
-        const int b = g & 1, here = min(CT, now.r.k_len - j * CT);
-        const uint32_t s_col = taddr + b * CT;
+      for (int k0 = 0; k0 < k_len; k0 += RT) {
+        const int here = min(RT, k_len - k0);
         // a warpgroup without rows in the pieces before this one waits for all of them: what bounds the wait is
         // the limit of the warps that are at work
-        if (!warp_wait(bar(F_S + 2 * wg + b), (g >> 1) & 1, abort_flag, j == 0 ? LONG_WAIT_CYCLES : WAIT_LIMIT_CYCLES)) { ok = false; break; }
+        if (!warp_wait(bar(F_S + wg), turn, abort_flag, k0 == 0 ? LONG_WAIT_CYCLES : WAIT_LIMIT_CYCLES)) { ok = false; break; }
         tc_fence_after();
-        if (warp_active) {
-          uint32_t x[2][32];
-          tmem_ld32(s_col, x[0]);
-          tmem_ld32(s_col + 32, x[1]);
+        if (rows > 0) {
+          uint32_t x[2][32], y[2][32], pk[16];
+          tmem_ld32(taddr, x[0]);
+          tmem_ld32(taddr + 32, x[1]);
           tmem_ld_wait_for(x[0]);
           tmem_ld_wait_for(x[1]);
-          if (here < CT) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (32 * h + e >= here) x[h][e] = 0xff800000u;   // keys behind the end: minus infinity
+          if (here > 64) {
+            tmem_ld32(taddr + 64, y[0]);
+            tmem_ld32(taddr + 96, y[1]);
           }
-          float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              asm("max.f32 %0, %0, %1, %2;" : "+f"(m4[2 * h]) : "f"(__uint_as_float(x[h][e])), "f"(__uint_as_float(x[h][e + 1])));
-              asm("max.f32 %0, %0, %1, %2;" : "+f"(m4[2 * h + 1]) : "f"(__uint_as_float(x[h][e + 2])), "f"(__uint_as_float(x[h][e + 3])));
+          if (here < 64) {
+            mask_32(x[0], here);
+            mask_32(x[1], here - 32);
+          }
+          float top = max_32(x[1], max_32(x[0], -INFINITY));
+          if (here > 64) {
+            tmem_ld_wait_for(y[0]);
+            tmem_ld_wait_for(y[1]);
+            if (here < RT) {
+              mask_32(y[0], here - 64);
+              mask_32(y[1], here - 96);
             }
+            top = max_32(y[1], max_32(y[0], top));
           }
-          const float top = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
           const bool grow = (top - m) * sl2 > 8.f;               // false for NaN and for -infinity over -infinity
           if (__any_sync(0xffffffffu, grow)) {
             const float factor = grow ? (m == -INFINITY ? 0.f : ex2_approx((m - top) * sl2)) : 1.f;
             if (grow) m = top;
             l *= factor;
-            if (j > 0) {
-              if (!warp_wait(bar(F_PV + 2 * wg + (b ^ 1)), ((g - 1) >> 1) & 1, abort_flag)) { ok = false; break; }
-              tc_fence_after();
+            if (k0 > 0) {                                        // the products of the last tile are complete: these scores are
               for (int e = 0; e < d / 16; ++e) {
                 uint32_t o[16];
                 tmem_ld16(taddr + F_O + (uint32_t)(16 * e), o);
@@ -451,43 +525,47 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
               }
             }
           }
-          // p = exp2((s - m) sl2), row sum, P (bf16 pairs) over the scores
+          // p = exp2((s - m) sl2), row sum, P (bf16 pairs) over scores that have been read
           const float nm = m == -INFINITY ? 0.f : -m * sl2;
           const float2 nmv = make_float2(nm, nm);
           float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float2 y = __ffma2_rn(make_float2(__uint_as_float(x[h][2 * e]), __uint_as_float(x[h][2 * e + 1])), sl2v, nmv);
-              const float2 p = make_float2(ex2_approx(y.x), ex2_approx(y.y));
-              l2[e & 1] = __fadd2_rn(l2[e & 1], p);
-              pk[e] = pack_bf16(p.x, p.y);
-            }
-            tmem_st16(s_col + (uint32_t)(16 * h), pk);
+          exp_32(x[0], sl2v, nmv, l2, pk);
+          tmem_st16(taddr, pk);
+          exp_32(x[1], sl2v, nmv, l2, pk);
+          tmem_st16(taddr + 16, pk);
+          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(F_P + 2 * wg));
+          if (here > 64) {
+            exp_32(y[0], sl2v, nmv, l2, pk);
+            tmem_st16(taddr + 64, pk);
+            exp_32(y[1], sl2v, nmv, l2, pk);
+            tmem_st16(taddr + 80, pk);
+            tmem_st_wait();
           }
           l2[0] = __fadd2_rn(l2[0], l2[1]);
           l += l2[0].x + l2[0].y;
-          tmem_st_wait();
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar(F_P + 2 * wg + 1));
+        } else {
+          tc_fence_before();
+          if (lane == 0) {
+            mbar_arrive(bar(F_P + 2 * wg));
+            mbar_arrive(bar(F_P + 2 * wg + 1));
+          }
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar(F_P + 2 * wg + b));
+        turn ^= 1;
       }
       if (!ok) break;
-      i = next(i + gridDim.x);
-      if (XT && i < total && !load_query()) break;
-      if (!warp_wait(bar(F_PV + 2 * wg + ((g - 1) & 1)), ((g - 1) >> 1) & 1, abort_flag)) break;
+      if (XT && i < all.total && !load_query()) break;
+      if (!warp_wait(bar(F_PV + wg), turn ^ 1, abort_flag)) break;
       tc_fence_after();
-      if (warp_active) {
-        const bool there = row < now.r.q_len;
-        const int64_t at = (int64_t)now.r.q_begin + row;
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
-        bf16* out = static_cast<bf16*>(c.out) + at * c.ldo + (int64_t)now.head * d;
-#pragma unroll
-        for (int s = 0; s < SLABS; ++s) store_row(out + 64 * s, taddr + F_O + 64 * s, d - 64 * s, inv, there);
-        if (there) c.lse[(int64_t)now.head * c.p.q_rows + at] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
+      if (rows > 0) {
+        store_rows(static_cast<bf16*>(c.out) + at0 * c.ldo + (int64_t)head * d, c.ldo, taddr + F_O, d, l == 0.f ? 0.f : 1.0f / l, rows,
+                   sb + L::OFF_OUT + warp * 2048, lane);
+        if (lane < rows) c.lse[(int64_t)head * c.p.q_rows + at0 + lane] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
       }
     }
   }
@@ -497,7 +575,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
   __syncthreads();
   tc_fence_after();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(c.dev_status, (int)VIT_ERR_TIMEOUT);
-  if (warp == MMA_WARP) {
+  if (warp == F_MMA_WARP) {
     __syncwarp();
     tmem_dealloc(tmem, TMEM_ALL);
   }
@@ -512,40 +590,41 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
 //         dv += P Y2, dk += dS Y1
 // Seven products instead of the five of a single pass, but every gradient is summed in one place in a fixed
 // order.  Two warpgroups take the tiles in turn, each with its own columns of tensor memory for S and dP:
-// while one is in its exp2 phase the tensor core works for the other.  X is in tensor memory (XT) where it
-// fits beside the accumulators: always for DQ, up to d = 80 for DKDV.
+// while one is in its exp2 phase the tensor core works for the other; one warp issues the scores, another the
+// second products.  X is in tensor memory (XT) where it fits beside the accumulators: always for DQ, up to
+// d = 80 for DKDV.
 struct BackwardMaps { CUtensorMap x1, x2, x3, y1, y2; };
+constexpr int B_MMA_WARP = 8 /* two */, B_TMA_WARP = 10, B_THREADS = 352;
 
-template <int SLABS, bool DKDV, bool XT>
+template <int SLABS, bool DKDV>
 struct BackwardCfg {
   static constexpr int XS = DKDV ? 2 : 3;              // tiles of X in shared memory; DQ: out, for delta
-  static constexpr int STAGES = SLABS == 1 ? 6 : DKDV ? 4 : 3;
+  static constexpr int STAGES = SLABS == 1 ? 5 : DKDV ? 4 : 3;
   static constexpr uint32_t XTILE = SLABS * RT * 128, YTILE = SLABS * CT * 128;
   static constexpr uint32_t OFF_Y = XS * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // DKDV: float [STAGES][2][64] -lse2, -delta of the columns
   static constexpr uint32_t OFF_ROW = OFF_COL + (DKDV ? STAGES * CT * 8 : 0);           // DQ: float2 [2][128] of the rows
-  static constexpr uint32_t OFF_BARS = OFF_ROW + (DKDV ? 0 : 2 * RT * 8), OFF_SEQ = OFF_BARS + 512;
+  static constexpr uint32_t OFF_OUT = OFF_ROW + (DKDV ? 0 : 2 * RT * 8), OFF_BARS = OFF_OUT + 8 * 2048, OFF_SEQ = OFF_BARS + 512;
   static constexpr uint32_t BYTES = OFF_SEQ + OFFSETS_BYTES + 1024;
   static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
 // columns: S and dP of the two warpgroups, then the accumulators (d each), then X1 and X2 (d / 2 each)
 constexpr uint32_t B_WG = 2 * CT, B_COLS = 2 * B_WG;
 enum BwdBar : int {
-  B_FULL = 0, B_FREE = B_FULL + 6, B_XS = B_FREE + 6 /* X in shared memory */, B_XSFREE, B_X /* in tensor memory */, B_XFREE, B_S, B_P = B_S + 2, B_SFREE = B_P + 2, B_ACC = B_SFREE + 2, B_ACCFREE,
-  B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 2
+  B_FULL = 0, B_FREE = B_FULL + 5, B_XS = B_FREE + 5 /* X in shared memory */, B_XSFREE, B_X /* in tensor memory */, B_XFREE,
+  B_S /* [wg] */, B_P = B_S + 2, B_SFREE = B_P + 2, B_ACC = B_SFREE + 2, B_ACCFREE, B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 2
 };
 
 template <int SLABS, bool DKDV, bool XT>
-__global__ void __launch_bounds__(TC_THREADS, 1)
-packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, int total, int tiles) {
-  using L = BackwardCfg<SLABS, DKDV, XT>;
+__global__ void __launch_bounds__(B_THREADS, 1)
+packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, const Pieces all) {
+  using L = BackwardCfg<SLABS, DKDV>;
   extern __shared__ uint8_t smem_raw[];
-  const int d = c.p.d, group = c.p.heads / c.p.kv_heads, x_heads = DKDV ? c.p.kv_heads : c.p.heads;
+  const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t sb = smem_u32(smem);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::OFF_BARS);
-  auto bar = [&](int i) { return smem_u32(&bars[i]); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(&bars[B_BARS]);
+  const uint32_t sb = smem_u32(smem), bars = sb + L::OFF_BARS;
+  auto bar = [&](int i) { return bars + (uint32_t)(8 * i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + L::OFF_BARS + 8 * B_BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   if (threadIdx.x == 0) {
     *abort_flag = 0;
@@ -553,7 +632,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       mbar_init(bar(i), i == B_P || i == B_P + 1 ? 4 : i == B_ACCFREE || i == B_X || (XT && i == B_XSFREE) ? 8 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
+  if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
   vit_attention_problem p = c.p;
   stage_offsets(p, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ));
   tc_fence_before();
@@ -562,19 +641,17 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   const uint32_t tmem = uniform(*tmem_slot);
   const uint32_t acc2 = B_COLS, acc1 = B_COLS + d, x1_col = B_COLS + (DKDV ? 2 : 1) * d, x2_col = x1_col + d / 2;   // dk or dq; dv
   Piece w;
-  auto find = [&](int i) { return find_piece(p, c.dev_status, i, total, tiles, x_heads, RT, DKDV, w); };
+  auto find = [&](int i) { return find_piece(p, c.dev_status, i, all, RT, DKDV, w); };
   // tiles of Y that a piece walks over, head after head
-  auto y_tiles_of = [&](const Piece& p) { return ((DKDV ? p.r.q_len : p.r.k_len) + CT - 1) / CT; };
+  auto y_tiles_of = [&] { return ((DKDV ? w.r.q_len : w.r.k_len) + CT - 1) / CT; };
 
-  if (warp >= MMA_WARP) give_registers();
-  else take_registers();
-  if (warp > TMA_WARP) {
-  } else if (warp == TMA_WARP) {
+  if (warp == B_TMA_WARP) {
     // ------------------------------------------------------------------ producer (the whole warp keeps step)
-    int t0 = 0, pieces = 0, armed = 0;
+    Ring<L::STAGES> ring;
+    int pieces = 0, n_all = 0;
     bool ok = true;
-    for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
-      const int y_tiles = y_tiles_of(w), n = DKDV ? group * y_tiles : y_tiles;
+    for (int i = find(blockIdx.x); i < all.total && ok; i = find(i + gridDim.x)) {
+      const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles;
       const int y_begin = DKDV ? w.r.q_begin : w.r.k_begin, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
       if (!warp_wait(bar(B_XSFREE), (pieces & 1) ^ 1, abort_flag)) break;
@@ -588,9 +665,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         }
       }
       ++pieces;
-      int yt = 0, yh = DKDV ? w.head * group : w.head / group;
-      for (int t = t0; t < t0 + n; ++t) {
-        const int st = t % L::STAGES, ph = (t / L::STAGES) & 1, y0 = yt * CT;
+      int y0 = 0, yh = DKDV ? w.head * group : group == 1 ? w.head : w.head / group;
+      for (int t = 0; t < n; ++t, ring.step()) {
+        const int st = ring.at;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE;
         // DKDV: the numbers of the tile's columns travel with it, negated; beyond the sequence
         // P = exp2(0 - infinity) = 0 and dS = 0.  They are in flight while this warp waits for the stage.
@@ -602,7 +679,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
             if (y0 + 32 * e + lane < y_len) v[e] = c.delta[(int64_t)yh * c.p.q_rows + y_begin + y0 + 32 * e + lane];
           }
         }
-        if (!warp_wait(bar(B_FREE + st), ph ^ 1, abort_flag)) { ok = false; break; }
+        if (!warp_wait(bar(B_FREE + st), ring.parity ^ 1, abort_flag)) { ok = false; break; }
         if (DKDV) {
           float* col = reinterpret_cast<float*>(smem + L::OFF_COL) + st * 2 * CT;
 #pragma unroll
@@ -612,7 +689,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
           }
           __syncwarp();
         }
-        armed = t + 1;
+        ++n_all;
         if (lane == 0) {
           mbar_arrive_expect_tx(bar(B_FULL + st), 2 * L::YTILE);
           for (int s = 0; s < SLABS; ++s) {
@@ -620,37 +697,36 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
             tma_load_3d(y + L::YTILE + s * CT * 128, &maps.y2, 64 * s, yh, y_begin + y0, bar(B_FULL + st));
           }
         }
-        if (++yt == y_tiles) { yt = 0; ++yh; }
+        y0 += CT;
+        if (y0 >= y_len) { y0 = 0; ++yh; }
       }
-      t0 += n;
     }
     __syncwarp();
     if (*abort_flag && lane == 0) {
       // a wait gave up somewhere: let the copies that were started land before the block leaves
       volatile int never = 0;
       if (pieces) mbar_wait_limit(bar(B_XS), (pieces - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
-      for (int t = armed > L::STAGES ? armed - L::STAGES : 0; t < armed; ++t)
+      for (int t = n_all > L::STAGES ? n_all - L::STAGES : 0; t < n_all; ++t)
         mbar_wait_limit(bar(B_FULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
     }
-  } else if (warp >= MMA_WARP) {
+  } else if (warp >= B_MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuers (whole warps keep step): one of the
     // scores, one of the second products
-    const bool scores = warp == MMA_WARP;
-    int t0 = 0, pieces = 0;
-    uint32_t phase = 0;                                          // bit b: parity of the next wait for warpgroup b's columns
+    const bool scores = warp == B_MMA_WARP;
+    Ring<L::STAGES> ring;
+    int pieces = 0, phase = 0;                                   // bit b of phase: parity of the next wait for warpgroup b's columns
     bool ok = true;
-    for (int i = find(blockIdx.x); i < total && ok; i = find(i + gridDim.x)) {
-      const int y_tiles = y_tiles_of(w), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
+    for (int i = find(blockIdx.x); i < all.total && ok; i = find(i + gridDim.x)) {
+      const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
       if (scores && !warp_spin(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
-      const int last = y_len - (y_tiles - 1) * CT;               // rows of a head's last tile
-      int yt = 0;                                                // tile of its head
-      for (int t = 0; t < n; ++t) {
-        const int st = (t0 + t) % L::STAGES, b = t & 1, here = yt == y_tiles - 1 ? last : CT, n16 = (here + 15) / 16;
+      int left = y_len;                                          // rows of this head from the present tile on
+      for (int t = 0; t < n; ++t, ring.step()) {
+        const int st = ring.at, b = t & 1, here = min(CT, left), n16 = (here + 15) / 16;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + b * B_WG;
-        if (++yt == y_tiles) yt = 0;
+        left = left > CT ? left - CT : y_len;
         if (scores) {
-          if (!warp_spin(bar(B_FULL + st), ((t0 + t) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
+          if (!warp_spin(bar(B_FULL + st), ring.parity, abort_flag)) { ok = false; break; }
           // rows of Y behind the end of the sequence become zero, whatever lies there: they meet weights of
           // zero in the second products, and give scores of zero in the first
           if (here < 16 * n16) {
@@ -659,28 +735,28 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
           }
           // S and dP overwrite P and dS of tile t - 2, once their products are complete
           if (!warp_spin(bar(B_SFREE + b), (phase >> b & 1) ^ 1, abort_flag)) { ok = false; break; }
-          phase ^= 1u << b;
+          phase ^= 1 << b;
           if (elect_one()) {
             tc_fence_after();
             if (XT) {
-              issue_scores_ts<SLABS>(s_col, tmem + x1_col, y, 16 * n16, d / 16);
-              issue_scores_ts<SLABS>(s_col + CT, tmem + x2_col, y + L::YTILE, 16 * n16, d / 16);
+              issue_scores_ts<SLABS, CT>(s_col, tmem + x1_col, y, 16 * n16, d / 16);
+              issue_scores_ts<SLABS, CT>(s_col + CT, tmem + x2_col, y + L::YTILE, 16 * n16, d / 16);
             } else {
-              issue_scores_ss<SLABS>(s_col, sb, y, 16 * n16, d / 16);
-              issue_scores_ss<SLABS>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
+              issue_scores_ss<SLABS, CT>(s_col, sb, y, 16 * n16, d / 16);
+              issue_scores_ss<SLABS, CT>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
             }
             umma_commit(bar(B_S + b));
             if (t == n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE));
           }
         } else {
           if (!warp_spin(bar(B_P + b), phase >> b & 1, abort_flag)) { ok = false; break; }
-          phase ^= 1u << b;
+          phase ^= 1 << b;
           // the accumulators of the last piece have been read
           if (t == 0 && !warp_spin(bar(B_ACCFREE), (pieces & 1) ^ 1, abort_flag)) { ok = false; break; }
           if (elect_one()) {
             tc_fence_after();
-            if (DKDV) issue_weighted(tmem + acc1, s_col, y + L::YTILE, d, n16, t == 0);
-            issue_weighted(tmem + acc2, s_col + CT, y, d, n16, t == 0);
+            if (DKDV) issue_weighted<CT>(tmem + acc1, s_col, y + L::YTILE, d, n16, t == 0);
+            issue_weighted<CT>(tmem + acc2, s_col + CT, y, d, n16, t == 0);
             umma_commit(bar(B_SFREE + b));
             umma_commit(bar(B_FREE + st));
             if (t == n - 1) umma_commit(bar(B_ACC));
@@ -688,40 +764,37 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         }
         __syncwarp();                                            // lanes that poll would hold up the one that issues
       }
-      t0 += n;
       ++pieces;
     }
     __syncwarp();
     if (*abort_flag && lane == 0) {
       volatile int never = 0;
-      umma_commit(bar(B_DRAIN + warp - MMA_WARP));
-      mbar_wait_limit(bar(B_DRAIN + warp - MMA_WARP), 0, &never, DRAIN_LIMIT_CYCLES);
+      umma_commit(bar(B_DRAIN + warp - B_MMA_WARP));
+      mbar_wait_limit(bar(B_DRAIN + warp - B_MMA_WARP), 0, &never, DRAIN_LIMIT_CYCLES);
     }
   } else {
     // ------------------------------------------------------------------ probabilities and their gradients
-    const int wg = warp >> 2, in_tile = (warp & 3) * 32 + lane;
-    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    const uint32_t taddr = lanes + wg * B_WG;
+    const int wg = warp >> 2, quarter = warp & 3, in_tile = quarter * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t taddr = lanes + wg * B_WG, stage = sb + L::OFF_OUT + warp * 2048;
     const float sl2 = c.p.scale * LOG2E;
     const float2 sl2v = make_float2(sl2, sl2);
-    int pieces = 0, t0 = 0;
-    uint32_t s_phase = 0;
-    bool ok = true;
-    auto grad1 = [&](const Piece& p, int64_t at) { return static_cast<bf16*>(c.dv) + at * c.lddv + (int64_t)p.head * d; };
-    auto grad2 = [&](const Piece& p, int64_t at) {
-      return DKDV ? static_cast<bf16*>(c.dk) + at * c.lddk + (int64_t)p.head * d : static_cast<bf16*>(c.dq) + at * c.lddq + (int64_t)p.head * d;
-    };
+    Ring<L::STAGES> ring;                                        // of every tile, this warpgroup's or not
+    int pieces = 0, s_phase = 0;
     // the next piece with something to walk over; rows that nothing meets get gradients of zero on the way
     auto next = [&](int i) {
-      for (i = find(i); i < total; i = find(i + gridDim.x)) {
-        if (y_tiles_of(w) > 0) break;
+      for (i = find(i); i < all.total; i = find(i + gridDim.x)) {
+        if (y_tiles_of() > 0) break;
         const int row = w.x0 + in_tile;
         const int64_t at = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row;
-        if (wg == 0 && row < (DKDV ? w.r.k_len : w.r.q_len))
+        if (wg == 0 && row < (DKDV ? w.r.k_len : w.r.q_len)) {
+          bf16* g2 = DKDV ? static_cast<bf16*>(c.dk) + at * c.lddk + (int64_t)w.head * d : static_cast<bf16*>(c.dq) + at * c.lddq + (int64_t)w.head * d;
+          bf16* g1 = static_cast<bf16*>(c.dv) + at * c.lddv + (int64_t)w.head * d;
           for (int e = 0; e < d; e += 8) {
-            *reinterpret_cast<uint4*>(grad2(w, at) + e) = make_uint4(0u, 0u, 0u, 0u);
-            if (DKDV) *reinterpret_cast<uint4*>(grad1(w, at) + e) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(g2 + e) = make_uint4(0u, 0u, 0u, 0u);
+            if (DKDV) *reinterpret_cast<uint4*>(g1 + e) = make_uint4(0u, 0u, 0u, 0u);
           }
+        }
       }
       return i;
     };
@@ -759,12 +832,11 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       return true;
     };
     int i = next(blockIdx.x);
-    ok = !XT || i >= total || load_x();
-    while (i < total && ok) {
-      const Piece now = w;
-      const int y_tiles = y_tiles_of(now), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? now.r.q_len : now.r.k_len;
-      const int x_len = DKDV ? now.r.k_len : now.r.q_len, row = now.x0 + in_tile;
-      const bool warp_active = now.x0 + (warp & 3) * 32 < x_len;
+    bool ok = !XT || i >= all.total || load_x();
+    while (i < all.total && ok) {
+      const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
+      const int head = w.head, row0 = w.x0 + quarter * 32, rows = min(32, (DKDV ? w.r.k_len : w.r.q_len) - row0);
+      const int64_t at0 = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row0;
       float2 nls = make_float2(0.f, 0.f), nde = nls;             // DQ: of this thread's row
       if (!DKDV) {
         if (!warp_wait(bar(B_X), pieces & 1, abort_flag)) break;
@@ -772,61 +844,57 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         nls = make_float2(-mine.x, -mine.x);
         nde = make_float2(-mine.y, -mine.y);
       }
-      int yt = wg % y_tiles;                                     // DKDV: tile of its head
-      for (int t = wg; t < n; t += 2) {
-        const int here = (DKDV ? yt : t) == y_tiles - 1 ? y_len - (y_tiles - 1) * CT : CT, nch = (here + 31) / 32;
-        const int st = (t0 + t) % L::STAGES;
+      int left = y_len;                                          // rows of this head from the present tile on
+      for (int t = 0; t < n; ++t, ring.step()) {
+        const int here = min(CT, left);
+        left = left > CT ? left - CT : y_len;
+        if ((t & 1) != wg) continue;
+        const int st = ring.at;
         const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2);   // four columns each: -lse2, then -delta
-        if (DKDV) {
-          yt = (yt + 2) % y_tiles;
-          if (!warp_wait(bar(B_FULL + st), ((t0 + t) / L::STAGES) & 1, abort_flag)) { ok = false; break; }
-        }
+        if (DKDV && !warp_wait(bar(B_FULL + st), ring.parity, abort_flag)) { ok = false; break; }
         if (!warp_wait(bar(B_S + wg), s_phase, abort_flag)) { ok = false; break; }
         s_phase ^= 1;
         tc_fence_after();
-        if (warp_active) {
-          uint32_t s[2][32], g[2][32];
-          tmem_ld32(taddr, s[0]);
-          tmem_ld32(taddr + CT, g[0]);
-          tmem_ld_wait_for(s[0]);
-          tmem_ld_wait_for(g[0]);
-          if (nch > 1) {
-            tmem_ld32(taddr + 32, s[1]);
-            tmem_ld32(taddr + CT + 32, g[1]);
-          }
+        if (rows > 0) {
+          // 16 columns at a time, those of the next step on their way
+          uint32_t s[2][16], g[2][16];
+          tmem_ld16(taddr, s[0]);
+          tmem_ld16(taddr + CT, g[0]);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (h >= nch) break;
-            if (h == 1) {
-              tmem_ld_wait_for(s[1]);
-              tmem_ld_wait_for(g[1]);
+          for (int h = 0; h < 4; ++h) {
+            if (16 * h >= here) break;
+            uint32_t (&sh)[16] = s[h & 1], (&gh)[16] = g[h & 1];
+            tmem_ld_wait_16(sh, gh);
+            if (h < 3 && 16 * (h + 1) < here) {
+              tmem_ld16(taddr + 16 * (h + 1), s[(h + 1) & 1]);
+              tmem_ld16(taddr + CT + 16 * (h + 1), g[(h + 1) & 1]);
             }
-            uint32_t pk[16], dk[16];
-            const int left = here - 32 * h;
+            uint32_t pk[8], dk[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) {
+            for (int q = 0; q < 4; ++q) {
               float4 a4 = make_float4(nls.x, nls.x, nls.x, nls.x), b4 = make_float4(nde.x, nde.x, nde.x, nde.x);
               if (DKDV) {
-                a4 = col[8 * h + q];
-                b4 = col[CT / 4 + 8 * h + q];
+                a4 = col[4 * h + q];
+                b4 = col[CT / 4 + 4 * h + q];
               }
 #pragma unroll
               for (int f = 0; f < 2; ++f) {
                 const int e = 2 * q + f;
                 const float2 a = f ? make_float2(a4.z, a4.w) : make_float2(a4.x, a4.y), b = f ? make_float2(b4.z, b4.w) : make_float2(b4.x, b4.y);
-                const float2 x = __ffma2_rn(make_float2(__uint_as_float(s[h][2 * e]), __uint_as_float(s[h][2 * e + 1])), sl2v, a);
-                float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                if (!DKDV && left < 32) {                        // keys behind the end
-                  if (2 * e >= left) p.x = 0.f;
-                  if (2 * e + 1 >= left) p.y = 0.f;
+                const float2 x = __ffma2_rn(make_float2(__uint_as_float(sh[2 * e]), __uint_as_float(sh[2 * e + 1])), sl2v, a);
+                float2 pr = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                if (!DKDV && here < CT) {                        // keys behind the end
+                  if (16 * h + 2 * e >= here) pr.x = 0.f;
+                  if (16 * h + 2 * e + 1 >= here) pr.y = 0.f;
                 }
-                const float2 y = __fmul2_rn(p, __fadd2_rn(make_float2(__uint_as_float(g[h][2 * e]), __uint_as_float(g[h][2 * e + 1])), b));
-                if (DKDV) pk[e] = pack_bf16(p.x, p.y);
+                const float2 y = __fmul2_rn(pr, __fadd2_rn(make_float2(__uint_as_float(gh[2 * e]), __uint_as_float(gh[2 * e + 1])), b));
+                if (DKDV) pk[e] = pack_bf16(pr.x, pr.y);
                 dk[e] = pack_bf16(y.x, y.y);
               }
             }
-            if (DKDV) tmem_st16(taddr + (uint32_t)(16 * h), pk);
-            tmem_st16(taddr + (uint32_t)(CT + 16 * h), dk);
+            // over scores that have been read: step h takes columns [8 h, 8 h + 8)
+            if (DKDV) tmem_st8(taddr + 8 * h, pk);
+            tmem_st8(taddr + CT + 8 * h, dk);
           }
           tmem_st_wait();
         }
@@ -835,10 +903,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         if (lane == 0) mbar_arrive(bar(B_P + wg));
       }
       if (!ok) break;
-      t0 += n;
       ++pieces;
       i = next(i + gridDim.x);
-      if (XT && i < total) {
+      if (XT && i < all.total) {
         // every score of the last piece is complete: its X may be overwritten
         if (!warp_wait(bar(B_XFREE), (pieces - 1) & 1, abort_flag)) break;
         tc_fence_after();
@@ -846,17 +913,15 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       }
       if (!warp_wait(bar(B_ACC), (pieces - 1) & 1, abort_flag)) break;
       tc_fence_after();
-      if (warp_active) {
-        const int64_t at = (int64_t)(DKDV ? now.r.k_begin : now.r.q_begin) + row;
-        const bool there = row < x_len;
-        // DKDV: dk by the first warpgroup, dv by the second; DQ: halves of the head
-        if (DKDV) {
-          bf16* to = wg == 0 ? grad2(now, at) : grad1(now, at);
-#pragma unroll
-          for (int s = 0; s < SLABS; ++s) store_row(to + 64 * s, lanes + (wg == 0 ? acc2 : acc1) + 64 * s, d - 64 * s, wg == 0 ? c.p.scale : 1.f, there);
-        } else {
-          const int half = d / 32 * 16, from = wg == 0 ? 0 : half;
-          store_row(grad2(now, at) + from, lanes + acc2 + from, wg == 0 ? half : d - half, c.p.scale, there);
+      if (rows > 0) {
+        if (DKDV) {                                              // dk by the first warpgroup, dv by the second
+          const int64_t ld = wg == 0 ? c.lddk : c.lddv;
+          store_rows(static_cast<bf16*>(wg == 0 ? c.dk : c.dv) + at0 * ld + (int64_t)head * d, ld, lanes + (wg == 0 ? acc2 : acc1), d,
+                     wg == 0 ? c.p.scale : 1.f, rows, stage, lane);
+        } else {                                                 // a part of the head each
+          const int from = wg == 0 ? 0 : d / 32 * 16, to = wg == 0 ? d / 32 * 16 : d;
+          store_rows(static_cast<bf16*>(c.dq) + at0 * c.lddq + (int64_t)head * d + from, c.lddq, lanes + acc2 + from, to - from, c.p.scale, rows,
+                     stage, lane);
         }
       }
       tc_fence_before();
@@ -870,7 +935,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   __syncthreads();
   tc_fence_after();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(c.dev_status, (int)VIT_ERR_TIMEOUT);
-  if (warp == MMA_WARP) {
+  if (warp == B_MMA_WARP) {
     __syncwarp();
     tmem_dealloc(tmem, TMEM_ALL);
   }
@@ -905,12 +970,12 @@ bool encode_heads(CUtensorMap* tm, const void* base, int64_t rows, int heads, in
 
 template <int SLABS, bool XT>
 cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
-  using L = ForwardCfg<SLABS, XT>;
+  using L = ForwardCfg<SLABS>;
   ForwardMaps m;
   if (!encode_heads(&m.q, c.q, c.p.q_rows, c.p.heads, c.p.d, c.ldq, RT)) return cudaErrorInvalidValue;
   if (c.p.k_rows > 0) {
-    if (!encode_heads(&m.k, c.k, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldk, CT)) return cudaErrorInvalidValue;
-    if (!encode_heads(&m.v, c.v, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldv, CT)) return cudaErrorInvalidValue;
+    if (!encode_heads(&m.k, c.k, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldk, RT)) return cudaErrorInvalidValue;
+    if (!encode_heads(&m.v, c.v, c.p.k_rows, c.p.kv_heads, c.p.d, c.ldv, RT)) return cudaErrorInvalidValue;
   } else {
     m.k = m.v = m.q;                                   // no keys at all: never used
   }
@@ -919,13 +984,13 @@ cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
   const int sms = current_device_sm_count();
   if (sms < 1) return cudaErrorInvalidDevice;
   const int tiles = (c.p.max_q + 2 * RT - 1) / (2 * RT), total = c.p.sequences * c.p.heads * tiles;
-  packed_forward_tc_kernel<SLABS, XT><<<total < sms ? total : sms, TC_THREADS, L::BYTES, s>>>(m, c, total, tiles);
+  packed_forward_tc_kernel<SLABS, XT><<<total < sms ? total : sms, F_THREADS, L::BYTES, s>>>(m, c, Pieces{total, divisor(tiles), divisor(c.p.heads)});
   return cudaGetLastError();
 }
 
 template <int SLABS, bool DKDV, bool XT>
 cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
-  using L = BackwardCfg<SLABS, DKDV, XT>;
+  using L = BackwardCfg<SLABS, DKDV>;
   BackwardMaps m;
   const void *x1 = DKDV ? c.k : c.q, *x2 = DKDV ? c.v : c.dout, *y1 = DKDV ? c.q : c.k, *y2 = DKDV ? c.dout : c.v;
   const int64_t lx1 = DKDV ? c.ldk : c.ldq, lx2 = DKDV ? c.ldv : c.lddo, ly1 = DKDV ? c.ldq : c.ldk, ly2 = DKDV ? c.lddo : c.ldv;
@@ -944,13 +1009,13 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
   const int sms = current_device_sm_count();
   if (sms < 1) return cudaErrorInvalidDevice;
   const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT, total = c.p.sequences * xh * tiles;
-  packed_backward_tc_kernel<SLABS, DKDV, XT><<<total < sms ? total : sms, TC_THREADS, L::BYTES, s>>>(m, c, total, tiles);
+  packed_backward_tc_kernel<SLABS, DKDV, XT><<<total < sms ? total : sms, B_THREADS, L::BYTES, s>>>(m, c, Pieces{total, divisor(tiles), divisor(xh)});
   return cudaGetLastError();
 }
 
 }  // namespace
 
-// Columns of tensor memory decide where a piece's rows are held: 2 x 64 + d + d / 2 of a warpgroup's 256 in
+// Columns of tensor memory decide where a piece's rows are held: 128 + d + d / 2 of a warpgroup's 256 in
 // the forward pass, 256 + 2 d + d of 512 for dk and dv, 256 + d + d for dq.
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s) {
   if (c.p.d <= 64) return launch_forward<1, true>(c, s);
