@@ -58,24 +58,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
 __device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag, long long limit = WAIT_LIMIT_CYCLES) {
   return __all_sync(0xffffffffu, mbar_wait_limit(bar, (uint32_t)parity, abort_flag, limit));
 }
-// the same without letting the hardware suspend the warp: for the warps that issue the products, which
-// otherwise take a few hundred cycles to come back
-__device__ __forceinline__ bool mbar_test(uint32_t bar, int parity) {
-  uint32_t done;
-  asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
-               : "=r"(done) : "r"(bar), "r"((uint32_t)parity) : "memory");
-  return done != 0;
-}
-__device__ __forceinline__ bool warp_spin(uint32_t bar, int parity, volatile int* abort_flag) {
-  if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-  const long long t0 = clock64();
-  for (;;) {
-    if (__all_sync(0xffffffffu, mbar_test(bar, parity))) return true;
-    const bool late = clock64() - t0 > WAIT_LIMIT_CYCLES;
-    if (late) *abort_flag = 1;
-    if (__any_sync(0xffffffffu, late || *abort_flag)) return false;
-  }
-}
 // rows [from, rows) of a tile of `slabs` slabs become zero; one warp, then visible to the tensor core
 __device__ __forceinline__ void zero_rows(uint32_t tile, int rows, int slabs, int from, int lane) {
   for (int s = 0; s < slabs; ++s)
@@ -271,7 +253,7 @@ constexpr uint32_t F_WG = 256, F_O = RT;
 enum FwdBar : int {
   F_KFULL = 0, F_KFREE = F_KFULL + 3, F_VFULL = F_KFREE + 3, F_VFREE = F_VFULL + 3, F_QFULL = F_VFREE + 3 /* [wg] shared memory */,
   F_QFREE = F_QFULL + 2, F_Q = F_QFREE + 2 /* [wg] tensor memory */, F_S = F_Q + 2 /* [wg] */, F_P = F_S + 2 /* [wg][half] */,
-  F_PV = F_P + 4 /* [wg] */, F_DRAIN = F_PV + 2 /* [MMA warp] */, F_BARS = F_DRAIN + 2
+  F_PV = F_P + 4 /* [wg] */, F_TURN = F_PV + 2 /* [warp] */, F_DRAIN = F_TURN + 8 /* [MMA warp] */, F_BARS = F_DRAIN + 2
 };
 
 // Row sums and packed probabilities of 32 scores
@@ -387,44 +369,58 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       if (n == 0) continue;
       const bool mine = w.x0 + h * RT < w.r.q_len;               // else the stages are passed on only
       if (mine) {
-        if (!warp_spin(bar((XT ? F_Q : F_QFULL) + h), seen, abort_flag)) break;
+        if (!warp_wait(bar((XT ? F_Q : F_QFULL) + h), seen, abort_flag)) break;
         seen ^= 1;
       }
-      for (int j = 0; j < n; ++j, ring.step()) {
-        const int st = ring.at, here = min(RT, w.r.k_len - j * RT), n16 = (here + 15) / 16;
-        const uint32_t ks = sb + L::OFF_K + st * L::TILE, vs = sb + L::OFF_V + st * L::TILE;
-        if (!warp_spin(bar(F_KFULL + st), ring.parity, abort_flag)) { ok = false; break; }
-        if (elect_one()) {
-          if (mine) {
-            // the scores overwrite P of the last tile: its product was issued before, by this warp
-            tc_fence_after();
-            if (XT) issue_scores_ts<SLABS, RT>(base, base + F_O + d, ks, 16 * n16, d / 16);
-            else issue_scores_ss<SLABS, RT>(base, q_smem, ks, 16 * n16, d / 16);
-            umma_commit(bar(F_S + h));
-            if (!XT && j == n - 1) umma_commit(bar(F_QFREE + h));
-          }
-          umma_commit(bar(F_KFREE + st));
+      // the scores of tile j (the elected lane): they overwrite P of tile j - 1, whose product this warp issued before
+      auto issue_scores = [&](int j, int st) {
+        const uint32_t ks = sb + L::OFF_K + st * L::TILE;
+        if (mine) {
+          const int cols = (min(RT, w.r.k_len - j * RT) + 15) / 16 * 16;
+          if (XT) issue_scores_ts<SLABS, RT>(base, base + F_O + d, ks, cols, d / 16);
+          else issue_scores_ss<SLABS, RT>(base, q_smem, ks, cols, d / 16);
+          umma_commit(bar(F_S + h));
+          if (!XT && j == n - 1) umma_commit(bar(F_QFREE + h));
         }
-        __syncwarp();                                            // lanes that poll would hold up the one that issues
-        if (!warp_spin(bar(F_VFULL + st), ring.parity, abort_flag)) { ok = false; break; }
+        umma_commit(bar(F_KFREE + st));
+      };
+      if (!warp_wait(bar(F_KFULL + ring.at), ring.parity, abort_flag)) break;
+      if (elect_one()) {
+        tc_fence_after();
+        issue_scores(0, ring.at);
+      }
+      __syncwarp();                                              // lanes that poll would hold up the one that issues
+      for (int j = 0; j < n; ++j) {
+        const int st = ring.at, here = min(RT, w.r.k_len - j * RT), n16 = (here + 15) / 16;
+        const uint32_t vs = sb + L::OFF_V + st * L::TILE;
+        if (!warp_wait(bar(F_VFULL + st), ring.parity, abort_flag)) { ok = false; break; }
+        ring.step();
         // rows of V behind the last key meet probabilities of zero: make them zero too, whatever lies there
         // (both warps write the same zeros; neither reads before its own are there)
         if (mine && here < 16 * n16) zero_rows(vs, RT, SLABS, here, lane);
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          if (!mine || 4 * half >= n16) break;
-          if (!warp_spin(bar(F_P + 2 * h + half), turn, abort_flag)) { ok = false; break; }
-          if (elect_one()) {
-            tc_fence_after();
-            issue_weighted<RT>(base + F_O, base + 64 * half, vs + half * 64 * 128, d, n16 - 4 * half, j == 0 && half == 0);
+        // the next tile's keys, so that its scores follow this tile's last product at once
+        if (j + 1 < n && !warp_wait(bar(F_KFULL + ring.at), ring.parity, abort_flag)) { ok = false; break; }
+        if (mine) {
+          if (!warp_wait(bar(F_P + 2 * h), turn, abort_flag)) { ok = false; break; }
+          if (n16 > 4) {
+            if (elect_one()) {
+              tc_fence_after();
+              issue_weighted<RT>(base + F_O, base, vs, d, 4, j == 0);
+            }
+            __syncwarp();
+            if (!warp_wait(bar(F_P + 2 * h + 1), turn, abort_flag)) { ok = false; break; }
           }
-          __syncwarp();
+          turn ^= 1;
         }
-        if (!ok) break;
-        if (mine) turn ^= 1;
         if (elect_one()) {
-          if (mine) umma_commit(bar(F_PV + h));
+          if (mine) {
+            tc_fence_after();
+            if (n16 > 4) issue_weighted<RT>(base + F_O, base + 64, vs + 64 * 128, d, n16 - 4, false);
+            else issue_weighted<RT>(base + F_O, base, vs, d, n16, j == 0);
+            umma_commit(bar(F_PV + h));
+          }
           umma_commit(bar(F_VFREE + st));
+          if (j + 1 < n) issue_scores(j + 1, ring.at);
         }
         __syncwarp();
       }
@@ -457,6 +453,9 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       return i;
     };
     int turn = 0, seen = 0;                                      // parities: tiles and pieces of this warpgroup so far
+    // A warp of each warpgroup shares a scheduler and its exp2 unit.  They take turns there, so that one fetches
+    // its scores, finds their maximum and waits for the tensor core while the other runs its exponentials.
+    int go = 0;
     // this thread's query of the next piece into tensor memory (the scores that used the last one are complete)
     auto load_query = [&] {
       if (!warp_wait(bar(F_QFULL + wg), seen, abort_flag, LONG_WAIT_CYCLES)) return false;
@@ -477,6 +476,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       const int head = w.head, k_len = w.r.k_len, row0 = w.x0 + wg * RT + quarter * 32;
       const int rows = min(32, w.r.q_len - row0);                // of this warp that exist; none if not positive
       const int64_t at0 = (int64_t)w.r.q_begin + row0;
+      const bool pair = w.r.q_len - w.x0 > RT;
       i = next(i + gridDim.x);                                   // looked up while the first scores are computed
       float m = -INFINITY, l = 0.f;                              // row maximum in use (raw scores), row sum
       for (int k0 = 0; k0 < k_len; k0 += RT) {
@@ -486,28 +486,21 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
         if (!warp_wait(bar(F_S + wg), turn, abort_flag, k0 == 0 ? LONG_WAIT_CYCLES : WAIT_LIMIT_CYCLES)) { ok = false; break; }
         tc_fence_after();
         if (rows > 0) {
-          uint32_t x[2][32], y[2][32], pk[16];
-          tmem_ld32(taddr, x[0]);
-          tmem_ld32(taddr + 32, x[1]);
-          tmem_ld_wait_for(x[0]);
-          tmem_ld_wait_for(x[1]);
-          if (here > 64) {
-            tmem_ld32(taddr + 64, y[0]);
-            tmem_ld32(taddr + 96, y[1]);
-          }
-          if (here < 64) {
-            mask_32(x[0], here);
-            mask_32(x[1], here - 32);
-          }
-          float top = max_32(x[1], max_32(x[0], -INFINITY));
-          if (here > 64) {
-            tmem_ld_wait_for(y[0]);
-            tmem_ld_wait_for(y[1]);
-            if (here < RT) {
-              mask_32(y[0], here - 64);
-              mask_32(y[1], here - 96);
+          // row maximum; the scores of the second 64 keys are fetched a second time when it is their turn
+          uint32_t x[2][32], pk[16];
+          float top = -INFINITY;
+#pragma unroll
+          for (int h = 1; h >= 0; --h) {
+            if (64 * h >= here) continue;
+            tmem_ld32(taddr + 64 * h, x[0]);
+            tmem_ld32(taddr + 64 * h + 32, x[1]);
+            tmem_ld_wait_for(x[0]);
+            tmem_ld_wait_for(x[1]);
+            if (here < 64 * h + 64) {
+              mask_32(x[0], here - 64 * h);
+              mask_32(x[1], here - 64 * h - 32);
             }
-            top = max_32(y[1], max_32(y[0], top));
+            top = max_32(x[1], max_32(x[0], top));
           }
           const bool grow = (top - m) * sl2 > 8.f;               // false for NaN and for -infinity over -infinity
           if (__any_sync(0xffffffffu, grow)) {
@@ -525,12 +518,14 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
               }
             }
           }
+          if (pair && !warp_wait(bar(F_TURN + warp), wg == 0 ? go ^ 1 : go, abort_flag)) { ok = false; break; }
           // p = exp2((s - m) sl2), row sum, P (bf16 pairs) over scores that have been read
           const float nm = m == -INFINITY ? 0.f : -m * sl2;
           const float2 nmv = make_float2(nm, nm);
           float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
           exp_32(x[0], sl2v, nmv, l2, pk);
           tmem_st16(taddr, pk);
+          if (here > 64) tmem_ld32(taddr + 64, x[0]);
           exp_32(x[1], sl2v, nmv, l2, pk);
           tmem_st16(taddr + 16, pk);
           tmem_st_wait();
@@ -538,18 +533,26 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(F_P + 2 * wg));
           if (here > 64) {
-            exp_32(y[0], sl2v, nmv, l2, pk);
+            tmem_ld_wait_for(x[0]);
+            tmem_ld32(taddr + 96, x[1]);
+            if (here < 96) mask_32(x[0], here - 64);
+            exp_32(x[0], sl2v, nmv, l2, pk);
+            tmem_ld_wait_for(x[1]);
             tmem_st16(taddr + 64, pk);
-            exp_32(y[1], sl2v, nmv, l2, pk);
+            if (here < RT) mask_32(x[1], here - 96);
+            exp_32(x[1], sl2v, nmv, l2, pk);
             tmem_st16(taddr + 80, pk);
             tmem_st_wait();
           }
+          if (pair && lane == 0) mbar_arrive(bar(F_TURN + (warp ^ 4)));
           l2[0] = __fadd2_rn(l2[0], l2[1]);
           l += l2[0].x + l2[0].y;
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(bar(F_P + 2 * wg + 1));
         } else {
+          if (pair && !warp_wait(bar(F_TURN + warp), wg == 0 ? go ^ 1 : go, abort_flag)) { ok = false; break; }
+          if (pair && lane == 0) mbar_arrive(bar(F_TURN + (warp ^ 4)));
           tc_fence_before();
           if (lane == 0) {
             mbar_arrive(bar(F_P + 2 * wg));
@@ -557,6 +560,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
           }
         }
         turn ^= 1;
+        if (pair) go ^= 1;
       }
       if (!ok) break;
       if (XT && i < all.total && !load_query()) break;
@@ -719,14 +723,14 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     for (int i = find(blockIdx.x); i < all.total && ok; i = find(i + gridDim.x)) {
       const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
-      if (scores && !warp_spin(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
+      if (scores && !warp_wait(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
       int left = y_len;                                          // rows of this head from the present tile on
       for (int t = 0; t < n; ++t, ring.step()) {
         const int st = ring.at, b = t & 1, here = min(CT, left), n16 = (here + 15) / 16;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + b * B_WG;
         left = left > CT ? left - CT : y_len;
         if (scores) {
-          if (!warp_spin(bar(B_FULL + st), ring.parity, abort_flag)) { ok = false; break; }
+          if (!warp_wait(bar(B_FULL + st), ring.parity, abort_flag)) { ok = false; break; }
           // rows of Y behind the end of the sequence become zero, whatever lies there: they meet weights of
           // zero in the second products, and give scores of zero in the first
           if (here < 16 * n16) {
@@ -734,7 +738,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
             zero_rows(y + L::YTILE, CT, SLABS, here, lane);
           }
           // S and dP overwrite P and dS of tile t - 2, once their products are complete
-          if (!warp_spin(bar(B_SFREE + b), (phase >> b & 1) ^ 1, abort_flag)) { ok = false; break; }
+          if (!warp_wait(bar(B_SFREE + b), (phase >> b & 1) ^ 1, abort_flag)) { ok = false; break; }
           phase ^= 1 << b;
           if (elect_one()) {
             tc_fence_after();
@@ -749,10 +753,10 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
             if (t == n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE));
           }
         } else {
-          if (!warp_spin(bar(B_P + b), phase >> b & 1, abort_flag)) { ok = false; break; }
+          if (!warp_wait(bar(B_P + b), phase >> b & 1, abort_flag)) { ok = false; break; }
           phase ^= 1 << b;
           // the accumulators of the last piece have been read
-          if (t == 0 && !warp_spin(bar(B_ACCFREE), (pieces & 1) ^ 1, abort_flag)) { ok = false; break; }
+          if (t == 0 && !warp_wait(bar(B_ACCFREE), (pieces & 1) ^ 1, abort_flag)) { ok = false; break; }
           if (elect_one()) {
             tc_fence_after();
             if (DKDV) issue_weighted<CT>(tmem + acc1, s_col, y + L::YTILE, d, n16, t == 0);
