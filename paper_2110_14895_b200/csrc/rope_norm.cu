@@ -5,11 +5,12 @@
 //   y = R (g x / sqrt(mean(x^2) + eps))      norm, gain, rotation
 //   u = R^T dy, xh = x rstd, w = g u:        dx = rstd (w - xh mean(w xh)),  dg = sum over rows and heads of u xh
 //
-// All of them are bound by HBM: every element is read once and written once, in 16-byte pieces.  A head
-// belongs to a power of two of neighbouring lanes, eight channels to a lane, so that the sums of the norm
-// are a few shuffles and nothing of a head leaves its warp.  The angles of a row are shared by its heads:
-// a block turns them into cosines and sines once, in shared memory, and every lane keeps those of its
-// eight channels in registers while it walks over the row's heads.
+// All of them are bound by HBM: every element is read once and written once, in 16-byte pieces.  A warp takes a
+// row (or an equal part of its heads) at a time; a head belongs to d / 8 neighbouring lanes, eight channels to a
+// lane, as many heads side by side as fit (d = 80: three heads on 30 lanes), so that the sums of the norm are a
+// few shuffles and nothing of a head leaves its warp.  The angles of a row are shared by its heads: the warp
+// turns them into cosines and sines once, in shared memory of its own, while its first heads are on their way,
+// and every lane keeps those of its eight channels in registers.  Warps never wait for one another.
 #include "vit_internal.h"
 
 #include <cmath>
@@ -18,19 +19,21 @@ namespace vit {
 
 namespace {
 
-constexpr int THREADS = 256;
+constexpr int WARPS = 4, THREADS = 32 * WARPS;
 constexpr int CH = 8;                       // channels of a lane
 constexpr int MAX_SMS = 256;
+constexpr int MAX_PAIRS = 64;               // of a head
 
 enum Rotation { INTERLEAVED = 0, HALVES_BY_LANES = 1, HALVES_ANY = 2 };
 enum Mode { TURN = 0, NORM_TURN = 1, NORM_TURN_GRAD = 2 };
 
 struct RopeNormArgs {
   int rows, heads, q_heads, d;
-  int n_pairs, axes, first_pair[5];         // axis a turns the pairs [first_pair[a], first_pair[a + 1])
-  int rows_per_block, row_blocks;
+  int lanes, side;                          // lanes of a head (d / 8), heads side by side in a warp
+  int n_pairs, first_pair[5];               // axis a turns the pairs [first_pair[a], first_pair[a + 1])
+  int split;                                // warps that share a row's heads
   float turn_sign;                          // +1: by the angle, -1: back
-  float eps;
+  float eps, inv_d;
   const int32_t* positions;                 // [axes][rows]
   const float* freqs;                       // [n_pairs]
   const float *q_gain, *k_gain;             // [d]
@@ -74,6 +77,11 @@ __device__ __forceinline__ void store_piece(float* a, const float (&f)[CH]) {
   reinterpret_cast<float4*>(a)[0] = make_float4(f[0], f[1], f[2], f[3]);
   reinterpret_cast<float4*>(a)[1] = make_float4(f[4], f[5], f[6], f[7]);
 }
+__device__ __forceinline__ void load_floats(float (&f)[CH], const float* a) {
+  Piece<float> p;
+  load_piece(p, a);
+  unpack(p, f);
+}
 __device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f(float v) { return v; }
 
@@ -86,219 +94,267 @@ __device__ __forceinline__ float2 turn_of(int32_t position, float freq) {
   return make_float2(c, s);
 }
 
-// One warp-aligned group of G lanes per (row, head).  HEADS heads of a group are in flight at a time.
-template <typename T, int G, int ROT, int MODE, int HEADS>
-__global__ void __launch_bounds__(THREADS)
-rope_norm_kernel(const RopeNormArgs p) {
-  extern __shared__ float2 table[];                     // [rows_per_block][n_pairs]
-  constexpr int GROUPS = THREADS / G;
-  const int lane = threadIdx.x % G, group = threadIdx.x / G;
-  const int per_row = GROUPS / p.rows_per_block;        // groups that share a row's heads
-  const int row_in_block = group / per_row, first_head = group % per_row;
-  const int c0 = lane * CH;
-  const bool active = c0 < p.d;
-  const int n = p.n_pairs;
+// Sum over the `lanes` lanes of a head (any number up to 16; `at` is this lane's place among them): the lanes
+// beyond the largest power of two are folded in first, and fetch the result at the end.
+__device__ __forceinline__ float head_sum(float v, int lanes, int at, int first) {
   const unsigned full = 0xffffffffu;
+  const int pow2 = lanes >= 16 ? 16 : lanes >= 8 ? 8 : lanes >= 4 ? 4 : 2;
+  if (pow2 < lanes) {
+    const float beyond = __shfl_sync(full, v, (first + at + pow2) & 31);
+    if (at + pow2 < lanes) v += beyond;
+  }
+  for (int s = pow2 >> 1; s > 0; s >>= 1) {
+    const float other = __shfl_sync(full, v, first + (at ^ s));
+    v += other;                                         // lanes beyond pow2 gather nothing of use
+  }
+  return pow2 < lanes ? __shfl_sync(full, v, first) : v;
+}
 
-  float qg[CH], kg[CH], dqg[CH], dkg[CH];
+// The eight channels that are partners of a lane's eight, for the heads in flight: from the lane that has them.
+__device__ __forceinline__ void fetch_partner(Piece<bf16>& to, const Piece<bf16>& p, int from) {
+  to.v.x = __shfl_sync(0xffffffffu, p.v.x, from);
+  to.v.y = __shfl_sync(0xffffffffu, p.v.y, from);
+  to.v.z = __shfl_sync(0xffffffffu, p.v.z, from);
+  to.v.w = __shfl_sync(0xffffffffu, p.v.w, from);
+}
+__device__ __forceinline__ void fetch_partner(Piece<float>& to, const Piece<float>& p, int from) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    to.v[i].x = __shfl_sync(0xffffffffu, p.v[i].x, from);
+    to.v[i].y = __shfl_sync(0xffffffffu, p.v[i].y, from);
+    to.v[i].z = __shfl_sync(0xffffffffu, p.v[i].z, from);
+    to.v[i].w = __shfl_sync(0xffffffffu, p.v[i].w, from);
+  }
+}
+
+// HEADS steps of a warp (of `side` heads each) are in flight at a time.
+template <typename T, int ROT, int MODE, int HEADS>
+__global__ void __launch_bounds__(THREADS, MODE == NORM_TURN_GRAD ? 4 : 5)
+rope_norm_kernel(const RopeNormArgs p) {
+  __shared__ float2 tables[WARPS][MAX_PAIRS];
+  extern __shared__ float share[];                      // NORM_TURN_GRAD: [WARPS * side][2][d]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float2* table = tables[warp];
+  const int slot = lane / p.lanes, at = lane - slot * p.lanes, first = slot * p.lanes;   // head of the step, place in it, its first lane
+  const bool active = slot < p.side;
+  const int c0 = at * CH, n = p.n_pairs;
+  const int first_lane = active ? first : 0;
+
+  float dq_gain[CH] = {}, dk_gain[CH] = {};             // NORM_TURN_GRAD: of this lane's channels, all rows and heads
+  // out[j] = v[j] * cs[j] + partner(v)[j] * sn[j] where the channel turns
+  int pair[CH];
+  uint32_t turning = 0;                                 // bit j: channel j turns
 #pragma unroll
   for (int j = 0; j < CH; ++j) {
-    qg[j] = MODE != TURN && active ? p.q_gain[c0 + j] : 0.f;
-    kg[j] = MODE != TURN && active ? p.k_gain[c0 + j] : 0.f;
-    dqg[j] = dkg[j] = 0.f;
+    const int c = c0 + j;
+    pair[j] = ROT == INTERLEAVED ? c >> 1 : c < n ? c : c - n;
+    if (active && pair[j] < n) turning |= 1u << j;
   }
+  // HALVES_BY_LANES: the partner's eight channels are those of one other lane of the head
+  const int partner_lane = ROT == HALVES_BY_LANES && (turning & 1) ? first + (c0 < n ? c0 + n : c0 - n) / CH : lane;
+  const bool every = 2 * n == p.d;                      // no channel is passed on
 
-  for (int rb = blockIdx.x; rb < p.row_blocks; rb += gridDim.x) {
-    const int64_t row0 = (int64_t)rb * p.rows_per_block;
-    if (rb != (int)blockIdx.x) __syncthreads();         // the table of the last rows is no longer read
-    for (int i = threadIdx.x; i < p.rows_per_block * n; i += THREADS) {
-      const int r = i / n, pair = i - r * n;
-      if (row0 + r < p.rows) {
-        int axis = 0;
-        while (pair >= p.first_pair[axis + 1]) ++axis;
-        table[i] = turn_of(p.positions[(int64_t)axis * p.rows + row0 + r], p.freqs[pair]);
-      }
-    }
-    __syncthreads();
-    const int64_t row = row0 + row_in_block;
-    const bool row_ok = row < p.rows;
-    // out[j] = v[j] * cs[j] + partner(v)[j] * sn[j] where the channel turns
+  const int64_t units = (int64_t)p.rows * p.split;      // a warp's piece of work: a row, or one of `split` parts of its heads
+  for (int64_t u = (int64_t)blockIdx.x * WARPS + warp; u < units; u += (int64_t)gridDim.x * WARPS) {
+    const int64_t row = p.split == 1 ? u : u / p.split;
+    const int part = (int)(u - row * p.split);
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx + c0;
+    const T* dy = static_cast<const T*>(p.dy) + (MODE == NORM_TURN_GRAD ? row * p.lddy + c0 : 0);
+    T* y = static_cast<T*>(p.y) + row * p.ldy + c0;
     float cs[CH], sn[CH];
-    int partner[CH];                                    // HALVES_ANY: the partner's channel
-    uint32_t turning = 0;                               // bit j: channel j turns
-#pragma unroll
-    for (int j = 0; j < CH; ++j) {
-      const int c = c0 + j;
-      int pair;
-      float sign;
-      if (ROT == INTERLEAVED) { pair = c >> 1; sign = (c & 1) ? 1.f : -1.f; partner[j] = c ^ 1; }
-      else if (c < n) { pair = c; sign = -1.f; partner[j] = c + n; }
-      else { pair = c - n; sign = 1.f; partner[j] = c - n; }
-      const bool turns = active && row_ok && pair < n;
-      const float2 t = turns ? table[row_in_block * n + pair] : make_float2(1.f, 0.f);
-      cs[j] = t.x;
-      sn[j] = sign * p.turn_sign * t.y;
-      if (turns) turning |= 1u << j; else partner[j] = c;
-    }
-    // HALVES_BY_LANES: the partner's eight channels are those of one other lane of the group
-    const int partner_lane = active ? partner[0] / CH : lane;
-
-    for (int hb = 0; hb < p.heads; hb += per_row * HEADS) {   // as many turns for every group: its warp shuffles
-      const int h0 = hb + first_head;
-      Piece<T> px[HEADS], pd[HEADS];
-      bool on[HEADS];
-#pragma unroll
-      for (int k = 0; k < HEADS; ++k) {                 // all loads in flight before the first use
-        const int h = h0 + k * per_row;
-        on[k] = active && row_ok && h < p.heads;
-        if (on[k]) {
-          load_piece(px[k], static_cast<const T*>(p.x) + row * p.ldx + (int64_t)h * p.d + c0);
-          if (MODE == NORM_TURN_GRAD) load_piece(pd[k], static_cast<const T*>(p.dy) + row * p.lddy + (int64_t)h * p.d + c0);
-        }
+    bool have_angles = false;
+    // query heads, then key heads (TURN: all of them as one)
+#pragma unroll 1
+    for (int kind = 0; kind < (MODE == TURN ? 1 : 2); ++kind) {
+      const int h_end = MODE == TURN ? p.heads : kind ? p.heads : p.q_heads;
+      const int h_begin = MODE == TURN || kind == 0 ? 0 : p.q_heads;
+      const int stride = p.split * p.side;              // heads of one step of all warps of the row
+      const float* gains = MODE == TURN ? nullptr : kind ? p.k_gain : p.q_gain;
+      float gain[CH] = {}, other_gain[CH] = {}, dg[CH] = {};   // other_gain: of the partners
+      if (MODE != TURN && active) {
+        load_floats(gain, gains + c0);
+        if (ROT == HALVES_BY_LANES && MODE == NORM_TURN) load_floats(other_gain, gains + (partner_lane - first) * CH);
       }
+#pragma unroll 1
+      for (int hb = h_begin + part * p.side; hb < h_end; hb += stride * HEADS) {
+        Piece<T> px[HEADS], pd[HEADS];
+        bool on[HEADS];
 #pragma unroll
-      for (int k = 0; k < HEADS; ++k) {
-        const int h = h0 + k * per_row;
-        const bool is_q = h < p.q_heads;
-        float x[CH] = {}, o[CH];
-        if (on[k]) unpack(px[k], x);
-        float rstd = 1.f;
-        if (MODE != TURN) {
-          float sq = 0.f;
-#pragma unroll
-          for (int j = 0; j < CH; ++j) sq = fmaf(x[j], x[j], sq);
-#pragma unroll
-          for (int s = G / 2; s > 0; s >>= 1) sq += __shfl_xor_sync(full, sq, s, G);
-          rstd = 1.0f / sqrtf(sq / (float)p.d + p.eps);
+        for (int k = 0; k < HEADS; ++k) {               // all loads in flight before the first use
+          const int h = hb + k * stride + slot;
+          on[k] = active && h < h_end;
+          if (on[k]) {
+            load_piece(px[k], x + (int64_t)h * p.d);
+            if (MODE == NORM_TURN_GRAD) load_piece(pd[k], dy + (int64_t)h * p.d);
+          } else {
+            px[k] = Piece<T>{};
+            if (MODE == NORM_TURN_GRAD) pd[k] = Piece<T>{};
+          }
         }
-        float v[CH] = {};                               // what is turned
-        if (MODE == NORM_TURN_GRAD) {
-          if (on[k]) unpack(pd[k], v);
-        } else {
+        if (!have_angles) {                             // of this row, while the loads are on their way
+          have_angles = true;
+          __syncwarp();                                 // the last row's have been read
+          for (int i = lane; i < n; i += 32) {
+            int axis = 0;
+            while (i >= p.first_pair[axis + 1]) ++axis;
+            table[i] = turn_of(p.positions[(int64_t)axis * p.rows + row], p.freqs[i]);
+          }
+          __syncwarp();
 #pragma unroll
-          for (int j = 0; j < CH; ++j) v[j] = MODE == NORM_TURN ? x[j] * rstd * (is_q ? qg[j] : kg[j]) : x[j];
+          for (int j = 0; j < CH; ++j) {
+            const float2 t = turning >> j & 1 ? table[pair[j]] : make_float2(1.f, 0.f);
+            const bool second = ROT == INTERLEAVED ? j & 1 : c0 + j >= n;
+            cs[j] = t.x;
+            sn[j] = second ? p.turn_sign * t.y : -p.turn_sign * t.y;
+          }
         }
 #pragma unroll
-        for (int j = 0; j < CH; ++j) {
-          float other;
+        for (int k = 0; k < HEADS; ++k) {
+          if (hb + k * stride >= h_end) break;          // the same for the whole warp
+          const int64_t h = hb + k * stride + slot;
+          float x_[CH], v[CH], o[CH], other[CH];
+          unpack(px[k], x_);
+          float rstd = 1.f;
+          if (MODE != TURN) {
+            float sq = 0.f;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) sq = fmaf(x_[j], x_[j], sq);
+            rstd = 1.0f / sqrtf(fmaf(head_sum(sq, p.lanes, at, first_lane), p.inv_d, p.eps));
+          }
+          // what is turned, and its partners: gradients as they come, values times gain (the norm's factor is
+          // the same for the whole head and comes last)
+          const Piece<T>& src = MODE == NORM_TURN_GRAD ? pd[k] : px[k];
+          if (MODE == NORM_TURN_GRAD) {
+            unpack(pd[k], v);
+          } else {
+#pragma unroll
+            for (int j = 0; j < CH; ++j) v[j] = MODE == NORM_TURN ? x_[j] * gain[j] : x_[j];
+          }
           if (ROT == INTERLEAVED) {
-            other = v[j ^ 1];
+#pragma unroll
+            for (int j = 0; j < CH; ++j) other[j] = v[j ^ 1];
           } else if (ROT == HALVES_BY_LANES) {
-            other = __shfl_sync(full, v[j], partner_lane, G);
+            Piece<T> pp;
+            fetch_partner(pp, src, partner_lane);
+            unpack(pp, other);
+            if (MODE == NORM_TURN) {
+#pragma unroll
+              for (int j = 0; j < CH; ++j) other[j] *= other_gain[j];
+            }
           } else {
             // the partner lies at any offset: read it again (it is in L1), before this head is written
-            other = 0.f;
-            if (on[k]) {
-              const int c = partner[j];
-              if (MODE == NORM_TURN_GRAD) {
-                other = to_f(static_cast<const T*>(p.dy)[row * p.lddy + (int64_t)h * p.d + c]);
-              } else {
-                other = to_f(static_cast<const T*>(p.x)[row * p.ldx + (int64_t)h * p.d + c]);
-                if (MODE == NORM_TURN) other *= rstd * (is_q ? p.q_gain[c] : p.k_gain[c]);
+#pragma unroll
+            for (int j = 0; j < CH; ++j) {
+              other[j] = 0.f;
+              if (on[k] && (turning >> j & 1)) {
+                const int c = c0 + j, q = c < n ? c + n : c - n;
+                other[j] = to_f((MODE == NORM_TURN_GRAD ? dy : x)[h * p.d + q - c0]);
+                if (MODE == NORM_TURN) other[j] *= gains[q];
               }
             }
           }
-          // a channel that does not turn is passed on as it is, whatever its partner holds
-          o[j] = turning >> j & 1 ? fmaf(v[j], cs[j], other * sn[j]) : v[j];
-        }
-        if (MODE == NORM_TURN_GRAD) {
-          float dot = 0.f;
+          if (every) {
 #pragma unroll
-          for (int j = 0; j < CH; ++j) {
-            const float xh = x[j] * rstd;
-            const float dg = o[j] * xh;
-            if (is_q) dqg[j] += dg; else dkg[j] += dg;   // lanes without a head hold x = 0
-            o[j] *= is_q ? qg[j] : kg[j];
-            dot = fmaf(o[j], xh, dot);
+            for (int j = 0; j < CH; ++j) o[j] = fmaf(v[j], cs[j], other[j] * sn[j]);
+          } else {
+            // a channel that does not turn is passed on as it is, whatever its partner holds
+#pragma unroll
+            for (int j = 0; j < CH; ++j) o[j] = turning >> j & 1 ? fmaf(v[j], cs[j], other[j] * sn[j]) : v[j];
           }
+          if (MODE == NORM_TURN) {
 #pragma unroll
-          for (int s = G / 2; s > 0; s >>= 1) dot += __shfl_xor_sync(full, dot, s, G);
-          const float mean = dot / (float)p.d;
+            for (int j = 0; j < CH; ++j) o[j] *= rstd;
+          }
+          if (MODE == NORM_TURN_GRAD) {
+            float dot = 0.f;
 #pragma unroll
-          for (int j = 0; j < CH; ++j) o[j] = rstd * (o[j] - x[j] * rstd * mean);
+            for (int j = 0; j < CH; ++j) {
+              x_[j] *= rstd;
+              dg[j] = fmaf(o[j], x_[j], dg[j]);
+              o[j] *= gain[j];
+              dot = fmaf(o[j], x_[j], dot);
+            }
+            const float mean = head_sum(dot, p.lanes, at, first_lane) * p.inv_d;
+#pragma unroll
+            for (int j = 0; j < CH; ++j) o[j] = rstd * fmaf(-mean, x_[j], o[j]);
+          }
+          if (ROT == HALVES_ANY) __syncwarp();          // in place: every lane has read before any writes
+          if (on[k]) store_piece(y + h * p.d, o);
         }
-        if (ROT == HALVES_ANY) __syncwarp();             // in place: every lane has read before any writes
-        if (on[k]) store_piece(static_cast<T*>(p.y) + row * p.ldy + (int64_t)h * p.d + c0, o);
+      }
+      if (MODE == NORM_TURN_GRAD) {
+#pragma unroll
+        for (int j = 0; j < CH; ++j) {
+          if (kind) dk_gain[j] += dg[j];
+          else dq_gain[j] += dg[j];
+        }
       }
     }
   }
 
   if (MODE == NORM_TURN_GRAD) {
-    // this block's share of the gains' gradients: its groups are added in a fixed order
-    __syncthreads();
-    float* share = reinterpret_cast<float*>(table);      // [GROUPS][2][d]
+    // this block's share of the gains' gradients: its heads are added in a fixed order
+    const int groups = WARPS * p.side;
     if (active) {
 #pragma unroll
       for (int j = 0; j < CH; ++j) {
-        share[(group * 2 + 0) * p.d + c0 + j] = dqg[j];
-        share[(group * 2 + 1) * p.d + c0 + j] = dkg[j];
+        share[((warp * p.side + slot) * 2 + 0) * p.d + c0 + j] = dq_gain[j];
+        share[((warp * p.side + slot) * 2 + 1) * p.d + c0 + j] = dk_gain[j];
       }
     }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * p.d; i += THREADS) {
       float sum = 0.f;
-      for (int g = 0; g < GROUPS; ++g) sum += share[g * 2 * p.d + i];
+      for (int g = 0; g < groups; ++g) sum += share[g * 2 * p.d + i];
       p.partial[(int64_t)blockIdx.x * 2 * p.d + i] = sum;
     }
   }
 }
 
-// dq_gain[c], dk_gain[c] = sum of the blocks' shares, in a fixed order: one warp per channel
-__global__ void __launch_bounds__(THREADS)
+// dq_gain[c], dk_gain[c] = sum of the blocks' shares, in a fixed order: 32 channels to a block, 32 threads to a
+// channel, all loads of a thread in flight together
+constexpr int GAIN_THREADS = 1024;
+__global__ void __launch_bounds__(GAIN_THREADS)
 gain_grad_kernel(const float* __restrict__ partial, int blocks, int d, float* __restrict__ dq_gain, float* __restrict__ dk_gain) {
-  const int i = (int)((blockIdx.x * THREADS + threadIdx.x) >> 5), lane = threadIdx.x & 31;
-  if (i >= 2 * d) return;
+  __shared__ float sums[32][33];
+  const int part = threadIdx.x >> 5, lane = threadIdx.x & 31, i = blockIdx.x * 32 + lane;
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // the shares are written by the kernel before this one
   float sum = 0.f;
-  for (int b = lane; b < blocks; b += 32) sum += partial[(int64_t)b * 2 * d + i];
+  if (i < 2 * d) {
+#pragma unroll 8
+    for (int b = part; b < blocks; b += 32) sum += partial[(int64_t)b * 2 * d + i];
+  }
+  sums[part][lane] = sum;
+  __syncthreads();
+  if (part == 0 && i < 2 * d) {
+    sum = 0.f;
 #pragma unroll
-  for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
-  if (lane == 0) (i < d ? dq_gain : dk_gain)[i < d ? i : i - d] = sum;
-}
-
-struct Shape { int rows_per_block, row_blocks, grid; size_t smem; };
-
-Shape shape_of(int mode, int rows, int heads, int d, int n_pairs, int G, int sms) {
-  Shape s;
-  const int groups = THREADS / G;
-  // As many rows to a block as leave each group about eight heads of a row, so that a row's angles
-  // serve many heads; fewer rows where the call would not fill the device otherwise.
-  int r = 1;
-  while (r * 2 <= groups && heads * r * 2 <= groups * 8 && (int64_t)rows / (r * 2) >= 2 * sms) r *= 2;
-  s.rows_per_block = r;
-  s.row_blocks = (rows + r - 1) / r;
-  s.grid = s.row_blocks;
-  if (mode == NORM_TURN_GRAD && s.grid > 4 * sms) s.grid = 4 * sms;   // one share of the gains' gradients per block
-  s.smem = (size_t)r * n_pairs * sizeof(float2);
-  if (mode == NORM_TURN_GRAD && s.smem < (size_t)groups * 2 * d * 4) s.smem = (size_t)groups * 2 * d * 4;
-  return s;
-}
-
-template <typename T, int G, int ROT, int MODE>
-cudaError_t launch_variant(RopeNormArgs& a, const Shape& s, cudaStream_t stream) {
-  constexpr int HEADS = MODE == NORM_TURN_GRAD ? 2 : 4;
-  rope_norm_kernel<T, G, ROT, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
-  return cudaGetLastError();
-}
-template <typename T, int G, int MODE>
-cudaError_t launch_rot(RopeNormArgs& a, bool interleaved, const Shape& s, cudaStream_t stream) {
-  if (interleaved || a.n_pairs == 0) return launch_variant<T, G, INTERLEAVED, MODE>(a, s, stream);
-  if (a.n_pairs % CH == 0) return launch_variant<T, G, HALVES_BY_LANES, MODE>(a, s, stream);
-  return launch_variant<T, G, HALVES_ANY, MODE>(a, s, stream);
-}
-template <typename T, int MODE>
-cudaError_t launch_lanes(RopeNormArgs& a, bool interleaved, const Shape& s, int G, cudaStream_t stream) {
-  switch (G) {
-    case 2: return launch_rot<T, 2, MODE>(a, interleaved, s, stream);
-    case 4: return launch_rot<T, 4, MODE>(a, interleaved, s, stream);
-    case 8: return launch_rot<T, 8, MODE>(a, interleaved, s, stream);
-    default: return launch_rot<T, 16, MODE>(a, interleaved, s, stream);
+    for (int b = 0; b < 32; ++b) sum += sums[b][lane];
+    (i < d ? dq_gain : dk_gain)[i < d ? i : i - d] = sum;
   }
 }
 
-int lanes_of(int d) {
-  int g = 2;
-  while (g * CH < d) g *= 2;
-  return g;
+struct Shape { int split, grid; size_t smem; };
+
+Shape shape_of(int mode, int rows, int heads, int d, int sms) {
+  Shape s;
+  const int side = 32 / (d / CH);
+  // a row's heads are shared by more warps where the rows alone would not fill the device
+  s.split = 1;
+  while (s.split < 8 && (int64_t)rows * s.split < (int64_t)sms * 16 && heads > 2 * s.split * side) s.split *= 2;
+  const int64_t blocks = ((int64_t)rows * s.split + WARPS - 1) / WARPS, most = (int64_t)sms * (mode == NORM_TURN_GRAD ? 4 : 32);
+  s.grid = (int)(blocks < most ? blocks : most);
+  s.smem = mode == NORM_TURN_GRAD ? (size_t)WARPS * side * 2 * d * sizeof(float) : 0;
+  return s;
+}
+
+template <typename T, int MODE>
+cudaError_t launch_mode(const RopeNormArgs& a, bool interleaved, const Shape& s, cudaStream_t stream) {
+  constexpr int HEADS = sizeof(T) == 4 || MODE == NORM_TURN_GRAD ? 2 : 4;
+  if (interleaved || a.n_pairs == 0) rope_norm_kernel<T, INTERLEAVED, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
+  else if (a.n_pairs % CH == 0) rope_norm_kernel<T, HALVES_BY_LANES, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
+  else rope_norm_kernel<T, HALVES_ANY, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -314,36 +370,39 @@ cudaError_t launch_rope_norm(const RopeNormCall& c, cudaStream_t s) {
   const int mode = c.dy ? NORM_TURN_GRAD : c.q_gain ? NORM_TURN : TURN;
   RopeNormArgs a{};
   a.rows = c.rows; a.heads = c.heads; a.q_heads = c.q_heads; a.d = c.d;
+  a.lanes = c.d / CH; a.side = 32 / a.lanes; a.inv_d = 1.0f / (float)c.d;
   if (c.rope) {
-    a.axes = c.rope->axes;
-    for (int i = 0; i < a.axes; ++i) a.first_pair[i + 1] = a.first_pair[i] + c.rope->pairs[i];
-    a.n_pairs = a.first_pair[a.axes];
+    for (int i = 0; i < c.rope->axes; ++i) a.first_pair[i + 1] = a.first_pair[i] + c.rope->pairs[i];
+    a.n_pairs = a.first_pair[c.rope->axes];
     a.positions = c.rope->positions; a.freqs = c.rope->freqs;
   }
   a.turn_sign = c.inverse != (mode == NORM_TURN_GRAD) ? -1.f : 1.f;
   a.eps = c.eps; a.q_gain = c.q_gain; a.k_gain = c.k_gain;
   a.x = c.x; a.ldx = c.ldx; a.dy = c.dy; a.lddy = c.lddy; a.y = c.y; a.ldy = c.ldy; a.partial = c.partial;
-  const int G = lanes_of(c.d);
-  const Shape sh = shape_of(mode, c.rows, c.heads, c.d, a.n_pairs, G, sms);
-  a.rows_per_block = sh.rows_per_block; a.row_blocks = sh.row_blocks;
+  const Shape sh = shape_of(mode, c.rows, c.heads, c.d, sms);
+  a.split = sh.split;
   const bool il = c.rope && c.rope->interleaved;
-  cudaError_t e;
   if (c.act_bf16)
-    e = mode == TURN ? launch_lanes<bf16, TURN>(a, il, sh, G, s) : mode == NORM_TURN ? launch_lanes<bf16, NORM_TURN>(a, il, sh, G, s)
-                                                                                     : launch_lanes<bf16, NORM_TURN_GRAD>(a, il, sh, G, s);
-  else
-    e = mode == TURN ? launch_lanes<float, TURN>(a, il, sh, G, s) : mode == NORM_TURN ? launch_lanes<float, NORM_TURN>(a, il, sh, G, s)
-                                                                                      : launch_lanes<float, NORM_TURN_GRAD>(a, il, sh, G, s);
-  return e;
+    return mode == TURN ? launch_mode<bf16, TURN>(a, il, sh, s) : mode == NORM_TURN ? launch_mode<bf16, NORM_TURN>(a, il, sh, s)
+                                                                                   : launch_mode<bf16, NORM_TURN_GRAD>(a, il, sh, s);
+  return mode == TURN ? launch_mode<float, TURN>(a, il, sh, s) : mode == NORM_TURN ? launch_mode<float, NORM_TURN>(a, il, sh, s)
+                                                                                  : launch_mode<float, NORM_TURN_GRAD>(a, il, sh, s);
 }
 
 cudaError_t launch_gain_grad(const RopeNormCall& c, float* dq_gain, float* dk_gain, cudaStream_t s) {
   const int sms = current_device_sm_count();
   if (sms < 1 || sms > MAX_SMS) return cudaErrorInvalidDevice;
-  int blocks = 0;                                        // no rows: the gradients are zero
-  if (c.rows > 0) blocks = shape_of(NORM_TURN_GRAD, c.rows, c.heads, c.d, 0, lanes_of(c.d), sms).grid;
-  gain_grad_kernel<<<(2 * c.d * 32 + THREADS - 1) / THREADS, THREADS, 0, s>>>(c.partial, blocks, c.d, dq_gain, dk_gain);
-  return cudaGetLastError();
+  const int blocks = c.rows > 0 ? shape_of(NORM_TURN_GRAD, c.rows, c.heads, c.d, sms).grid : 0;   // no rows: the gradients are zero
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((2 * c.d + 31) / 32);
+  cfg.blockDim = dim3(GAIN_THREADS);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];                           // its launch overlaps the end of the kernel before it
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, gain_grad_kernel, (const float*)c.partial, blocks, c.d, dq_gain, dk_gain);
 }
 
 }  // namespace vit
