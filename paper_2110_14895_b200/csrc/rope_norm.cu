@@ -311,6 +311,297 @@ rope_norm_kernel(const RopeNormArgs p) {
   }
 }
 
+// ---------------------------------------------------------------------- every channel turns (2 n = d)
+// The usual case.  What bounds it besides HBM is the number of instructions (the kernel above takes 2900 for a row
+// of 32 heads of 80 channels, 133 us at 32896 rows): a lane holds 16 channels of a head, both channels of its eight
+// pairs among them, so that turning needs no exchange; sums run over d / 16 lanes; arithmetic is on pairs of values.
+struct Sixteen { float2 a[4], b[4]; };       // HALVES: channels 8 at ..., n + 8 at ...; INTERLEAVED: 16 consecutive ones
+
+template <typename T> struct Piece16;
+template <> struct Piece16<bf16> { uint4 v[2]; };
+template <> struct Piece16<float> { float4 v[4]; };
+__device__ __forceinline__ void load16(Piece16<bf16>& p, const bf16* a, int second) {
+  p.v[0] = *reinterpret_cast<const uint4*>(a);
+  p.v[1] = *reinterpret_cast<const uint4*>(a + second);
+}
+__device__ __forceinline__ void load16(Piece16<float>& p, const float* a, int second) {
+  p.v[0] = reinterpret_cast<const float4*>(a)[0];
+  p.v[1] = reinterpret_cast<const float4*>(a)[1];
+  p.v[2] = reinterpret_cast<const float4*>(a + second)[0];
+  p.v[3] = reinterpret_cast<const float4*>(a + second)[1];
+}
+__device__ __forceinline__ void zero16(Piece16<bf16>& p) { p.v[0] = p.v[1] = make_uint4(0u, 0u, 0u, 0u); }
+__device__ __forceinline__ void zero16(Piece16<float>& p) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p.v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+__device__ __forceinline__ float2 low_high(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ void open16(const Piece16<bf16>& p, Sixteen& f) {
+  f.a[0] = low_high(p.v[0].x); f.a[1] = low_high(p.v[0].y); f.a[2] = low_high(p.v[0].z); f.a[3] = low_high(p.v[0].w);
+  f.b[0] = low_high(p.v[1].x); f.b[1] = low_high(p.v[1].y); f.b[2] = low_high(p.v[1].z); f.b[3] = low_high(p.v[1].w);
+}
+__device__ __forceinline__ void open16(const Piece16<float>& p, Sixteen& f) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    f.a[2 * i] = make_float2(p.v[i].x, p.v[i].y);
+    f.a[2 * i + 1] = make_float2(p.v[i].z, p.v[i].w);
+    f.b[2 * i] = make_float2(p.v[2 + i].x, p.v[2 + i].y);
+    f.b[2 * i + 1] = make_float2(p.v[2 + i].z, p.v[2 + i].w);
+  }
+}
+__device__ __forceinline__ uint32_t rounded(float2 f) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void store16(bf16* a, int second, const Sixteen& f) {     // the one rounding to bf16
+  *reinterpret_cast<uint4*>(a) = make_uint4(rounded(f.a[0]), rounded(f.a[1]), rounded(f.a[2]), rounded(f.a[3]));
+  *reinterpret_cast<uint4*>(a + second) = make_uint4(rounded(f.b[0]), rounded(f.b[1]), rounded(f.b[2]), rounded(f.b[3]));
+}
+__device__ __forceinline__ void store16(float* a, int second, const Sixteen& f) {
+  reinterpret_cast<float4*>(a)[0] = make_float4(f.a[0].x, f.a[0].y, f.a[1].x, f.a[1].y);
+  reinterpret_cast<float4*>(a)[1] = make_float4(f.a[2].x, f.a[2].y, f.a[3].x, f.a[3].y);
+  reinterpret_cast<float4*>(a + second)[0] = make_float4(f.b[0].x, f.b[0].y, f.b[1].x, f.b[1].y);
+  reinterpret_cast<float4*>(a + second)[1] = make_float4(f.b[2].x, f.b[2].y, f.b[3].x, f.b[3].y);
+}
+
+// Sums over the lanes of a head (1 to 8, not always a power of two), N heads step by step together
+struct HeadSum { int lanes, pow2, first, beyond, from[3]; };
+__device__ __forceinline__ HeadSum head_sum_plan(int lanes, int at, int first) {
+  HeadSum p;
+  p.lanes = lanes;
+  p.first = first;
+  p.pow2 = lanes >= 8 ? 8 : lanes >= 4 ? 4 : lanes >= 2 ? 2 : 1;
+  p.beyond = at + p.pow2 < lanes ? first + at + p.pow2 : -1;
+#pragma unroll
+  for (int k = 0; k < 3; ++k) p.from[k] = (first + (at ^ (4 >> k))) & 31;
+  return p;
+}
+template <int N>
+__device__ __forceinline__ void head_sums(float (&v)[N], const HeadSum& p) {
+  const unsigned full = 0xffffffffu;
+  if (p.pow2 < p.lanes) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float beyond = __shfl_sync(full, v[i], p.beyond & 31);
+      if (p.beyond >= 0) v[i] += beyond;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 3; ++k)
+    if (p.pow2 > 4 >> k) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += __shfl_sync(full, v[i], p.from[k]);   // lanes beyond pow2 gather nothing of use
+    }
+  if (p.pow2 < p.lanes) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(full, v[i], p.first);
+  }
+}
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+
+// STEPS steps of a warp (of `side` heads each) are in flight at a time.  INTERLEAVED: values 2 i, 2 i + 1 of the
+// sixteen are a pair; HALVES: value i of a and of b.
+template <typename T, bool IL, int MODE, int STEPS>
+__global__ void __launch_bounds__(THREADS, MODE == NORM_TURN_GRAD ? 3 : 4)
+rope_norm_full_kernel(const RopeNormArgs p) {
+  __shared__ float2 tables[WARPS][MAX_PAIRS];
+  extern __shared__ float share[];                      // NORM_TURN_GRAD: [WARPS * side][2][d]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float2* table = tables[warp];
+  const int slot = lane / p.lanes, at = lane - slot * p.lanes;
+  const bool active = slot < p.side;
+  const int n = p.n_pairs, c0 = active ? (IL ? 16 * at : 8 * at) : 0, second = IL ? 8 : n;   // first channel of a, and of b behind it
+  const HeadSum sums = head_sum_plan(p.lanes, at, active ? slot * p.lanes : 0);
+  const int step = p.split * p.side;                    // heads from one step of the warp to its next
+  const int64_t units = (int64_t)p.rows * p.split, next_unit = (int64_t)gridDim.x * WARPS;
+
+  // a lane turns up to two of a row's pairs into the table; their positions are fetched a row ahead
+  const int32_t* from[2];
+  float freq[2] = {0.f, 0.f};
+  int ahead[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    int axis = 0;
+    from[e] = p.positions;
+    if (lane + 32 * e < n) {
+      while (lane + 32 * e >= p.first_pair[axis + 1]) ++axis;
+      from[e] = p.positions + (int64_t)axis * p.rows;
+      freq[e] = p.freqs[lane + 32 * e];
+    }
+  }
+  const int64_t u0 = (int64_t)blockIdx.x * WARPS + warp;
+  if (u0 < units) {
+    const int64_t row = p.split == 1 ? u0 : u0 / p.split;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) ahead[e] = from[e][row];
+  }
+  float2 dg[2][8];                                      // gradients of the gains: of query and of key heads
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dg[k][j] = make_float2(0.f, 0.f);
+
+#pragma unroll 1
+  for (int64_t u = u0; u < units; u += next_unit) {
+    const int64_t row = p.split == 1 ? u : u / p.split;
+    const int first_head = ((int)(u - row * p.split)) * p.side + slot;
+    const T* x = static_cast<const T*>(p.x) + row * p.ldx + c0;
+    const T* dy = MODE == NORM_TURN_GRAD ? static_cast<const T*>(p.dy) + row * p.lddy + c0 : nullptr;
+    T* y = static_cast<T*>(p.y) + row * p.ldy + c0;
+    bool have_angles = false;
+    Sixteen cs;                                         // of the eight pairs: a = cosines, b = sines
+#pragma unroll
+    for (int kind = 0; kind < (MODE == TURN ? 1 : 2); ++kind) {
+      const int h_begin = kind ? p.q_heads : 0, h_end = MODE == TURN || kind ? p.heads : p.q_heads;
+      Sixteen gain;
+      bool have_gains = false;
+#pragma unroll 1
+      for (int h0 = h_begin + first_head - slot; h0 < h_end; h0 += step * STEPS) {
+        Piece16<T> px[STEPS], pd[STEPS];
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {               // all loads in flight before the first use
+          const int h = h0 + slot + k * step;
+          zero16(px[k]);
+          if (MODE == NORM_TURN_GRAD) zero16(pd[k]);
+          if (active && h < h_end) {
+            load16(px[k], x + h * p.d, second);
+            if (MODE == NORM_TURN_GRAD) load16(pd[k], dy + h * p.d, second);
+          }
+        }
+        if (!have_angles) {                             // of this row, while the loads are on their way
+          have_angles = true;
+          __syncwarp();                                 // the last row's have been read
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            if (lane + 32 * e < n) table[lane + 32 * e] = turn_of(ahead[e], freq[e]);
+          __syncwarp();
+          const int64_t un = u + next_unit;
+          if (un < units) {
+            const int64_t rn = p.split == 1 ? un : un / p.split;
+#pragma unroll
+            for (int e = 0; e < 2; ++e) ahead[e] = from[e][rn];
+          }
+          const float4* t = reinterpret_cast<const float4*>(table + 8 * at);     // (c0, s0, c1, s1)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float4 v = t[j];
+            cs.a[j] = make_float2(v.x, v.z);
+            cs.b[j] = make_float2(p.turn_sign * v.y, p.turn_sign * v.w);
+          }
+        }
+        if (MODE != TURN && !have_gains) {
+          have_gains = true;
+          const float* g = (kind ? p.k_gain : p.q_gain) + c0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            gain.a[j] = *reinterpret_cast<const float2*>(g + 2 * j);
+            gain.b[j] = *reinterpret_cast<const float2*>(g + second + 2 * j);
+          }
+        }
+        float rstd[STEPS];
+        if (MODE != TURN) {
+          // the heads' sums of squares step by step together: every step waits for a shuffle
+#pragma unroll
+          for (int k = 0; k < STEPS; ++k) {
+            Sixteen v;
+            open16(px[k], v);
+            float2 sq = __fmul2_rn(v.a[0], v.a[0]);
+#pragma unroll
+            for (int j = 1; j < 4; ++j) sq = __ffma2_rn(v.a[j], v.a[j], sq);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sq = __ffma2_rn(v.b[j], v.b[j], sq);
+            rstd[k] = sq.x + sq.y;
+          }
+          head_sums(rstd, sums);
+#pragma unroll
+          for (int k = 0; k < STEPS; ++k) rstd[k] = rsqrtf(fmaf(rstd[k], p.inv_d, p.eps));
+        }
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+          Sixteen v, o;
+          open16(MODE == NORM_TURN_GRAD ? pd[k] : px[k], v);
+          if (MODE == NORM_TURN) {
+            const float2 r = twice(rstd[k]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              v.a[j] = __fmul2_rn(v.a[j], __fmul2_rn(gain.a[j], r));
+              v.b[j] = __fmul2_rn(v.b[j], __fmul2_rn(gain.b[j], r));
+            }
+          }
+          if (IL) {
+            // pair q is v.a[q] (q < 4) or v.b[q - 4]; its cosine and sine are element q of cs.a and cs.b
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              const float2 w = q < 4 ? v.a[q & 3] : v.b[q & 3];
+              const float c = q & 1 ? cs.a[q >> 1].y : cs.a[q >> 1].x, s = q & 1 ? cs.b[q >> 1].y : cs.b[q >> 1].x;
+              const float2 turned = make_float2(fmaf(w.x, c, -(w.y * s)), fmaf(w.y, c, w.x * s));
+              if (q < 4) o.a[q & 3] = turned;
+              else o.b[q & 3] = turned;
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float2 minus = make_float2(-cs.b[j].x, -cs.b[j].y);
+              o.a[j] = __ffma2_rn(v.a[j], cs.a[j], __fmul2_rn(v.b[j], minus));
+              o.b[j] = __ffma2_rn(v.b[j], cs.a[j], __fmul2_rn(v.a[j], cs.b[j]));
+            }
+          }
+          const int h = h0 + slot + k * step;
+          if (MODE == NORM_TURN_GRAD) {
+            if (!(active && h < h_end)) rstd[k] = 0.f;  // adds nothing to the gains' gradients
+            Sixteen xh;
+            open16(px[k], xh);
+            const float2 r = twice(rstd[k]);
+            float2 dot = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              xh.a[j] = __fmul2_rn(xh.a[j], r);
+              xh.b[j] = __fmul2_rn(xh.b[j], r);
+              dg[kind][j] = __ffma2_rn(o.a[j], xh.a[j], dg[kind][j]);
+              dg[kind][4 + j] = __ffma2_rn(o.b[j], xh.b[j], dg[kind][4 + j]);
+              o.a[j] = __fmul2_rn(o.a[j], gain.a[j]);
+              o.b[j] = __fmul2_rn(o.b[j], gain.b[j]);
+              dot = __ffma2_rn(o.a[j], xh.a[j], dot);
+              dot = __ffma2_rn(o.b[j], xh.b[j], dot);
+            }
+            float mean[1] = {dot.x + dot.y};
+            head_sums(mean, sums);
+            const float2 f = twice(-mean[0] * p.inv_d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              o.a[j] = __fmul2_rn(r, __ffma2_rn(f, xh.a[j], o.a[j]));
+              o.b[j] = __fmul2_rn(r, __ffma2_rn(f, xh.b[j], o.b[j]));
+            }
+          }
+          if (active && h < h_end) store16(y + h * p.d, second, o);
+        }
+      }
+    }
+  }
+
+  if (MODE == NORM_TURN_GRAD) {
+    // this block's share of the gains' gradients: its heads are added in a fixed order
+    const int groups = WARPS * p.side;
+    if (active) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        float* to = share + ((warp * p.side + slot) * 2 + k) * p.d + c0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          *reinterpret_cast<float2*>(to + 2 * j) = dg[k][j];
+          *reinterpret_cast<float2*>(to + second + 2 * j) = dg[k][4 + j];
+        }
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * p.d; i += THREADS) {
+      float sum = 0.f;
+      for (int g = 0; g < groups; ++g) sum += share[g * 2 * p.d + i];
+      p.partial[(int64_t)blockIdx.x * 2 * p.d + i] = sum;
+    }
+  }
+}
+
 // dq_gain[c], dk_gain[c] = sum of the blocks' shares, in a fixed order: 32 channels to a block, 32 threads to a
 // channel, all loads of a thread in flight together
 constexpr int GAIN_THREADS = 1024;
@@ -336,9 +627,9 @@ gain_grad_kernel(const float* __restrict__ partial, int blocks, int d, float* __
 
 struct Shape { int split, grid; size_t smem; };
 
-Shape shape_of(int mode, int rows, int heads, int d, int sms) {
+Shape shape_of(int mode, int rows, int heads, int d, bool full, int sms) {
   Shape s;
-  const int side = 32 / (d / CH);
+  const int side = 32 / (d / (full ? 16 : CH));
   // a row's heads are shared by more warps where the rows alone would not fill the device
   s.split = 1;
   while (s.split < 8 && (int64_t)rows * s.split < (int64_t)sms * 16 && heads > 2 * s.split * side) s.split *= 2;
@@ -351,7 +642,11 @@ Shape shape_of(int mode, int rows, int heads, int d, int sms) {
 template <typename T, int MODE>
 cudaError_t launch_mode(const RopeNormArgs& a, bool interleaved, const Shape& s, cudaStream_t stream) {
   constexpr int HEADS = sizeof(T) == 4 || MODE == NORM_TURN_GRAD ? 2 : 4;
-  if (interleaved || a.n_pairs == 0) rope_norm_kernel<T, INTERLEAVED, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
+  constexpr int STEPS = sizeof(T) == 4 ? (MODE == NORM_TURN_GRAD ? 1 : 2) : MODE == NORM_TURN_GRAD ? 2 : 3;
+  if (2 * a.n_pairs == a.d) {
+    if (interleaved) rope_norm_full_kernel<T, true, MODE, STEPS><<<s.grid, THREADS, s.smem, stream>>>(a);
+    else rope_norm_full_kernel<T, false, MODE, STEPS><<<s.grid, THREADS, s.smem, stream>>>(a);
+  } else if (interleaved || a.n_pairs == 0) rope_norm_kernel<T, INTERLEAVED, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
   else if (a.n_pairs % CH == 0) rope_norm_kernel<T, HALVES_BY_LANES, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
   else rope_norm_kernel<T, HALVES_ANY, MODE, HEADS><<<s.grid, THREADS, s.smem, stream>>>(a);
   return cudaGetLastError();
@@ -370,7 +665,7 @@ cudaError_t launch_rope_norm(const RopeNormCall& c, cudaStream_t s) {
   const int mode = c.dy ? NORM_TURN_GRAD : c.q_gain ? NORM_TURN : TURN;
   RopeNormArgs a{};
   a.rows = c.rows; a.heads = c.heads; a.q_heads = c.q_heads; a.d = c.d;
-  a.lanes = c.d / CH; a.side = 32 / a.lanes; a.inv_d = 1.0f / (float)c.d;
+  a.inv_d = 1.0f / (float)c.d;
   if (c.rope) {
     for (int i = 0; i < c.rope->axes; ++i) a.first_pair[i + 1] = a.first_pair[i] + c.rope->pairs[i];
     a.n_pairs = a.first_pair[c.rope->axes];
@@ -379,7 +674,9 @@ cudaError_t launch_rope_norm(const RopeNormCall& c, cudaStream_t s) {
   a.turn_sign = c.inverse != (mode == NORM_TURN_GRAD) ? -1.f : 1.f;
   a.eps = c.eps; a.q_gain = c.q_gain; a.k_gain = c.k_gain;
   a.x = c.x; a.ldx = c.ldx; a.dy = c.dy; a.lddy = c.lddy; a.y = c.y; a.ldy = c.ldy; a.partial = c.partial;
-  const Shape sh = shape_of(mode, c.rows, c.heads, c.d, sms);
+  const bool full = 2 * a.n_pairs == c.d;
+  a.lanes = c.d / (full ? 16 : CH); a.side = 32 / a.lanes;
+  const Shape sh = shape_of(mode, c.rows, c.heads, c.d, full, sms);
   a.split = sh.split;
   const bool il = c.rope && c.rope->interleaved;
   if (c.act_bf16)
@@ -392,7 +689,10 @@ cudaError_t launch_rope_norm(const RopeNormCall& c, cudaStream_t s) {
 cudaError_t launch_gain_grad(const RopeNormCall& c, float* dq_gain, float* dk_gain, cudaStream_t s) {
   const int sms = current_device_sm_count();
   if (sms < 1 || sms > MAX_SMS) return cudaErrorInvalidDevice;
-  const int blocks = c.rows > 0 ? shape_of(NORM_TURN_GRAD, c.rows, c.heads, c.d, sms).grid : 0;   // no rows: the gradients are zero
+  int n_pairs = 0;
+  for (int i = 0; c.rope && i < c.rope->axes; ++i) n_pairs += c.rope->pairs[i];
+  const bool full = 2 * n_pairs == c.d;
+  const int blocks = c.rows > 0 ? shape_of(NORM_TURN_GRAD, c.rows, c.heads, c.d, full, sms).grid : 0;   // no rows: the gradients are zero
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((2 * c.d + 31) / 32);
   cfg.blockDim = dim3(GAIN_THREADS);
