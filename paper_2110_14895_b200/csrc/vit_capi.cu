@@ -761,6 +761,7 @@ int vit_op_rope_axes(vit_handle* h, int dtype, int rows, int heads, int d, const
   if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by))) return VIT_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   RopeNormCall c{};
+  c.dev_status = h->dev_status;
   c.act_bf16 = dtype == VIT_BF16; c.inverse = inverse != 0; c.rows = rows; c.heads = heads; c.q_heads = heads; c.d = d; c.rope = rope;
   c.x = x; c.ldx = ldx; c.y = y; c.ldy = ldy;
   VIT_LAUNCH(h, VIT_PROF_OP, launch_rope_norm(c, s));
@@ -780,6 +781,7 @@ int vit_op_qk_norm_rope(vit_handle* h, int dtype, int rows, int q_heads, int k_h
   if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by))) return VIT_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   RopeNormCall c{};
+  c.dev_status = h->dev_status;
   c.act_bf16 = dtype == VIT_BF16; c.rows = rows; c.heads = q_heads + k_heads; c.q_heads = q_heads; c.d = d; c.rope = rope;
   c.q_gain = q_gain; c.k_gain = k_gain; c.eps = eps; c.x = x; c.ldx = ldx; c.y = y; c.ldy = ldy;
   VIT_LAUNCH(h, VIT_PROF_OP, launch_rope_norm(c, s));
@@ -814,6 +816,7 @@ int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads
   if (ws_bytes < need) return VIT_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   RopeNormCall c{};
+  c.dev_status = h->dev_status;
   c.act_bf16 = dtype == VIT_BF16; c.rows = rows; c.heads = q_heads + k_heads; c.q_heads = q_heads; c.d = d; c.rope = rope;
   c.q_gain = q_gain; c.k_gain = k_gain; c.eps = eps; c.x = x; c.ldx = ldx; c.dy = dy; c.lddy = lddy; c.y = dx; c.ldy = lddx;
   c.partial = static_cast<float*>(ws);

@@ -168,6 +168,7 @@ struct RopeNormCall {
   const void* dy; int64_t lddy;
   void* y;        int64_t ldy;
   float* partial;
+  int* dev_status;
 };
 size_t qk_norm_rope_backward_bytes(int d);
 cudaError_t launch_rope_norm(const RopeNormCall& c, cudaStream_t s);
