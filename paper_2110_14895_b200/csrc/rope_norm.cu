@@ -13,6 +13,7 @@
 // and every lane keeps those of its eight channels in registers.  Warps never wait for one another.
 #include "vit_internal.h"
 #include "sm100_ptx.cuh"
+#include "lane_groups.cuh"
 
 #include <cmath>
 
@@ -97,22 +98,6 @@ __device__ __forceinline__ float2 turn_of(int32_t position, float freq) {
   return make_float2(c, s);
 }
 
-// Sum over the `lanes` lanes of a head (any number up to 16; `at` is this lane's place among them): the lanes
-// beyond the largest power of two are folded in first, and fetch the result at the end.
-__device__ __forceinline__ float head_sum(float v, int lanes, int at, int first) {
-  const unsigned full = 0xffffffffu;
-  const int pow2 = lanes >= 16 ? 16 : lanes >= 8 ? 8 : lanes >= 4 ? 4 : 2;
-  if (pow2 < lanes) {
-    const float beyond = __shfl_sync(full, v, (first + at + pow2) & 31);
-    if (at + pow2 < lanes) v += beyond;
-  }
-  for (int s = pow2 >> 1; s > 0; s >>= 1) {
-    const float other = __shfl_sync(full, v, first + (at ^ s));
-    v += other;                                         // lanes beyond pow2 gather nothing of use
-  }
-  return pow2 < lanes ? __shfl_sync(full, v, first) : v;
-}
-
 // The eight channels that are partners of a lane's eight, for the heads in flight: from the lane that has them.
 __device__ __forceinline__ void fetch_partner(Piece<bf16>& to, const Piece<bf16>& p, int from) {
   to.v.x = __shfl_sync(0xffffffffu, p.v.x, from);
@@ -156,6 +141,7 @@ rope_norm_kernel(const RopeNormArgs p) {
   // HALVES_BY_LANES: the partner's eight channels are those of one other lane of the head
   const int partner_lane = ROT == HALVES_BY_LANES && (turning & 1) ? first + (c0 < n ? c0 + n : c0 - n) / CH : lane;
   const bool every = 2 * n == p.d;                      // no channel is passed on
+  const HeadSum sums = head_sum_plan(p.lanes, at, first_lane);
 
   const int64_t units = (int64_t)p.rows * p.split;      // a warp's piece of work: a row, or one of `split` parts of its heads
   for (int64_t u = (int64_t)blockIdx.x * WARPS + warp; u < units; u += (int64_t)gridDim.x * WARPS) {
@@ -222,7 +208,7 @@ rope_norm_kernel(const RopeNormArgs p) {
             float sq = 0.f;
 #pragma unroll
             for (int j = 0; j < CH; ++j) sq = fmaf(x_[j], x_[j], sq);
-            rstd = 1.0f / sqrtf(fmaf(head_sum(sq, p.lanes, at, first_lane), p.inv_d, p.eps));
+            rstd = 1.0f / sqrtf(fmaf(head_sum(sq, sums), p.inv_d, p.eps));
           }
           // what is turned, and its partners: gradients as they come, values times gain (the norm's factor is
           // the same for the whole head and comes last)
@@ -277,7 +263,7 @@ rope_norm_kernel(const RopeNormArgs p) {
               o[j] *= gain[j];
               dot = fmaf(o[j], x_[j], dot);
             }
-            const float mean = head_sum(dot, p.lanes, at, first_lane) * p.inv_d;
+            const float mean = head_sum(dot, sums) * p.inv_d;
 #pragma unroll
             for (int j = 0; j < CH; ++j) o[j] = rstd * fmaf(-mean, x_[j], o[j]);
           }
@@ -367,39 +353,6 @@ __device__ __forceinline__ void store16(float* a, int second, const Sixteen& f) 
   reinterpret_cast<float4*>(a + second)[1] = make_float4(f.b[2].x, f.b[2].y, f.b[3].x, f.b[3].y);
 }
 
-// Sums over the lanes of a head (1 to 8, not always a power of two), N heads step by step together
-struct HeadSum { int lanes, pow2, first, beyond, from[3]; };
-__device__ __forceinline__ HeadSum head_sum_plan(int lanes, int at, int first) {
-  HeadSum p;
-  p.lanes = lanes;
-  p.first = first;
-  p.pow2 = lanes >= 8 ? 8 : lanes >= 4 ? 4 : lanes >= 2 ? 2 : 1;
-  p.beyond = at + p.pow2 < lanes ? first + at + p.pow2 : -1;
-#pragma unroll
-  for (int k = 0; k < 3; ++k) p.from[k] = (first + (at ^ (4 >> k))) & 31;
-  return p;
-}
-template <int N>
-__device__ __forceinline__ void head_sums(float (&v)[N], const HeadSum& p) {
-  const unsigned full = 0xffffffffu;
-  if (p.pow2 < p.lanes) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float beyond = __shfl_sync(full, v[i], p.beyond & 31);
-      if (p.beyond >= 0) v[i] += beyond;
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 3; ++k)
-    if (p.pow2 > 4 >> k) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += __shfl_sync(full, v[i], p.from[k]);   // lanes beyond pow2 gather nothing of use
-    }
-  if (p.pow2 < p.lanes) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(full, v[i], p.first);
-  }
-}
 __device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
 
 // One row to shared memory, counted on an mbarrier

@@ -269,7 +269,7 @@ bool attention_problem_ok(int dtype, const vit_attention_problem* p) {
 bool attention_fits(const vit_attention_problem* p) {
   const int64_t longest = p->max_q > p->max_k ? p->max_q : p->max_k;
   const int64_t per = (int64_t)p->heads * ((longest + 63) / 64 + 1);
-  return p->sequences == 0 || per <= INT32_MAX / p->sequences;
+  return p->sequences == 0 || per <= INT32_MAX / 8 / p->sequences;      // (up to eight blocks where there are few queries)
 }
 size_t attention_packed_ws(int dtype, const vit_attention_problem& p, bool backward) {
   return backward ? align_up((size_t)p.heads * p.q_rows * sizeof(float2), 256) : 0;
@@ -849,7 +849,8 @@ int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_proble
   PackedCall c{};
   c.p = p; c.q = q; c.ldq = ldq; c.k = k; c.ldk = ldk; c.v = v; c.ldv = ldv; c.out = out; c.ldo = ldo; c.lse = lse;
   c.dev_status = h->dev_status;
-  if (dtype == VIT_BF16) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_bf16(c, s));
+  if (attention_rows_supported(p)) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_rows(c, dtype == VIT_BF16, s));
+  else if (dtype == VIT_BF16) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_bf16(c, s));
   else VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_f32(c, s));
   return VIT_OK;
 }
