@@ -19,29 +19,34 @@ namespace {
 constexpr int WARPS = 4, THREADS = 32 * WARPS, UNROLL = 4;
 
 struct Eight { float v[8]; };
-__device__ __forceinline__ Eight load8(const float* a) {
-  const float4 u = reinterpret_cast<const float4*>(a)[0], v = reinterpret_cast<const float4*>(a)[1];
-  return Eight{{u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w}};
+template <typename T> struct Raw;                          // eight channels as they lie in memory
+template <> struct Raw<bf16> { uint4 v; };
+template <> struct Raw<float> { float4 v[2]; };
+__device__ __forceinline__ Raw<float> load8(const float* a) {
+  return Raw<float>{{reinterpret_cast<const float4*>(a)[0], reinterpret_cast<const float4*>(a)[1]}};
 }
-__device__ __forceinline__ Eight load8(const bf16* a) {
-  const uint4 u = *reinterpret_cast<const uint4*>(a);
+__device__ __forceinline__ Raw<bf16> load8(const bf16* a) { return Raw<bf16>{*reinterpret_cast<const uint4*>(a)}; }
+__device__ __forceinline__ Eight open8(const Raw<float>& r) {
+  return Eight{{r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w, r.v[1].x, r.v[1].y, r.v[1].z, r.v[1].w}};
+}
+__device__ __forceinline__ Eight open8(const Raw<bf16>& r) {
+  const uint4 u = r.v;
   return Eight{{__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16), __uint_as_float(u.y & 0xffff0000u),
                 __uint_as_float(u.z << 16), __uint_as_float(u.z & 0xffff0000u), __uint_as_float(u.w << 16), __uint_as_float(u.w & 0xffff0000u)}};
 }
 __device__ __forceinline__ void store1(float* a, float v) { *a = v; }
 __device__ __forceinline__ void store1(bf16* a, float v) { *a = __float2bfloat16_rn(v); }
 
-__device__ __forceinline__ float peer_float(uint32_t own_addr, uint32_t rank) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(ptx::map_to_cta(own_addr, rank)));
-  return v;
+__device__ __forceinline__ void peer_store(uint32_t own_addr, uint32_t rank, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ptx::map_to_cta(own_addr, rank)), "f"(v) : "memory");
 }
 
 // grid: clusters of `splits` blocks, one per (sequence, key head, ROWS rows)
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(THREADS)
 packed_rows_kernel(const PackedCall c, int row_blocks, int splits) {
-  extern __shared__ __align__(16) float sm[];              // [groups][ROWS][d + 2], then [ROWS][d + 2]: weighted values, maximum, sum
+  // [groups][ROWS][d + 2]: weighted values, maximum, sum; then the same of the cluster's blocks, in its first one: [splits][ROWS][d + 2]
+  extern __shared__ __align__(16) float sm[];
   const int d = c.p.d, lanes = d / 8, side = 32 / lanes, groups = WARPS * side, width = d + 2;
   const int item = blockIdx.x / splits, rank = blockIdx.x % splits;
   const int rb = item % row_blocks, kv = item / row_blocks % c.p.kv_heads, seq = item / row_blocks / c.p.kv_heads;
@@ -50,6 +55,7 @@ packed_rows_kernel(const PackedCall c, int row_blocks, int splits) {
   if (!seq_range(c.p, seq, r, c.dev_status)) return;       // the whole cluster leaves
   const int row0 = rb * ROWS, rows = min(ROWS, r.q_len * group - row0);   // row = query * group + head of the group
   if (rows <= 0) return;
+  if (splits > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // this block runs
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slot = lane / lanes, at = lane - slot * lanes;
   const bool active = slot < side;
   const HeadSum sums = head_sum_plan(lanes, at, active ? slot * lanes : 0);
@@ -61,7 +67,7 @@ packed_rows_kernel(const PackedCall c, int row_blocks, int splits) {
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
     const int row = row0 + min(i, rows - 1);
-    q[i] = load8(static_cast<const T*>(c.q) + ((int64_t)r.q_begin + row / group) * c.ldq + (int64_t)(kv * group + row % group) * d + c0);
+    q[i] = open8(load8(static_cast<const T*>(c.q) + ((int64_t)r.q_begin + row / group) * c.ldq + (int64_t)(kv * group + row % group) * d + c0));
     m[i] = -INFINITY;
     l[i] = 0.f;
 #pragma unroll
@@ -73,20 +79,32 @@ packed_rows_kernel(const PackedCall c, int row_blocks, int splits) {
   const int chunk = (r.k_len + splits - 1) / splits, begin = min(r.k_len, rank * chunk), end = min(r.k_len, begin + chunk);
   const T* kp = static_cast<const T*>(c.k) + (int64_t)kv * d + c0;
   const T* vp = static_cast<const T*>(c.v) + (int64_t)kv * d + c0;
+  // the keys of the next round are on their way while this one's are worked on; keys that are not there are zero
+  // (nothing of what lies behind them is looked at) and get probabilities of zero
+  Raw<T> kn[UNROLL], vn[UNROLL];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const int key = k0 + u * groups + slot;
+      kn[u] = Raw<T>{};
+      vn[u] = Raw<T>{};
+      if (active && key < end) {
+        kn[u] = load8(kp + ((int64_t)r.k_begin + key) * c.ldk);
+        vn[u] = load8(vp + ((int64_t)r.k_begin + key) * c.ldv);
+      }
+    }
+  };
+  fetch(begin + warp * side);
   for (int k0 = begin + warp * side; k0 < end; k0 += groups * UNROLL) {
     Eight kk[UNROLL], vv[UNROLL];
     bool there[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {                     // all loads in flight before the first use
-      const int key = k0 + u * groups + slot;
-      there[u] = active && key < end;
-      kk[u] = Eight{};
-      vv[u] = Eight{};                                     // nothing of what lies behind the keys is looked at
-      if (there[u]) {
-        kk[u] = load8(kp + ((int64_t)r.k_begin + key) * c.ldk);
-        vv[u] = load8(vp + ((int64_t)r.k_begin + key) * c.ldv);
-      }
+    for (int u = 0; u < UNROLL; ++u) {
+      there[u] = active && k0 + u * groups + slot < end;
+      kk[u] = open8(kn[u]);
+      vv[u] = open8(vn[u]);
     }
+    if (k0 + groups * UNROLL < end) fetch(k0 + groups * UNROLL);
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       float s[UNROLL];
@@ -131,7 +149,9 @@ packed_rows_kernel(const PackedCall c, int row_blocks, int splits) {
   }
   __syncthreads();
   // the block's groups of lanes, in order: every channel gathers the common maximum for itself
-  float* mine = sm + groups * ROWS * width;
+  float* joined = sm + groups * ROWS * width;
+  const uint32_t mine = ptx::smem_u32(joined + rank * ROWS * width);
+  if (splits > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");                // the first block runs
   for (int e = threadIdx.x; e < ROWS * d; e += THREADS) {
     const int i = e / d, ch = e - i * d;
     float top = -INFINITY, sum = 0.f, o = 0.f;
@@ -143,31 +163,32 @@ packed_rows_kernel(const PackedCall c, int row_blocks, int splits) {
       sum = fmaf(f, from[d + 1], sum);
       o = fmaf(f, from[ch], o);
     }
-    mine[i * width + ch] = o;
+    peer_store(mine + (uint32_t)(i * width + ch) * 4, 0, o);
     if (ch == 0) {
-      mine[i * width + d] = top;
-      mine[i * width + d + 1] = sum;
+      peer_store(mine + (uint32_t)(i * width + d) * 4, 0, top);
+      peer_store(mine + (uint32_t)(i * width + d + 1) * 4, 0, sum);
     }
   }
-  ptx::cluster_sync();
-  // the blocks, in order; each writes its share of the channels
-  const uint32_t base = ptx::smem_u32(mine);
-  for (int e = rank * THREADS + threadIdx.x; e < rows * d; e += splits * THREADS) {
+  if (splits > 1) ptx::cluster_sync();
+  else __syncthreads();
+  if (rank != 0) return;
+  // the blocks, in order
+  for (int e = threadIdx.x; e < rows * d; e += THREADS) {
     const int i = e / d, ch = e - i * d;
     float top = -INFINITY, sum = 0.f, o = 0.f;
-    for (int b = 0; b < splits; ++b) top = fmaxf(top, peer_float(base + (uint32_t)(i * width + d) * 4, b));
+    for (int b = 0; b < splits; ++b) top = fmaxf(top, joined[(b * ROWS + i) * width + d]);
     const float ref = top == -INFINITY ? 0.f : top;
     for (int b = 0; b < splits; ++b) {
-      const float f = exp2f(peer_float(base + (uint32_t)(i * width + d) * 4, b) - ref);
-      sum = fmaf(f, peer_float(base + (uint32_t)(i * width + d + 1) * 4, b), sum);
-      o = fmaf(f, peer_float(base + (uint32_t)(i * width + ch) * 4, b), o);
+      const float* from = joined + (b * ROWS + i) * width;
+      const float f = exp2f(from[d] - ref);
+      sum = fmaf(f, from[d + 1], sum);
+      o = fmaf(f, from[ch], o);
     }
     const int row = row0 + i, head = kv * group + row % group;
     const int64_t to = (int64_t)r.q_begin + row / group;
     store1(static_cast<T*>(c.out) + to * c.ldo + (int64_t)head * d + ch, sum == 0.f ? 0.f : o / sum);      // no keys: zero
     if (ch == 0) c.lse[(int64_t)head * c.p.q_rows + to] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
   }
-  ptx::cluster_sync();                                      // no block leaves while another reads its shared memory
 }
 
 template <typename T, int ROWS>
@@ -180,7 +201,7 @@ cudaError_t launch_variant(const PackedCall& c, cudaStream_t s) {
   int splits = 1;
   while (splits < 8 && items * splits < 2 * sms && c.p.max_k > 64 * splits) splits *= 2;
   const int lanes = c.p.d / 8, groups = WARPS * (32 / lanes);
-  const size_t smem = (size_t)(groups + 1) * ROWS * (c.p.d + 2) * sizeof(float);
+  const size_t smem = (size_t)(groups + splits) * ROWS * (c.p.d + 2) * sizeof(float);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(items * splits));
   cfg.blockDim = dim3(THREADS);
