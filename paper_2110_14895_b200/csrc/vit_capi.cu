@@ -849,7 +849,7 @@ int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_proble
   PackedCall c{};
   c.p = p; c.q = q; c.ldq = ldq; c.k = k; c.ldk = ldk; c.v = v; c.ldv = ldv; c.out = out; c.ldo = ldo; c.lse = lse;
   c.dev_status = h->dev_status;
-  if (attention_rows_supported(p)) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_rows(c, dtype == VIT_BF16, s));
+  if (attention_rows_supported(p, dtype == VIT_BF16)) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_rows(c, dtype == VIT_BF16, s));
   else if (dtype == VIT_BF16) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_bf16(c, s));
   else VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_f32(c, s));
   return VIT_OK;

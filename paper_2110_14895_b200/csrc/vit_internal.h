@@ -185,10 +185,8 @@ struct PackedCall {
   float2* delta;                            // backward: [heads][q_rows] (lse log2(e), rowsum(dout * out))
   int* dev_status;
 };
-// up to this many queries (times heads that share a key head) of a sequence go to the kernel for few rows
-// (attention_rows.cu); beyond, to those that work on tiles of scores
-constexpr int ATTENTION_MAX_ROWS = 8;
-bool attention_rows_supported(const vit_attention_problem& p);
+// a few queries (times heads that share a key head) of a sequence go to the kernel for few rows (attention_rows.cu)
+bool attention_rows_supported(const vit_attention_problem& p, bool act_bf16);
 cudaError_t launch_attention_rows(const PackedCall& c, bool act_bf16, cudaStream_t s);
 cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s);
