@@ -106,15 +106,15 @@ __device__ __forceinline__ void issue_scores_ss(uint32_t d_tmem, uint32_t x, uin
       umma_bf16(d_tmem, xd + (uint64_t)((k >> 2) * (RT * 8) + 2 * (k & 3)), yd + (uint64_t)((k >> 2) * (Y_ROWS * 8) + 2 * (k & 3)), id,
                 k > 0 ? 1u : 0u);
 }
-// D[128 x d] (+)= P[128 x 64] . Y[64 rows x d], `ksteps` of the four steps of 16 rows; P packed in tensor memory;
-// y: the first of the 64 rows in a tile of Y_ROWS
-template <int Y_ROWS>
+// D[128 x d] (+)= P[128 x 64] . Y[64 rows x d], `ksteps` of the four steps of 16 rows; P packed in tensor memory, in
+// 32 columns or (HALVES) in 16 at the start of each half of 64; y: the first of the 64 rows in a tile of Y_ROWS
+template <int Y_ROWS, bool HALVES>
 __device__ __forceinline__ void issue_weighted(uint32_t d_tmem, uint32_t p_tmem, uint32_t y, int d, int ksteps, bool first) {
   const uint32_t id = idesc(d, true);
   const uint64_t yd = desc_sw128(y, Y_ROWS * 128);
 #pragma unroll
   for (int k = 0; k < 4; ++k)
-    if (k < ksteps) umma_bf16_ts(d_tmem, p_tmem + (uint32_t)(8 * k), yd + (uint64_t)(k * 128), id, first && k == 0 ? 0u : 1u);
+    if (k < ksteps) umma_bf16_ts(d_tmem, p_tmem + (uint32_t)(8 * k + (HALVES && k >= 2 ? 16 : 0)), yd + (uint64_t)(k * 128), id, first && k == 0 ? 0u : 1u);
 }
 // The 16 channels 16 g ... of a row of a swizzled tile of 128 rows in shared memory
 __device__ __forceinline__ void read_16(uint32_t (&w)[8], uint32_t tile, int row, int g) {
@@ -405,7 +405,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
           if (n16 > 4) {
             if (elect_one()) {
               tc_fence_after();
-              issue_weighted<RT>(base + F_O, base, vs, d, 4, j == 0);
+              issue_weighted<RT, false>(base + F_O, base, vs, d, 4, j == 0);
             }
             __syncwarp();
             if (!warp_wait(bar(F_P + 2 * h + 1), turn, abort_flag)) { ok = false; break; }
@@ -415,8 +415,8 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
         if (elect_one()) {
           if (mine) {
             tc_fence_after();
-            if (n16 > 4) issue_weighted<RT>(base + F_O, base + 64, vs + 64 * 128, d, n16 - 4, false);
-            else issue_weighted<RT>(base + F_O, base, vs, d, n16, j == 0);
+            if (n16 > 4) issue_weighted<RT, false>(base + F_O, base + 64, vs + 64 * 128, d, n16 - 4, false);
+            else issue_weighted<RT, false>(base + F_O, base, vs, d, n16, j == 0);
             umma_commit(bar(F_PV + h));
           }
           umma_commit(bar(F_VFREE + st));
@@ -593,12 +593,12 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
 //   DKDV: X = K, V; Y = Q, dout of every query head that shares the key head (scores transposed);
 //         dv += P Y2, dk += dS Y1
 // Seven products instead of the five of a single pass, but every gradient is summed in one place in a fixed
-// order.  Two warpgroups take the tiles in turn, each with its own columns of tensor memory for S and dP:
-// while one is in its exp2 phase the tensor core works for the other; one warp issues the scores, another the
-// second products.  X is in tensor memory (XT) where it fits beside the accumulators: always for DQ, up to
+// order.  Tiles alternate between two places in tensor memory for S and dP, each with two warpgroups that take 32
+// of its 64 columns: while one pair is in its exp2 phase the tensor core works for the other, and four warps a
+// scheduler hide each other's latencies; one warp issues the scores, another the second products.  X is in tensor memory (XT) where it fits beside the accumulators: always for DQ, up to
 // d = 80 for DKDV.
 struct BackwardMaps { CUtensorMap x1, x2, x3, y1, y2; };
-constexpr int B_MMA_WARP = 8 /* two */, B_TMA_WARP = 10, B_THREADS = 352;
+constexpr int B_MMA_WARP = 16 /* two */, B_TMA_WARP = 18, B_THREADS = 608;
 
 template <int SLABS, bool DKDV>
 struct BackwardCfg {
@@ -633,7 +633,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < B_BARS; ++i)
-      mbar_init(bar(i), i == B_P || i == B_P + 1 ? 4 : i == B_ACCFREE || i == B_X || (XT && i == B_XSFREE) ? 8 : 1);
+      mbar_init(bar(i), i == B_P || i == B_P + 1 || i == B_ACCFREE ? 8 : i == B_X ? 16 : XT && i == B_XSFREE ? (DKDV ? 8 : 12) : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
@@ -759,8 +759,8 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
           if (t == 0 && !warp_wait(bar(B_ACCFREE), (pieces & 1) ^ 1, abort_flag)) { ok = false; break; }
           if (elect_one()) {
             tc_fence_after();
-            if (DKDV) issue_weighted<CT>(tmem + acc1, s_col, y + L::YTILE, d, n16, t == 0);
-            issue_weighted<CT>(tmem + acc2, s_col + CT, y, d, n16, t == 0);
+            if (DKDV) issue_weighted<CT, true>(tmem + acc1, s_col, y + L::YTILE, d, n16, t == 0);
+            issue_weighted<CT, true>(tmem + acc2, s_col + CT, y, d, n16, t == 0);
             umma_commit(bar(B_SFREE + b));
             umma_commit(bar(B_FREE + st));
             if (t == n - 1) umma_commit(bar(B_ACC));
@@ -778,9 +778,10 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     }
   } else {
     // ------------------------------------------------------------------ probabilities and their gradients
-    const int wg = warp >> 2, quarter = warp & 3, in_tile = quarter * 32 + lane;
+    // warpgroups 0, 1: the two halves of the even tiles' columns; 2, 3: of the odd tiles'
+    const int wg = warp >> 2, place = wg >> 1, half = wg & 1, quarter = warp & 3, in_tile = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t taddr = lanes + wg * B_WG, stage = sb + L::OFF_OUT + warp * 2048;
+    const uint32_t taddr = lanes + place * B_WG + half * 32, stage = sb + L::OFF_OUT + (warp & 7) * 2048;
     const float sl2 = c.p.scale * LOG2E;
     const float2 sl2v = make_float2(sl2, sl2);
     Ring<L::STAGES> ring;                                        // of every tile, this warpgroup's or not
@@ -802,36 +803,38 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       }
       return i;
     };
-    // this thread's row of X1 (first warpgroup) or X2 (second) of piece w into tensor memory; the second
-    // warpgroup of DQ has dout and takes its product with out on the way
+    // Rows of X1 (first warpgroup) and X2 (second) of piece w into tensor memory; the third of DQ takes the
+    // product of dout and out.  All of them answer for it, so that none is a piece behind.
     auto load_x = [&] {
-      if (!warp_wait(bar(B_XS), pieces & 1, abort_flag)) return false;
-      row_to_tmem<SLABS>(lanes + (wg == 0 ? x1_col : x2_col), sb + wg * L::XTILE, in_tile, d);
-      if (!DKDV && wg == 1) {
-        const int row = w.x0 + in_tile;
-        const int64_t i = (int64_t)w.head * c.p.q_rows + w.r.q_begin + row;
-        const bool there = row < w.r.q_len;
-        const float lse = there ? c.lse[i] : 0.f;
-        float delta = 0.f;
-#pragma unroll
-        for (int g = 0; g < 4 * SLABS; ++g)
-          if (g < d / 16) {
+      if (wg < (DKDV ? 2 : 3)) {
+        if (!warp_wait(bar(B_XS), pieces & 1, abort_flag)) return false;
+        if (wg < 2) {
+          row_to_tmem<SLABS>(lanes + (wg == 0 ? x1_col : x2_col), sb + wg * L::XTILE, in_tile, d);
+          tmem_st_wait();
+          tc_fence_before();
+        } else {
+          const int row = w.x0 + in_tile;
+          const int64_t i = (int64_t)w.head * c.p.q_rows + w.r.q_begin + row;
+          const bool there = row < w.r.q_len;
+          const float lse = there ? c.lse[i] : 0.f;
+          float delta = 0.f;
+#pragma unroll 2
+          for (int g = 0; g < d / 16; ++g) {
             uint32_t u[8], v[8];
             read_16(u, sb + L::XTILE, in_tile, g);
             read_16(v, sb + 2 * L::XTILE, in_tile, g);
 #pragma unroll
             for (int e = 0; e < 8; ++e) delta = dot2(u[e], v[e], delta);
           }
-        const float2 mine = make_float2(lse * LOG2E, delta);
-        reinterpret_cast<float2*>(smem + L::OFF_ROW)[(pieces & 1) * RT + in_tile] = mine;
-        if (there) c.delta[i] = mine;
+          const float2 mine = make_float2(lse * LOG2E, delta);
+          reinterpret_cast<float2*>(smem + L::OFF_ROW)[(pieces & 1) * RT + in_tile] = mine;
+          if (there) c.delta[i] = mine;
+        }
       }
-      tmem_st_wait();
-      tc_fence_before();
       __syncwarp();
       if (lane == 0) {
         mbar_arrive(bar(B_X));
-        mbar_arrive(bar(B_XSFREE));
+        if (wg < (DKDV ? 2 : 3)) mbar_arrive(bar(B_XSFREE));
       }
       return true;
     };
@@ -850,29 +853,24 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       }
       int left = y_len;                                          // rows of this head from the present tile on
       for (int t = 0; t < n; ++t, ring.step()) {
-        const int here = min(CT, left);
+        const int here = min(CT, left) - 32 * half;              // of this warpgroup's 32 columns
         left = left > CT ? left - CT : y_len;
-        if ((t & 1) != wg) continue;
+        if ((t & 1) != place) continue;
         const int st = ring.at;
-        const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2);   // four columns each: -lse2, then -delta
+        // four columns each: -lse2, then -delta
+        const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2) + 8 * half;
         if (DKDV && !warp_wait(bar(B_FULL + st), ring.parity, abort_flag)) { ok = false; break; }
-        if (!warp_wait(bar(B_S + wg), s_phase, abort_flag)) { ok = false; break; }
+        if (!warp_wait(bar(B_S + place), s_phase, abort_flag)) { ok = false; break; }
         s_phase ^= 1;
         tc_fence_after();
-        if (rows > 0) {
-          // 16 columns at a time, those of the next step on their way
-          uint32_t s[2][16], g[2][16];
-          tmem_ld16(taddr, s[0]);
-          tmem_ld16(taddr + CT, g[0]);
+        if (rows > 0 && here > 0) {
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
+          for (int h = 0; h < 2; ++h) {
             if (16 * h >= here) break;
-            uint32_t (&sh)[16] = s[h & 1], (&gh)[16] = g[h & 1];
+            uint32_t sh[16], gh[16];
+            tmem_ld16(taddr + 16 * h, sh);
+            tmem_ld16(taddr + CT + 16 * h, gh);
             tmem_ld_wait_16(sh, gh);
-            if (h < 3 && 16 * (h + 1) < here) {
-              tmem_ld16(taddr + 16 * (h + 1), s[(h + 1) & 1]);
-              tmem_ld16(taddr + CT + 16 * (h + 1), g[(h + 1) & 1]);
-            }
             uint32_t pk[8], dk[8];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -887,7 +885,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
                 const float2 a = f ? make_float2(a4.z, a4.w) : make_float2(a4.x, a4.y), b = f ? make_float2(b4.z, b4.w) : make_float2(b4.x, b4.y);
                 const float2 x = __ffma2_rn(make_float2(__uint_as_float(sh[2 * e]), __uint_as_float(sh[2 * e + 1])), sl2v, a);
                 float2 pr = make_float2(ex2_approx(x.x), ex2_approx(x.y));
-                if (!DKDV && here < CT) {                        // keys behind the end
+                if (!DKDV && here < 32) {                        // keys behind the end
                   if (16 * h + 2 * e >= here) pr.x = 0.f;
                   if (16 * h + 2 * e + 1 >= here) pr.y = 0.f;
                 }
@@ -896,7 +894,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
                 dk[e] = pack_bf16(y.x, y.y);
               }
             }
-            // over scores that have been read: step h takes columns [8 h, 8 h + 8)
+            // over scores that this warp has read: step h takes columns [8 h, 8 h + 8) of its 32
             if (DKDV) tmem_st8(taddr + 8 * h, pk);
             tmem_st8(taddr + CT + 8 * h, dk);
           }
@@ -904,7 +902,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bar(B_P + wg));
+        if (lane == 0) mbar_arrive(bar(B_P + place));
       }
       if (!ok) break;
       ++pieces;
@@ -915,10 +913,12 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         tc_fence_after();
         if (!load_x()) break;
       }
+      if (wg >= 2) continue;
+      // the first two warpgroups store the sums
       if (!warp_wait(bar(B_ACC), (pieces - 1) & 1, abort_flag)) break;
       tc_fence_after();
       if (rows > 0) {
-        if (DKDV) {                                              // dk by the first warpgroup, dv by the second
+        if (DKDV) {                                              // dk and dv
           const int64_t ld = wg == 0 ? c.lddk : c.lddv;
           store_rows(static_cast<bf16*>(wg == 0 ? c.dk : c.dv) + at0 * ld + (int64_t)head * d, ld, lanes + (wg == 0 ? acc2 : acc1), d,
                      wg == 0 ? c.p.scale : 1.f, rows, stage, lane);
