@@ -82,7 +82,7 @@ packed_forward_kernel(const PackedCall c) {
   const int tiles = (c.p.max_q + BT - 1) / BT;
   const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
   SeqRange r;
-  if (!seq_range(c.p, seq, r, c.dev_status)) return;
+  if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
   const int q0 = tile * BT;
   if (q0 >= r.q_len) return;
   const int q_here = min(BT, r.q_len - q0), d = c.p.d;
@@ -203,7 +203,7 @@ packed_dkdv_kernel(const PackedCall c) {
   const int tiles = (c.p.max_k + BT - 1) / BT;
   const int tile = blockIdx.x % tiles, kv = blockIdx.x / tiles % c.p.kv_heads, seq = blockIdx.x / tiles / c.p.kv_heads;
   SeqRange r;
-  if (!seq_range(c.p, seq, r, c.dev_status)) return;
+  if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
   const int k0 = tile * BT;
   if (k0 >= r.k_len) return;
   const int k_here = min(BT, r.k_len - k0), d = c.p.d, group = c.p.heads / c.p.kv_heads;
@@ -273,7 +273,7 @@ packed_dq_kernel(const PackedCall c) {
   const int tiles = (c.p.max_q + BT - 1) / BT;
   const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
   SeqRange r;
-  if (!seq_range(c.p, seq, r, c.dev_status)) return;
+  if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
   const int q0 = tile * BT;
   if (q0 >= r.q_len) return;
   const int q_here = min(BT, r.q_len - q0), d = c.p.d, kv = head / (c.p.heads / c.p.kv_heads);

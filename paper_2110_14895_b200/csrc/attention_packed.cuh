@@ -8,12 +8,12 @@ struct SeqRange { int q_begin, q_len, k_begin, k_len; };
 
 // The offsets live on the device and are the caller's: a sequence whose rows are not in order, not inside
 // the buffers or more than the call allowed for is skipped, and the status word says so.
-__device__ __forceinline__ bool seq_range(const vit_attention_problem& p, int seq, SeqRange& r, int* dev_status) {
+__device__ __forceinline__ bool seq_range(const vit_attention_problem& p, int seq, SeqRange& r, int* dev_status, bool report) {
   const int qb = p.q_offsets[seq], qe = p.q_offsets[seq + 1], kb = p.k_offsets[seq], ke = p.k_offsets[seq + 1];
   const bool ok = qb >= 0 && qe >= qb && qe <= p.q_rows && qe - qb <= p.max_q &&
                   kb >= 0 && ke >= kb && ke <= p.k_rows && ke - kb <= p.max_k;
   if (!ok) {
-    if (threadIdx.x == 0) atomicExch(dev_status, (int)VIT_ERR_OFFSETS);
+    if (report) atomicExch(dev_status, (int)VIT_ERR_OFFSETS);
     return false;
   }
   r = SeqRange{qb, qe - qb, kb, ke - kb};

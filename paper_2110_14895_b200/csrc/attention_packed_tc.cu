@@ -54,9 +54,14 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
       "l"(reinterpret_cast<uint64_t>(tm)), "r"(c), "r"(head), "r"(row), "r"(bar)
       : "memory");
 }
-// a bounded wait of a whole warp: all lanes leave with the same answer
+// a bounded wait of a whole warp: all lanes leave with the same answer.  Only the first look is in line: the
+// kernels wait in many places, and their code has to fit the instruction cache.
+__device__ __noinline__ bool wait_on(uint32_t bar, int parity, volatile int* abort_flag, long long limit) {
+  return mbar_wait_limit(bar, (uint32_t)parity, abort_flag, limit);
+}
 __device__ __forceinline__ bool warp_wait(uint32_t bar, int parity, volatile int* abort_flag, long long limit = WAIT_LIMIT_CYCLES) {
-  return __all_sync(0xffffffffu, mbar_wait_limit(bar, (uint32_t)parity, abort_flag, limit));
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, (uint32_t)parity))) return true;
+  return __all_sync(0xffffffffu, wait_on(bar, parity, abort_flag, limit));
 }
 // rows [from, rows) of a tile of `slabs` slabs become zero; one warp, then visible to the tensor core
 __device__ __forceinline__ void zero_rows(uint32_t tile, int rows, int slabs, int from, int lane) {
@@ -174,45 +179,70 @@ __device__ __forceinline__ void store_rows(bf16* dst, int64_t ld, uint32_t taddr
   }
 }
 
-// Division by a number that is the same for the whole launch: q = (t + ((n - t) >> 1)) >> shift with
-// t = high word of n * mul (Granlund and Montgomery's method for 32 bits)
-struct Divisor { uint32_t d, mul, shift; };
-Divisor divisor(uint32_t d) {
-  uint32_t l = 0;
-  while (l < 32 && ((uint64_t)1 << l) < d) ++l;
-  return Divisor{d, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1), l > 0 ? l - 1 : 0};
-}
-__device__ __forceinline__ uint32_t divide(uint32_t n, const Divisor& v) {
-  if (v.d == 1) return n;
-  const uint32_t t = __umulhi(n, v.mul);
-  return (t + ((n - t) >> 1)) >> v.shift;
-}
-struct Pieces { int total; Divisor tiles, heads; };             // of a launch: number, tiles of a sequence, heads
-
-// The sequences' offsets are kept in shared memory where they fit: every role of a block looks at them for every piece.
-constexpr int MAX_STAGED = 1024;
-constexpr uint32_t OFFSETS_BYTES = 2 * (MAX_STAGED + 1) * 4 + 8;
-__device__ __forceinline__ void stage_offsets(vit_attention_problem& p, int32_t* to) {
-  if (p.sequences > MAX_STAGED) return;
-  for (int i = threadIdx.x; i <= p.sequences; i += (int)blockDim.x) {
-    to[i] = p.q_offsets[i];
-    to[MAX_STAGED + 1 + i] = p.k_offsets[i];
-  }
-  p.q_offsets = to;
-  p.k_offsets = to + MAX_STAGED + 1;
-}
-
 // A piece of work: `span` rows of one head of one sequence.
 struct Piece { int head, x0; SeqRange r; };
-// The first piece from number i on (in steps of the grid) whose rows exist; i >= total if there is none.
-__device__ __forceinline__ int find_piece(const vit_attention_problem& p, int* status, int i, const Pieces& all, int span, bool of_keys, Piece& w) {
-  for (; i < all.total; i += (int)gridDim.x) {
-    const uint32_t hs = divide((uint32_t)i, all.tiles), seq = divide(hs, all.heads);
-    w.head = (int)(hs - seq * all.heads.d);
-    w.x0 = (int)((uint32_t)i - hs * all.tiles.d) * span;
-    if (seq_range(p, (int)seq, w.r, status) && w.x0 < (of_keys ? w.r.k_len : w.r.q_len)) break;
+// A block's pieces are looked up once, at its start: numbers blockIdx.x, + gridDim.x, ... of those whose rows exist, so
+// that every block gets the same number of them however the lengths differ.
+constexpr int MAX_PIECES = 128, SEQ_CHUNK = 512;                 // of a block; sequences looked at together
+constexpr uint32_t TABLE_BYTES = MAX_PIECES * 32;
+__device__ __forceinline__ Piece piece_at(uint32_t table, int n) {
+  Piece w;
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.head), "=r"(w.x0), "=r"(w.r.q_begin), "=r"(w.r.q_len) : "r"(table + 32u * n));
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w.r.k_begin), "=r"(w.r.k_len) : "r"(table + 32u * n + 16));
+  return w;
+}
+// All threads of the block; ends with a barrier.  `of_keys`: pieces are of the keys' rows, else of the queries'.
+// before: shared memory for 5 SEQ_CHUNK + 1 numbers that is not needed afterwards.  Returns the number of the block's pieces.
+__device__ __forceinline__ int find_pieces(const vit_attention_problem& p, int* status, int span, bool of_keys, int heads, int32_t* table, int32_t* before) {
+  int carry = 0;
+  for (int s0 = 0; s0 < p.sequences; s0 += SEQ_CHUNK) {
+    const int chunk = min(SEQ_CHUNK, p.sequences - s0);
+    int4* ranges = reinterpret_cast<int4*>(before + SEQ_CHUNK + 4);
+    for (int s = threadIdx.x; s < chunk; s += (int)blockDim.x) {
+      SeqRange r{0, 0, 0, 0};
+      seq_range(p, s0 + s, r, status, true);
+      before[s] = ((of_keys ? r.k_len : r.q_len) + span - 1) / span * heads;
+      ranges[s] = make_int4(r.q_begin, r.q_len, r.k_begin, r.k_len);
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {                                      // counts become the number of pieces before each sequence
+      int sum = carry;
+      for (int b = 0; b < chunk; b += 32) {
+        const int s = b + (int)threadIdx.x, n = s < chunk ? before[s] : 0;
+        int up = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int other = __shfl_up_sync(0xffffffffu, up, o);
+          if ((int)threadIdx.x >= o) up += other;
+        }
+        if (s < chunk) before[s] = sum + up - n;
+        sum += __shfl_sync(0xffffffffu, up, 31);
+      }
+      if (threadIdx.x == 0) before[chunk] = sum;
+    }
+    __syncthreads();
+    const int end = before[chunk];
+    for (int j = threadIdx.x; j < MAX_PIECES; j += (int)blockDim.x) {
+      const int i = (int)blockIdx.x + j * (int)gridDim.x;
+      if (i < carry || i >= end) continue;
+      int lo = 0, hi = chunk;                                    // before[lo] <= i < before[hi]
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (before[mid] <= i) lo = mid;
+        else hi = mid;
+      }
+      const int4 r = ranges[lo];
+      const int tiles = ((of_keys ? r.w : r.y) + span - 1) / span, k = i - before[lo], head = k / tiles;
+      int32_t* to = table + 8 * j;
+      *reinterpret_cast<int4*>(to) = make_int4(head, (k - head * tiles) * span, r.x, r.y);
+      to[4] = r.z;
+      to[5] = r.w;
+    }
+    __syncthreads();                                             // `before` is read no more
+    carry = end;
   }
-  return i;
+  __syncthreads();
+  return carry > (int)blockIdx.x ? (carry - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
 }
 // Place in a ring of stages and the parity of its present round
 template <int N>
@@ -244,7 +274,7 @@ struct ForwardCfg {
   static constexpr uint32_t TILE = SLABS * RT * 128;             // of queries, keys or values
   static constexpr uint32_t OFF_K = 2 * TILE, OFF_V = OFF_K + STAGES * TILE, OFF_OUT = OFF_V + STAGES * TILE;
   static constexpr uint32_t OFF_BARS = OFF_OUT + 8 * 2048, OFF_SEQ = OFF_BARS + 512;
-  static constexpr uint32_t BYTES = OFF_SEQ + OFFSETS_BYTES + 1024;
+  static constexpr uint32_t BYTES = OFF_SEQ + TABLE_BYTES + 1024;
   static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
 // Columns of a warpgroup (256): scores (128), the accumulator (d), the queries (d / 2) where they fit (XT).
@@ -286,7 +316,7 @@ __device__ __forceinline__ void mask_32(uint32_t (&x)[32], int left) {
 
 template <int SLABS, bool XT>
 __global__ void __launch_bounds__(F_THREADS, 1)
-packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedCall c, const Pieces all) {
+packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedCall c) {
   using L = ForwardCfg<SLABS>;
   extern __shared__ uint8_t smem_raw[];
   const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
@@ -306,14 +336,19 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == F_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
-  vit_attention_problem p = c.p;
-  stage_offsets(p, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ));
+  const int pieces = find_pieces(c.p, c.dev_status, 2 * RT, false, c.p.heads, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ),
+                                 reinterpret_cast<int32_t*>(smem));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
-  auto find = [&](int i, Piece& w) { return find_piece(p, c.dev_status, i, all, 2 * RT, false, w); };
   Piece w;
+  int at_piece = 0;
+  auto advance = [&] {
+    if (at_piece >= pieces) return false;
+    w = piece_at(sb + L::OFF_SEQ, at_piece++);
+    return true;
+  };
 
   if (warp == F_TMA_WARP) {
     // ------------------------------------------------------------------ TMA producer
@@ -321,7 +356,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       Ring<L::STAGES> ring;
       int q0 = 0, q1 = 0, n_all = 0;                             // tiles of queries of each warpgroup, of keys so far
       bool ok = true;
-      for (int i = find(blockIdx.x, w); i < all.total && ok; i = find(i + gridDim.x, w)) {
+      while (ok && advance()) {
         const int n = (w.r.k_len + RT - 1) / RT, kv = group == 1 ? w.head : w.head / group;
         if (n == 0) continue;
 #pragma unroll
@@ -364,7 +399,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     Ring<L::STAGES> ring;
     int seen = 0, turn = 0;                                      // parities: pieces and tiles of this warpgroup so far
     bool ok = true;
-    for (int i = find(blockIdx.x, w); i < all.total && ok; i = find(i + gridDim.x, w)) {
+    while (ok && advance()) {
       const int n = (w.r.k_len + RT - 1) / RT;
       if (n == 0) continue;
       const bool mine = w.x0 + h * RT < w.r.q_len;               // else the stages are passed on only
@@ -438,10 +473,10 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     const float sl2 = c.p.scale * LOG2E;
     const float2 sl2v = make_float2(sl2, sl2);
     // the next piece that has keys and rows for this warpgroup; queries without keys are finished on the way
-    auto next = [&](int i) {
-      for (i = find(i, w); i < all.total; i = find(i + gridDim.x, w)) {
+    auto next = [&] {
+      while (advance()) {
         if (w.x0 + wg * RT >= w.r.q_len) continue;
-        if (w.r.k_len > 0) break;
+        if (w.r.k_len > 0) return true;
         const int row = w.x0 + wg * RT + quarter * 32 + lane;
         if (row < w.r.q_len) {
           const int64_t at = (int64_t)w.r.q_begin + row;
@@ -450,7 +485,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
           c.lse[(int64_t)w.head * c.p.q_rows + at] = -INFINITY;
         }
       }
-      return i;
+      return false;
     };
     int turn = 0, seen = 0;                                      // parities: tiles and pieces of this warpgroup so far
     // A warp of each warpgroup shares a scheduler and its exp2 unit.  They take turns there, so that one fetches
@@ -470,14 +505,14 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       }
       return true;
     };
-    int i = next(blockIdx.x);
-    bool ok = !XT || i >= all.total || load_query();
-    while (i < all.total && ok) {
+    bool more = next();
+    bool ok = !XT || !more || load_query();
+    while (more && ok) {
       const int head = w.head, k_len = w.r.k_len, row0 = w.x0 + wg * RT + quarter * 32;
       const int rows = min(32, w.r.q_len - row0);                // of this warp that exist; none if not positive
       const int64_t at0 = (int64_t)w.r.q_begin + row0;
       const bool pair = w.r.q_len - w.x0 > RT;
-      i = next(i + gridDim.x);                                   // looked up while the first scores are computed
+      more = next();                                             // looked up while the first scores are computed
       float m = -INFINITY, l = 0.f;                              // row maximum in use (raw scores), row sum
       for (int k0 = 0; k0 < k_len; k0 += RT) {
         const int here = min(RT, k_len - k0);
@@ -563,7 +598,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
         if (pair) go ^= 1;
       }
       if (!ok) break;
-      if (XT && i < all.total && !load_query()) break;
+      if (XT && more && !load_query()) break;
       if (!warp_wait(bar(F_PV + wg), turn ^ 1, abort_flag)) break;
       tc_fence_after();
       if (rows > 0) {
@@ -608,7 +643,7 @@ struct BackwardCfg {
   static constexpr uint32_t OFF_Y = XS * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // DKDV: float [STAGES][2][64] -lse2, -delta of the columns
   static constexpr uint32_t OFF_ROW = OFF_COL + (DKDV ? STAGES * CT * 8 : 0);           // DQ: float2 [2][128] of the rows
   static constexpr uint32_t OFF_OUT = OFF_ROW + (DKDV ? 0 : 2 * RT * 8), OFF_BARS = OFF_OUT + 8 * 2048, OFF_SEQ = OFF_BARS + 512;
-  static constexpr uint32_t BYTES = OFF_SEQ + OFFSETS_BYTES + 1024;
+  static constexpr uint32_t BYTES = OFF_SEQ + TABLE_BYTES + 1024;
   static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
 // columns: S and dP of the two warpgroups, then the accumulators (d each), then X1 and X2 (d / 2 each)
@@ -620,7 +655,7 @@ enum BwdBar : int {
 
 template <int SLABS, bool DKDV, bool XT>
 __global__ void __launch_bounds__(B_THREADS, 1)
-packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, const Pieces all) {
+packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c) {
   using L = BackwardCfg<SLABS, DKDV>;
   extern __shared__ uint8_t smem_raw[];
   const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
@@ -637,15 +672,20 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
-  vit_attention_problem p = c.p;
-  stage_offsets(p, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ));
+  const int pieces_in_all = find_pieces(c.p, c.dev_status, RT, DKDV, DKDV ? c.p.kv_heads : c.p.heads,
+                                        reinterpret_cast<int32_t*>(smem + L::OFF_SEQ), reinterpret_cast<int32_t*>(smem));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
   const uint32_t acc2 = B_COLS, acc1 = B_COLS + d, x1_col = B_COLS + (DKDV ? 2 : 1) * d, x2_col = x1_col + d / 2;   // dk or dq; dv
   Piece w;
-  auto find = [&](int i) { return find_piece(p, c.dev_status, i, all, RT, DKDV, w); };
+  int at_piece = 0;
+  auto advance = [&] {
+    if (at_piece >= pieces_in_all) return false;
+    w = piece_at(sb + L::OFF_SEQ, at_piece++);
+    return true;
+  };
   // tiles of Y that a piece walks over, head after head
   auto y_tiles_of = [&] { return ((DKDV ? w.r.q_len : w.r.k_len) + CT - 1) / CT; };
 
@@ -654,7 +694,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     Ring<L::STAGES> ring;
     int pieces = 0, n_all = 0;
     bool ok = true;
-    for (int i = find(blockIdx.x); i < all.total && ok; i = find(i + gridDim.x)) {
+    while (ok && advance()) {
       const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles;
       const int y_begin = DKDV ? w.r.q_begin : w.r.k_begin, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
@@ -720,7 +760,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     Ring<L::STAGES> ring;
     int pieces = 0, phase = 0;                                   // bit b of phase: parity of the next wait for warpgroup b's columns
     bool ok = true;
-    for (int i = find(blockIdx.x); i < all.total && ok; i = find(i + gridDim.x)) {
+    while (ok && advance()) {
       const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
       if (scores && !warp_wait(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
@@ -787,9 +827,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     Ring<L::STAGES> ring;                                        // of every tile, this warpgroup's or not
     int pieces = 0, s_phase = 0;
     // the next piece with something to walk over; rows that nothing meets get gradients of zero on the way
-    auto next = [&](int i) {
-      for (i = find(i); i < all.total; i = find(i + gridDim.x)) {
-        if (y_tiles_of() > 0) break;
+    auto next = [&] {
+      while (advance()) {
+        if (y_tiles_of() > 0) return true;
         const int row = w.x0 + in_tile;
         const int64_t at = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row;
         if (wg == 0 && row < (DKDV ? w.r.k_len : w.r.q_len)) {
@@ -801,7 +841,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
           }
         }
       }
-      return i;
+      return false;
     };
     // Rows of X1 (first warpgroup) and X2 (second) of piece w into tensor memory; the third of DQ takes the
     // product of dout and out.  All of them answer for it, so that none is a piece behind.
@@ -838,9 +878,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       }
       return true;
     };
-    int i = next(blockIdx.x);
-    bool ok = !XT || i >= all.total || load_x();
-    while (i < all.total && ok) {
+    bool more = next();
+    bool ok = !XT || !more || load_x();
+    while (more && ok) {
       const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
       const int head = w.head, row0 = w.x0 + quarter * 32, rows = min(32, (DKDV ? w.r.k_len : w.r.q_len) - row0);
       const int64_t at0 = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row0;
@@ -906,8 +946,8 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       }
       if (!ok) break;
       ++pieces;
-      i = next(i + gridDim.x);
-      if (XT && i < all.total) {
+      more = next();
+      if (XT && more) {
         // every score of the last piece is complete: its X may be overwritten
         if (!warp_wait(bar(B_XFREE), (pieces - 1) & 1, abort_flag)) break;
         tc_fence_after();
@@ -972,6 +1012,12 @@ bool encode_heads(CUtensorMap* tm, const void* base, int64_t rows, int heads, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// one persistent block per SM; more where its table of pieces would not hold its share
+int grid_of(int total, int sms) {
+  const int least = (total + MAX_PIECES - 1) / MAX_PIECES, most = total < sms ? total : sms;
+  return least > most ? least : most;
+}
+
 template <int SLABS, bool XT>
 cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
   using L = ForwardCfg<SLABS>;
@@ -988,7 +1034,7 @@ cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
   const int sms = current_device_sm_count();
   if (sms < 1) return cudaErrorInvalidDevice;
   const int tiles = (c.p.max_q + 2 * RT - 1) / (2 * RT), total = c.p.sequences * c.p.heads * tiles;
-  packed_forward_tc_kernel<SLABS, XT><<<total < sms ? total : sms, F_THREADS, L::BYTES, s>>>(m, c, Pieces{total, divisor(tiles), divisor(c.p.heads)});
+  packed_forward_tc_kernel<SLABS, XT><<<grid_of(total, sms), F_THREADS, L::BYTES, s>>>(m, c);
   return cudaGetLastError();
 }
 
@@ -1013,7 +1059,7 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
   const int sms = current_device_sm_count();
   if (sms < 1) return cudaErrorInvalidDevice;
   const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT, total = c.p.sequences * xh * tiles;
-  packed_backward_tc_kernel<SLABS, DKDV, XT><<<total < sms ? total : sms, B_THREADS, L::BYTES, s>>>(m, c, Pieces{total, divisor(tiles), divisor(xh)});
+  packed_backward_tc_kernel<SLABS, DKDV, XT><<<grid_of(total, sms), B_THREADS, L::BYTES, s>>>(m, c);
   return cudaGetLastError();
 }
 

@@ -52,7 +52,7 @@ packed_rows_kernel(const PackedCall c, int row_blocks, int splits) {
   const int rb = item % row_blocks, kv = item / row_blocks % c.p.kv_heads, seq = item / row_blocks / c.p.kv_heads;
   const int group = c.p.heads / c.p.kv_heads;
   SeqRange r;
-  if (!seq_range(c.p, seq, r, c.dev_status)) return;       // the whole cluster leaves
+  if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;       // the whole cluster leaves
   const int row0 = rb * ROWS, rows = min(ROWS, r.q_len * group - row0);   // row = query * group + head of the group
   if (rows <= 0) return;
   if (splits > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");      // this block runs
