@@ -179,6 +179,32 @@ __device__ __forceinline__ void store_rows(bf16* dst, int64_t ld, uint32_t taddr
   }
 }
 
+// the same in fp32, 16 columns at a time
+__device__ __forceinline__ void store_rows(float* dst, int64_t ld, uint32_t taddr, int cols, float by, int rows, uint32_t stage, int lane) {
+  for (int c = 0; c < cols; c += 16) {
+    uint32_t o[16];
+    tmem_ld16(taddr + (uint32_t)c, o);
+    tmem_ld_wait();
+    asm volatile("" : "+r"(o[0]), "+r"(o[1]), "+r"(o[2]), "+r"(o[3]), "+r"(o[4]), "+r"(o[5]), "+r"(o[6]), "+r"(o[7]), "+r"(o[8]), "+r"(o[9]),
+                 "+r"(o[10]), "+r"(o[11]), "+r"(o[12]), "+r"(o[13]), "+r"(o[14]), "+r"(o[15]));      // nothing reads them before the wait
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + (uint32_t)(lane * 64 + ((q ^ ((lane >> 1) & 3)) << 4))), "r"(o[4 * q]),
+                   "r"(o[4 * q + 1]), "r"(o[4 * q + 2]), "r"(o[4 * q + 3]) : "memory");
+    __syncwarp();
+    const int q = lane & 3;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int r = 8 * e + (lane >> 2);
+      float4 v;
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                   : "r"(stage + (uint32_t)(r * 64 + ((q ^ ((r >> 1) & 3)) << 4))));
+      if (r < rows) *reinterpret_cast<float4*>(dst + r * ld + c + 4 * q) = make_float4(v.x * by, v.y * by, v.z * by, v.w * by);
+    }
+    __syncwarp();
+  }
+}
+
 // A piece of work: `span` rows of one head of one sequence.
 struct Piece { int head, x0; SeqRange r; };
 // A block's pieces are looked up once, at its start: numbers blockIdx.x, + gridDim.x, ... of those whose rows exist, so
@@ -632,7 +658,10 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
 // of its 64 columns: while one pair is in its exp2 phase the tensor core works for the other, and four warps a
 // scheduler hide each other's latencies; one warp issues the scores, another the second products.  X is in tensor memory (XT) where it fits beside the accumulators: always for DQ, up to
 // d = 80 for DKDV.
+// Where there are few pieces, each is walked over in `parts` equal parts by different blocks: their sums go to
+// partial [part][dk, dv or dq][row][heads * d] in fp32, and a last kernel adds them in order.
 struct BackwardMaps { CUtensorMap x1, x2, x3, y1, y2; };
+struct Parts { int log2; float* partial; };
 constexpr int B_MMA_WARP = 16 /* two */, B_TMA_WARP = 18, B_THREADS = 608;
 
 template <int SLABS, bool DKDV>
@@ -655,7 +684,7 @@ enum BwdBar : int {
 
 template <int SLABS, bool DKDV, bool XT>
 __global__ void __launch_bounds__(B_THREADS, 1)
-packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c) {
+packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, const Parts parts) {
   using L = BackwardCfg<SLABS, DKDV>;
   extern __shared__ uint8_t smem_raw[];
   const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
@@ -672,7 +701,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
-  const int pieces_in_all = find_pieces(c.p, c.dev_status, RT, DKDV, DKDV ? c.p.kv_heads : c.p.heads,
+  const int pieces_in_all = find_pieces(c.p, c.dev_status, RT, DKDV, (DKDV ? c.p.kv_heads : c.p.heads) << parts.log2,
                                         reinterpret_cast<int32_t*>(smem + L::OFF_SEQ), reinterpret_cast<int32_t*>(smem));
   tc_fence_before();
   __syncthreads();
@@ -680,14 +709,18 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   const uint32_t tmem = uniform(*tmem_slot);
   const uint32_t acc2 = B_COLS, acc1 = B_COLS + d, x1_col = B_COLS + (DKDV ? 2 : 1) * d, x2_col = x1_col + d / 2;   // dk or dq; dv
   Piece w;
-  int at_piece = 0;
+  int at_piece = 0, part = 0, y_tiles = 0, t_begin = 0, n = 0;     // of piece w: part, tiles of a head of Y, first tile and number of tiles of the part
   auto advance = [&] {
     if (at_piece >= pieces_in_all) return false;
     w = piece_at(sb + L::OFF_SEQ, at_piece++);
+    part = w.head & ((1 << parts.log2) - 1);
+    w.head >>= parts.log2;
+    y_tiles = ((DKDV ? w.r.q_len : w.r.k_len) + CT - 1) / CT;
+    const int whole = DKDV ? group * y_tiles : y_tiles;            // tiles of Y, head after head
+    t_begin = (int)((int64_t)whole * part >> parts.log2);
+    n = (int)((int64_t)whole * (part + 1) >> parts.log2) - t_begin;
     return true;
   };
-  // tiles of Y that a piece walks over, head after head
-  auto y_tiles_of = [&] { return ((DKDV ? w.r.q_len : w.r.k_len) + CT - 1) / CT; };
 
   if (warp == B_TMA_WARP) {
     // ------------------------------------------------------------------ producer (the whole warp keeps step)
@@ -695,7 +728,6 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     int pieces = 0, n_all = 0;
     bool ok = true;
     while (ok && advance()) {
-      const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles;
       const int y_begin = DKDV ? w.r.q_begin : w.r.k_begin, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
       if (!warp_wait(bar(B_XSFREE), (pieces & 1) ^ 1, abort_flag)) break;
@@ -709,7 +741,8 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         }
       }
       ++pieces;
-      int y0 = 0, yh = DKDV ? w.head * group : group == 1 ? w.head : w.head / group;
+      const int heads_on = DKDV && t_begin > 0 ? t_begin / y_tiles : 0;
+      int y0 = (t_begin - heads_on * y_tiles) * CT, yh = DKDV ? w.head * group + heads_on : group == 1 ? w.head : w.head / group;
       for (int t = 0; t < n; ++t, ring.step()) {
         const int st = ring.at;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE;
@@ -761,10 +794,10 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     int pieces = 0, phase = 0;                                   // bit b of phase: parity of the next wait for warpgroup b's columns
     bool ok = true;
     while (ok && advance()) {
-      const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
+      const int y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (n == 0) continue;
       if (scores && !warp_wait(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
-      int left = y_len;                                          // rows of this head from the present tile on
+      int left = y_len - (t_begin > 0 ? t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
       for (int t = 0; t < n; ++t, ring.step()) {
         const int st = ring.at, b = t & 1, here = min(CT, left), n16 = (here + 15) / 16;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + b * B_WG;
@@ -826,15 +859,25 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     const float2 sl2v = make_float2(sl2, sl2);
     Ring<L::STAGES> ring;                                        // of every tile, this warpgroup's or not
     int pieces = 0, s_phase = 0;
+    // a row of piece w's part: of dk (or dq) or of dv
+    const int64_t x_rows = DKDV ? c.p.k_rows : c.p.q_rows, x_width = (int64_t)(DKDV ? c.p.kv_heads : c.p.heads) * d;
+    auto partial_row = [&](int tensor, int64_t row) {
+      return parts.partial + (((int64_t)part * (DKDV ? 2 : 1) + tensor) * x_rows + row) * x_width + (int64_t)w.head * d;
+    };
     // the next piece with something to walk over; rows that nothing meets get gradients of zero on the way
     auto next = [&] {
       while (advance()) {
-        if (y_tiles_of() > 0) return true;
+        if (n > 0) return true;
         const int row = w.x0 + in_tile;
         const int64_t at = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row;
         if (wg == 0 && row < (DKDV ? w.r.k_len : w.r.q_len)) {
           bf16* g2 = DKDV ? static_cast<bf16*>(c.dk) + at * c.lddk + (int64_t)w.head * d : static_cast<bf16*>(c.dq) + at * c.lddq + (int64_t)w.head * d;
           bf16* g1 = static_cast<bf16*>(c.dv) + at * c.lddv + (int64_t)w.head * d;
+          if (parts.log2 > 0) {
+            for (int t = 0; t < (DKDV ? 2 : 1); ++t)
+              for (int e = 0; e < d; e += 4) *reinterpret_cast<float4*>(partial_row(t, at) + e) = make_float4(0.f, 0.f, 0.f, 0.f);
+            continue;
+          }
           for (int e = 0; e < d; e += 8) {
             *reinterpret_cast<uint4*>(g2 + e) = make_uint4(0u, 0u, 0u, 0u);
             if (DKDV) *reinterpret_cast<uint4*>(g1 + e) = make_uint4(0u, 0u, 0u, 0u);
@@ -881,7 +924,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     bool more = next();
     bool ok = !XT || !more || load_x();
     while (more && ok) {
-      const int y_tiles = y_tiles_of(), n = DKDV ? group * y_tiles : y_tiles, y_len = DKDV ? w.r.q_len : w.r.k_len;
+      const int y_len = DKDV ? w.r.q_len : w.r.k_len;
       const int head = w.head, row0 = w.x0 + quarter * 32, rows = min(32, (DKDV ? w.r.k_len : w.r.q_len) - row0);
       const int64_t at0 = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row0;
       float2 nls = make_float2(0.f, 0.f), nde = nls;             // DQ: of this thread's row
@@ -891,7 +934,8 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         nls = make_float2(-mine.x, -mine.x);
         nde = make_float2(-mine.y, -mine.y);
       }
-      int left = y_len;                                          // rows of this head from the present tile on
+      float* sums = parts.log2 > 0 ? partial_row(DKDV ? wg & 1 : 0, at0) : nullptr;
+      int left = y_len - (t_begin > 0 ? t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
       for (int t = 0; t < n; ++t, ring.step()) {
         const int here = min(CT, left) - 32 * half;              // of this warpgroup's 32 columns
         left = left > CT ? left - CT : y_len;
@@ -958,12 +1002,14 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       if (!warp_wait(bar(B_ACC), (pieces - 1) & 1, abort_flag)) break;
       tc_fence_after();
       if (rows > 0) {
-        if (DKDV) {                                              // dk and dv
+        const int from = DKDV || wg == 0 ? 0 : d / 32 * 16, to = DKDV || wg == 1 ? d : d / 32 * 16;   // dk, dv; or a part of dq each
+        if (sums) {
+          store_rows(sums + from, x_width, lanes + (DKDV && wg == 1 ? acc1 : acc2) + from, to - from, 1.f, rows, stage, lane);
+        } else if (DKDV) {
           const int64_t ld = wg == 0 ? c.lddk : c.lddv;
           store_rows(static_cast<bf16*>(wg == 0 ? c.dk : c.dv) + at0 * ld + (int64_t)head * d, ld, lanes + (wg == 0 ? acc2 : acc1), d,
                      wg == 0 ? c.p.scale : 1.f, rows, stage, lane);
-        } else {                                                 // a part of the head each
-          const int from = wg == 0 ? 0 : d / 32 * 16, to = wg == 0 ? d / 32 * 16 : d;
+        } else {
           store_rows(static_cast<bf16*>(c.dq) + at0 * c.lddq + (int64_t)head * d + from, c.lddq, lanes + acc2 + from, to - from, c.p.scale, rows,
                      stage, lane);
         }
@@ -982,6 +1028,37 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (warp == B_MMA_WARP) {
     __syncwarp();
     tmem_dealloc(tmem, TMEM_ALL);
+  }
+}
+
+// The sums of the parts, in order, times the factor of the gradient, rounded once: 16 rows of a sequence to a block
+constexpr int ADD_ROWS = 16;
+template <bool DKDV>
+__global__ void __launch_bounds__(256) add_parts_kernel(const PackedCall c, const Parts parts) {
+  const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + ADD_ROWS - 1) / ADD_ROWS, seq = blockIdx.x / tiles, row0 = blockIdx.x % tiles * ADD_ROWS;
+  SeqRange r;
+  if (!seq_range(c.p, seq, r, c.dev_status, false)) return;
+  const int rows = min(ADD_ROWS, (DKDV ? r.k_len : r.q_len) - row0);
+  if (rows <= 0) return;
+  const int64_t all_rows = DKDV ? c.p.k_rows : c.p.q_rows, at = (int64_t)(DKDV ? r.k_begin : r.q_begin) + row0;
+  const int width = (DKDV ? c.p.kv_heads : c.p.heads) * c.p.d, pieces = width / 8;
+#pragma unroll
+  for (int tensor = 0; tensor < (DKDV ? 2 : 1); ++tensor) {
+    bf16* to = static_cast<bf16*>(DKDV ? (tensor ? c.dv : c.dk) : c.dq);
+    const int64_t ld = DKDV ? (tensor ? c.lddv : c.lddk) : c.lddq;
+    const float by = tensor ? 1.f : c.p.scale;
+    for (int i = threadIdx.x; i < rows * pieces; i += 256) {
+      const int row = i / pieces, ch = (i - row * pieces) * 8;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+      for (int k = 0; k < 1 << parts.log2; ++k) {
+        const float4* from = reinterpret_cast<const float4*>(parts.partial + (((int64_t)k * (DKDV ? 2 : 1) + tensor) * all_rows + at + row) * width + ch);
+        const float4 u = from[0], v = from[1];
+        a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
+        b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
+      }
+      *reinterpret_cast<uint4*>(to + (at + row) * ld + ch) = make_uint4(pack_bf16(a.x * by, a.y * by), pack_bf16(a.z * by, a.w * by),
+                                                                        pack_bf16(b.x * by, b.y * by), pack_bf16(b.z * by, b.w * by));
+    }
   }
 }
 
@@ -1038,6 +1115,21 @@ cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+// The parts of a piece of the backward pass: so many that there are two pieces to an SM or so, of eight tiles at least,
+// eight at most (4 sequences of up to 4097, 8 heads over 2 key heads of 128: dk and dv 269 us in one part, PARTS_US in four)
+int log2_parts(const vit_attention_problem& p, bool dkdv) {
+  const int64_t pieces = (int64_t)p.sequences * (dkdv ? p.kv_heads : p.heads) * (((dkdv ? p.max_k : p.max_q) + RT - 1) / RT);
+  const int64_t tiles = (int64_t)(dkdv ? p.heads / p.kv_heads : 1) * (((dkdv ? p.max_q : p.max_k) + CT - 1) / CT);
+  int log2 = 0;
+  while (log2 < 3 && pieces << log2 < 296 && tiles >> (log2 + 1) >= 8) ++log2;
+  return log2;
+}
+size_t partial_floats(const vit_attention_problem& p, bool dkdv) {
+  const int log2 = log2_parts(p, dkdv);
+  if (log2 == 0) return 0;
+  return ((size_t)(dkdv ? 2 * (size_t)p.k_rows * p.kv_heads : (size_t)p.q_rows * p.heads) * p.d) << log2;
+}
+
 template <int SLABS, bool DKDV, bool XT>
 cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
   using L = BackwardCfg<SLABS, DKDV>;
@@ -1058,15 +1150,25 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
   if (cudaError_t e = ensure_dynamic_smem(done, packed_backward_tc_kernel<SLABS, DKDV, XT>, (int)L::BYTES)) return e;
   const int sms = current_device_sm_count();
   if (sms < 1) return cudaErrorInvalidDevice;
-  const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT, total = c.p.sequences * xh * tiles;
-  packed_backward_tc_kernel<SLABS, DKDV, XT><<<grid_of(total, sms), B_THREADS, L::BYTES, s>>>(m, c);
-  return cudaGetLastError();
+  const Parts parts{log2_parts(c.p, DKDV), c.partial};
+  const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT, total = (c.p.sequences * xh * tiles) << parts.log2;
+  packed_backward_tc_kernel<SLABS, DKDV, XT><<<grid_of(total, sms), B_THREADS, L::BYTES, s>>>(m, c, parts);
+  if (cudaError_t e = cudaGetLastError()) return e;
+  if (parts.log2 > 0) {
+    add_parts_kernel<DKDV><<<c.p.sequences * (((DKDV ? c.p.max_k : c.p.max_q) + ADD_ROWS - 1) / ADD_ROWS), 256, 0, s>>>(c, parts);
+    return cudaGetLastError();
+  }
+  return cudaSuccess;
 }
 
 }  // namespace
 
 // Columns of tensor memory decide where a piece's rows are held: 128 + d + d / 2 of a warpgroup's 256 in
 // the forward pass, 256 + 2 d + d of 512 for dk and dv, 256 + d + d for dq.
+size_t attention_partial_floats(const vit_attention_problem& p) {
+  const size_t a = partial_floats(p, true), b = partial_floats(p, false);    // one after the other
+  return a > b ? a : b;
+}
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s) {
   if (c.p.d <= 64) return launch_forward<1, true>(c, s);
   return c.p.d <= 80 ? launch_forward<2, true>(c, s) : launch_forward<2, false>(c, s);

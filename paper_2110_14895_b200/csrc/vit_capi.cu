@@ -271,8 +271,11 @@ bool attention_fits(const vit_attention_problem* p) {
   const int64_t per = (int64_t)p->heads * ((longest + 63) / 64 + 1);
   return p->sequences == 0 || per <= INT32_MAX / 8 / p->sequences;      // (up to eight blocks where there are few queries)
 }
+// backward: (lse, delta) of every query row and head, then the sums of the parts of the work
+size_t attention_delta_bytes(const vit_attention_problem& p) { return align_up((size_t)p.heads * p.q_rows * sizeof(float2), 256); }
 size_t attention_packed_ws(int dtype, const vit_attention_problem& p, bool backward) {
-  return backward ? align_up((size_t)p.heads * p.q_rows * sizeof(float2), 256) : 0;
+  if (!backward) return 0;
+  return attention_delta_bytes(p) + (dtype == VIT_BF16 ? align_up(attention_partial_floats(p) * sizeof(float), 256) : 0);
 }
 
 }  // namespace
@@ -888,6 +891,7 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
   c.lse = const_cast<float*>(lse); c.dout = dout; c.lddo = lddo;
   c.dq = dq; c.lddq = lddq; c.dk = dk; c.lddk = lddk; c.dv = dv; c.lddv = lddv;
   c.delta = static_cast<float2*>(ws);
+  c.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + attention_delta_bytes(p));
   c.dev_status = h->dev_status;
   const bool b16 = dtype == VIT_BF16;
   const bool queries = p.q_rows > 0 && p.max_q > 0, keys = p.k_rows > 0 && p.max_k > 0;

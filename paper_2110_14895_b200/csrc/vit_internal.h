@@ -183,8 +183,10 @@ struct PackedCall {
   const void* dout;       int64_t lddo;
   void *dq, *dk, *dv;     int64_t lddq, lddk, lddv;
   float2* delta;                            // backward: [heads][q_rows] (lse log2(e), rowsum(dout * out))
+  float* partial;                           // backward, bf16: sums of the parts of the work (attention_partial_floats)
   int* dev_status;
 };
+size_t attention_partial_floats(const vit_attention_problem& p);
 // a few queries (times heads that share a key head) of a sequence go to the kernel for few rows (attention_rows.cu)
 bool attention_rows_supported(const vit_attention_problem& p, bool act_bf16);
 cudaError_t launch_attention_rows(const PackedCall& c, bool act_bf16, cudaStream_t s);

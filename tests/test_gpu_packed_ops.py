@@ -353,6 +353,8 @@ ATTENTION_CASES = [
     ([100, 3, 40], [7, 0, 300], 2, 2, 32), ([0, 70, 20], [50, 0, 129], 4, 1, 64), ([1, 1, 1, 1], [577, 1, 0, 1030], 4, 4, 64),
     ([2, 3, 1], [1025, 64, 2000], 6, 2, 80), ([700, 385], None, 2, 2, 64), ([1, 1], [3000, 129], 3, 1, 128), ([513], [1], 2, 2, 128),
     ([1100], None, 1, 1, 80), ([256, 255, 384], None, 1, 1, 16),
+    # few and long: the work on a tile of keys (or queries) is shared out, also for the short sequences beside them
+    ([1300, 20, 0, 530], None, 8, 2, 64), ([2100, 70], None, 4, 1, 128), ([30, 700], [2000, 1], 2, 2, 48),
 ]
 
 
