@@ -5,8 +5,10 @@
 //   p = exp(s - lse), delta = rowsum(dout * out), ds = p (dout v^T - delta)
 //   dv = p^T dout, dk = scale ds^T q, dq = scale ds k                                 (backward)
 //
-// A block of 256 threads works on 64 x 64 scores at a time, 4 x 4 of them to a thread; operands are
-// staged in shared memory, rows behind the end of a sequence are zero there.  The backward
+// A block of 128 threads works on 32 x 32 scores at a time, 4 x 2 of them to a thread; operands are
+// staged in shared memory, rows behind the end of a sequence are zero there.  Tiles of 64 with 256 threads need
+// fewer reads of shared memory for a product, but leave one block of eight warps to an SM and a quarter of the
+// blocks (FP32_US).  The backward
 // pass is two kernels, one that keeps a tile of keys and walks over the queries (dk, dv) and one that
 // keeps a tile of queries and walks over the keys (dq): seven products instead of five, but every
 // gradient is summed by one block in a fixed order, so that results do not depend on the schedule.
@@ -17,13 +19,13 @@ namespace vit {
 
 namespace {
 
-constexpr int BT = 64;              // rows and columns of a tile of scores
-constexpr int THREADS = 256;
+constexpr int BT = 32;              // rows and columns of a tile of scores
+constexpr int THREADS = 128;
 constexpr int PS = BT + 4;          // row stride of a tile of probabilities
 
 __device__ __forceinline__ float4 load4(const float* a) { return *reinterpret_cast<const float4*>(a); }
 
-// rows [row0, row0 + 64) of one head as fp32 [64][DP + 4]; rows >= end and columns >= d are zero
+// rows [row0, row0 + 32) of one head as fp32 [32][DP + 4]; rows >= end and columns >= d are zero
 template <int DP>
 __device__ __forceinline__ void load_tile(float* dst, const float* base, int64_t ld, int64_t row0, int rows, int d) {
   for (int i = threadIdx.x; i < BT * (DP / 4); i += THREADS) {
@@ -35,48 +37,55 @@ __device__ __forceinline__ void load_tile(float* dst, const float* base, int64_t
 
 // acc[i][j] = a[ty * 4 + i] . b[tx + 16 j] over the head's channels
 template <int DP>
-__device__ __forceinline__ void scores(float (&acc)[4][4], const float* a, const float* b, int tx, int ty) {
+__device__ __forceinline__ void scores(float (&acc)[4][2], const float* a, const float* b, int tx, int ty) {
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+    for (int j = 0; j < 2; ++j) acc[i][j] = 0.f;
 #pragma unroll 4
   for (int c = 0; c < DP; c += 4) {
-    float4 x[4], y[4];
+    float4 x[4], y[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = load4(a + (ty * 4 + i) * (DP + 4) + c);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = load4(b + (tx + 16 * j) * (DP + 4) + c);
+    for (int j = 0; j < 2; ++j) y[j] = load4(b + (tx + 16 * j) * (DP + 4) + c);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 2; ++j)
         acc[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, acc[i][j]))));
   }
 }
 
-// acc[i][cc] += sum over t of w[t][ty * 4 + i] * x[t][tx + 16 cc]      (w transposed: rows are the summed index)
+// acc[i][cc] += sum over t of w[t][ty * 4 + i] * x[t][2 tx + 32 cc, + 1]      (rows of w and x are the summed index)
 template <int DP>
-__device__ __forceinline__ void accumulate_t(float (&acc)[4][DP / 16], const float* w, const float* x, int tx, int ty) {
-#pragma unroll 2
+__device__ __forceinline__ void accumulate_t(float2 (&acc)[4][DP / 32], const float* w, const float* x, int tx, int ty) {
+#pragma unroll 4
   for (int t = 0; t < BT; ++t) {
     const float4 p = load4(w + t * PS + ty * 4);
 #pragma unroll
-    for (int cc = 0; cc < DP / 16; ++cc) {
-      const float v = x[t * (DP + 4) + tx + 16 * cc];
-      acc[0][cc] = fmaf(p.x, v, acc[0][cc]);
-      acc[1][cc] = fmaf(p.y, v, acc[1][cc]);
-      acc[2][cc] = fmaf(p.z, v, acc[2][cc]);
-      acc[3][cc] = fmaf(p.w, v, acc[3][cc]);
+    for (int cc = 0; cc < DP / 32; ++cc) {
+      const float2 v = *reinterpret_cast<const float2*>(x + t * (DP + 4) + 2 * tx + 32 * cc);
+      acc[0][cc] = __ffma2_rn(make_float2(p.x, p.x), v, acc[0][cc]);
+      acc[1][cc] = __ffma2_rn(make_float2(p.y, p.y), v, acc[1][cc]);
+      acc[2][cc] = __ffma2_rn(make_float2(p.z, p.z), v, acc[2][cc]);
+      acc[3][cc] = __ffma2_rn(make_float2(p.w, p.w), v, acc[3][cc]);
     }
   }
+}
+// a row's channels of this thread
+template <int DP>
+__device__ __forceinline__ void store_row(float* dst, const float2 (&acc)[DP / 32], float by, int tx, int d) {
+#pragma unroll
+  for (int cc = 0; cc < DP / 32; ++cc)
+    if (2 * tx + 32 * cc < d) *reinterpret_cast<float2*>(dst + 2 * tx + 32 * cc) = make_float2(acc[cc].x * by, acc[cc].y * by);
 }
 
 template <int DP>
 __global__ void __launch_bounds__(THREADS)
 packed_forward_kernel(const PackedCall c) {
   extern __shared__ __align__(16) float sm[];
-  float* qs = sm;                               // [64][DP + 4]
+  float* qs = sm;                               // [32][DP + 4]
   float* ks = qs + BT * (DP + 4);               // keys, then values
   float* ps = ks + BT * (DP + 4);               // [key][query]: probabilities, transposed
   const int tiles = (c.p.max_q + BT - 1) / BT;
@@ -94,19 +103,20 @@ packed_forward_kernel(const PackedCall c) {
   const float sl2 = c.p.scale * 1.4426950408889634f;
 
   load_tile<DP>(qs, q, c.ldq, (int64_t)r.q_begin + q0, q_here, d);
-  float m[4], l[4], o[4][DP / 16];
+  float m[4], l[4];
+  float2 o[4][DP / 32];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     m[i] = -INFINITY;
     l[i] = 0.f;
 #pragma unroll
-    for (int cc = 0; cc < DP / 16; ++cc) o[i][cc] = 0.f;
+    for (int cc = 0; cc < DP / 32; ++cc) o[i][cc] = make_float2(0.f, 0.f);
   }
   for (int k0 = 0; k0 < r.k_len; k0 += BT) {
     const int k_here = min(BT, r.k_len - k0);
     load_tile<DP>(ks, k, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
     __syncthreads();
-    float s[4][4];
+    float s[4][2];
     scores<DP>(s, qs, ks, tx, ty);
     __syncthreads();
     load_tile<DP>(ks, v, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
@@ -114,7 +124,7 @@ packed_forward_kernel(const PackedCall c) {
     for (int i = 0; i < 4; ++i) {
       float top = m[i];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 2; ++j) {
         s[i][j] = tx + 16 * j < k_here ? s[i][j] * sl2 : -INFINITY;
         top = fmaxf(top, s[i][j]);
       }
@@ -125,14 +135,14 @@ packed_forward_kernel(const PackedCall c) {
       m[i] = top;
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 2; ++j) {
         s[i][j] = exp2f(s[i][j] - ref);
         sum += s[i][j];
         ps[(tx + 16 * j) * PS + ty * 4 + i] = s[i][j];
       }
       l[i] = l[i] * keep + sum;                            // this lane's part of the row sum
 #pragma unroll
-      for (int cc = 0; cc < DP / 16; ++cc) o[i][cc] *= keep;
+      for (int cc = 0; cc < DP / 32; ++cc) o[i][cc] = __fmul2_rn(o[i][cc], make_float2(keep, keep));
     }
     __syncthreads();
     accumulate_t<DP>(o, ps, ks, tx, ty);
@@ -147,9 +157,7 @@ packed_forward_kernel(const PackedCall c) {
     const int64_t at = (int64_t)r.q_begin + q0 + row;
     const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];     // no keys: zero
     float* out = static_cast<float*>(c.out) + at * c.ldo + (int64_t)head * d;
-#pragma unroll
-    for (int cc = 0; cc < DP / 16; ++cc)
-      if (tx + 16 * cc < d) out[tx + 16 * cc] = o[i][cc] * inv;
+    store_row<DP>(out, o[i], inv, tx, d);
     if (tx == 0) c.lse[(int64_t)head * c.p.q_rows + at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718055994531f;
   }
 }
@@ -177,14 +185,14 @@ packed_delta_kernel(const PackedCall c) {
 }
 
 // p and ds of a tile: s = q k^T, dp = dout v^T; rows beyond q_here and keys beyond k_here give zero
-__device__ __forceinline__ void grad_scores(float (&s)[4][4], float (&dp)[4][4], const float* lse2, const float* delta, float sl2,
+__device__ __forceinline__ void grad_scores(float (&s)[4][2], float (&dp)[4][2], const float* lse2, const float* delta, float sl2,
                                             int q_here, int k_here, int tx, int ty) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = ty * 4 + i;
     const float ls = lse2[row], de = delta[row];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 2; ++j) {
       const bool there = row < q_here && tx + 16 * j < k_here;
       const float p = there ? exp2f(fmaf(s[i][j], sl2, -ls)) : 0.f;
       dp[i][j] = there ? p * (dp[i][j] - de) : 0.f;
@@ -211,11 +219,11 @@ packed_dkdv_kernel(const PackedCall c) {
   const float sl2 = c.p.scale * 1.4426950408889634f;
   load_tile<DP>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
   load_tile<DP>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
-  float dk[4][DP / 16], dv[4][DP / 16];
+  float2 dk[4][DP / 32], dv[4][DP / 32];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int cc = 0; cc < DP / 16; ++cc) dk[i][cc] = dv[i][cc] = 0.f;
+    for (int cc = 0; cc < DP / 32; ++cc) dk[i][cc] = dv[i][cc] = make_float2(0.f, 0.f);
   for (int head = kv * group; head < (kv + 1) * group; ++head) {
     for (int q0 = 0; q0 < r.q_len; q0 += BT) {
       const int q_here = min(BT, r.q_len - q0);
@@ -230,14 +238,14 @@ packed_dkdv_kernel(const PackedCall c) {
         delta[threadIdx.x] = v.y;
       }
       __syncthreads();
-      float s[4][4], dp[4][4];
+      float s[4][2], dp[4][2];
       scores<DP>(s, qs, ks, tx, ty);
       scores<DP>(dp, os, vs, tx, ty);
       grad_scores(s, dp, lse2, delta, sl2, q_here, k_here, tx, ty);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
           ps[(ty * 4 + i) * PS + tx + 16 * j] = s[i][j];
           ds[(ty * 4 + i) * PS + tx + 16 * j] = dp[i][j];
         }
@@ -254,12 +262,8 @@ packed_dkdv_kernel(const PackedCall c) {
     const int64_t at = (int64_t)r.k_begin + k0 + row;
     float* gk = static_cast<float*>(c.dk) + at * c.lddk + (int64_t)kv * d;
     float* gv = static_cast<float*>(c.dv) + at * c.lddv + (int64_t)kv * d;
-#pragma unroll
-    for (int cc = 0; cc < DP / 16; ++cc)
-      if (tx + 16 * cc < d) {
-        gk[tx + 16 * cc] = dk[i][cc] * c.p.scale;
-        gv[tx + 16 * cc] = dv[i][cc];
-      }
+    store_row<DP>(gk, dk[i], c.p.scale, tx, d);
+    store_row<DP>(gv, dv[i], 1.f, tx, d);
   }
 }
 
@@ -289,24 +293,24 @@ packed_dq_kernel(const PackedCall c) {
     lse2[threadIdx.x] = v.x;
     delta[threadIdx.x] = v.y;
   }
-  float dq[4][DP / 16];
+  float2 dq[4][DP / 32];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int cc = 0; cc < DP / 16; ++cc) dq[i][cc] = 0.f;
+    for (int cc = 0; cc < DP / 32; ++cc) dq[i][cc] = make_float2(0.f, 0.f);
   for (int k0 = 0; k0 < r.k_len; k0 += BT) {
     const int k_here = min(BT, r.k_len - k0);
     load_tile<DP>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
     load_tile<DP>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
     __syncthreads();
-    float s[4][4], dp[4][4];
+    float s[4][2], dp[4][2];
     scores<DP>(s, qs, ks, tx, ty);
     scores<DP>(dp, os, vs, tx, ty);
     grad_scores(s, dp, lse2, delta, sl2, q_here, k_here, tx, ty);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) ds[(tx + 16 * j) * PS + ty * 4 + i] = dp[i][j];
+      for (int j = 0; j < 2; ++j) ds[(tx + 16 * j) * PS + ty * 4 + i] = dp[i][j];
     __syncthreads();
     accumulate_t<DP>(dq, ds, ks, tx, ty);
     __syncthreads();
@@ -316,9 +320,7 @@ packed_dq_kernel(const PackedCall c) {
     const int row = ty * 4 + i;
     if (row >= q_here) continue;
     float* g = static_cast<float*>(c.dq) + (at + row) * c.lddq + (int64_t)head * d;
-#pragma unroll
-    for (int cc = 0; cc < DP / 16; ++cc)
-      if (tx + 16 * cc < d) g[tx + 16 * cc] = dq[i][cc] * c.p.scale;
+    store_row<DP>(g, dq[i], c.p.scale, tx, d);
   }
 }
 

@@ -265,10 +265,10 @@ bool attention_problem_ok(int dtype, const vit_attention_problem* p) {
   if ((int64_t)p->heads * p->d > INT32_MAX) return false;
   return p->scale > 0.f && p->scale <= 3.402823466e38f;
 }
-// blocks of the launches: one per sequence, head and tile of at least 64 rows
+// blocks of the launches: one per sequence, head and tile of at least 32 rows
 bool attention_fits(const vit_attention_problem* p) {
   const int64_t longest = p->max_q > p->max_k ? p->max_q : p->max_k;
-  const int64_t per = (int64_t)p->heads * ((longest + 63) / 64 + 1);
+  const int64_t per = (int64_t)p->heads * ((longest + 31) / 32 + 1);
   return p->sequences == 0 || per <= INT32_MAX / 8 / p->sequences;      // (up to eight blocks where there are few queries)
 }
 // backward: (lse, delta) of every query row and head, then the sums of the parts of the work
