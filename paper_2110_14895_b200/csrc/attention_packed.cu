@@ -14,6 +14,7 @@
 // gradient is summed by one block in a fixed order, so that results do not depend on the schedule.
 #include "vit_internal.h"
 #include "attention_packed.cuh"
+#include "sm100_ptx.cuh"
 
 namespace vit {
 
@@ -25,15 +26,19 @@ constexpr int PS = BT + 4;          // row stride of a tile of probabilities
 
 __device__ __forceinline__ float4 load4(const float* a) { return *reinterpret_cast<const float4*>(a); }
 
-// rows [row0, row0 + 32) of one head as fp32 [32][DP + 4]; rows >= end and columns >= d are zero
-template <int DP>
-__device__ __forceinline__ void load_tile(float* dst, const float* base, int64_t ld, int64_t row0, int rows, int d) {
-  for (int i = threadIdx.x; i < BT * (DP / 4); i += THREADS) {
+// rows [row0, row0 + 32) of one head as [32][DP + 4], on their way with cp.async by N threads; rows behind the
+// `rows` that exist and columns >= d become zero
+template <int DP, int N>
+__device__ __forceinline__ void fetch_tile(float* dst, const float* base, int64_t ld, int64_t row0, int rows, int d, int tid) {
+  for (int i = tid; i < BT * (DP / 4); i += N) {
     const int r = i / (DP / 4), c = (i % (DP / 4)) * 4;
-    const float4 v = r < rows && c < d ? load4(base + (row0 + r) * ld + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-    *reinterpret_cast<float4*>(dst + r * (DP + 4) + c) = v;
+    const bool there = r < rows && c < d;
+    ptx::cp_async_16(ptx::smem_u32(dst + r * (DP + 4) + c), there ? base + (row0 + r) * ld + c : base, there ? 16u : 0u);
   }
 }
+__device__ __forceinline__ void fetched() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_fetched() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // acc[i][j] = a[ty * 4 + i] . b[tx + 16 j] over the head's channels
 template <int DP>
@@ -58,10 +63,10 @@ __device__ __forceinline__ void scores(float (&acc)[4][2], const float* a, const
 }
 
 // acc[i][cc] += sum over t of w[t][ty * 4 + i] * x[t][2 tx + 32 cc, + 1]      (rows of w and x are the summed index)
-template <int DP>
+template <int DP, int N = BT>
 __device__ __forceinline__ void accumulate_t(float2 (&acc)[4][DP / 32], const float* w, const float* x, int tx, int ty) {
 #pragma unroll 4
-  for (int t = 0; t < BT; ++t) {
+  for (int t = 0; t < N; ++t) {
     const float4 p = load4(w + t * PS + ty * 4);
 #pragma unroll
     for (int cc = 0; cc < DP / 32; ++cc) {
@@ -85,9 +90,8 @@ template <int DP>
 __global__ void __launch_bounds__(THREADS)
 packed_forward_kernel(const PackedCall c) {
   extern __shared__ __align__(16) float sm[];
-  float* qs = sm;                               // [32][DP + 4]
-  float* ks = qs + BT * (DP + 4);               // keys, then values
-  float* ps = ks + BT * (DP + 4);               // [key][query]: probabilities, transposed
+  constexpr int TILE = BT * (DP + 4);
+  float *qs = sm, *kv_s = qs + TILE, *ps = kv_s + 4 * TILE;   // kv_s: [stage][keys, values]; ps: [key][query]
   const int tiles = (c.p.max_q + BT - 1) / BT;
   const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
   SeqRange r;
@@ -97,12 +101,17 @@ packed_forward_kernel(const PackedCall c) {
   const int q_here = min(BT, r.q_len - q0), d = c.p.d;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int kv = head / (c.p.heads / c.p.kv_heads);
-  const float* q = static_cast<const float*>(c.q) + (int64_t)head * d;
   const float* k = static_cast<const float*>(c.k) + (int64_t)kv * d;
   const float* v = static_cast<const float*>(c.v) + (int64_t)kv * d;
   const float sl2 = c.p.scale * 1.4426950408889634f;
-
-  load_tile<DP>(qs, q, c.ldq, (int64_t)r.q_begin + q0, q_here, d);
+  auto fetch = [&](int k0, int stage) {
+    const int here = min(BT, r.k_len - k0);
+    fetch_tile<DP, THREADS>(kv_s + 2 * stage * TILE, k, c.ldk, (int64_t)r.k_begin + k0, here, d, threadIdx.x);
+    fetch_tile<DP, THREADS>(kv_s + (2 * stage + 1) * TILE, v, c.ldv, (int64_t)r.k_begin + k0, here, d, threadIdx.x);
+  };
+  fetch_tile<DP, THREADS>(qs, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, (int64_t)r.q_begin + q0, q_here, d, threadIdx.x);
+  if (r.k_len > 0) fetch(0, 0);
+  fetched();
   float m[4], l[4];
   float2 o[4][DP / 32];
 #pragma unroll
@@ -112,14 +121,16 @@ packed_forward_kernel(const PackedCall c) {
 #pragma unroll
     for (int cc = 0; cc < DP / 32; ++cc) o[i][cc] = make_float2(0.f, 0.f);
   }
-  for (int k0 = 0; k0 < r.k_len; k0 += BT) {
+  int stage = 0;
+  for (int k0 = 0; k0 < r.k_len; k0 += BT, stage ^= 1) {
     const int k_here = min(BT, r.k_len - k0);
-    load_tile<DP>(ks, k, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
+    const float *ks = kv_s + 2 * stage * TILE, *vs = ks + TILE;
+    if (k0 + BT < r.k_len) fetch(k0 + BT, stage ^ 1);
+    fetched();
+    wait_fetched<1>();
     __syncthreads();
     float s[4][2];
     scores<DP>(s, qs, ks, tx, ty);
-    __syncthreads();
-    load_tile<DP>(ks, v, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float top = m[i];
@@ -145,8 +156,8 @@ packed_forward_kernel(const PackedCall c) {
       for (int cc = 0; cc < DP / 32; ++cc) o[i][cc] = __fmul2_rn(o[i][cc], make_float2(keep, keep));
     }
     __syncthreads();
-    accumulate_t<DP>(o, ps, ks, tx, ty);
-    __syncthreads();
+    accumulate_t<DP>(o, ps, vs, tx, ty);
+    __syncthreads();                                       // this stage and ps may be written again
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -156,10 +167,10 @@ packed_forward_kernel(const PackedCall c) {
     if (row >= q_here) continue;
     const int64_t at = (int64_t)r.q_begin + q0 + row;
     const float inv = l[i] == 0.f ? 0.f : 1.0f / l[i];     // no keys: zero
-    float* out = static_cast<float*>(c.out) + at * c.ldo + (int64_t)head * d;
-    store_row<DP>(out, o[i], inv, tx, d);
+    store_row<DP>(static_cast<float*>(c.out) + at * c.ldo + (int64_t)head * d, o[i], inv, tx, d);
     if (tx == 0) c.lse[(int64_t)head * c.p.q_rows + at] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * 0.69314718055994531f;
   }
+  wait_fetched<0>();
 }
 
 // (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head
@@ -184,96 +195,102 @@ packed_delta_kernel(const PackedCall c) {
   if (lane == 0) c.delta[at] = make_float2(c.lse[at] * 1.4426950408889634f, sum);
 }
 
-// p and ds of a tile: s = q k^T, dp = dout v^T; rows beyond q_here and keys beyond k_here give zero
-__device__ __forceinline__ void grad_scores(float (&s)[4][2], float (&dp)[4][2], const float* lse2, const float* delta, float sl2,
-                                            int q_here, int k_here, int tx, int ty) {
+// The gradient kernels have two groups of 128 threads: one has the scores and their probabilities, the other the
+// gradients of the probabilities; then each has one sum (dv and dk, or half of the keys for dq).
+constexpr int GRAD_THREADS = 2 * THREADS;
+
+// One tile's P (by group 0) and dS (by group 1): [row of w][column of w] as the sums want it
+template <int DP, bool BY_QUERY>
+__device__ __forceinline__ void grad_scores(float* ps, float* ds, const float* qs, const float* os, const float* ks, const float* vs,
+                                            const float2* rows, float sl2, int q_here, int k_here, int group, int tx, int ty) {
+  float s[4][2];
+  scores<DP>(s, group ? os : qs, group ? vs : ks, tx, ty);
+  auto place = [&](int i, int j) { return BY_QUERY ? (ty * 4 + i) * PS + tx + 16 * j : (tx + 16 * j) * PS + ty * 4 + i; };
+  if (group == 0) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = ty * 4 + i;
-    const float ls = lse2[row], de = delta[row];
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const bool there = row < q_here && tx + 16 * j < k_here;
-      const float p = there ? exp2f(fmaf(s[i][j], sl2, -ls)) : 0.f;
-      dp[i][j] = there ? p * (dp[i][j] - de) : 0.f;
-      s[i][j] = p;
-    }
+      for (int j = 0; j < 2; ++j) {
+        const bool there = ty * 4 + i < q_here && tx + 16 * j < k_here;
+        ps[place(i, j)] = there ? exp2f(fmaf(s[i][j], sl2, -rows[ty * 4 + i].x)) : 0.f;
+      }
+  }
+  __syncthreads();
+  if (group == 1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const bool there = ty * 4 + i < q_here && tx + 16 * j < k_here;
+        ds[place(i, j)] = there ? ps[place(i, j)] * (s[i][j] - rows[ty * 4 + i].y) : 0.f;
+      }
   }
 }
 
 template <int DP>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(GRAD_THREADS)
 packed_dkdv_kernel(const PackedCall c) {
   extern __shared__ __align__(16) float sm[];
   constexpr int TILE = BT * (DP + 4);
-  float *ks = sm, *vs = ks + TILE, *qs = vs + TILE, *os = qs + TILE, *ps = os + TILE, *ds = ps + BT * PS;   // ps, ds: [query][key]
-  float *lse2 = ds + BT * PS, *delta = lse2 + BT;
+  float *ks = sm, *vs = ks + TILE, *qo = vs + TILE, *ps = qo + 4 * TILE, *ds = ps + BT * PS;   // qo: [stage][q, dout]; ps, ds: [query][key]
+  float2* rows = reinterpret_cast<float2*>(ds + BT * PS);                                      // [stage][32]: lse log2(e), delta
   const int tiles = (c.p.max_k + BT - 1) / BT;
   const int tile = blockIdx.x % tiles, kv = blockIdx.x / tiles % c.p.kv_heads, seq = blockIdx.x / tiles / c.p.kv_heads;
   SeqRange r;
   if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
   const int k0 = tile * BT;
   if (k0 >= r.k_len) return;
-  const int k_here = min(BT, r.k_len - k0), d = c.p.d, group = c.p.heads / c.p.kv_heads;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int k_here = min(BT, r.k_len - k0), d = c.p.d, heads = c.p.heads / c.p.kv_heads;
+  const int group = threadIdx.x / THREADS, tid = threadIdx.x % THREADS, tx = tid & 15, ty = tid >> 4;
   const float sl2 = c.p.scale * 1.4426950408889634f;
-  load_tile<DP>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
-  load_tile<DP>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
-  float2 dk[4][DP / 32], dv[4][DP / 32];
+  const int q_tiles = (r.q_len + BT - 1) / BT, n = heads * q_tiles;
+  auto fetch = [&](int t, int stage) {                      // queries (group 0) or their dout (group 1), and their numbers
+    const int head = kv * heads + t / q_tiles, q0 = t % q_tiles * BT, here = min(BT, r.q_len - q0);
+    const int64_t at = (int64_t)r.q_begin + q0;
+    if (group == 0) fetch_tile<DP, THREADS>(qo + 2 * stage * TILE, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, at, here, d, tid);
+    else fetch_tile<DP, THREADS>(qo + (2 * stage + 1) * TILE, static_cast<const float*>(c.dout) + (int64_t)head * d, c.lddo, at, here, d, tid);
+    if (group == 0 && tid < here) rows[stage * BT + tid] = c.delta[(int64_t)head * c.p.q_rows + at + tid];
+  };
+  if (group == 0) fetch_tile<DP, THREADS>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d, tid);
+  else fetch_tile<DP, THREADS>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d, tid);
+  if (n > 0) fetch(0, 0);
+  fetched();
+  float2 acc[4][DP / 32];                                   // of dv (group 0) or dk (group 1)
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int cc = 0; cc < DP / 32; ++cc) dk[i][cc] = dv[i][cc] = make_float2(0.f, 0.f);
-  for (int head = kv * group; head < (kv + 1) * group; ++head) {
-    for (int q0 = 0; q0 < r.q_len; q0 += BT) {
-      const int q_here = min(BT, r.q_len - q0);
-      const int64_t at = (int64_t)r.q_begin + q0;
-      load_tile<DP>(qs, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
-      load_tile<DP>(os, static_cast<const float*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
-      if (threadIdx.x < BT) {
-        const bool there = (int)threadIdx.x < q_here;
-        const int64_t i = (int64_t)head * c.p.q_rows + at + threadIdx.x;
-        const float2 v = there ? c.delta[i] : make_float2(0.f, 0.f);
-        lse2[threadIdx.x] = v.x;
-        delta[threadIdx.x] = v.y;
-      }
-      __syncthreads();
-      float s[4][2], dp[4][2];
-      scores<DP>(s, qs, ks, tx, ty);
-      scores<DP>(dp, os, vs, tx, ty);
-      grad_scores(s, dp, lse2, delta, sl2, q_here, k_here, tx, ty);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          ps[(ty * 4 + i) * PS + tx + 16 * j] = s[i][j];
-          ds[(ty * 4 + i) * PS + tx + 16 * j] = dp[i][j];
-        }
-      __syncthreads();
-      accumulate_t<DP>(dv, ps, os, tx, ty);
-      accumulate_t<DP>(dk, ds, qs, tx, ty);
-      __syncthreads();
-    }
+    for (int cc = 0; cc < DP / 32; ++cc) acc[i][cc] = make_float2(0.f, 0.f);
+  for (int t = 0; t < n; ++t) {
+    const int stage = t & 1, q_here = min(BT, r.q_len - t % q_tiles * BT);
+    if (t + 1 < n) fetch(t + 1, stage ^ 1);
+    fetched();
+    wait_fetched<1>();
+    __syncthreads();
+    const float *qs = qo + 2 * stage * TILE, *os = qs + TILE;
+    grad_scores<DP, true>(ps, ds, qs, os, ks, vs, rows + stage * BT, sl2, q_here, k_here, group, tx, ty);
+    if (group == 0) accumulate_t<DP>(acc, ps, os, tx, ty);
+    else asm volatile("bar.sync 1, 128;" ::: "memory");     // ds is written and read by this group alone
+    if (group == 1) accumulate_t<DP>(acc, ds, qs, tx, ty);
+    __syncthreads();                                        // this stage, ps and ds may be written again
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = ty * 4 + i;
     if (row >= k_here) continue;
     const int64_t at = (int64_t)r.k_begin + k0 + row;
-    float* gk = static_cast<float*>(c.dk) + at * c.lddk + (int64_t)kv * d;
-    float* gv = static_cast<float*>(c.dv) + at * c.lddv + (int64_t)kv * d;
-    store_row<DP>(gk, dk[i], c.p.scale, tx, d);
-    store_row<DP>(gv, dv[i], 1.f, tx, d);
+    if (group == 0) store_row<DP>(static_cast<float*>(c.dv) + at * c.lddv + (int64_t)kv * d, acc[i], 1.f, tx, d);
+    else store_row<DP>(static_cast<float*>(c.dk) + at * c.lddk + (int64_t)kv * d, acc[i], c.p.scale, tx, d);
   }
+  wait_fetched<0>();
 }
 
 template <int DP>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(GRAD_THREADS)
 packed_dq_kernel(const PackedCall c) {
   extern __shared__ __align__(16) float sm[];
   constexpr int TILE = BT * (DP + 4);
-  float *qs = sm, *os = qs + TILE, *ks = os + TILE, *vs = ks + TILE, *ds = vs + TILE;       // ds: [key][query]
-  float *lse2 = ds + BT * PS, *delta = lse2 + BT;
+  float *qs = sm, *os = qs + TILE, *kv_s = os + TILE, *ps = kv_s + 4 * TILE, *ds = ps + BT * PS;    // kv_s: [stage][k, v]; ps, ds: [key][query]
+  float2* rows = reinterpret_cast<float2*>(ds + BT * PS);
   const int tiles = (c.p.max_q + BT - 1) / BT;
   const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
   SeqRange r;
@@ -281,46 +298,54 @@ packed_dq_kernel(const PackedCall c) {
   const int q0 = tile * BT;
   if (q0 >= r.q_len) return;
   const int q_here = min(BT, r.q_len - q0), d = c.p.d, kv = head / (c.p.heads / c.p.kv_heads);
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int group = threadIdx.x / THREADS, tid = threadIdx.x % THREADS, tx = tid & 15, ty = tid >> 4;
   const float sl2 = c.p.scale * 1.4426950408889634f;
   const int64_t at = (int64_t)r.q_begin + q0;
-  load_tile<DP>(qs, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d);
-  load_tile<DP>(os, static_cast<const float*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d);
-  if (threadIdx.x < BT) {
-    const bool there = (int)threadIdx.x < q_here;
-    const int64_t i = (int64_t)head * c.p.q_rows + at + threadIdx.x;
-    const float2 v = there ? c.delta[i] : make_float2(0.f, 0.f);
-    lse2[threadIdx.x] = v.x;
-    delta[threadIdx.x] = v.y;
-  }
-  float2 dq[4][DP / 32];
+  const float* base = static_cast<const float*>(group ? c.v : c.k) + (int64_t)kv * d;
+  auto fetch = [&](int k0, int stage) {                     // keys (group 0) or values (group 1)
+    fetch_tile<DP, THREADS>(kv_s + (2 * stage + group) * TILE, base, group ? c.ldv : c.ldk, (int64_t)r.k_begin + k0, min(BT, r.k_len - k0), d, tid);
+  };
+  if (group == 0) fetch_tile<DP, THREADS>(qs, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d, tid);
+  else fetch_tile<DP, THREADS>(os, static_cast<const float*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d, tid);
+  if (r.k_len > 0) fetch(0, 0);
+  fetched();
+  if (group == 0 && tid < q_here) rows[tid] = c.delta[(int64_t)head * c.p.q_rows + at + tid];
+  float2 acc[4][DP / 32];                                   // of dq, over one half of every tile's keys
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int cc = 0; cc < DP / 32; ++cc) dq[i][cc] = make_float2(0.f, 0.f);
-  for (int k0 = 0; k0 < r.k_len; k0 += BT) {
+    for (int cc = 0; cc < DP / 32; ++cc) acc[i][cc] = make_float2(0.f, 0.f);
+  int stage = 0;
+  for (int k0 = 0; k0 < r.k_len; k0 += BT, stage ^= 1) {
     const int k_here = min(BT, r.k_len - k0);
-    load_tile<DP>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d);
-    load_tile<DP>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d);
+    if (k0 + BT < r.k_len) fetch(k0 + BT, stage ^ 1);
+    fetched();
+    wait_fetched<1>();
     __syncthreads();
-    float s[4][2], dp[4][2];
-    scores<DP>(s, qs, ks, tx, ty);
-    scores<DP>(dp, os, vs, tx, ty);
-    grad_scores(s, dp, lse2, delta, sl2, q_here, k_here, tx, ty);
+    const float *ks = kv_s + 2 * stage * TILE, *vs = ks + TILE;
+    grad_scores<DP, false>(ps, ds, qs, os, ks, vs, rows, sl2, q_here, k_here, group, tx, ty);
+    __syncthreads();
+    accumulate_t<DP, BT / 2>(acc, ds + group * (BT / 2) * PS, ks + group * (BT / 2) * (DP + 4), tx, ty);
+    __syncthreads();                                        // this stage, ps and ds may be written again
+  }
+  // the two halves, in order, through the first stage's memory
+  wait_fetched<0>();
+  __syncthreads();
+  float2* other = reinterpret_cast<float2*>(kv_s) + tid * (4 * (DP / 32) + 1);
+  if (group == 1) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) ds[(tx + 16 * j) * PS + ty * 4 + i] = dp[i][j];
-    __syncthreads();
-    accumulate_t<DP>(dq, ds, ks, tx, ty);
-    __syncthreads();
+      for (int cc = 0; cc < DP / 32; ++cc) other[i * (DP / 32) + cc] = acc[i][cc];
   }
+  __syncthreads();
+  if (group == 1) return;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = ty * 4 + i;
-    if (row >= q_here) continue;
-    float* g = static_cast<float*>(c.dq) + (at + row) * c.lddq + (int64_t)head * d;
-    store_row<DP>(g, dq[i], c.p.scale, tx, d);
+#pragma unroll
+    for (int cc = 0; cc < DP / 32; ++cc) acc[i][cc] = __fadd2_rn(acc[i][cc], other[i * (DP / 32) + cc]);
+    if (row < q_here) store_row<DP>(static_cast<float*>(c.dq) + (at + row) * c.lddq + (int64_t)head * d, acc[i], c.p.scale, tx, d);
   }
 }
 
@@ -331,19 +356,19 @@ cudaError_t launch_variant(const PackedCall& c, Which w, cudaStream_t s) {
   constexpr size_t tile = (size_t)BT * (DP + 4) * 4, prob = (size_t)BT * PS * 4;
   if (w == FORWARD) {
     static PerDeviceFlag done;
-    const size_t smem = 2 * tile + prob;
+    const size_t smem = 5 * tile + prob;
     if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_kernel<DP>, (int)smem)) return e;
     packed_forward_kernel<DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
   } else if (w == DKDV) {
     static PerDeviceFlag done;
-    const size_t smem = 4 * tile + 2 * prob + 2 * BT * 4;
+    const size_t smem = 6 * tile + 2 * prob + 2 * BT * sizeof(float2);
     if (cudaError_t e = ensure_dynamic_smem(done, packed_dkdv_kernel<DP>, (int)smem)) return e;
-    packed_dkdv_kernel<DP><<<c.p.sequences * c.p.kv_heads * ((c.p.max_k + BT - 1) / BT), THREADS, smem, s>>>(c);
+    packed_dkdv_kernel<DP><<<c.p.sequences * c.p.kv_heads * ((c.p.max_k + BT - 1) / BT), GRAD_THREADS, smem, s>>>(c);
   } else {
     static PerDeviceFlag done;
-    const size_t smem = 4 * tile + prob + 2 * BT * 4;
+    const size_t smem = 6 * tile + 2 * prob + BT * sizeof(float2);
     if (cudaError_t e = ensure_dynamic_smem(done, packed_dq_kernel<DP>, (int)smem)) return e;
-    packed_dq_kernel<DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
+    packed_dq_kernel<DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), GRAD_THREADS, smem, s>>>(c);
   }
   return cudaGetLastError();
 }
