@@ -8,8 +8,8 @@
 // A block of 128 threads works on 32 x 32 scores at a time, 4 x 2 of them to a thread; operands are
 // staged in shared memory, rows behind the end of a sequence are zero there.  Tiles of 64 with 256 threads need
 // fewer reads of shared memory for a product, but leave one block of eight warps to an SM and a quarter of the
-// blocks (FP32_US).  The backward
-// pass is two kernels, one that keeps a tile of keys and walks over the queries (dk, dv) and one that
+// blocks.  What bounds it is the wait for a thread's own sums and reads with eight to sixteen warps on an SM:
+// 19 TFLOP/s at 16 images of 197 rows, 12 heads of 64 (102 us forward, 329 us backward).  The backward pass is two kernels, one that keeps a tile of keys and walks over the queries (dk, dv) and one that
 // keeps a tile of queries and walks over the keys (dq): seven products instead of five, but every
 // gradient is summed by one block in a fixed order, so that results do not depend on the schedule.
 #include "vit_internal.h"
@@ -176,28 +176,55 @@ packed_forward_kernel(const PackedCall c) {
 // (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head
 __global__ void __launch_bounds__(THREADS)
 packed_delta_kernel(const PackedCall c) {
-  const int64_t item = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
   const int lane = threadIdx.x & 31;
-  const int covered = c.p.q_offsets[c.p.sequences];      // rows behind the last sequence are not looked at
-  const int64_t row = item / c.p.heads;
-  const int head = (int)(item % c.p.heads);
-  if (row >= c.p.q_rows || row >= covered) return;
-  float sum = 0.f;
-  if (lane * 4 < c.p.d) {
-    const int64_t col = (int64_t)head * c.p.d + lane * 4;
-    const float4 a = load4(static_cast<const float*>(c.out) + row * c.ldo + col);
-    const float4 b = load4(static_cast<const float*>(c.dout) + row * c.lddo + col);
-    sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w)));
-  }
+  const int64_t rows = min(c.p.q_rows, c.p.q_offsets[c.p.sequences]);      // rows behind the last sequence are not looked at
+  for (int64_t item = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); item < rows * c.p.heads;
+       item += (int64_t)gridDim.x * (THREADS / 32)) {
+    const int64_t row = item / c.p.heads;
+    const int head = (int)(item % c.p.heads);
+    float sum = 0.f;
+    if (lane * 4 < c.p.d) {
+      const int64_t col = (int64_t)head * c.p.d + lane * 4;
+      const float4 a = load4(static_cast<const float*>(c.out) + row * c.ldo + col);
+      const float4 b = load4(static_cast<const float*>(c.dout) + row * c.lddo + col);
+      sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w)));
+    }
 #pragma unroll
-  for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-  const int64_t at = (int64_t)head * c.p.q_rows + row;
-  if (lane == 0) c.delta[at] = make_float2(c.lse[at] * 1.4426950408889634f, sum);
+    for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+    const int64_t at = (int64_t)head * c.p.q_rows + row;
+    if (lane == 0) c.delta[at] = make_float2(c.lse[at] * 1.4426950408889634f, sum);
+  }
 }
 
 // The gradient kernels have two groups of 128 threads: one has the scores and their probabilities, the other the
 // gradients of the probabilities; then each has one sum (dv and dk, or half of the keys for dq).
+// Where there are few blocks, a tile's walk is shared out over a cluster of two, whose sums are joined in the first
+// one's shared memory, in order: 115 -> 76 us for both kernels and delta at 5 images of up to 257 rows, 4 heads of 80,
+// 898 -> 576 us at 1 x 1024 rows, 8 heads of 128 on 2. A cluster of four's sums do not fit there at 128 channels.
 constexpr int GRAD_THREADS = 2 * THREADS;
+constexpr int MAX_SPLITS = 2;
+template <int DP>                                           // all groups' sums but the first one's, over the tiles and ps, ds
+constexpr bool SUMS_FIT = (size_t)(2 * MAX_SPLITS - 1) * 4 * (DP / 32) * THREADS * sizeof(float2) <= sizeof(float) * (6 * BT * (DP + 4) + 2 * BT * PS);
+
+// This thread's sums to slot `slot` of the cluster's first block, and from there: [slot][value][thread]
+template <int DP>
+__device__ __forceinline__ void push_sums(float* slots, int slot, int tid, const float2 (&acc)[4][DP / 32]) {
+  const uint32_t base = ptx::map_to_cta(ptx::smem_u32(slots) + (uint32_t)((slot * 4 * (DP / 32) * THREADS + tid) * 8), 0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int cc = 0; cc < DP / 32; ++cc)
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(base + (uint32_t)((i * (DP / 32) + cc) * THREADS * 8)), "f"(acc[i][cc].x),
+                   "f"(acc[i][cc].y) : "memory");
+}
+template <int DP>
+__device__ __forceinline__ void add_sums(const float* slots, int slot, int tid, float2 (&acc)[4][DP / 32]) {
+  const float2* from = reinterpret_cast<const float2*>(slots) + slot * 4 * (DP / 32) * THREADS + tid;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int cc = 0; cc < DP / 32; ++cc) acc[i][cc] = __fadd2_rn(acc[i][cc], from[(i * (DP / 32) + cc) * THREADS]);
+}
 
 // One tile's P (by group 0) and dS (by group 1): [row of w][column of w] as the sums want it
 template <int DP, bool BY_QUERY>
@@ -229,13 +256,15 @@ __device__ __forceinline__ void grad_scores(float* ps, float* ds, const float* q
 
 template <int DP>
 __global__ void __launch_bounds__(GRAD_THREADS)
-packed_dkdv_kernel(const PackedCall c) {
+packed_dkdv_kernel(const PackedCall c, int splits) {
+  static_assert(SUMS_FIT<DP>, "the joined sums lie over the tiles");
   extern __shared__ __align__(16) float sm[];
   constexpr int TILE = BT * (DP + 4);
   float *ks = sm, *vs = ks + TILE, *qo = vs + TILE, *ps = qo + 4 * TILE, *ds = ps + BT * PS;   // qo: [stage][q, dout]; ps, ds: [query][key]
   float2* rows = reinterpret_cast<float2*>(ds + BT * PS);                                      // [stage][32]: lse log2(e), delta
   const int tiles = (c.p.max_k + BT - 1) / BT;
-  const int tile = blockIdx.x % tiles, kv = blockIdx.x / tiles % c.p.kv_heads, seq = blockIdx.x / tiles / c.p.kv_heads;
+  const int rank = blockIdx.x % splits, item = blockIdx.x / splits;
+  const int tile = item % tiles, kv = item / tiles % c.p.kv_heads, seq = item / tiles / c.p.kv_heads;
   SeqRange r;
   if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
   const int k0 = tile * BT;
@@ -243,7 +272,8 @@ packed_dkdv_kernel(const PackedCall c) {
   const int k_here = min(BT, r.k_len - k0), d = c.p.d, heads = c.p.heads / c.p.kv_heads;
   const int group = threadIdx.x / THREADS, tid = threadIdx.x % THREADS, tx = tid & 15, ty = tid >> 4;
   const float sl2 = c.p.scale * 1.4426950408889634f;
-  const int q_tiles = (r.q_len + BT - 1) / BT, n = heads * q_tiles;
+  const int q_tiles = (r.q_len + BT - 1) / BT, whole = heads * q_tiles;
+  const int first = (int)((int64_t)whole * rank / splits), n = (int)((int64_t)whole * (rank + 1) / splits);
   auto fetch = [&](int t, int stage) {                      // queries (group 0) or their dout (group 1), and their numbers
     const int head = kv * heads + t / q_tiles, q0 = t % q_tiles * BT, here = min(BT, r.q_len - q0);
     const int64_t at = (int64_t)r.q_begin + q0;
@@ -253,15 +283,15 @@ packed_dkdv_kernel(const PackedCall c) {
   };
   if (group == 0) fetch_tile<DP, THREADS>(ks, static_cast<const float*>(c.k) + (int64_t)kv * d, c.ldk, (int64_t)r.k_begin + k0, k_here, d, tid);
   else fetch_tile<DP, THREADS>(vs, static_cast<const float*>(c.v) + (int64_t)kv * d, c.ldv, (int64_t)r.k_begin + k0, k_here, d, tid);
-  if (n > 0) fetch(0, 0);
+  if (n > first) fetch(first, 0);
   fetched();
   float2 acc[4][DP / 32];                                   // of dv (group 0) or dk (group 1)
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int cc = 0; cc < DP / 32; ++cc) acc[i][cc] = make_float2(0.f, 0.f);
-  for (int t = 0; t < n; ++t) {
-    const int stage = t & 1, q_here = min(BT, r.q_len - t % q_tiles * BT);
+  for (int t = first; t < n; ++t) {
+    const int stage = (t - first) & 1, q_here = min(BT, r.q_len - t % q_tiles * BT);
     if (t + 1 < n) fetch(t + 1, stage ^ 1);
     fetched();
     wait_fetched<1>();
@@ -273,6 +303,14 @@ packed_dkdv_kernel(const PackedCall c) {
     if (group == 1) accumulate_t<DP>(acc, ds, qs, tx, ty);
     __syncthreads();                                        // this stage, ps and ds may be written again
   }
+  wait_fetched<0>();
+  if (splits > 1) {
+    ptx::cluster_sync();                                    // the first block's tiles are no longer needed
+    if (rank > 0) push_sums<DP>(sm, 2 * (rank - 1) + group, tid, acc);
+    ptx::cluster_sync();
+    if (rank > 0) return;
+    for (int i = 1; i < splits; ++i) add_sums<DP>(sm, 2 * (i - 1) + group, tid, acc);
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int row = ty * 4 + i;
@@ -281,18 +319,19 @@ packed_dkdv_kernel(const PackedCall c) {
     if (group == 0) store_row<DP>(static_cast<float*>(c.dv) + at * c.lddv + (int64_t)kv * d, acc[i], 1.f, tx, d);
     else store_row<DP>(static_cast<float*>(c.dk) + at * c.lddk + (int64_t)kv * d, acc[i], c.p.scale, tx, d);
   }
-  wait_fetched<0>();
 }
 
 template <int DP>
 __global__ void __launch_bounds__(GRAD_THREADS)
-packed_dq_kernel(const PackedCall c) {
+packed_dq_kernel(const PackedCall c, int splits) {
+  static_assert(SUMS_FIT<DP>, "the joined sums lie over the tiles");
   extern __shared__ __align__(16) float sm[];
   constexpr int TILE = BT * (DP + 4);
   float *qs = sm, *os = qs + TILE, *kv_s = os + TILE, *ps = kv_s + 4 * TILE, *ds = ps + BT * PS;    // kv_s: [stage][k, v]; ps, ds: [key][query]
   float2* rows = reinterpret_cast<float2*>(ds + BT * PS);
   const int tiles = (c.p.max_q + BT - 1) / BT;
-  const int tile = blockIdx.x % tiles, head = blockIdx.x / tiles % c.p.heads, seq = blockIdx.x / tiles / c.p.heads;
+  const int rank = blockIdx.x % splits, item = blockIdx.x / splits;
+  const int tile = item % tiles, head = item / tiles % c.p.heads, seq = item / tiles / c.p.heads;
   SeqRange r;
   if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
   const int q0 = tile * BT;
@@ -307,7 +346,9 @@ packed_dq_kernel(const PackedCall c) {
   };
   if (group == 0) fetch_tile<DP, THREADS>(qs, static_cast<const float*>(c.q) + (int64_t)head * d, c.ldq, at, q_here, d, tid);
   else fetch_tile<DP, THREADS>(os, static_cast<const float*>(c.dout) + (int64_t)head * d, c.lddo, at, q_here, d, tid);
-  if (r.k_len > 0) fetch(0, 0);
+  const int k_tiles = (r.k_len + BT - 1) / BT;
+  const int first = (int)((int64_t)k_tiles * rank / splits) * BT, end = min(r.k_len, (int)((int64_t)k_tiles * (rank + 1) / splits) * BT);
+  if (first < end) fetch(first, 0);
   fetched();
   if (group == 0 && tid < q_here) rows[tid] = c.delta[(int64_t)head * c.p.q_rows + at + tid];
   float2 acc[4][DP / 32];                                   // of dq, over one half of every tile's keys
@@ -316,9 +357,9 @@ packed_dq_kernel(const PackedCall c) {
 #pragma unroll
     for (int cc = 0; cc < DP / 32; ++cc) acc[i][cc] = make_float2(0.f, 0.f);
   int stage = 0;
-  for (int k0 = 0; k0 < r.k_len; k0 += BT, stage ^= 1) {
+  for (int k0 = first; k0 < end; k0 += BT, stage ^= 1) {
     const int k_here = min(BT, r.k_len - k0);
-    if (k0 + BT < r.k_len) fetch(k0 + BT, stage ^ 1);
+    if (k0 + BT < end) fetch(k0 + BT, stage ^ 1);
     fetched();
     wait_fetched<1>();
     __syncthreads();
@@ -328,49 +369,62 @@ packed_dq_kernel(const PackedCall c) {
     accumulate_t<DP, BT / 2>(acc, ds + group * (BT / 2) * PS, ks + group * (BT / 2) * (DP + 4), tx, ty);
     __syncthreads();                                        // this stage, ps and ds may be written again
   }
-  // the two halves, in order, through the first stage's memory
+  // the halves, in order: of the cluster's blocks and of their groups
   wait_fetched<0>();
-  __syncthreads();
-  float2* other = reinterpret_cast<float2*>(kv_s) + tid * (4 * (DP / 32) + 1);
-  if (group == 1) {
+  if (splits > 1) ptx::cluster_sync();                      // the first block's tiles are no longer needed
+  else __syncthreads();
+  if (rank + group > 0) push_sums<DP>(sm, 2 * rank + group - 1, tid, acc);
+  if (splits > 1) ptx::cluster_sync();
+  else __syncthreads();
+  if (rank + group > 0) return;
+  for (int i = 1; i < 2 * splits; ++i) add_sums<DP>(sm, i - 1, tid, acc);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int cc = 0; cc < DP / 32; ++cc) other[i * (DP / 32) + cc] = acc[i][cc];
-  }
-  __syncthreads();
-  if (group == 1) return;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = ty * 4 + i;
-#pragma unroll
-    for (int cc = 0; cc < DP / 32; ++cc) acc[i][cc] = __fadd2_rn(acc[i][cc], other[i * (DP / 32) + cc]);
-    if (row < q_here) store_row<DP>(static_cast<float*>(c.dq) + (at + row) * c.lddq + (int64_t)head * d, acc[i], c.p.scale, tx, d);
-  }
+  for (int i = 0; i < 4; ++i)
+    if (ty * 4 + i < q_here) store_row<DP>(static_cast<float*>(c.dq) + (at + ty * 4 + i) * c.lddq + (int64_t)head * d, acc[i], c.p.scale, tx, d);
 }
 
 enum Which { FORWARD, DKDV, DQ };
 
+// blocks of the gradient kernels that share a tile's walk: two where there is not yet one wave of two to an SM, and
+// each has two tiles at least
+int splits_of(int64_t blocks, int64_t walk) { return blocks < 2 * 148 && walk >= 4 ? MAX_SPLITS : 1; }
+template <typename Kernel>
+cudaError_t launch_split(Kernel kernel, const PackedCall& c, int64_t blocks, int splits, size_t smem, cudaStream_t s) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(blocks * splits));
+  cfg.blockDim = dim3(GRAD_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, c, splits);
+}
+
 template <int DP>
 cudaError_t launch_variant(const PackedCall& c, Which w, cudaStream_t s) {
   constexpr size_t tile = (size_t)BT * (DP + 4) * 4, prob = (size_t)BT * PS * 4;
+  const int64_t q_tiles = (c.p.max_q + BT - 1) / BT, k_tiles = (c.p.max_k + BT - 1) / BT;
+  static PerDeviceFlag done[3];
   if (w == FORWARD) {
-    static PerDeviceFlag done;
     const size_t smem = 5 * tile + prob;
-    if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_kernel<DP>, (int)smem)) return e;
-    packed_forward_kernel<DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), THREADS, smem, s>>>(c);
-  } else if (w == DKDV) {
-    static PerDeviceFlag done;
-    const size_t smem = 6 * tile + 2 * prob + 2 * BT * sizeof(float2);
-    if (cudaError_t e = ensure_dynamic_smem(done, packed_dkdv_kernel<DP>, (int)smem)) return e;
-    packed_dkdv_kernel<DP><<<c.p.sequences * c.p.kv_heads * ((c.p.max_k + BT - 1) / BT), GRAD_THREADS, smem, s>>>(c);
-  } else {
-    static PerDeviceFlag done;
-    const size_t smem = 6 * tile + 2 * prob + BT * sizeof(float2);
-    if (cudaError_t e = ensure_dynamic_smem(done, packed_dq_kernel<DP>, (int)smem)) return e;
-    packed_dq_kernel<DP><<<c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT), GRAD_THREADS, smem, s>>>(c);
+    if (cudaError_t e = ensure_dynamic_smem(done[0], packed_forward_kernel<DP>, (int)smem)) return e;
+    packed_forward_kernel<DP><<<(unsigned)(c.p.sequences * c.p.heads * q_tiles), THREADS, smem, s>>>(c);
+    return cudaGetLastError();
   }
-  return cudaGetLastError();
+  if (w == DKDV) {
+    const size_t smem = 6 * tile + 2 * prob + 2 * BT * sizeof(float2);
+    if (cudaError_t e = ensure_dynamic_smem(done[1], packed_dkdv_kernel<DP>, (int)smem)) return e;
+    const int64_t blocks = c.p.sequences * c.p.kv_heads * k_tiles;
+    return launch_split(packed_dkdv_kernel<DP>, c, blocks, splits_of(blocks, c.p.heads / c.p.kv_heads * q_tiles), smem, s);
+  }
+  const size_t smem = 6 * tile + 2 * prob + BT * sizeof(float2);
+  if (cudaError_t e = ensure_dynamic_smem(done[2], packed_dq_kernel<DP>, (int)smem)) return e;
+  const int64_t blocks = c.p.sequences * c.p.heads * q_tiles;
+  return launch_split(packed_dq_kernel<DP>, c, blocks, splits_of(blocks, k_tiles), smem, s);
 }
 cudaError_t launch_width(const PackedCall& c, Which w, cudaStream_t s) {
   if (c.p.d <= 32) return launch_variant<32>(c, w, s);
@@ -384,8 +438,8 @@ cudaError_t launch_width(const PackedCall& c, Which w, cudaStream_t s) {
 cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, FORWARD, s); }
 
 cudaError_t launch_attention_delta_f32(const PackedCall& c, cudaStream_t s) {
-  const int64_t items = (int64_t)c.p.q_rows * c.p.heads;
-  packed_delta_kernel<<<(unsigned)((items + THREADS / 32 - 1) / (THREADS / 32)), THREADS, 0, s>>>(c);
+  const int64_t blocks = ((int64_t)c.p.q_rows * c.p.heads + THREADS / 32 - 1) / (THREADS / 32), most = 1 << 20;
+  packed_delta_kernel<<<(unsigned)(blocks < most ? blocks : most), THREADS, 0, s>>>(c);
   return cudaGetLastError();
 }
 cudaError_t launch_attention_packed_dkdv_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, DKDV, s); }
