@@ -302,9 +302,10 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
  * serve such a layer between its QKV product and its output product, in inference and fine-tuning.
  * Rows have strides of their own (`ld...`, in elements), so that queries, keys and values can be read
  * from, and their gradients written to, the column blocks of one [rows, (heads + 2 kv_heads) * d] buffer.
- * Common rules, checked before anything is launched: pointers 16-byte aligned; d a multiple of 16, at
- * most 128; a stride at least as wide as its heads and a multiple of 8; no output may overlap an input
- * or another output unless stated (column blocks of one buffer with the same stride do not overlap).
+ * Common rules, checked before anything is launched: pointers 16-byte aligned (offsets: 4); d a multiple
+ * of 16, at most 128; heads * d below 2^31; a stride at least as wide as its heads and a multiple of 8; no
+ * output may overlap an input or another output unless stated (column blocks of one buffer with the same
+ * stride do not overlap).
  * Sums, norms and softmax statistics are fp32; bf16 results are rounded once.
  * Results do not depend on the schedule: the same call gives the same bits. */
 

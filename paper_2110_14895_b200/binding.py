@@ -353,13 +353,16 @@ def vit_op_attention(h, dtype, images, T, heads, d, qkv, out, stream=0):
     _check(lib().vit_op_attention(h, dtype, images, T, heads, d, qkv, out, stream), "vit_op_attention")
 
 
+_FOUR = c_int32 * 4
+
+
 def make_rope(axis_pairs, freqs, positions, interleaved=False) -> VitRope:
     """Rotary positions: channel pairs per axis (1 to 4 axes), device pointers of the pairs' fp32 frequencies and of
     the int32 positions [axes][rows]."""
     n = len(axis_pairs)
     if not 1 <= n <= 4:
         raise ValueError("one to four axes")
-    return VitRope(n, (c_int32 * 4)(*axis_pairs), 1 if interleaved else 0, positions, freqs)
+    return VitRope(n, _FOUR(*axis_pairs), 1 if interleaved else 0, positions, freqs)
 
 
 def make_attention_problem(sequences, heads, kv_heads, d, q_rows, max_q, q_offsets, k_rows, max_k, k_offsets,

@@ -83,7 +83,7 @@ __device__ __forceinline__ void tmem_ld_wait_16(uint32_t (&r)[16], uint32_t (&t)
                : "memory");
 }
 // One lane of the warp, chosen by the hardware.  The products are issued behind this and not behind
-// `lane == 0`: their operands then stay in uniform registers (110 -> about 20 cycles to issue one).
+// `lane == 0`: their operands then stay in uniform registers (110 cycles -> what the product itself takes, 31 at 64 columns).
 __device__ __forceinline__ bool elect_one() {
   uint32_t one;
   asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}\n" : "=r"(one));
@@ -267,6 +267,7 @@ __device__ __forceinline__ int find_pieces(const vit_attention_problem& p, int* 
     __syncthreads();                                             // `before` is read no more
     carry = end;
   }
+  ptx::fence_proxy_async_smem();                                 // the copies come to where `before` was
   __syncthreads();
   return carry > (int)blockIdx.x ? (carry - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
 }
@@ -1116,7 +1117,8 @@ cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
 }
 
 // The parts of a piece of the backward pass: so many that there are two pieces to an SM or so, of eight tiles at least,
-// eight at most (4 sequences of up to 4097, 8 heads over 2 key heads of 128: dk and dv 269 us in one part, PARTS_US in four)
+// eight at most (4 sequences of up to 4097, 8 heads over 2 key heads of 128:
+// dk and dv 269 us in one part, 211 and 6 for the sum in two)
 int log2_parts(const vit_attention_problem& p, bool dkdv) {
   const int64_t pieces = (int64_t)p.sequences * (dkdv ? p.kv_heads : p.heads) * (((dkdv ? p.max_k : p.max_q) + RT - 1) / RT);
   const int64_t tiles = (int64_t)(dkdv ? p.heads / p.kv_heads : 1) * (((dkdv ? p.max_q : p.max_k) + CT - 1) / CT);
@@ -1163,6 +1165,7 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
 
 }  // namespace
 
+bool attention_in_parts(const vit_attention_problem& p, bool dkdv) { return log2_parts(p, dkdv) > 0; }
 // Columns of tensor memory decide where a piece's rows are held: 128 + d + d / 2 of a warpgroup's 256 in
 // the forward pass, 256 + 2 d + d of 512 for dk and dv, 256 + d + d for dq.
 size_t attention_partial_floats(const vit_attention_problem& p) {

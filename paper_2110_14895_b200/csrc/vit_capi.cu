@@ -258,12 +258,25 @@ bool rope_ok(const vit_rope* r, int d) {
   return 2 * n <= d && r->positions && r->freqs && !misaligned(r->positions) && !misaligned(r->freqs);
 }
 
+// whether an output lies over the positions or frequencies
+bool rope_overlaps(const vit_rope* r, int rows, const Block& out) {
+  if (!r) return false;
+  const int64_t n = (int64_t)r->pairs[0] + (r->axes > 1 ? r->pairs[1] : 0) + (r->axes > 2 ? r->pairs[2] : 0) + (r->axes > 3 ? r->pairs[3] : 0);
+  return blocks_overlap(out, Block{r->positions, 1, (int64_t)r->axes * rows, (int64_t)r->axes * rows, 4}) ||
+         blocks_overlap(out, Block{r->freqs, 1, n, n, 4});
+}
+
 bool attention_problem_ok(int dtype, const vit_attention_problem* p) {
   if (!p || !head_ok(dtype, p->d) || p->sequences < 0 || p->heads < 1 || p->kv_heads < 1 || p->heads % p->kv_heads) return false;
   if (p->q_rows < 0 || p->k_rows < 0 || p->max_q < 0 || p->max_k < 0 || !p->q_offsets || !p->k_offsets) return false;
   if ((reinterpret_cast<uintptr_t>(p->q_offsets) | reinterpret_cast<uintptr_t>(p->k_offsets)) & 3) return false;
   if ((int64_t)p->heads * p->d > INT32_MAX) return false;
   return p->scale > 0.f && p->scale <= 3.402823466e38f;
+}
+// whether an output lies over the offsets
+bool offsets_overlap(const vit_attention_problem& p, const Block& out) {
+  const int64_t n = (int64_t)p.sequences + 1;
+  return blocks_overlap(out, Block{p.q_offsets, 1, n, n, 4}) || blocks_overlap(out, Block{p.k_offsets, 1, n, n, 4});
 }
 // blocks of the launches: one per sequence, head and tile of at least 32 rows
 bool attention_fits(const vit_attention_problem* p) {
@@ -758,10 +771,11 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
 
 int vit_op_rope_axes(vit_handle* h, int dtype, int rows, int heads, int d, const vit_rope* rope, int inverse,
                      const void* x, int64_t ldx, void* y, int64_t ldy, void* stream) {
-  if (!h || rows < 0 || heads < 1 || !head_ok(dtype, d) || !rope || !rope_ok(rope, d) || !on_own_device(h)) return VIT_ERR_INVALID_ARG;
+  if (!h || rows < 0 || heads < 1 || !head_ok(dtype, d) || (int64_t)heads * d > INT32_MAX || !rope || !rope_ok(rope, d) || !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
   const size_t es = element_bytes(dtype);
   const Block bx{x, rows, (int64_t)heads * d, ldx, es}, by{y, rows, (int64_t)heads * d, ldy, es};
-  if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by))) return VIT_ERR_INVALID_ARG;
+  if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by)) || rope_overlaps(rope, rows, by)) return VIT_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   RopeNormCall c{};
   c.dev_status = h->dev_status;
@@ -781,7 +795,9 @@ int vit_op_qk_norm_rope(vit_handle* h, int dtype, int rows, int q_heads, int k_h
   const size_t es = element_bytes(dtype);
   const int64_t width = ((int64_t)q_heads + k_heads) * d;
   const Block bx{x, rows, width, ldx, es}, by{y, rows, width, ldy, es};
-  if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by))) return VIT_ERR_INVALID_ARG;
+  if (width > INT32_MAX || !block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by))) return VIT_ERR_INVALID_ARG;
+  if (rope_overlaps(rope, rows, by) || blocks_overlap(by, Block{q_gain, 1, d, d, 4}) || blocks_overlap(by, Block{k_gain, 1, d, d, 4}))
+    return VIT_ERR_INVALID_ARG;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   RopeNormCall c{};
   c.dev_status = h->dev_status;
@@ -809,12 +825,15 @@ int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads
   const int64_t width = ((int64_t)q_heads + k_heads) * d;
   const Block bx{x, rows, width, ldx, es}, bdy{dy, rows, width, lddy, es}, bdx{dx, rows, width, lddx, es};
   const Block bgq{dq_gain, 1, d, d, 4}, bgk{dk_gain, 1, d, d, 4}, bws{ws, 1, (int64_t)need, (int64_t)need, 1};
-  if (!block_ok(bx) || !block_ok(bdy) || !block_ok(bdx)) return VIT_ERR_INVALID_ARG;
+  if (width > INT32_MAX || !block_ok(bx) || !block_ok(bdy) || !block_ok(bdx)) return VIT_ERR_INVALID_ARG;
   if ((!same_block(bx, bdx) && blocks_overlap(bx, bdx)) || (!same_block(bdy, bdx) && blocks_overlap(bdy, bdx)) ||
       blocks_overlap(bgq, bgk))
     return VIT_ERR_INVALID_ARG;
   for (const Block* b : {&bx, &bdy, &bdx, &bgq, &bgk})
     if (blocks_overlap(*b, bws) || (b != &bgq && blocks_overlap(*b, bgq)) || (b != &bgk && blocks_overlap(*b, bgk)))
+      return VIT_ERR_INVALID_ARG;
+  for (const Block* b : {&bdx, &bgq, &bgk, &bws})
+    if (rope_overlaps(rope, rows, *b) || blocks_overlap(*b, Block{q_gain, 1, d, d, 4}) || blocks_overlap(*b, Block{k_gain, 1, d, d, 4}))
       return VIT_ERR_INVALID_ARG;
   if (ws_bytes < need) return VIT_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -846,6 +865,7 @@ int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_proble
   if (!block_ok(bq) || !block_ok(bk) || !block_ok(bv) || !block_ok(bo) || (need && (!ws || misaligned(ws)))) return VIT_ERR_INVALID_ARG;
   for (const Block* b : {&bq, &bk, &bv, &bo, &bl})
     if ((b != &bo && blocks_overlap(*b, bo)) || (b != &bl && blocks_overlap(*b, bl)) || blocks_overlap(*b, bws)) return VIT_ERR_INVALID_ARG;
+  if (offsets_overlap(p, bo) || offsets_overlap(p, bl)) return VIT_ERR_INVALID_ARG;
   if (ws_bytes < need) return VIT_ERR_WORKSPACE;
   if (p.sequences == 0 || p.q_rows == 0 || p.max_q == 0) return VIT_OK;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -882,6 +902,7 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
       if (blocks_overlap(to[i], b)) return VIT_ERR_INVALID_ARG;
     for (int j = 0; j < i; ++j)
       if (blocks_overlap(to[i], to[j])) return VIT_ERR_INVALID_ARG;
+    if (offsets_overlap(p, to[i])) return VIT_ERR_INVALID_ARG;
   }
   if (ws_bytes < need) return VIT_ERR_WORKSPACE;
   if (p.sequences == 0) return VIT_OK;
@@ -899,6 +920,7 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
   if (!b16 && queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta_f32(c, s));
   if (queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, b16 ? launch_attention_packed_dq_bf16(c, s) : launch_attention_packed_dq_f32(c, s));
   if (keys) VIT_LAUNCH(h, VIT_PROF_ATTENTION, b16 ? launch_attention_packed_dkdv_bf16(c, s) : launch_attention_packed_dkdv_f32(c, s));
+  if (b16) h->launches.fetch_add((queries && attention_in_parts(p, false)) + (keys && attention_in_parts(p, true)), std::memory_order_relaxed);
   return VIT_OK;
 }
 

@@ -186,6 +186,7 @@ struct PackedCall {
   float* partial;                           // backward, bf16: sums of the parts of the work (attention_partial_floats)
   int* dev_status;
 };
+bool attention_in_parts(const vit_attention_problem& p, bool dkdv);         // bf16: a second kernel adds the parts
 size_t attention_partial_floats(const vit_attention_problem& p);
 // a few queries (times heads that share a key head) of a sequence go to the kernel for few rows (attention_rows.cu)
 bool attention_rows_supported(const vit_attention_problem& p, bool act_bf16);

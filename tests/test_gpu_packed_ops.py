@@ -127,6 +127,9 @@ NORM_CASES = [
     # rows, q heads, k heads, d, pairs
     (1, 1, 1, 16, (8,)), (197, 12, 12, 64, (16, 16)), (33, 9, 3, 48, (8, 7, 8)), (257, 16, 16, 80, (20, 20)),
     (10, 4, 1, 128, (16, 24, 24)), (515, 0, 5, 96, (13, 9)), (64, 3, 0, 112, ()), (3001, 2, 2, 32, (4, 4, 4, 4)),
+    # many rows: they come through the rings in shared memory, of four, three and two rows; or are too long for them
+    (5003, 3, 2, 64, (16, 16)), (4737, 2, 2, 128, (16, 24, 24)), (4990, 12, 12, 64, (16, 16)), (4750, 20, 20, 112, (28, 28)),
+    (5001, 5, 5, 80, (11, 9)),
 ]
 
 
@@ -355,6 +358,10 @@ ATTENTION_CASES = [
     ([1100], None, 1, 1, 80), ([256, 255, 384], None, 1, 1, 16),
     # few and long: the work on a tile of keys (or queries) is shared out, also for the short sequences beside them
     ([1300, 20, 0, 530], None, 8, 2, 64), ([2100, 70], None, 4, 1, 128), ([30, 700], [2000, 1], 2, 2, 48),
+    ([1500, 3], None, 2, 1, 96), ([900, 1030], None, 2, 2, 112),
+    # as many queries as the kernel for few of them takes (four rows in bf16, eight in fp32), and one more
+    ([1, 1, 0], [1030, 5, 3], 8, 1, 64), ([2, 1], [300, 0], 4, 2, 128), ([4, 3], [700, 70], 2, 2, 112), ([8, 2], [333, 65], 2, 2, 48),
+    ([9, 5], [333, 65], 1, 1, 16),
 ]
 
 
@@ -513,6 +520,141 @@ def test_packed_attention_gradients_against_differences(ctx):
         assert abs(near - want) <= abs(far - near) + 1e-3 * max(1.0, abs(want)) * 0.1 + 4e-4, (near, far, want)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_packed_attention_bad_offsets_where_long_walks_are_shared(ctx, dtype):
+    vit, m = ctx
+    p = Packed(vit, [1300, 600, 530], [1300, 600, 530], 8, 2, 64, dtype, trail=8)
+    good = p.forward(m)
+    good_grads = p.backward(m, *good)
+    m.check()
+    p.k_off[3] = p.k_rows + 1
+    out, lse = p.forward(m)
+    dq, dkv = p.backward(m, *good)
+    with pytest.raises(vit.VitError) as e:
+        m.check()
+    assert e.value.status == vit.VIT_ERR_OFFSETS
+    assert torch.equal(out[:1900], good[0][:1900]) and torch.equal(lse[:, :1900], good[1][:, :1900])
+    assert torch.equal(dq[:1900], good_grads[0][:1900]) and torch.equal(dkv[:1900], good_grads[1][:1900])
+    assert (out[1900:] == 33).all() and (lse[:, 1900:] == 33).all() and (dq[1900:] == 33).all() and (dkv[1900:] == 33).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("sequences,n", [(9700, 5), (513, 9), (700, 1)])
+def test_packed_attention_of_many_short_sequences(ctx, dtype, sequences, n):
+    """More sequences than a block looks up at a time, and more pieces than its table holds."""
+    vit, m = ctx
+    heads, d = 2, 32
+    p = Packed(vit, [n] * sequences, [n] * sequences, heads, heads, d, dtype, trail=3)
+    out, lse = p.forward(m)
+    dq, dkv = p.backward(m, out, lse)
+    m.check()
+    half, width, rows = HALF[dtype], heads * d, sequences * n
+    cut = lambda t: t[:rows].double().reshape(sequences, n, heads, d).transpose(1, 2)
+    q, k, v, o, do = (cut(t) for t in (p.q, p.k, p.v, out[:, :width], p.dout))
+    s = p.scale * q @ k.transpose(-1, -2)
+    e = (d + 8) * 2.0 ** -24 * (p.scale * q.abs() @ k.abs().transpose(-1, -2)).max() + 2.0 ** -20
+    w, want = torch.logsumexp(s, -1), torch.softmax(s, -1) @ v
+    got_lse = lse[:, :rows].double().reshape(heads, sequences, n).transpose(0, 1)
+    tol = half * want.abs() + (half * 1.01 + 2 * e + (n + 16) * 2.0 ** -24) * (torch.softmax(s, -1) @ v.abs())
+    assert ((o - want).abs() <= tol).all()
+    assert ((got_lse - w).abs() <= e + (n + 16) * 2.0 ** -24 + 2.0 ** -22 * w.abs()).all()
+    prob = torch.exp(s - got_lse[..., None])
+    ds = prob * (do @ v.transpose(-1, -2) - (do * o).sum(-1, keepdim=True))
+    dds = ds.abs() * (half * 1.01 + 2 * e) + prob * (d + 8) * 2.0 ** -24 * (do.abs() @ v.abs().transpose(-1, -2) +
+                                                                         (do * o).abs().sum(-1, keepdim=True))
+    acc = (n + 16) * 2.0 ** -24
+    spread = p.scale * (dds + acc * ds.abs())
+    for got, exact, tol in ((cut(dq[:, :width]), p.scale * ds @ k, spread @ k.abs()),
+                            (cut(dkv[:, :width]), p.scale * ds.transpose(-1, -2) @ q, spread.transpose(-1, -2) @ q.abs()),
+                            (cut(dkv[:, width:2 * width]), prob.transpose(-1, -2) @ do,
+                             ((half * 1.01 + 2 * e + acc) * prob).transpose(-1, -2) @ do.abs())):
+        assert ((got - exact).abs() <= half * exact.abs() + tol).all()
+    assert (out[rows:] == 33).all() and (dq[rows:] == 33).all() and (dkv[rows:] == 33).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_far_apart(ctx, dtype):
+    """Strides that put the rows behind 2^31 elements: the bits of the dense call."""
+    vit, m = ctx
+    ld, rows, heads, d = 2 ** 24 + 8, 150, 2, 64
+    dt, width = _dt(vit, dtype), 2 * 64
+    assert (rows - 20) * ld > 2 ** 31
+    far = torch.empty(rows * ld, dtype=dtype, device="cuda").view(rows, ld)     # columns: q, k, v, out, dout, dq, dk, dv
+    assert width * 8 <= ld
+    block = lambda i: far[:, i * width:(i + 1) * width]
+    gen = _gen(31)
+    dense = [_normal(gen, rows, width, dtype=dtype) for _ in range(3)] + [torch.empty(rows, width, dtype=dtype, device="cuda")]
+    dense += [_normal(gen, rows, width, dtype=dtype)] + [torch.empty_like(dense[0]) for _ in range(3)]
+    for i, t in enumerate(dense):
+        block(i).copy_(t)
+    q_off = torch.tensor([0, 20, 150], dtype=torch.int32, device="cuda")
+    one = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    lse = torch.empty(heads, rows, device="cuda")
+    for off, q_rows, max_q in ((q_off, rows, 130), (one, 2, 1)):               # and with one query to a sequence
+        problem = vit.make_attention_problem(2, heads, heads, d, q_rows, max_q, off.data_ptr(), rows, 130, q_off.data_ptr(), 0.125)
+        n = vit.vit_attention_packed_bytes(dt, problem, True)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        for get, step in ((lambda i: dense[i], width), (block, ld)):
+            q, k, v, o, do, dq, dk, dv = (get(i).data_ptr() for i in range(8))
+            vit.vit_op_attention_packed(m.h, dt, problem, q, step, k, step, v, step, o, step, lse.data_ptr(), 0, 0)
+            vit.vit_op_attention_packed_backward(m.h, dt, problem, q, step, k, step, v, step, o, step, lse.data_ptr(), do, step, dq, step,
+                                                 dk, step, dv, step, ws.data_ptr(), n)
+            m.check()
+        for i in (3, 5):
+            assert torch.equal(block(i)[:q_rows], dense[i][:q_rows])
+        for i in (6, 7):
+            assert torch.equal(block(i), dense[i])
+    gains = 1 + _normal(gen, 2, d, scale=0.1)
+    freqs, positions = _rope_inputs(gen, rows, (16, 16), 50)
+    rope = vit.make_rope((16, 16), freqs.data_ptr(), positions.data_ptr())
+    n = vit.vit_qk_norm_rope_backward_bytes(rows, 1, 1, d)
+    ws, dg = torch.empty(n, dtype=torch.uint8, device="cuda"), torch.empty(2, 2, d, device="cuda")
+    for j, (get, step) in enumerate(((lambda i: dense[i], width), (block, ld))):
+        x, y, z, dy, dx = (get(i).data_ptr() for i in (0, 1, 2, 4, 5))
+        vit.vit_op_rope_axes(m.h, dt, rows, heads, d, rope, False, x, step, y, step)
+        vit.vit_op_qk_norm_rope(m.h, dt, rows, 1, 1, d, gains[0].data_ptr(), gains[1].data_ptr(), EPS, rope, x, step, z, step)
+        vit.vit_op_qk_norm_rope_backward(m.h, dt, rows, 1, 1, d, gains[0].data_ptr(), gains[1].data_ptr(), EPS, rope, x, step, dy, step,
+                                         dx, step, dg[j, 0].data_ptr(), dg[j, 1].data_ptr(), ws.data_ptr(), n)
+        m.check()
+    for i in (1, 2, 5):
+        assert torch.equal(block(i), dense[i])
+    assert torch.equal(dg[0], dg[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_two_streams_at_once(ctx, dtype):
+    """Calls on two streams, each with a workspace of its own, give the bits of calls one after the other."""
+    vit, m = ctx
+    problems = [Packed(vit, [700, 385], [700, 385], 4, 2, 80, dtype, seed=1), Packed(vit, [1, 1, 1], [577, 40, 1030], 4, 4, 64, dtype, seed=2),
+                Packed(vit, [2100], [2100], 4, 1, 64, dtype, seed=3)]
+    alone = []
+    for p in problems:
+        out, lse = p.forward(m)
+        alone.append((out, lse, *p.backward(m, out, lse)))
+        m.check()
+    dt = _dt(vit, dtype)
+    streams = [torch.cuda.Stream() for _ in problems]
+    results, keep = [], []
+    for p in problems:
+        out, lse = torch.full_like(alone[len(results)][0], 33.0), torch.full_like(alone[len(results)][1], 33.0)
+        results.append((out, lse, torch.full_like(p.qbuf, 33.0), torch.full_like(p.kvbuf, 33.0)))
+        keep.append(torch.empty(vit.vit_attention_packed_bytes(dt, p.problem, True), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for p, s, (out, lse, dq, dkv), ws in zip(problems, streams, results, keep):
+            kw, s = p.kv * p.d, s.cuda_stream
+            ops = (p.q.data_ptr(), p.ldq, p.k.data_ptr(), p.ldkv, p.v.data_ptr(), p.ldkv)
+            vit.vit_op_attention_packed(m.h, dt, p.problem, *ops, out.data_ptr(), out.stride(0), lse.data_ptr(), 0, 0, s)
+            vit.vit_op_attention_packed_backward(m.h, dt, p.problem, *ops, out.data_ptr(), out.stride(0), lse.data_ptr(), p.dout.data_ptr(),
+                                                 p.dout.stride(0), dq.data_ptr(), p.ldq, dkv.data_ptr(), p.ldkv, dkv[:, kw:].data_ptr(),
+                                                 p.ldkv, ws.data_ptr(), ws.numel(), s)
+    torch.cuda.synchronize()
+    m.check()
+    for a, b in zip(alone, results):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+
+
 # ------------------------------------------------------------------------------- the layer, as it is used
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_layer_of_packed_images(ctx, dtype):
@@ -624,20 +766,24 @@ def test_packed_ops_refuse(ctx):
                  (0, 64, 2, 64, vit.make_rope((30, 8), fp, pp), 0, xp, 256, yp, 256), (0, 64, 2, 64, vit.make_rope((-1, 8), fp, pp), 0, xp, 256, yp, 256),
                  (0, 64, 2, 64, vit.make_rope((8, 8), 0, pp), 0, xp, 256, yp, 256), (0, 64, 2, 64, good, 0, xp, 120, yp, 256),
                  (0, 64, 2, 64, good, 0, xp, 132, yp, 256), (0, 64, 2, 64, good, 0, xp + 2, 256, yp, 256), (0, 64, 2, 64, good, 0, 0, 256, yp, 256),
-                 (0, 32, 2, 64, good, 0, xp, 256, xp + 128, 256), (0, 32, 2, 64, good, 0, xp, 256, xp + 512, 256)]:
+                 (0, 32, 2, 64, good, 0, xp, 256, xp + 128, 256), (0, 32, 2, 64, good, 0, xp, 256, xp + 512, 256),
+                 (0, 1, 2, 64, good, 0, xp, 256, pp, 256), (0, 1, 2, 64, good, 0, xp, 256, fp, 256),
+                 (0, 1, 2 ** 28, 64, good, 0, xp, 2 ** 34, yp, 2 ** 34)]:
         refused(bad, vit.vit_op_rope_axes, m.h, *args)
     norm = (0, 64, 1, 1, 64, fp, fp, EPS, good)
     for i, v in [(1, -1), (2, -1), (4, 40), (5, 0), (6, fp + 4), (7, -1.0), (7, float("nan"))]:
         args = list(norm)
         args[i] = v
         refused(bad, vit.vit_op_qk_norm_rope, m.h, *args, xp, 256, yp, 256)
+    refused(bad, vit.vit_op_qk_norm_rope, m.h, 0, 1, *norm[2:], xp, 256, fp, 256)
     n = vit.vit_qk_norm_rope_backward_bytes(64, 1, 1, 64)
     ws = torch.empty(n, dtype=torch.uint8, device="cuda")
     dg = torch.empty(2, 64, device="cuda")
     dx = torch.zeros_like(x)
     tail = [xp, 256, yp, 256, dx.data_ptr(), 256, dg[0].data_ptr(), dg[1].data_ptr(), ws.data_ptr(), n]
     refused(vit.VIT_ERR_WORKSPACE, vit.vit_op_qk_norm_rope_backward, m.h, *norm, *tail[:-1], n - 1)
-    for i, v in [(6, 0), (7, dg[0].data_ptr()), (8, 0), (4, xp + 16), (6, dx.data_ptr()), (8, dx.data_ptr())]:
+    for i, v in [(6, 0), (7, dg[0].data_ptr()), (8, 0), (4, xp + 16), (6, dx.data_ptr()), (8, dx.data_ptr()), (6, fp),
+                 (7, pp)]:
         args = list(tail)
         args[i] = v
         refused(bad, vit.vit_op_qk_norm_rope_backward, m.h, *norm, *args)
@@ -657,7 +803,8 @@ def test_packed_ops_refuse(ctx):
         refused(bad, forward, vit.make_attention_problem(*args))
     ok = vit.make_attention_problem(*base)
     refused(bad, forward, ok, 7)
-    for kw in (dict(q=xp + 2), dict(q=0), dict(ldq=252), dict(ldq=248), dict(out=xp), dict(out=kv.data_ptr()), dict(l=0), dict(l=o.data_ptr())):
+    for kw in (dict(q=xp + 2), dict(q=0), dict(ldq=252), dict(ldq=248), dict(out=xp), dict(out=kv.data_ptr()), dict(l=0), dict(l=o.data_ptr()),
+               dict(l=off.data_ptr())):
         refused(bad, lambda: forward(ok, **kw))
     huge = vit.make_attention_problem(2 ** 30, *base[1:])
     refused(vit.VIT_ERR_TOO_LARGE, forward, huge)
@@ -667,7 +814,8 @@ def test_packed_ops_refuse(ctx):
     rest = [xp, 256, kv.data_ptr(), 256, kv[:, 128:].data_ptr(), 256, o.data_ptr(), 256, lse.data_ptr(), yp, 256, dq.data_ptr(), 256,
             dkv.data_ptr(), 256, dkv[:, 128:].data_ptr(), 256, big.data_ptr(), nb]
     refused(vit.VIT_ERR_WORKSPACE, vit.vit_op_attention_packed_backward, m.h, 0, ok, *rest[:-1], nb - 1)
-    for i, v in [(0, 0), (8, 0), (9, yp + 2), (11, xp), (13, dkv.data_ptr() + 64), (15, dq.data_ptr()), (17, 0), (17, dq.data_ptr())]:
+    for i, v in [(0, 0), (8, 0), (9, yp + 2), (11, xp), (13, dkv.data_ptr() + 64), (15, dq.data_ptr()), (17, 0), (17, dq.data_ptr()),
+                 (17, off.data_ptr())]:
         args = list(rest)
         args[i] = v
         refused(bad, vit.vit_op_attention_packed_backward, m.h, 0, ok, *args)
