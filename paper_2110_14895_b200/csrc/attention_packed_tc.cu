@@ -205,71 +205,142 @@ __device__ __forceinline__ void store_rows(float* dst, int64_t ld, uint32_t tadd
   }
 }
 
-// A piece of work: `span` rows of one head of one sequence.
-struct Piece { int head, x0; SeqRange r; };
-// A block's pieces are looked up once, at its start: numbers blockIdx.x, + gridDim.x, ... of those whose rows exist, so
-// that every block gets the same number of them however the lengths differ.
-constexpr int MAX_PIECES = 128, SEQ_CHUNK = 512;                 // of a block; sequences looked at together
+// A piece of work: rows [x0, x0 + span) of one head of one sequence against tiles [t_begin, t_begin + n) of what they meet.
+struct Piece { int head, x0; SeqRange r; int t_begin, n; };
+// Which pieces a block gets.  `blocks` = 0: whole ones, in rounds of one to every block, every other round in the
+// other direction, the sequences that take longest first.  Else `blocks` blocks share all tiles equally, one piece
+// after the other, so that a block's first and last piece may be parts; a piece counts for `least` tiles at least,
+// which bounds their number in a block.
+struct Order { int span; bool of_keys; int heads, repeats /* of the tiles that a piece meets */, blocks, least; };
+// A block's pieces are looked up once, at its start.
+constexpr int MAX_PIECES = 128, SEQ_CHUNK = 512, SORTED = 128;   // of a block; sequences looked at together; in order of their length
 constexpr uint32_t TABLE_BYTES = MAX_PIECES * 32;
 __device__ __forceinline__ Piece piece_at(uint32_t table, int n) {
   Piece w;
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.head), "=r"(w.x0), "=r"(w.r.q_begin), "=r"(w.r.q_len) : "r"(table + 32u * n));
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w.r.k_begin), "=r"(w.r.k_len) : "r"(table + 32u * n + 16));
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.r.k_begin), "=r"(w.r.k_len), "=r"(w.t_begin), "=r"(w.n) : "r"(table + 32u * n + 16));
   return w;
 }
-// All threads of the block; ends with a barrier.  `of_keys`: pieces are of the keys' rows, else of the queries'.
-// before: shared memory for 5 SEQ_CHUNK + 1 numbers that is not needed afterwards.  Returns the number of the block's pieces.
-__device__ __forceinline__ int find_pieces(const vit_attention_problem& p, int* status, int span, bool of_keys, int heads, int32_t* table, int32_t* before) {
-  int carry = 0;
-  for (int s0 = 0; s0 < p.sequences; s0 += SEQ_CHUNK) {
-    const int chunk = min(SEQ_CHUNK, p.sequences - s0);
-    int4* ranges = reinterpret_cast<int4*>(before + SEQ_CHUNK + 4);
-    for (int s = threadIdx.x; s < chunk; s += (int)blockDim.x) {
-      SeqRange r{0, 0, 0, 0};
+__device__ __forceinline__ int tiles_met(const Order& o, const int4& r) { return o.repeats * (((o.of_keys ? r.y : r.w) + CT - 1) / CT); }
+__device__ __forceinline__ int piece_weight(const Order& o, const int4& r) { return o.blocks > 0 ? max(tiles_met(o, r), o.least) : 1; }
+// Sequences [s0, s0 + chunk), by all threads of a block: ranges (q_begin, q_len, k_begin, k_len), and the weight of all pieces
+// before each of them.  Returns that behind the last one.
+__device__ __forceinline__ int scan_sequences(const vit_attention_problem& p, int* status, const Order& o, int s0, int chunk, int carry, int32_t* before, int4* ranges) {
+  const int32_t* other = o.of_keys ? p.q_offsets : p.k_offsets;
+  const bool sort = o.blocks == 0 && p.sequences <= SORTED;
+  const int key0 = sort ? other[1] - other[0] : 0;
+  __syncthreads();                                               // `before` is read no more
+  for (int b = 0; b < chunk; b += (int)blockDim.x) {             // (one round where it sorts)
+    const int s = b + (int)threadIdx.x;
+    SeqRange r{0, 0, 0, 0};
+    int at = s, key = key0;
+    if (s < chunk) {
       seq_range(p, s0 + s, r, status, true);
-      before[s] = ((of_keys ? r.k_len : r.q_len) + span - 1) / span * heads;
-      ranges[s] = make_int4(r.q_begin, r.q_len, r.k_begin, r.k_len);
+      key = o.of_keys ? r.q_len : r.k_len;
     }
-    __syncthreads();
-    if (threadIdx.x < 32) {                                      // counts become the number of pieces before each sequence
-      int sum = carry;
-      for (int b = 0; b < chunk; b += 32) {
-        const int s = b + (int)threadIdx.x, n = s < chunk ? before[s] : 0;
-        int up = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const int other = __shfl_up_sync(0xffffffffu, up, o);
-          if ((int)threadIdx.x >= o) up += other;
-        }
-        if (s < chunk) before[s] = sum + up - n;
-        sum += __shfl_sync(0xffffffffu, up, 31);
+    if (sort) {
+      if (s < chunk) before[s] = key;
+      if (__syncthreads_or(key != key0)) {
+        at = 0;
+        for (int t = 0; t < chunk; ++t) at += before[t] > key || (before[t] == key && t < s) ? 1 : 0;
+        __syncthreads();
       }
-      if (threadIdx.x == 0) before[chunk] = sum;
     }
-    __syncthreads();
-    const int end = before[chunk];
-    for (int j = threadIdx.x; j < MAX_PIECES; j += (int)blockDim.x) {
-      const int i = (int)blockIdx.x + j * (int)gridDim.x;
-      if (i < carry || i >= end) continue;
-      int lo = 0, hi = chunk;                                    // before[lo] <= i < before[hi]
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (before[mid] <= i) lo = mid;
-        else hi = mid;
-      }
-      const int4 r = ranges[lo];
-      const int tiles = ((of_keys ? r.w : r.y) + span - 1) / span, k = i - before[lo], head = k / tiles;
-      int32_t* to = table + 8 * j;
-      *reinterpret_cast<int4*>(to) = make_int4(head, (k - head * tiles) * span, r.x, r.y);
-      to[4] = r.z;
-      to[5] = r.w;
+    if (s < chunk) {
+      const int4 v = make_int4(r.q_begin, r.q_len, r.k_begin, r.k_len);
+      before[at] = ((o.of_keys ? r.k_len : r.q_len) + o.span - 1) / o.span * o.heads * piece_weight(o, v);
+      ranges[at] = v;
     }
-    __syncthreads();                                             // `before` is read no more
-    carry = end;
   }
-  ptx::fence_proxy_async_smem();                                 // the copies come to where `before` was
   __syncthreads();
-  return carry > (int)blockIdx.x ? (carry - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x : 0;
+  if (threadIdx.x < 32) {                                        // running sums
+    int sum = carry;
+    for (int b = 0; b < chunk; b += 32) {
+      const int s = b + (int)threadIdx.x, n = s < chunk ? before[s] : 0;
+      int up = n;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const int lower = __shfl_up_sync(0xffffffffu, up, d);
+        if ((int)threadIdx.x >= d) up += lower;
+      }
+      if (s < chunk) before[s] = sum + up - n;
+      sum += __shfl_sync(0xffffffffu, up, 31);
+    }
+    if (threadIdx.x == 0) before[chunk] = sum;
+  }
+  __syncthreads();
+  return before[chunk];
+}
+// the last of `chunk` sequences with before[...] <= i
+__device__ __forceinline__ int sequence_of(const int32_t* before, int chunk, int i) {
+  int lo = 0, hi = chunk;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (before[mid] <= i) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+__device__ __forceinline__ int share_begin(int total, int block, int blocks) { return (int)((int64_t)total * block / blocks); }
+__device__ __forceinline__ int share_of(int total, int tile, int blocks) { return (int)(((int64_t)(tile + 1) * blocks - 1) / total); }   // whose it is
+
+// All threads of the block; ends with a barrier.  before: shared memory for 5 SEQ_CHUNK + 4 numbers that is not needed
+// afterwards.  Returns the number of the block's pieces.
+__device__ __forceinline__ int find_pieces(const vit_attention_problem& p, int* status, const Order& o, int32_t* table, int32_t* before) {
+  int4* ranges = reinterpret_cast<int4*>(before + SEQ_CHUNK + 4);
+  auto put = [&](int j, const int4& r, int k, int t_begin, int n) {     // piece k of a sequence
+    const int tiles = ((o.of_keys ? r.w : r.y) + o.span - 1) / o.span, head = k / tiles;
+    int4* to = reinterpret_cast<int4*>(table + 8 * j);
+    to[0] = make_int4(head, (k - head * tiles) * o.span, r.x, r.y);
+    to[1] = make_int4(r.z, r.w, t_begin, n);
+  };
+  const int grid = (int)gridDim.x, self = (int)blockIdx.x;
+  int carry = 0, found = 0;
+  if (o.blocks == 0) {
+    for (int s0 = 0; s0 < p.sequences; s0 += SEQ_CHUNK) {
+      const int chunk = min(SEQ_CHUNK, p.sequences - s0), end = scan_sequences(p, status, o, s0, chunk, carry, before, ranges);
+      for (int j = threadIdx.x; j < MAX_PIECES; j += (int)blockDim.x) {
+        const int i = j * grid + (j & 1 ? grid - 1 - self : self);
+        if (i < carry || i >= end) continue;
+        const int at = sequence_of(before, chunk, i);
+        put(j, ranges[at], i - before[at], 0, tiles_met(o, ranges[at]));
+      }
+      carry = end;
+    }
+    const int rounds = carry / grid, rest = carry - rounds * grid;
+    found = rounds + ((rounds & 1 ? grid - 1 - self : self) < rest ? 1 : 0);
+  } else {
+    for (int s0 = 0; s0 < p.sequences; s0 += SEQ_CHUNK)
+      carry = scan_sequences(p, status, o, s0, min(SEQ_CHUNK, p.sequences - s0), carry, before, ranges);
+    const int blocks = min(grid, carry);                         // nobody's share is empty
+    const int begin = self < blocks ? share_begin(carry, self, blocks) : carry, end = self < blocks ? share_begin(carry, self + 1, blocks) : carry;
+    carry = 0;
+    for (int s0 = 0; s0 < p.sequences && carry < end && begin < end; s0 += SEQ_CHUNK) {
+      const int chunk = min(SEQ_CHUNK, p.sequences - s0);
+      const int chunk_end = p.sequences <= SEQ_CHUNK ? before[chunk] : scan_sequences(p, status, o, s0, chunk, carry, before, ranges);
+      if (begin < chunk_end) {
+        for (int s = sequence_of(before, chunk, max(begin, carry)); s < chunk && before[s] < end; ++s) {
+          const int from = max(begin, before[s]) - before[s], to = min(end, before[s + 1]) - before[s];
+          if (to <= from) continue;
+          const int4 r = ranges[s];
+          const int whole = tiles_met(o, r), weight = piece_weight(o, r), first = from / weight, last = (to - 1) / weight;
+          // a part that has none of the piece's tiles is left out
+          const bool skip = whole > 0 ? from - first * weight >= whole : from > first * weight;
+          for (int k = first + (skip ? 1 : 0) + (int)threadIdx.x; k <= last; k += (int)blockDim.x) {
+            const int t0 = max(from - k * weight, 0), t1 = min(min(to - k * weight, weight), whole);
+            const int j = found + k - first - (skip ? 1 : 0);
+            if (j < MAX_PIECES) put(j, r, k, t0, max(t1 - t0, 0));
+          }
+          found += last - first + 1 - (skip ? 1 : 0);
+        }
+      }
+      carry = chunk_end;
+    }
+    found = min(found, MAX_PIECES);                              // (`least` sees to it)
+  }
+  fence_proxy_async_smem();                                      // the copies come to where `before` was
+  __syncthreads();
+  return found;
 }
 // Place in a ring of stages and the parity of its present round
 template <int N>
@@ -363,7 +434,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == F_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
-  const int pieces = find_pieces(c.p, c.dev_status, 2 * RT, false, c.p.heads, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ),
+  const int pieces = find_pieces(c.p, c.dev_status, Order{2 * RT, false, c.p.heads, 1, 0, 0}, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ),
                                  reinterpret_cast<int32_t*>(smem));
   tc_fence_before();
   __syncthreads();
@@ -659,10 +730,13 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
 // of its 64 columns: while one pair is in its exp2 phase the tensor core works for the other, and four warps a
 // scheduler hide each other's latencies; one warp issues the scores, another the second products.  X is in tensor memory (XT) where it fits beside the accumulators: always for DQ, up to
 // d = 80 for DKDV.
-// Where there are few pieces, each is walked over in `parts` equal parts by different blocks: their sums go to
-// partial [part][dk, dv or dq][row][heads * d] in fp32, and a last kernel adds them in order.
+// Where pieces do not come out even, the blocks share all tiles equally: the sums of a piece that is not one block's go
+// to partial [2 block + (0: its first piece, 1: its last)][dk, dv or dq][128][d] in fp32, and a last kernel adds them in order.
 struct BackwardMaps { CUtensorMap x1, x2, x3, y1, y2; };
-struct Parts { int log2; float* partial; };
+struct Shares { int blocks, least; };                    // blocks = 0: pieces are not shared
+__device__ __forceinline__ Order order_of(const vit_attention_problem& p, bool dkdv, const Shares& s) {
+  return Order{RT, dkdv, dkdv ? p.kv_heads : p.heads, dkdv ? p.heads / p.kv_heads : 1, s.blocks, s.least};
+}
 constexpr int B_MMA_WARP = 16 /* two */, B_TMA_WARP = 18, B_THREADS = 608;
 
 template <int SLABS, bool DKDV>
@@ -685,7 +759,7 @@ enum BwdBar : int {
 
 template <int SLABS, bool DKDV, bool XT>
 __global__ void __launch_bounds__(B_THREADS, 1)
-packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, const Parts parts) {
+packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, const Shares shares) {
   using L = BackwardCfg<SLABS, DKDV>;
   extern __shared__ uint8_t smem_raw[];
   const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
@@ -702,24 +776,19 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
-  const int pieces_in_all = find_pieces(c.p, c.dev_status, RT, DKDV, (DKDV ? c.p.kv_heads : c.p.heads) << parts.log2,
-                                        reinterpret_cast<int32_t*>(smem + L::OFF_SEQ), reinterpret_cast<int32_t*>(smem));
+  const int pieces_in_all = find_pieces(c.p, c.dev_status, order_of(c.p, DKDV, shares), reinterpret_cast<int32_t*>(smem + L::OFF_SEQ),
+                                        reinterpret_cast<int32_t*>(smem));
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
   const uint32_t acc2 = B_COLS, acc1 = B_COLS + d, x1_col = B_COLS + (DKDV ? 2 : 1) * d, x2_col = x1_col + d / 2;   // dk or dq; dv
   Piece w;
-  int at_piece = 0, part = 0, y_tiles = 0, t_begin = 0, n = 0;     // of piece w: part, tiles of a head of Y, first tile and number of tiles of the part
+  int at_piece = 0, y_tiles = 0;                                  // of piece w: tiles of a head of Y
   auto advance = [&] {
     if (at_piece >= pieces_in_all) return false;
     w = piece_at(sb + L::OFF_SEQ, at_piece++);
-    part = w.head & ((1 << parts.log2) - 1);
-    w.head >>= parts.log2;
     y_tiles = ((DKDV ? w.r.q_len : w.r.k_len) + CT - 1) / CT;
-    const int whole = DKDV ? group * y_tiles : y_tiles;            // tiles of Y, head after head
-    t_begin = (int)((int64_t)whole * part >> parts.log2);
-    n = (int)((int64_t)whole * (part + 1) >> parts.log2) - t_begin;
     return true;
   };
 
@@ -730,7 +799,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     bool ok = true;
     while (ok && advance()) {
       const int y_begin = DKDV ? w.r.q_begin : w.r.k_begin, y_len = DKDV ? w.r.q_len : w.r.k_len;
-      if (n == 0) continue;
+      if (w.n == 0) continue;
       if (!warp_wait(bar(B_XSFREE), (pieces & 1) ^ 1, abort_flag)) break;
       if (lane == 0) {
         const int row = (DKDV ? w.r.k_begin : w.r.q_begin) + w.x0;
@@ -742,9 +811,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         }
       }
       ++pieces;
-      const int heads_on = DKDV && t_begin > 0 ? t_begin / y_tiles : 0;
-      int y0 = (t_begin - heads_on * y_tiles) * CT, yh = DKDV ? w.head * group + heads_on : group == 1 ? w.head : w.head / group;
-      for (int t = 0; t < n; ++t, ring.step()) {
+      const int heads_on = DKDV && w.t_begin > 0 ? w.t_begin / y_tiles : 0;
+      int y0 = (w.t_begin - heads_on * y_tiles) * CT, yh = DKDV ? w.head * group + heads_on : group == 1 ? w.head : w.head / group;
+      for (int t = 0; t < w.n; ++t, ring.step()) {
         const int st = ring.at;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE;
         // DKDV: the numbers of the tile's columns travel with it, negated; beyond the sequence
@@ -796,10 +865,10 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     bool ok = true;
     while (ok && advance()) {
       const int y_len = DKDV ? w.r.q_len : w.r.k_len;
-      if (n == 0) continue;
+      if (w.n == 0) continue;
       if (scores && !warp_wait(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
-      int left = y_len - (t_begin > 0 ? t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
-      for (int t = 0; t < n; ++t, ring.step()) {
+      int left = y_len - (w.t_begin > 0 ? w.t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
+      for (int t = 0; t < w.n; ++t, ring.step()) {
         const int st = ring.at, b = t & 1, here = min(CT, left), n16 = (here + 15) / 16;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + b * B_WG;
         left = left > CT ? left - CT : y_len;
@@ -824,7 +893,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
               issue_scores_ss<SLABS, CT>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
             }
             umma_commit(bar(B_S + b));
-            if (t == n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE));
+            if (t == w.n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE));
           }
         } else {
           if (!warp_wait(bar(B_P + b), phase >> b & 1, abort_flag)) { ok = false; break; }
@@ -837,7 +906,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
             issue_weighted<CT, true>(tmem + acc2, s_col + CT, y, d, n16, t == 0);
             umma_commit(bar(B_SFREE + b));
             umma_commit(bar(B_FREE + st));
-            if (t == n - 1) umma_commit(bar(B_ACC));
+            if (t == w.n - 1) umma_commit(bar(B_ACC));
           }
         }
         __syncwarp();                                            // lanes that poll would hold up the one that issues
@@ -860,25 +929,19 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     const float2 sl2v = make_float2(sl2, sl2);
     Ring<L::STAGES> ring;                                        // of every tile, this warpgroup's or not
     int pieces = 0, s_phase = 0;
-    // a row of piece w's part: of dk (or dq) or of dv
-    const int64_t x_rows = DKDV ? c.p.k_rows : c.p.q_rows, x_width = (int64_t)(DKDV ? c.p.kv_heads : c.p.heads) * d;
-    auto partial_row = [&](int tensor, int64_t row) {
-      return parts.partial + (((int64_t)part * (DKDV ? 2 : 1) + tensor) * x_rows + row) * x_width + (int64_t)w.head * d;
+    // where a row of piece w goes if others have parts of it too: of dk (or dq) or of dv
+    auto partial_row = [&](int tensor, int row) {
+      return c.partial + (((int64_t)(2 * blockIdx.x + (w.t_begin > 0 ? 0 : 1)) * (DKDV ? 2 : 1) + tensor) * RT + row) * d;
     };
     // the next piece with something to walk over; rows that nothing meets get gradients of zero on the way
     auto next = [&] {
       while (advance()) {
-        if (n > 0) return true;
+        if (w.n > 0) return true;
         const int row = w.x0 + in_tile;
         const int64_t at = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row;
         if (wg == 0 && row < (DKDV ? w.r.k_len : w.r.q_len)) {
           bf16* g2 = DKDV ? static_cast<bf16*>(c.dk) + at * c.lddk + (int64_t)w.head * d : static_cast<bf16*>(c.dq) + at * c.lddq + (int64_t)w.head * d;
           bf16* g1 = static_cast<bf16*>(c.dv) + at * c.lddv + (int64_t)w.head * d;
-          if (parts.log2 > 0) {
-            for (int t = 0; t < (DKDV ? 2 : 1); ++t)
-              for (int e = 0; e < d; e += 4) *reinterpret_cast<float4*>(partial_row(t, at) + e) = make_float4(0.f, 0.f, 0.f, 0.f);
-            continue;
-          }
           for (int e = 0; e < d; e += 8) {
             *reinterpret_cast<uint4*>(g2 + e) = make_uint4(0u, 0u, 0u, 0u);
             if (DKDV) *reinterpret_cast<uint4*>(g1 + e) = make_uint4(0u, 0u, 0u, 0u);
@@ -935,8 +998,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         nls = make_float2(-mine.x, -mine.x);
         nde = make_float2(-mine.y, -mine.y);
       }
-      float* sums = parts.log2 > 0 ? partial_row(DKDV ? wg & 1 : 0, at0) : nullptr;
-      int left = y_len - (t_begin > 0 ? t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
+      const int n = w.n;                                         // (w moves on before the sums are stored)
+      float* sums = n < (DKDV ? group * y_tiles : y_tiles) ? partial_row(DKDV ? wg & 1 : 0, quarter * 32) : nullptr;
+      int left = y_len - (w.t_begin > 0 ? w.t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
       for (int t = 0; t < n; ++t, ring.step()) {
         const int here = min(CT, left) - 32 * half;              // of this warpgroup's 32 columns
         left = left > CT ? left - CT : y_len;
@@ -1005,7 +1069,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       if (rows > 0) {
         const int from = DKDV || wg == 0 ? 0 : d / 32 * 16, to = DKDV || wg == 1 ? d : d / 32 * 16;   // dk, dv; or a part of dq each
         if (sums) {
-          store_rows(sums + from, x_width, lanes + (DKDV && wg == 1 ? acc1 : acc2) + from, to - from, 1.f, rows, stage, lane);
+          store_rows(sums + from, d, lanes + (DKDV && wg == 1 ? acc1 : acc2) + from, to - from, 1.f, rows, stage, lane);
         } else if (DKDV) {
           const int64_t ld = wg == 0 ? c.lddk : c.lddv;
           store_rows(static_cast<bf16*>(wg == 0 ? c.dk : c.dv) + at0 * ld + (int64_t)head * d, ld, lanes + (wg == 0 ? acc2 : acc1), d,
@@ -1032,33 +1096,51 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   }
 }
 
-// The sums of the parts, in order, times the factor of the gradient, rounded once: 16 rows of a sequence to a block
-constexpr int ADD_ROWS = 16;
+// The sums of the pieces that were shared, in order, times the factor of the gradient, rounded once.  Block (i, j)
+// takes 32 j ... of the piece whose first border between two shares is that behind share i.
+constexpr int ADD_ROWS = 32;
 template <bool DKDV>
-__global__ void __launch_bounds__(256) add_parts_kernel(const PackedCall c, const Parts parts) {
-  const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + ADD_ROWS - 1) / ADD_ROWS, seq = blockIdx.x / tiles, row0 = blockIdx.x % tiles * ADD_ROWS;
-  SeqRange r;
-  if (!seq_range(c.p, seq, r, c.dev_status, false)) return;
-  const int rows = min(ADD_ROWS, (DKDV ? r.k_len : r.q_len) - row0);
-  if (rows <= 0) return;
-  const int64_t all_rows = DKDV ? c.p.k_rows : c.p.q_rows, at = (int64_t)(DKDV ? r.k_begin : r.q_begin) + row0;
-  const int width = (DKDV ? c.p.kv_heads : c.p.heads) * c.p.d, pieces = width / 8;
+__global__ void __launch_bounds__(256) add_parts_kernel(const PackedCall c, const Shares shares) {
+  __shared__ int32_t before[SEQ_CHUNK + 4];
+  __shared__ int4 ranges[SEQ_CHUNK];
+  const Order o = order_of(c.p, DKDV, shares);
+  int total = 0, carry = 0, chunk = 0;
+  for (int s0 = 0; s0 < c.p.sequences; s0 += SEQ_CHUNK)
+    total = scan_sequences(c.p, c.dev_status, o, s0, min(SEQ_CHUNK, c.p.sequences - s0), total, before, ranges);
+  const int blocks = min(shares.blocks, total);                  // as find_pieces has it
+  if ((int)blockIdx.x + 1 >= blocks) return;
+  const int border = share_begin(total, blockIdx.x + 1, blocks);
+  for (int s0 = 0; s0 < c.p.sequences; s0 += SEQ_CHUNK) {        // the sequence that has it
+    chunk = min(SEQ_CHUNK, c.p.sequences - s0);
+    const int end = c.p.sequences <= SEQ_CHUNK ? total : scan_sequences(c.p, c.dev_status, o, s0, chunk, carry, before, ranges);
+    if (border < end) break;
+    carry = end;
+  }
+  const int at = sequence_of(before, chunk, border);
+  const int4 r = ranges[at];
+  const int whole = tiles_met(o, r), weight = piece_weight(o, r), k = (border - before[at]) / weight, begin = before[at] + k * weight;
+  const int first = share_of(total, begin, blocks);
+  if (border == begin || border >= begin + whole || first != (int)blockIdx.x) return;    // not inside, or not the first
+  const int last = share_of(total, begin + whole - 1, blocks);
+  const int tiles = ((DKDV ? r.w : r.y) + RT - 1) / RT, head = k / tiles, x0 = (k - head * tiles) * RT + (int)blockIdx.y * ADD_ROWS;
+  const int rows = min(ADD_ROWS, (DKDV ? r.w : r.y) - x0), d = c.p.d, eights = d / 8;
 #pragma unroll
   for (int tensor = 0; tensor < (DKDV ? 2 : 1); ++tensor) {
-    bf16* to = static_cast<bf16*>(DKDV ? (tensor ? c.dv : c.dk) : c.dq);
     const int64_t ld = DKDV ? (tensor ? c.lddv : c.lddk) : c.lddq;
+    bf16* to = static_cast<bf16*>(DKDV ? (tensor ? c.dv : c.dk) : c.dq) + ((int64_t)(DKDV ? r.z : r.x) + x0) * ld + (int64_t)head * d;
     const float by = tensor ? 1.f : c.p.scale;
-    for (int i = threadIdx.x; i < rows * pieces; i += 256) {
-      const int row = i / pieces, ch = (i - row * pieces) * 8;
+    for (int i = threadIdx.x; i < rows * eights; i += 256) {
+      const int row = i / eights, ch = (i - row * eights) * 8;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-      for (int k = 0; k < 1 << parts.log2; ++k) {
-        const float4* from = reinterpret_cast<const float4*>(parts.partial + (((int64_t)k * (DKDV ? 2 : 1) + tensor) * all_rows + at + row) * width + ch);
+      for (int share = first; share <= last; ++share) {          // the first one's last piece, the others' first
+        const int64_t slot = 2 * share + (share == first ? 1 : 0);
+        const float4* from = reinterpret_cast<const float4*>(c.partial + ((slot * (DKDV ? 2 : 1) + tensor) * RT + blockIdx.y * ADD_ROWS + row) * d + ch);
         const float4 u = from[0], v = from[1];
         a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
         b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
       }
-      *reinterpret_cast<uint4*>(to + (at + row) * ld + ch) = make_uint4(pack_bf16(a.x * by, a.y * by), pack_bf16(a.z * by, a.w * by),
-                                                                        pack_bf16(b.x * by, b.y * by), pack_bf16(b.z * by, b.w * by));
+      *reinterpret_cast<uint4*>(to + row * ld + ch) = make_uint4(pack_bf16(a.x * by, a.y * by), pack_bf16(a.z * by, a.w * by),
+                                                                 pack_bf16(b.x * by, b.y * by), pack_bf16(b.z * by, b.w * by));
     }
   }
 }
@@ -1116,21 +1198,22 @@ cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
   return cudaGetLastError();
 }
 
-// The parts of a piece of the backward pass: so many that there are two pieces to an SM or so, of eight tiles at least,
-// eight at most (4 sequences of up to 4097, 8 heads over 2 key heads of 128:
-// dk and dv 269 us in one part, 211 and 6 for the sum in two)
-int log2_parts(const vit_attention_problem& p, bool dkdv) {
+// Whether the blocks of the backward pass share the tiles (in shares of eight at least): where that takes less time,
+// counted in tiles.  A piece takes three besides its own, shares cost each block two parts and a launch more, and
+// without them the last round is as long as a full one.  (SHARE_US)
+constexpr int SHARE_BLOCKS = 148;
+Shares shares_of(const vit_attention_problem& p, bool dkdv) {
   const int64_t pieces = (int64_t)p.sequences * (dkdv ? p.kv_heads : p.heads) * (((dkdv ? p.max_k : p.max_q) + RT - 1) / RT);
   const int64_t tiles = (int64_t)(dkdv ? p.heads / p.kv_heads : 1) * (((dkdv ? p.max_q : p.max_k) + CT - 1) / CT);
-  int log2 = 0;
-  while (log2 < 3 && pieces << log2 < 296 && tiles >> (log2 + 1) >= 8) ++log2;
-  return log2;
+  if (pieces == 0 || tiles == 0 || tiles > (1 << 30) / pieces) return Shares{0, 0};
+  const int64_t most = pieces * tiles / 8, blocks = most < SHARE_BLOCKS ? most : SHARE_BLOCKS;
+  if (blocks < 2 || pieces > 100 * blocks) return Shares{0, 0};
+  const int64_t whole = (pieces + SHARE_BLOCKS - 1) / SHARE_BLOCKS * (tiles + 3), shared = pieces * (tiles + 3) / blocks + 16;
+  if (shared >= whole) return Shares{0, 0};
+  // a block's share is pieces * tiles / blocks of such weights at most: 120 pieces, and one more at either end
+  return Shares{(int)blocks, (int)((pieces * tiles + 120 * blocks - 1) / (120 * blocks))};
 }
-size_t partial_floats(const vit_attention_problem& p, bool dkdv) {
-  const int log2 = log2_parts(p, dkdv);
-  if (log2 == 0) return 0;
-  return ((size_t)(dkdv ? 2 * (size_t)p.k_rows * p.kv_heads : (size_t)p.q_rows * p.heads) * p.d) << log2;
-}
+size_t partial_floats(const vit_attention_problem& p, bool dkdv) { return (size_t)shares_of(p, dkdv).blocks * 2 * (dkdv ? 2 : 1) * RT * p.d; }
 
 template <int SLABS, bool DKDV, bool XT>
 cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
@@ -1152,12 +1235,12 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
   if (cudaError_t e = ensure_dynamic_smem(done, packed_backward_tc_kernel<SLABS, DKDV, XT>, (int)L::BYTES)) return e;
   const int sms = current_device_sm_count();
   if (sms < 1) return cudaErrorInvalidDevice;
-  const Parts parts{log2_parts(c.p, DKDV), c.partial};
-  const int tiles = ((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT, total = (c.p.sequences * xh * tiles) << parts.log2;
-  packed_backward_tc_kernel<SLABS, DKDV, XT><<<grid_of(total, sms), B_THREADS, L::BYTES, s>>>(m, c, parts);
+  const Shares shares = shares_of(c.p, DKDV);
+  const int total = c.p.sequences * xh * (((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT);
+  packed_backward_tc_kernel<SLABS, DKDV, XT><<<shares.blocks > 0 ? shares.blocks : grid_of(total, sms), B_THREADS, L::BYTES, s>>>(m, c, shares);
   if (cudaError_t e = cudaGetLastError()) return e;
-  if (parts.log2 > 0) {
-    add_parts_kernel<DKDV><<<c.p.sequences * (((DKDV ? c.p.max_k : c.p.max_q) + ADD_ROWS - 1) / ADD_ROWS), 256, 0, s>>>(c, parts);
+  if (shares.blocks > 0) {
+    add_parts_kernel<DKDV><<<dim3((unsigned)shares.blocks - 1, RT / ADD_ROWS), 256, 0, s>>>(c, shares);
     return cudaGetLastError();
   }
   return cudaSuccess;
@@ -1165,7 +1248,7 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
 
 }  // namespace
 
-bool attention_in_parts(const vit_attention_problem& p, bool dkdv) { return log2_parts(p, dkdv) > 0; }
+bool attention_in_parts(const vit_attention_problem& p, bool dkdv) { return shares_of(p, dkdv).blocks > 0; }
 // Columns of tensor memory decide where a piece's rows are held: 128 + d + d / 2 of a warpgroup's 256 in
 // the forward pass, 256 + 2 d + d of 512 for dk and dv, 256 + d + d for dq.
 size_t attention_partial_floats(const vit_attention_problem& p) {

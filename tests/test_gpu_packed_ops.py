@@ -525,7 +525,6 @@ def test_packed_attention_bad_offsets_where_long_walks_are_shared(ctx, dtype):
     vit, m = ctx
     p = Packed(vit, [1300, 600, 530], [1300, 600, 530], 8, 2, 64, dtype, trail=8)
     good = p.forward(m)
-    good_grads = p.backward(m, *good)
     m.check()
     p.k_off[3] = p.k_rows + 1
     out, lse = p.forward(m)
@@ -534,8 +533,11 @@ def test_packed_attention_bad_offsets_where_long_walks_are_shared(ctx, dtype):
         m.check()
     assert e.value.status == vit.VIT_ERR_OFFSETS
     assert torch.equal(out[:1900], good[0][:1900]) and torch.equal(lse[:, :1900], good[1][:, :1900])
-    assert torch.equal(dq[:1900], good_grads[0][:1900]) and torch.equal(dkv[:1900], good_grads[1][:1900])
-    assert (out[1900:] == 33).all() and (lse[:, 1900:] == 33).all() and (dq[1900:] == 33).all() and (dkv[1900:] == 33).all()
+    assert (out[1900:] == 33).all() and (lse[:, 1900:] == 33).all()
+    # how the walks are cut into shares follows the lengths: the others' gradients are the definition's, and those of
+    # this sequence are left alone
+    p.ql, p.kl, p.covered_q, p.covered_k = p.ql[:2], p.kl[:2], slice(0, 1900), slice(0, 1900)
+    p.check_backward(*good, dq, dkv)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
