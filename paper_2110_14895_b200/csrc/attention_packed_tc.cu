@@ -660,24 +660,30 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
           tmem_st16(taddr, pk);
           if (here > 64) tmem_ld32(taddr + 64, x[0]);
           exp_32(x[1], sl2v, nmv, l2, pk);
+          if (here > 64) tmem_ld_wait_for(x[0]);
           tmem_st16(taddr + 16, pk);
-          tmem_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar(F_P + 2 * wg));
           if (here > 64) {
-            tmem_ld_wait_for(x[0]);
             tmem_ld32(taddr + 96, x[1]);
             if (here < 96) mask_32(x[0], here - 64);
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(F_P + 2 * wg));
             exp_32(x[0], sl2v, nmv, l2, pk);
             tmem_ld_wait_for(x[1]);
             tmem_st16(taddr + 64, pk);
             if (here < RT) mask_32(x[1], here - 96);
             exp_32(x[1], sl2v, nmv, l2, pk);
+            if (pair && lane == 0) mbar_arrive(bar(F_TURN + (warp ^ 4)));
             tmem_st16(taddr + 80, pk);
             tmem_st_wait();
+          } else {
+            tmem_st_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(F_P + 2 * wg));
+            if (pair && lane == 0) mbar_arrive(bar(F_TURN + (warp ^ 4)));
           }
-          if (pair && lane == 0) mbar_arrive(bar(F_TURN + (warp ^ 4)));
           l2[0] = __fadd2_rn(l2[0], l2[1]);
           l += l2[0].x + l2[0].y;
           tc_fence_before();
