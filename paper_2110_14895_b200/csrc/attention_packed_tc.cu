@@ -672,10 +672,12 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
             exp_32(x[0], sl2v, nmv, l2, pk);
             tmem_ld_wait_for(x[1]);
             tmem_st16(taddr + 64, pk);
-            if (here < RT) mask_32(x[1], here - 96);
-            exp_32(x[1], sl2v, nmv, l2, pk);
+            if (here > 96) {
+              if (here < RT) mask_32(x[1], here - 96);
+              exp_32(x[1], sl2v, nmv, l2, pk);
+            }
             if (pair && lane == 0) mbar_arrive(bar(F_TURN + (warp ^ 4)));
-            tmem_st16(taddr + 80, pk);
+            if (here > 96) tmem_st16(taddr + 80, pk);
             tmem_st_wait();
           } else {
             tmem_st_wait();
