@@ -54,6 +54,7 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm,
       "l"(reinterpret_cast<uint64_t>(tm)), "r"(c), "r"(head), "r"(row), "r"(bar)
       : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* tm) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tm)) : "memory"); }
 // a bounded wait of a whole warp: all lanes leave with the same answer.  Only the first look is in line: the
 // kernels wait in many places, and their code has to fit the instruction cache.
 __device__ __noinline__ bool wait_on(uint32_t bar, int parity, volatile int* abort_flag, long long limit) {
@@ -167,15 +168,19 @@ __device__ __forceinline__ void store_rows(bf16* dst, int64_t ld, uint32_t taddr
     }
     __syncwarp();
     const int q = lane & 3;
+    uint4 v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = 8 * e + (lane >> 2);
-      uint4 v;
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[e].x), "=r"(v[e].y), "=r"(v[e].z), "=r"(v[e].w)
                    : "r"(stage + (uint32_t)(r * 64 + ((q ^ ((r >> 1) & 3)) << 4))));
-      if (r < rows && c + 8 * q < cols) *reinterpret_cast<uint4*>(dst + r * ld + c + 8 * q) = v;
     }
     __syncwarp();
+    if (c + 8 * q < cols) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (8 * e + (lane >> 2) < rows) *reinterpret_cast<uint4*>(dst + (8 * e + (lane >> 2)) * ld + c + 8 * q) = v[e];
+    }
   }
 }
 
@@ -208,12 +213,12 @@ __device__ __forceinline__ void store_rows(float* dst, int64_t ld, uint32_t tadd
 // A piece of work: rows [x0, x0 + span) of one head of one sequence against tiles [t_begin, t_begin + n) of what they meet.
 struct Piece { int head, x0; SeqRange r; int t_begin, n; };
 // Which pieces a block gets.  `blocks` = 0: whole ones, in rounds of one to every block, every other round in the
-// other direction, the sequences that take longest first.  Else `blocks` blocks share all tiles equally, one piece
+// other direction (128 images of 257 rows: a block would get all of one kind, 256 rows or one).  Else `blocks` blocks share all tiles equally, one piece
 // after the other, so that a block's first and last piece may be parts; a piece counts for `least` tiles at least,
 // which bounds their number in a block.
 struct Order { int span; bool of_keys; int heads, repeats /* of the tiles that a piece meets */, blocks, least; };
 // A block's pieces are looked up once, at its start.
-constexpr int MAX_PIECES = 128, SEQ_CHUNK = 512, SORTED = 128;   // of a block; sequences looked at together; in order of their length
+constexpr int MAX_PIECES = 128, SEQ_CHUNK = 512, SCAN_INTS = SEQ_CHUNK + 4 + SEQ_CHUNK / 32;   // of a block; sequences looked at together; scan_sequences' `before`
 constexpr uint32_t TABLE_BYTES = MAX_PIECES * 32;
 __device__ __forceinline__ Piece piece_at(uint32_t table, int n) {
   Piece w;
@@ -226,50 +231,39 @@ __device__ __forceinline__ int piece_weight(const Order& o, const int4& r) { ret
 // Sequences [s0, s0 + chunk), by all threads of a block: ranges (q_begin, q_len, k_begin, k_len), and the weight of all pieces
 // before each of them.  Returns that behind the last one.
 __device__ __forceinline__ int scan_sequences(const vit_attention_problem& p, int* status, const Order& o, int s0, int chunk, int carry, int32_t* before, int4* ranges) {
-  const int32_t* other = o.of_keys ? p.q_offsets : p.k_offsets;
-  const bool sort = o.blocks == 0 && p.sequences <= SORTED;
-  const int key0 = sort ? other[1] - other[0] : 0;
   __syncthreads();                                               // `before` is read no more
-  for (int b = 0; b < chunk; b += (int)blockDim.x) {             // (one round where it sorts)
-    const int s = b + (int)threadIdx.x;
+  const int warps = (int)blockDim.x / 32, warp = (int)threadIdx.x / 32, lane = (int)threadIdx.x & 31;
+  for (int b = warp * 32; b < chunk; b += warps * 32) {          // running sums of 32 sequences each
+    const int s = b + lane;
     SeqRange r{0, 0, 0, 0};
-    int at = s, key = key0;
-    if (s < chunk) {
-      seq_range(p, s0 + s, r, status, true);
-      key = o.of_keys ? r.q_len : r.k_len;
-    }
-    if (sort) {
-      if (s < chunk) before[s] = key;
-      if (__syncthreads_or(key != key0)) {
-        at = 0;
-        for (int t = 0; t < chunk; ++t) at += before[t] > key || (before[t] == key && t < s) ? 1 : 0;
-        __syncthreads();
-      }
-    }
-    if (s < chunk) {
-      const int4 v = make_int4(r.q_begin, r.q_len, r.k_begin, r.k_len);
-      before[at] = ((o.of_keys ? r.k_len : r.q_len) + o.span - 1) / o.span * o.heads * piece_weight(o, v);
-      ranges[at] = v;
-    }
-  }
-  __syncthreads();
-  if (threadIdx.x < 32) {                                        // running sums
-    int sum = carry;
-    for (int b = 0; b < chunk; b += 32) {
-      const int s = b + (int)threadIdx.x, n = s < chunk ? before[s] : 0;
-      int up = n;
+    if (s < chunk) seq_range(p, s0 + s, r, status, true);
+    const int4 v = make_int4(r.q_begin, r.q_len, r.k_begin, r.k_len);
+    const int n = ((o.of_keys ? r.k_len : r.q_len) + o.span - 1) / o.span * o.heads * piece_weight(o, v);
+    int up = n;
 #pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const int lower = __shfl_up_sync(0xffffffffu, up, d);
-        if ((int)threadIdx.x >= d) up += lower;
-      }
-      if (s < chunk) before[s] = sum + up - n;
-      sum += __shfl_sync(0xffffffffu, up, 31);
+    for (int d = 1; d < 32; d <<= 1) {
+      const int lower = __shfl_up_sync(0xffffffffu, up, d);
+      if (lane >= d) up += lower;
     }
-    if (threadIdx.x == 0) before[chunk] = sum;
+    if (s < chunk) {
+      before[s] = up - n;
+      ranges[s] = v;
+    }
+    if (lane == 31) before[SEQ_CHUNK + 4 + b / 32] = up;
   }
   __syncthreads();
-  return before[chunk];
+  int sum = carry, mine = 0;                                     // and of all of them
+  for (int b = 0; b < chunk; b += 32) {
+    if (b == warp * 32) mine = sum;
+    sum += before[SEQ_CHUNK + 4 + b / 32];
+  }
+  for (int b = warp * 32, at = mine; b < chunk; b += warps * 32) {
+    if (b + lane < chunk) before[b + lane] += at;
+    for (int k = b; k < b + warps * 32 && k < chunk; k += 32) at += before[SEQ_CHUNK + 4 + k / 32];
+  }
+  if (threadIdx.x == 0) before[chunk] = sum;
+  __syncthreads();
+  return sum;
 }
 // the last of `chunk` sequences with before[...] <= i
 __device__ __forceinline__ int sequence_of(const int32_t* before, int chunk, int i) {
@@ -284,10 +278,10 @@ __device__ __forceinline__ int sequence_of(const int32_t* before, int chunk, int
 __device__ __forceinline__ int share_begin(int total, int block, int blocks) { return (int)((int64_t)total * block / blocks); }
 __device__ __forceinline__ int share_of(int total, int tile, int blocks) { return (int)(((int64_t)(tile + 1) * blocks - 1) / total); }   // whose it is
 
-// All threads of the block; ends with a barrier.  before: shared memory for 5 SEQ_CHUNK + 4 numbers that is not needed
+// All threads of the block; ends with a barrier.  before: shared memory for SCAN_INTS + 4 SEQ_CHUNK numbers that is not needed
 // afterwards.  Returns the number of the block's pieces.
 __device__ __forceinline__ int find_pieces(const vit_attention_problem& p, int* status, const Order& o, int32_t* table, int32_t* before) {
-  int4* ranges = reinterpret_cast<int4*>(before + SEQ_CHUNK + 4);
+  int4* ranges = reinterpret_cast<int4*>(before + SCAN_INTS);
   auto put = [&](int j, const int4& r, int k, int t_begin, int n) {     // piece k of a sequence
     const int tiles = ((o.of_keys ? r.w : r.y) + o.span - 1) / o.span, head = k / tiles;
     int4* to = reinterpret_cast<int4*>(table + 8 * j);
@@ -434,6 +428,7 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == F_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
+  if (warp == F_TMA_WARP && lane < 3) prefetch_map(&maps.q + lane);
   const int pieces = find_pieces(c.p, c.dev_status, Order{2 * RT, false, c.p.heads, 1, 0, 0}, reinterpret_cast<int32_t*>(smem + L::OFF_SEQ),
                                  reinterpret_cast<int32_t*>(smem));
   tc_fence_before();
@@ -606,9 +601,8 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
     bool more = next();
     bool ok = !XT || !more || load_query();
     while (more && ok) {
-      const int head = w.head, k_len = w.r.k_len, row0 = w.x0 + wg * RT + quarter * 32;
-      const int rows = min(32, w.r.q_len - row0);                // of this warp that exist; none if not positive
-      const int64_t at0 = (int64_t)w.r.q_begin + row0;
+      const int k_len = w.r.k_len, number = at_piece - 1;
+      const int rows = min(32, w.r.q_len - (w.x0 + wg * RT + quarter * 32));   // of this warp that exist; none if not positive
       const bool pair = w.r.q_len - w.x0 > RT;
       more = next();                                             // looked up while the first scores are computed
       float m = -INFINITY, l = 0.f;                              // row maximum in use (raw scores), row sum
@@ -708,9 +702,11 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
       if (!warp_wait(bar(F_PV + wg), turn ^ 1, abort_flag)) break;
       tc_fence_after();
       if (rows > 0) {
-        store_rows(static_cast<bf16*>(c.out) + at0 * c.ldo + (int64_t)head * d, c.ldo, taddr + F_O, d, l == 0.f ? 0.f : 1.0f / l, rows,
+        const Piece done = piece_at(sb + L::OFF_SEQ, number);    // looked up again: not kept in registers meanwhile
+        const int64_t at0 = (int64_t)done.r.q_begin + done.x0 + wg * RT + quarter * 32;
+        store_rows(static_cast<bf16*>(c.out) + at0 * c.ldo + (int64_t)done.head * d, c.ldo, taddr + F_O, d, l == 0.f ? 0.f : 1.0f / l, rows,
                    sb + L::OFF_OUT + warp * 2048, lane);
-        if (lane < rows) c.lse[(int64_t)head * c.p.q_rows + at0 + lane] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
+        if (lane < rows) c.lse[(int64_t)done.head * c.p.q_rows + at0 + lane] = l == 0.f ? -INFINITY : fmaf(m, c.p.scale, log2f(l) * LN2);
       }
     }
   }
@@ -784,6 +780,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
+  if (warp == B_TMA_WARP && lane < 5) prefetch_map(&maps.x1 + lane);
   const int pieces_in_all = find_pieces(c.p, c.dev_status, order_of(c.p, DKDV, shares), reinterpret_cast<int32_t*>(smem + L::OFF_SEQ),
                                         reinterpret_cast<int32_t*>(smem));
   tc_fence_before();
@@ -1109,7 +1106,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
 constexpr int ADD_ROWS = 32;
 template <bool DKDV>
 __global__ void __launch_bounds__(256) add_parts_kernel(const PackedCall c, const Shares shares) {
-  __shared__ int32_t before[SEQ_CHUNK + 4];
+  __shared__ int32_t before[SCAN_INTS];
   __shared__ int4 ranges[SEQ_CHUNK];
   const Order o = order_of(c.p, DKDV, shares);
   int total = 0, carry = 0, chunk = 0;
