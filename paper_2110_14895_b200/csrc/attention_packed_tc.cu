@@ -743,28 +743,32 @@ __device__ __forceinline__ Order order_of(const vit_attention_problem& p, bool d
 }
 constexpr int B_MMA_WARP = 16 /* two */, B_TMA_WARP = 18, B_THREADS = 608;
 
-template <int SLABS, bool DKDV>
+template <int SLABS, bool DKDV, bool XT>
 struct BackwardCfg {
+  static constexpr int PLACES = SLABS == 1 ? 3 : 2;    // for S and dP in tensor memory
+  static constexpr int XBUF = !XT && SLABS == 1 ? 2 : 1;
   static constexpr int XS = DKDV ? 2 : 3;              // tiles of X in shared memory; DQ: out, for delta
   static constexpr int STAGES = SLABS == 1 ? 5 : DKDV ? 4 : 3;
   static constexpr uint32_t XTILE = SLABS * RT * 128, YTILE = SLABS * CT * 128;
-  static constexpr uint32_t OFF_Y = XS * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // DKDV: float [STAGES][2][64] -lse2, -delta of the columns
+  static constexpr uint32_t OFF_Y = XBUF * XS * XTILE, OFF_COL = OFF_Y + STAGES * 2 * YTILE;   // DKDV: float [STAGES][2][64] -lse2, -delta of the columns
   static constexpr uint32_t OFF_ROW = OFF_COL + (DKDV ? STAGES * CT * 8 : 0);           // DQ: float2 [2][128] of the rows
   static constexpr uint32_t OFF_OUT = OFF_ROW + (DKDV ? 0 : 2 * RT * 8), OFF_BARS = OFF_OUT + 8 * 2048, OFF_SEQ = OFF_BARS + 512;
   static constexpr uint32_t BYTES = OFF_SEQ + TABLE_BYTES + 1024;
   static_assert(BYTES <= 227 * 1024, "fits an SM");
 };
 // columns: S and dP of the two warpgroups, then the accumulators (d each), then X1 and X2 (d / 2 each)
-constexpr uint32_t B_WG = 2 * CT, B_COLS = 2 * B_WG;
+constexpr uint32_t B_WG = 2 * CT;
 enum BwdBar : int {
-  B_FULL = 0, B_FREE = B_FULL + 5, B_XS = B_FREE + 5 /* X in shared memory */, B_XSFREE, B_X /* in tensor memory */, B_XFREE,
-  B_S /* [wg] */, B_P = B_S + 2, B_SFREE = B_P + 2, B_ACC = B_SFREE + 2, B_ACCFREE, B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 2
+  B_FULL = 0, B_FREE = B_FULL + 5, B_XS = B_FREE + 5 /* X in shared memory */, B_XSFREE = B_XS + 2, B_X = B_XSFREE + 2 /* in tensor memory */, B_XFREE,
+  B_S /* [tile % 6, or % 2] */, B_P = B_S + 6 /* [place] */, B_SFREE = B_P + 3, B_ACC = B_SFREE + 3, B_ACCFREE, B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 2
 };
 
 template <int SLABS, bool DKDV, bool XT>
 __global__ void __launch_bounds__(B_THREADS, 1)
 packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const PackedCall c, const Shares shares) {
-  using L = BackwardCfg<SLABS, DKDV>;
+  using L = BackwardCfg<SLABS, DKDV, XT>;
+  constexpr int PLACES = L::PLACES, XBUF = L::XBUF, ROUND = PLACES == 3 ? 6 : 2;   // tiles until place and warpgroups are the same again
+  constexpr uint32_t B_COLS = PLACES * B_WG;
   extern __shared__ uint8_t smem_raw[];
   const int d = c.p.d, group = c.p.heads / c.p.kv_heads;
   const int warp = (int)uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -776,7 +780,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < B_BARS; ++i)
-      mbar_init(bar(i), i == B_P || i == B_P + 1 || i == B_ACCFREE ? 8 : i == B_X ? 16 : XT && i == B_XSFREE ? (DKDV ? 8 : 12) : 1);
+      mbar_init(bar(i), (i >= B_P && i < B_P + PLACES) || i == B_ACCFREE ? 8 : i == B_X ? 16 : XT && i == B_XSFREE ? (DKDV ? 8 : 12) : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
@@ -805,14 +809,16 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     while (ok && advance()) {
       const int y_begin = DKDV ? w.r.q_begin : w.r.k_begin, y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (w.n == 0) continue;
-      if (!warp_wait(bar(B_XSFREE), (pieces & 1) ^ 1, abort_flag)) break;
+      const int x_at = XBUF == 2 ? pieces & 1 : 0;
+      const uint32_t xs = sb + x_at * L::XS * L::XTILE;
+      if (!warp_wait(bar(B_XSFREE + x_at), (pieces / XBUF & 1) ^ 1, abort_flag)) break;
       if (lane == 0) {
         const int row = (DKDV ? w.r.k_begin : w.r.q_begin) + w.x0;
-        mbar_arrive_expect_tx(bar(B_XS), L::XS * L::XTILE);
+        mbar_arrive_expect_tx(bar(B_XS + x_at), L::XS * L::XTILE);
         for (int s = 0; s < SLABS; ++s) {
-          tma_load_3d(sb + s * RT * 128, &maps.x1, 64 * s, w.head, row, bar(B_XS));
-          tma_load_3d(sb + L::XTILE + s * RT * 128, &maps.x2, 64 * s, w.head, row, bar(B_XS));
-          if (!DKDV) tma_load_3d(sb + 2 * L::XTILE + s * RT * 128, &maps.x3, 64 * s, w.head, row, bar(B_XS));
+          tma_load_3d(xs + s * RT * 128, &maps.x1, 64 * s, w.head, row, bar(B_XS + x_at));
+          tma_load_3d(xs + L::XTILE + s * RT * 128, &maps.x2, 64 * s, w.head, row, bar(B_XS + x_at));
+          if (!DKDV) tma_load_3d(xs + 2 * L::XTILE + s * RT * 128, &maps.x3, 64 * s, w.head, row, bar(B_XS + x_at));
         }
       }
       ++pieces;
@@ -857,7 +863,8 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     if (*abort_flag && lane == 0) {
       // a wait gave up somewhere: let the copies that were started land before the block leaves
       volatile int never = 0;
-      if (pieces) mbar_wait_limit(bar(B_XS), (pieces - 1) & 1, &never, DRAIN_LIMIT_CYCLES);
+      for (int i = pieces > XBUF ? pieces - XBUF : 0; i < pieces; ++i)
+        mbar_wait_limit(bar(B_XS + i % XBUF), i / XBUF & 1, &never, DRAIN_LIMIT_CYCLES);
       for (int t = n_all > L::STAGES ? n_all - L::STAGES : 0; t < n_all; ++t)
         mbar_wait_limit(bar(B_FULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
     }
@@ -871,10 +878,14 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     while (ok && advance()) {
       const int y_len = DKDV ? w.r.q_len : w.r.k_len;
       if (w.n == 0) continue;
-      if (scores && !warp_wait(bar(XT ? B_X : B_XS), pieces & 1, abort_flag)) break;
+      const int x_at = XBUF == 2 ? pieces & 1 : 0;
+      const uint32_t xs = sb + x_at * L::XS * L::XTILE;
+      if (scores && !warp_wait(bar(XT ? B_X : B_XS + x_at), pieces / XBUF & 1, abort_flag)) break;
       int left = y_len - (w.t_begin > 0 ? w.t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
+      int b = -1;                                                // place of tile t
       for (int t = 0; t < w.n; ++t, ring.step()) {
-        const int st = ring.at, b = t & 1, here = min(CT, left), n16 = (here + 15) / 16;
+        b = b + 1 == PLACES ? 0 : b + 1;
+        const int st = ring.at, here = min(CT, left), n16 = (here + 15) / 16;
         const uint32_t y = sb + L::OFF_Y + st * 2 * L::YTILE, s_col = tmem + b * B_WG;
         left = left > CT ? left - CT : y_len;
         if (scores) {
@@ -894,11 +905,11 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
               issue_scores_ts<SLABS, CT>(s_col, tmem + x1_col, y, 16 * n16, d / 16);
               issue_scores_ts<SLABS, CT>(s_col + CT, tmem + x2_col, y + L::YTILE, 16 * n16, d / 16);
             } else {
-              issue_scores_ss<SLABS, CT>(s_col, sb, y, 16 * n16, d / 16);
-              issue_scores_ss<SLABS, CT>(s_col + CT, sb + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
+              issue_scores_ss<SLABS, CT>(s_col, xs, y, 16 * n16, d / 16);
+              issue_scores_ss<SLABS, CT>(s_col + CT, xs + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
             }
-            umma_commit(bar(B_S + b));
-            if (t == w.n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE));
+            umma_commit(bar(B_S + t % ROUND));
+            if (t == w.n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE + x_at));
           }
         } else {
           if (!warp_wait(bar(B_P + b), phase >> b & 1, abort_flag)) { ok = false; break; }
@@ -927,17 +938,13 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   } else {
     // ------------------------------------------------------------------ probabilities and their gradients
     // warpgroups 0, 1: the two halves of the even tiles' columns; 2, 3: of the odd tiles'
-    const int wg = warp >> 2, place = wg >> 1, half = wg & 1, quarter = warp & 3, in_tile = quarter * 32 + lane;
+    const int wg = warp >> 2, odd = wg >> 1, half = wg & 1, quarter = warp & 3, in_tile = quarter * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t taddr = lanes + place * B_WG + half * 32, stage = sb + L::OFF_OUT + (warp & 7) * 2048;
+    const uint32_t stage = sb + L::OFF_OUT + (warp & 7) * 2048;
     const float sl2 = c.p.scale * LOG2E;
     const float2 sl2v = make_float2(sl2, sl2);
     Ring<L::STAGES> ring;                                        // of every tile, this warpgroup's or not
     int pieces = 0, s_phase = 0;
-    // where a row of piece w goes if others have parts of it too: of dk (or dq) or of dv
-    auto partial_row = [&](int tensor, int row) {
-      return c.partial + (((int64_t)(2 * blockIdx.x + (w.t_begin > 0 ? 0 : 1)) * (DKDV ? 2 : 1) + tensor) * RT + row) * d;
-    };
     // the next piece with something to walk over; rows that nothing meets get gradients of zero on the way
     auto next = [&] {
       while (advance()) {
@@ -994,8 +1001,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
     bool ok = !XT || !more || load_x();
     while (more && ok) {
       const int y_len = DKDV ? w.r.q_len : w.r.k_len;
-      const int head = w.head, row0 = w.x0 + quarter * 32, rows = min(32, (DKDV ? w.r.k_len : w.r.q_len) - row0);
-      const int64_t at0 = (int64_t)(DKDV ? w.r.k_begin : w.r.q_begin) + row0;
+      const int number = at_piece - 1, rows = min(32, (DKDV ? w.r.k_len : w.r.q_len) - (w.x0 + quarter * 32));
       float2 nls = make_float2(0.f, 0.f), nde = nls;             // DQ: of this thread's row
       if (!DKDV) {
         if (!warp_wait(bar(B_X), pieces & 1, abort_flag)) break;
@@ -1003,19 +1009,19 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         nls = make_float2(-mine.x, -mine.x);
         nde = make_float2(-mine.y, -mine.y);
       }
-      const int n = w.n;                                         // (w moves on before the sums are stored)
-      float* sums = n < (DKDV ? group * y_tiles : y_tiles) ? partial_row(DKDV ? wg & 1 : 0, quarter * 32) : nullptr;
+      const int n = w.n;                                         // (w moves on)
       int left = y_len - (w.t_begin > 0 ? w.t_begin % y_tiles : 0) * CT;   // rows of this head from the present tile on
       for (int t = 0; t < n; ++t, ring.step()) {
         const int here = min(CT, left) - 32 * half;              // of this warpgroup's 32 columns
         left = left > CT ? left - CT : y_len;
-        if ((t & 1) != place) continue;
-        const int st = ring.at;
+        if ((t & 1) != odd) continue;
+        const int st = ring.at, place = t % PLACES, s_bar = t % ROUND;
+        const uint32_t taddr = lanes + place * B_WG + half * 32;
         // four columns each: -lse2, then -delta
         const float4* col = reinterpret_cast<const float4*>(smem + L::OFF_COL) + st * (CT / 2) + 8 * half;
         if (DKDV && !warp_wait(bar(B_FULL + st), ring.parity, abort_flag)) { ok = false; break; }
-        if (!warp_wait(bar(B_S + place), s_phase, abort_flag)) { ok = false; break; }
-        s_phase ^= 1;
+        if (!warp_wait(bar(B_S + s_bar), s_phase >> s_bar & 1, abort_flag)) { ok = false; break; }
+        s_phase ^= 1 << s_bar;
         tc_fence_after();
         if (rows > 0 && here > 0) {
 #pragma unroll
@@ -1072,6 +1078,10 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
       if (!warp_wait(bar(B_ACC), (pieces - 1) & 1, abort_flag)) break;
       tc_fence_after();
       if (rows > 0) {
+        const Piece done = piece_at(sb + L::OFF_SEQ, number);    // looked up again: not kept in registers meanwhile
+        const int64_t at0 = (int64_t)(DKDV ? done.r.k_begin : done.r.q_begin) + done.x0 + quarter * 32;
+        const int whole = ((DKDV ? done.r.q_len : done.r.k_len) + CT - 1) / CT * (DKDV ? group : 1), head = done.head;
+        float* sums = n < whole ? c.partial + (((int64_t)(2 * blockIdx.x + (done.t_begin > 0 ? 0 : 1)) * (DKDV ? 2 : 1) + (DKDV ? wg & 1 : 0)) * RT + quarter * 32) * d : nullptr;
         const int from = DKDV || wg == 0 ? 0 : d / 32 * 16, to = DKDV || wg == 1 ? d : d / 32 * 16;   // dk, dv; or a part of dq each
         if (sums) {
           store_rows(sums + from, d, lanes + (DKDV && wg == 1 ? acc1 : acc2) + from, to - from, 1.f, rows, stage, lane);
@@ -1222,7 +1232,7 @@ size_t partial_floats(const vit_attention_problem& p, bool dkdv) { return (size_
 
 template <int SLABS, bool DKDV, bool XT>
 cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
-  using L = BackwardCfg<SLABS, DKDV>;
+  using L = BackwardCfg<SLABS, DKDV, XT>;
   BackwardMaps m;
   const void *x1 = DKDV ? c.k : c.q, *x2 = DKDV ? c.v : c.dout, *y1 = DKDV ? c.q : c.k, *y2 = DKDV ? c.dout : c.v;
   const int64_t lx1 = DKDV ? c.ldk : c.ldq, lx2 = DKDV ? c.ldv : c.lddo, ly1 = DKDV ? c.ldq : c.ldk, ly2 = DKDV ? c.lddo : c.ldv;
@@ -1265,7 +1275,7 @@ cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s) {
   return c.p.d <= 80 ? launch_forward<2, true>(c, s) : launch_forward<2, false>(c, s);
 }
 cudaError_t launch_attention_packed_dkdv_bf16(const PackedCall& c, cudaStream_t s) {
-  if (c.p.d <= 64) return launch_backward<1, true, true>(c, s);
+  if (c.p.d <= 64) return launch_backward<1, true, false>(c, s);
   return c.p.d <= 80 ? launch_backward<2, true, true>(c, s) : launch_backward<2, true, false>(c, s);
 }
 cudaError_t launch_attention_packed_dq_bf16(const PackedCall& c, cudaStream_t s) {
