@@ -741,7 +741,7 @@ struct Shares { int blocks, least; };                    // blocks = 0: pieces a
 __device__ __forceinline__ Order order_of(const vit_attention_problem& p, bool dkdv, const Shares& s) {
   return Order{RT, dkdv, dkdv ? p.kv_heads : p.heads, dkdv ? p.heads / p.kv_heads : 1, s.blocks, s.least};
 }
-constexpr int B_MMA_WARP = 16 /* two */, B_TMA_WARP = 18, B_THREADS = 608;
+constexpr int B_MMA_WARP = 16 /* S; 17: second products, 19: dP */, B_TMA_WARP = 18, B_THREADS = 640;
 
 template <int SLABS, bool DKDV, bool XT>
 struct BackwardCfg {
@@ -760,7 +760,7 @@ struct BackwardCfg {
 constexpr uint32_t B_WG = 2 * CT;
 enum BwdBar : int {
   B_FULL = 0, B_FREE = B_FULL + 5, B_XS = B_FREE + 5 /* X in shared memory */, B_XSFREE = B_XS + 2, B_X = B_XSFREE + 2 /* in tensor memory */, B_XFREE,
-  B_S /* [tile % 6, or % 2] */, B_P = B_S + 6 /* [place] */, B_SFREE = B_P + 3, B_ACC = B_SFREE + 3, B_ACCFREE, B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 2
+  B_S /* [tile % 6, or % 2] */, B_P = B_S + 6 /* [place] */, B_SFREE = B_P + 3, B_ACC = B_SFREE + 3, B_ACCFREE, B_ROW, B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 4
 };
 
 template <int SLABS, bool DKDV, bool XT>
@@ -780,7 +780,7 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < B_BARS; ++i)
-      mbar_init(bar(i), (i >= B_P && i < B_P + PLACES) || i == B_ACCFREE ? 8 : i == B_X ? 16 : XT && i == B_XSFREE ? (DKDV ? 8 : 12) : 1);
+      mbar_init(bar(i), (i >= B_P && i < B_P + PLACES) || i == B_ACCFREE ? 8 : i == B_X ? 16 : (i >= B_S && i < B_S + ROUND) || i == B_XFREE || (!XT && (i == B_XSFREE || i == B_XSFREE + 1)) ? 2 : XT && i == B_XSFREE ? (DKDV ? 8 : 12) : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
@@ -869,9 +869,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         mbar_wait_limit(bar(B_FULL + t % L::STAGES), (t / L::STAGES) & 1, &never, DRAIN_LIMIT_CYCLES);
     }
   } else if (warp >= B_MMA_WARP) {
-    // ------------------------------------------------------------------ MMA issuers (whole warps keep step): one of the
-    // scores, one of the second products
-    const bool scores = warp == B_MMA_WARP;
+    // ------------------------------------------------------------------ MMA issuers (whole warps keep step): one of S, one
+    // of dP, one of the second products
+    const bool scores = warp != B_MMA_WARP + 1, first = warp == B_MMA_WARP;
     Ring<L::STAGES> ring;
     int pieces = 0, phase = 0;                                   // bit b of phase: parity of the next wait for warpgroup b's columns
     bool ok = true;
@@ -893,21 +893,15 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
           // rows of Y behind the end of the sequence become zero, whatever lies there: they meet weights of
           // zero in the second products, and give scores of zero in the first
           if (here < 16 * n16) {
-            zero_rows(y, CT, SLABS, here, lane);
-            zero_rows(y + L::YTILE, CT, SLABS, here, lane);
+            zero_rows(first ? y : y + L::YTILE, CT, SLABS, here, lane);
           }
           // S and dP overwrite P and dS of tile t - 2, once their products are complete
           if (!warp_wait(bar(B_SFREE + b), (phase >> b & 1) ^ 1, abort_flag)) { ok = false; break; }
           phase ^= 1 << b;
           if (elect_one()) {
             tc_fence_after();
-            if (XT) {
-              issue_scores_ts<SLABS, CT>(s_col, tmem + x1_col, y, 16 * n16, d / 16);
-              issue_scores_ts<SLABS, CT>(s_col + CT, tmem + x2_col, y + L::YTILE, 16 * n16, d / 16);
-            } else {
-              issue_scores_ss<SLABS, CT>(s_col, xs, y, 16 * n16, d / 16);
-              issue_scores_ss<SLABS, CT>(s_col + CT, xs + L::XTILE, y + L::YTILE, 16 * n16, d / 16);
-            }
+            if (XT) issue_scores_ts<SLABS, CT>(first ? s_col : s_col + CT, tmem + (first ? x1_col : x2_col), first ? y : y + L::YTILE, 16 * n16, d / 16);
+            else issue_scores_ss<SLABS, CT>(first ? s_col : s_col + CT, first ? xs : xs + L::XTILE, first ? y : y + L::YTILE, 16 * n16, d / 16);
             umma_commit(bar(B_S + t % ROUND));
             if (t == w.n - 1) umma_commit(bar(XT ? B_XFREE : B_XSFREE + x_at));
           }
