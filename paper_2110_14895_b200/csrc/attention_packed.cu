@@ -317,7 +317,7 @@ packed_dkdv_kernel(const PackedCall c, int splits) {
     if (row >= k_here) continue;
     const int64_t at = (int64_t)r.k_begin + k0 + row;
     if (group == 0) store_row<DP>(static_cast<float*>(c.dv) + at * c.lddv + (int64_t)kv * d, acc[i], 1.f, tx, d);
-    else store_row<DP>(static_cast<float*>(c.dk) + at * c.lddk + (int64_t)kv * d, acc[i], c.p.scale, tx, d);
+    else store_row<DP>(static_cast<float*>(c.dk) + at * c.lddk + (int64_t)kv * d, acc[i], gradient_scale(c.p, r.k_len), tx, d);
   }
 }
 
@@ -380,7 +380,7 @@ packed_dq_kernel(const PackedCall c, int splits) {
   for (int i = 1; i < 2 * splits; ++i) add_sums<DP>(sm, i - 1, tid, acc);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (ty * 4 + i < q_here) store_row<DP>(static_cast<float*>(c.dq) + (at + ty * 4 + i) * c.lddq + (int64_t)head * d, acc[i], c.p.scale, tx, d);
+    if (ty * 4 + i < q_here) store_row<DP>(static_cast<float*>(c.dq) + (at + ty * 4 + i) * c.lddq + (int64_t)head * d, acc[i], gradient_scale(c.p, r.k_len), tx, d);
 }
 
 enum Which { FORWARD, DKDV, DQ };

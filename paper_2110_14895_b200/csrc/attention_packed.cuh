@@ -20,4 +20,8 @@ __device__ __forceinline__ bool seq_range(const vit_attention_problem& p, int se
   return true;
 }
 
+// The factor of dq and dk.  The one probability of a sequence with one key is 1 whatever its score, so that its
+// gradient is zero; dout v and dout out are summed in different orders and leave a rounding of it.
+__device__ __forceinline__ float gradient_scale(const vit_attention_problem& p, int k_len) { return k_len == 1 ? 0.f : p.scale; }
+
 }  // namespace vit

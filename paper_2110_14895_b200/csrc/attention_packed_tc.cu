@@ -1082,9 +1082,9 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         } else if (DKDV) {
           const int64_t ld = wg == 0 ? c.lddk : c.lddv;
           store_rows(static_cast<bf16*>(wg == 0 ? c.dk : c.dv) + at0 * ld + (int64_t)head * d, ld, lanes + (wg == 0 ? acc2 : acc1), d,
-                     wg == 0 ? c.p.scale : 1.f, rows, stage, lane);
+                     wg == 0 ? gradient_scale(c.p, done.r.k_len) : 1.f, rows, stage, lane);
         } else {
-          store_rows(static_cast<bf16*>(c.dq) + at0 * c.lddq + (int64_t)head * d + from, c.lddq, lanes + acc2 + from, to - from, c.p.scale, rows,
+          store_rows(static_cast<bf16*>(c.dq) + at0 * c.lddq + (int64_t)head * d + from, c.lddq, lanes + acc2 + from, to - from, gradient_scale(c.p, done.r.k_len), rows,
                      stage, lane);
         }
       }
@@ -1137,7 +1137,7 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const PackedCall c, cons
   for (int tensor = 0; tensor < (DKDV ? 2 : 1); ++tensor) {
     const int64_t ld = DKDV ? (tensor ? c.lddv : c.lddk) : c.lddq;
     bf16* to = static_cast<bf16*>(DKDV ? (tensor ? c.dv : c.dk) : c.dq) + ((int64_t)(DKDV ? r.z : r.x) + x0) * ld + (int64_t)head * d;
-    const float by = tensor ? 1.f : c.p.scale;
+    const float by = tensor ? 1.f : gradient_scale(c.p, r.w);
     for (int i = threadIdx.x; i < rows * eights; i += 256) {
       const int row = i / eights, ch = (i - row * eights) * 8;
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;

@@ -493,6 +493,28 @@ def test_packed_attention_bad_offsets_are_reported(ctx, dtype, bad):
     assert torch.equal(dq[qs], good_grads[0][qs]) and torch.equal(dkv[ks], good_grads[1][ks])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("ql,kl,heads,kv,d", [([1, 1, 1], [1, 1, 1], 3, 1, 96), ([40, 513, 3, 70], [1, 1, 0, 65], 2, 2, 64),
+                                             ([2600, 2600], [1, 1], 8, 1, 128)])
+def test_packed_attention_of_one_key_passes_no_gradient_to_its_score(ctx, dtype, ql, kl, heads, kv, d):
+    """The softmax of one number is 1: dq and dk are zero, and not a rounding; what is not a number stays so."""
+    vit, m = ctx
+    p = Packed(vit, ql, kl, heads, kv, d, dtype, seed=6)
+    out, lse = p.forward(m)
+    dq, dkv = p.backward(m, out, lse)
+    m.check()
+    p.check_backward(out, lse, dq, dkv)
+    for (qs, ks), b in zip(p.sequences(), kl):
+        if b == 1:
+            assert (dq[qs, :heads * d] == 0).all() and (dkv[ks, :kv * d] == 0).all() and (dkv[ks, kv * d:2 * kv * d] != 0).any()
+    qs, ks = next(p.sequences())
+    p.v[ks] = float("nan")
+    out, lse = p.forward(m)
+    dq, dkv = p.backward(m, out, lse)
+    m.check()
+    assert torch.isnan(dq[qs, :heads * d]).all() and torch.isnan(dkv[ks, :kv * d]).all()
+
+
 def test_packed_attention_gradients_against_differences(ctx):
     """Directional derivatives of the library's own forward pass in fp32."""
     vit, m = ctx
