@@ -352,10 +352,13 @@ struct Ring {
 // A piece is 256 queries of a head: warps 0-3 and 4-7 hold 128 of them each and share the keys, which come
 // in tiles of 128; warps 8 and 9 issue the products of one warpgroup each, warp 10 the copies.  The scores of
 // a warpgroup's next tile come only after its last probabilities were used: the two warpgroups fall into step
-// so that one runs its exponentials while the tensor core works for the other (a warp of each shares a
-// scheduler and its exp2 unit, 8 cycles for 32 of them, which bounds the kernel up to d = 128: 1024 cycles for
-// 2 x 128 x 64 scores).  The accumulator is rescaled only when a row's maximum has grown by more than 2^8
-// since the last time (probabilities stay below 2^8, the row sum in fp32): rarely after the first tile.
+// so that one runs its exponentials while the tensor core works for the other.  What bounds the kernel is this
+// chain: a warp of each warpgroup shares a scheduler and its exp2 unit, 8 cycles for 32 of them, 2048 cycles for
+// 2 x 128 x 128 scores, and a round takes 3200 (64 channels, 4096 keys: 680 TFLOP/s; 830 at 80 channels, 1180 at
+// 128).  Scores in halves of a tile, issued one ahead, cost as much in waits as they save at 64 channels; four
+// warpgroups with 64 keys each are slower (470 us for 417).  What is kept in registers over the tiles decides more:
+// with 100 bytes spilled the kernel is 5 % slower.  The accumulator is rescaled only when a row's maximum has grown
+// by more than 2^8 since the last time (probabilities stay below 2^8, the row sum in fp32): rarely after the first tile.
 struct ForwardMaps { CUtensorMap q, k, v; };
 constexpr int F_MMA_WARP = 8 /* two */, F_TMA_WARP = 10, F_THREADS = 352;
 constexpr uint32_t TMEM_ALL = 512;
@@ -730,10 +733,15 @@ packed_forward_tc_kernel(const __grid_constant__ ForwardMaps maps, const PackedC
 //   DKDV: X = K, V; Y = Q, dout of every query head that shares the key head (scores transposed);
 //         dv += P Y2, dk += dS Y1
 // Seven products instead of the five of a single pass, but every gradient is summed in one place in a fixed
-// order.  Tiles alternate between two places in tensor memory for S and dP, each with two warpgroups that take 32
-// of its 64 columns: while one pair is in its exp2 phase the tensor core works for the other, and four warps a
-// scheduler hide each other's latencies; one warp issues the scores, another the second products.  X is in tensor memory (XT) where it fits beside the accumulators: always for DQ, up to
-// d = 80 for DKDV.
+// order.  Tiles alternate between places in tensor memory for S and dP, and between two pairs of warpgroups that
+// take 32 of the 64 columns each: while one pair is in its exp2 phase the tensor core works for the other, and four
+// warps a scheduler hide each other's latencies.  Warps 16 and 19 issue S and dP, warp 17 the second products.
+// Up to 64 channels there are three places (2 x 128 x 3 columns, then the accumulators), so that scores are ready
+// before a pair comes to them: 4 x 4096 rows, 16 heads of 64: 1208 us with two, 1045 with three.  X is in tensor
+// memory (XT) where it fits beside that: for DQ, and for DKDV between 65 and 80 channels; else in shared memory,
+// twice where there is room.  What bounds both kernels is the length of a tile's way from S to P to the second
+// products and, with four or five tiles to a piece, the change of pieces (18 % and 23 % of the tensor pipe at 64
+// images of 197 rows, 52 % and 56 % at four of up to 4097).
 // Where pieces do not come out even, the blocks share all tiles equally: the sums of a piece that is not one block's go
 // to partial [2 block + (0: its first piece, 1: its last)][dk, dv or dq][128][d] in fp32, and a last kernel adds them in order.
 struct BackwardMaps { CUtensorMap x1, x2, x3, y1, y2; };
@@ -760,7 +768,7 @@ struct BackwardCfg {
 constexpr uint32_t B_WG = 2 * CT;
 enum BwdBar : int {
   B_FULL = 0, B_FREE = B_FULL + 5, B_XS = B_FREE + 5 /* X in shared memory */, B_XSFREE = B_XS + 2, B_X = B_XSFREE + 2 /* in tensor memory */, B_XFREE,
-  B_S /* [tile % 6, or % 2] */, B_P = B_S + 6 /* [place] */, B_SFREE = B_P + 3, B_ACC = B_SFREE + 3, B_ACCFREE, B_ROW, B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 4
+  B_S /* [tile % 6, or % 2] */, B_P = B_S + 6 /* [place] */, B_SFREE = B_P + 3, B_ACC = B_SFREE + 3, B_ACCFREE, B_DRAIN /* [MMA warp] */, B_BARS = B_DRAIN + 4
 };
 
 template <int SLABS, bool DKDV, bool XT>
@@ -780,7 +788,15 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < B_BARS; ++i)
-      mbar_init(bar(i), (i >= B_P && i < B_P + PLACES) || i == B_ACCFREE ? 8 : i == B_X ? 16 : (i >= B_S && i < B_S + ROUND) || i == B_XFREE || (!XT && (i == B_XSFREE || i == B_XSFREE + 1)) ? 2 : XT && i == B_XSFREE ? (DKDV ? 8 : 12) : 1);
+    {
+      const bool x_free = i == B_XSFREE || i == B_XSFREE + 1;
+      int count = 1;
+      if ((i >= B_P && i < B_P + PLACES) || i == B_ACCFREE) count = 8;
+      else if (i == B_X) count = 16;
+      else if ((i >= B_S && i < B_S + ROUND) || i == B_XFREE || (!XT && x_free)) count = 2;    // S and dP
+      else if (x_free) count = DKDV ? 8 : 12;
+      mbar_init(bar(i), count);
+    }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == B_MMA_WARP) tmem_alloc(smem_u32(tmem_slot), TMEM_ALL);
@@ -1075,7 +1091,8 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
         const Piece done = piece_at(sb + L::OFF_SEQ, number);    // looked up again: not kept in registers meanwhile
         const int64_t at0 = (int64_t)(DKDV ? done.r.k_begin : done.r.q_begin) + done.x0 + quarter * 32;
         const int whole = ((DKDV ? done.r.q_len : done.r.k_len) + CT - 1) / CT * (DKDV ? group : 1), head = done.head;
-        float* sums = n < whole ? c.partial + (((int64_t)(2 * blockIdx.x + (done.t_begin > 0 ? 0 : 1)) * (DKDV ? 2 : 1) + (DKDV ? wg & 1 : 0)) * RT + quarter * 32) * d : nullptr;
+        const int64_t slot = 2 * blockIdx.x + (done.t_begin > 0 ? 0 : 1);
+        float* sums = n < whole ? c.partial + ((slot * (DKDV ? 2 : 1) + (DKDV ? wg & 1 : 0)) * RT + quarter * 32) * d : nullptr;
         const int from = DKDV || wg == 0 ? 0 : d / 32 * 16, to = DKDV || wg == 1 ? d : d / 32 * 16;   // dk, dv; or a part of dq each
         if (sums) {
           store_rows(sums + from, d, lanes + (DKDV && wg == 1 ? acc1 : acc2) + from, to - from, 1.f, rows, stage, lane);
@@ -1209,7 +1226,9 @@ cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
 
 // Whether the blocks of the backward pass share the tiles (in shares of eight at least): where that takes less time,
 // counted in tiles.  A piece takes three besides its own, shares cost each block two parts and a launch more, and
-// without them the last round is as long as a full one.  (SHARE_US)
+// without them the last round is as long as a full one.
+// (4 sequences of up to 4097, 8 heads over 2 key heads of 128: dq 161 us in whole pieces, 149 and 6 for the sums in
+// shares; dk and dv 269 in whole pieces, 184 and 10 in shares.)
 constexpr int SHARE_BLOCKS = 148;
 Shares shares_of(const vit_attention_problem& p, bool dkdv) {
   const int64_t pieces = (int64_t)p.sequences * (dkdv ? p.kv_heads : p.heads) * (((dkdv ? p.max_k : p.max_q) + RT - 1) / RT);
