@@ -362,6 +362,8 @@ ATTENTION_CASES = [
     # as many queries as the kernel for few of them takes (four rows in bf16, eight in fp32), and one more
     ([1, 1, 0], [1030, 5, 3], 8, 1, 64), ([2, 1], [300, 0], 4, 2, 128), ([4, 3], [700, 70], 2, 2, 112), ([8, 2], [333, 65], 2, 2, 48),
     ([9, 5], [333, 65], 1, 1, 16),
+    # shares in which a short sequence counts for more tiles than it has
+    ([3000, 1, 0, 70], None, 8, 2, 64), ([2600, 3, 0, 129], None, 8, 2, 128),
 ]
 
 
@@ -594,6 +596,24 @@ def test_packed_attention_of_many_short_sequences(ctx, dtype, sequences, n):
                              ((half * 1.01 + 2 * e + acc) * prob).transpose(-1, -2) @ do.abs())):
         assert ((got - exact).abs() <= half * exact.abs() + tol).all()
     assert (out[rows:] == 33).all() and (dq[rows:] == 33).all() and (dkv[rows:] == 33).all()
+
+
+def test_packed_attention_shares_over_many_sequences(ctx):
+    """More sequences than are looked at together, where the blocks share the tiles of the gradients."""
+    vit, m = ctx
+    rng = np.random.default_rng(8)
+    ql = [1000 if i % 50 == 7 else int(n) for i, n in enumerate(rng.integers(0, 41, 600))]
+    kl = [128 if i % 50 == 7 else int(n) for i, n in enumerate(rng.integers(0, 129, 600))]
+    p = Packed(vit, ql, kl, 1, 1, 64, torch.bfloat16, lead=2, trail=4)
+    out, lse = p.forward(m)
+    m.check()
+    p.check_forward(out, lse)
+    dq, dkv = p.backward(m, out, lse)
+    m.check()
+    p.check_backward(out, lse, dq, dkv)
+    dq2, dkv2 = p.backward(m, out, lse)
+    m.check()
+    assert torch.equal(dq, dq2) and torch.equal(dkv, dkv2)
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
