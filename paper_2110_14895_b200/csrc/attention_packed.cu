@@ -199,7 +199,7 @@ packed_delta_kernel(const PackedCall c) {
 // The gradient kernels have two groups of 128 threads: one has the scores and their probabilities, the other the
 // gradients of the probabilities; then each has one sum (dv and dk, or half of the keys for dq).
 // Where there are few blocks, a tile's walk is shared out over a cluster of two, whose sums are joined in the first
-// one's shared memory, in order: 115 -> 76 us for both kernels and delta at 5 images of up to 257 rows, 4 heads of 80,
+// one's shared memory, in order: 115 -> 76 us at 5 images of up to 257 rows, 4 heads of 80 (dq, dk and dv, delta),
 // 898 -> 576 us at 1 x 1024 rows, 8 heads of 128 on 2. A cluster of four's sums do not fit there at 128 channels.
 constexpr int GRAD_THREADS = 2 * THREADS;
 constexpr int MAX_SPLITS = 2;
@@ -255,15 +255,14 @@ __device__ __forceinline__ void grad_scores(float* ps, float* ds, const float* q
 }
 
 template <int DP>
-__global__ void __launch_bounds__(GRAD_THREADS)
-packed_dkdv_kernel(const PackedCall c, int splits) {
+__device__ __forceinline__ void dkdv_tile(const PackedCall& c, int splits, int block) {
   static_assert(SUMS_FIT<DP>, "the joined sums lie over the tiles");
   extern __shared__ __align__(16) float sm[];
   constexpr int TILE = BT * (DP + 4);
   float *ks = sm, *vs = ks + TILE, *qo = vs + TILE, *ps = qo + 4 * TILE, *ds = ps + BT * PS;   // qo: [stage][q, dout]; ps, ds: [query][key]
   float2* rows = reinterpret_cast<float2*>(ds + BT * PS);                                      // [stage][32]: lse log2(e), delta
   const int tiles = (c.p.max_k + BT - 1) / BT;
-  const int rank = blockIdx.x % splits, item = blockIdx.x / splits;
+  const int rank = block % splits, item = block / splits;
   const int tile = item % tiles, kv = item / tiles % c.p.kv_heads, seq = item / tiles / c.p.kv_heads;
   SeqRange r;
   if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
@@ -322,15 +321,14 @@ packed_dkdv_kernel(const PackedCall c, int splits) {
 }
 
 template <int DP>
-__global__ void __launch_bounds__(GRAD_THREADS)
-packed_dq_kernel(const PackedCall c, int splits) {
+__device__ __forceinline__ void dq_tile(const PackedCall& c, int splits, int block) {
   static_assert(SUMS_FIT<DP>, "the joined sums lie over the tiles");
   extern __shared__ __align__(16) float sm[];
   constexpr int TILE = BT * (DP + 4);
   float *qs = sm, *os = qs + TILE, *kv_s = os + TILE, *ps = kv_s + 4 * TILE, *ds = ps + BT * PS;    // kv_s: [stage][k, v]; ps, ds: [key][query]
   float2* rows = reinterpret_cast<float2*>(ds + BT * PS);
   const int tiles = (c.p.max_q + BT - 1) / BT;
-  const int rank = blockIdx.x % splits, item = blockIdx.x / splits;
+  const int rank = block % splits, item = block / splits;
   const int tile = item % tiles, head = item / tiles % c.p.heads, seq = item / tiles / c.p.heads;
   SeqRange r;
   if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
@@ -383,15 +381,38 @@ packed_dq_kernel(const PackedCall c, int splits) {
     if (ty * 4 + i < q_here) store_row<DP>(static_cast<float*>(c.dq) + (at + ty * 4 + i) * c.lddq + (int64_t)head * d, acc[i], gradient_scale(c.p, r.k_len), tx, d);
 }
 
-enum Which { FORWARD, DKDV, DQ };
+// Both in one launch: neither fills the device by itself where there are few rows, and neither waits for the other's
+// last blocks.  The first `dkdv_blocks` have dk and dv.  (5 images of up to 257 rows, 4 heads of 80:
+// 74 us in two launches, 58 in one; 16 images of 197, 12 heads of 64: 328 and 301.)
+template <int DP>
+__global__ void __launch_bounds__(GRAD_THREADS)
+packed_grads_kernel(const PackedCall c, int splits, int dkdv_blocks) {
+  if ((int)blockIdx.x < dkdv_blocks) dkdv_tile<DP>(c, splits, blockIdx.x);
+  else dq_tile<DP>(c, splits, blockIdx.x - dkdv_blocks);
+}
 
-// blocks of the gradient kernels that share a tile's walk: two where there is not yet one wave of two to an SM, and
-// each has two tiles at least
-int splits_of(int64_t blocks, int64_t walk) { return blocks < 2 * 148 && walk >= 4 ? MAX_SPLITS : 1; }
-template <typename Kernel>
-cudaError_t launch_split(Kernel kernel, const PackedCall& c, int64_t blocks, int splits, size_t smem, cudaStream_t s) {
+
+template <int DP>
+cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
+  constexpr size_t smem = 5 * (size_t)BT * (DP + 4) * 4 + (size_t)BT * PS * 4;
+  static PerDeviceFlag done;
+  if (cudaError_t e = ensure_dynamic_smem(done, packed_forward_kernel<DP>, (int)smem)) return e;
+  packed_forward_kernel<DP><<<(unsigned)(c.p.sequences * c.p.heads * ((c.p.max_q + BT - 1) / BT)), THREADS, smem, s>>>(c);
+  return cudaGetLastError();
+}
+
+template <int DP>
+cudaError_t launch_grads(const PackedCall& c, cudaStream_t s) {
+  constexpr size_t smem = 6 * (size_t)BT * (DP + 4) * 4 + 2 * (size_t)BT * PS * 4 + 2 * BT * sizeof(float2);
+  static PerDeviceFlag done;
+  if (cudaError_t e = ensure_dynamic_smem(done, packed_grads_kernel<DP>, (int)smem)) return e;
+  const int64_t q_tiles = (c.p.max_q + BT - 1) / BT, k_tiles = (c.p.max_k + BT - 1) / BT, sequences = c.p.sequences;
+  const int64_t dkdv = c.p.k_rows > 0 ? sequences * c.p.kv_heads * k_tiles : 0, dq = c.p.q_rows > 0 ? sequences * c.p.heads * q_tiles : 0;
+  // two blocks share a tile's walk (of four tiles or more) where that takes a sixth of the rounds of two blocks to an SM away
+  const int64_t wave = 2 * 148, rounds = (dkdv + dq + wave - 1) / wave, halves = (2 * (dkdv + dq) + wave - 1) / wave;
+  const int splits = 3 * halves <= 5 * rounds && k_tiles >= 4 && c.p.heads / c.p.kv_heads * q_tiles >= 4 ? MAX_SPLITS : 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(blocks * splits));
+  cfg.gridDim = dim3((unsigned)((dkdv + dq) * splits));
   cfg.blockDim = dim3(GRAD_THREADS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -401,48 +422,22 @@ cudaError_t launch_split(Kernel kernel, const PackedCall& c, int64_t blocks, int
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, c, splits);
-}
-
-template <int DP>
-cudaError_t launch_variant(const PackedCall& c, Which w, cudaStream_t s) {
-  constexpr size_t tile = (size_t)BT * (DP + 4) * 4, prob = (size_t)BT * PS * 4;
-  const int64_t q_tiles = (c.p.max_q + BT - 1) / BT, k_tiles = (c.p.max_k + BT - 1) / BT;
-  static PerDeviceFlag done[3];
-  if (w == FORWARD) {
-    const size_t smem = 5 * tile + prob;
-    if (cudaError_t e = ensure_dynamic_smem(done[0], packed_forward_kernel<DP>, (int)smem)) return e;
-    packed_forward_kernel<DP><<<(unsigned)(c.p.sequences * c.p.heads * q_tiles), THREADS, smem, s>>>(c);
-    return cudaGetLastError();
-  }
-  if (w == DKDV) {
-    const size_t smem = 6 * tile + 2 * prob + 2 * BT * sizeof(float2);
-    if (cudaError_t e = ensure_dynamic_smem(done[1], packed_dkdv_kernel<DP>, (int)smem)) return e;
-    const int64_t blocks = c.p.sequences * c.p.kv_heads * k_tiles;
-    return launch_split(packed_dkdv_kernel<DP>, c, blocks, splits_of(blocks, c.p.heads / c.p.kv_heads * q_tiles), smem, s);
-  }
-  const size_t smem = 6 * tile + 2 * prob + BT * sizeof(float2);
-  if (cudaError_t e = ensure_dynamic_smem(done[2], packed_dq_kernel<DP>, (int)smem)) return e;
-  const int64_t blocks = c.p.sequences * c.p.heads * q_tiles;
-  return launch_split(packed_dq_kernel<DP>, c, blocks, splits_of(blocks, k_tiles), smem, s);
-}
-cudaError_t launch_width(const PackedCall& c, Which w, cudaStream_t s) {
-  if (c.p.d <= 32) return launch_variant<32>(c, w, s);
-  if (c.p.d <= 64) return launch_variant<64>(c, w, s);
-  if (c.p.d <= 96) return launch_variant<96>(c, w, s);
-  return launch_variant<128>(c, w, s);
+  return cudaLaunchKernelEx(&cfg, packed_grads_kernel<DP>, c, splits, (int)(dkdv * splits));
 }
 
 }  // namespace
 
-cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, FORWARD, s); }
+cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) {
+  return c.p.d <= 32 ? launch_forward<32>(c, s) : c.p.d <= 64 ? launch_forward<64>(c, s) : c.p.d <= 96 ? launch_forward<96>(c, s) : launch_forward<128>(c, s);
+}
 
 cudaError_t launch_attention_delta_f32(const PackedCall& c, cudaStream_t s) {
   const int64_t blocks = ((int64_t)c.p.q_rows * c.p.heads + THREADS / 32 - 1) / (THREADS / 32), most = 1 << 20;
   packed_delta_kernel<<<(unsigned)(blocks < most ? blocks : most), THREADS, 0, s>>>(c);
   return cudaGetLastError();
 }
-cudaError_t launch_attention_packed_dkdv_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, DKDV, s); }
-cudaError_t launch_attention_packed_dq_f32(const PackedCall& c, cudaStream_t s) { return launch_width(c, DQ, s); }
+cudaError_t launch_attention_packed_grads_f32(const PackedCall& c, cudaStream_t s) {
+  return c.p.d <= 32 ? launch_grads<32>(c, s) : c.p.d <= 64 ? launch_grads<64>(c, s) : c.p.d <= 96 ? launch_grads<96>(c, s) : launch_grads<128>(c, s);
+}
 
 }  // namespace vit

@@ -916,11 +916,15 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
   c.dev_status = h->dev_status;
   const bool b16 = dtype == VIT_BF16;
   const bool queries = p.q_rows > 0 && p.max_q > 0, keys = p.k_rows > 0 && p.max_k > 0;
-  // dq comes first: in bf16 mode its kernel also leaves lse and delta of every row for the other one
-  if (!b16 && queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta_f32(c, s));
-  if (queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, b16 ? launch_attention_packed_dq_bf16(c, s) : launch_attention_packed_dq_f32(c, s));
-  if (keys) VIT_LAUNCH(h, VIT_PROF_ATTENTION, b16 ? launch_attention_packed_dkdv_bf16(c, s) : launch_attention_packed_dkdv_f32(c, s));
-  if (b16) h->launches.fetch_add((queries && attention_in_parts(p, false)) + (keys && attention_in_parts(p, true)), std::memory_order_relaxed);
+  if (!b16) {
+    if (queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta_f32(c, s));
+    if (queries || keys) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_grads_f32(c, s));
+    return VIT_OK;
+  }
+  // dq comes first: its kernel also leaves lse and delta of every row for the other one
+  if (queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dq_bf16(c, s));
+  if (keys) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dkdv_bf16(c, s));
+  h->launches.fetch_add((queries && attention_in_parts(p, false)) + (keys && attention_in_parts(p, true)), std::memory_order_relaxed);
   return VIT_OK;
 }
 

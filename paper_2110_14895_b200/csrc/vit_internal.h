@@ -195,8 +195,7 @@ cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s);
 // the kernels of the backward pass, in this order; delta is part of dq in bf16 mode
 cudaError_t launch_attention_delta_f32(const PackedCall& c, cudaStream_t s);
-cudaError_t launch_attention_packed_dq_f32(const PackedCall& c, cudaStream_t s);
-cudaError_t launch_attention_packed_dkdv_f32(const PackedCall& c, cudaStream_t s);
+cudaError_t launch_attention_packed_grads_f32(const PackedCall& c, cudaStream_t s);       // dk, dv and dq, behind delta
 cudaError_t launch_attention_packed_dq_bf16(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_dkdv_bf16(const PackedCall& c, cudaStream_t s);
 
