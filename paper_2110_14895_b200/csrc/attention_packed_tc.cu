@@ -1227,8 +1227,8 @@ cudaError_t launch_forward(const PackedCall& c, cudaStream_t s) {
 // Whether the blocks of the backward pass share the tiles (in shares of eight at least): where that takes less time,
 // counted in tiles.  A piece takes three besides its own, shares cost each block two parts and a launch more, and
 // without them the last round is as long as a full one.
-// (4 sequences of up to 4097, 8 heads over 2 key heads of 128: dq 161 us in whole pieces, 149 and 6 for the sums in
-// shares; dk and dv 269 in whole pieces, 184 and 10 in shares.)
+// (4 sequences of up to 4097, 8 heads over 2 key heads of 128: dq 161 us in whole pieces, 144 and 8 for the sums in
+// shares; dk and dv 269 in whole pieces, 172 and 9 in shares.)
 constexpr int SHARE_BLOCKS = 148;
 Shares shares_of(const vit_attention_problem& p, bool dkdv) {
   const int64_t pieces = (int64_t)p.sequences * (dkdv ? p.kv_heads : p.heads) * (((dkdv ? p.max_k : p.max_q) + RT - 1) / RT);
