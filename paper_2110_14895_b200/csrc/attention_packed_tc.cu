@@ -803,6 +803,8 @@ packed_backward_tc_kernel(const __grid_constant__ BackwardMaps maps, const Packe
   if (warp == B_TMA_WARP && lane < 5) prefetch_map(&maps.x1 + lane);
   const int pieces_in_all = find_pieces(c.p, c.dev_status, order_of(c.p, DKDV, shares), reinterpret_cast<int32_t*>(smem + L::OFF_SEQ),
                                         reinterpret_cast<int32_t*>(smem));
+  if (DKDV) asm volatile("griddepcontrol.wait;" ::: "memory");               // the kernel before this one leaves delta
+  else asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1265,8 +1267,18 @@ cudaError_t launch_backward(const PackedCall& c, cudaStream_t s) {
   if (sms < 1) return cudaErrorInvalidDevice;
   const Shares shares = shares_of(c.p, DKDV);
   const int total = c.p.sequences * xh * (((DKDV ? c.p.max_k : c.p.max_q) + RT - 1) / RT);
-  packed_backward_tc_kernel<SLABS, DKDV, XT><<<shares.blocks > 0 ? shares.blocks : grid_of(total, sms), B_THREADS, L::BYTES, s>>>(m, c, shares);
-  if (cudaError_t e = cudaGetLastError()) return e;
+  // dk and dv look their pieces up while the last blocks of dq (or of its sums) are at work, if that was launched before them
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(shares.blocks > 0 ? shares.blocks : grid_of(total, sms)));
+  cfg.blockDim = dim3(B_THREADS);
+  cfg.dynamicSmemBytes = L::BYTES;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = DKDV && c.p.q_rows > 0 && c.p.max_q > 0 ? 1 : 0;
+  if (cudaError_t e = cudaLaunchKernelEx(&cfg, packed_backward_tc_kernel<SLABS, DKDV, XT>, m, c, shares)) return e;
   if (shares.blocks > 0) {
     add_parts_kernel<DKDV><<<dim3((unsigned)shares.blocks - 1, RT / ADD_ROWS), 256, 0, s>>>(c, shares);
     return cudaGetLastError();
