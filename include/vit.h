@@ -307,6 +307,8 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
  * output may overlap an input or another output unless stated (column blocks of one buffer with the same
  * stride do not overlap).
  * Sums, norms and softmax statistics are fp32; bf16 results are rounded once.
+ * Scratch holds nothing between calls; calls that may run at the same time (on two streams, or in graphs that are
+ * replayed together) need scratch of their own.
  * Results do not depend on the schedule: the same call gives the same bits. */
 
 /* Rotary positions on one to four axes (row and column of a patch, frame of a video).  Pair i of a head

@@ -618,25 +618,25 @@ rope_norm_full_kernel(const RopeNormArgs p) {
   }
 }
 
-// dq_gain[c], dk_gain[c] = sum of the blocks' shares, in a fixed order: 32 channels to a block, 32 threads to a
-// channel, all loads of a thread in flight together
-constexpr int GAIN_THREADS = 1024;
+// dq_gain[c], dk_gain[c] = sum of the blocks' shares, in a fixed order: 8 channels (a sector) to a block, 128 threads to
+// a channel, all loads of a thread in flight together
+constexpr int GAIN_THREADS = 1024, GAIN_CHANNELS = 8;
 __global__ void __launch_bounds__(GAIN_THREADS)
 gain_grad_kernel(const float* __restrict__ partial, int blocks, int d, float* __restrict__ dq_gain, float* __restrict__ dk_gain) {
-  __shared__ float sums[32][33];
-  const int part = threadIdx.x >> 5, lane = threadIdx.x & 31, i = blockIdx.x * 32 + lane;
+  __shared__ float sums[GAIN_THREADS / 32][GAIN_CHANNELS];
+  const int channel = threadIdx.x & (GAIN_CHANNELS - 1), part = threadIdx.x / GAIN_CHANNELS, i = blockIdx.x * GAIN_CHANNELS + channel;
   asm volatile("griddepcontrol.wait;" ::: "memory");     // the shares are written by the kernel before this one
   float sum = 0.f;
-  if (i < 2 * d) {
 #pragma unroll 8
-    for (int b = part; b < blocks; b += 32) sum += partial[(int64_t)b * 2 * d + i];
-  }
-  sums[part][lane] = sum;
+  for (int b = part; b < blocks; b += GAIN_THREADS / GAIN_CHANNELS) sum += partial[(int64_t)b * 2 * d + i];
+  sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+  sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+  if ((threadIdx.x & 31) < GAIN_CHANNELS) sums[threadIdx.x >> 5][channel] = sum;
   __syncthreads();
-  if (part == 0 && i < 2 * d) {
+  if (threadIdx.x < GAIN_CHANNELS) {
     sum = 0.f;
 #pragma unroll
-    for (int b = 0; b < 32; ++b) sum += sums[b][lane];
+    for (int b = 0; b < GAIN_THREADS / 32; ++b) sum += sums[b][channel];
     (i < d ? dq_gain : dk_gain)[i < d ? i : i - d] = sum;
   }
 }
@@ -731,7 +731,7 @@ cudaError_t launch_gain_grad(const RopeNormCall& c, float* dq_gain, float* dk_ga
   const bool full = 2 * n_pairs == c.d;
   const int blocks = c.rows > 0 ? shape_of(NORM_TURN_GRAD, c.rows, c.heads, c.d, full, c.act_bf16 ? 2 : 4, sms).grid : 0;   // no rows: the gradients are zero
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((2 * c.d + 31) / 32);
+  cfg.gridDim = dim3(2 * c.d / GAIN_CHANNELS);                   // (d is a multiple of 16)
   cfg.blockDim = dim3(GAIN_THREADS);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];                           // its launch overlaps the end of the kernel before it
