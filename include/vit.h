@@ -375,7 +375,8 @@ int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_proble
                             void* ws, size_t ws_bytes, void* stream);
 
 /* Gradients of vit_op_attention_packed from its operands, its two results and dout.  The probabilities are
- * computed again from lse.  dk and dv of a key head are summed over the query heads that share it.
+ * computed again from lse.  dk and dv of a key head are summed over the query heads that share it.  Long sums are
+ * cut where the lengths of all sequences of the call say, so that beside other sequences the last bit may differ.
  *   dq: activations [q_rows, heads * d]; dk, dv: [k_rows, kv_heads * d]. */
 int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attention_problem* problem, const void* q,
                                      int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
