@@ -9,9 +9,10 @@
 // staged in shared memory, rows behind the end of a sequence are zero there.  Tiles of 64 with 256 threads need
 // fewer reads of shared memory for a product, but leave one block of eight warps to an SM and a quarter of the
 // blocks.  What bounds it is the wait for a thread's own sums and reads with eight to sixteen warps on an SM:
-// 19 TFLOP/s at 16 images of 197 rows, 12 heads of 64 (100 us forward, 301 us backward).  The backward pass has two kinds of blocks, one that keeps a tile of keys and walks over the queries (dk, dv) and one that
-// keeps a tile of queries and walks over the keys (dq): seven products instead of five, but every
-// gradient is summed by one block in a fixed order, so that results do not depend on the schedule.
+// 19 TFLOP/s at 16 images of 197 rows, 12 heads of 64 (100 us forward, 301 us backward).  The backward pass has
+// two kinds of blocks, one that keeps a tile of keys and walks over the queries (dk, dv) and one that keeps a tile
+// of queries and walks over the keys (dq): seven products instead of five, but every gradient is summed by one
+// block, or by two and in order, so that results do not depend on the schedule.
 #include "vit_internal.h"
 #include "attention_packed.cuh"
 #include "sm100_ptx.cuh"
