@@ -174,12 +174,14 @@ packed_forward_kernel(const PackedCall c) {
   wait_fetched<0>();
 }
 
-// (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head
+// (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head.
+// All rows of the buffers, whether a sequence covers them or not: the offsets are the caller's, and a bad one (the last
+// one among them) says nothing of how far the other sequences reach.
 __global__ void __launch_bounds__(THREADS)
 packed_delta_kernel(const PackedCall c) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
-  const int64_t rows = min(c.p.q_rows, c.p.q_offsets[c.p.sequences]);      // rows behind the last sequence are not looked at
+  const int64_t rows = c.p.q_rows;
   for (int64_t item = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); item < rows * c.p.heads;
        item += (int64_t)gridDim.x * (THREADS / 32)) {
     const int64_t row = item / c.p.heads;

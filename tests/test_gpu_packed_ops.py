@@ -873,3 +873,44 @@ def test_packed_ops_of_nothing(ctx):
     vit.vit_op_attention_packed(m.h, 0, p, 0, 128, 0, 128, 0, 128, 0, 128, 0, 0, 0)
     vit.vit_op_attention_packed_backward(m.h, 0, p, 0, 128, 0, 128, 0, 128, 0, 128, 0, 0, 128, 0, 128, 0, 128, 0, 128, 0, 0)
     m.check()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("last", [30, -1, -2 ** 31])
+def test_packed_attention_bad_last_offset_leaves_the_others_alone(ctx, dtype, last):
+    """Whatever the last offset says, the gradients of the sequences before the last one are those of the good call."""
+    vit, m = ctx
+    p = Packed(vit, [40, 50, 60], [40, 50, 60], 4, 2, 64, dtype, trail=30)
+    good = p.forward(m)
+    good_grads = p.backward(m, *good)
+    m.check()
+    for off in (p.q_off, p.k_off):
+        off[3] = last
+    out, lse = p.forward(m)
+    dq, dkv = p.backward(m, *good)              # (its scratch holds NaN)
+    with pytest.raises(vit.VitError) as e:
+        m.check()
+    assert e.value.status == vit.VIT_ERR_OFFSETS
+    assert torch.equal(out[:90], good[0][:90]) and torch.equal(lse[:, :90], good[1][:, :90])
+    assert torch.equal(dq[:90], good_grads[0][:90]) and torch.equal(dkv[:90], good_grads[1][:90])
+    for t in (out, dq, dkv):
+        assert (t[90:] == 33).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_packed_attention_sequence_behind_the_last_offset(ctx, dtype):
+    """After a step backwards the last offset is not the largest: what lies behind it is still a sequence's."""
+    vit, m = ctx
+    p = Packed(vit, [60, 40], [60, 40], 4, 2, 64, dtype, lead=50)
+    parts = torch.tensor([90, 150, 50, 90], dtype=torch.int32, device="cuda")      # rows 90 ... 149, none, rows 50 ... 89
+    p.q_off, p.k_off = parts, parts.clone()
+    p.problem = vit.make_attention_problem(3, 4, 2, 64, 150, 60, p.q_off.data_ptr(), 150, 60, p.k_off.data_ptr(), p.scale)
+    p.sequences = lambda: [(slice(90, 150),) * 2, (slice(50, 90),) * 2]
+    p.covered_q = p.covered_k = slice(50, 150)
+    out, lse = p.forward(m)
+    dq, dkv = p.backward(m, out, lse)
+    with pytest.raises(vit.VitError) as e:
+        m.check()
+    assert e.value.status == vit.VIT_ERR_OFFSETS
+    p.check_forward(out, lse)
+    p.check_backward(out, lse, dq, dkv)
