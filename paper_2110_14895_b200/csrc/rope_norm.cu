@@ -209,6 +209,8 @@ rope_norm_kernel(const RopeNormArgs p) {
 #pragma unroll
             for (int j = 0; j < CH; ++j) sq = fmaf(x_[j], x_[j], sq);
             rstd = 1.0f / sqrtf(fmaf(head_sum(sq, sums), p.inv_d, p.eps));
+            // a place without a head adds nothing to the gains' gradients (with eps = 0 its factor would be infinite)
+            if (MODE == NORM_TURN_GRAD && !on[k]) rstd = 0.f;
           }
           // what is turned, and its partners: gradients as they come, values times gain (the norm's factor is
           // the same for the whole head and comes last)

@@ -914,3 +914,49 @@ def test_packed_attention_sequence_behind_the_last_offset(ctx, dtype):
     assert e.value.status == vit.VIT_ERR_OFFSETS
     p.check_forward(out, lse)
     p.check_backward(out, lse, dq, dkv)
+
+
+@pytest.mark.parametrize("rows,hq,hk,d,pairs", [
+    # heads that leave places of a warp empty: rotation of a part, none, and of all channels
+    (33, 16, 4, 80, (11, 9)), (40, 3, 1, 112, ()), (21, 6, 3, 64, (9, 8)), (300, 5, 2, 48, (8, 8)), (33, 16, 4, 80, (20, 20)), (5000, 3, 2, 64, (16, 16)),
+])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_qk_norm_rope_with_eps_of_zero(ctx, rows, hq, hk, d, pairs, interleaved, dtype):
+    """Without eps the norm of every head that is not zero is finite, and so are all gradients."""
+    vit, m = ctx
+    gen = _gen(rows + d)
+    heads, width = hq + hk, (hq + hk) * d
+    x, dy = _normal(gen, rows, width, scale=1.3, dtype=dtype), _normal(gen, rows, width, scale=0.5, dtype=dtype)
+    gains = 1 + _normal(gen, 2, d, scale=0.2)
+    rope = freqs = positions = None
+    if pairs:
+        freqs, positions = _rope_inputs(gen, rows, pairs, 50)
+        rope = vit.make_rope(pairs, freqs.data_ptr(), positions.data_ptr(), interleaved)
+    n = vit.vit_qk_norm_rope_backward_bytes(rows, hq, hk, d)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda")
+    y, dx, dg = torch.empty_like(x), torch.empty_like(x), torch.empty(2, d, device="cuda")
+    args = (m.h, _dt(vit, dtype), rows, hq, hk, d, gains[0].data_ptr(), gains[1].data_ptr(), 0.0, rope)
+    vit.vit_op_qk_norm_rope(*args, x.data_ptr(), width, y.data_ptr(), width)
+    vit.vit_op_qk_norm_rope_backward(*args, x.data_ptr(), width, dy.data_ptr(), width, dx.data_ptr(), width, dg[0].data_ptr(),
+                                     dg[1].data_ptr(), ws.data_ptr(), n)
+    m.check()
+    x64, dy64 = (t.double().unflatten(1, (heads, d)) for t in (x, dy))
+    x64.requires_grad_()
+    g64 = [g.double().requires_grad_() for g in gains]
+    rstd = 1 / (x64 * x64).mean(-1, keepdim=True).sqrt()
+    scaled = torch.cat([part * g for part, g in zip((x64 * rstd).split([hq, hk], 1), g64)], 1)
+    want = _turn64(scaled, pairs, freqs, positions, interleaved) if pairs else scaled
+    wx, *wg = torch.autograd.grad(want, [x64] + g64, dy64)
+    want, rstd, scaled = want.detach(), rstd.detach(), scaled.detach()
+    # the bounds of the test with eps: a sum of d squares, a root, a division; the rotation mixes two channels of a head
+    rel32 = (d + 24) * 2.0 ** -24
+    tol = HALF[dtype] * want.abs() + rel32 * scaled.abs().amax(-1, keepdim=True) * math.sqrt(2)
+    assert ((y.double().unflatten(1, (heads, d)) - want).abs() <= tol).all()
+    xh, gain_max = (x64.detach() * rstd).abs(), gains.abs().max().double()
+    u = dy64.abs().amax(-1, keepdim=True) * math.sqrt(2)
+    tol = HALF[dtype] * wx.abs() + 4 * rel32 * rstd * (gain_max * u + xh * gain_max * u * xh.mean(-1, keepdim=True))
+    assert ((dx.double().unflatten(1, (heads, d)) - wx).abs() <= tol).all()
+    for got, exact, part, count in zip(dg, wg, (u * xh).split([hq, hk], 1), (hq, hk)):
+        tol = (rel32 * 4 + 2.0 ** -24 * min(rows * count, 4096)) * part.sum((0, 1))
+        assert ((got.double() - exact).abs() <= tol).all()
