@@ -356,8 +356,8 @@ int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads
  * VIT_ERR_OFFSETS.  Rows that no sequence covers are left as they were. */
 typedef struct vit_attention_problem {
   int32_t sequences, heads, kv_heads, d;
-  int32_t q_rows, max_q;      /* rows of q; bound on the length of a sequence's queries */
-  int32_t k_rows, max_k;      /* rows of k and v; bound on the length of its keys */
+  int32_t q_rows, max_q;      /* rows of q; bound on the length of a sequence's queries (any, INT32_MAX too) */
+  int32_t k_rows, max_k;      /* rows of k and v; bound on the length of its keys; rows: at most INT32_MAX - 1024 */
   const int32_t* q_offsets;   /* dev [sequences + 1] */
   const int32_t* k_offsets;   /* dev [sequences + 1] */
   float scale;                /* of the scores, usually 1 / sqrt(d); finite and positive */

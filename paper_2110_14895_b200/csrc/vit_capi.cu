@@ -278,8 +278,19 @@ bool offsets_overlap(const vit_attention_problem& p, const Block& out) {
   const int64_t n = (int64_t)p.sequences + 1;
   return blocks_overlap(out, Block{p.q_offsets, 1, n, n, 4}) || blocks_overlap(out, Block{p.k_offsets, 1, n, n, 4});
 }
+// The kernels count rows and tiles in 32 bits and round up to whole tiles, shares and rounds (512 rows at most).
+constexpr int32_t MAX_PACKED_ROWS = INT32_MAX - 1024;
+// The problem as the kernels get it: a bound beyond the buffer (INT32_MAX for "any length") says no more than the
+// buffer's rows do, which no sequence exceeds.
+vit_attention_problem bounded(const vit_attention_problem& problem) {
+  vit_attention_problem p = problem;
+  if (p.max_q > p.q_rows) p.max_q = p.q_rows;
+  if (p.max_k > p.k_rows) p.max_k = p.k_rows;
+  return p;
+}
 // blocks of the launches: one per sequence, head and tile of at least 32 rows
 bool attention_fits(const vit_attention_problem* p) {
+  if (p->q_rows > MAX_PACKED_ROWS || p->k_rows > MAX_PACKED_ROWS) return false;
   const int64_t longest = p->max_q > p->max_k ? p->max_q : p->max_k;
   const int64_t per = (int64_t)p->heads * ((longest + 31) / 32 + 1);
   return p->sequences == 0 || per <= INT32_MAX / 8 / p->sequences;      // (up to eight blocks where there are few queries)
@@ -848,16 +859,17 @@ int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads
 }
 
 size_t vit_attention_packed_bytes(int dtype, const vit_attention_problem* problem, int backward) {
-  if (!attention_problem_ok(dtype, problem) || !attention_fits(problem)) return 0;
-  return attention_packed_ws(dtype, *problem, backward != 0);
+  if (!attention_problem_ok(dtype, problem)) return 0;
+  const vit_attention_problem p = bounded(*problem);
+  return attention_fits(&p) ? attention_packed_ws(dtype, p, backward != 0) : 0;
 }
 
 int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_problem* problem, const void* q, int64_t ldq,
                             const void* k, int64_t ldk, const void* v, int64_t ldv, void* out, int64_t ldo, float* lse,
                             void* ws, size_t ws_bytes, void* stream) {
   if (!h || !attention_problem_ok(dtype, problem) || (problem->q_rows > 0 && (!lse || misaligned(lse))) || !on_own_device(h)) return VIT_ERR_INVALID_ARG;
-  if (!attention_fits(problem)) return VIT_ERR_TOO_LARGE;
-  const vit_attention_problem& p = *problem;
+  const vit_attention_problem p = bounded(*problem);
+  if (!attention_fits(&p)) return VIT_ERR_TOO_LARGE;
   const size_t es = element_bytes(dtype), need = attention_packed_ws(dtype, p, false);
   const int64_t wq = (int64_t)p.heads * p.d, wk = (int64_t)p.kv_heads * p.d;
   const Block bq{q, p.q_rows, wq, ldq, es}, bk{k, p.k_rows, wk, ldk, es}, bv{v, p.k_rows, wk, ldv, es}, bo{out, p.q_rows, wq, ldo, es};
@@ -884,8 +896,8 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
                                      void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* ws,
                                      size_t ws_bytes, void* stream) {
   if (!h || !attention_problem_ok(dtype, problem) || (problem->q_rows > 0 && (!lse || misaligned(lse))) || !on_own_device(h)) return VIT_ERR_INVALID_ARG;
-  if (!attention_fits(problem)) return VIT_ERR_TOO_LARGE;
-  const vit_attention_problem& p = *problem;
+  const vit_attention_problem p = bounded(*problem);
+  if (!attention_fits(&p)) return VIT_ERR_TOO_LARGE;
   const size_t es = element_bytes(dtype), need = attention_packed_ws(dtype, p, true);
   const int64_t wq = (int64_t)p.heads * p.d, wk = (int64_t)p.kv_heads * p.d;
   const Block in[] = {{q, p.q_rows, wq, ldq, es}, {k, p.k_rows, wk, ldk, es}, {v, p.k_rows, wk, ldv, es},

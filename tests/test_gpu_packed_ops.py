@@ -960,3 +960,33 @@ def test_qk_norm_rope_with_eps_of_zero(ctx, rows, hq, hk, d, pairs, interleaved,
     for got, exact, part, count in zip(dg, wg, (u * xh).split([hq, hk], 1), (hq, hk)):
         tol = (rel32 * 4 + 2.0 ** -24 * min(rows * count, 4096)) * part.sum((0, 1))
         assert ((got.double() - exact).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("ql,kl,heads,kv", [([197, 70], None, 2, 1), ([1300, 20], None, 8, 2), ([1, 1], [577, 40], 2, 2), ([130], None, 1, 1)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_packed_attention_without_a_bound_of_the_lengths(ctx, ql, kl, heads, kv, dtype):
+    """max_q and max_k may be anything that is long enough, the largest number among them."""
+    vit, m = ctx
+    p = Packed(vit, ql, kl or ql, heads, kv, 64, dtype, lead=2, trail=6)
+    for max_q, max_k in ((2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31 - 40, 2 ** 31 - 1), (p.q_rows, 2 ** 31 - 33)):
+        p.problem.max_q, p.problem.max_k = max_q, max_k
+        out, lse = p.forward(m)
+        dq, dkv = p.backward(m, out, lse)
+        m.check()
+        p.check_forward(out, lse)
+        p.check_backward(out, lse, dq, dkv)
+
+
+def test_packed_attention_refuses_rows_that_it_cannot_count(ctx):
+    vit, m = ctx
+    x = torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda")
+    off = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    a, o, before = x.data_ptr(), off.data_ptr(), m.launches
+    for q_rows, k_rows in ((2 ** 31 - 1, 1), (1, 2 ** 31 - 1), (2 ** 31 - 1024, 1)):
+        p = vit.make_attention_problem(1, 1, 1, 64, q_rows, 1, o, k_rows, 1, o, 0.125)
+        for call in (lambda: vit.vit_op_attention_packed(m.h, 0, p, a, 64, a, 64, a, 64, a, 64, a, 0, 0),
+                     lambda: vit.vit_op_attention_packed_backward(m.h, 0, p, a, 64, a, 64, a, 64, a, 64, a, a, 64, a, 64, a, 64, a, 64, 0, 0)):
+            with pytest.raises(vit.VitError) as e:
+                call()
+            assert e.value.status == vit.VIT_ERR_TOO_LARGE
+    assert m.launches == before

@@ -63,3 +63,24 @@ def test_calls_without_a_handle_are_refused():
         with pytest.raises(vit.VitError) as e:
             call()
         assert e.value.status == vit.VIT_ERR_INVALID_ARG
+
+
+ANY = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("dtype", [vit.VIT_BF16, vit.VIT_FP32])
+@pytest.mark.parametrize("heads,kv_heads,q_rows,k_rows", [(1, 1, 5000, 5000), (2, 1, 100, 90), (8, 2, 16388, 16388), (1, 1, 0, 7)])
+def test_a_bound_beyond_the_buffers_says_what_their_rows_say(dtype, heads, kv_heads, q_rows, k_rows):
+    shape = dict(dtype=dtype, sequences=1, heads=heads, kv_heads=kv_heads, q_rows=q_rows, k_rows=k_rows)
+    whole = _bytes(max_q=q_rows, max_k=k_rows, **shape)
+    for max_q, max_k in ((ANY, ANY), (ANY, k_rows), (q_rows, ANY), (ANY - 31, ANY - 100), (q_rows + 1, k_rows + 1)):
+        assert _bytes(max_q=max_q, max_k=max_k, **shape) == whole
+    assert whole > 0 or q_rows == 0
+    assert _bytes(dtype=dtype, sequences=1000, heads=64, kv_heads=64, max_q=ANY, max_k=ANY) > 0
+
+
+def test_rows_that_the_kernels_cannot_count_have_no_size():
+    one = dict(sequences=1, heads=1, kv_heads=1, d=16, max_q=1, max_k=1)
+    for rows in (ANY, ANY - 1023):
+        assert _bytes(**one, q_rows=rows) == 0 and _bytes(**one, k_rows=rows) == 0
+    assert _bytes(**one, q_rows=ANY - 1024, k_rows=ANY - 1024) >= 8 * (ANY - 1024)
