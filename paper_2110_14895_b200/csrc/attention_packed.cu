@@ -174,6 +174,14 @@ packed_forward_kernel(const PackedCall c) {
   wait_fetched<0>();
 }
 
+// What the other kernels say of bad offsets, for a call that has no rows to work on
+__global__ void __launch_bounds__(THREADS)
+check_offsets_kernel(const PackedCall c) {
+  SeqRange r;
+  for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < c.p.sequences; i += (int64_t)gridDim.x * THREADS)
+    seq_range(c.p, (int)i, r, c.dev_status, true);
+}
+
 // (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head.
 // All rows of the buffers, whether a sequence covers them or not: the offsets are the caller's, and a bad one (the last
 // one among them) says nothing of how far the other sequences reach.
@@ -447,6 +455,11 @@ cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s) {
   return c.p.d <= 32 ? launch_forward<32>(c, s) : c.p.d <= 64 ? launch_forward<64>(c, s) : c.p.d <= 96 ? launch_forward<96>(c, s) : launch_forward<128>(c, s);
 }
 
+cudaError_t launch_check_offsets(const PackedCall& c, cudaStream_t s) {
+  const int blocks = (int)(((int64_t)c.p.sequences + THREADS - 1) / THREADS);
+  check_offsets_kernel<<<(unsigned)(blocks < 1024 ? blocks : 1024), THREADS, 0, s>>>(c);
+  return cudaGetLastError();
+}
 cudaError_t launch_attention_delta_f32(const PackedCall& c, cudaStream_t s) {
   const int64_t blocks = ((int64_t)c.p.q_rows * c.p.heads + THREADS / 32 - 1) / (THREADS / 32), most = 1 << 20;
   packed_delta_kernel<<<(unsigned)(blocks < most ? blocks : most), THREADS, 0, s>>>(c);

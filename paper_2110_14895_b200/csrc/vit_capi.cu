@@ -879,12 +879,13 @@ int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_proble
     if ((b != &bo && blocks_overlap(*b, bo)) || (b != &bl && blocks_overlap(*b, bl)) || blocks_overlap(*b, bws)) return VIT_ERR_INVALID_ARG;
   if (offsets_overlap(p, bo) || offsets_overlap(p, bl)) return VIT_ERR_INVALID_ARG;
   if (ws_bytes < need) return VIT_ERR_WORKSPACE;
-  if (p.sequences == 0 || p.q_rows == 0 || p.max_q == 0) return VIT_OK;
+  if (p.sequences == 0) return VIT_OK;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   PackedCall c{};
   c.p = p; c.q = q; c.ldq = ldq; c.k = k; c.ldk = ldk; c.v = v; c.ldv = ldv; c.out = out; c.ldo = ldo; c.lse = lse;
   c.dev_status = h->dev_status;
-  if (attention_rows_supported(p, dtype == VIT_BF16)) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_rows(c, dtype == VIT_BF16, s));
+  if (p.max_q == 0) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_check_offsets(c, s));      // (no rows: a bound of zero)
+  else if (attention_rows_supported(p, dtype == VIT_BF16)) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_rows(c, dtype == VIT_BF16, s));
   else if (dtype == VIT_BF16) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_bf16(c, s));
   else VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_f32(c, s));
   return VIT_OK;
@@ -928,9 +929,13 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
   c.dev_status = h->dev_status;
   const bool b16 = dtype == VIT_BF16;
   const bool queries = p.q_rows > 0 && p.max_q > 0, keys = p.k_rows > 0 && p.max_k > 0;
+  if (!queries && !keys) {
+    VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_check_offsets(c, s));
+    return VIT_OK;
+  }
   if (!b16) {
     if (queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_delta_f32(c, s));
-    if (queries || keys) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_grads_f32(c, s));
+    VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_grads_f32(c, s));
     return VIT_OK;
   }
   // dq comes first: its kernel also leaves lse and delta of every row for the other one

@@ -191,6 +191,7 @@ size_t attention_partial_floats(const vit_attention_problem& p);
 // a few queries (times heads that share a key head) of a sequence go to the kernel for few rows (attention_rows.cu)
 bool attention_rows_supported(const vit_attention_problem& p, bool act_bf16);
 cudaError_t launch_attention_rows(const PackedCall& c, bool act_bf16, cudaStream_t s);
+cudaError_t launch_check_offsets(const PackedCall& c, cudaStream_t s);      // for calls without rows
 cudaError_t launch_attention_packed_f32(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_bf16(const PackedCall& c, cudaStream_t s);
 // the kernels of the backward pass, in this order; delta is part of dq in bf16 mode

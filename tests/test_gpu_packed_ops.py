@@ -990,3 +990,39 @@ def test_packed_attention_refuses_rows_that_it_cannot_count(ctx):
                 call()
             assert e.value.status == vit.VIT_ERR_TOO_LARGE
     assert m.launches == before
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_packed_attention_bad_offsets_are_reported_where_nothing_is_computed(ctx, dtype):
+    """No rows, or a bound of zero, but offsets that say otherwise; nothing is said where they fit."""
+    vit, m = ctx
+    dt, d = _dt(vit, dtype), 64
+    x, lse = torch.full((20, d), 33.0, dtype=dtype, device="cuda"), torch.full((1, 20), 33.0, device="cuda")
+    grads = torch.full((3, 20, d), 33.0, dtype=dtype, device="cuda")
+    empty, some = (torch.tensor(o, dtype=torch.int32, device="cuda") for o in ([0, 0, 0], [0, 5, 5]))
+    low = torch.tensor([-1, -1, -1], dtype=torch.int32, device="cuda")
+    for q_off, k_off, q_rows, max_q, k_rows, max_k, ok in [
+            (empty, empty, 20, 0, 20, 0, True), (empty, empty, 0, 0, 0, 0, True), (some, empty, 20, 0, 20, 0, False), (some, empty, 0, 5, 0, 0, False),
+            (empty, some, 20, 0, 20, 0, False), (empty, low, 0, 0, 0, 0, False), (low, empty, 20, 0, 20, 0, False), (some, some, 20, 0, 20, 5, False)]:
+        problem = vit.make_attention_problem(2, 1, 1, d, q_rows, max_q, q_off.data_ptr(), k_rows, max_k, k_off.data_ptr(), 0.125)
+        n = vit.vit_attention_packed_bytes(dt, problem, True)
+        ws = torch.empty(n + 16, dtype=torch.uint8, device="cuda")
+        q, out = x.data_ptr(), grads[0].data_ptr()
+
+        def forward():
+            vit.vit_op_attention_packed(m.h, dt, problem, q, d, q, d, q, d, out, d, lse.data_ptr(), 0, 0)
+
+        def backward():
+            vit.vit_op_attention_packed_backward(m.h, dt, problem, q, d, q, d, q, d, q, d, lse.data_ptr(), q, d, grads[0].data_ptr(), d,
+                                                 grads[1].data_ptr(), d, grads[2].data_ptr(), d, ws.data_ptr(), n)
+
+        for call in (forward, backward):
+            call()
+            if ok:
+                m.check()
+                continue
+            with pytest.raises(vit.VitError) as e:
+                m.check()
+            assert e.value.status == vit.VIT_ERR_OFFSETS
+            m.check()
+        assert (lse == 33).all() and (grads == 33).all()
