@@ -314,8 +314,8 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
 /* Rotary positions on one to four axes (row and column of a patch, frame of a video).  Pair i of a head
  * (0 <= i < n, n = sum of pairs[a]) belongs to the axis whose section it lies in: the first pairs[0]
  * pairs to axis 0, the next pairs[1] to axis 1, and so on.  It is turned by the angle
- * positions[axis * rows + row] * freqs[i] (radians; the product is taken in 64 bits, so that far
- * positions keep their angle).  Channels from 2 n on are passed on as they are. */
+ * positions[axis * rows + row] * freqs[i] (radians; whole turns are taken off in 64 bits and more, so that
+ * angles of up to 2^52 keep 32 bits).  Channels from 2 n on are passed on as they are. */
 typedef struct vit_rope {
   int32_t axes;               /* 1 ... 4 */
   int32_t pairs[4];           /* pairs of channels of each axis, >= 0; 2 n <= d */

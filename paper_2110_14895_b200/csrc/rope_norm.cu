@@ -89,12 +89,16 @@ __device__ __forceinline__ void load_floats(float (&f)[CH], const float* a) {
 __device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f(float v) { return v; }
 
-// Cosine and sine of position * freq.  The product of a 31-bit position and a 24-bit frequency is exact
-// in 64 bits; whole turns are taken off there, so that far positions keep their angle to 32 bits.
+// Cosine and sine of position * freq.  The product of a 31-bit position and a 24-bit frequency has 55 bits, two more
+// than a double: product and turns are taken in two parts each, so that the part of a turn that is left is good to
+// 32 bits for angles up to 2^52 (one part alone is off by |angle| 2^-52: 4e-7 at 2^31, 0.3 at 2^31 times a frequency
+// of 10^6).  __dmul_rn: the products whose rounding is made up for must not become part of a sum.
 __device__ __forceinline__ float2 turn_of(int32_t position, float freq) {
-  const double turns = (double)position * (double)freq * 0.15915494309189533577;
+  constexpr double PER_TURN = 0.15915494309189533577, PER_TURN_REST = -9.839338337591243e-18;      // 1 / (2 pi)
+  const double p = position, f = freq, angle = __dmul_rn(p, f), turns = __dmul_rn(angle, PER_TURN);
+  const double rest = fma(angle, PER_TURN, -turns) + fma(fma(p, f, -angle), PER_TURN, angle * PER_TURN_REST);
   float s, c;
-  sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
+  sincospif((float)(2.0 * ((turns - rint(turns)) + rest)), &s, &c);
   return make_float2(c, s);
 }
 

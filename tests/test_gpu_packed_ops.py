@@ -1,6 +1,7 @@
 """Operators of a layer over packed images (rotation, query/key norm, attention and their gradients)
 against their definitions in 64 bits, called through the C boundary."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -1026,3 +1027,38 @@ def test_packed_attention_bad_offsets_are_reported_where_nothing_is_computed(ctx
             assert e.value.status == vit.VIT_ERR_OFFSETS
             m.check()
         assert (lse == 33).all() and (grads == 33).all()
+
+
+def _unit_turns(positions, freqs):
+    """cos and sin of position * freq, the angle reduced in exact fractions."""
+    two_pi = 2 * Fraction(3141592653589793238462643383279502884197169399375105820974944, 10 ** 60)
+    unit = np.empty((len(positions), len(freqs), 2))
+    for i, position in enumerate(positions):
+        for j, freq in enumerate(freqs):
+            angle = Fraction(position) * Fraction(freq)
+            angle -= two_pi * round(angle / two_pi)
+            unit[i, j] = math.cos(angle), math.sin(angle)
+    return torch.tensor(unit, device="cuda")
+
+
+@pytest.mark.parametrize("d", [16, 32])                # all channels turn, or half of them
+def test_rope_axes_at_the_ends_of_the_range(ctx, d):
+    """The whole range of positions, with frequencies from far below 1 to far above, keeps its angle."""
+    vit, m = ctx
+    rng = np.random.default_rng(3)
+    far = [2 ** 31 - 1, -2 ** 31, 2 ** 31 - 2, -2 ** 31 + 1, 2 ** 29 + 1, -2 ** 30 - 1, 0, 1]
+    positions = far + [int(s) * (2 ** 31 - 1 - int(n)) for s, n in zip(rng.choice([-1, 1], 248), rng.integers(0, 2 ** 20, 248))]
+    freqs = torch.tensor([1.0, 0.9, 0.77, 1e-4, 3.3, 31.4, 100.0, 1e6], device="cuda")
+    where = torch.tensor([positions], dtype=torch.int32, device="cuda")
+    rows = len(positions)
+    x, y = torch.zeros(rows, d, device="cuda"), torch.empty(rows, d, device="cuda")
+    x[:, :8] = 1                                       # pair i is (1, 0): its turn is (cos, sin)
+    want = _unit_turns(positions, [float(f) for f in freqs])
+    rope = vit.make_rope((8,), freqs.data_ptr(), where.data_ptr())
+    for inverse in (False, True):
+        vit.vit_op_rope_axes(m.h, vit.VIT_FP32, rows, 1, d, rope, inverse, x.data_ptr(), d, y.data_ptr(), d)
+        m.check()
+        # the remaining half turns, at most 1, are rounded once (pi 2^-25 as an angle); 2 ulp of the functions
+        tol = (math.pi / 2 + 2) * 2.0 ** -24
+        assert ((y[:, :8].double() - want[..., 0]).abs() <= tol).all()
+        assert ((y[:, 8:16].double() - (-1 if inverse else 1) * want[..., 1]).abs() <= tol).all()
