@@ -26,6 +26,10 @@ constexpr int CH = 8;                       // channels of a lane
 constexpr int MAX_SMS = 256;
 constexpr int MAX_PAIRS = 64;               // of a head
 
+// A row's cosines and sines, one table to a warp; read in pieces of two pairs
+struct alignas(16) TurnTable { float2 of[MAX_PAIRS]; };
+static_assert(alignof(TurnTable) >= alignof(float4) && sizeof(TurnTable) % alignof(float4) == 0, "every warp's table can be read as float4");
+
 enum Rotation { INTERLEAVED = 0, HALVES_BY_LANES = 1, HALVES_ANY = 2 };
 enum Mode { TURN = 0, NORM_TURN = 1, NORM_TURN_GRAD = 2 };
 
@@ -123,10 +127,10 @@ __device__ __forceinline__ void fetch_partner(Piece<float>& to, const Piece<floa
 template <typename T, int ROT, int MODE, int HEADS>
 __global__ void __launch_bounds__(THREADS, MODE == NORM_TURN_GRAD ? 4 : 5)
 rope_norm_kernel(const RopeNormArgs p) {
-  __shared__ float2 tables[WARPS][MAX_PAIRS];
+  __shared__ TurnTable tables[WARPS];
   extern __shared__ float share[];                      // NORM_TURN_GRAD: [WARPS * side][2][d]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float2* table = tables[warp];
+  float2* table = tables[warp].of;
   const int slot = lane / p.lanes, at = lane - slot * p.lanes, first = slot * p.lanes;   // head of the step, place in it, its first lane
   const bool active = slot < p.side;
   const int c0 = at * CH, n = p.n_pairs;
@@ -376,12 +380,12 @@ __device__ __forceinline__ void copy_row(uint32_t dst, const void* src, uint32_t
 template <typename T, bool IL, int MODE, int STEPS, bool RING>
 __global__ void __launch_bounds__(THREADS, MODE == NORM_TURN_GRAD ? 3 : 4)
 rope_norm_full_kernel(const RopeNormArgs p) {
-  __shared__ float2 tables[WARPS][MAX_PAIRS];
+  __shared__ TurnTable tables[WARPS];
   __shared__ uint64_t bars[WARPS][4];
   __shared__ int given_up;
   extern __shared__ __align__(16) float share[];        // rings; at the end, NORM_TURN_GRAD: [WARPS * side][2][d]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float2* table = tables[warp];
+  float2* table = tables[warp].of;
   const int slot = lane / p.lanes, at = lane - slot * p.lanes;
   const bool active = slot < p.side;
   const int n = p.n_pairs, c0 = active ? (IL ? 16 * at : 8 * at) : 0, second = IL ? 8 : n;   // first channel of a, and of b behind it
