@@ -84,3 +84,20 @@ def test_rows_that_the_kernels_cannot_count_have_no_size():
     for rows in (ANY, ANY - 1023):
         assert _bytes(**one, q_rows=rows) == 0 and _bytes(**one, k_rows=rows) == 0
     assert _bytes(**one, q_rows=ANY - 1024, k_rows=ANY - 1024) >= 8 * (ANY - 1024)
+
+
+@pytest.mark.parametrize("dtype", [vit.VIT_BF16, vit.VIT_FP32])
+def test_backward_scratch_holds_two_floats_per_query_and_head(dtype):
+    """Log-sum-exp and delta of every query row and head, in 32 bits each."""
+    for heads, kv_heads, q_rows in ((4, 2, 100), (1, 1, 1), (12, 12, 12608), (3, 3, 2 ** 30)):
+        got = _bytes(dtype, sequences=1, heads=heads, kv_heads=kv_heads, q_rows=q_rows, max_q=1, max_k=1)
+        assert 8 * heads * q_rows <= got < 8 * heads * q_rows + 4096
+
+
+def test_backward_scratch_holds_the_parts_of_shared_sums():
+    """bf16, long sequences: 148 blocks leave two parts each, of 128 rows of dk and of dv in 32 bits."""
+    rows, heads, d = 4 * 4097, 8, 128
+    long = dict(sequences=4, heads=heads, kv_heads=2, d=d, q_rows=rows, max_q=4097, k_rows=rows, max_k=4097)
+    assert _bytes(vit.VIT_BF16, **long) >= 8 * heads * rows + 148 * 2 * 2 * 128 * d * 4
+    assert _bytes(vit.VIT_FP32, **long) < 8 * heads * rows + 4096
+    assert _bytes(vit.VIT_BF16, backward=False, **long) == 0
