@@ -320,8 +320,8 @@ typedef struct vit_rope {
   int32_t axes;               /* 1 ... 4 */
   int32_t pairs[4];           /* pairs of channels of each axis, >= 0; 2 n <= d */
   int32_t interleaved;        /* pair i is the channels (2 i, 2 i + 1) if not 0, else (i, n + i) */
-  const int32_t* positions;   /* dev [axes][rows] */
-  const float* freqs;         /* dev [n] */
+  const int32_t* positions;   /* dev [axes][rows]; may be NULL if rows or n is 0 */
+  const float* freqs;         /* dev [n]; may be NULL if n is 0 */
 } vit_rope;
 
 /* y = x with every head's pairs turned; inverse != 0 turns them back, which is also the gradient.

@@ -248,14 +248,15 @@ size_t element_bytes(int dtype) { return dtype == VIT_BF16 ? 2 : 4; }
 
 bool head_ok(int dtype, int d) { return (dtype == VIT_BF16 || dtype == VIT_FP32) && d >= 16 && d <= 128 && d % 16 == 0; }
 
-bool rope_ok(const vit_rope* r, int d) {
+bool rope_ok(const vit_rope* r, int rows, int d) {
   if (r->axes < 1 || r->axes > 4) return false;
   int64_t n = 0;
   for (int a = 0; a < r->axes; ++a) {
     if (r->pairs[a] < 0) return false;
     n += r->pairs[a];
   }
-  return 2 * n <= d && r->positions && r->freqs && !misaligned(r->positions) && !misaligned(r->freqs);
+  // no rows: no positions; no pairs: no frequencies either (an empty tensor's pointer is null)
+  return 2 * n <= d && (n == 0 || r->freqs) && (n == 0 || rows == 0 || r->positions) && !misaligned(r->positions) && !misaligned(r->freqs);
 }
 
 // whether an output lies over the positions or frequencies
@@ -782,7 +783,7 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
 
 int vit_op_rope_axes(vit_handle* h, int dtype, int rows, int heads, int d, const vit_rope* rope, int inverse,
                      const void* x, int64_t ldx, void* y, int64_t ldy, void* stream) {
-  if (!h || rows < 0 || heads < 1 || !head_ok(dtype, d) || (int64_t)heads * d > INT32_MAX || !rope || !rope_ok(rope, d) || !on_own_device(h))
+  if (!h || rows < 0 || heads < 1 || !head_ok(dtype, d) || (int64_t)heads * d > INT32_MAX || !rope || !rope_ok(rope, rows, d) || !on_own_device(h))
     return VIT_ERR_INVALID_ARG;
   const size_t es = element_bytes(dtype);
   const Block bx{x, rows, (int64_t)heads * d, ldx, es}, by{y, rows, (int64_t)heads * d, ldy, es};
@@ -801,7 +802,7 @@ int vit_op_qk_norm_rope(vit_handle* h, int dtype, int rows, int q_heads, int k_h
                         int64_t ldy, void* stream) {
   if (!h || rows < 0 || q_heads < 0 || k_heads < 0 || (int64_t)q_heads + k_heads < 1 || (int64_t)q_heads + k_heads > INT32_MAX ||
       !head_ok(dtype, d) || !q_gain || !k_gain || misaligned(q_gain) || misaligned(k_gain) || !(eps >= 0.f) ||
-      (rope && !rope_ok(rope, d)) || !on_own_device(h))
+      (rope && !rope_ok(rope, rows, d)) || !on_own_device(h))
     return VIT_ERR_INVALID_ARG;
   const size_t es = element_bytes(dtype);
   const int64_t width = ((int64_t)q_heads + k_heads) * d;
@@ -829,7 +830,7 @@ int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads
                                  float* dq_gain, float* dk_gain, void* ws, size_t ws_bytes, void* stream) {
   if (!h || rows < 0 || q_heads < 0 || k_heads < 0 || (int64_t)q_heads + k_heads < 1 || (int64_t)q_heads + k_heads > INT32_MAX ||
       !head_ok(dtype, d) || !q_gain || !k_gain || misaligned(q_gain) || misaligned(k_gain) || !(eps >= 0.f) ||
-      (rope && !rope_ok(rope, d)) || !dq_gain || !dk_gain || misaligned(dq_gain) || misaligned(dk_gain) || !ws || misaligned(ws) ||
+      (rope && !rope_ok(rope, rows, d)) || !dq_gain || !dk_gain || misaligned(dq_gain) || misaligned(dk_gain) || !ws || misaligned(ws) ||
       !on_own_device(h))
     return VIT_ERR_INVALID_ARG;
   const size_t es = element_bytes(dtype), need = qk_norm_rope_backward_bytes(d);

@@ -1062,3 +1062,29 @@ def test_rope_axes_at_the_ends_of_the_range(ctx, d):
         tol = (math.pi / 2 + 2) * 2.0 ** -24
         assert ((y[:, :8].double() - want[..., 0]).abs() <= tol).all()
         assert ((y[:, 8:16].double() - (-1 if inverse else 1) * want[..., 1]).abs() <= tol).all()
+
+
+def test_rope_of_no_rows_or_no_pairs(ctx):
+    """Empty positions and frequencies have no address; nothing of them is read."""
+    vit, m = ctx
+    g, dg = torch.ones(32, device="cuda"), torch.full((2, 32), float("nan"), device="cuda")
+    freqs = torch.ones(16, device="cuda")
+    ws = torch.empty(vit.vit_qk_norm_rope_backward_bytes(3, 1, 1, 32), dtype=torch.uint8, device="cuda")
+    for rows, rope in ((0, vit.make_rope((8, 8), freqs.data_ptr(), 0)), (0, vit.make_rope((0, 0), 0, 0)), (3, vit.make_rope((0,), 0, 0))):
+        x = _normal(_gen(2), rows, 64)
+        y, z, dx = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+        args = (m.h, vit.VIT_FP32, rows, 1, 1, 32, g.data_ptr(), g.data_ptr(), EPS)
+        vit.vit_op_rope_axes(m.h, vit.VIT_FP32, rows, 2, 32, rope, False, x.data_ptr(), 64, y.data_ptr(), 64)
+        vit.vit_op_qk_norm_rope(*args, rope, x.data_ptr(), 64, y.data_ptr(), 64)
+        vit.vit_op_qk_norm_rope_backward(*args, rope, x.data_ptr(), 64, x.data_ptr(), 64, dx.data_ptr(), 64, dg[0].data_ptr(), dg[1].data_ptr(),
+                                         ws.data_ptr(), ws.numel())
+        vit.vit_op_qk_norm_rope(*args, None, x.data_ptr(), 64, z.data_ptr(), 64)
+        m.check()
+        assert torch.equal(y, z) and torch.isfinite(dg).all() and ((dg == 0).all() if rows == 0 else torch.isfinite(dx).all())
+        vit.vit_op_rope_axes(m.h, vit.VIT_FP32, rows, 2, 32, rope, False, x.data_ptr(), 64, y.data_ptr(), 64)
+        m.check()
+        assert torch.equal(y, x)
+    for rope in (vit.make_rope((8, 8), freqs.data_ptr(), 0), vit.make_rope((8, 8), 0, freqs.data_ptr())):
+        with pytest.raises(vit.VitError) as e:
+            vit.vit_op_rope_axes(m.h, vit.VIT_FP32, 3, 2, 32, rope, False, x.data_ptr(), 64, y.data_ptr(), 64)
+        assert e.value.status == vit.VIT_ERR_INVALID_ARG
