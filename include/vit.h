@@ -299,14 +299,18 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
 
 /* ---- packed images: position rotation, query/key norm, attention and their gradients ---------
  * A batch of images of different sizes is one buffer of tokens, image after image.  These operations
- * serve such a layer between its QKV product and its output product, in inference and fine-tuning.
+ * serve such a layer between its QKV product and its output product, forwards and backwards.  The gradients of the
+ * layer's other parts (linear products, LayerNorm, GELU) are not in this library, and the stage calls above do not use
+ * these operations: a caller's own training or serving loop does.
  * Rows have strides of their own (`ld...`, in elements), so that queries, keys and values can be read
  * from, and their gradients written to, the column blocks of one [rows, (heads + 2 kv_heads) * d] buffer.
  * Common rules, checked before anything is launched: pointers 16-byte aligned (offsets: 4); d a multiple
  * of 16, at most 128; heads * d below 2^31; a stride at least as wide as its heads and a multiple of 8; no
  * output may overlap an input or another output unless stated (column blocks of one buffer with the same
  * stride do not overlap).
- * Sums, norms and softmax statistics are fp32; bf16 results are rounded once.
+ * Sums, norms and softmax statistics are fp32; bf16 results are rounded once.  In bf16 attention of more than a few
+ * queries, probabilities and the gradients of the scores are rounded to bf16 as operands of their products (half a
+ * step, 2^-8), and probabilities below 2^-126 count as zero.
  * Scratch holds nothing between calls; calls that may run at the same time (on two streams, or in graphs that are
  * replayed together) need scratch of their own.
  * Results do not depend on the schedule: the same call gives the same bits. */
@@ -353,7 +357,8 @@ int vit_op_qk_norm_rope_backward(vit_handle* h, int dtype, int rows, int q_heads
  * reads key head j / (heads / kv_heads).
  * The offsets are read on the device.  A sequence whose offsets are out of order, reach outside the buffers or
  * make it longer than max_q / max_k is skipped, its rows are left as they were, and vit_check_status reports
- * VIT_ERR_OFFSETS.  Rows that no sequence covers are left as they were. */
+ * VIT_ERR_OFFSETS.  The other sequences are computed; where a step backwards makes two of them overlap, a row that they
+ * share gets the result of either.  Rows that no sequence covers are left as they were. */
 typedef struct vit_attention_problem {
   int32_t sequences, heads, kv_heads, d;
   int32_t q_rows, max_q;      /* rows of q; bound on the length of a sequence's queries (any, INT32_MAX too) */
@@ -363,13 +368,14 @@ typedef struct vit_attention_problem {
   float scale;                /* of the scores, usually 1 / sqrt(d); finite and positive */
 } vit_attention_problem;
 
-/* Bytes of scratch for vit_op_attention_packed (backward == 0) or its gradients; 0 if none is needed or an
- * argument is invalid. */
+/* Bytes of scratch for vit_op_attention_packed (backward == 0; it needs none at present) or its gradients; 0 if none
+ * is needed, an argument is invalid or the problem is too large. */
 size_t vit_attention_packed_bytes(int dtype, const vit_attention_problem* problem, int backward);
 
 /* out[r, j] = softmax(scale q[r, j] . k^T) v over the row's sequence, and lse[j * q_rows + r] = log of the sum
  * of exp(scale q[r, j] . k), which the gradients need.  A query without keys gives out = 0, lse = -infinity.
- *   q, out: activations [q_rows, heads * d]; k, v: [k_rows, kv_heads * d]; lse: dev fp32 [heads][q_rows]. */
+ *   q, out: activations [q_rows, heads * d]; k, v: [k_rows, kv_heads * d]; lse: dev fp32 [heads][q_rows], always
+ *   written. */
 int vit_op_attention_packed(vit_handle* h, int dtype, const vit_attention_problem* problem, const void* q, int64_t ldq,
                             const void* k, int64_t ldk, const void* v, int64_t ldv, void* out, int64_t ldo, float* lse,
                             void* ws, size_t ws_bytes, void* stream);

@@ -9,7 +9,7 @@
 // staged in shared memory, rows behind the end of a sequence are zero there.  Tiles of 64 with 256 threads need
 // fewer reads of shared memory for a product, but leave one block of eight warps to an SM and a quarter of the
 // blocks.  What bounds it is the wait for a thread's own sums and reads with eight to sixteen warps on an SM:
-// 19 TFLOP/s at 16 images of 197 rows, 12 heads of 64 (100 us forward, 301 us backward).  The backward pass has
+// 18 TFLOP/s forward and 16 backward at 16 images of 197 rows, 12 heads of 64 (103 and 308 us).  The backward pass has
 // two kinds of blocks, one that keeps a tile of keys and walks over the queries (dk, dv) and one that keeps a tile
 // of queries and walks over the keys (dq): seven products instead of five, but every gradient is summed by one
 // block, or by two and in order, so that results do not depend on the schedule.
@@ -421,7 +421,8 @@ cudaError_t launch_grads(const PackedCall& c, cudaStream_t s) {
   if (cudaError_t e = ensure_dynamic_smem(done, packed_grads_kernel<DP>, (int)smem)) return e;
   const int64_t q_tiles = (c.p.max_q + BT - 1) / BT, k_tiles = (c.p.max_k + BT - 1) / BT, sequences = c.p.sequences;
   const int64_t dkdv = c.p.k_rows > 0 ? sequences * c.p.kv_heads * k_tiles : 0, dq = c.p.q_rows > 0 ? sequences * c.p.heads * q_tiles : 0;
-  // two blocks share a tile's walk (of four tiles or more) where that takes a sixth of the rounds of two blocks to an SM away
+  // Two blocks share a tile's walk (of four tiles or more) where that takes a sixth of the rounds away.  Two blocks to an SM
+  // are counted for every head size: so many fit from 65 channels on, where this was measured (80 and 128); three do below.
   const int64_t wave = 2 * 148, rounds = (dkdv + dq + wave - 1) / wave, halves = (2 * (dkdv + dq) + wave - 1) / wave;
   const int splits = 3 * halves <= 5 * rounds && k_tiles >= 4 && c.p.heads / c.p.kv_heads * q_tiles >= 4 ? MAX_SPLITS : 1;
   cudaLaunchConfig_t cfg = {};

@@ -354,8 +354,8 @@ struct Ring {
 // a warpgroup's next tile come only after its last probabilities were used: the two warpgroups fall into step
 // so that one runs its exponentials while the tensor core works for the other.  What bounds the kernel is this
 // chain: a warp of each warpgroup shares a scheduler and its exp2 unit, 8 cycles for 32 of them, 2048 cycles for
-// 2 x 128 x 128 scores, and a round takes 3200 (64 channels, 4096 keys: 680 TFLOP/s; 830 at 80 channels, 1180 at
-// 128).  Scores in halves of a tile, issued one ahead, cost as much in waits as they save at 64 channels; four
+// 2 x 128 x 128 scores, and a round takes 3200 (4 x 4096 rows, 16 heads of 64 channels: 402 us, 684 TFLOP/s; 411 us,
+// 836 at 80 channels; 466 us, 1179 at 128).  Scores in halves of a tile, issued one ahead, cost as much in waits as they save at 64 channels; four
 // warpgroups with 64 keys each are slower (470 us for 417).  What is kept in registers over the tiles decides more:
 // with 100 bytes spilled the kernel is 5 % slower.  The accumulator is rescaled only when a row's maximum has grown
 // by more than 2^8 since the last time (probabilities stay below 2^8, the row sum in fp32): rarely after the first tile.
@@ -1200,7 +1200,8 @@ bool encode_heads(CUtensorMap* tm, const void* base, int64_t rows, int heads, in
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// one persistent block per SM; more where its table of pieces would not hold its share
+// One persistent block per SM; more where its table of pieces would not hold its share: just above 128 pieces to an SM
+// (18944 in all, counted with max_q) a second round of few blocks takes as long as the first.
 int grid_of(int total, int sms) {
   const int least = (total + MAX_PIECES - 1) / MAX_PIECES, most = total < sms ? total : sms;
   return least > most ? least : most;

@@ -225,6 +225,7 @@ cudaError_t launch_rows(const PackedCall& c, cudaStream_t s) {
 
 // Four rows at most in bf16 (2 images of 1025 tokens, 16 heads of 64: 5.9, 7.1, 11 and 22 us for 1, 2, 4 and 8 rows,
 // against 18 us of the kernel that works on tiles of 128 rows), eight in fp32, whose other kernel has no tensor core.
+// Measured with few images, where latency counts; with many, where the crossing lies is not known.
 bool attention_rows_supported(const vit_attention_problem& p, bool act_bf16) {
   return (int64_t)p.max_q * (p.heads / p.kv_heads) <= (act_bf16 ? 4 : 8);
 }
