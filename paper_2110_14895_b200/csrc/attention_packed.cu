@@ -9,7 +9,7 @@
 // staged in shared memory, rows behind the end of a sequence are zero there.  Tiles of 64 with 256 threads need
 // fewer reads of shared memory for a product, but leave one block of eight warps to an SM and a quarter of the
 // blocks.  What bounds it is the wait for a thread's own sums and reads with eight to sixteen warps on an SM:
-// 18 TFLOP/s forward and 16 backward at 16 images of 197 rows, 12 heads of 64 (103 and 308 us).  The backward pass has
+// 18 TFLOP/s forward and 16 backward at 16 images of 197 rows, 12 heads of 64 (103 and 302 us).  The backward pass has
 // two kinds of blocks, one that keeps a tile of keys and walks over the queries (dk, dv) and one that keeps a tile
 // of queries and walks over the keys (dq): seven products instead of five, but every gradient is summed by one
 // block, or by two and in order, so that results do not depend on the schedule.
@@ -182,28 +182,35 @@ check_offsets_kernel(const PackedCall c) {
     seq_range(c.p, (int)i, r, c.dev_status, true);
 }
 
-// (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out: one warp per row and head.
-// All rows of the buffers, whether a sequence covers them or not: the offsets are the caller's, and a bad one (the last
-// one among them) says nothing of how far the other sequences reach.
+// (lse log2(e), delta)[head][row], delta = sum over the head's channels of dout * out, of the rows of the sequences
+// that the gradients accept and of no others.  A block takes a few rows of one head, a warp two of them.
+constexpr int DELTA_ROWS = 2 * THREADS / 32;
 __global__ void __launch_bounds__(THREADS)
 packed_delta_kernel(const PackedCall c) {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int lane = threadIdx.x & 31;
-  const int64_t rows = c.p.q_rows;
-  for (int64_t item = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); item < rows * c.p.heads;
-       item += (int64_t)gridDim.x * (THREADS / 32)) {
-    const int64_t row = item / c.p.heads;
-    const int head = (int)(item % c.p.heads);
-    float sum = 0.f;
-    if (lane * 4 < c.p.d) {
-      const int64_t col = (int64_t)head * c.p.d + lane * 4;
-      const float4 a = load4(static_cast<const float*>(c.out) + row * c.ldo + col);
-      const float4 b = load4(static_cast<const float*>(c.dout) + row * c.lddo + col);
-      sum = fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w)));
+  const int tiles = (c.p.max_q + DELTA_ROWS - 1) / DELTA_ROWS;
+  const int head = blockIdx.x % c.p.heads, tile = blockIdx.x / c.p.heads % tiles, seq = blockIdx.x / c.p.heads / tiles;
+  SeqRange r;
+  if (!seq_range(c.p, seq, r, c.dev_status, threadIdx.x == 0)) return;
+  const int lane = threadIdx.x & 31, row0 = tile * DELTA_ROWS + 2 * (int)(threadIdx.x >> 5);
+  const int64_t col = (int64_t)head * c.p.d + lane * 4;
+  float4 a[2], b[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    a[i] = b[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (row0 + i < r.q_len && lane * 4 < c.p.d) {
+      const int64_t row = (int64_t)r.q_begin + row0 + i;
+      a[i] = load4(static_cast<const float*>(c.out) + row * c.ldo + col);
+      b[i] = load4(static_cast<const float*>(c.dout) + row * c.lddo + col);
     }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (row0 + i >= r.q_len) return;                       // the same for the whole warp
+    float sum = fmaf(a[i].x, b[i].x, fmaf(a[i].y, b[i].y, fmaf(a[i].z, b[i].z, a[i].w * b[i].w)));
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-    const int64_t at = (int64_t)head * c.p.q_rows + row;
+    const int64_t at = (int64_t)head * c.p.q_rows + r.q_begin + row0 + i;
     if (lane == 0) c.delta[at] = make_float2(c.lse[at] * 1.4426950408889634f, sum);
   }
 }
@@ -462,8 +469,7 @@ cudaError_t launch_check_offsets(const PackedCall& c, cudaStream_t s) {
   return cudaGetLastError();
 }
 cudaError_t launch_attention_delta_f32(const PackedCall& c, cudaStream_t s) {
-  const int64_t blocks = ((int64_t)c.p.q_rows * c.p.heads + THREADS / 32 - 1) / (THREADS / 32), most = 1 << 20;
-  packed_delta_kernel<<<(unsigned)(blocks < most ? blocks : most), THREADS, 0, s>>>(c);
+  packed_delta_kernel<<<(unsigned)(c.p.sequences * c.p.heads * ((c.p.max_q + DELTA_ROWS - 1) / DELTA_ROWS)), THREADS, 0, s>>>(c);
   return cudaGetLastError();
 }
 cudaError_t launch_attention_packed_grads_f32(const PackedCall& c, cudaStream_t s) {
