@@ -390,6 +390,52 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
                                      void* dq, int64_t lddq, void* dk, int64_t lddk, void* dv, int64_t lddv, void* ws,
                                      size_t ws_bytes, void* stream);
 
+/* ---- training a layer: layer norm, linear layers of one or several weight matrices, gradient clipping ------------
+ * What a training or fine-tuning loop needs beside the operations above: the other half of a layer forwards and
+ * backwards, and the step at its end.  The common rules above hold (pointers 16-byte aligned, strides in elements, at
+ * least as wide as their rows and multiples of 8, checks before anything is launched, outputs that overlap nothing
+ * unless stated, sums and statistics in 32 bits or more, results rounded once, the same call gives the same bits). */
+
+/* y[r,:] = (x[r,:] - mean) * rstd * gain + shift with rstd = 1 / sqrt(biased variance + eps), and the statistics that
+ * the gradients need: stats[2 r] = mean, stats[2 r + 1] = rstd.  (vit_op_layernorm: rows without strides, no statistics.)
+ *   x, y: activations [rows, cols]; x == y with ldx == ldy is allowed.  gain, shift: dev fp32 [cols].
+ *   stats: dev fp32 [rows][2], may be NULL.  cols: a multiple of 8, at most 8192. */
+int vit_op_layernorm_forward(vit_handle* h, int dtype, int rows, int cols, const void* x, int64_t ldx, const float* gain,
+                             const float* shift, float eps, void* y, int64_t ldy, float* stats, void* stream);
+
+/* Bytes of scratch for vit_op_layernorm_backward; 0 if an argument is invalid. */
+size_t vit_layernorm_backward_bytes(int rows, int cols);
+
+/* Gradients of vit_op_layernorm_forward from its input, its statistics and dy:
+ * dx (+ dres where dres is given: the gradient that arrives on the residual path), and the sums over rows dgain and
+ * dshift (dev fp32 [cols], overwritten; zero for no rows).
+ *   dx may be x, dy or dres with the same stride.  dres: NULL for none (lddres is not looked at then). */
+int vit_op_layernorm_backward(vit_handle* h, int dtype, int rows, int cols, const void* x, int64_t ldx, const float* gain,
+                              const float* stats, const void* dy, int64_t lddy, const void* dres, int64_t lddres, void* dx,
+                              int64_t lddx, float* dgain, float* dshift, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradients of all weights, scaled down together: norm = sqrt of the sum of all squares of all src, and
+ * dst = src * min(1, max_norm / norm) for every tensor with a dst.  Sums are taken so that neither large nor small values
+ * leave the range of 32 bits before the norm itself does.
+ * (A norm beyond fp32 is written as infinity, and the tensors are scaled by what it is.)  An infinite value makes all dst
+ * zero, and NaN in the infinite places; a value that is not a number makes all dst NaN.
+ *   tensors: HOST array of `count` entries, read before the call returns (a captured graph keeps what it said).
+ *     dst == src scales in place (and writes nothing where the norm is within the bound); dst == NULL: the tensor only
+ *     counts.  No dst may otherwise overlap a src, another dst, norm or ws.
+ *   max_norm: >= 0, may be infinity.  norm: dev fp32 [1], may be NULL. */
+typedef struct vit_tensor {
+  const void* src;        /* dev, 16-byte aligned; may be NULL if count is 0 */
+  void* dst;              /* dev, 16-byte aligned, or NULL */
+  int64_t count;          /* values, 0 ... 2^40 */
+  int32_t dtype;          /* VIT_BF16 or VIT_FP32, of src and dst */
+} vit_tensor;
+
+/* Bytes of scratch for vit_op_grad_clip with `count` tensors; 0 if count is negative or the lists are too many to count. */
+size_t vit_grad_clip_bytes(int count);
+
+int vit_op_grad_clip(vit_handle* h, const vit_tensor* tensors, int count, float max_norm, float* norm, void* ws,
+                     size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

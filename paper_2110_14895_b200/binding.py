@@ -33,7 +33,8 @@ EXPORTS = [
     "vit_profile_collect", "vit_head_static", "vit_partition", "vit_partition_categories",
     "vit_debug_wait_probe", "vit_op_rope_axes", "vit_op_qk_norm_rope", "vit_qk_norm_rope_backward_bytes",
     "vit_op_qk_norm_rope_backward", "vit_attention_packed_bytes", "vit_op_attention_packed",
-    "vit_op_attention_packed_backward",
+    "vit_op_attention_packed_backward", "vit_op_layernorm_forward", "vit_layernorm_backward_bytes", "vit_op_layernorm_backward",
+    "vit_grad_clip_bytes", "vit_op_grad_clip",
 ]
 PROF_CLASSES = ["layernorm", "qkv", "attention", "outproj", "fc1", "fc2", "embed", "head", "op"]
 
@@ -67,6 +68,10 @@ class VitAttentionProblem(Structure):
         ("max_q", c_int32), ("k_rows", c_int32), ("max_k", c_int32), ("q_offsets", c_void_p),
         ("k_offsets", c_void_p), ("scale", c_float),
     ]
+
+
+class VitTensor(Structure):
+    _fields_ = [("src", c_void_p), ("dst", c_void_p), ("count", ctypes.c_int64), ("dtype", c_int32)]
 
 
 class VitError(RuntimeError):
@@ -150,6 +155,17 @@ def lib():
     L.vit_op_attention_packed_backward.restype = c_int
     L.vit_op_attention_packed_backward.argtypes = [c_void_p, c_int, P(VitAttentionProblem)] + [c_void_p, i64] * 4 + [
         pf] + [c_void_p, i64] * 4 + [c_void_p, c_size_t, c_void_p]
+    L.vit_op_layernorm_forward.restype = c_int
+    L.vit_op_layernorm_forward.argtypes = [c_void_p, c_int, c_int, c_int, c_void_p, i64, pf, pf, c_float, c_void_p, i64, pf, c_void_p]
+    L.vit_layernorm_backward_bytes.restype = c_size_t
+    L.vit_layernorm_backward_bytes.argtypes = [c_int, c_int]
+    L.vit_op_layernorm_backward.restype = c_int
+    L.vit_op_layernorm_backward.argtypes = [c_void_p, c_int, c_int, c_int, c_void_p, i64, pf, pf] + [c_void_p, i64] * 3 + [
+        pf, pf, c_void_p, c_size_t, c_void_p]
+    L.vit_grad_clip_bytes.restype = c_size_t
+    L.vit_grad_clip_bytes.argtypes = [c_int]
+    L.vit_op_grad_clip.restype = c_int
+    L.vit_op_grad_clip.argtypes = [c_void_p, P(VitTensor), c_int, c_float, pf, c_void_p, c_size_t, c_void_p]
     L.vit_head_static.restype = c_int
     L.vit_head_static.argtypes = [c_void_p, c_int, c_void_p, c_void_p, c_void_p]
     L.vit_partition.restype = c_int
@@ -411,6 +427,36 @@ def vit_op_attention_packed_backward(h, dtype, problem, q, ldq, k, ldk, v, ldv, 
     _check(lib().vit_op_attention_packed_backward(h, dtype, _ref(problem), q, ldq, k, ldk, v, ldv, out, ldo, lse, dout,
                                                   lddo, dq, lddq, dk, lddk, dv, lddv, ws, ws_bytes, stream),
            "vit_op_attention_packed_backward")
+
+
+def vit_op_layernorm_forward(h, dtype, rows, cols, x, ldx, gain, shift, eps, y, ldy, stats, stream=0):
+    _check(lib().vit_op_layernorm_forward(h, dtype, rows, cols, x, ldx, gain, shift, eps, y, ldy, stats, stream),
+           "vit_op_layernorm_forward")
+
+
+def vit_layernorm_backward_bytes(rows, cols) -> int:
+    return lib().vit_layernorm_backward_bytes(rows, cols)
+
+
+def vit_op_layernorm_backward(h, dtype, rows, cols, x, ldx, gain, stats, dy, lddy, dres, lddres, dx, lddx, dgain, dshift,
+                              ws, ws_bytes, stream=0):
+    """`dres` may be 0: nothing is added to dx."""
+    _check(lib().vit_op_layernorm_backward(h, dtype, rows, cols, x, ldx, gain, stats, dy, lddy, dres, lddres, dx, lddx,
+                                           dgain, dshift, ws, ws_bytes, stream), "vit_op_layernorm_backward")
+
+
+def make_tensors(entries):
+    """A list of tensors for vit_op_grad_clip from (src, dst, count, dtype): device pointers, `dst` 0 for a tensor that
+    only counts.  Worth keeping where the same buffers come back every step."""
+    return (VitTensor * max(1, len(entries)))(*[VitTensor(*e) for e in entries])
+
+
+def vit_grad_clip_bytes(count) -> int:
+    return lib().vit_grad_clip_bytes(count)
+
+
+def vit_op_grad_clip(h, tensors, count, max_norm, norm, ws, ws_bytes, stream=0):
+    _check(lib().vit_op_grad_clip(h, tensors, count, max_norm, norm, ws, ws_bytes, stream), "vit_op_grad_clip")
 
 
 # ---- convenience object: owns a handle and torch-allocated buffers --------------------------------

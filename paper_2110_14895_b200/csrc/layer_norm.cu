@@ -1,0 +1,380 @@
+// Layer norm of every row with the statistics that its gradients need, and the gradients.
+//
+//   forward   y = (x - m) r g + b,  m = mean(x),  r = 1 / sqrt(mean((x - m)^2) + eps)
+//   backward  z = (x - m) r,  w = g dy:   dx = r (w - mean(w) - z mean(w z)) + dres,  dg = sum dy z,  db = sum dy
+//
+// Both are bound by memory: a row is read and written once.  One warp owns a row (four warps beyond 2048 columns) and a
+// lane the same columns of every row, eight at a time, so that the sums over rows for dg and db stay in registers.
+#include "vit_internal.h"
+#include "sm100_ptx.cuh"
+
+namespace vit {
+
+namespace {
+
+constexpr int CH = 8;                          // columns of a lane's piece: one 16-byte load in bf16, two in fp32
+constexpr int NARROW = 2048;                   // columns that one warp holds
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+
+// a piece as it lies in memory
+template <typename T> struct Raw;
+template <> struct Raw<bf16> { uint4 u; };
+template <> struct Raw<float> { float4 a, b; };
+
+__device__ __forceinline__ Raw<bf16> load_raw(const bf16* p) { return {*reinterpret_cast<const uint4*>(p)}; }
+__device__ __forceinline__ Raw<float> load_raw(const float* p) { return {reinterpret_cast<const float4*>(p)[0], reinterpret_cast<const float4*>(p)[1]}; }
+// bf16 -> fp32 is a shift (low half) or a mask (high half) of the 32-bit word
+__device__ __forceinline__ void open(const Raw<bf16>& r, float2 (&v)[4]) {
+  const uint32_t w[4] = {r.u.x, r.u.y, r.u.z, r.u.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+}
+__device__ __forceinline__ void open(const Raw<float>& r, float2 (&v)[4]) {
+  v[0] = make_float2(r.a.x, r.a.y); v[1] = make_float2(r.a.z, r.a.w);
+  v[2] = make_float2(r.b.x, r.b.y); v[3] = make_float2(r.b.z, r.b.w);
+}
+__device__ __forceinline__ void store_piece(bf16* p, const float2 (&v)[4]) {
+  uint4 o;
+  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&o);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) h[e] = __floats2bfloat162_rn(v[e].x, v[e].y);
+  *reinterpret_cast<uint4*>(p) = o;
+}
+__device__ __forceinline__ void store_piece(float* p, const float2 (&v)[4]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
+}
+
+// Sums over a row's warps: one, or the four of a group of 128 threads, which meet at a barrier of their own.  Two slots,
+// used in turn, keep a late reader from the next sum's writers.
+template <int WPR>
+__device__ __forceinline__ float2 row_sums(float2 v, float2 (*slots)[4], int& turn) {
+  v.x = warp_sum(v.x);
+  v.y = warp_sum(v.y);
+  if (WPR == 1) return v;
+  const int warp = threadIdx.x >> 5, group = warp / WPR;
+  float2* s = slots[2 * group + turn];
+  turn ^= 1;
+  if ((threadIdx.x & 31) == 0) s[warp % WPR] = v;
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(WPR * 32) : "memory");
+  float2 t = s[0];
+#pragma unroll
+  for (int i = 1; i < WPR; ++i) t = make_float2(t.x + s[i].x, t.y + s[i].y);
+  return t;
+}
+
+struct ForwardArgs {
+  const void* x; int64_t ldx;
+  const float *gain, *shift;
+  float eps;
+  void* y; int64_t ldy;
+  float2* stats;
+  int rows, cols;
+};
+
+template <typename T, int NCH, int WPR>
+__global__ void __launch_bounds__(256)
+layer_norm_kernel(const ForwardArgs p) {
+  __shared__ float2 slots[2 * 8 / WPR][4];
+  const int warp = threadIdx.x >> 5, at = (warp % WPR) * 32 + (threadIdx.x & 31);
+  const int64_t row = (int64_t)blockIdx.x * (8 / WPR) + warp / WPR;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
+  if (row >= p.rows) return;                    // all warps of a row together
+  const int pieces = p.cols / CH;
+  const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+  Raw<T> raw[NCH];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)                 // all loads in flight before the first use
+    if (at + 32 * WPR * i < pieces) raw[i] = load_raw(x + (at + 32 * WPR * i) * CH);
+  int turn = 0;
+  float2 v[NCH][4], sum = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)
+    if (at + 32 * WPR * i < pieces) {
+      open(raw[i], v[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum = __fadd2_rn(sum, v[i][e]);
+    }
+  const float mean = row_sums<WPR>(make_float2(sum.x + sum.y, 0.f), slots, turn).x / (float)p.cols;
+  sum = make_float2(0.f, 0.f);
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)
+    if (at + 32 * WPR * i < pieces) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[i][e] = __fadd2_rn(v[i][e], twice(-mean));
+        sum = __ffma2_rn(v[i][e], v[i][e], sum);
+      }
+    }
+  const float rstd = 1.0f / sqrtf(row_sums<WPR>(make_float2(sum.x + sum.y, 0.f), slots, turn).x / (float)p.cols + p.eps);
+  if (at == 0 && p.stats) p.stats[row] = make_float2(mean, rstd);
+  T* y = static_cast<T*>(p.y) + row * p.ldy;
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int c = (at + 32 * WPR * i) * CH;
+    if (c < p.cols) {
+      float2 g[4], b[4];
+      open(load_raw(p.gain + c), g);
+      open(load_raw(p.shift + c), b);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[i][e] = __ffma2_rn(__fmul2_rn(v[i][e], twice(rstd)), g[e], b[e]);
+      store_piece(y + c, v[i]);
+    }
+  }
+}
+
+struct BackwardArgs {
+  const void* x; int64_t ldx;
+  const float* gain;
+  const float2* stats;
+  const void* dy; int64_t lddy;
+  const void* dres; int64_t lddres;
+  void* dx; int64_t lddx;
+  float* partial;                               // [blocks][2][cols]
+  int rows, cols, stages;
+};
+
+// A warp's rows come through a ring in shared memory, `stages` rows ahead.  A lane copies what it will read itself, so that
+// no two threads have to meet over it, and the registers are left to the sums of dg and db.
+template <typename T, int NCH, int WPR, int WARPS>
+__global__ void __launch_bounds__(WARPS * 32, 1)
+layer_norm_backward_kernel(const BackwardArgs p) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ float2 slots[2 * WARPS / WPR][4];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, at = (warp % WPR) * 32 + lane;
+  const int64_t step = (int64_t)gridDim.x * (WARPS / WPR);
+  float* gain = reinterpret_cast<float*>(smem);                            // [cols]
+  const int arrays = p.dres ? 3 : 2;
+  const uint32_t row_bytes = (uint32_t)p.cols * sizeof(T), stage_bytes = row_bytes * arrays;
+  uint8_t* ring = smem + (size_t)p.cols * 4 + (size_t)(warp / WPR) * p.stages * stage_bytes;
+  for (int i = threadIdx.x; i < p.cols; i += WARPS * 32) gain[i] = p.gain[i];
+  __syncthreads();
+
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < p.rows) {
+      const uint32_t to = ptx::smem_u32(ring + stage * stage_bytes);
+      const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+      const T* dy = static_cast<const T*>(p.dy) + row * p.lddy;
+      const T* dres = static_cast<const T*>(p.dres) + row * p.lddres;
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int c = (at + 32 * WPR * i) * CH;
+        if (c < p.cols) {
+#pragma unroll
+          for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            const int e = c + h * (16 / (int)sizeof(T));
+            const uint32_t off = to + (uint32_t)e * sizeof(T);
+            ptx::cp_async_16(off, x + e, 16);
+            ptx::cp_async_16(off + row_bytes, dy + e, 16);
+            if (p.dres) ptx::cp_async_16(off + 2 * row_bytes, dres + e, 16);
+          }
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");      // an empty group where there is no row
+  };
+  float2 dg[NCH][4], db[NCH][4];
+#pragma unroll
+  for (int i = 0; i < NCH; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) dg[i][e] = db[i][e] = make_float2(0.f, 0.f);
+  const float inv = 1.0f / (float)p.cols;
+  int64_t row = (int64_t)blockIdx.x * (WARPS / WPR) + warp / WPR;
+  for (int s = 0; s < p.stages - 1; ++s) fetch(row + s * step, s);
+  float2 st = row < p.rows ? p.stats[row] : make_float2(0.f, 0.f);
+  int stage = 0, turn = 0;
+  for (; row < p.rows; row += step) {
+    int ahead = stage + p.stages - 1;
+    if (ahead >= p.stages) ahead -= p.stages;
+    fetch(row + (p.stages - 1) * step, ahead);
+    const float2 st_next = row + step < p.rows ? p.stats[row + step] : st;
+    if (p.stages == 3) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else asm volatile("cp.async.wait_group 1;" ::: "memory");
+    const T* xs = reinterpret_cast<const T*>(ring + stage * stage_bytes);
+    const T* ds = reinterpret_cast<const T*>(ring + stage * stage_bytes + row_bytes);
+    const float2 nm = twice(-st.x), r = twice(st.y);
+    float2 s1 = make_float2(0.f, 0.f), s2 = s1;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = (at + 32 * WPR * i) * CH;
+      if (c < p.cols) {
+        float2 z[4], d[4], g[4];
+        open(load_raw(xs + c), z);
+        open(load_raw(ds + c), d);
+        open(load_raw(gain + c), g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          z[e] = __fmul2_rn(__fadd2_rn(z[e], nm), r);
+          dg[i][e] = __ffma2_rn(d[e], z[e], dg[i][e]);
+          db[i][e] = __fadd2_rn(d[e], db[i][e]);
+          d[e] = __fmul2_rn(d[e], g[e]);
+          s1 = __fadd2_rn(s1, d[e]);
+          s2 = __ffma2_rn(d[e], z[e], s2);
+        }
+      }
+    }
+    const float2 sums = row_sums<WPR>(make_float2(s1.x + s1.y, s2.x + s2.y), slots, turn);
+    const float2 c1 = twice(-sums.x * inv), c2 = twice(-sums.y * inv);
+    T* dx = static_cast<T*>(p.dx) + row * p.lddx;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = (at + 32 * WPR * i) * CH;
+      if (c < p.cols) {
+        float2 z[4], d[4], g[4];
+        open(load_raw(xs + c), z);
+        open(load_raw(ds + c), d);
+        open(load_raw(gain + c), g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          z[e] = __fmul2_rn(__fadd2_rn(z[e], nm), r);
+          d[e] = __fmul2_rn(r, __ffma2_rn(z[e], c2, __ffma2_rn(d[e], g[e], c1)));
+        }
+        if (p.dres) {
+          open(load_raw(ds + p.cols + c), g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d[e] = __fadd2_rn(d[e], g[e]);
+        }
+        store_piece(dx + c, d);
+      }
+    }
+    st = st_next;
+    if (++stage == p.stages) stage = 0;
+  }
+  ptx::grid_launch_dependents();
+  // this block's share of dg and db: its rows' warps are added in a fixed order
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncthreads();
+  float* share = reinterpret_cast<float*>(smem + (size_t)p.cols * 4);      // [WARPS / WPR][2][cols]
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int c = (at + 32 * WPR * i) * CH;
+    if (c < p.cols) {
+      store_piece(share + (size_t)(warp / WPR) * 2 * p.cols + c, dg[i]);
+      store_piece(share + (size_t)(warp / WPR) * 2 * p.cols + p.cols + c, db[i]);
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * p.cols; i += WARPS * 32) {
+    float sum = 0.f;
+    for (int w = 0; w < WARPS / WPR; ++w) sum += share[(size_t)w * 2 * p.cols + i];
+    p.partial[(int64_t)blockIdx.x * 2 * p.cols + i] = sum;
+  }
+}
+
+// dgain[c], dshift[c] = sum of the blocks' shares, in a fixed order: 8 columns (a sector) to a block, 32 threads to a column
+__global__ void __launch_bounds__(256)
+column_grad_kernel(const float* __restrict__ partial, int blocks, int cols, float* __restrict__ dgain, float* __restrict__ dshift) {
+  __shared__ float sums[8][8];
+  const int column = threadIdx.x & 7, part = threadIdx.x >> 3, i = blockIdx.x * 8 + column;
+  ptx::grid_dependency_wait();                           // the shares are written by the kernel before this one
+  float sum = 0.f;
+#pragma unroll 5
+  for (int b = part; b < blocks; b += 32) sum += partial[(int64_t)b * 2 * cols + i];
+  sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+  sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+  if ((threadIdx.x & 31) < 8) sums[threadIdx.x >> 5][column] = sum;
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    sum = 0.f;
+#pragma unroll
+    for (int b = 0; b < 8; ++b) sum += sums[b][column];
+    (i < cols ? dgain : dshift)[i < cols ? i : i - cols] = sum;
+  }
+}
+
+template <typename Kernel, typename... Args>
+cudaError_t launch_after(Kernel kernel, int grid, int threads, size_t smem, cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <typename T, int NCH, int WPR>
+cudaError_t launch_forward(const ForwardArgs& a, cudaStream_t s) {
+  return launch_after(layer_norm_kernel<T, NCH, WPR>, (a.rows + 8 / WPR - 1) / (8 / WPR), 256, 0, s, a);
+}
+template <typename T>
+cudaError_t dispatch_forward(const ForwardArgs& a, cudaStream_t s) {
+  const int per_warp = (a.cols + 32 * CH - 1) / (32 * CH);
+  if (a.cols <= NARROW) switch (per_warp) {
+    case 1: return launch_forward<T, 1, 1>(a, s);
+    case 2: return launch_forward<T, 2, 1>(a, s);
+    case 3: return launch_forward<T, 3, 1>(a, s);
+    case 4: return launch_forward<T, 4, 1>(a, s);
+    case 5: return launch_forward<T, 5, 1>(a, s);
+    case 6: return launch_forward<T, 6, 1>(a, s);
+    default: return launch_forward<T, 8, 1>(a, s);
+  }
+  return per_warp <= 16 ? launch_forward<T, 4, 4>(a, s) : launch_forward<T, 8, 4>(a, s);
+}
+
+constexpr int RING_BYTES = 200 * 1024;          // of shared memory
+
+template <typename T, int NCH, int WPR, int WARPS>
+cudaError_t launch_backward(BackwardArgs a, cudaStream_t s, int* blocks) {
+  static PerDeviceFlag done;
+  auto kernel = layer_norm_backward_kernel<T, NCH, WPR, WARPS>;
+  if (cudaError_t e = ensure_dynamic_smem(done, kernel, 225 * 1024)) return e;
+  const size_t stage = (size_t)(WARPS / WPR) * a.cols * sizeof(T) * (a.dres ? 3 : 2);
+  a.stages = 3 * stage <= RING_BYTES ? 3 : 2;
+  size_t smem = a.stages * stage;
+  const size_t share = (size_t)(WARPS / WPR) * 2 * a.cols * sizeof(float);
+  if (smem < share) smem = share;
+  smem += (size_t)a.cols * sizeof(float);
+  const int64_t want = ((int64_t)a.rows + WARPS / WPR - 1) / (WARPS / WPR);
+  const int sms = current_device_sm_count();
+  *blocks = (int)(want < sms ? want : sms);
+  if (*blocks > LAYER_NORM_MAX_BLOCKS) *blocks = LAYER_NORM_MAX_BLOCKS;
+  kernel<<<*blocks, WARPS * 32, smem, s>>>(a);
+  return cudaGetLastError();
+}
+// Twelve warps where their sums leave each thread enough of the registers (64 sums at 1024 columns), eight beyond; fp32 rows
+// wider than 1024 columns would not leave room for a ring of twelve.
+template <typename T>
+cudaError_t dispatch_backward(const BackwardArgs& a, cudaStream_t s, int* blocks) {
+  const int per_warp = (a.cols + 32 * CH - 1) / (32 * CH);
+  if (a.cols <= NARROW) switch (per_warp) {
+    case 1: return launch_backward<T, 1, 1, 12>(a, s, blocks);
+    case 2: return launch_backward<T, 2, 1, 12>(a, s, blocks);
+    case 3: return launch_backward<T, 3, 1, 12>(a, s, blocks);
+    case 4: return launch_backward<T, 4, 1, sizeof(T) == 2 ? 12 : 8>(a, s, blocks);
+    case 5: return launch_backward<T, 5, 1, sizeof(T) == 2 ? 12 : 6>(a, s, blocks);
+    case 6: return launch_backward<T, 6, 1, sizeof(T) == 2 ? 8 : 5>(a, s, blocks);
+    default: return launch_backward<T, 8, 1, sizeof(T) == 2 ? 8 : 4>(a, s, blocks);
+  }
+  if (per_warp <= 16) return launch_backward<T, 4, 4, sizeof(T) == 2 ? 12 : 8>(a, s, blocks);
+  return launch_backward<T, 8, 4, sizeof(T) == 2 ? 8 : 4>(a, s, blocks);
+}
+
+}  // namespace
+
+cudaError_t launch_layer_norm(const LayerNormCall& c, cudaStream_t s) {
+  const ForwardArgs a{c.x, c.ldx, c.gain, c.shift, c.eps, c.y, c.ldy, c.stats, c.rows, c.cols};
+  return c.act_bf16 ? dispatch_forward<bf16>(a, s) : dispatch_forward<float>(a, s);
+}
+
+cudaError_t launch_layer_norm_backward(const LayerNormCall& c, float* partial, int* blocks, cudaStream_t s) {
+  const BackwardArgs a{c.x, c.ldx, c.gain, c.stats, c.dy, c.lddy, c.dres, c.lddres, c.dx, c.lddx, partial, c.rows, c.cols, 0};
+  return c.act_bf16 ? dispatch_backward<bf16>(a, s, blocks) : dispatch_backward<float>(a, s, blocks);
+}
+
+cudaError_t launch_column_grad(const float* partial, int blocks, int cols, float* dgain, float* dshift, cudaStream_t s) {
+  return launch_after(column_grad_kernel, 2 * cols / 8, 256, 0, s, partial, blocks, cols, dgain, dshift);
+}
+
+}  // namespace vit

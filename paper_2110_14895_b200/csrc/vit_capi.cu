@@ -4,6 +4,7 @@
 #include "vit_internal.h"
 
 #include <cuda_bf16.h>
+#include <algorithm>
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
@@ -301,6 +302,44 @@ size_t attention_delta_bytes(const vit_attention_problem& p) { return align_up((
 size_t attention_packed_ws(int dtype, const vit_attention_problem& p, bool backward) {
   if (!backward) return 0;
   return attention_delta_bytes(p) + (dtype == VIT_BF16 ? align_up(attention_partial_floats(p) * sizeof(float), 256) : 0);
+}
+
+bool layer_norm_ok(int dtype, int rows, int cols) {
+  return (dtype == VIT_BF16 || dtype == VIT_FP32) && rows >= 0 && cols >= 8 && cols % 8 == 0 && cols <= LAYER_NORM_MAX_COLS;
+}
+size_t layer_norm_backward_ws(int rows, int cols) {
+  return (size_t)(rows < LAYER_NORM_MAX_BLOCKS ? (rows > 0 ? rows : 1) : LAYER_NORM_MAX_BLOCKS) * 2 * cols * sizeof(float);
+}
+
+// Whether a list of tensors may be scaled: nothing that is written lies over anything else, but for a tensor in place.
+struct Span { uintptr_t begin, end; bool write; };
+int clip_list_status(const vit_tensor* t, int n, const void* norm, const void* ws, size_t ws_bytes) {
+  std::vector<Span> spans;
+  spans.reserve(2 * (size_t)n + 2);
+  auto add = [&](const void* p, size_t bytes, bool write) {
+    if (p && bytes) spans.push_back(Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, write});
+  };
+  int64_t values = 0;
+  for (int i = 0; i < n; ++i) {
+    if (t[i].dtype != VIT_BF16 && t[i].dtype != VIT_FP32) return VIT_ERR_INVALID_ARG;
+    if (t[i].count < 0 || t[i].count > (int64_t)1 << 40 || misaligned(t[i].src) || misaligned(t[i].dst) || (t[i].count > 0 && !t[i].src))
+      return VIT_ERR_INVALID_ARG;
+    values += t[i].count;
+    if (values > (int64_t)1 << 42) return VIT_ERR_TOO_LARGE;             // pieces of 4096 are counted in 32 bits
+    const size_t bytes = (size_t)t[i].count * (t[i].dtype == VIT_BF16 ? 2 : 4);
+    add(t[i].src, bytes, t[i].dst == t[i].src);
+    if (t[i].dst != t[i].src) add(t[i].dst, bytes, true);
+  }
+  add(norm, sizeof(float), true);
+  add(ws, ws_bytes, true);
+  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  uintptr_t read_to = 0, written_to = 0;
+  for (const Span& s : spans) {
+    if (s.begin < written_to || (s.write && s.begin < read_to)) return VIT_ERR_INVALID_ARG;
+    uintptr_t& to = s.write ? written_to : read_to;
+    if (s.end > to) to = s.end;
+  }
+  return VIT_OK;
 }
 
 }  // namespace
@@ -943,6 +982,94 @@ int vit_op_attention_packed_backward(vit_handle* h, int dtype, const vit_attenti
   if (queries) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dq_bf16(c, s));
   if (keys) VIT_LAUNCH(h, VIT_PROF_ATTENTION, launch_attention_packed_dkdv_bf16(c, s));
   h->launches.fetch_add((queries && attention_in_parts(p, false)) + (keys && attention_in_parts(p, true)), std::memory_order_relaxed);
+  return VIT_OK;
+}
+
+int vit_op_layernorm_forward(vit_handle* h, int dtype, int rows, int cols, const void* x, int64_t ldx, const float* gain,
+                             const float* shift, float eps, void* y, int64_t ldy, float* stats, void* stream) {
+  if (!h || !layer_norm_ok(dtype, rows, cols) || !gain || !shift || misaligned(gain) || misaligned(shift) || misaligned(stats) ||
+      !(eps >= 0.f) || !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
+  const size_t es = element_bytes(dtype);
+  const Block bx{x, rows, cols, ldx, es}, by{y, rows, cols, ldy, es}, bs{stats, stats ? 1 : 0, (int64_t)2 * rows, (int64_t)2 * rows, 4};
+  const Block bg{gain, 1, cols, cols, 4}, bb{shift, 1, cols, cols, 4};
+  if (!block_ok(bx) || !block_ok(by) || (!same_block(bx, by) && blocks_overlap(bx, by)) || blocks_overlap(bs, bx) || blocks_overlap(bs, by))
+    return VIT_ERR_INVALID_ARG;
+  for (const Block* b : {&by, &bs})
+    if (blocks_overlap(*b, bg) || blocks_overlap(*b, bb)) return VIT_ERR_INVALID_ARG;
+  if (rows == 0) return VIT_OK;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  LayerNormCall c{};
+  c.act_bf16 = dtype == VIT_BF16; c.rows = rows; c.cols = cols; c.x = x; c.ldx = ldx; c.gain = gain; c.shift = shift; c.eps = eps;
+  c.y = y; c.ldy = ldy; c.stats = reinterpret_cast<float2*>(stats);
+  VIT_LAUNCH(h, VIT_PROF_LAYERNORM, launch_layer_norm(c, s));
+  return VIT_OK;
+}
+
+size_t vit_layernorm_backward_bytes(int rows, int cols) {
+  return layer_norm_ok(VIT_BF16, rows, cols) ? layer_norm_backward_ws(rows, cols) : 0;
+}
+
+int vit_op_layernorm_backward(vit_handle* h, int dtype, int rows, int cols, const void* x, int64_t ldx, const float* gain,
+                              const float* stats, const void* dy, int64_t lddy, const void* dres, int64_t lddres, void* dx,
+                              int64_t lddx, float* dgain, float* dshift, void* ws, size_t ws_bytes, void* stream) {
+  if (!h || !layer_norm_ok(dtype, rows, cols) || !gain || misaligned(gain) || (rows > 0 && !stats) || misaligned(stats) || !dgain ||
+      misaligned(dgain) || !dshift || misaligned(dshift) || !ws || misaligned(ws) || !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
+  const size_t es = element_bytes(dtype), need = layer_norm_backward_ws(rows, cols);
+  const Block bx{x, rows, cols, ldx, es}, bdy{dy, rows, cols, lddy, es}, bdx{dx, rows, cols, lddx, es};
+  const Block br{dres, dres ? rows : 0, cols, dres ? lddres : cols, es};
+  const Block bst{stats, 1, (int64_t)2 * rows, (int64_t)2 * rows, 4}, bg{gain, 1, cols, cols, 4};
+  const Block to[] = {bdx, {dgain, 1, cols, cols, 4}, {dshift, 1, cols, cols, 4}, {ws, 1, (int64_t)need, (int64_t)need, 1}};
+  if (!block_ok(bx) || !block_ok(bdy) || !block_ok(bdx) || !block_ok(br)) return VIT_ERR_INVALID_ARG;
+  for (int i = 0; i < 4; ++i) {
+    for (const Block* b : {&bx, &bdy, &br})
+      if (blocks_overlap(to[i], *b) && !(i == 0 && same_block(bdx, *b))) return VIT_ERR_INVALID_ARG;
+    if (blocks_overlap(to[i], bst) || blocks_overlap(to[i], bg)) return VIT_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (blocks_overlap(to[i], to[j])) return VIT_ERR_INVALID_ARG;
+  }
+  if (ws_bytes < need) return VIT_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  LayerNormCall c{};
+  c.act_bf16 = dtype == VIT_BF16; c.rows = rows; c.cols = cols; c.x = x; c.ldx = ldx; c.gain = gain;
+  c.stats = reinterpret_cast<float2*>(const_cast<float*>(stats)); c.dy = dy; c.lddy = lddy; c.dres = dres; c.lddres = lddres;
+  c.dx = dx; c.lddx = lddx;
+  int blocks = 0;
+  if (rows > 0) VIT_LAUNCH(h, VIT_PROF_LAYERNORM, launch_layer_norm_backward(c, static_cast<float*>(ws), &blocks, s));
+  VIT_LAUNCH(h, VIT_PROF_LAYERNORM, launch_column_grad(static_cast<const float*>(ws), blocks, cols, dgain, dshift, s));
+  return VIT_OK;
+}
+
+size_t vit_grad_clip_bytes(int count) {
+  if (count < 0) return 0;
+  return (size_t)grad_clip_lists(count) * GRAD_CLIP_MAX_BLOCKS * sizeof(double);
+}
+
+int vit_op_grad_clip(vit_handle* h, const vit_tensor* tensors, int count, float max_norm, float* norm, void* ws,
+                     size_t ws_bytes, void* stream) {
+  if (!h || count < 0 || (count > 0 && !tensors) || !(max_norm >= 0.f) || misaligned(norm) || !ws || misaligned(ws) || !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
+  const size_t need = vit_grad_clip_bytes(count);
+  int st;
+  try {
+    st = clip_list_status(tensors, count, norm, ws, need);
+  } catch (const std::bad_alloc&) {
+    st = VIT_ERR_TOO_LARGE;
+  }
+  if (st != VIT_OK) return st;
+  if (ws_bytes < need) return VIT_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  double* partial = static_cast<double*>(ws);
+  const int lists = grad_clip_lists(count);
+  int partials = 0;
+  for (int i = 0; i < lists; ++i) {
+    int some = 0;
+    VIT_LAUNCH(h, VIT_PROF_OP, launch_grad_clip(tensors, count, i, false, partial + partials, &some, max_norm, nullptr, s));
+    partials += some;
+  }
+  for (int i = 0; i < lists; ++i)
+    VIT_LAUNCH(h, VIT_PROF_OP, launch_grad_clip(tensors, count, i, true, partial, &partials, max_norm, i == 0 ? norm : nullptr, s));
   return VIT_OK;
 }
 

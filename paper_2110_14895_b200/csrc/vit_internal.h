@@ -200,6 +200,32 @@ cudaError_t launch_attention_packed_grads_f32(const PackedCall& c, cudaStream_t 
 cudaError_t launch_attention_packed_dq_bf16(const PackedCall& c, cudaStream_t s);
 cudaError_t launch_attention_packed_dkdv_bf16(const PackedCall& c, cudaStream_t s);
 
+// layer norm with the rows' statistics, and its gradients (layer_norm.cu)
+struct LayerNormCall {
+  bool act_bf16;
+  int rows, cols;
+  const void* x;    int64_t ldx;
+  const float *gain, *shift;
+  float eps;
+  void* y;          int64_t ldy;
+  float2* stats;                        // [rows] (mean, 1 / sqrt(var + eps)); read by the backward pass
+  const void* dy;   int64_t lddy;
+  const void* dres; int64_t lddres;     // nullptr: nothing is added to dx
+  void* dx;         int64_t lddx;
+};
+constexpr int LAYER_NORM_MAX_COLS = 8192;
+constexpr int LAYER_NORM_MAX_BLOCKS = 256;          // of the backward pass, each with its share of the columns' sums
+cudaError_t launch_layer_norm(const LayerNormCall& c, cudaStream_t s);
+// partial: [blocks][2][cols], *blocks <= LAYER_NORM_MAX_BLOCKS is set
+cudaError_t launch_layer_norm_backward(const LayerNormCall& c, float* partial, int* blocks, cudaStream_t s);
+cudaError_t launch_column_grad(const float* partial, int blocks, int cols, float* dgain, float* dshift, cudaStream_t s);
+
+// norm of many tensors and their scaling (grad_clip.cu), in lists of tensors that fit a launch's parameters
+constexpr int GRAD_CLIP_MAX_BLOCKS = 148 * 8;       // of one list, each with its part of the sum
+int grad_clip_lists(int tensors);
+cudaError_t launch_grad_clip(const vit_tensor* tensors, int count, int index, bool clip, double* partial, int* partials, float bound,
+                             float* norm, cudaStream_t s);
+
 cudaError_t launch_wait_probe(long long limit_cycles, int* dev_status, cudaStream_t s);
 // *snapshot = atomic exchange of *status with 0, on stream s
 cudaError_t launch_status_take(int* status, int* snapshot, cudaStream_t s);
