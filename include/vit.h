@@ -414,6 +414,48 @@ int vit_op_layernorm_backward(vit_handle* h, int dtype, int rows, int cols, cons
                               const float* stats, const void* dy, int64_t lddy, const void* dres, int64_t lddres, void* dx,
                               int64_t lddx, float* dgain, float* dshift, void* ws, size_t ws_bytes, void* stream);
 
+/* Linear layers whose rows come in groups, each with weights of its own: tokens sorted by expert.  One group is an
+ * ordinary linear layer (vit_op_linear's product with strides, and the gradients that it lacks).
+ * The rows of group g are offsets[g] ... offsets[g+1] - 1.  The offsets are read on the device.  A group whose offsets are
+ * out of order or reach outside the rows is skipped, its rows (or weights' gradients) are left as they were, and
+ * vit_check_status reports VIT_ERR_OFFSETS; the other groups are computed; where a step backwards makes two of them
+ * overlap, what is written to the rows that they share is undefined.  Rows that no group covers are left as they were. */
+typedef struct vit_grouped_problem {
+  int32_t groups;                     /* >= 1 */
+  int32_t rows;                       /* of the activations; at most INT32_MAX - 1024 */
+  int32_t in_features, out_features;  /* multiples of 8 */
+  const int32_t* offsets;             /* dev [groups + 1], or NULL for one group of all rows */
+} vit_grouped_problem;
+
+/* out[r,:] = f(x[r,:] . w[g]^T + bias[g]) for the rows r of every group g.
+ *   x: activations [rows, in_features]; out: [rows, out_features]; w: [groups][out_features][in_features] in the
+ *   activation type; bias: dev fp32 [groups][out_features], or NULL for none.
+ *   epilogue: 0 = none, 1 = erf-GELU, 2 = add residual [rows, out_features] (residual == out with the same stride is allowed;
+ *   residual is not looked at otherwise).  pre: with epilogue 1, NULL or [rows, out_features]: receives the argument of the
+ *   GELU, which its gradient needs; not looked at otherwise.
+ * Sums are fp32.  The GELU is taken of the sums before they are rounded. */
+int vit_op_linear_grouped(vit_handle* h, int dtype, const vit_grouped_problem* problem, const void* x, int64_t ldx,
+                          const void* w, const float* bias, int epilogue, const void* residual, int64_t ldr, void* out,
+                          int64_t ldo, void* pre, int64_t ldp, void* stream);
+
+/* Gradient of its rows: dx[r,:] = (dout[r,:] . w[g]) * gelu'(pre[r,:]).  pre: [rows, in_features], the argument of a GELU
+ * that made x (so that dx is the gradient of that argument), or NULL for no such factor; pre == dx with the same stride is
+ * allowed.  dx: [rows, in_features]. */
+int vit_op_linear_grouped_backward_input(vit_handle* h, int dtype, const vit_grouped_problem* problem, const void* dout,
+                                         int64_t lddout, const void* w, const void* pre, int64_t ldp, void* dx,
+                                         int64_t lddx, void* stream);
+
+/* Bytes of scratch for vit_op_linear_grouped_backward_weights; 0 if an argument is invalid or the problem is too large. */
+size_t vit_linear_grouped_backward_weights_bytes(int dtype, const vit_grouped_problem* problem);
+
+/* Gradients of its weights: dw[g] = sum over the rows r of group g of dout[r,:]^T x[r,:] ([groups][out_features]
+ * [in_features], activation type) and dbias[g] = sum of dout[r,:] (dev fp32 [groups][out_features], or NULL for none).  Both
+ * are overwritten, with zeros for a group without rows.  Long sums are cut where the lengths of all groups of the call say,
+ * so that beside other groups the last bit may differ. */
+int vit_op_linear_grouped_backward_weights(vit_handle* h, int dtype, const vit_grouped_problem* problem, const void* x,
+                                           int64_t ldx, const void* dout, int64_t lddout, void* dw, float* dbias, void* ws,
+                                           size_t ws_bytes, void* stream);
+
 /* The gradients of all weights, scaled down together: norm = sqrt of the sum of all squares of all src, and
  * dst = src * min(1, max_norm / norm) for every tensor with a dst.  Sums are taken so that neither large nor small values
  * leave the range of 32 bits before the norm itself does.

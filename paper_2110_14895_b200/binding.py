@@ -34,7 +34,8 @@ EXPORTS = [
     "vit_debug_wait_probe", "vit_op_rope_axes", "vit_op_qk_norm_rope", "vit_qk_norm_rope_backward_bytes",
     "vit_op_qk_norm_rope_backward", "vit_attention_packed_bytes", "vit_op_attention_packed",
     "vit_op_attention_packed_backward", "vit_op_layernorm_forward", "vit_layernorm_backward_bytes", "vit_op_layernorm_backward",
-    "vit_grad_clip_bytes", "vit_op_grad_clip",
+    "vit_op_linear_grouped", "vit_op_linear_grouped_backward_input", "vit_linear_grouped_backward_weights_bytes",
+    "vit_op_linear_grouped_backward_weights", "vit_grad_clip_bytes", "vit_op_grad_clip",
 ]
 PROF_CLASSES = ["layernorm", "qkv", "attention", "outproj", "fc1", "fc2", "embed", "head", "op"]
 
@@ -67,6 +68,12 @@ class VitAttentionProblem(Structure):
         ("sequences", c_int32), ("heads", c_int32), ("kv_heads", c_int32), ("d", c_int32), ("q_rows", c_int32),
         ("max_q", c_int32), ("k_rows", c_int32), ("max_k", c_int32), ("q_offsets", c_void_p),
         ("k_offsets", c_void_p), ("scale", c_float),
+    ]
+
+
+class VitGroupedProblem(Structure):
+    _fields_ = [
+        ("groups", c_int32), ("rows", c_int32), ("in_features", c_int32), ("out_features", c_int32), ("offsets", c_void_p),
     ]
 
 
@@ -162,6 +169,17 @@ def lib():
     L.vit_op_layernorm_backward.restype = c_int
     L.vit_op_layernorm_backward.argtypes = [c_void_p, c_int, c_int, c_int, c_void_p, i64, pf, pf] + [c_void_p, i64] * 3 + [
         pf, pf, c_void_p, c_size_t, c_void_p]
+    L.vit_op_linear_grouped.restype = c_int
+    L.vit_op_linear_grouped.argtypes = [c_void_p, c_int, P(VitGroupedProblem), c_void_p, i64, c_void_p, pf, c_int, c_void_p, i64,
+                                        c_void_p, i64, c_void_p, i64, c_void_p]
+    L.vit_op_linear_grouped_backward_input.restype = c_int
+    L.vit_op_linear_grouped_backward_input.argtypes = [c_void_p, c_int, P(VitGroupedProblem), c_void_p, i64, c_void_p, c_void_p, i64,
+                                                       c_void_p, i64, c_void_p]
+    L.vit_linear_grouped_backward_weights_bytes.restype = c_size_t
+    L.vit_linear_grouped_backward_weights_bytes.argtypes = [c_int, P(VitGroupedProblem)]
+    L.vit_op_linear_grouped_backward_weights.restype = c_int
+    L.vit_op_linear_grouped_backward_weights.argtypes = [c_void_p, c_int, P(VitGroupedProblem), c_void_p, i64, c_void_p, i64, c_void_p,
+                                                         pf, c_void_p, c_size_t, c_void_p]
     L.vit_grad_clip_bytes.restype = c_size_t
     L.vit_grad_clip_bytes.argtypes = [c_int]
     L.vit_op_grad_clip.restype = c_int
@@ -443,6 +461,33 @@ def vit_op_layernorm_backward(h, dtype, rows, cols, x, ldx, gain, stats, dy, ldd
     """`dres` may be 0: nothing is added to dx."""
     _check(lib().vit_op_layernorm_backward(h, dtype, rows, cols, x, ldx, gain, stats, dy, lddy, dres, lddres, dx, lddx,
                                            dgain, dshift, ws, ws_bytes, stream), "vit_op_layernorm_backward")
+
+
+def make_grouped_problem(groups, rows, in_features, out_features, offsets) -> VitGroupedProblem:
+    """Rows in groups: device pointer of int32 offsets [groups + 1], 0 for one group of all rows."""
+    return VitGroupedProblem(groups, rows, in_features, out_features, offsets)
+
+
+def vit_op_linear_grouped(h, dtype, problem, x, ldx, w, bias, epilogue, residual, ldr, out, ldo, pre, ldp, stream=0):
+    """`bias`, `residual` and `pre` may be 0."""
+    _check(lib().vit_op_linear_grouped(h, dtype, _ref(problem), x, ldx, w, bias, epilogue, residual, ldr, out, ldo, pre, ldp,
+                                       stream), "vit_op_linear_grouped")
+
+
+def vit_op_linear_grouped_backward_input(h, dtype, problem, dout, lddout, w, pre, ldp, dx, lddx, stream=0):
+    """`pre` may be 0: no GELU before the layer."""
+    _check(lib().vit_op_linear_grouped_backward_input(h, dtype, _ref(problem), dout, lddout, w, pre, ldp, dx, lddx, stream),
+           "vit_op_linear_grouped_backward_input")
+
+
+def vit_linear_grouped_backward_weights_bytes(dtype, problem) -> int:
+    return lib().vit_linear_grouped_backward_weights_bytes(dtype, _ref(problem))
+
+
+def vit_op_linear_grouped_backward_weights(h, dtype, problem, x, ldx, dout, lddout, dw, dbias, ws, ws_bytes, stream=0):
+    """`dbias` may be 0: not computed."""
+    _check(lib().vit_op_linear_grouped_backward_weights(h, dtype, _ref(problem), x, ldx, dout, lddout, dw, dbias, ws, ws_bytes,
+                                                        stream), "vit_op_linear_grouped_backward_weights")
 
 
 def make_tensors(entries):

@@ -1,0 +1,197 @@
+// What the kernels of linear layers by group share: where a group's rows lie, how the work is cut, GELU and its slope.
+#pragma once
+#include "vit_internal.h"
+#include "sm100_ptx.cuh"
+
+namespace vit {
+
+// The offsets live on the device and are the caller's: a group whose rows are not in order or not inside the buffer is
+// skipped, and the status word says so.  Without offsets there is one group, of all rows.
+__device__ __forceinline__ bool group_rows(const GroupedShape& p, int g, int& begin, int& end) {
+  begin = 0;
+  end = p.rows;
+  if (p.offsets) {
+    begin = p.offsets[g];
+    end = p.offsets[g + 1];
+  }
+  return begin >= 0 && end >= begin && end <= p.rows;
+}
+
+__device__ __forceinline__ int warp_scan(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int lower = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v += lower;
+  }
+  return v;
+}
+__device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int64_t lower = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v += lower;
+  }
+  return v;
+}
+
+// Which group a unit of work belongs to.  Units are numbered group after group; a warp looks at 32 groups at a time and
+// asks for ever larger numbers.  All lanes call together and get the same answer.
+struct GroupAt { int group, begin, end; int64_t before; };       // its rows, and the units before it
+template <typename Count>                                        // Count: (rows of a group) -> its units
+struct GroupWalk {
+  const GroupedShape& p;
+  Count count;
+  int lane, g0, begin, end;
+  int64_t base, upto, chunk;                                      // units before the 32 groups, up to this lane's group, of all 32
+
+  __device__ __forceinline__ GroupWalk(const GroupedShape& shape, Count c, int lane_) : p(shape), count(c), lane(lane_), g0(0), base(0) { load(); }
+  __device__ __forceinline__ void load() {
+    const int g = g0 + lane;
+    int64_t n = 0;
+    begin = end = 0;
+    if (g < p.groups) {
+      if (group_rows(p, g, begin, end)) n = count(end - begin);
+      else begin = end = 0;
+    }
+    upto = warp_scan(n, lane);
+    chunk = __shfl_sync(0xffffffffu, upto, 31);
+  }
+  __device__ __forceinline__ bool find(int64_t unit, GroupAt& at) {
+    while (unit - base >= chunk) {
+      if (g0 + 32 >= p.groups) return false;
+      base += chunk;
+      g0 += 32;
+      load();
+    }
+    const uint32_t later = __ballot_sync(0xffffffffu, base + upto > unit);
+    const int who = __ffs((int)later) - 1;
+    at.group = g0 + who;
+    at.begin = __shfl_sync(0xffffffffu, begin, who);
+    at.end = __shfl_sync(0xffffffffu, end, who);
+    const int64_t before = __shfl_up_sync(0xffffffffu, upto, 1);
+    at.before = base + (who == 0 ? 0 : __shfl_sync(0xffffffffu, before, who));
+    return true;
+  }
+};
+// all units of all groups; one warp
+template <typename Count>
+__device__ __forceinline__ int64_t all_units(const GroupedShape& p, Count count, int lane) {
+  int64_t sum = 0;
+  for (int g = lane; g < p.groups; g += 32) {
+    int begin, end;
+    if (group_rows(p, g, begin, end)) sum += count(end - begin);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum;
+}
+__device__ __forceinline__ void report_bad_groups(const GroupedShape& p, int* dev_status, int lane) {
+  for (int g = lane; g < p.groups; g += 32) {
+    int begin, end;
+    if (!group_rows(p, g, begin, end)) atomicExch(dev_status, (int)VIT_ERR_OFFSETS);
+  }
+}
+
+// Tiles of `span` rows by `across` columns' tiles.
+struct TileCount {
+  int span, across;
+  __device__ __forceinline__ int64_t operator()(int rows) const { return (int64_t)((rows + span - 1) / span) * across; }
+};
+
+// The weights' gradients sum over a group's rows, tile by tile of [out][in], 64 rows to a unit (a group without rows has one
+// for every tile: its zeros).  All units of all tiles lie in one line, and the blocks get equal stretches of it: long sums are
+// cut where few tiles would leave blocks idle, and groups of any lengths come out even.  A block's first and last tile may
+// be parts; each part has one owner and the parts are joined in the order of their rows.
+constexpr int DW_BLOCKS = 148, DW_ROWS = 64, DW_LEAST = 8;       // blocks at most; units of a stretch at least, unless there are fewer tiles than blocks
+struct SumCount {
+  int tiles;
+  __device__ __forceinline__ int64_t operator()(int rows) const { return (int64_t)tiles * (rows > DW_ROWS ? (rows + DW_ROWS - 1) / DW_ROWS : 1); }
+};
+struct AllTiles {
+  int tiles;
+  __device__ __forceinline__ int64_t operator()(int) const { return tiles; }
+};
+struct Stretches {
+  int64_t total;
+  int blocks;
+  __device__ __forceinline__ Stretches(const GroupedShape& p, int tiles, int most, int lane) {
+    total = all_units(p, SumCount{tiles}, lane);
+    const int64_t whole = all_units(p, AllTiles{tiles}, lane), wanted = total / DW_LEAST > whole ? total / DW_LEAST : whole;
+    blocks = (int)(wanted < most ? wanted : most);
+    if (blocks < 1) blocks = 1;
+  }
+  __device__ __forceinline__ int64_t begin(int block) const { return block >= blocks ? total : total * block / blocks; }
+  __device__ __forceinline__ int owner(int64_t unit) const { return (int)(((unit + 1) * blocks - 1) / total); }
+};
+// A block's work on one tile: units [from, to) of `all`.  slot: where a part's sums are kept, the stretch's first or last.
+struct Part {
+  int group, begin, end, tile, from, to, all;
+  __device__ __forceinline__ bool whole() const { return from == 0 && to == all; }
+  __device__ __forceinline__ int slot() const { return from == 0 ? 1 : 0; }
+  __device__ __forceinline__ int blocks() const { return end > begin ? to - from : 0; }      // of 64 rows
+};
+__device__ __forceinline__ bool next_part(GroupWalk<SumCount>& walk, int64_t& unit, int64_t stop, Part& part) {
+  GroupAt at;
+  if (unit >= stop || !walk.find(unit, at)) return false;
+  const int rows = at.end - at.begin, all = rows > DW_ROWS ? (rows + DW_ROWS - 1) / DW_ROWS : 1;
+  const int64_t local = unit - at.before, tile = local / all;
+  part.group = at.group;
+  part.begin = at.begin;
+  part.end = at.end;
+  part.tile = (int)tile;
+  part.all = all;
+  part.from = (int)(local - tile * all);
+  const int64_t left = stop - unit;
+  part.to = left < all - part.from ? part.from + (int)left : all;
+  unit += part.to - part.from;
+  return true;
+}
+
+// gelu(v) = v Phi(v) and its slope Phi(v) + v phi(v), with a = |v| and
+//   erfc(a / sqrt 2) = (a1 t + ... + a5 t^5) e,  t = 1 / (1 + p a / sqrt 2),  e = exp(-a^2 / 2)
+// (Abramowitz & Stegun 7.1.26, |error| <= 1.5e-7), two values at a time.  a is held at 24, where e is zero in 32 bits, so
+// that infinities give their limits.
+struct Gelu2 { float2 half_erfc, e, a; };       // 0.5 erfc(a / sqrt 2), exp(-a^2 / 2), |v|
+__device__ __forceinline__ Gelu2 gelu_parts(float2 v) {
+  Gelu2 g;
+  g.a = make_float2(fabsf(v.x), fabsf(v.y));
+  g.a.x = g.a.x > 24.f ? 24.f : g.a.x;          // (a value that is not a number stays one)
+  g.a.y = g.a.y > 24.f ? 24.f : g.a.y;
+  const float kp = 0.3275911f * 0.70710678118654752440f;
+  const float2 den = __ffma2_rn(make_float2(kp, kp), g.a, make_float2(1.0f, 1.0f));
+  float2 t;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.x) : "f"(den.x));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t.y) : "f"(den.y));
+  const float ke = -0.5f * 1.4426950408889634f;
+  const float2 arg = __fmul2_rn(__fmul2_rn(g.a, g.a), make_float2(ke, ke));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(g.e.x) : "f"(arg.x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(g.e.y) : "f"(arg.y));
+  const float c5 = 0.5f * 1.061405429f, c4 = 0.5f * -1.453152027f, c3 = 0.5f * 1.421413741f, c2 = 0.5f * -0.284496736f,
+              c1 = 0.5f * 0.254829592f;
+  float2 q = __ffma2_rn(make_float2(c5, c5), t, make_float2(c4, c4));
+  q = __ffma2_rn(q, t, make_float2(c3, c3));
+  q = __ffma2_rn(q, t, make_float2(c2, c2));
+  q = __ffma2_rn(q, t, make_float2(c1, c1));
+  g.half_erfc = __fmul2_rn(__fmul2_rn(q, t), g.e);
+  return g;
+}
+__device__ __forceinline__ float2 gelu_2(float2 v) {
+  const Gelu2 g = gelu_parts(v);
+  return __ffma2_rn(make_float2(-g.a.x, -g.a.y), g.half_erfc, make_float2(fmaxf(v.x, 0.f), fmaxf(v.y, 0.f)));
+}
+__device__ __forceinline__ float2 gelu_slope_2(float2 v) {
+  const Gelu2 g = gelu_parts(v);
+  const float k = -0.39894228040143267794f;     // -1 / sqrt(2 pi)
+  const float2 below = __ffma2_rn(__fmul2_rn(make_float2(k, k), g.a), g.e, g.half_erfc);       // the slope at -a; 1 - it at a
+  return make_float2(v.x > 0.f ? 1.f - below.x : below.x, v.y > 0.f ? 1.f - below.y : below.y);
+}
+// in 32 bits, with the library's error function
+__device__ __forceinline__ float gelu_f32(float v) {
+  return v < -24.f ? -0.f : v > 24.f ? v : 0.5f * v * erfcf(v * -0.70710678118654752440f);
+}
+__device__ __forceinline__ float gelu_slope_f32(float v) {
+  const float a = v < -24.f ? -24.f : v > 24.f ? 24.f : v;
+  return fmaf(0.39894228040143267794f * a, expf(-0.5f * a * a), 0.5f * erfcf(a * -0.70710678118654752440f));
+}
+
+}  // namespace vit

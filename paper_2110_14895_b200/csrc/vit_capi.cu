@@ -311,6 +311,36 @@ size_t layer_norm_backward_ws(int rows, int cols) {
   return (size_t)(rows < LAYER_NORM_MAX_BLOCKS ? (rows > 0 ? rows : 1) : LAYER_NORM_MAX_BLOCKS) * 2 * cols * sizeof(float);
 }
 
+bool grouped_ok(int dtype, const vit_grouped_problem* p) {
+  return p && (dtype == VIT_BF16 || dtype == VIT_FP32) && p->groups >= 1 && p->rows >= 0 && p->in_features >= 8 && p->in_features % 8 == 0 &&
+         p->out_features >= 8 && p->out_features % 8 == 0 && (p->offsets || p->groups == 1) &&
+         !(reinterpret_cast<uintptr_t>(p->offsets) & 3);
+}
+// The kernels count tiles and rows in 32 bits; weights of all groups are read through one map, whose strides are of 40 bits.
+bool grouped_fits(const vit_grouped_problem* p) {
+  if (p->rows > MAX_PACKED_ROWS) return false;
+  const int64_t widest = p->in_features > p->out_features ? p->in_features : p->out_features;
+  const int64_t tiles = ((int64_t)p->rows / 64 + p->groups) * ((widest + 63) / 64);
+  const int64_t weights = (int64_t)p->in_features * p->out_features;
+  const int64_t sums = ((int64_t)p->in_features / 128 + 1) * ((int64_t)p->out_features / 128 + 1);      // tiles of a group's weights
+  return tiles <= INT32_MAX / 2 && weights <= (int64_t)1 << 36 && p->groups <= INT64_MAX / 16 / weights && sums <= INT32_MAX / 2;
+}
+// whether an output lies over the offsets or any other operand
+bool over_offsets(const vit_grouped_problem* p, const Block& out) {
+  return p->offsets && blocks_overlap(out, Block{p->offsets, 1, (int64_t)p->groups + 1, (int64_t)p->groups + 1, 4});
+}
+size_t grouped_ws(int dtype, const vit_grouped_problem* p) {
+  return align_up(grouped_dw_floats(dtype == VIT_BF16, GroupedShape{p->groups, p->rows, p->offsets}, p->in_features, p->out_features) * sizeof(float), 256);
+}
+GroupedCall grouped_call(const vit_handle* h, const vit_grouped_problem* p) {
+  GroupedCall c{};
+  c.shape = GroupedShape{p->groups, p->rows, p->offsets};
+  c.in = p->in_features;
+  c.out_features = p->out_features;
+  c.dev_status = h->dev_status;
+  return c;
+}
+
 // Whether a list of tensors may be scaled: nothing that is written lies over anything else, but for a tensor in place.
 struct Span { uintptr_t begin, end; bool write; };
 int clip_list_status(const vit_tensor* t, int n, const void* norm, const void* ws, size_t ws_bytes) {
@@ -733,7 +763,7 @@ const char* vit_status_string(int status) {
     case VIT_ERR_CUDA: return "CUDA call or kernel launch failed";
     case VIT_ERR_TIMEOUT: return "a bounded wait inside a kernel expired";
     case VIT_ERR_NO_DEVICE: return "no usable sm_100 device";
-    case VIT_ERR_OFFSETS: return "offsets of a packed sequence out of order, out of range or longer than the call's bound";
+    case VIT_ERR_OFFSETS: return "offsets of a packed sequence or group out of order, out of range or longer than the call's bound";
     case VIT_ERR_INFEASIBLE: return "no partition fits the devices' memory";
     case VIT_ERR_TOO_LARGE: return "problem larger than the fixed scratch of this allocation-free entry point";
   }
@@ -1038,6 +1068,89 @@ int vit_op_layernorm_backward(vit_handle* h, int dtype, int rows, int cols, cons
   int blocks = 0;
   if (rows > 0) VIT_LAUNCH(h, VIT_PROF_LAYERNORM, launch_layer_norm_backward(c, static_cast<float*>(ws), &blocks, s));
   VIT_LAUNCH(h, VIT_PROF_LAYERNORM, launch_column_grad(static_cast<const float*>(ws), blocks, cols, dgain, dshift, s));
+  return VIT_OK;
+}
+
+int vit_op_linear_grouped(vit_handle* h, int dtype, const vit_grouped_problem* problem, const void* x, int64_t ldx,
+                          const void* w, const float* bias, int epilogue, const void* residual, int64_t ldr, void* out,
+                          int64_t ldo, void* pre, int64_t ldp, void* stream) {
+  if (!h || !grouped_ok(dtype, problem) || epilogue < 0 || epilogue > 2 || !w || misaligned(w) || misaligned(bias) || !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
+  const vit_grouped_problem& p = *problem;
+  if (!grouped_fits(&p)) return VIT_ERR_TOO_LARGE;
+  if (epilogue != 1) pre = nullptr;
+  const size_t es = element_bytes(dtype);
+  const int64_t in = p.in_features, to = p.out_features, weights = p.groups * in * to, biases = p.groups * to;
+  const Block bx{x, p.rows, in, ldx, es}, bo{out, p.rows, to, ldo, es}, bw{w, 1, weights, weights, es};
+  const Block br{residual, epilogue == 2 ? p.rows : 0, to, epilogue == 2 ? ldr : to, es}, bb{bias, bias ? 1 : 0, biases, biases, 4};
+  const Block bp{pre, pre ? p.rows : 0, to, pre ? ldp : to, es};
+  if (!block_ok(bx) || !block_ok(bo) || !block_ok(br) || !block_ok(bp)) return VIT_ERR_INVALID_ARG;
+  for (const Block* b : {&bo, &bp}) {
+    if (blocks_overlap(*b, bx) || blocks_overlap(*b, bw) || blocks_overlap(*b, bb) || over_offsets(&p, *b)) return VIT_ERR_INVALID_ARG;
+    if (blocks_overlap(*b, br) && !same_block(*b, br)) return VIT_ERR_INVALID_ARG;
+  }
+  if (blocks_overlap(bo, bp)) return VIT_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  GroupedCall c = grouped_call(h, problem);
+  c.epilogue = epilogue; c.x = x; c.ldx = ldx; c.w = w; c.bias = bias; c.residual = residual; c.ldr = ldr; c.pre = pre; c.ldp = ldp;
+  c.y = out; c.ldy = ldo;
+  if (p.rows == 0) VIT_LAUNCH(h, VIT_PROF_OP, launch_check_groups(c, s));
+  else if (dtype == VIT_BF16) VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_rows_bf16(c, s));
+  else VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_rows_f32(c, s));
+  return VIT_OK;
+}
+
+int vit_op_linear_grouped_backward_input(vit_handle* h, int dtype, const vit_grouped_problem* problem, const void* dout,
+                                         int64_t lddout, const void* w, const void* pre, int64_t ldp, void* dx,
+                                         int64_t lddx, void* stream) {
+  if (!h || !grouped_ok(dtype, problem) || !w || misaligned(w) || !on_own_device(h)) return VIT_ERR_INVALID_ARG;
+  const vit_grouped_problem& p = *problem;
+  if (!grouped_fits(&p)) return VIT_ERR_TOO_LARGE;
+  const size_t es = element_bytes(dtype);
+  const int64_t in = p.in_features, from = p.out_features, weights = p.groups * in * from;
+  const Block bd{dout, p.rows, from, lddout, es}, bx{dx, p.rows, in, lddx, es}, bw{w, 1, weights, weights, es};
+  const Block bp{pre, pre ? p.rows : 0, in, pre ? ldp : in, es};
+  if (!block_ok(bd) || !block_ok(bx) || !block_ok(bp) || blocks_overlap(bx, bd) || blocks_overlap(bx, bw) || over_offsets(&p, bx) ||
+      (blocks_overlap(bx, bp) && !same_block(bx, bp)))
+    return VIT_ERR_INVALID_ARG;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  GroupedCall c = grouped_call(h, problem);
+  c.backward = true; c.x = dout; c.ldx = lddout; c.w = w; c.pre = const_cast<void*>(pre); c.ldp = ldp; c.y = dx; c.ldy = lddx;
+  if (p.rows == 0) VIT_LAUNCH(h, VIT_PROF_OP, launch_check_groups(c, s));
+  else if (dtype == VIT_BF16) VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_rows_bf16(c, s));
+  else VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_rows_f32(c, s));
+  return VIT_OK;
+}
+
+size_t vit_linear_grouped_backward_weights_bytes(int dtype, const vit_grouped_problem* problem) {
+  return grouped_ok(dtype, problem) && grouped_fits(problem) ? grouped_ws(dtype, problem) : 0;
+}
+
+int vit_op_linear_grouped_backward_weights(vit_handle* h, int dtype, const vit_grouped_problem* problem, const void* x,
+                                           int64_t ldx, const void* dout, int64_t lddout, void* dw, float* dbias, void* ws,
+                                           size_t ws_bytes, void* stream) {
+  if (!h || !grouped_ok(dtype, problem) || !dw || misaligned(dw) || misaligned(dbias) || !ws || misaligned(ws) || !on_own_device(h))
+    return VIT_ERR_INVALID_ARG;
+  const vit_grouped_problem& p = *problem;
+  if (!grouped_fits(&p)) return VIT_ERR_TOO_LARGE;
+  const size_t es = element_bytes(dtype), need = grouped_ws(dtype, problem);
+  const int64_t in = p.in_features, to = p.out_features, weights = p.groups * in * to, biases = p.groups * to;
+  const Block bx{x, p.rows, in, ldx, es}, bd{dout, p.rows, to, lddout, es};
+  const Block outs[] = {{dw, 1, weights, weights, es}, {dbias, dbias ? 1 : 0, biases, biases, 4}, {ws, 1, (int64_t)need, (int64_t)need, 1}};
+  if (!block_ok(bx) || !block_ok(bd)) return VIT_ERR_INVALID_ARG;
+  for (int i = 0; i < 3; ++i) {
+    if (blocks_overlap(outs[i], bx) || blocks_overlap(outs[i], bd) || over_offsets(&p, outs[i])) return VIT_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (blocks_overlap(outs[i], outs[j])) return VIT_ERR_INVALID_ARG;
+  }
+  if (ws_bytes < need) return VIT_ERR_WORKSPACE;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const bool b16 = dtype == VIT_BF16;
+  GroupedCall c = grouped_call(h, problem);
+  c.x = x; c.ldx = ldx; c.dout = dout; c.lddout = lddout; c.dw = dw; c.dbias = dbias; c.partial = static_cast<float*>(ws);
+  if (b16) VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_dw_bf16(c, s));
+  else VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_dw_f32(c, s));
+  if (grouped_dw_plan(c, b16).blocks > 1) VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_join(c, b16, s));
   return VIT_OK;
 }
 

@@ -226,6 +226,35 @@ int grad_clip_lists(int tensors);
 cudaError_t launch_grad_clip(const vit_tensor* tensors, int count, int index, bool clip, double* partial, int* partials, float bound,
                              float* norm, cudaStream_t s);
 
+// linear layers by group (linear_grouped_tc.cu, linear_grouped_dw.cu, linear_grouped_f32.cu)
+struct GroupedShape { int groups, rows; const int32_t* offsets; };      // offsets: nullptr for one group of all rows
+struct GroupedCall {
+  GroupedShape shape;
+  int in, out_features;
+  bool backward;                        // rows kernels: the input gradient
+  int epilogue;                         // forward: 0 none, 1 GELU, 2 residual
+  const void* x;        int64_t ldx;    // the rows that are multiplied: x forwards, dout backwards
+  const void* w;                        // [groups][out_features][in]
+  const float* bias;                    // [groups][out_features] or nullptr
+  const void* residual; int64_t ldr;
+  void* pre;            int64_t ldp;    // GELU's argument: written forwards, read backwards; nullptr for none
+  void* y;              int64_t ldy;    // out forwards, dx backwards
+  const void* dout;     int64_t lddout; // weight gradients, with x
+  void* dw;  float* dbias;              // [groups][out_features][in], [groups][out_features] or nullptr
+  float* partial;                       // grouped_dw_floats
+  int* dev_status;
+};
+cudaError_t launch_check_groups(const GroupedCall& c, cudaStream_t s);      // for calls without rows
+cudaError_t launch_grouped_rows_bf16(const GroupedCall& c, cudaStream_t s);
+cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s);
+// weight gradients: blocks share all work equally and leave the sums of cut tiles in `partial`, a second kernel joins them
+size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int out_features);
+struct GroupedDw { int tiles_in, tiles, blocks; float *part, *part_bias; };        // [blocks][2] tiles and rows of them
+GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16);
+cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s);
+cudaError_t launch_grouped_dw_f32(const GroupedCall& c, cudaStream_t s);
+cudaError_t launch_grouped_join(const GroupedCall& c, bool act_bf16, cudaStream_t s);
+
 cudaError_t launch_wait_probe(long long limit_cycles, int* dev_status, cudaStream_t s);
 // *snapshot = atomic exchange of *status with 0, on stream s
 cudaError_t launch_status_take(int* status, int* snapshot, cudaStream_t s);

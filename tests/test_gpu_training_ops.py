@@ -363,3 +363,293 @@ def test_grad_clip_refusals(ctx):
     call([(A, 0, 64, 1), (A, 0, 64, 1)])                   # read twice, written nowhere
     m.check()
     assert m.launches == before + 4
+
+
+# ------------------------------------------------------------------------------------ linear layers by group
+LAYERS = [
+    # lengths of the groups, rows before the first and behind the last, in, out
+    ([1], 0, 0, 8, 8), ([5], 0, 0, 16, 24), ([130], 2, 3, 64, 64), ([0, 7, 0, 0, 1], 1, 9, 72, 40), ([127, 128, 129], 0, 1, 136, 264),
+    ([256, 257, 31, 32, 33], 5, 5, 200, 328), ([64, 63, 65, 0, 15, 16, 17], 0, 0, 128, 256), ([1000], 0, 7, 192, 768), ([40] * 70, 3, 0, 48, 96),
+    ([3000, 0, 500, 1], 0, 0, 256, 512), ([700, 900], 11, 0, 1024, 64), ([0, 0], 0, 4, 64, 64), ([1, 1, 1, 1], 0, 0, 640, 8),
+    ([9000], 0, 0, 64, 128), ([2500, 2500, 2500], 1, 1, 512, 1288), ([6400], 0, 0, 1280, 1280),
+]
+LAYER_CASES = pytest.mark.parametrize("lengths,before,behind,k,n", LAYERS, ids=lambda v: "%dx%d" % (len(v), max(v)) if isinstance(v, list) else str(v))
+
+
+class Layer:
+    """Rows in groups with rows of nobody around them, which hold no numbers."""
+
+    def __init__(self, vit, m, lengths, before, behind, k, n, dtype, seed=0):
+        self.vit, self.m, self.k, self.n, self.dtype = vit, m, k, n, dtype
+        self.gen = _gen(sum(lengths) + 31 * k + n + seed)
+        self.rows, self.lengths, self.first = before + sum(lengths) + behind, lengths, before
+        edges = [before]
+        for length in lengths:
+            edges.append(edges[-1] + length)
+        self.spans = list(zip(edges, edges[1:]))
+        self.offsets = torch.tensor(edges, dtype=torch.int32, device="cuda")
+        self.covered = torch.zeros(self.rows, dtype=torch.bool, device="cuda")
+        self.covered[before:edges[-1]] = True
+        self.w = _normal(self.gen, len(lengths), n, k, scale=k ** -0.5, dtype=dtype)
+        self.problem = vit.make_grouped_problem(len(lengths), self.rows, k, n, self.offsets.data_ptr())
+
+    def some(self, width, ld, scale=1.0):
+        t = torch.full((self.rows, ld), float("nan"), dtype=self.dtype, device="cuda")
+        values = _normal(self.gen, self.rows, width, scale=scale, dtype=self.dtype)
+        t[self.covered, :width] = values[self.covered]
+        return t
+
+    def blank(self, ld):
+        return torch.full((self.rows, ld), 77.0, dtype=self.dtype, device="cuda")
+
+    def forward(self, x, bias=None, epilogue=0, residual=None, out=None, pre=None, w=None):
+        p = lambda t: t.data_ptr() if t is not None else 0
+        ld = lambda t: t.stride(0) if t is not None else 0
+        self.vit.vit_op_linear_grouped(self.m.h, _dt(self.vit, self.dtype), self.problem, p(x), x.stride(0), p(self.w if w is None else w), p(bias),
+                                       epilogue, p(residual), ld(residual), p(out), out.stride(0), p(pre), ld(pre))
+        self.m.check()
+        return out
+
+    def input_grad(self, dout, pre, dx):
+        self.vit.vit_op_linear_grouped_backward_input(self.m.h, _dt(self.vit, self.dtype), self.problem, dout.data_ptr(), dout.stride(0),
+                                                      self.w.data_ptr(), pre.data_ptr() if pre is not None else 0,
+                                                      pre.stride(0) if pre is not None else 0, dx.data_ptr(), dx.stride(0))
+        self.m.check()
+        return dx
+
+    def weight_grads(self, x, dout, bias=True, problem=None):
+        problem = problem or self.problem
+        dw = torch.full((len(self.lengths), self.n, self.k), 77.0, dtype=self.dtype, device="cuda")
+        db = torch.full((len(self.lengths), self.n), 77.0, device="cuda") if bias else None
+        size = self.vit.vit_linear_grouped_backward_weights_bytes(_dt(self.vit, self.dtype), problem)
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+        self.vit.vit_op_linear_grouped_backward_weights(self.m.h, _dt(self.vit, self.dtype), problem, x.data_ptr(), x.stride(0),
+                                                        dout.data_ptr(), dout.stride(0), dw.data_ptr(), db.data_ptr() if bias else 0,
+                                                        ws.data_ptr(), size)
+        self.m.check()
+        return dw, db
+
+    def products(self, a, transposed):
+        """Each row times its group's weights (or their transpose) in 64 bits, and the sums of the terms' sizes."""
+        width = self.k if transposed else self.n
+        out, size = (torch.full((self.rows, width), 77.0, dtype=torch.float64, device="cuda") for _ in range(2))
+        for g, (b, e) in enumerate(self.spans):
+            w = self.w[g].double() if transposed else self.w[g].double().t()
+            out[b:e], size[b:e] = a[b:e].double() @ w, a[b:e].double().abs() @ w.abs()
+        return out, size
+
+
+# sums in 32 bits: in bf16 sixteen products and the sum before are added with two bits less than a rounding keeps, in fp32 a
+# chain of as many roundings as products
+def _sum_error(length, dtype):
+    return ((length / 16 + 2) * 4 if dtype == torch.bfloat16 else length + 2) * STEP
+
+
+def _gelu64(v):
+    return 0.5 * v * torch.erfc(-v / math.sqrt(2))
+
+
+def _slope64(v):
+    return 0.5 * torch.erfc(-v / math.sqrt(2)) + v * torch.exp(-0.5 * v * v) / math.sqrt(2 * math.pi)
+
+
+@LAYER_CASES
+@BOTH
+def test_linear_grouped(ctx, lengths, before, behind, k, n, dtype):
+    vit, m = ctx
+    l = Layer(vit, m, lengths, before, behind, k, n, dtype)
+    x, residual = l.some(k, k + 8), l.some(n, n + 16)
+    bias = _normal(l.gen, len(lengths), n, scale=0.3)
+    want, size = l.products(x[:, :k], False)
+    err = _sum_error(k, dtype) * size
+    rows = l.covered
+    biased = want.clone()
+    for g, (b, e) in enumerate(l.spans):
+        biased[b:e] += bias[g].double()
+    err_b = err + STEP * (biased.abs() + size)
+
+    def check(got, want, tol):
+        assert ((got[rows][:, :n].double() - want[rows]).abs() <= (tol + HALF[dtype] * want.abs())[rows]).all()
+        assert (got[~rows] == 77).all() and (got[:, n:] == 77).all()
+
+    check(l.forward(x, out=l.blank(n + 24)), want, err)
+    plain = l.forward(x, bias, out=l.blank(n + 8))
+    check(plain, biased, err_b)
+    # |slope of gelu| <= 1.13; the error function's approximation is good to 1.5e-7 and its parts to 2^-20
+    tol = 1.13 * err_b + 1e-7 * biased.abs() + 2.5e-7
+    pre = l.blank(n + 40)
+    out = l.forward(x, bias, 1, out=l.blank(n + 8), pre=pre)
+    check(out, _gelu64(biased), tol)
+    assert torch.equal(pre[:, :n][rows], plain[:, :n][rows]) and (pre[~rows] == 77).all() and (pre[:, n:] == 77).all()
+    again = l.forward(x, bias, 1, out=l.blank(n + 8))
+    assert torch.equal(again, out)
+    summed = l.forward(x, bias, 2, residual=residual, out=l.blank(n + 8))
+    check(summed, biased + residual[:, :n].double().nan_to_num(0), err_b + STEP * (biased.abs() + residual[:, :n].double().abs().nan_to_num(0)))
+    own = residual.clone()
+    l.forward(x, bias, 2, residual=own, out=own)
+    assert torch.equal(own[:, :n][rows], summed[:, :n][rows]) and torch.equal(own[:, n:].isnan(), residual[:, n:].isnan())
+
+
+@LAYER_CASES
+@BOTH
+def test_linear_grouped_input_grad(ctx, lengths, before, behind, k, n, dtype):
+    vit, m = ctx
+    l = Layer(vit, m, lengths, before, behind, k, n, dtype)
+    dout, pre = l.some(n, n + 8), l.some(k, k + 8, scale=1.5)
+    want, size = l.products(dout[:, :n], True)
+    err = _sum_error(n, dtype) * size
+    rows = l.covered
+    dx = l.input_grad(dout, None, l.blank(k + 16))
+    assert ((dx[rows][:, :k].double() - want[rows]).abs() <= (err + HALF[dtype] * want.abs())[rows]).all()
+    assert (dx[~rows] == 77).all() and (dx[:, k:] == 77).all()
+    # the slope's two parts are good to 1e-6
+    slope = _slope64(pre[:, :k].double())
+    got = l.input_grad(dout, pre, l.blank(k + 24))
+    tol = err * slope.abs() + (want.abs() + err) * 1.2e-6 + HALF[dtype] * (want * slope).abs()
+    assert ((got[rows][:, :k].double() - (want * slope)[rows]).abs() <= tol[rows]).all()
+    assert (got[~rows] == 77).all() and (got[:, k:] == 77).all()
+    own = pre.clone()
+    l.input_grad(dout, own, own)
+    assert torch.equal(own[:, :k][rows], got[:, :k][rows])
+
+
+@LAYER_CASES
+@BOTH
+def test_linear_grouped_weight_grads(ctx, lengths, before, behind, k, n, dtype):
+    vit, m = ctx
+    l = Layer(vit, m, lengths, before, behind, k, n, dtype)
+    x, dout = l.some(k, k + 8), l.some(n, n + 16, scale=0.5)
+    dw, db = l.weight_grads(x, dout)
+    for g, (b, e) in enumerate(l.spans):
+        d, v = dout[b:e, :n].double(), x[b:e, :k].double()
+        want, size = d.t() @ v, d.abs().t() @ v.abs()
+        parts = 150                                                             # a sum may be cut between all blocks
+        assert ((dw[g].double() - want).abs() <= (_sum_error(e - b, dtype) + parts * STEP) * size + HALF[dtype] * want.abs()).all()
+        # 16 values at a time, their sums one after the other, four lanes and the parts
+        assert ((db[g].double() - d.sum(0)).abs() <= ((e - b) / 16 + 24 + parts) * STEP * d.abs().sum(0)).all()
+    again, none = l.weight_grads(x, dout, bias=False)
+    assert torch.equal(again, dw)
+    assert torch.equal(l.weight_grads(x, dout)[1], db)
+
+
+@BOTH
+def test_linear_without_offsets_is_one_group(ctx, dtype):
+    vit, m = ctx
+    l = Layer(vit, m, [333], 0, 0, 96, 136, dtype)
+    x, dout, bias = l.some(96, 96), l.some(136, 136), _normal(l.gen, 1, 136)
+    first = [l.forward(x, bias, out=l.blank(136)), l.input_grad(dout, None, l.blank(96)), *l.weight_grads(x, dout)]
+    l.problem = vit.make_grouped_problem(1, 333, 96, 136, 0)
+    second = [l.forward(x, bias, out=l.blank(136)), l.input_grad(dout, None, l.blank(96)), *l.weight_grads(x, dout)]
+    assert all(torch.equal(a, b) for a, b in zip(first, second))
+    # and an ordinary linear layer gives the same sums
+    y = torch.empty(333, 136, dtype=dtype, device="cuda")
+    vit.vit_op_linear(m.h, _dt(vit, dtype), 333, 136, 96, x.data_ptr(), l.w.data_ptr(), bias.data_ptr(), 0, 0, y.data_ptr())
+    m.check()
+    want, size = l.products(x, False)
+    assert ((first[0].double() - y.double()).abs() <= 2 * (HALF[dtype] * want.abs() + (_sum_error(96, dtype) + 4 * STEP) * (size + 4)) + HALF[dtype] * 4).all()
+
+
+@BOTH
+def test_groups_do_not_mix(ctx, dtype):
+    """What is not a number in one group, in its rows or its weights, stays there."""
+    vit, m = ctx
+    lengths = [70, 33, 200, 1]
+    l = Layer(vit, m, lengths, 0, 0, 72, 88, dtype)
+    x, dout, pre = l.some(72, 72), l.some(88, 88), l.some(72, 72)
+    clean = [l.forward(x, out=l.blank(88)), l.input_grad(dout, pre, l.blank(72)), *l.weight_grads(x, dout)]
+    b, e = l.spans[1]
+    for t in (x, dout, pre):
+        t[b:e] = float("nan")
+    x[b], dout[e - 1] = float("inf"), float("-inf")
+    l.w[1] = float("nan")
+    wild = [l.forward(x, out=l.blank(88)), l.input_grad(dout, pre, l.blank(72)), *l.weight_grads(x, dout)]
+    for i, (a, c) in enumerate(zip(clean, wild)):
+        if i < 2:
+            others = torch.ones(l.rows, dtype=torch.bool, device="cuda")
+            others[b:e] = False
+            assert torch.equal(a[others], c[others]) and c[b:e].isnan().all()
+        else:
+            assert torch.equal(a[[0, 2, 3]], c[[0, 2, 3]]) and c[1].isnan().all()
+
+
+@BOTH
+def test_gelu_and_its_slope_far_out(ctx, dtype):
+    """Arguments of any size, infinite ones too."""
+    vit, m = ctx
+    k = 64
+    values = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 0.5, -0.5, 3, -3, 5.5, -5.5, 9, -9, 13, -13, 30, -30, 1e4, -1e4, 1e30, -1e30, math.inf, -math.inf,
+                           math.nan, 1.0], device="cuda").to(dtype)
+    rows = len(values)
+    l = Layer(vit, m, [rows], 0, 0, k, k, dtype)
+    l.w[0] = torch.eye(k, device="cuda").to(dtype)
+    x = torch.zeros(rows, k, dtype=dtype, device="cuda")
+    x[:20, 0] = values[:20]
+    out = l.forward(x, None, 1, out=l.blank(k))
+    want = _gelu64(values[:20].double())
+    assert ((out[:20, 0].double() - want).abs() <= HALF[dtype] * want.abs() + 2.5e-7 * values[:20].double().abs().clamp(max=24)).all()
+    pre = values[:, None].expand(rows, k).contiguous()
+    ones = torch.ones(rows, k, dtype=dtype, device="cuda")
+    dx = l.input_grad(ones, pre, l.blank(k))[:, 0].double()
+    want = _slope64(values.double())
+    want[20:22] = torch.tensor([1.0, 0.0], device="cuda")                       # the limits
+    want[18:20] = torch.tensor([1.0, 0.0], device="cuda")                       # (not a number in 64 bits: infinity times zero)
+    assert dx[22].isnan()
+    keep = torch.arange(rows, device="cuda") != 22
+    assert ((dx - want)[keep].abs() <= (HALF[dtype] * want.abs() + 1.2e-6)[keep]).all()
+    bias = torch.zeros(1, k, device="cuda")
+    bias[0, :3] = torch.tensor([math.inf, -math.inf, math.nan], device="cuda")
+    out = l.forward(torch.zeros_like(x), bias, 1, out=l.blank(k))
+    assert (out[:, 0] == math.inf).all() and (out[:, 1] == 0).all() and out[:, 2].isnan().all() and (out[:, 3:] == 0).all()
+
+
+@pytest.mark.parametrize("edges", [[0, 40, 30, 90], [0, -1, 50, 90], [10, 20, 200, 90], [0, 2 ** 31 - 1, 60, 90], [50, 0, 60, 91]])
+@BOTH
+def test_groups_with_bad_offsets_are_skipped_and_reported(ctx, edges, dtype):
+    vit, m = ctx
+    l = Layer(vit, m, [90, 0, 0], 0, 0, 64, 72, dtype)
+    x, dout = l.some(64, 64), l.some(72, 72)
+    l.offsets.copy_(torch.tensor(edges, dtype=torch.int32))
+    good = [g for g, (b, e) in enumerate(zip(edges, edges[1:])) if 0 <= b <= e <= 90]
+    dt = _dt(vit, dtype)
+
+    def reported(call):
+        call()
+        with pytest.raises(vit.VitError) as e:
+            m.check()
+        assert e.value.status == vit.VIT_ERR_OFFSETS
+        m.check()
+
+    out, dx = l.blank(72), l.blank(64)
+    dw, db = torch.full((3, 72, 64), 77.0, dtype=dtype, device="cuda"), torch.full((3, 72), 77.0, device="cuda")
+    n = vit.vit_linear_grouped_backward_weights_bytes(dt, l.problem)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    reported(lambda: vit.vit_op_linear_grouped(m.h, dt, l.problem, x.data_ptr(), 64, l.w.data_ptr(), 0, 0, 0, 0, out.data_ptr(), 72, 0, 0))
+    reported(lambda: vit.vit_op_linear_grouped_backward_input(m.h, dt, l.problem, dout.data_ptr(), 72, l.w.data_ptr(), 0, 0, dx.data_ptr(), 64))
+    reported(lambda: vit.vit_op_linear_grouped_backward_weights(m.h, dt, l.problem, x.data_ptr(), 64, dout.data_ptr(), 72, dw.data_ptr(),
+                                                                db.data_ptr(), ws.data_ptr(), n))
+    owners = torch.zeros(90, dtype=torch.int32, device="cuda")
+    for g in good:
+        owners[edges[g]:edges[g + 1]] += 1
+    touched = owners > 0
+    for g in range(3):
+        b, e = edges[g], edges[g + 1]
+        if g not in good:
+            assert (dw[g] == 77).all() and (db[g] == 77).all()
+            continue
+        xs, ds, w = x[b:e].double(), dout[b:e].double(), l.w[g].double()
+        for got, want, size, length in ((out[b:e], xs @ w.t(), xs.abs() @ w.abs().t(), 64), (dx[b:e], ds @ w, ds.abs() @ w.abs(), 72),
+                                        (dw[g], ds.t() @ xs, ds.abs().t() @ xs.abs(), e - b)):
+            fine = (got.double() - want).abs() <= HALF[dtype] * want.abs() + (_sum_error(length, dtype) + 8 * STEP) * size
+            if got.shape[0] == e - b and got.data_ptr() != dw[g].data_ptr():
+                fine = fine[owners[b:e] == 1]               # rows that two groups share are undefined
+            assert fine.all()
+    assert (out[~touched] == 77).all() and (dx[~touched] == 77).all()
+    # without rows every group that is not empty is a bad one
+    none = vit.make_grouped_problem(3, 0, 64, 72, l.offsets.data_ptr())
+    reported(lambda: vit.vit_op_linear_grouped(m.h, dt, none, 0, 64, l.w.data_ptr(), 0, 0, 0, 0, 0, 72, 0, 0))
+    l.offsets.zero_()
+    vit.vit_op_linear_grouped(m.h, dt, none, 0, 64, l.w.data_ptr(), 0, 0, 0, 0, 0, 72, 0, 0)
+    vit.vit_op_linear_grouped_backward_input(m.h, dt, none, 0, 72, l.w.data_ptr(), 0, 0, 0, 64)
+    vit.vit_op_linear_grouped_backward_weights(m.h, dt, none, 0, 64, 0, 72, dw.data_ptr(), db.data_ptr(), ws.data_ptr(), n)
+    m.check()
+    assert (dw == 0).all() and (db == 0).all()
