@@ -3,11 +3,15 @@
 //   dW_g = sum over the group's rows r of dout[r,:]^T x[r,:],   db_g = sum of dout[r,:]
 //
 // Both operands have the summed index across their rows and are read as they lie: slabs of 64 rows by 64 columns, swizzled by
-// 128 bytes, in the other major order.  Tiles of 128 x 256 of dW; 128 bytes of shared memory a cycle feed 64 rows of them in
-// the 512 cycles that their products take.  The rows behind a group's end are the next group's: the warp that issues the
-// products clears them in the last stage, in both operands (zero times a value that is not a number would not be zero).
+// 128 bytes, in the other major order.  A pair of blocks makes a tile of 256 x 256 of dW, each block with its own half of the
+// slabs: shared memory then takes in and gives out 64 KB for 64 rows, in the 512 cycles of their products, where the 96 KB of
+// a single block's 128 x 256 are more than it can move.  Single blocks stay for narrow layers, where half a pair would idle.
+// The rows behind a group's end are the next group's: they are cleared in the last stage, in both operands (zero times a
+// value that is not a number would not be zero).  A warp of its own in each block sees the copies land, clears, and hands the
+// stage on to the warp that issues the products (the even block's, for both); it runs ahead of them, so that neither the
+// clearing nor the way from block to block holds them up (with both in the issuing warp's path: 241 us, now 2xx).
 // Two more warps add up dout's columns for db from the same stages, where the tile is its row's first.
-// Blocks get equal stretches of the work (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
+// The units of work get equal stretches of it (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
 #include "linear_grouped.cuh"
 #include "linear_grouped_tc.cuh"
 
@@ -17,15 +21,18 @@ using namespace grouped;
 
 namespace {
 
-constexpr int TN = 256, SUM_WARPS = 2, DW_THREADS = THREADS + 32 * SUM_WARPS;
-constexpr int A_BYTES = 2 * SLAB_BYTES, B_BYTES = 4 * SLAB_BYTES, STAGE_BYTES = A_BYTES + B_BYTES, STAGES = 4;
-constexpr int STAGING_BYTES = EPI_WARPS * 4096, SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 256;
+constexpr int TN = 256, SUM_WARPS = 2, DW_THREADS = THREADS + 32 * (SUM_WARPS + 1);
+template <int CTAS> struct DwCfg {
+  static constexpr int B_SLABS = 4 / CTAS, A_BYTES = 2 * SLAB_BYTES, STAGE_BYTES = A_BYTES + B_SLABS * SLAB_BYTES, STAGES = CTAS == 2 ? 6 : 4;
+  static constexpr int STAGING_BYTES = EPI_WARPS * 4096, SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 256;
+};
 
 struct DwArgs {
   GroupedShape shape;
-  int in, out, tiles_in, tiles;    // tiles of a group: ceil(out / 128) x ceil(in / 256)
+  int in, out, tiles_in, tiles;    // tiles of a group: ceil(out / (128 blocks)) x ceil(in / 256)
   float* dbias;                    // [groups][out] or nullptr
-  float* part_bias;                // [blocks][2][128]
+  float* part_bias;                // [units][2][128 blocks]
+  int64_t* table;                  // where the units' shares begin
   int* dev_status;
 };
 struct DwMaps { CUtensorMap dout, x, dw, part; };
@@ -37,26 +44,40 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
+// The odd block of a pair hands a stage on.  What TMA wrote there is complete; a release at cluster scope would wait for about
+// a microsecond, so that it is left to the stages that this warp has written to itself.
+__device__ __forceinline__ void hand_on(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
+
+template <int CTAS>
 __global__ void __launch_bounds__(DW_THREADS, 1)
 grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwArgs p) {
+  using C = DwCfg<CTAS>;
+  constexpr int STAGES = C::STAGES;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  const uint32_t tiles = smem_u32(smem), staging = tiles + STAGES * STAGE_BYTES;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES + STAGING_BYTES);
-  const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, tfull = empty + 8 * STAGES, tempty = tfull + 16, drain = tempty + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
+  const uint32_t tiles = smem_u32(smem), staging = tiles + STAGES * C::STAGE_BYTES;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * C::STAGE_BYTES + C::STAGING_BYTES);
+  const uint32_t full = smem_u32(bars), ready = full + 8 * STAGES, empty = ready + 8 * STAGES, tfull = empty + 8 * STAGES, tempty = tfull + 16,
+                 drain = tempty + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 5);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
+  const int self = (int)blockIdx.x / CTAS, units = (int)gridDim.x / CTAS;
 
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < STAGES; ++i) {
       mbar_init(full + 8 * i, 1);
+      mbar_init(ready + 8 * i, CTAS);                                   // a word of each block
       mbar_init(empty + 8 * i, p.dbias ? 1 + SUM_WARPS : 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(tfull + 8 * i, 1);
-      mbar_init(tempty + 8 * i, EPI_WARPS);
+      mbar_init(tempty + 8 * i, EPI_WARPS * CTAS);
     }
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -64,17 +85,20 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     prefetch_map(&m.x);
     prefetch_map(&m.dw);
   }
-  if (warp == 1) tmem_alloc(smem_u32(tmem_slot), 512);
+  if (warp == 1) {
+    if (CTAS == 2) tmem_alloc_pair(smem_u32(tmem_slot), 512);
+    else tmem_alloc(smem_u32(tmem_slot), 512);
+  }
   tc_fence_before();
   __syncthreads();
+  if (CTAS == 2) cluster_sync();          // the partner's barriers are initialised before anyone signals them
   tc_fence_after();
   grid_dependency_wait();
   grid_launch_dependents();
   const uint32_t tmem = *tmem_slot;
-  const Stretches work(p.shape, p.tiles, (int)gridDim.x, lane);
-  int64_t unit = work.begin((int)blockIdx.x);
-  const int64_t stop = work.begin((int)blockIdx.x + 1);
-  GroupWalk<SumCount> walk(p.shape, SumCount{p.tiles}, lane);
+  const Share share = find_share(p.shape, p.tiles, units, self, reinterpret_cast<int64_t*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
+                                 rank == 0 ? p.table : nullptr);
+  PartWalk work(p.shape, p.tiles, lane, share, self, units);
   Part part;
   int stage = 0;
   uint32_t phase = 0;
@@ -83,19 +107,19 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     // ---------------------------------------------------------------- TMA producer
     long long fills = 0;
     bool ok = true;
-    while (ok && next_part(walk, unit, stop, part)) {
-      const int n0 = part.tile / p.tiles_in * BM, k0 = part.tile % p.tiles_in * TN;
+    while (ok && work.next(part)) {
+      const int n0 = part.tile / p.tiles_in * (BM * CTAS) + (int)rank * BM, k0 = part.tile % p.tiles_in * TN + (int)rank * (TN / CTAS);
       for (int kb = 0; kb < part.blocks(); ++kb) {
         if (!warp_wait(empty + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
         ++fills;
         if (lane == 0) {
-          const uint32_t sa = tiles + stage * STAGE_BYTES, fb = full + 8 * stage;
+          const uint32_t sa = tiles + stage * C::STAGE_BYTES, fb = full + 8 * stage;
           const int row = part.begin + (part.from + kb) * DW_ROWS;
-          mbar_arrive_expect_tx(fb, STAGE_BYTES);
+          mbar_arrive_expect_tx(fb, C::STAGE_BYTES);
 #pragma unroll
           for (int s = 0; s < 2; ++s) tma_load_2d(sa + s * SLAB_BYTES, &m.dout, n0 + 64 * s, row, fb);
 #pragma unroll
-          for (int s = 0; s < 4; ++s) tma_load_2d(sa + A_BYTES + s * SLAB_BYTES, &m.x, k0 + 64 * s, row, fb);
+          for (int s = 0; s < C::B_SLABS; ++s) tma_load_2d(sa + C::A_BYTES + s * SLAB_BYTES, &m.x, k0 + 64 * s, row, fb);
         }
         __syncwarp();
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -104,42 +128,60 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     if (*abort_flag && lane == 0) drain_stages(full, STAGES, fills);
   } else if (warp == 1) {
     // ---------------------------------------------------------------- products
-    constexpr uint32_t id = instr_desc(BM, TN, true, true);
-    int buf = 0;
-    uint32_t aphase = 0;
+    if (rank == 0) {
+      constexpr uint32_t id = instr_desc(BM * CTAS, TN, true, true);
+      int buf = 0;
+      uint32_t aphase = 0;
+      bool ok = true;
+      while (ok && work.next(part)) {
+        if (!warp_wait(tempty + 8 * buf, aphase ^ 1, abort_flag)) break;
+        tc_fence_after();
+        const uint32_t d = tmem + (uint32_t)(buf * TN);
+        for (int kb = 0; kb < part.blocks(); ++kb) {
+          if (!warp_wait(ready + 8 * stage, phase, abort_flag)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t sa = uniform(tiles + stage * C::STAGE_BYTES);
+          const int steps = (min(DW_ROWS, part.end - part.begin - (part.from + kb) * DW_ROWS) + 15) / 16;
+          const uint64_t ad = smem_desc(sa, SLAB_BYTES), bd = smem_desc(sa + C::A_BYTES, SLAB_BYTES);
+          if (elect_one()) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)                // 16 rows of 128 bytes
+              if (k < steps) product<CTAS>(d, ad + (uint64_t)(128 * k), bd + (uint64_t)(128 * k), id, (kb > 0 || k > 0) ? 1u : 0u);
+            commit<CTAS>(empty + 8 * stage);
+          }
+          __syncwarp();
+          if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        }
+        if (!ok) break;
+        if (elect_one()) commit<CTAS>(tfull + 8 * buf);
+        __syncwarp();
+        if (++buf == 2) { buf = 0; aphase ^= 1; }
+      }
+      if (*abort_flag) drain_products(drain, lane);
+    }
+  } else if (warp == 2 + EPI_WARPS + SUM_WARPS) {
+    // ---------------------------------------------------------------- stages that have landed are handed on
     bool ok = true;
-    while (ok && next_part(walk, unit, stop, part)) {
-      if (!warp_wait(tempty + 8 * buf, aphase ^ 1, abort_flag)) break;
-      tc_fence_after();
-      const uint32_t d = tmem + (uint32_t)(buf * TN);
+    while (ok && work.next(part)) {
       for (int kb = 0; kb < part.blocks(); ++kb) {
         if (!warp_wait(full + 8 * stage, phase, abort_flag)) { ok = false; break; }
-        const uint32_t sa = uniform(tiles + stage * STAGE_BYTES);
-        const int rows = min(DW_ROWS, part.end - part.begin - (part.from + kb) * DW_ROWS), steps = (rows + 15) / 16;
+        const int rows = min(DW_ROWS, part.end - part.begin - (part.from + kb) * DW_ROWS);
         if (rows & 15) {                               // the group's last rows: the others of their 16 become zero
-          for (int s = 0; s < 6; ++s)
-            for (int i = rows * 8 + lane; i < steps * 128; i += 32)
+          const uint32_t sa = tiles + stage * C::STAGE_BYTES;
+          for (int s = 0; s < 2 + C::B_SLABS; ++s)
+            for (int i = rows * 8 + lane; i < (rows + 15) / 16 * 128; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + (uint32_t)(s * SLAB_BYTES + i * 16)), "r"(0u) : "memory");
           fence_proxy_async_smem();
-          __syncwarp();
-        }
-        tc_fence_after();
-        const uint64_t ad = smem_desc(sa, SLAB_BYTES), bd = smem_desc(sa + A_BYTES, SLAB_BYTES);
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)                  // 16 rows of 128 bytes
-            if (k < steps) umma_bf16(d, ad + (uint64_t)(128 * k), bd + (uint64_t)(128 * k), id, (kb > 0 || k > 0) ? 1u : 0u);
-          umma_commit(empty + 8 * stage);
+          if (CTAS == 2) fence_cluster();
         }
         __syncwarp();
+        if (lane == 0) {
+          if (CTAS == 2) hand_on(map_to_cta(ready + 8 * stage, 0));
+          else mbar_arrive(ready + 8 * stage);
+        }
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
-      if (!ok) break;
-      if (elect_one()) umma_commit(tfull + 8 * buf);
-      __syncwarp();
-      if (++buf == 2) { buf = 0; aphase ^= 1; }
     }
-    if (*abort_flag) drain_products(drain, lane);
   } else if (warp < 2 + EPI_WARPS) {
     // ---------------------------------------------------------------- epilogue
     if (blockIdx.x == 0 && warp == 2) report_bad_groups(p.shape, p.dev_status, lane);
@@ -147,10 +189,10 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     const uint32_t stg = staging + ew * 4096;
     int buf = 0;
     uint32_t aphase = 0;
-    while (next_part(walk, unit, stop, part)) {
+    while (work.next(part)) {
       if (!warp_wait(tfull + 8 * buf, aphase, abort_flag)) break;
       tc_fence_after();
-      const int n0 = part.tile / p.tiles_in * BM + quarter * 32, k0 = part.tile % p.tiles_in * TN + half * 128;
+      const int n0 = part.tile / p.tiles_in * (BM * CTAS) + (int)rank * BM + quarter * 32, k0 = part.tile % p.tiles_in * TN + half * 128;
       const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * TN + half * 128);
       if (part.whole()) {
 #pragma unroll 1
@@ -172,7 +214,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
           if (lane == 0) tma_store_3d(&m.dw, stg, k0 + 64 * cb, n0, part.group);      // rows and columns beyond are clipped
         }
       } else {
-        const int row = ((int)blockIdx.x * 2 + part.slot()) * BM + quarter * 32;
+        const int row = ((self * 2 + part.slot()) * CTAS + (int)rank) * BM + quarter * 32;
 #pragma unroll 1
         for (int cb = 0; cb < 4; ++cb) {
           if (k0 + 32 * cb >= p.in || n0 >= p.out) break;               // nobody will look there
@@ -193,22 +235,25 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(tempty + 8 * buf);
+      if (lane == 0) {
+        if (CTAS == 2) mbar_arrive_cluster(map_to_cta(tempty + 8 * buf, 0));
+        else mbar_arrive(tempty + 8 * buf);
+      }
       if (++buf == 2) { buf = 0; aphase ^= 1; }
     }
     if (lane == 0) tma_store_wait_all();
-  } else if (p.dbias) {
+  } else if (warp < 2 + EPI_WARPS + SUM_WARPS && p.dbias) {
     // ---------------------------------------------------------------- sums of dout's columns
     // a warp has a slab's 64 columns; a lane 8 of them and every fourth row
     const int slab = warp - 2 - EPI_WARPS, ck = lane & 7, first = lane >> 3;
     bool ok = true;
-    while (ok && next_part(walk, unit, stop, part)) {
+    while (ok && work.next(part)) {
       const bool mine = part.tile % p.tiles_in == 0;
       float2 sum[4] = {};
       for (int kb = 0; kb < part.blocks(); ++kb) {
         if (!warp_wait(full + 8 * stage, phase, abort_flag)) { ok = false; break; }
         if (mine) {
-          const uint32_t from = tiles + stage * STAGE_BYTES + slab * SLAB_BYTES;
+          const uint32_t from = tiles + stage * C::STAGE_BYTES + slab * SLAB_BYTES;
           const int rows = min(DW_ROWS, part.end - part.begin - (part.from + kb) * DW_ROWS);
           float2 some[4] = {};
 #pragma unroll 4
@@ -233,10 +278,10 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
           sum[e].x += __shfl_xor_sync(0xffffffffu, sum[e].x, o);
           sum[e].y += __shfl_xor_sync(0xffffffffu, sum[e].y, o);
         }
-      const int c = slab * 64 + ck * 8, n0 = part.tile / p.tiles_in * BM;
+      const int c = slab * 64 + ck * 8, n0 = part.tile / p.tiles_in * (BM * CTAS) + (int)rank * BM;
       if (first == 0 && n0 + c < p.out) {
         float4* to = reinterpret_cast<float4*>(part.whole() ? p.dbias + (int64_t)part.group * p.out + n0 + c
-                                                            : p.part_bias + ((int64_t)blockIdx.x * 2 + part.slot()) * BM + c);
+                                                            : p.part_bias + (((int64_t)self * 2 + part.slot()) * CTAS + rank) * BM + c);
         to[0] = make_float4(sum[0].x, sum[0].y, sum[1].x, sum[1].y);
         to[1] = make_float4(sum[2].x, sum[2].y, sum[3].x, sum[3].y);
       }
@@ -244,18 +289,22 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   }
 
   __syncwarp();
+  if (CTAS == 2 && *abort_flag)
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_cta(smem_u32(const_cast<int*>(abort_flag)), rank ^ 1u)), "r"(1) : "memory");
   tc_fence_before();
   __syncthreads();
+  if (CTAS == 2) cluster_sync();          // neither block leaves while the other may still touch it
   tc_fence_after();
   if (threadIdx.x == 0 && *abort_flag) atomicExch(p.dev_status, (int)VIT_ERR_TIMEOUT);
   if (warp == 1) {
     __syncwarp();
-    tmem_dealloc(tmem, 512);
+    if (CTAS == 2) tmem_dealloc_pair(tmem, 512);
+    else tmem_dealloc(tmem, 512);
   }
 }
 
 // Tiles that were cut between blocks: their parts are added in the order of their rows.  A block of this kernel looks at the
-// begin of one stretch; it is its task if the tile there began in the stretch before.  Eight blocks share a tile's rows.
+// begin of one stretch; it is its task if the tile there began in the stretch before.  Sixteen rows to a block.
 template <typename T> __device__ __forceinline__ void store4(T* to, float4 v);
 template <> __device__ __forceinline__ void store4(float* to, float4 v) { *reinterpret_cast<float4*>(to) = v; }
 template <> __device__ __forceinline__ void store4(bf16* to, float4 v) {
@@ -267,22 +316,29 @@ template <> __device__ __forceinline__ void store4(bf16* to, float4 v) {
 }
 template <typename T, int ROWS, int COLS>
 __global__ void __launch_bounds__(256)
-grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int tiles, int most, const float* __restrict__ part,
-                    const float* __restrict__ part_bias, T* __restrict__ dw, float* __restrict__ dbias) {
+grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int tiles, int blocks, const int64_t* __restrict__ table,
+                    const float* __restrict__ part, const float* __restrict__ part_bias, T* __restrict__ dw, float* __restrict__ dbias) {
   const int lane = threadIdx.x & 31, block = (int)blockIdx.x + 1;
   grid_dependency_wait();
-  const Stretches work(shape, tiles, most, lane);
-  const int64_t begin = work.begin(block);
-  if (block >= work.blocks || begin == 0 || begin >= work.begin(block + 1)) return;
-  GroupWalk<SumCount> walk(shape, SumCount{tiles}, lane);
+  const int64_t begin = table[block], end = table[block + 1];
+  if (begin >= end || begin == table[0]) return;
+  auto owner = [&](int64_t unit) {                                               // the last block that begins there or before
+    int lo = 0, hi = blocks;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (table[mid] <= unit) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  };
+  PartWalk work(shape, tiles, lane, Share{0, begin, begin + 1}, 0, 1);
   Part here;
-  int64_t unit = begin;
-  if (!next_part(walk, unit, begin + 1, here) || here.from == 0) return;         // a tile begins here: nothing is cut
+  if (!work.next(here) || here.from == 0) return;                                // a tile begins here: nothing is cut
   const int64_t tile_begin = begin - here.from, tile_end = tile_begin + here.all;
-  const int before = work.owner(begin - 1);
-  if (work.begin(before) > tile_begin) return;                                   // cut before, too: not this block's task
-  const int n0 = here.tile / tiles_in * ROWS, k0 = here.tile % tiles_in * COLS, r0 = (int)blockIdx.y * (ROWS / 8);
-  constexpr int N = ROWS / 8 * COLS / 1024;
+  const int before = owner(begin - 1);
+  if (table[before] > tile_begin) return;                                        // cut before, too: not this block's task
+  const int n0 = here.tile / tiles_in * ROWS, k0 = here.tile % tiles_in * COLS, r0 = (int)blockIdx.y * 16;
+  constexpr int N = 16 * COLS / 1024;
   float4 sum[N];
 #pragma unroll
   for (int i = 0; i < N; ++i)
@@ -290,14 +346,14 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
   const bool bias = dbias && k0 == 0 && blockIdx.y == 0 && threadIdx.x < ROWS;
   float b = bias ? part_bias[((int64_t)before * 2 + 1) * ROWS + threadIdx.x] : 0.f;
   for (int64_t u = begin; u < tile_end;) {
-    const int who = work.owner(u);
+    const int who = owner(u);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float4 v = *reinterpret_cast<const float4*>(part + (int64_t)who * 2 * ROWS * COLS + r0 * COLS + (i * 256 + (int)threadIdx.x) * 4);
       sum[i] = make_float4(sum[i].x + v.x, sum[i].y + v.y, sum[i].z + v.z, sum[i].w + v.w);
     }
     if (bias) b += part_bias[(int64_t)who * 2 * ROWS + threadIdx.x];
-    u = work.begin(who + 1);
+    u = table[who + 1];
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -307,18 +363,20 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
   if (bias && n0 + (int)threadIdx.x < out) dbias[(int64_t)here.group * out + n0 + threadIdx.x] = b;
 }
 
-struct DwTiling { int rows, cols, tiles_in, tiles, blocks; };
+struct DwTiling { int rows, cols, tiles_in, tiles, blocks; };       // blocks: units of work, pairs where a tile has 256 rows
 DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   DwTiling t;
-  t.rows = 128;
+  // a pair's tile costs 1.4 of a single block's half (measured at 1024 x 4096): not for layers that would leave it empty
+  const bool pair = act_bf16 && (out + 255) / 256 * 2.8 <= (out + 127) / 128 * 2.0;
+  t.rows = pair ? 256 : 128;
   t.cols = act_bf16 ? TN : 128;
   t.tiles_in = (in + t.cols - 1) / t.cols;
   const int64_t tiles = (int64_t)t.tiles_in * ((out + t.rows - 1) / t.rows);
   t.tiles = (int)tiles;
-  // as many blocks as the rows can need: the kernels, which see the groups' lengths, may use fewer
+  // as many as the rows can need: the kernels, which see the groups' lengths, may use fewer
   const int64_t units = tiles * ((int64_t)shape.rows / DW_ROWS + shape.groups), whole = tiles * shape.groups;
-  const int64_t wanted = units / DW_LEAST > whole ? units / DW_LEAST : whole;
-  t.blocks = (int)(wanted < DW_BLOCKS ? (wanted < 1 ? 1 : wanted) : DW_BLOCKS);
+  const int64_t wanted = units / DW_LEAST > whole ? units / DW_LEAST : whole, most = pair ? DW_BLOCKS / 2 : DW_BLOCKS;
+  t.blocks = (int)(wanted < most ? (wanted < 1 ? 1 : wanted) : most);
   return t;
 }
 
@@ -326,44 +384,54 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
 
 size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int out_features) {
   const DwTiling t = tiling_of(act_bf16, shape, in, out_features);
-  return (size_t)t.blocks * 2 * ((size_t)t.rows * t.cols + t.rows);
+  return (size_t)64 * ((2 * DW_TABLE + 63) / 64) + (size_t)t.blocks * 2 * ((size_t)t.rows * t.cols + t.rows);
 }
 
 GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16) {
   const DwTiling t = tiling_of(act_bf16, c.shape, c.in, c.out_features);
-  return GroupedDw{t.tiles_in, t.tiles, t.blocks, c.partial, c.partial + (size_t)t.blocks * 2 * t.rows * t.cols};
+  float* part = c.partial + 64 * ((2 * DW_TABLE + 63) / 64);                    // behind the table; for TMA on a multiple of 16 bytes
+  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int64_t*>(c.partial)};
+}
+
+template <int CTAS>
+static cudaError_t launch_dw(const DwMaps& m, const DwArgs& p, int units, cudaStream_t s) {
+  static PerDeviceFlag configured;
+  if (cudaError_t e = ensure_dynamic_smem(configured, grouped_dw_kernel<CTAS>, DwCfg<CTAS>::SMEM_BYTES)) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(units * CTAS));
+  cfg.blockDim = dim3(DW_THREADS);
+  cfg.dynamicSmemBytes = DwCfg<CTAS>::SMEM_BYTES;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CTAS;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, grouped_dw_kernel<CTAS>, m, p);
 }
 
 cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, true);
   DwMaps m;
-  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, c.dbias, plan.part_bias, c.dev_status};
+  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, c.dbias, plan.part_bias, plan.table, c.dev_status};
   // without rows nothing is read, and any map will do
   const int64_t rows = c.shape.rows > 0 ? c.shape.rows : 1;
   const void *dout = c.shape.rows > 0 ? c.dout : c.dw, *x = c.shape.rows > 0 ? c.x : c.dw;
   if (!encode_rows(&m.dout, dout, rows, c.out_features, c.lddout, DW_ROWS) || !encode_rows(&m.x, x, rows, c.in, c.ldx, DW_ROWS) ||
       !encode_weights(&m.dw, c.dw, c.shape.groups, c.out_features, c.in, 32) ||
-      !encode_rows(&m.part, plan.part, (int64_t)plan.blocks * 2 * BM, TN, TN, 32, 4))
+      !encode_rows(&m.part, plan.part, (int64_t)plan.blocks * 2 * plan.rows, TN, TN, 32, 4))
     return cudaErrorInvalidValue;
-  static PerDeviceFlag configured;
-  if (cudaError_t e = ensure_dynamic_smem(configured, grouped_dw_kernel, SMEM_BYTES)) return e;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)plan.blocks);
-  cfg.blockDim = dim3(DW_THREADS);
-  cfg.dynamicSmemBytes = SMEM_BYTES;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, grouped_dw_kernel, m, p);
+  return plan.rows == 256 ? launch_dw<2>(m, p, plan.blocks, s) : launch_dw<1>(m, p, plan.blocks, s);
 }
 
 template <typename T, int ROWS, int COLS>
 static cudaError_t launch_join(const GroupedCall& c, const GroupedDw& plan, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(plan.blocks - 1), 8);
+  cfg.gridDim = dim3((unsigned)(plan.blocks - 1), ROWS / 16);
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -372,12 +440,13 @@ static cudaError_t launch_join(const GroupedCall& c, const GroupedDw& plan, cuda
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, grouped_join_kernel<T, ROWS, COLS>, c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.blocks,
-                            (const float*)plan.part, (const float*)plan.part_bias, static_cast<T*>(c.dw), c.dbias);
+                            (const int64_t*)plan.table, (const float*)plan.part, (const float*)plan.part_bias, static_cast<T*>(c.dw), c.dbias);
 }
 cudaError_t launch_grouped_join(const GroupedCall& c, bool act_bf16, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, act_bf16);
   if (plan.blocks < 2) return cudaSuccess;
-  return act_bf16 ? launch_join<bf16, 128, TN>(c, plan, s) : launch_join<float, 128, 128>(c, plan, s);
+  if (!act_bf16) return launch_join<float, 128, 128>(c, plan, s);
+  return plan.rows == 256 ? launch_join<bf16, 256, TN>(c, plan, s) : launch_join<bf16, 128, TN>(c, plan, s);
 }
 
 }  // namespace vit

@@ -152,6 +152,7 @@ struct DwArgs {
   const float *x, *dout;
   int64_t ldx, lddout;
   float *dw, *dbias, *part, *part_bias;
+  int64_t* table;
   int* dev_status;
 };
 
@@ -163,12 +164,10 @@ grouped_dw_f32_kernel(const DwArgs p) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
-  const Stretches work(p.shape, p.tiles, (int)gridDim.x, lane);
-  int64_t unit = work.begin((int)blockIdx.x);
-  const int64_t stop = work.begin((int)blockIdx.x + 1);
-  GroupWalk<SumCount> walk(p.shape, SumCount{p.tiles}, lane);
+  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, reinterpret_cast<int64_t*>(&a[0][0][0]), p.table);
+  PartWalk work(p.shape, p.tiles, lane, share, (int)blockIdx.x, (int)gridDim.x);
   Part part;
-  while (next_part(walk, unit, stop, part)) {
+  while (work.next(part)) {
     const int n0 = part.tile / p.tiles_in * T, k0 = part.tile % p.tiles_in * T;
     const int64_t r0 = part.begin + (int64_t)part.from * DW_ROWS;
     const int rows = (int)(min((int64_t)part.end, part.begin + (int64_t)part.to * DW_ROWS) - r0);      // none for an empty group
@@ -262,7 +261,7 @@ cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s) {
 cudaError_t launch_grouped_dw_f32(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, false);
   const DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, static_cast<const float*>(c.x), static_cast<const float*>(c.dout),
-                 c.ldx, c.lddout, static_cast<float*>(c.dw), c.dbias, plan.part, plan.part_bias, c.dev_status};
+                 c.ldx, c.lddout, static_cast<float*>(c.dw), c.dbias, plan.part, plan.part_bias, plan.table, c.dev_status};
   return launch_after(grouped_dw_f32_kernel, plan.blocks, p, s);
 }
 

@@ -323,7 +323,8 @@ bool grouped_fits(const vit_grouped_problem* p) {
   const int64_t tiles = ((int64_t)p->rows / 64 + p->groups) * ((widest + 63) / 64);
   const int64_t weights = (int64_t)p->in_features * p->out_features;
   const int64_t sums = ((int64_t)p->in_features / 128 + 1) * ((int64_t)p->out_features / 128 + 1);      // tiles of a group's weights
-  return tiles <= INT32_MAX / 2 && weights <= (int64_t)1 << 36 && p->groups <= INT64_MAX / 16 / weights && sums <= INT32_MAX / 2;
+  const int64_t units = (int64_t)p->rows / 64 + p->groups;
+  return tiles <= INT32_MAX / 2 && weights <= (int64_t)1 << 36 && p->groups <= INT64_MAX / 16 / weights && sums <= INT32_MAX / 2 / units;
 }
 // whether an output lies over the offsets or any other operand
 bool over_offsets(const vit_grouped_problem* p, const Block& out) {

@@ -20,7 +20,9 @@ class _Shape:
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--op", required=True, choices=["linear", "linear_ln", "attention", "layernorm", "rowstats", "rope_axes", "qk_norm_rope",
-                                                   "qk_norm_rope_backward", "attention_packed", "attention_packed_backward"])
+                                                   "qk_norm_rope_backward", "attention_packed", "attention_packed_backward", "layernorm_forward",
+                                                   "layernorm_backward", "linear_grouped", "linear_grouped_backward_input",
+                                                   "linear_grouped_backward_weights", "grad_clip"])
     ap.add_argument("--M", type=int, default=32896)
     ap.add_argument("--N", type=int, default=1280)
     ap.add_argument("--K", type=int, default=1280)
@@ -29,6 +31,8 @@ def main():
     ap.add_argument("--T", type=int, default=257)
     ap.add_argument("--heads", type=int, default=16)
     ap.add_argument("--d", type=int, default=80)
+    ap.add_argument("--groups", type=int, default=1)
+    ap.add_argument("--dtype", choices=["bf16", "fp32"], default="bf16", help="of the operations that training needs")
     ap.add_argument("--reps", type=int, default=5)
     a = ap.parse_args()
     cfg = vit.make_config(_Shape, vit.VIT_BF16, 1)
@@ -111,6 +115,53 @@ def main():
                "qk_norm_rope_backward": lambda: vit.vit_op_qk_norm_rope_backward(*common, dy.data_ptr(), H, y.data_ptr(), H,
                                                                                  dg[0].data_ptr(), dg[1].data_ptr(), ws.data_ptr(), n)}[a.op]
         work = a.M * H * 2 * (3.0 if a.op.endswith("backward") else 2.0) / 1e-3   # bytes, scaled so the print below reads GB/s
+        unit = "GB/s"
+    elif a.op in ("layernorm_forward", "layernorm_backward"):
+        # --M rows of --N columns; the backward pass with the residual path's gradient
+        dt, t = (vit.VIT_BF16, bf) if a.dtype == "bf16" else (vit.VIT_FP32, torch.float32)
+        x, dy, dres = (torch.randn(a.M, a.N, device="cuda").to(t) for _ in range(3))
+        y, stats = torch.empty_like(x), torch.empty(a.M, 2, device="cuda")
+        g, dg = torch.ones(2, a.N, device="cuda"), torch.empty(2, a.N, device="cuda")
+        n = vit.vit_layernorm_backward_bytes(a.M, a.N)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        fwd = lambda: vit.vit_op_layernorm_forward(h, dt, a.M, a.N, x.data_ptr(), a.N, g[0].data_ptr(), g[1].data_ptr(), 1e-6, y.data_ptr(),
+                                                   a.N, stats.data_ptr())
+        fwd()
+        run = fwd if a.op == "layernorm_forward" else lambda: vit.vit_op_layernorm_backward(
+            h, dt, a.M, a.N, x.data_ptr(), a.N, g[0].data_ptr(), stats.data_ptr(), dy.data_ptr(), a.N, dres.data_ptr(), a.N, y.data_ptr(), a.N,
+            dg[0].data_ptr(), dg[1].data_ptr(), ws.data_ptr(), n)
+        work = a.M * a.N * x.element_size() * (2.0 if a.op == "layernorm_forward" else 4.0) / 1e-3   # bytes, as above
+        unit = "GB/s"
+    elif a.op.startswith("linear_grouped"):
+        # --M rows in --groups groups of growing lengths, --K in, --N out; --epilogue 1 keeps GELU's argument (or reads it, backwards)
+        dt, t = (vit.VIT_BF16, bf) if a.dtype == "bf16" else (vit.VIT_FP32, torch.float32)
+        edges = [a.M * g * (g + a.groups) // (2 * a.groups * a.groups) for g in range(a.groups + 1)]
+        off = torch.tensor(edges, dtype=torch.int32, device="cuda")
+        x, dx, pre_k = (torch.randn(a.M, a.K, device="cuda").to(t) for _ in range(3))
+        out, res, pre_n = (torch.randn(a.M, a.N, device="cuda").to(t) for _ in range(3))
+        w = (torch.randn(a.groups, a.N, a.K, device="cuda") / a.K ** 0.5).to(t)
+        b, db, dw = torch.randn(a.groups, a.N, device="cuda"), torch.empty(a.groups, a.N, device="cuda"), torch.empty_like(w)
+        p = vit.make_grouped_problem(a.groups, a.M, a.K, a.N, off.data_ptr())
+        n = vit.vit_linear_grouped_backward_weights_bytes(dt, p)
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        run = {"linear_grouped": lambda: vit.vit_op_linear_grouped(
+                   h, dt, p, x.data_ptr(), a.K, w.data_ptr(), b.data_ptr(), a.epilogue, res.data_ptr(), a.N, out.data_ptr(), a.N,
+                   pre_n.data_ptr() if a.epilogue == 1 else 0, a.N),
+               "linear_grouped_backward_input": lambda: vit.vit_op_linear_grouped_backward_input(
+                   h, dt, p, res.data_ptr(), a.N, w.data_ptr(), pre_k.data_ptr() if a.epilogue == 1 else 0, a.K, dx.data_ptr(), a.K),
+               "linear_grouped_backward_weights": lambda: vit.vit_op_linear_grouped_backward_weights(
+                   h, dt, p, x.data_ptr(), a.K, res.data_ptr(), a.N, dw.data_ptr(), db.data_ptr(), ws.data_ptr(), n)}[a.op]
+        work = 2.0 * a.M * a.N * a.K
+        unit = "TFLOP/s"
+    elif a.op == "grad_clip":
+        # --groups tensors of --M x --N values
+        grads = [torch.randn(a.M, a.N, device="cuda").to(bf) for _ in range(a.groups)]
+        clipped = [torch.empty_like(t) for t in grads]
+        tensors = vit.make_tensors([(t.data_ptr(), c.data_ptr(), t.numel(), vit.VIT_BF16) for t, c in zip(grads, clipped)])
+        n, norm = vit.vit_grad_clip_bytes(a.groups), torch.empty(1, device="cuda")
+        ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+        run = lambda: vit.vit_op_grad_clip(h, tensors, a.groups, 1.0, norm.data_ptr(), ws.data_ptr(), n)
+        work = 2.0 * a.groups * a.M * a.N * 2 / 1e-3   # bytes, as above
         unit = "GB/s"
     else:
         x = torch.randn(a.M, a.N, device="cuda").to(bf)
