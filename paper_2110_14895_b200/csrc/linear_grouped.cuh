@@ -104,12 +104,14 @@ struct TileCount {
 };
 
 // The weights' gradients sum over a group's rows, tile by tile of [out][in], 64 rows to a unit (a group without rows has one
-// for every tile: its zeros).  Tiles are numbered group after group.  All but about the last tile of each block go round: tile i
-// to block i mod blocks, so that the blocks are in the same group at the same rows at a time and find them in L2 (in stretches
+// for every tile: its zeros).  Tiles are numbered group after group.  Whole rounds of them go to the blocks in turn, tile i to
+// block i mod blocks, so that the blocks are in the same group at the same rows at a time and find them in L2 (in stretches
 // of neighbouring tiles all groups were read at once: 1.1 GB from memory for 0.26, and 213 us, at 25216 rows of 16 groups).
-// The last tiles' units lie in one line, of which a block gets as much as makes its work the mean: groups of any lengths come
-// out even, and a long sum with few tiles is cut between all blocks.  A block's first and last tile there may be parts; each
-// part has one owner, and the parts are joined in the order of their rows.
+// The other tiles' units, with several groups a round's at least, lie in one line, of which a block gets as much as makes its
+// work the mean: groups of any lengths come out even, and a long sum with few tiles is cut between all blocks.  A block's first
+// and last tile there may be parts; each part has one owner, and the parts are joined in the order of their rows.
+// Parts begin in the middle where that brings all blocks to the same rows modulo a share: at a time t of its share a block is
+// at unit t + k share of its tile, for some k.
 constexpr int DW_BLOCKS = 148, DW_ROWS = 64, DW_LEAST = 8;       // blocks at most; units of a share of the line at least, unless there are fewer tiles than blocks
 struct SumCount {
   int tiles;
@@ -118,7 +120,7 @@ struct SumCount {
   __device__ __forceinline__ int64_t operator()(int rows) const { return (int64_t)tiles * (whole ? 1 : of(rows)); }
 };
 // What a block does: tiles self, self + blocks, ... below `round`, then units [begin, end) of all.
-struct Share { int round; int64_t begin, end; };
+struct Share { int round; int64_t begin, end; int beat; };      // beat: the mean share
 // begins: of all blocks in the line (absolute units), and behind the last one its end; what a second kernel needs.
 constexpr int DW_TABLE = DW_BLOCKS + 1, DW_SCRATCH = 2 * DW_TABLE;           // 64-bit numbers; of shared memory while the shares are found
 
@@ -126,7 +128,7 @@ constexpr int DW_TABLE = DW_BLOCKS + 1, DW_SCRATCH = 2 * DW_TABLE;           // 
 __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, int blocks, int self, int64_t* scratch, int64_t* table) {
   const int lane = threadIdx.x & 31;
   const int64_t whole = all_units(p, SumCount{tiles, true}, lane), total = all_units(p, SumCount{tiles, false}, lane);
-  const int round = whole / blocks >= 2 ? ((int)(whole / blocks) - 1) * blocks : 0;
+  const int rounds = (int)(whole / blocks), round = (p.groups == 1 ? rounds : rounds > 0 ? rounds - 1 : 0) * blocks;
   int64_t *loads = scratch, *begins = scratch + DW_TABLE;
   for (int c = threadIdx.x; c < blocks; c += (int)blockDim.x) loads[c] = 0;
   __syncthreads();
@@ -178,26 +180,27 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
       if (shares <= line + open || k == 15) break;
       level -= (shares - line) / open;
     }
-    // without a round: no more blocks than have something to do
-    int used = blocks;
-    if (round == 0) {
-      const int64_t wanted = total / DW_LEAST > whole ? total / DW_LEAST : whole;
-      used = (int)(wanted < blocks ? (wanted < 1 ? 1 : wanted) : blocks);
-      shares = used;
-    }
+    // a short line goes to as many blocks as get something to do, the same to each
+    const int64_t left = whole - round, wanted = line / DW_LEAST > left ? line / DW_LEAST : left;
+    const bool few = wanted < blocks;
+    const int used = (int)(wanted < 1 ? 1 : wanted);
+    if (few) shares = used;
     int64_t before = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = lane + 32 * i;
-      const int64_t mine = round == 0 ? (c < used ? 1 : 0) : load[i] < level ? level - load[i] : 0;
+      const int64_t mine = few ? (c < used ? 1 : 0) : load[i] < level ? level - load[i] : 0;
       const int64_t upto = warp_scan(mine, lane);
       if (c < blocks) begins[c] = done + (shares > 0 ? line * (before + upto - mine) / shares : 0);
       before += __shfl_sync(0xffffffffu, upto, 31);
     }
-    if (lane == 0) begins[blocks] = total;
+    if (lane == 0) {
+      begins[blocks] = total;
+      loads[0] = (line + (few ? used : blocks) - 1) / (few ? used : blocks);
+    }
   }
   __syncthreads();
-  const Share share{round, begins[self], begins[self + 1]};
+  const Share share{round, begins[self], begins[self + 1], (int)loads[0]};
   if (table && self == 0)
     for (int c = threadIdx.x; c <= blocks; c += (int)blockDim.x) table[c] = begins[c];
   __syncthreads();                                               // the scratch is free again
@@ -206,7 +209,8 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
 
 // A block's work on one tile: units [from, to) of `all`.  slot: where a part's sums are kept, the share's first or last.
 struct Part {
-  int group, begin, end, tile, from, to, all;
+  int group, begin, end, tile, from, to, all, first;             // first: the unit that it begins with
+  __device__ __forceinline__ int unit(int i) const { return first + i < to ? first + i : first + i - (to - from); }
   __device__ __forceinline__ bool whole() const { return from == 0 && to == all; }
   __device__ __forceinline__ int slot() const { return from == 0 ? 1 : 0; }
   __device__ __forceinline__ int blocks() const { return end > begin ? to - from : 0; }      // of 64 rows
@@ -223,7 +227,7 @@ struct PartWalk {
     GroupAt g;
     if (walk.count.whole) {
       if (at < share.round && walk.find(at, g)) {
-        part = Part{g.group, g.begin, g.end, (int)(at - g.before), 0, 0, SumCount::of(g.end - g.begin)};
+        part = Part{g.group, g.begin, g.end, (int)(at - g.before), 0, 0, SumCount::of(g.end - g.begin), 0};
         part.to = part.all;
         at += blocks;
         return true;
@@ -235,9 +239,13 @@ struct PartWalk {
     if (at >= share.end || !walk.find(at, g)) return false;
     const int all = SumCount::of(g.end - g.begin);
     const int64_t local = at - g.before, tile = local / all;
-    part = Part{g.group, g.begin, g.end, (int)tile, (int)(local - tile * all), 0, all};
+    part = Part{g.group, g.begin, g.end, (int)tile, (int)(local - tile * all), 0, all, 0};
     const int64_t left = share.end - at;
     part.to = left < all - part.from ? part.from + (int)left : all;
+    // the first unit in it that is the time of the share, modulo the beat
+    const int time = (int)((at - share.begin) % share.beat), late = (part.from - time) % share.beat;
+    part.first = part.from + (late > 0 ? share.beat - late : -late);
+    if (part.first >= part.to) part.first = part.from;
     at += part.to - part.from;
     return true;
   }

@@ -114,7 +114,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         ++fills;
         if (lane == 0) {
           const uint32_t sa = tiles + stage * C::STAGE_BYTES, fb = full + 8 * stage;
-          const int row = part.begin + (part.from + kb) * DW_ROWS;
+          const int row = part.begin + part.unit(kb) * DW_ROWS;
           mbar_arrive_expect_tx(fb, C::STAGE_BYTES);
 #pragma unroll
           for (int s = 0; s < 2; ++s) tma_load_2d(sa + s * SLAB_BYTES, &m.dout, n0 + 64 * s, row, fb);
@@ -141,7 +141,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
           if (!warp_wait(ready + 8 * stage, phase, abort_flag)) { ok = false; break; }
           tc_fence_after();
           const uint32_t sa = uniform(tiles + stage * C::STAGE_BYTES);
-          const int steps = (min(DW_ROWS, part.end - part.begin - (part.from + kb) * DW_ROWS) + 15) / 16;
+          const int steps = (min(DW_ROWS, part.end - part.begin - part.unit(kb) * DW_ROWS) + 15) / 16;
           const uint64_t ad = smem_desc(sa, SLAB_BYTES), bd = smem_desc(sa + C::A_BYTES, SLAB_BYTES);
           if (elect_one()) {
 #pragma unroll
@@ -165,7 +165,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     while (ok && work.next(part)) {
       for (int kb = 0; kb < part.blocks(); ++kb) {
         if (!warp_wait(full + 8 * stage, phase, abort_flag)) { ok = false; break; }
-        const int rows = min(DW_ROWS, part.end - part.begin - (part.from + kb) * DW_ROWS);
+        const int rows = min(DW_ROWS, part.end - part.begin - part.unit(kb) * DW_ROWS);
         if (rows & 15) {                               // the group's last rows: the others of their 16 become zero
           const uint32_t sa = tiles + stage * C::STAGE_BYTES;
           for (int s = 0; s < 2 + C::B_SLABS; ++s)
@@ -254,7 +254,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         if (!warp_wait(full + 8 * stage, phase, abort_flag)) { ok = false; break; }
         if (mine) {
           const uint32_t from = tiles + stage * C::STAGE_BYTES + slab * SLAB_BYTES;
-          const int rows = min(DW_ROWS, part.end - part.begin - (part.from + kb) * DW_ROWS);
+          const int rows = min(DW_ROWS, part.end - part.begin - part.unit(kb) * DW_ROWS);
           float2 some[4] = {};
 #pragma unroll 4
           for (int r = first; r < rows; r += 4) {
@@ -322,20 +322,12 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
   grid_dependency_wait();
   const int64_t begin = table[block], end = table[block + 1];
   if (begin >= end || begin == table[0]) return;
-  auto owner = [&](int64_t unit) {                                               // the last block that begins there or before
-    int lo = 0, hi = blocks;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (table[mid] <= unit) lo = mid;
-      else hi = mid;
-    }
-    return lo;
-  };
-  PartWalk work(shape, tiles, lane, Share{0, begin, begin + 1}, 0, 1);
+  PartWalk work(shape, tiles, lane, Share{0, begin, begin + 1, 1}, 0, 1);
   Part here;
   if (!work.next(here) || here.from == 0) return;                                // a tile begins here: nothing is cut
   const int64_t tile_begin = begin - here.from, tile_end = tile_begin + here.all;
-  const int before = owner(begin - 1);
+  int before = block - 1;
+  while (table[before] == begin) --before;                                       // blocks without a share
   if (table[before] > tile_begin) return;                                        // cut before, too: not this block's task
   const int n0 = here.tile / tiles_in * ROWS, k0 = here.tile % tiles_in * COLS, r0 = (int)blockIdx.y * 16;
   constexpr int N = 16 * COLS / 1024;
@@ -345,15 +337,16 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
     sum[i] = *reinterpret_cast<const float4*>(part + ((int64_t)before * 2 + 1) * ROWS * COLS + r0 * COLS + (i * 256 + (int)threadIdx.x) * 4);
   const bool bias = dbias && k0 == 0 && blockIdx.y == 0 && threadIdx.x < ROWS;
   float b = bias ? part_bias[((int64_t)before * 2 + 1) * ROWS + threadIdx.x] : 0.f;
-  for (int64_t u = begin; u < tile_end;) {
-    const int who = owner(u);
+#pragma unroll 4
+  for (int who = block; who < blocks && table[who] < tile_end; ++who) {          // (some have no share: they are added as zeros)
+    const bool some = table[who + 1] > table[who];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float4 v = *reinterpret_cast<const float4*>(part + (int64_t)who * 2 * ROWS * COLS + r0 * COLS + (i * 256 + (int)threadIdx.x) * 4);
+      const float4 v = some ? *reinterpret_cast<const float4*>(part + (int64_t)who * 2 * ROWS * COLS + r0 * COLS + (i * 256 + (int)threadIdx.x) * 4)
+                            : make_float4(0.f, 0.f, 0.f, 0.f);
       sum[i] = make_float4(sum[i].x + v.x, sum[i].y + v.y, sum[i].z + v.z, sum[i].w + v.w);
     }
-    if (bias) b += part_bias[(int64_t)who * 2 * ROWS + threadIdx.x];
-    u = table[who + 1];
+    if (bias && some) b += part_bias[(int64_t)who * 2 * ROWS + threadIdx.x];
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
