@@ -112,7 +112,9 @@ struct TileCount {
 // and last tile there may be parts; each part has one owner, and the parts are joined in the order of their rows.
 // Parts begin in the middle where that brings all blocks to the same rows modulo a share: at a time t of its share a block is
 // at unit t + k share of its tile, for some k.
-constexpr int DW_BLOCKS = 148, DW_ROWS = 64, DW_LEAST = 8;       // blocks at most; units of a share of the line at least, unless there are fewer tiles than blocks
+// Blocks at most; units of a share of the line at least (a part costs about as much as this many), unless there are fewer tiles
+// than blocks: a unit takes 0.3 us on the tensor cores, 5 us on the fp32 pipes.
+constexpr int DW_BLOCKS = 148, DW_BLOCKS_F32 = 296, DW_ROWS = 64, DW_LEAST = 8, DW_LEAST_F32 = 1;
 struct SumCount {
   int tiles;
   bool whole;                                                    // counts tiles, not units
@@ -122,10 +124,10 @@ struct SumCount {
 // What a block does: tiles self, self + blocks, ... below `round`, then units [begin, end) of all.
 struct Share { int round; int64_t begin, end; int beat; };      // beat: the mean share
 // begins: of all blocks in the line (absolute units), and behind the last one its end; what a second kernel needs.
-constexpr int DW_TABLE = DW_BLOCKS + 1, DW_SCRATCH = 2 * DW_TABLE;           // 64-bit numbers; of shared memory while the shares are found
+constexpr int DW_TABLE = DW_BLOCKS_F32 + 1, DW_SCRATCH = 2 * DW_TABLE;           // 64-bit numbers; of shared memory while the shares are found
 
 // All threads of a block, which get the same answer in every block.
-__device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, int blocks, int self, int64_t* scratch, int64_t* table) {
+__device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, int blocks, int self, int least, int64_t* scratch, int64_t* table) {
   const int lane = threadIdx.x & 31;
   const int64_t whole = all_units(p, SumCount{tiles, true}, lane), total = all_units(p, SumCount{tiles, false}, lane);
   const int rounds = (int)(whole / blocks), round = (p.groups == 1 ? rounds : rounds > 0 ? rounds - 1 : 0) * blocks;
@@ -134,8 +136,8 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
   __syncthreads();
   if (round > 0) {
     // units that go round to block c: of a group's tiles [t0, t1) those that are c modulo the blocks
-    const int slices = (int)blockDim.x / blocks, slice = (int)threadIdx.x / blocks, c = (int)threadIdx.x % blocks;
-    if (slice < slices) {
+    const int slices = max((int)blockDim.x / blocks, 1), slice = (int)threadIdx.x / blocks;
+    for (int c = (int)threadIdx.x % blocks; c < blocks && slice < slices; c += slices > 1 ? blocks : (int)blockDim.x) {
       const int per = (p.groups + slices - 1) / slices;
       int64_t sum = 0;
       for (int g = 0, t0 = 0; g < min(p.groups, (slice + 1) * per) && t0 < round; ++g) {
@@ -150,7 +152,7 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
     __syncthreads();
   }
   if (threadIdx.x < 32) {
-    constexpr int N = (DW_BLOCKS + 31) / 32;
+    constexpr int N = (DW_BLOCKS_F32 + 31) / 32;
     int64_t load[N], done = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -181,7 +183,7 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
       level -= (shares - line) / open;
     }
     // a short line goes to as many blocks as get something to do, the same to each
-    const int64_t left = whole - round, wanted = line / DW_LEAST > left ? line / DW_LEAST : left;
+    const int64_t left = whole - round, wanted = line / least > left ? line / least : left;
     const bool few = wanted < blocks;
     const int used = (int)(wanted < 1 ? 1 : wanted);
     if (few) shares = used;

@@ -96,7 +96,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   grid_dependency_wait();
   grid_launch_dependents();
   const uint32_t tmem = *tmem_slot;
-  const Share share = find_share(p.shape, p.tiles, units, self, reinterpret_cast<int64_t*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
+  const Share share = find_share(p.shape, p.tiles, units, self, DW_LEAST, reinterpret_cast<int64_t*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
                                  rank == 0 ? p.table : nullptr);
   PartWalk work(p.shape, p.tiles, lane, share, self, units);
   Part part;
@@ -368,7 +368,8 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   t.tiles = (int)tiles;
   // as many as the rows can need: the kernels, which see the groups' lengths, may use fewer
   const int64_t units = tiles * ((int64_t)shape.rows / DW_ROWS + shape.groups), whole = tiles * shape.groups;
-  const int64_t wanted = units / DW_LEAST > whole ? units / DW_LEAST : whole, most = pair ? DW_BLOCKS / 2 : DW_BLOCKS;
+  const int64_t least = act_bf16 ? DW_LEAST : DW_LEAST_F32, wanted = units / least > whole ? units / least : whole;
+  const int64_t most = pair ? DW_BLOCKS / 2 : act_bf16 ? DW_BLOCKS : DW_BLOCKS_F32;
   t.blocks = (int)(wanted < most ? (wanted < 1 ? 1 : wanted) : most);
   return t;
 }

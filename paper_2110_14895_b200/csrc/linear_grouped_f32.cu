@@ -1,7 +1,8 @@
 // Linear layers by group in the fp32 mode, on the fp32 pipes: rows times their group's weights forwards and backwards, and the
 // weights' gradients.  Tiles of the result in registers, 16 of the summed index at a time through shared memory, the next 16
 // under way while these are multiplied; two products to an instruction (packed fp32).
-// Measured against the floor of 148 SMs x 128 products a cycle; 128 x 128 tiles where there are enough of them to go round.
+// 128 x 128 tiles where there are enough of them to go round, else 64 x 64, whose sums are shared by a cluster of blocks and
+// joined in its shared memory as long as blocks are left over.
 #include "linear_grouped.cuh"
 
 namespace vit {
@@ -64,24 +65,66 @@ __device__ __forceinline__ void multiply(Tile<T>& acc, const float (*a)[T + 4], 
 
 struct RowsArgs {
   GroupedShape shape;
-  int width, sum, epilogue, tiles_n;
+  int width, sum, epilogue, tiles_n, split;
   const float *x, *w, *bias, *residual;
   float *pre, *y;
   int64_t ldx, ldr, ldp, ldy;
   int* dev_status;
 };
 
+// four values of a row of the result: bias, GELU, residual or GELU's slope, and out
+template <bool BACKWARD>
+__device__ __forceinline__ void finish(const RowsArgs& p, int group, int64_t row, int c, float4 sum) {
+  float v[4] = {sum.x, sum.y, sum.z, sum.w};
+  if (BACKWARD) {
+    if (p.pre) {
+      const float4 o = *reinterpret_cast<const float4*>(p.pre + row * p.ldp + c);
+      const float f[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] *= gelu_slope_f32(f[e]);
+    }
+  } else {
+    if (p.bias) {
+      const float4 o = *reinterpret_cast<const float4*>(p.bias + (int64_t)group * p.width + c);
+      v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
+    }
+    if (p.epilogue == 1) {
+      if (p.pre) *reinterpret_cast<float4*>(p.pre + row * p.ldp + c) = make_float4(v[0], v[1], v[2], v[3]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = gelu_f32(v[e]);
+    } else if (p.epilogue == 2) {
+      const float4 o = *reinterpret_cast<const float4*>(p.residual + row * p.ldr + c);
+      v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
+    }
+  }
+  *reinterpret_cast<float4*>(p.y + row * p.ldy + c) = make_float4(v[0], v[1], v[2], v[3]);
+}
+__device__ __forceinline__ float4 read_cluster(const float* here, uint32_t rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(ptx::map_to_cta(ptx::smem_u32(here), rank)) : "memory");
+  return v;
+}
+
+template <int T> union Stages {
+  struct { float a[2][KS][T + 4], b[2][KS][T + 4]; } s;
+  float sums[T == SMALL ? T : 1][T + 4];               // a block's part of a tile whose sums are shared
+};
+
 template <int T, bool BACKWARD>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, T == WIDE ? 2 : 4)
 grouped_rows_f32_kernel(const RowsArgs p) {
-  __shared__ __align__(16) float a[2][KS][T + 4], b[2][KS][T + 4];
+  __shared__ __align__(16) Stages<T> mem;
+  auto &a = mem.s.a, &b = mem.s.b;
   const int lane = threadIdx.x & 31, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int split = T == SMALL ? p.split : 1, self = (int)blockIdx.x / split, units = (int)gridDim.x / split;
+  const uint32_t rank = blockIdx.x % split;            // in the cluster that shares a tile's sums
+  const int share = (p.sum + KS * split - 1) / (KS * split) * KS, k_begin = (int)rank * share, k_end = min(p.sum, k_begin + share);
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
   GroupWalk<TileCount> walk(p.shape, TileCount{T, p.tiles_n}, lane);
   GroupAt at;
-  for (int64_t tile = blockIdx.x; walk.find(tile, at); tile += gridDim.x) {
+  for (int64_t tile = self; walk.find(tile, at); tile += units) {
     const int local = (int)(tile - at.before), row0 = at.begin + local / p.tiles_n * T, col0 = local % p.tiles_n * T;
     const int rows = min(T, at.end - row0), cols = min(T, p.width - col0);
     const float* x = p.x + (int64_t)row0 * p.ldx;
@@ -90,19 +133,19 @@ grouped_rows_f32_kernel(const RowsArgs p) {
     const int64_t ldw = BACKWARD ? p.width : p.sum;
     Tile<T> acc = {};
     float4 va[T / 64], vb[T / 64];
-    fetch<T, false>(va, x, p.ldx, rows, p.sum);
-    fetch<T, BACKWARD>(vb, w, ldw, cols, p.sum);
+    auto get = [&](int k) {
+      fetch<T, false>(va, x + k, p.ldx, rows, k_end - k);
+      fetch<T, BACKWARD>(vb, w + (BACKWARD ? (int64_t)k * ldw : (int64_t)k), ldw, cols, k_end - k);
+    };
+    get(k_begin);
     __syncthreads();                                    // the tile before has been multiplied
     keep<T, false>(va, a[0]);
     keep<T, BACKWARD>(vb, b[0]);
     __syncthreads();
     int now = 0;
-    for (int k = 0; k < p.sum; k += KS, now ^= 1) {
-      const bool more = k + KS < p.sum;
-      if (more) {
-        fetch<T, false>(va, x + k + KS, p.ldx, rows, p.sum - k - KS);
-        fetch<T, BACKWARD>(vb, w + (BACKWARD ? (int64_t)(k + KS) * ldw : (int64_t)(k + KS)), ldw, cols, p.sum - k - KS);
-      }
+    for (int k = k_begin; k < k_end; k += KS, now ^= 1) {
+      const bool more = k + KS < k_end;
+      if (more) get(k + KS);
       multiply<T>(acc, a[now], b[now]);
       if (more) {
         keep<T, false>(va, a[now ^ 1]);
@@ -110,38 +153,36 @@ grouped_rows_f32_kernel(const RowsArgs p) {
       }
       __syncthreads();
     }
+    if (split == 1) {
 #pragma unroll
-    for (int i = 0; i < T / 16; ++i) {
-      const int row = row0 + part_at<T>(i, ty);
-      if (row >= at.end) continue;
+      for (int i = 0; i < T / 16; ++i) {
+        const int row = row0 + part_at<T>(i, ty);
+        if (row >= at.end) continue;
 #pragma unroll
-      for (int h = 0; h < T / 64; ++h) {
-        const int c = col0 + 64 * h + 4 * tx;
-        if (c >= p.width) continue;
-        float v[4] = {acc.v[i][2 * h].x, acc.v[i][2 * h].y, acc.v[i][2 * h + 1].x, acc.v[i][2 * h + 1].y};
-        if (BACKWARD) {
-          if (p.pre) {
-            const float4 o = *reinterpret_cast<const float4*>(p.pre + row * p.ldp + c);
-            const float f[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] *= gelu_slope_f32(f[e]);
-          }
-        } else {
-          if (p.bias) {
-            const float4 o = *reinterpret_cast<const float4*>(p.bias + (int64_t)at.group * p.width + c);
-            v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
-          }
-          if (p.epilogue == 1) {
-            if (p.pre) *reinterpret_cast<float4*>(p.pre + row * p.ldp + c) = make_float4(v[0], v[1], v[2], v[3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = gelu_f32(v[e]);
-          } else if (p.epilogue == 2) {
-            const float4 o = *reinterpret_cast<const float4*>(p.residual + row * p.ldr + c);
-            v[0] += o.x; v[1] += o.y; v[2] += o.z; v[3] += o.w;
-          }
+        for (int h = 0; h < T / 64; ++h) {
+          const int c = col0 + 64 * h + 4 * tx;
+          if (c < p.width)
+            finish<BACKWARD>(p, at.group, row, c, make_float4(acc.v[i][2 * h].x, acc.v[i][2 * h].y, acc.v[i][2 * h + 1].x, acc.v[i][2 * h + 1].y));
         }
-        *reinterpret_cast<float4*>(p.y + row * p.ldy + c) = make_float4(v[0], v[1], v[2], v[3]);
       }
+    } else if (T == SMALL) {
+      // every block leaves its part where the others can read it, and finishes some of the rows
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(&mem.sums[(4 * ty + i) % (T == SMALL ? T : 1)][4 * tx]) = make_float4(acc.v[i][0].x, acc.v[i][0].y, acc.v[i][1].x, acc.v[i][1].y);
+      ptx::cluster_sync();
+      for (int i = threadIdx.x; i < T / split * 16; i += THREADS) {
+        const int r = (int)rank * (T / split) + i / 16, c = i % 16 * 4;
+        if (row0 + r >= at.end || col0 + c >= p.width) continue;
+        const float* from = &mem.sums[r % (T == SMALL ? T : 1)][c];
+        float4 sum = read_cluster(from, 0);
+        for (int k = 1; k < split; ++k) {
+          const float4 v = read_cluster(from, (uint32_t)k);
+          sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+        }
+        finish<BACKWARD>(p, at.group, row0 + r, col0 + c, sum);
+      }
+      ptx::cluster_sync();                              // nobody reads there any more
     }
   }
 }
@@ -156,7 +197,7 @@ struct DwArgs {
   int* dev_status;
 };
 
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(THREADS, 2)
 grouped_dw_f32_kernel(const DwArgs p) {
   constexpr int T = WIDE;
   __shared__ __align__(16) float a[2][KS][T + 4], b[2][KS][T + 4];
@@ -164,7 +205,7 @@ grouped_dw_f32_kernel(const DwArgs p) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
-  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, reinterpret_cast<int64_t*>(&a[0][0][0]), p.table);
+  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, DW_LEAST_F32, reinterpret_cast<int64_t*>(&a[0][0][0]), p.table);
   PartWalk work(p.shape, p.tiles, lane, share, (int)blockIdx.x, (int)gridDim.x);
   Part part;
   while (work.next(part)) {
@@ -220,16 +261,20 @@ grouped_dw_f32_kernel(const DwArgs p) {
 }
 
 template <typename Kernel, typename Args>
-cudaError_t launch_after(Kernel kernel, int grid, const Args& args, cudaStream_t s) {
+cudaError_t launch_after(Kernel kernel, int grid, const Args& args, cudaStream_t s, int cluster = 1) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);
   cfg.stream = s;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
@@ -244,7 +289,7 @@ cudaError_t launch_check_groups(const GroupedCall& c, cudaStream_t s) {
 }
 
 cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s) {
-  RowsArgs p{c.shape, c.backward ? c.in : c.out_features, c.backward ? c.out_features : c.in, c.epilogue, 0, static_cast<const float*>(c.x),
+  RowsArgs p{c.shape, c.backward ? c.in : c.out_features, c.backward ? c.out_features : c.in, c.epilogue, 0, 1, static_cast<const float*>(c.x),
              static_cast<const float*>(c.w), c.bias, static_cast<const float*>(c.residual), static_cast<float*>(c.pre), static_cast<float*>(c.y),
              c.ldx, c.ldr, c.ldp, c.ldy, c.dev_status};
   const int sms = current_device_sm_count();
@@ -252,10 +297,13 @@ cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s) {
   const bool wide = tiles(WIDE) >= 2 * (int64_t)sms;
   const int t = wide ? WIDE : SMALL;
   p.tiles_n = (p.width + t - 1) / t;
+  // at least 64 of a sum to a block, and no more blocks than run at once
+  if (!wide)
+    while (p.split < 8 && tiles(t) * p.split * 2 <= (int64_t)sms * 2 && p.sum >= 128 * p.split) p.split *= 2;
   const int64_t most = (int64_t)sms * (wide ? 2 : 4);
-  const int grid = (int)(tiles(t) < most ? tiles(t) : most);
-  if (c.backward) return wide ? launch_after(grouped_rows_f32_kernel<WIDE, true>, grid, p, s) : launch_after(grouped_rows_f32_kernel<SMALL, true>, grid, p, s);
-  return wide ? launch_after(grouped_rows_f32_kernel<WIDE, false>, grid, p, s) : launch_after(grouped_rows_f32_kernel<SMALL, false>, grid, p, s);
+  const int grid = (int)(tiles(t) < most ? tiles(t) : most) * p.split;
+  if (c.backward) return wide ? launch_after(grouped_rows_f32_kernel<WIDE, true>, grid, p, s) : launch_after(grouped_rows_f32_kernel<SMALL, true>, grid, p, s, p.split);
+  return wide ? launch_after(grouped_rows_f32_kernel<WIDE, false>, grid, p, s) : launch_after(grouped_rows_f32_kernel<SMALL, false>, grid, p, s, p.split);
 }
 
 cudaError_t launch_grouped_dw_f32(const GroupedCall& c, cudaStream_t s) {
