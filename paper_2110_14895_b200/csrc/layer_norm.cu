@@ -51,12 +51,12 @@ __device__ __forceinline__ void store_piece(float* p, const float2 (&v)[4]) {
   reinterpret_cast<float4*>(p)[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
 }
 
-// Sums over a row's warps: one, or the four of a group of 128 threads, which meet at a barrier of their own.  Two slots,
+// One or two sums (N) over a row's warps: one, or the four of a group of 128 threads, which meet at a barrier of their own.  Two slots,
 // used in turn, keep a late reader from the next sum's writers.
-template <int WPR>
+template <int WPR, int N>
 __device__ __forceinline__ float2 row_sums(float2 v, float2 (*slots)[4], int& turn) {
   v.x = warp_sum(v.x);
-  v.y = warp_sum(v.y);
+  if (N == 2) v.y = warp_sum(v.y);
   if (WPR == 1) return v;
   const int warp = threadIdx.x >> 5, group = warp / WPR;
   float2* s = slots[2 * group + turn];
@@ -78,43 +78,67 @@ struct ForwardArgs {
   int rows, cols;
 };
 
-template <typename T, int NCH, int WPR>
-__global__ void __launch_bounds__(256)
+// R rows at a time share the loads of gain and shift, which are four times a bf16 row's own: 32896 rows of 1280 columns take 36
+// us one at a time (whatever the number of warps, with or without rows fetched ahead), 31 with two, 32 with three or four.
+constexpr int FORWARD_THREADS = 128;
+template <typename T, int NCH, int WPR, int R>            // R: 1 or 2
+__global__ void __launch_bounds__(FORWARD_THREADS)
 layer_norm_kernel(const ForwardArgs p) {
-  __shared__ float2 slots[2 * 8 / WPR][4];
+  __shared__ float2 slots[2][4];
   const int warp = threadIdx.x >> 5, at = (warp % WPR) * 32 + (threadIdx.x & 31);
-  const int64_t row = (int64_t)blockIdx.x * (8 / WPR) + warp / WPR;
+  const int64_t row = ((int64_t)blockIdx.x * (FORWARD_THREADS / 32 / WPR) + warp / WPR) * R;
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (row >= p.rows) return;                    // all warps of a row together
-  const int pieces = p.cols / CH;
   const T* x = static_cast<const T*>(p.x) + row * p.ldx;
-  Raw<T> raw[NCH];
+  Raw<T> raw[R][NCH];
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)                 // all loads in flight before the first use
-    if (at + 32 * WPR * i < pieces) raw[i] = load_raw(x + (at + 32 * WPR * i) * CH);
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {             // all loads in flight before the first use
+      const int c = (at + 32 * WPR * i) * CH;
+      if (c < p.cols && row + r < p.rows) raw[r][i] = load_raw(x + r * p.ldx + c);
+    }
   int turn = 0;
-  float2 v[NCH][4], sum = make_float2(0.f, 0.f);
+  float mean[R], rstd[R];
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)
-    if (at + 32 * WPR * i < pieces) {
-      open(raw[i], v[i]);
+  for (int r = 0; r < R; ++r) {
+    float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum = __fadd2_rn(sum, v[i][e]);
-    }
-  const float mean = row_sums<WPR>(make_float2(sum.x + sum.y, 0.f), slots, turn).x / (float)p.cols;
-  sum = make_float2(0.f, 0.f);
+    for (int i = 0; i < NCH; ++i)
+      if ((at + 32 * WPR * i) * CH < p.cols) {
+        float2 v[4];
+        open(raw[r][i], v);
 #pragma unroll
-  for (int i = 0; i < NCH; ++i)
-    if (at + 32 * WPR * i < pieces) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[i][e] = __fadd2_rn(v[i][e], twice(-mean));
-        sum = __ffma2_rn(v[i][e], v[i][e], sum);
+        for (int e = 0; e < 4; ++e) sum = __fadd2_rn(sum, v[e]);
       }
-    }
-  const float rstd = 1.0f / sqrtf(row_sums<WPR>(make_float2(sum.x + sum.y, 0.f), slots, turn).x / (float)p.cols + p.eps);
-  if (at == 0 && p.stats) p.stats[row] = make_float2(mean, rstd);
+    mean[r] = sum.x + sum.y;
+  }
+  float2 both = row_sums<WPR, R>(make_float2(mean[0], mean[R - 1]), slots, turn);
+  mean[0] = both.x / (float)p.cols;
+  if (R == 2) mean[R - 1] = both.y / (float)p.cols;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+      if ((at + 32 * WPR * i) * CH < p.cols) {
+        float2 v[4];
+        open(raw[r][i], v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] = __fadd2_rn(v[e], twice(-mean[r]));
+          sum = __ffma2_rn(v[e], v[e], sum);
+        }
+      }
+    rstd[r] = sum.x + sum.y;
+  }
+  both = row_sums<WPR, R>(make_float2(rstd[0], rstd[R - 1]), slots, turn);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    rstd[r] = 1.0f / sqrtf((r == 0 ? both.x : both.y) / (float)p.cols + p.eps);
+    if (at == 0 && p.stats && row + r < p.rows) p.stats[row + r] = make_float2(mean[r], rstd[r]);
+  }
   T* y = static_cast<T*>(p.y) + row * p.ldy;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
@@ -124,8 +148,13 @@ layer_norm_kernel(const ForwardArgs p) {
       open(load_raw(p.gain + c), g);
       open(load_raw(p.shift + c), b);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[i][e] = __ffma2_rn(__fmul2_rn(v[i][e], twice(rstd)), g[e], b[e]);
-      store_piece(y + c, v[i]);
+      for (int r = 0; r < R; ++r) {
+        float2 v[4];
+        open(raw[r][i], v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __ffma2_rn(__fmul2_rn(__fadd2_rn(v[e], twice(-mean[r])), twice(rstd[r])), g[e], b[e]);
+        if (row + r < p.rows) store_piece(y + r * p.ldy + c, v);
+      }
     }
   }
 }
@@ -154,9 +183,6 @@ layer_norm_backward_kernel(const BackwardArgs p) {
   const int arrays = p.dres ? 3 : 2;
   const uint32_t row_bytes = (uint32_t)p.cols * sizeof(T), stage_bytes = row_bytes * arrays;
   uint8_t* ring = smem + (size_t)p.cols * 4 + (size_t)(warp / WPR) * p.stages * stage_bytes;
-  for (int i = threadIdx.x; i < p.cols; i += WARPS * 32) gain[i] = p.gain[i];
-  __syncthreads();
-
   auto fetch = [&](int64_t row, int stage) {
     if (row < p.rows) {
       const uint32_t to = ptx::smem_u32(ring + stage * stage_bytes);
@@ -187,7 +213,11 @@ layer_norm_backward_kernel(const BackwardArgs p) {
     for (int e = 0; e < 4; ++e) dg[i][e] = db[i][e] = make_float2(0.f, 0.f);
   const float inv = 1.0f / (float)p.cols;
   int64_t row = (int64_t)blockIdx.x * (WARPS / WPR) + warp / WPR;
+  ptx::grid_dependency_wait();
+  ptx::grid_launch_dependents();
   for (int s = 0; s < p.stages - 1; ++s) fetch(row + s * step, s);
+  for (int i = 4 * threadIdx.x; i < p.cols; i += WARPS * 128) *reinterpret_cast<float4*>(gain + i) = *reinterpret_cast<const float4*>(p.gain + i);
+  __syncthreads();
   float2 st = row < p.rows ? p.stats[row] : make_float2(0.f, 0.f);
   int stage = 0, turn = 0;
   for (; row < p.rows; row += step) {
@@ -220,7 +250,7 @@ layer_norm_backward_kernel(const BackwardArgs p) {
         }
       }
     }
-    const float2 sums = row_sums<WPR>(make_float2(s1.x + s1.y, s2.x + s2.y), slots, turn);
+    const float2 sums = row_sums<WPR, 2>(make_float2(s1.x + s1.y, s2.x + s2.y), slots, turn);
     const float2 c1 = twice(-sums.x * inv), c2 = twice(-sums.y * inv);
     T* dx = static_cast<T*>(p.dx) + row * p.lddx;
 #pragma unroll
@@ -247,7 +277,6 @@ layer_norm_backward_kernel(const BackwardArgs p) {
     st = st_next;
     if (++stage == p.stages) stage = 0;
   }
-  ptx::grid_launch_dependents();
   // this block's share of dg and db: its rows' warps are added in a fixed order
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
@@ -261,22 +290,35 @@ layer_norm_backward_kernel(const BackwardArgs p) {
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * p.cols; i += WARPS * 32) {
-    float sum = 0.f;
-    for (int w = 0; w < WARPS / WPR; ++w) sum += share[(size_t)w * 2 * p.cols + i];
-    p.partial[(int64_t)blockIdx.x * 2 * p.cols + i] = sum;
+  for (int i = 4 * threadIdx.x; i < 2 * p.cols; i += WARPS * 128) {
+    float4 sum = *reinterpret_cast<const float4*>(share + i);
+#pragma unroll
+    for (int w = 1; w < WARPS / WPR; ++w) {
+      const float4 v = *reinterpret_cast<const float4*>(share + (size_t)w * 2 * p.cols + i);
+      sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+    }
+    *reinterpret_cast<float4*>(p.partial + (int64_t)blockIdx.x * 2 * p.cols + i) = sum;
   }
 }
 
-// dgain[c], dshift[c] = sum of the blocks' shares, in a fixed order: 8 columns (a sector) to a block, 32 threads to a column
-__global__ void __launch_bounds__(256)
+// dgain[c], dshift[c] = sum of the blocks' shares, in a fixed order: 8 columns (a sector) to a block, 32 threads to a column, all
+// loads of a thread in flight together (one after the other they took 8 us for 148 shares of 1024 columns, now 4)
+constexpr int COLUMN_THREADS = 256;
+__global__ void __launch_bounds__(COLUMN_THREADS)
 column_grad_kernel(const float* __restrict__ partial, int blocks, int cols, float* __restrict__ dgain, float* __restrict__ dshift) {
-  __shared__ float sums[8][8];
+  __shared__ float sums[COLUMN_THREADS / 32][8];
   const int column = threadIdx.x & 7, part = threadIdx.x >> 3, i = blockIdx.x * 8 + column;
   ptx::grid_dependency_wait();                           // the shares are written by the kernel before this one
-  float sum = 0.f;
-#pragma unroll 5
-  for (int b = part; b < blocks; b += 32) sum += partial[(int64_t)b * 2 * cols + i];
+  ptx::grid_launch_dependents();
+  constexpr int N = LAYER_NORM_MAX_BLOCKS / (COLUMN_THREADS / 8);
+  float v[N], sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int b = part + k * (COLUMN_THREADS / 8);
+    v[k] = b < blocks ? partial[(int64_t)b * 2 * cols + i] : 0.f;
+  }
+#pragma unroll
+  for (int k = 0; k < N; ++k) sum += v[k];
   sum += __shfl_xor_sync(0xffffffffu, sum, 8);
   sum += __shfl_xor_sync(0xffffffffu, sum, 16);
   if ((threadIdx.x & 31) < 8) sums[threadIdx.x >> 5][column] = sum;
@@ -284,7 +326,7 @@ column_grad_kernel(const float* __restrict__ partial, int blocks, int cols, floa
   if (threadIdx.x < 8) {
     sum = 0.f;
 #pragma unroll
-    for (int b = 0; b < 8; ++b) sum += sums[b][column];
+    for (int b = 0; b < COLUMN_THREADS / 32; ++b) sum += sums[b][column];
     (i < cols ? dgain : dshift)[i < cols ? i : i - cols] = sum;
   }
 }
@@ -304,34 +346,43 @@ cudaError_t launch_after(Kernel kernel, int grid, int threads, size_t smem, cuda
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <typename T, int NCH, int WPR>
+template <typename T, int NCH, int WPR, int R>
 cudaError_t launch_forward(const ForwardArgs& a, cudaStream_t s) {
-  return launch_after(layer_norm_kernel<T, NCH, WPR>, (a.rows + 8 / WPR - 1) / (8 / WPR), 256, 0, s, a);
+  constexpr int ROWS = FORWARD_THREADS / 32 / WPR * R;
+  return launch_after(layer_norm_kernel<T, NCH, WPR, R>, (int)(((int64_t)a.rows + ROWS - 1) / ROWS), FORWARD_THREADS, 0, s, a);
+}
+// two rows to a warp where there are rows enough for 16 warps an SM, and registers for them
+template <typename T, int NCH>
+cudaError_t launch_narrow(const ForwardArgs& a, cudaStream_t s) {
+  if constexpr (NCH * sizeof(T) <= 12)
+    if (a.rows >= 32 * current_device_sm_count()) return launch_forward<T, NCH, 1, 2>(a, s);
+  return launch_forward<T, NCH, 1, 1>(a, s);
 }
 template <typename T>
 cudaError_t dispatch_forward(const ForwardArgs& a, cudaStream_t s) {
   const int per_warp = (a.cols + 32 * CH - 1) / (32 * CH);
   if (a.cols <= NARROW) switch (per_warp) {
-    case 1: return launch_forward<T, 1, 1>(a, s);
-    case 2: return launch_forward<T, 2, 1>(a, s);
-    case 3: return launch_forward<T, 3, 1>(a, s);
-    case 4: return launch_forward<T, 4, 1>(a, s);
-    case 5: return launch_forward<T, 5, 1>(a, s);
-    case 6: return launch_forward<T, 6, 1>(a, s);
-    default: return launch_forward<T, 8, 1>(a, s);
+    case 1: return launch_narrow<T, 1>(a, s);
+    case 2: return launch_narrow<T, 2>(a, s);
+    case 3: return launch_narrow<T, 3>(a, s);
+    case 4: return launch_narrow<T, 4>(a, s);
+    case 5: return launch_narrow<T, 5>(a, s);
+    case 6: return launch_narrow<T, 6>(a, s);
+    default: return launch_narrow<T, 8>(a, s);
   }
-  return per_warp <= 16 ? launch_forward<T, 4, 4>(a, s) : launch_forward<T, 8, 4>(a, s);
+  if (per_warp <= 16) return launch_forward<T, 4, 4, sizeof(T) == 2 ? 2 : 1>(a, s);
+  return launch_forward<T, 8, 4, 1>(a, s);
 }
 
-constexpr int RING_BYTES = 200 * 1024;          // of shared memory
+constexpr size_t SHARED_BYTES = 225 * 1024;
 
 template <typename T, int NCH, int WPR, int WARPS>
 cudaError_t launch_backward(BackwardArgs a, cudaStream_t s, int* blocks) {
   static PerDeviceFlag done;
   auto kernel = layer_norm_backward_kernel<T, NCH, WPR, WARPS>;
-  if (cudaError_t e = ensure_dynamic_smem(done, kernel, 225 * 1024)) return e;
+  if (cudaError_t e = ensure_dynamic_smem(done, kernel, (int)SHARED_BYTES)) return e;
   const size_t stage = (size_t)(WARPS / WPR) * a.cols * sizeof(T) * (a.dres ? 3 : 2);
-  a.stages = 3 * stage <= RING_BYTES ? 3 : 2;
+  a.stages = 3 * stage + (size_t)a.cols * sizeof(float) <= SHARED_BYTES ? 3 : 2;
   size_t smem = a.stages * stage;
   const size_t share = (size_t)(WARPS / WPR) * 2 * a.cols * sizeof(float);
   if (smem < share) smem = share;
@@ -340,25 +391,22 @@ cudaError_t launch_backward(BackwardArgs a, cudaStream_t s, int* blocks) {
   const int sms = current_device_sm_count();
   *blocks = (int)(want < sms ? want : sms);
   if (*blocks > LAYER_NORM_MAX_BLOCKS) *blocks = LAYER_NORM_MAX_BLOCKS;
-  kernel<<<*blocks, WARPS * 32, smem, s>>>(a);
-  return cudaGetLastError();
+  return launch_after(kernel, *blocks, WARPS * 32, smem, s, a);
 }
-// Twelve warps where their sums leave each thread enough of the registers (64 sums at 1024 columns), eight beyond; fp32 rows
-// wider than 1024 columns would not leave room for a ring of twelve.
+// The sums of dg and db are what a thread needs registers for: with a warp to a row of 1024 columns 64, twelve warps fit an SM
+// and wait for one another's instructions (22 us at 12608 rows); two warps to a row leave room for twenty (xx us).  fp32 rows
+// are twice as long in the ring.
 template <typename T>
 cudaError_t dispatch_backward(const BackwardArgs& a, cudaStream_t s, int* blocks) {
-  const int per_warp = (a.cols + 32 * CH - 1) / (32 * CH);
-  if (a.cols <= NARROW) switch (per_warp) {
-    case 1: return launch_backward<T, 1, 1, 12>(a, s, blocks);
-    case 2: return launch_backward<T, 2, 1, 12>(a, s, blocks);
-    case 3: return launch_backward<T, 3, 1, 12>(a, s, blocks);
-    case 4: return launch_backward<T, 4, 1, sizeof(T) == 2 ? 12 : 8>(a, s, blocks);
-    case 5: return launch_backward<T, 5, 1, sizeof(T) == 2 ? 12 : 6>(a, s, blocks);
-    case 6: return launch_backward<T, 6, 1, sizeof(T) == 2 ? 8 : 5>(a, s, blocks);
-    default: return launch_backward<T, 8, 1, sizeof(T) == 2 ? 8 : 4>(a, s, blocks);
-  }
-  if (per_warp <= 16) return launch_backward<T, 4, 4, sizeof(T) == 2 ? 12 : 8>(a, s, blocks);
-  return launch_backward<T, 8, 4, sizeof(T) == 2 ? 8 : 4>(a, s, blocks);
+  constexpr bool F = sizeof(T) == 4;
+  if (a.cols <= 256) return launch_backward<T, 1, 1, 16>(a, s, blocks);
+  if (a.cols <= 512) return launch_backward<T, 2, 1, 16>(a, s, blocks);
+  if (a.cols <= 768) return launch_backward<T, 3, 1, 12>(a, s, blocks);
+  if (a.cols <= 1024) return launch_backward<T, 2, 2, F ? 16 : 20>(a, s, blocks);
+  if (a.cols <= 1536) return launch_backward<T, 3, 2, F ? 12 : 16>(a, s, blocks);
+  if (a.cols <= 2048) return launch_backward<T, 2, 4, F ? 16 : 20>(a, s, blocks);
+  if (a.cols <= 4096) return launch_backward<T, 4, 4, F ? 8 : 12>(a, s, blocks);
+  return launch_backward<T, 8, 4, F ? 4 : 8>(a, s, blocks);
 }
 
 }  // namespace
@@ -374,7 +422,7 @@ cudaError_t launch_layer_norm_backward(const LayerNormCall& c, float* partial, i
 }
 
 cudaError_t launch_column_grad(const float* partial, int blocks, int cols, float* dgain, float* dshift, cudaStream_t s) {
-  return launch_after(column_grad_kernel, 2 * cols / 8, 256, 0, s, partial, blocks, cols, dgain, dshift);
+  return launch_after(column_grad_kernel, 2 * cols / 8, COLUMN_THREADS, 0, s, partial, blocks, cols, dgain, dshift);
 }
 
 }  // namespace vit
