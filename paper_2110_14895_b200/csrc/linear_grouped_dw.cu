@@ -21,7 +21,7 @@ using namespace grouped;
 
 namespace {
 
-constexpr int TN = 256, SUM_WARPS = 2, DW_THREADS = THREADS + 32 * (SUM_WARPS + 1);
+constexpr int TN = 256, EPI_WARPS = 8, SUM_WARPS = 2, DW_THREADS = 32 * (2 + EPI_WARPS + SUM_WARPS + 1);
 template <int CTAS> struct DwCfg {
   static constexpr int B_SLABS = 4 / CTAS, A_BYTES = 2 * SLAB_BYTES, STAGE_BYTES = A_BYTES + B_SLABS * SLAB_BYTES, STAGES = CTAS == 2 ? 6 : 4;
   static constexpr int STAGING_BYTES = EPI_WARPS * 4096, SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 256;
@@ -198,17 +198,19 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
 #pragma unroll 1
         for (int cb = 0; cb < 2; ++cb) {
           if (k0 + 64 * cb >= p.in || n0 >= p.out) break;
-          uint32_t r[64];
-          tmem_ld32(taddr + 64 * cb, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
-          tmem_ld32(taddr + 64 * cb + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
-          tmem_ld_wait();
-          float2 v[32];
-#pragma unroll
-          for (int e = 0; e < 32; ++e)
-            v[e] = part.end > part.begin ? make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])) : make_float2(0.f, 0.f);
           if (lane == 0) tma_store_wait_read();
           __syncwarp();
-          put_rows(v, stg, lane);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[32];
+            tmem_ld32(taddr + 64 * cb + 32 * h, r);
+            tmem_ld_wait();
+            float2 v[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              v[e] = part.end > part.begin ? make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1])) : make_float2(0.f, 0.f);
+            put_half(v, stg, lane, h);
+          }
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) tma_store_3d(&m.dw, stg, k0 + 64 * cb, n0, part.group);      // rows and columns beyond are clipped
@@ -235,10 +237,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        if (CTAS == 2) mbar_arrive_cluster(map_to_cta(tempty + 8 * buf, 0));
-        else mbar_arrive(tempty + 8 * buf);
-      }
+      if (lane == 0) give_back<CTAS>(tempty + 8 * buf);
       if (++buf == 2) { buf = 0; aphase ^= 1; }
     }
     if (lane == 0) tma_store_wait_all();

@@ -3,8 +3,8 @@
 //   forward          out[r,:] = f(x[r,:] . W_g^T + b_g),      f: identity, GELU (the argument kept too), + residual
 //   input gradient   dx[r,:] = (dout[r,:] . W_g) gelu'(pre[r,:])
 //
-// Persistent blocks, one per SM: a producer warp (TMA), a warp that issues the products, eight epilogue warps, two
-// accumulators in tensor memory, so that a tile's epilogue runs beside the next tile's products.  Tiles are numbered group
+// Persistent blocks, one per SM: a producer warp (TMA), a warp that issues the products, eight or sixteen epilogue warps,
+// two accumulators in tensor memory, so that a tile's epilogue runs beside the next tile's products.  Tiles are numbered group
 // after group; each warp finds its tiles in the offsets by itself, 32 groups at a look, so that a call needs neither a
 // launch nor a table for them.  A tile begins at its group's first row (TMA copies may begin at any row) and its rows behind
 // the group's end are computed and left unwritten: whole pieces of 32 rows leave by TMA, the last one row by row.
@@ -29,8 +29,11 @@ enum Finish : int { F_BIAS = 0, F_GELU = 1, F_GELU_PRE = 2, F_RESIDUAL = 3, F_SL
 template <int BN, int CTAS, int FINISH> struct Cfg {
   static constexpr int B_ROWS = BN / CTAS;                 // columns of the result whose weights this block loads
   static constexpr int A_BYTES = BM * BK * 2, B_BYTES = B_ROWS * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int BUFFERS = FINISH == F_BIAS || FINISH == F_GELU ? 1 : 2;      // 4 KB pieces of an epilogue warp
-  static constexpr int STAGING_BYTES = EPI_WARPS * BUFFERS * 4096;
+  // An epilogue warp has 32 rows and 64 columns of a tile at a time, and 4 KB of shared memory for them.  Eight warps are
+  // enough to add a bias, and leave room for a stage more (163 against 168 us at 25216 rows of 16 groups, 1024 x 4096);
+  // GELU, its slope (213 against 200 us) and what is read besides take sixteen.
+  static constexpr int EPI_WARPS = BN == 256 && FINISH != F_BIAS ? 16 : 8, STEPS = BN / 16 / EPI_WARPS, THREADS = (2 + EPI_WARPS) * 32;
+  static constexpr int STAGING_BYTES = EPI_WARPS * 4096;
   static constexpr int ROOM = 232448 - 1024 /* alignment */ - 512 /* barriers */ - STAGING_BYTES;
   static constexpr int STAGES = ROOM / STAGE_BYTES < 6 ? ROOM / STAGE_BYTES : 6;
   static constexpr int TMEM_COLS = 2 * BN;
@@ -49,7 +52,7 @@ struct RowsArgs {
 struct RowsMaps { CUtensorMap a, w, out, other; };     // other: the argument written, or the residual / argument read
 
 template <int BN, int CTAS, int FINISH, bool ACROSS>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(Cfg<BN, CTAS, FINISH>::THREADS, 1)
 grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ RowsArgs p) {
   using C = Cfg<BN, CTAS, FINISH>;
   extern __shared__ uint8_t smem_raw[];
@@ -57,8 +60,8 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
   const uint32_t tiles = smem_u32(smem), staging = tiles + C::STAGES * C::STAGE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + C::STAGES * C::STAGE_BYTES + C::STAGING_BYTES);
   const uint32_t full = smem_u32(bars), empty = full + 8 * C::STAGES, tfull = empty + 8 * C::STAGES, tempty = tfull + 16,
-                 landed = tempty + 16 /* [EPI_WARPS][2] */, drain = landed + 16 * EPI_WARPS;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4 + 2 * EPI_WARPS + 1);
+                 landed = tempty + 16 /* [EPI_WARPS] */, drain = landed + 8 * C::EPI_WARPS;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * C::STAGES + 4 + C::EPI_WARPS + 1);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -73,9 +76,9 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(tfull + 8 * i, 1);
-      mbar_init(tempty + 8 * i, EPI_WARPS * CTAS);
+      mbar_init(tempty + 8 * i, C::EPI_WARPS * CTAS);
     }
-    for (int i = 0; i < 2 * EPI_WARPS; ++i) mbar_init(landed + 8 * i, 1);
+    for (int i = 0; i < C::EPI_WARPS; ++i) mbar_init(landed + 8 * i, 1);
     mbar_init(drain, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     prefetch_map(&m.a);
@@ -165,108 +168,113 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
     // ---------------------------------------------------------------- epilogue
     if (blockIdx.x == 0 && warp == 2) report_bad_groups(p.shape, p.dev_status, lane);
     GroupWalk<TileCount> walk(p.shape, count, lane);
-    const int ew = warp - 2, quarter = warp & 3, half = ew >> 2;       // lanes of tensor memory it may read; its half of the columns
-    constexpr int COLS = BN / 2;
-    const uint32_t stg = staging + ew * (C::BUFFERS * 4096), bar = landed + 16 * ew;
-    int buf = 0, piece = 0;
-    uint32_t aphase = 0, lphase = 0;               // lphase: a bit for each piece
-    bool ok = true, coming = false;                // coming: a copy into the piece that nobody has waited for
-    for (int64_t tile = unit; ok && walk.find(tile, at); tile += units) {
+    const int ew = warp - 2, quarter = warp & 3, column = (ew >> 2) * (64 * C::STEPS);      // lanes of tensor memory it may read; its columns
+    const uint32_t piece = staging + ew * 4096, bar = landed + 8 * ew;
+    int buf = 0;
+    uint32_t aphase = 0, lphase = 0;
+    bool ok = true, coming = false;                                     // coming: a copy into the piece that nobody has waited for
+    for (int64_t tile = unit; walk.find(tile, at); tile += units) {
       const int local = (int)(tile - at.before), mt = local / p.tiles_n;
-      const int row0 = at.begin + mt * (BM * CTAS) + (int)rank * BM + quarter * 32, col0 = (local - mt * p.tiles_n) * BN + half * COLS;
+      const int row0 = at.begin + mt * (BM * CTAS) + (int)rank * BM + quarter * 32, col0 = (local - mt * p.tiles_n) * BN + column;
       const int rows = min(32, at.end - row0);                          // of this warp's 32; none or less: nothing is written
-      const float* bias = p.bias ? p.bias + (int64_t)at.group * p.width : nullptr;
 #pragma unroll 1
-      for (int cb = 0; cb < COLS / 64; ++cb) {
-        const int c0 = col0 + 64 * cb;
-        if (c0 >= p.width || rows <= 0) break;                          // the same for the whole warp
-        const uint32_t mine = stg + (C::BUFFERS == 2 ? piece * 4096u : 0u);
-        if (FINISH == F_RESIDUAL || FINISH == F_SLOPE) {
-          if (lane == 0) {                                              // comes while the accumulator is awaited
-            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            mbar_arrive_expect_tx(bar + 8 * piece, 4096);
-            tma_load_2d(mine, &m.other, c0, row0, bar + 8 * piece);
+      for (int step = 0; step < C::STEPS; ++step) {
+        const int c0 = col0 + 64 * step;
+        const bool some = rows > 0 && c0 < p.width, last = step == C::STEPS - 1;       // the same for the whole warp
+        if (some && (FINISH == F_RESIDUAL || FINISH == F_SLOPE)) {
+          if (lane == 0) {                                                // comes while the accumulator is awaited
+            tma_store_wait_read();
+            mbar_arrive_expect_tx(bar, 4096);
+            tma_load_2d(piece, &m.other, c0, row0, bar);
           }
           coming = true;
           __syncwarp();
         }
-        if (cb == 0) {
-          if (!warp_wait(tfull + 8 * buf, aphase, abort_flag)) { ok = false; break; }
+        if (step == 0 && !warp_wait(tfull + 8 * buf, aphase, abort_flag)) { ok = false; break; }
+        if (some) {
           tc_fence_after();
-        }
-        uint32_t r[64];
-        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + half * COLS + 64 * cb);
-        tmem_ld32(taddr, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
-        tmem_ld32(taddr + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
-        tmem_ld_wait();
-        float2 v[32];
+          // 32 columns at a time: with sixteen warps a thread has 96 registers
+          const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN + column + 64 * step);
+          const float* bias = FINISH != F_SLOPE && p.bias ? p.bias + (int64_t)at.group * p.width + c0 : nullptr;
+          auto sums = [&](float2 (&v)[16], int h) {
+            uint32_t r[32];
+            tmem_ld32(taddr + 32 * h, r);
+            float4 b[8];                                                // under way with the sums
+            if (FINISH != F_SLOPE) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = make_float2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
-        if (FINISH != F_SLOPE && bias) {
-#pragma unroll
-          for (int g = 0; g < 16; ++g) {
-            if (c0 + 4 * g < p.width) {
-              const float4 b = __ldg(reinterpret_cast<const float4*>(bias + c0) + g);
-              v[2 * g] = __fadd2_rn(v[2 * g], make_float2(b.x, b.y));
-              v[2 * g + 1] = __fadd2_rn(v[2 * g + 1], make_float2(b.z, b.w));
+              for (int g = 0; g < 8; ++g)
+                b[g] = bias && c0 + 32 * h + 4 * g < p.width ? __ldg(reinterpret_cast<const float4*>(bias + 32 * h) + g) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
-          }
-        }
-        if (FINISH == F_GELU_PRE) {
-          // the argument goes out first, through a piece of its own
-          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-          __syncwarp();
-          put_rows(v, stg, lane);
-          send_rows(&m.other, p.pre, p.ldp, stg, row0, c0, rows, p.width, lane);
-        }
-        if (FINISH == F_GELU || FINISH == F_GELU_PRE) {
+            tmem_ld_wait();
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = gelu_2(v[e]);
-        }
-        uint32_t to = mine;
-        if (FINISH == F_RESIDUAL || FINISH == F_SLOPE) {
-          if (!warp_wait(bar + 8 * piece, lphase >> piece & 1, abort_flag)) { ok = false; break; }
-          lphase ^= 1u << piece;
-          coming = false;
-#pragma unroll
-          for (int ck = 0; ck < 8; ++ck) {
-            uint32_t w[4];
-            read_chunk(w, mine, lane, ck);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 o = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
-              if (FINISH == F_RESIDUAL) v[4 * ck + e] = __fadd2_rn(v[4 * ck + e], o);
-              else v[4 * ck + e] = __fmul2_rn(v[4 * ck + e], gelu_slope_2(o));
+            for (int g = 0; g < 8; ++g) {
+              v[2 * g] = make_float2(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1]));
+              v[2 * g + 1] = make_float2(__uint_as_float(r[4 * g + 2]), __uint_as_float(r[4 * g + 3]));
+              if (FINISH != F_SLOPE) {
+                v[2 * g] = __fadd2_rn(v[2 * g], make_float2(b[g].x, b[g].y));
+                v[2 * g + 1] = __fadd2_rn(v[2 * g + 1], make_float2(b[g].z, b[g].w));
+              }
             }
+          };
+          if (FINISH == F_GELU_PRE) {                                     // the argument goes out first
+            if (lane == 0) tma_store_wait_read();
+            __syncwarp();
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+              float2 v[16];
+              sums(v, h);
+              put_half(v, piece, lane, h);
+            }
+            send_rows(&m.other, p.pre, p.ldp, piece, row0, c0, rows, p.width, lane);
           }
-          piece ^= 1;
-        } else {
-          to = FINISH == F_GELU_PRE ? stg + 4096u : stg;
-          if (lane == 0) {
-            if (FINISH == F_GELU_PRE) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-            else tma_store_wait_read();                                 // the store before has left the buffer
+          if (FINISH == F_RESIDUAL || FINISH == F_SLOPE) {
+            if (!warp_wait(bar, lphase, abort_flag)) { ok = false; break; }
+            lphase ^= 1;
+            coming = false;
           }
-          __syncwarp();
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            float2 v[16];
+            sums(v, h);
+            if (h == 1 && last) {                                         // all of the accumulator has been read
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) give_back<CTAS>(tempty + 8 * buf);
+            }
+            if (FINISH == F_GELU || FINISH == F_GELU_PRE) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[e] = gelu_2(v[e]);
+            }
+            if (FINISH == F_RESIDUAL || FINISH == F_SLOPE) {
+#pragma unroll
+              for (int ck = 0; ck < 4; ++ck) {
+                uint32_t w[4];
+                read_chunk(w, piece, lane, 4 * h + ck);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float2 o = make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+                  if (FINISH == F_RESIDUAL) v[4 * ck + e] = __fadd2_rn(v[4 * ck + e], o);
+                  else v[4 * ck + e] = __fmul2_rn(v[4 * ck + e], gelu_slope_2(o));
+                }
+              }
+            } else if (h == 0) {
+              if (lane == 0) tma_store_wait_read();                       // the store before has left the piece
+              __syncwarp();
+            }
+            put_half(v, piece, lane, h);
+          }
+          send_rows(&m.out, p.out, p.ldo, piece, row0, c0, rows, p.width, lane);
+        } else if (last && lane == 0) {
+          give_back<CTAS>(tempty + 8 * buf);
         }
-        put_rows(v, to, lane);
-        send_rows(&m.out, p.out, p.ldo, to, row0, c0, rows, p.width, lane);
       }
       if (!ok) break;
-      if (col0 >= p.width || rows <= 0) {                               // nothing was awaited yet
-        if (!warp_wait(tfull + 8 * buf, aphase, abort_flag)) break;
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {                                                  // the accumulator goes back to the warp that issues the products
-        if (CTAS == 2) mbar_arrive_cluster(map_to_cta(tempty + 8 * buf, 0));
-        else mbar_arrive(tempty + 8 * buf);
-      }
       if (++buf == 2) { buf = 0; aphase ^= 1; }
     }
     if (lane == 0) {
       if (coming) {
         volatile int never = 0;
-        mbar_wait_limit(bar + 8 * piece, lphase >> piece & 1, &never, DRAIN_LIMIT_CYCLES);
+        mbar_wait_limit(bar, lphase, &never, DRAIN_LIMIT_CYCLES);
       }
       tma_store_wait_all();
     }
@@ -313,7 +321,7 @@ cudaError_t launch_variant(const RowsLaunch& l, cudaStream_t s) {
   if (cudaError_t e = ensure_dynamic_smem(configured, kernel, C::SMEM_BYTES)) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)l.grid);
-  cfg.blockDim = dim3(THREADS);
+  cfg.blockDim = dim3(C::THREADS);
   cfg.dynamicSmemBytes = C::SMEM_BYTES;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];

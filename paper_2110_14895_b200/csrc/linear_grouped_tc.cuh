@@ -12,8 +12,6 @@ using namespace ptx;
 
 constexpr int BM = 128;                        // rows of an operand tile = lanes of tensor memory
 constexpr int BK = 64;                         // of the summed index per stage: 128 bytes, one swizzle row
-constexpr int EPI_WARPS = 8;
-constexpr int THREADS = (2 + EPI_WARPS) * 32;
 constexpr uint32_t SLAB_BYTES = 64 * 128;      // 64 rows of the summed index by 64 columns
 constexpr long long DRAIN_LIMIT_CYCLES = 1ll << 24;    // teardown after a failed wait: ~10 ms per barrier
 
@@ -57,6 +55,12 @@ __device__ __forceinline__ void commit(uint32_t bar) {
   if (CTAS == 2) umma_commit_pair(bar);
   else umma_commit(bar);
 }
+// an epilogue warp has done with an accumulator: to the warp that issues the products (the even block's of a pair)
+template <int CTAS>
+__device__ __forceinline__ void give_back(uint32_t bar) {
+  if (CTAS == 2) mbar_arrive_cluster(map_to_cta(bar, 0));
+  else mbar_arrive(bar);
+}
 // a bounded wait of a whole warp: all lanes leave with the same answer
 static __device__ __noinline__ bool wait_on(uint32_t bar, int parity, volatile int* abort_flag) { return mbar_wait(bar, (uint32_t)parity, abort_flag); }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
@@ -92,20 +96,20 @@ __device__ __forceinline__ uint32_t chunk_at(uint32_t piece, int row, int chunk)
 __device__ __forceinline__ void read_chunk(uint32_t (&w)[4], uint32_t piece, int row, int chunk) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(chunk_at(piece, row, chunk)) : "memory");
 }
-__device__ __forceinline__ void put_rows(const float2 (&v)[32], uint32_t piece, int lane) {
+__device__ __forceinline__ void put_half(const float2 (&v)[16], uint32_t piece, int lane, int half) {
 #pragma unroll
-  for (int ck = 0; ck < 8; ++ck) {
+  for (int ck = 0; ck < 4; ++ck) {
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       __nv_bfloat162 h = __floats2bfloat162_rn(v[4 * ck + e].x, v[4 * ck + e].y);
       w[e] = *reinterpret_cast<uint32_t*>(&h);
     }
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk_at(piece, lane, ck)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk_at(piece, lane, 4 * half + ck)), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3])
+                 : "memory");
   }
 }
-// Sends the piece: by TMA where all 32 rows are the group's, else row by row.  One bulk group either way, so that waits for
-// "all but the last" mean the same pieces.
+// Sends the piece: by TMA where all 32 rows are the group's, else row by row.
 __device__ __forceinline__ void send_rows(const CUtensorMap* tm, bf16* out, int64_t ld, uint32_t piece, int row0, int c0, int rows, int width,
                                           int lane) {
   if (rows == 32) {
@@ -121,7 +125,6 @@ __device__ __forceinline__ void send_rows(const CUtensorMap* tm, bf16* out, int6
     read_chunk(w, piece, r, ck);
     if (c0 + 8 * ck < width) *reinterpret_cast<uint4*>(out + (int64_t)(row0 + r) * ld + c0 + 8 * ck) = make_uint4(w[0], w[1], w[2], w[3]);
   }
-  if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   __syncwarp();
 }
 
