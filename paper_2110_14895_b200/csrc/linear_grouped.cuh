@@ -78,17 +78,10 @@ struct GroupWalk {
     return true;
   }
 };
-// all units of all groups; one warp
-template <typename Count>
-__device__ __forceinline__ int64_t all_units(const GroupedShape& p, Count count, int lane) {
-  int64_t sum = 0;
-  for (int g = lane; g < p.groups; g += 32) {
-    int begin, end;
-    if (group_rows(p, g, begin, end)) sum += count(end - begin);
-  }
+__device__ __forceinline__ int64_t warp_sum64(int64_t v) {
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  return sum;
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
 __device__ __forceinline__ void report_bad_groups(const GroupedShape& p, int* dev_status, int lane) {
   for (int g = lane; g < p.groups; g += 32) {
@@ -126,11 +119,24 @@ struct Share { int round; int64_t begin, end; int beat; };      // beat: the mea
 // begins: of all blocks in the line (absolute units), and behind the last one its end; what a second kernel needs.
 constexpr int DW_TABLE = DW_BLOCKS_F32 + 1, DW_SCRATCH = 2 * DW_TABLE;           // 64-bit numbers; of shared memory while the shares are found
 
-// All threads of a block, which get the same answer in every block.
-__device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, int blocks, int self, int least, int64_t* scratch, int64_t* table) {
+// All threads of a block, which get the same answer in every block.  cuts: whether tiles may be cut.
+__device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, int blocks, int self, int least, int cuts, int64_t* scratch, int64_t* table) {
   const int lane = threadIdx.x & 31;
-  const int64_t whole = all_units(p, SumCount{tiles, true}, lane), total = all_units(p, SumCount{tiles, false}, lane);
-  const int rounds = (int)(whole / blocks), round = (p.groups == 1 ? rounds : rounds > 0 ? rounds - 1 : 0) * blocks;
+  int64_t total = 0, whole = 0;
+  for (int g = lane; g < p.groups; g += 32) {
+    int begin, end;
+    if (group_rows(p, g, begin, end)) {
+      total += SumCount::of(end - begin);
+      ++whole;
+    }
+  }
+  total = warp_sum64(total) * tiles;
+  whole = warp_sum64(whole) * tiles;
+  if (cuts == 0) {                                               // all tiles go round
+    __syncthreads();
+    return Share{(int)whole, 0, 0, 1};
+  }
+  const int rounds = (int)whole / blocks, round = (p.groups == 1 ? rounds : rounds > 0 ? rounds - 1 : 0) * blocks;
   int64_t *loads = scratch, *begins = scratch + DW_TABLE;
   for (int c = threadIdx.x; c < blocks; c += (int)blockDim.x) loads[c] = 0;
   __syncthreads();
@@ -160,16 +166,15 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
       load[i] = c < blocks ? loads[c] : INT64_MAX;
       if (c < blocks) done += load[i];
     }
-    auto all_lanes = [](int64_t v) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-      return v;
-    };
-    done = all_lanes(done);
+    done = warp_sum64(done);
     const int64_t line = total - done;
-    // the level up to which the line fills the blocks; those above it get nothing
-    int64_t level = (total + blocks - 1) / blocks, shares = 0;
-    for (int k = 0; k < 16; ++k) {
+    // a short line goes to as many blocks as get something to do, the same to each
+    const int64_t left = whole - round, wanted = line / least > left ? line / least : left;
+    const bool few = wanted < blocks;
+    const int used = (int)(wanted < 1 ? 1 : wanted);
+    // else to the level up to which the line fills the blocks; those above it get nothing
+    int64_t level = (total + blocks - 1) / blocks, shares = used;
+    for (int k = 0; !few && k < 16; ++k) {
       int64_t sum = 0, open = 0;
 #pragma unroll
       for (int i = 0; i < N; ++i)
@@ -177,19 +182,15 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
           sum += level - load[i];
           ++open;
         }
-      shares = all_lanes(sum);
-      open = all_lanes(open);
+      shares = warp_sum64(sum);
+      open = warp_sum64(open);
       if (shares <= line + open || k == 15) break;
       level -= (shares - line) / open;
     }
-    // a short line goes to as many blocks as get something to do, the same to each
-    const int64_t left = whole - round, wanted = line / least > left ? line / least : left;
-    const bool few = wanted < blocks;
-    const int used = (int)(wanted < 1 ? 1 : wanted);
-    if (few) shares = used;
     int64_t before = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      if (32 * i >= blocks) break;
       const int c = lane + 32 * i;
       const int64_t mine = few ? (c < used ? 1 : 0) : load[i] < level ? level - load[i] : 0;
       const int64_t upto = warp_scan(mine, lane);

@@ -29,7 +29,7 @@ template <int CTAS> struct DwCfg {
 
 struct DwArgs {
   GroupedShape shape;
-  int in, out, tiles_in, tiles;    // tiles of a group: ceil(out / (128 blocks)) x ceil(in / 256)
+  int in, out, tiles_in, tiles, cuts;  // tiles of a group: ceil(out / (128 blocks)) x ceil(in / 256)
   float* dbias;                    // [groups][out] or nullptr
   float* part_bias;                // [units][2][128 blocks]
   int64_t* table;                  // where the units' shares begin
@@ -96,7 +96,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   grid_dependency_wait();
   grid_launch_dependents();
   const uint32_t tmem = *tmem_slot;
-  const Share share = find_share(p.shape, p.tiles, units, self, DW_LEAST, reinterpret_cast<int64_t*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
+  const Share share = find_share(p.shape, p.tiles, units, self, DW_LEAST, p.cuts, reinterpret_cast<int64_t*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
                                  rank == 0 ? p.table : nullptr);
   PartWalk work(p.shape, p.tiles, lane, share, self, units);
   Part part;
@@ -355,7 +355,7 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
   if (bias && n0 + (int)threadIdx.x < out) dbias[(int64_t)here.group * out + n0 + threadIdx.x] = b;
 }
 
-struct DwTiling { int rows, cols, tiles_in, tiles, blocks; };       // blocks: units of work, pairs where a tile has 256 rows
+struct DwTiling { int rows, cols, tiles_in, tiles, blocks; bool cuts; };       // blocks: units of work, pairs where a tile has 256 rows
 DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   DwTiling t;
   // a pair's tile costs 1.4 of a single block's half (measured at 1024 x 4096): not for layers that would leave it empty
@@ -369,7 +369,9 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   const int64_t units = tiles * ((int64_t)shape.rows / DW_ROWS + shape.groups), whole = tiles * shape.groups;
   const int64_t least = act_bf16 ? DW_LEAST : DW_LEAST_F32, wanted = units / least > whole ? units / least : whole;
   const int64_t most = pair ? DW_BLOCKS / 2 : act_bf16 ? DW_BLOCKS : DW_BLOCKS_F32;
-  t.blocks = (int)(wanted < most ? (wanted < 1 ? 1 : wanted) : most);
+  // few rows: no tile is worth a cut, and neither parts nor a second kernel are needed
+  t.cuts = shape.rows > least * DW_ROWS;
+  t.blocks = (int)((t.cuts ? wanted : whole) < most ? (wanted < 1 ? 1 : t.cuts ? wanted : whole) : most);
   return t;
 }
 
@@ -377,13 +379,13 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
 
 size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int out_features) {
   const DwTiling t = tiling_of(act_bf16, shape, in, out_features);
-  return (size_t)64 * ((2 * DW_TABLE + 63) / 64) + (size_t)t.blocks * 2 * ((size_t)t.rows * t.cols + t.rows);
+  return (size_t)64 * ((2 * DW_TABLE + 63) / 64) + (t.cuts ? (size_t)t.blocks : 0) * 2 * ((size_t)t.rows * t.cols + t.rows);
 }
 
 GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16) {
   const DwTiling t = tiling_of(act_bf16, c.shape, c.in, c.out_features);
   float* part = c.partial + 64 * ((2 * DW_TABLE + 63) / 64);                    // behind the table; for TMA on a multiple of 16 bytes
-  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int64_t*>(c.partial)};
+  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, t.cuts, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int64_t*>(c.partial)};
 }
 
 template <int CTAS>
@@ -410,13 +412,13 @@ static cudaError_t launch_dw(const DwMaps& m, const DwArgs& p, int units, cudaSt
 cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, true);
   DwMaps m;
-  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, c.dbias, plan.part_bias, plan.table, c.dev_status};
+  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.cuts, c.dbias, plan.part_bias, plan.table, c.dev_status};
   // without rows nothing is read, and any map will do
   const int64_t rows = c.shape.rows > 0 ? c.shape.rows : 1;
   const void *dout = c.shape.rows > 0 ? c.dout : c.dw, *x = c.shape.rows > 0 ? c.x : c.dw;
   if (!encode_rows(&m.dout, dout, rows, c.out_features, c.lddout, DW_ROWS) || !encode_rows(&m.x, x, rows, c.in, c.ldx, DW_ROWS) ||
       !encode_weights(&m.dw, c.dw, c.shape.groups, c.out_features, c.in, 32) ||
-      !encode_rows(&m.part, plan.part, (int64_t)plan.blocks * 2 * plan.rows, TN, TN, 32, 4))
+      !encode_rows(&m.part, plan.cuts ? plan.part : c.partial, (int64_t)plan.blocks * 2 * plan.rows, TN, TN, 32, 4))
     return cudaErrorInvalidValue;
   return plan.rows == 256 ? launch_dw<2>(m, p, plan.blocks, s) : launch_dw<1>(m, p, plan.blocks, s);
 }
@@ -437,7 +439,6 @@ static cudaError_t launch_join(const GroupedCall& c, const GroupedDw& plan, cuda
 }
 cudaError_t launch_grouped_join(const GroupedCall& c, bool act_bf16, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, act_bf16);
-  if (plan.blocks < 2) return cudaSuccess;
   if (!act_bf16) return launch_join<float, 128, 128>(c, plan, s);
   return plan.rows == 256 ? launch_join<bf16, 256, TN>(c, plan, s) : launch_join<bf16, 128, TN>(c, plan, s);
 }

@@ -1151,7 +1151,7 @@ int vit_op_linear_grouped_backward_weights(vit_handle* h, int dtype, const vit_g
   c.x = x; c.ldx = ldx; c.dout = dout; c.lddout = lddout; c.dw = dw; c.dbias = dbias; c.partial = static_cast<float*>(ws);
   if (b16) VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_dw_bf16(c, s));
   else VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_dw_f32(c, s));
-  if (grouped_dw_plan(c, b16).blocks > 1) VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_join(c, b16, s));
+  if (grouped_dw_plan(c, b16).cuts && grouped_dw_plan(c, b16).blocks > 1) VIT_LAUNCH(h, VIT_PROF_OP, launch_grouped_join(c, b16, s));
   return VIT_OK;
 }
 
