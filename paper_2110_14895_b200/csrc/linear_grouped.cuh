@@ -25,24 +25,16 @@ __device__ __forceinline__ int warp_scan(int v, int lane) {
   }
   return v;
 }
-__device__ __forceinline__ int64_t warp_scan(int64_t v, int lane) {
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const int64_t lower = __shfl_up_sync(0xffffffffu, v, d);
-    if (lane >= d) v += lower;
-  }
-  return v;
-}
 
 // Which group a unit of work belongs to.  Units are numbered group after group; a warp looks at 32 groups at a time and
-// asks for ever larger numbers.  All lanes call together and get the same answer.
-struct GroupAt { int group, begin, end; int64_t before; };       // its rows, and the units before it
+// asks for ever larger numbers.  All lanes call together and get the same answer.  Units fit 32 bits (checked on the host).
+struct GroupAt { int group, begin, end, before; };               // its rows, and the units before it
 template <typename Count>                                        // Count: (rows of a group) -> its units
 struct GroupWalk {
   const GroupedShape& p;
   Count count;
   int lane, g0, begin, end;
-  int64_t base, upto, chunk;                                      // units before the 32 groups, up to this lane's group, of all 32
+  int base, upto, chunk;                                          // units before the 32 groups, up to this lane's group, of all 32
 
   __device__ __forceinline__ GroupWalk(const GroupedShape& shape, Count c, int lane_) : p(shape), count(c), lane(lane_), g0(0), base(0) { load(); }
   __device__ __forceinline__ void restart() {
@@ -52,7 +44,7 @@ struct GroupWalk {
   }
   __device__ __forceinline__ void load() {
     const int g = g0 + lane;
-    int64_t n = 0;
+    int n = 0;
     begin = end = 0;
     if (g < p.groups) {
       if (group_rows(p, g, begin, end)) n = count(end - begin);
@@ -61,7 +53,7 @@ struct GroupWalk {
     upto = warp_scan(n, lane);
     chunk = __shfl_sync(0xffffffffu, upto, 31);
   }
-  __device__ __forceinline__ bool find(int64_t unit, GroupAt& at) {
+  __device__ __forceinline__ bool find(int unit, GroupAt& at) {
     while (unit - base >= chunk) {
       if (g0 + 32 >= p.groups) return false;
       base += chunk;
@@ -73,16 +65,12 @@ struct GroupWalk {
     at.group = g0 + who;
     at.begin = __shfl_sync(0xffffffffu, begin, who);
     at.end = __shfl_sync(0xffffffffu, end, who);
-    const int64_t before = __shfl_up_sync(0xffffffffu, upto, 1);
+    const int before = __shfl_up_sync(0xffffffffu, upto, 1);
     at.before = base + (who == 0 ? 0 : __shfl_sync(0xffffffffu, before, who));
     return true;
   }
 };
-__device__ __forceinline__ int64_t warp_sum64(int64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
+__device__ __forceinline__ int warp_total(int v) { return __reduce_add_sync(0xffffffffu, v); }
 __device__ __forceinline__ void report_bad_groups(const GroupedShape& p, int* dev_status, int lane) {
   for (int g = lane; g < p.groups; g += 32) {
     int begin, end;
@@ -93,7 +81,7 @@ __device__ __forceinline__ void report_bad_groups(const GroupedShape& p, int* de
 // Tiles of `span` rows by `across` columns' tiles.
 struct TileCount {
   int span, across;
-  __device__ __forceinline__ int64_t operator()(int rows) const { return (int64_t)((rows + span - 1) / span) * across; }
+  __device__ __forceinline__ int operator()(int rows) const { return (rows + span - 1) / span * across; }
 };
 
 // The weights' gradients sum over a group's rows, tile by tile of [out][in], 64 rows to a unit (a group without rows has one
@@ -112,17 +100,17 @@ struct SumCount {
   int tiles;
   bool whole;                                                    // counts tiles, not units
   static __device__ __forceinline__ int of(int rows) { return rows > DW_ROWS ? (rows + DW_ROWS - 1) / DW_ROWS : 1; }
-  __device__ __forceinline__ int64_t operator()(int rows) const { return (int64_t)tiles * (whole ? 1 : of(rows)); }
+  __device__ __forceinline__ int operator()(int rows) const { return tiles * (whole ? 1 : of(rows)); }
 };
 // What a block does: tiles self, self + blocks, ... below `round`, then units [begin, end) of all.
-struct Share { int round; int64_t begin, end; int beat; };      // beat: the mean share
-// begins: of all blocks in the line (absolute units), and behind the last one its end; what a second kernel needs.
-constexpr int DW_TABLE = DW_BLOCKS_F32 + 1, DW_SCRATCH = 2 * DW_TABLE;           // 64-bit numbers; of shared memory while the shares are found
+struct Share { int round, begin, end, beat; };                  // beat: the mean share
+// begins: of all blocks in the line (units of all), and behind the last one its end; what a second kernel needs.
+constexpr int DW_TABLE = DW_BLOCKS_F32 + 1, DW_SCRATCH = 2 * DW_TABLE;        // numbers; of shared memory while the shares are found
 
 // All threads of a block, which get the same answer in every block.  cuts: whether tiles may be cut.
-__device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, int blocks, int self, int least, int cuts, int64_t* scratch, int64_t* table) {
+__device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, int blocks, int self, int least, int cuts, int* scratch, int* table) {
   const int lane = threadIdx.x & 31;
-  int64_t total = 0, whole = 0;
+  int total = 0, whole = 0;
   for (int g = lane; g < p.groups; g += 32) {
     int begin, end;
     if (group_rows(p, g, begin, end)) {
@@ -130,84 +118,88 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
       ++whole;
     }
   }
-  total = warp_sum64(total) * tiles;
-  whole = warp_sum64(whole) * tiles;
-  if (cuts == 0) {                                               // all tiles go round
-    __syncthreads();
-    return Share{(int)whole, 0, 0, 1};
+  total = warp_total(total) * tiles;
+  whole = warp_total(whole) * tiles;
+  if (cuts == 0) return Share{whole, 0, 0, 1};                   // all tiles go round
+  const int rounds = whole / blocks, round = (p.groups == 1 ? rounds : rounds > 0 ? rounds - 1 : 0) * blocks;
+  if (round == 0) {
+    // the same to each, but to no more blocks than get something to do
+    const int wanted = max(total / least, whole), used = min(max(wanted, 1), blocks);
+    const double each = (double)total / used;
+    auto begin = [&](int c) { return c >= used ? total : (int)(each * c); };
+    if (table && self == 0)
+      for (int c = threadIdx.x; c <= blocks; c += (int)blockDim.x) table[c] = begin(c);
+    return Share{0, begin(self), begin(self + 1), max((int)each, 1)};
   }
-  const int rounds = (int)whole / blocks, round = (p.groups == 1 ? rounds : rounds > 0 ? rounds - 1 : 0) * blocks;
-  int64_t *loads = scratch, *begins = scratch + DW_TABLE;
+  int *loads = scratch, *begins = scratch + DW_TABLE;
   for (int c = threadIdx.x; c < blocks; c += (int)blockDim.x) loads[c] = 0;
   __syncthreads();
-  if (round > 0) {
+  {
     // units that go round to block c: of a group's tiles [t0, t1) those that are c modulo the blocks
     const int slices = max((int)blockDim.x / blocks, 1), slice = (int)threadIdx.x / blocks;
     for (int c = (int)threadIdx.x % blocks; c < blocks && slice < slices; c += slices > 1 ? blocks : (int)blockDim.x) {
       const int per = (p.groups + slices - 1) / slices;
-      int64_t sum = 0;
+      int sum = 0;
       for (int g = 0, t0 = 0; g < min(p.groups, (slice + 1) * per) && t0 < round; ++g) {
         int begin, end;
         if (!group_rows(p, g, begin, end)) continue;
         const int t1 = min(t0 + tiles, round);
-        if (g >= slice * per) sum += (int64_t)((t1 - 1 - c + blocks) / blocks - (t0 - 1 - c + blocks) / blocks) * SumCount::of(end - begin);
+        if (g >= slice * per) sum += ((t1 - 1 - c + blocks) / blocks - (t0 - 1 - c + blocks) / blocks) * SumCount::of(end - begin);
         t0 = t1;
       }
-      atomicAdd(reinterpret_cast<unsigned long long*>(&loads[c]), (unsigned long long)sum);        // whole numbers: any order
+      atomicAdd(&loads[c], sum);                                 // whole numbers: any order
     }
     __syncthreads();
   }
   if (threadIdx.x < 32) {
     constexpr int N = (DW_BLOCKS_F32 + 31) / 32;
-    int64_t load[N], done = 0;
+    int load[N], done = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = lane + 32 * i;
-      load[i] = c < blocks ? loads[c] : INT64_MAX;
+      load[i] = c < blocks ? loads[c] : INT32_MAX;
       if (c < blocks) done += load[i];
     }
-    done = warp_sum64(done);
-    const int64_t line = total - done;
-    // a short line goes to as many blocks as get something to do, the same to each
-    const int64_t left = whole - round, wanted = line / least > left ? line / least : left;
+    done = warp_total(done);
+    const int line = total - done, left = whole - round, wanted = max(line / least, left);
+    // a short line goes to as many blocks as get something to do, the same to each; else the line fills the blocks up to a
+    // level, and those above it get nothing
     const bool few = wanted < blocks;
-    const int used = (int)(wanted < 1 ? 1 : wanted);
-    // else to the level up to which the line fills the blocks; those above it get nothing
-    int64_t level = (total + blocks - 1) / blocks, shares = used;
+    const int used = few ? max(wanted, 1) : blocks;
+    int level = (int)(((int64_t)total + blocks - 1) / blocks), shares = used;
     for (int k = 0; !few && k < 16; ++k) {
-      int64_t sum = 0, open = 0;
+      int sum = 0, open = 0;
 #pragma unroll
       for (int i = 0; i < N; ++i)
         if (load[i] < level) {
           sum += level - load[i];
           ++open;
         }
-      shares = warp_sum64(sum);
-      open = warp_sum64(open);
+      shares = warp_total(sum);
+      open = warp_total(open);
       if (shares <= line + open || k == 15) break;
       level -= (shares - line) / open;
     }
-    int64_t before = 0;
+    const double each = shares > 0 ? (double)line / shares : 0.0;
+    int before = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       if (32 * i >= blocks) break;
-      const int c = lane + 32 * i;
-      const int64_t mine = few ? (c < used ? 1 : 0) : load[i] < level ? level - load[i] : 0;
-      const int64_t upto = warp_scan(mine, lane);
-      if (c < blocks) begins[c] = done + (shares > 0 ? line * (before + upto - mine) / shares : 0);
+      const int c = lane + 32 * i, mine = few ? (c < used ? 1 : 0) : load[i] < level ? level - load[i] : 0;
+      const int upto = warp_scan(mine, lane);
+      if (c < blocks) begins[c] = done + (int)(each * (before + upto - mine));
       before += __shfl_sync(0xffffffffu, upto, 31);
     }
     if (lane == 0) {
       begins[blocks] = total;
-      loads[0] = (line + (few ? used : blocks) - 1) / (few ? used : blocks);
+      loads[0] = max(line / used, 1);
     }
   }
   __syncthreads();
-  const Share share{round, begins[self], begins[self + 1], (int)loads[0]};
+  const Share share{round, begins[self], begins[self + 1], loads[0]};
   if (table && self == 0)
     for (int c = threadIdx.x; c <= blocks; c += (int)blockDim.x) table[c] = begins[c];
-  __syncthreads();                                               // the scratch is free again
-  return share;
+  return share;                                                  // (the scratch is in use until the block has met again)
 }
 
 // A block's work on one tile: units [from, to) of `all`.  slot: where a part's sums are kept, the share's first or last.
@@ -222,15 +214,14 @@ struct Part {
 struct PartWalk {
   GroupWalk<SumCount> walk;
   Share share;
-  int64_t at;
-  int blocks;
+  int at, blocks;
   __device__ __forceinline__ PartWalk(const GroupedShape& p, int tiles, int lane, const Share& s, int self, int blocks_)
       : walk(p, SumCount{tiles, s.round > 0}, lane), share(s), at(s.round > 0 ? self : s.begin), blocks(blocks_) {}
   __device__ __forceinline__ bool next(Part& part) {
     GroupAt g;
     if (walk.count.whole) {
       if (at < share.round && walk.find(at, g)) {
-        part = Part{g.group, g.begin, g.end, (int)(at - g.before), 0, 0, SumCount::of(g.end - g.begin), 0};
+        part = Part{g.group, g.begin, g.end, at - g.before, 0, 0, SumCount::of(g.end - g.begin), 0};
         part.to = part.all;
         at += blocks;
         return true;
@@ -241,12 +232,11 @@ struct PartWalk {
     }
     if (at >= share.end || !walk.find(at, g)) return false;
     const int all = SumCount::of(g.end - g.begin);
-    const int64_t local = at - g.before, tile = local / all;
-    part = Part{g.group, g.begin, g.end, (int)tile, (int)(local - tile * all), 0, all, 0};
-    const int64_t left = share.end - at;
-    part.to = left < all - part.from ? part.from + (int)left : all;
+    const int local = at - g.before, tile = local / all;
+    part = Part{g.group, g.begin, g.end, tile, local - tile * all, 0, all, 0};
+    part.to = min(all, part.from + share.end - at);
     // the first unit in it that is the time of the share, modulo the beat
-    const int time = (int)((at - share.begin) % share.beat), late = (part.from - time) % share.beat;
+    const int late = (part.from - (at - share.begin)) % share.beat;
     part.first = part.from + (late > 0 ? share.beat - late : -late);
     if (part.first >= part.to) part.first = part.from;
     at += part.to - part.from;

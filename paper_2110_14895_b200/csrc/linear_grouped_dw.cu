@@ -21,7 +21,7 @@ using namespace grouped;
 
 namespace {
 
-constexpr int TN = 256, EPI_WARPS = 8, SUM_WARPS = 2, DW_THREADS = 32 * (2 + EPI_WARPS + SUM_WARPS + 1);
+constexpr int TN = 256, EPI_WARPS = 8, SUM_WARPS = 4, DW_THREADS = 32 * (2 + EPI_WARPS + SUM_WARPS + 1);
 template <int CTAS> struct DwCfg {
   static constexpr int B_SLABS = 4 / CTAS, A_BYTES = 2 * SLAB_BYTES, STAGE_BYTES = A_BYTES + B_SLABS * SLAB_BYTES, STAGES = CTAS == 2 ? 6 : 4;
   static constexpr int STAGING_BYTES = EPI_WARPS * 4096, SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 256;
@@ -32,10 +32,11 @@ struct DwArgs {
   int in, out, tiles_in, tiles, cuts;  // tiles of a group: ceil(out / (128 blocks)) x ceil(in / 256)
   float* dbias;                    // [groups][out] or nullptr
   float* part_bias;                // [units][2][128 blocks]
-  int64_t* table;                  // where the units' shares begin
+  float* part;                     // [units][2][epilogue warps of the blocks][4][8][32][4]: parts of tiles, as the warps hold them
+  int* table;                      // where the units' shares begin
   int* dev_status;
 };
-struct DwMaps { CUtensorMap dout, x, dw, part; };
+struct DwMaps { CUtensorMap dout, x, dw; };
 
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(tm)), "r"(src),
@@ -96,8 +97,9 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   grid_dependency_wait();
   grid_launch_dependents();
   const uint32_t tmem = *tmem_slot;
-  const Share share = find_share(p.shape, p.tiles, units, self, DW_LEAST, p.cuts, reinterpret_cast<int64_t*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
+  const Share share = find_share(p.shape, p.tiles, units, self, DW_LEAST, p.cuts, reinterpret_cast<int*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
                                  rank == 0 ? p.table : nullptr);
+  __syncthreads();
   PartWalk work(p.shape, p.tiles, lane, share, self, units);
   Part part;
   int stage = 0;
@@ -216,23 +218,16 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
           if (lane == 0) tma_store_3d(&m.dw, stg, k0 + 64 * cb, n0, part.group);      // rows and columns beyond are clipped
         }
       } else {
-        const int row = ((self * 2 + part.slot()) * CTAS + (int)rank) * BM + quarter * 32;
+        // 4 columns of 32 rows side by side; columns and rows that do not exist, too: they are not looked at
+        float* to = p.part + (((int64_t)(self * 2 + part.slot()) * CTAS + rank) * EPI_WARPS + ew) * (32 * 128) + lane * 4;
 #pragma unroll 1
-        for (int cb = 0; cb < 4; ++cb) {
-          if (k0 + 32 * cb >= p.in || n0 >= p.out) break;               // nobody will look there
+        for (int q = 0; q < 4; ++q) {
           uint32_t r[32];
-          tmem_ld32(taddr + 32 * cb, r);
+          tmem_ld32(taddr + 32 * q, r);
           tmem_ld_wait();
-          if (lane == 0) tma_store_wait_read();
-          __syncwarp();
 #pragma unroll
-          for (int ck = 0; ck < 8; ++ck)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(chunk_at(stg, lane, ck)), "r"(r[4 * ck]), "r"(r[4 * ck + 1]),
-                         "r"(r[4 * ck + 2]), "r"(r[4 * ck + 3])
-                         : "memory");
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) tma_store_2d(&m.part, stg, half * 128 + 32 * cb, row);
+          for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<uint4*>(to + (q * 8 + e) * 128) = make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);
         }
       }
       tc_fence_before();
@@ -243,8 +238,8 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     if (lane == 0) tma_store_wait_all();
   } else if (warp < 2 + EPI_WARPS + SUM_WARPS && p.dbias) {
     // ---------------------------------------------------------------- sums of dout's columns
-    // a warp has a slab's 64 columns; a lane 8 of them and every fourth row
-    const int slab = warp - 2 - EPI_WARPS, ck = lane & 7, first = lane >> 3;
+    // a warp has 32 columns; a lane 8 of them and every eighth row, such that eight lanes meet all banks
+    const int sw = warp - 2 - EPI_WARPS, slab = sw >> 1, ck = (sw & 1) * 4 + (lane & 3), first = (lane >> 3) | (lane & 4);
     bool ok = true;
     while (ok && work.next(part)) {
       const bool mine = part.tile % p.tiles_in == 0;
@@ -253,15 +248,18 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         if (!warp_wait(full + 8 * stage, phase, abort_flag)) { ok = false; break; }
         if (mine) {
           const uint32_t from = tiles + stage * C::STAGE_BYTES + slab * SLAB_BYTES;
-          const int rows = min(DW_ROWS, part.end - part.begin - part.unit(kb) * DW_ROWS);
-          float2 some[4] = {};
-#pragma unroll 4
-          for (int r = first; r < rows; r += 4) {
-            uint32_t w[4];
-            read_chunk(w, from, r, ck);
+          const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS;
+          uint32_t w[8][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) some[e] = __fadd2_rn(some[e], make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)));
-          }
+          for (int i = 0; i < 8; ++i) read_chunk(w[i], from, first + 8 * i, ck);
+          float2 some[4] = {};
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (first + 8 * i < rows) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                some[e] = __fadd2_rn(some[e], make_float2(__uint_as_float(w[i][e] << 16), __uint_as_float(w[i][e] & 0xffff0000u)));
+            }
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[e] = __fadd2_rn(sum[e], some[e]);
         }
@@ -273,12 +271,12 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int o = 8; o < 32; o <<= 1) {
+        for (int o = 4; o < 32; o <<= 1) {
           sum[e].x += __shfl_xor_sync(0xffffffffu, sum[e].x, o);
           sum[e].y += __shfl_xor_sync(0xffffffffu, sum[e].y, o);
         }
       const int c = slab * 64 + ck * 8, n0 = part.tile / p.tiles_in * (BM * CTAS) + (int)rank * BM;
-      if (first == 0 && n0 + c < p.out) {
+      if (lane < 4 && n0 + c < p.out) {
         float4* to = reinterpret_cast<float4*>(part.whole() ? p.dbias + (int64_t)part.group * p.out + n0 + c
                                                             : p.part_bias + (((int64_t)self * 2 + part.slot()) * CTAS + rank) * BM + c);
         to[0] = make_float4(sum[0].x, sum[0].y, sum[1].x, sum[1].y);
@@ -303,7 +301,8 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
 }
 
 // Tiles that were cut between blocks: their parts are added in the order of their rows.  A block of this kernel looks at the
-// begin of one stretch; it is its task if the tile there began in the stretch before.  Sixteen rows to a block.
+// begin of one share; it is its task if the tile there began in the share before.  Several blocks share a tile: a warp's 32 x 128
+// of the tensor-core kernel, 16 rows of the fp32 one.
 template <typename T> __device__ __forceinline__ void store4(T* to, float4 v);
 template <> __device__ __forceinline__ void store4(float* to, float4 v) { *reinterpret_cast<float4*>(to) = v; }
 template <> __device__ __forceinline__ void store4(bf16* to, float4 v) {
@@ -313,46 +312,64 @@ template <> __device__ __forceinline__ void store4(bf16* to, float4 v) {
   o.y = *reinterpret_cast<uint32_t*>(&hi);
   *reinterpret_cast<uint2*>(to) = o;
 }
+constexpr int JOIN_THREADS = 256;
 template <typename T, int ROWS, int COLS>
-__global__ void __launch_bounds__(256)
-grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int tiles, int blocks, const int64_t* __restrict__ table,
+__global__ void __launch_bounds__(JOIN_THREADS)
+grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int tiles, int blocks, const int* __restrict__ table,
                     const float* __restrict__ part, const float* __restrict__ part_bias, T* __restrict__ dw, float* __restrict__ dbias) {
+  constexpr bool WARPS = sizeof(T) == 2;                          // parts lie as the epilogue warps of the tensor-core kernel hold them
+  constexpr int N = (WARPS ? 32 * 128 : 16 * COLS) / 4 / JOIN_THREADS;
   const int lane = threadIdx.x & 31, block = (int)blockIdx.x + 1;
   grid_dependency_wait();
-  const int64_t begin = table[block], end = table[block + 1];
+  grid_launch_dependents();
+  const int begin = table[block], end = table[block + 1];
   if (begin >= end || begin == table[0]) return;
   PartWalk work(shape, tiles, lane, Share{0, begin, begin + 1, 1}, 0, 1);
   Part here;
   if (!work.next(here) || here.from == 0) return;                                // a tile begins here: nothing is cut
-  const int64_t tile_begin = begin - here.from, tile_end = tile_begin + here.all;
+  const int tile_begin = begin - here.from, tile_end = tile_begin + here.all;
   int before = block - 1;
   while (table[before] == begin) --before;                                       // blocks without a share
   if (table[before] > tile_begin) return;                                        // cut before, too: not this block's task
-  const int n0 = here.tile / tiles_in * ROWS, k0 = here.tile % tiles_in * COLS, r0 = (int)blockIdx.y * 16;
-  constexpr int N = 16 * COLS / 1024;
+  const int n0 = here.tile / tiles_in * ROWS, k0 = here.tile % tiles_in * COLS, piece = (int)blockIdx.y;
+  const float* mine = part + (WARPS ? piece * (32 * 128) : piece * 16 * COLS) + 4 * threadIdx.x;
   float4 sum[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-    sum[i] = *reinterpret_cast<const float4*>(part + ((int64_t)before * 2 + 1) * ROWS * COLS + r0 * COLS + (i * 256 + (int)threadIdx.x) * 4);
-  const bool bias = dbias && k0 == 0 && blockIdx.y == 0 && threadIdx.x < ROWS;
+  for (int i = 0; i < N; ++i) sum[i] = *reinterpret_cast<const float4*>(mine + ((int64_t)before * 2 + 1) * ROWS * COLS + 4 * JOIN_THREADS * i);
+  const bool bias = dbias && k0 == 0 && piece == 0 && threadIdx.x < ROWS;
   float b = bias ? part_bias[((int64_t)before * 2 + 1) * ROWS + threadIdx.x] : 0.f;
 #pragma unroll 4
   for (int who = block; who < blocks && table[who] < tile_end; ++who) {          // (some have no share: they are added as zeros)
     const bool some = table[who + 1] > table[who];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float4 v = some ? *reinterpret_cast<const float4*>(part + (int64_t)who * 2 * ROWS * COLS + r0 * COLS + (i * 256 + (int)threadIdx.x) * 4)
-                            : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 v = some ? *reinterpret_cast<const float4*>(mine + (int64_t)who * 2 * ROWS * COLS + 4 * JOIN_THREADS * i) : make_float4(0.f, 0.f, 0.f, 0.f);
       sum[i] = make_float4(sum[i].x + v.x, sum[i].y + v.y, sum[i].z + v.z, sum[i].w + v.w);
     }
     if (bias && some) b += part_bias[(int64_t)who * 2 * ROWS + threadIdx.x];
   }
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int at = (i * 256 + (int)threadIdx.x) * 4, n = n0 + r0 + at / COLS, k = k0 + at % COLS;
-    if (n < out && k < in) store4(dw + ((int64_t)here.group * out + n) * in + k, sum[i]);
-  }
   if (bias && n0 + (int)threadIdx.x < out) dbias[(int64_t)here.group * out + n0 + threadIdx.x] = b;
+  if (WARPS) {
+    // rows belong to lanes there; here they are written side by side
+    __shared__ float turned[32][128 + 4];
+    // warp 2 + w of a block has the rows of its quarter of tensor memory
+    const int block_of_pair = piece / EPI_WARPS, w = piece % EPI_WARPS;
+    const int row0 = block_of_pair * BM + ((w + 2) & 3) * 32, col0 = (w >> 2) * 128;
+#pragma unroll
+    for (int i = 0; i < N; ++i) *reinterpret_cast<float4*>(&turned[lane][4 * ((JOIN_THREADS / 32) * i + (threadIdx.x >> 5))]) = sum[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = i * JOIN_THREADS + (int)threadIdx.x, r = at / 32, c = at % 32 * 4, n = n0 + row0 + r, k = k0 + col0 + c;
+      if (n < out && k < in) store4(dw + ((int64_t)here.group * out + n) * in + k, *reinterpret_cast<const float4*>(&turned[r][c]));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int at = (i * JOIN_THREADS + (int)threadIdx.x) * 4, n = n0 + piece * 16 + at / COLS, k = k0 + at % COLS;
+      if (n < out && k < in) store4(dw + ((int64_t)here.group * out + n) * in + k, sum[i]);
+    }
+  }
 }
 
 struct DwTiling { int rows, cols, tiles_in, tiles, blocks; bool cuts; };       // blocks: units of work, pairs where a tile has 256 rows
@@ -379,13 +396,13 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
 
 size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int out_features) {
   const DwTiling t = tiling_of(act_bf16, shape, in, out_features);
-  return (size_t)64 * ((2 * DW_TABLE + 63) / 64) + (t.cuts ? (size_t)t.blocks : 0) * 2 * ((size_t)t.rows * t.cols + t.rows);
+  return (size_t)64 * ((DW_TABLE + 63) / 64) + (t.cuts ? (size_t)t.blocks : 0) * 2 * ((size_t)t.rows * t.cols + t.rows);
 }
 
 GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16) {
   const DwTiling t = tiling_of(act_bf16, c.shape, c.in, c.out_features);
-  float* part = c.partial + 64 * ((2 * DW_TABLE + 63) / 64);                    // behind the table; for TMA on a multiple of 16 bytes
-  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, t.cuts, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int64_t*>(c.partial)};
+  float* part = c.partial + 64 * ((DW_TABLE + 63) / 64);                        // behind the table
+  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, t.cuts, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int*>(c.partial)};
 }
 
 template <int CTAS>
@@ -412,13 +429,12 @@ static cudaError_t launch_dw(const DwMaps& m, const DwArgs& p, int units, cudaSt
 cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, true);
   DwMaps m;
-  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.cuts, c.dbias, plan.part_bias, plan.table, c.dev_status};
+  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.cuts, c.dbias, plan.part_bias, plan.part, plan.table, c.dev_status};
   // without rows nothing is read, and any map will do
   const int64_t rows = c.shape.rows > 0 ? c.shape.rows : 1;
   const void *dout = c.shape.rows > 0 ? c.dout : c.dw, *x = c.shape.rows > 0 ? c.x : c.dw;
   if (!encode_rows(&m.dout, dout, rows, c.out_features, c.lddout, DW_ROWS) || !encode_rows(&m.x, x, rows, c.in, c.ldx, DW_ROWS) ||
-      !encode_weights(&m.dw, c.dw, c.shape.groups, c.out_features, c.in, 32) ||
-      !encode_rows(&m.part, plan.cuts ? plan.part : c.partial, (int64_t)plan.blocks * 2 * plan.rows, TN, TN, 32, 4))
+      !encode_weights(&m.dw, c.dw, c.shape.groups, c.out_features, c.in, 32))
     return cudaErrorInvalidValue;
   return plan.rows == 256 ? launch_dw<2>(m, p, plan.blocks, s) : launch_dw<1>(m, p, plan.blocks, s);
 }
@@ -426,8 +442,8 @@ cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s) {
 template <typename T, int ROWS, int COLS>
 static cudaError_t launch_join(const GroupedCall& c, const GroupedDw& plan, cudaStream_t s) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(plan.blocks - 1), ROWS / 16);
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3((unsigned)(plan.blocks - 1), sizeof(T) == 2 ? ROWS * COLS / (32 * 128) : ROWS / 16);
+  cfg.blockDim = dim3(JOIN_THREADS);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -435,7 +451,7 @@ static cudaError_t launch_join(const GroupedCall& c, const GroupedDw& plan, cuda
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, grouped_join_kernel<T, ROWS, COLS>, c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.blocks,
-                            (const int64_t*)plan.table, (const float*)plan.part, (const float*)plan.part_bias, static_cast<T*>(c.dw), c.dbias);
+                            (const int*)plan.table, (const float*)plan.part, (const float*)plan.part_bias, static_cast<T*>(c.dw), c.dbias);
 }
 cudaError_t launch_grouped_join(const GroupedCall& c, bool act_bf16, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, act_bf16);

@@ -124,8 +124,8 @@ grouped_rows_f32_kernel(const RowsArgs p) {
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
   GroupWalk<TileCount> walk(p.shape, TileCount{T, p.tiles_n}, lane);
   GroupAt at;
-  for (int64_t tile = self; walk.find(tile, at); tile += units) {
-    const int local = (int)(tile - at.before), row0 = at.begin + local / p.tiles_n * T, col0 = local % p.tiles_n * T;
+  for (int tile = self; walk.find(tile, at); tile += units) {
+    const int local = tile - at.before, row0 = at.begin + local / p.tiles_n * T, col0 = local % p.tiles_n * T;
     const int rows = min(T, at.end - row0), cols = min(T, p.width - col0);
     const float* x = p.x + (int64_t)row0 * p.ldx;
     // weights [out][in]: forwards a column of the result is a row of them, backwards a column
@@ -193,7 +193,7 @@ struct DwArgs {
   const float *x, *dout;
   int64_t ldx, lddout;
   float *dw, *dbias, *part, *part_bias;
-  int64_t* table;
+  int* table;
   int* dev_status;
 };
 
@@ -205,7 +205,8 @@ grouped_dw_f32_kernel(const DwArgs p) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
-  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, DW_LEAST_F32, p.cuts, reinterpret_cast<int64_t*>(&a[0][0][0]), p.table);
+  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, DW_LEAST_F32, p.cuts, reinterpret_cast<int*>(&a[0][0][0]), p.table);
+  __syncthreads();
   PartWalk work(p.shape, p.tiles, lane, share, (int)blockIdx.x, (int)gridDim.x);
   Part part;
   while (work.next(part)) {

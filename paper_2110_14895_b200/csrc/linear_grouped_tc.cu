@@ -107,8 +107,8 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
     uint32_t phase = 0;
     long long fills = 0;                           // stages filled so far (this block's share)
     bool ok = true;
-    for (int64_t tile = unit; ok && walk.find(tile, at); tile += units) {
-      const int local = (int)(tile - at.before), mt = local / p.tiles_n;
+    for (int tile = unit; ok && walk.find(tile, at); tile += units) {
+      const int local = tile - at.before, mt = local / p.tiles_n;
       const int row = at.begin + mt * (BM * CTAS) + (int)rank * BM, col = (local - mt * p.tiles_n) * BN + (int)rank * C::B_ROWS;
       for (int kb = 0; kb < blocks_k; ++kb) {
         if (!warp_wait(empty + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
@@ -139,7 +139,7 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
       int stage = 0, buf = 0;
       uint32_t phase = 0, aphase = 0;
       bool ok = true;
-      for (int64_t tile = unit; ok && walk.find(tile, at); tile += units) {
+      for (int tile = unit; ok && walk.find(tile, at); tile += units) {
         if (!warp_wait(tempty + 8 * buf, aphase ^ 1, abort_flag)) break;
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(buf * BN);
@@ -173,8 +173,8 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
     int buf = 0;
     uint32_t aphase = 0, lphase = 0;
     bool ok = true, coming = false;                                     // coming: a copy into the piece that nobody has waited for
-    for (int64_t tile = unit; walk.find(tile, at); tile += units) {
-      const int local = (int)(tile - at.before), mt = local / p.tiles_n;
+    for (int tile = unit; walk.find(tile, at); tile += units) {
+      const int local = tile - at.before, mt = local / p.tiles_n;
       const int row0 = at.begin + mt * (BM * CTAS) + (int)rank * BM + quarter * 32, col0 = (local - mt * p.tiles_n) * BN + column;
       const int rows = min(32, at.end - row0);                          // of this warp's 32; none or less: nothing is written
 #pragma unroll 1
@@ -350,12 +350,12 @@ cudaError_t launch_finish(const GroupedCall& c, int finish, const RowsLaunch& l,
 
 namespace grouped {
 
-bool encode_rows(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int es) {
+bool encode_rows(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
   const EncodeTiledFn fn = encoder();
   if (!fn || !base) return false;
-  const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * es};
-  const cuuint32_t box[2] = {(cuuint32_t)(128 / es), (cuuint32_t)box_rows}, one[2] = {1, 1};
-  return fn(tm, es == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(base), dim, stride, box, one,
+  const cuuint64_t dim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, stride[1] = {(cuuint64_t)ld * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, one[2] = {1, 1};
+  return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dim, stride, box, one,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }

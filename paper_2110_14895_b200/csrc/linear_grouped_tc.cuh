@@ -128,8 +128,8 @@ __device__ __forceinline__ void send_rows(const CUtensorMap* tm, bf16* out, int6
   __syncwarp();
 }
 
-// ---- host: maps of bf16 (or, es == 4, fp32) matrices in 128-byte-swizzled boxes of 128 bytes by `box_rows` rows
-bool encode_rows(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows, int es = 2);
+// ---- host: maps of matrices in 128-byte-swizzled boxes of 64 columns by `box_rows` rows
+bool encode_rows(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
 // the weights of all groups, [groups][rows][cols]
 bool encode_weights(CUtensorMap* tm, const void* base, int groups, int rows, int cols, int box_rows);
 

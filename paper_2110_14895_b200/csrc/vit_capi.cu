@@ -316,15 +316,15 @@ bool grouped_ok(int dtype, const vit_grouped_problem* p) {
          p->out_features >= 8 && p->out_features % 8 == 0 && (p->offsets || p->groups == 1) &&
          !(reinterpret_cast<uintptr_t>(p->offsets) & 3);
 }
-// The kernels count tiles and rows in 32 bits; weights of all groups are read through one map, whose strides are of 40 bits.
+// The kernels count tiles and units of 64 rows in 32 bits, also where wrong offsets make every group as long as the buffer;
+// the weights of all groups are read through one map, whose strides are of 40 bits.
 bool grouped_fits(const vit_grouped_problem* p) {
   if (p->rows > MAX_PACKED_ROWS) return false;
   const int64_t widest = p->in_features > p->out_features ? p->in_features : p->out_features;
-  const int64_t tiles = ((int64_t)p->rows / 64 + p->groups) * ((widest + 63) / 64);
-  const int64_t weights = (int64_t)p->in_features * p->out_features;
+  const int64_t weights = (int64_t)p->in_features * p->out_features, units = p->groups * ((int64_t)p->rows / 64 + 1);
   const int64_t sums = ((int64_t)p->in_features / 128 + 1) * ((int64_t)p->out_features / 128 + 1);      // tiles of a group's weights
-  const int64_t units = (int64_t)p->rows / 64 + p->groups;
-  return tiles <= INT32_MAX / 2 && weights <= (int64_t)1 << 36 && p->groups <= INT64_MAX / 16 / weights && sums <= INT32_MAX / 2 / units;
+  return weights <= (int64_t)1 << 36 && p->groups <= INT64_MAX / 16 / weights && units <= INT32_MAX / 2 / ((widest + 63) / 64) &&
+         units <= INT32_MAX / 2 / sums;
 }
 // whether an output lies over the offsets or any other operand
 bool over_offsets(const vit_grouped_problem* p, const Block& out) {
