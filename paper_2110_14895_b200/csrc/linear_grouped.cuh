@@ -139,13 +139,20 @@ __device__ __forceinline__ Share find_share(const GroupedShape& p, int tiles, in
     const int slices = max((int)blockDim.x / blocks, 1), slice = (int)threadIdx.x / blocks;
     for (int c = (int)threadIdx.x % blocks; c < blocks && slice < slices; c += slices > 1 ? blocks : (int)blockDim.x) {
       const int per = (p.groups + slices - 1) / slices;
-      int sum = 0;
+      // every group has `tiles` of them: q or q + 1 are c modulo the blocks, by where its first one lies
+      const int q = tiles / blocks, r = tiles % blocks;
+      int sum = 0, at = 0;                                       // at: t0 modulo the blocks
       for (int g = 0, t0 = 0; g < min(p.groups, (slice + 1) * per) && t0 < round; ++g) {
         int begin, end;
         if (!group_rows(p, g, begin, end)) continue;
-        const int t1 = min(t0 + tiles, round);
-        if (g >= slice * per) sum += ((t1 - 1 - c + blocks) / blocks - (t0 - 1 - c + blocks) / blocks) * SumCount::of(end - begin);
-        t0 = t1;
+        if (g >= slice * per) {
+          const int from = c >= at ? c - at : c - at + blocks;   // of the first of them behind t0
+          const int n = t0 + tiles <= round ? q + (from < r ? 1 : 0) : (round - t0 - from + blocks - 1) / blocks;
+          sum += n * SumCount::of(end - begin);
+        }
+        t0 += tiles;
+        at += r;
+        if (at >= blocks) at -= blocks;
       }
       atomicAdd(&loads[c], sum);                                 // whole numbers: any order
     }
