@@ -343,12 +343,13 @@ GroupedCall grouped_call(const vit_handle* h, const vit_grouped_problem* p) {
 }
 
 // Whether a list of tensors may be scaled: nothing that is written lies over anything else, but for a tensor in place.
-struct Span { uintptr_t begin, end; bool write; };
+struct Span { uintptr_t begin, end; };
 int clip_list_status(const vit_tensor* t, int n, const void* norm, const void* ws, size_t ws_bytes) {
-  std::vector<Span> spans;
-  spans.reserve(2 * (size_t)n + 2);
-  auto add = [&](const void* p, size_t bytes, bool write) {
-    if (p && bytes) spans.push_back(Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes, write});
+  std::vector<Span> reads, writes;
+  reads.reserve((size_t)n);
+  writes.reserve((size_t)n + 2);
+  auto add = [](std::vector<Span>& to, const void* p, size_t bytes) {
+    if (p && bytes) to.push_back(Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes});
   };
   int64_t values = 0;
   for (int i = 0; i < n; ++i) {
@@ -356,21 +357,27 @@ int clip_list_status(const vit_tensor* t, int n, const void* norm, const void* w
     if (t[i].count < 0 || t[i].count > (int64_t)1 << 40 || misaligned(t[i].src) || misaligned(t[i].dst) || (t[i].count > 0 && !t[i].src))
       return VIT_ERR_INVALID_ARG;
     values += t[i].count;
-    if (values > (int64_t)1 << 42) return VIT_ERR_TOO_LARGE;             // pieces of 4096 are counted in 32 bits
+    if (values > (int64_t)1 << 42) return VIT_ERR_TOO_LARGE;             // pieces are counted in 32 bits
     const size_t bytes = (size_t)t[i].count * (t[i].dtype == VIT_BF16 ? 2 : 4);
-    add(t[i].src, bytes, t[i].dst == t[i].src);
-    if (t[i].dst != t[i].src) add(t[i].dst, bytes, true);
+    if (t[i].dst != t[i].src) add(reads, t[i].src, bytes);
+    add(writes, t[i].dst, bytes);
   }
-  add(norm, sizeof(float), true);
-  add(ws, ws_bytes, true);
-  std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
+  add(writes, norm, sizeof(float));
+  add(writes, ws, ws_bytes);
+  const auto before = [](const Span& a, const Span& b) { return a.begin < b.begin; };
+  for (std::vector<Span>* v : {&reads, &writes})                         // (views of one buffer come in order)
+    if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
+  size_t r = 0;
   uintptr_t read_to = 0, written_to = 0;
-  for (const Span& s : spans) {
-    if (s.begin < written_to || (s.write && s.begin < read_to)) return VIT_ERR_INVALID_ARG;
-    uintptr_t& to = s.write ? written_to : read_to;
-    if (s.end > to) to = s.end;
+  for (const Span& w : writes) {
+    for (; r < reads.size() && reads[r].begin <= w.begin; ++r) {
+      if (reads[r].begin < written_to) return VIT_ERR_INVALID_ARG;
+      if (reads[r].end > read_to) read_to = reads[r].end;
+    }
+    if (w.begin < written_to || w.begin < read_to) return VIT_ERR_INVALID_ARG;
+    written_to = w.end;
   }
-  return VIT_OK;
+  return r < reads.size() && reads[r].begin < written_to ? VIT_ERR_INVALID_ARG : VIT_OK;
 }
 
 }  // namespace

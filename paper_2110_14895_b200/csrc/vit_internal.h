@@ -221,7 +221,7 @@ cudaError_t launch_layer_norm_backward(const LayerNormCall& c, float* partial, i
 cudaError_t launch_column_grad(const float* partial, int blocks, int cols, float* dgain, float* dshift, cudaStream_t s);
 
 // norm of many tensors and their scaling (grad_clip.cu), in lists of tensors that fit a launch's parameters
-constexpr int GRAD_CLIP_MAX_BLOCKS = 148 * 8;       // of one list, each with its part of the sum
+constexpr int GRAD_CLIP_MAX_BLOCKS = 148 * 4;       // of one list, each with its part of the sum
 int grad_clip_lists(int tensors);
 cudaError_t launch_grad_clip(const vit_tensor* tensors, int count, int index, bool clip, double* partial, int* partials, float bound,
                              float* norm, cudaStream_t s);
