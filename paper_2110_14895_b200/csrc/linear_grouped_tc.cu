@@ -24,8 +24,6 @@ using namespace grouped;
 
 namespace {
 
-enum Finish : int { F_BIAS = 0, F_GELU = 1, F_GELU_PRE = 2, F_RESIDUAL = 3, F_SLOPE = 4 };
-
 template <int BN, int CTAS, int FINISH> struct Cfg {
   static constexpr int B_ROWS = BN / CTAS;                 // columns of the result whose weights this block loads
   static constexpr int A_BYTES = BM * BK * 2, B_BYTES = B_ROWS * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
@@ -336,7 +334,7 @@ cudaError_t launch_variant(const RowsLaunch& l, cudaStream_t s) {
   return cudaLaunchKernelEx(&cfg, kernel, l.m, l.p);
 }
 template <int BN, int CTAS>
-cudaError_t launch_finish(const GroupedCall& c, int finish, const RowsLaunch& l, cudaStream_t s) {
+cudaError_t launch_finish(const GroupedCall& c, Finish finish, const RowsLaunch& l, cudaStream_t s) {
   if (c.backward) return finish == F_SLOPE ? launch_variant<BN, CTAS, F_SLOPE, true>(l, s) : launch_variant<BN, CTAS, F_BIAS, true>(l, s);
   switch (finish) {
     case F_GELU: return launch_variant<BN, CTAS, F_GELU, false>(l, s);
@@ -377,13 +375,15 @@ cudaError_t launch_grouped_rows_bf16(const GroupedCall& c, cudaStream_t s) {
   const int width = c.backward ? c.in : c.out_features, sum = c.backward ? c.out_features : c.in;
   const int sms = current_device_sm_count();
   if (sms < 2) return cudaErrorInvalidDevice;
+  const Finish finish = c.backward ? (c.pre ? F_SLOPE : F_BIAS) : c.epilogue == 1 ? (c.pre ? F_GELU_PRE : F_GELU) : c.epilogue == 2 ? F_RESIDUAL : F_BIAS;
+  const int split = grouped_few_split(c.shape, width, sum);
+  if (split > 1) return launch_grouped_few_bf16(c, finish, split, s);
   auto tiles = [&](int span) { return c.shape.groups == 1 ? (double)((c.shape.rows + (int64_t)span - 1) / span) : (double)c.shape.rows / span + 0.5 * c.shape.groups; };
   auto rounds = [](double n, int units) { return n <= units ? 1.0 : n / units < 8 ? (double)(int64_t)(n / units + 0.999) : n / units; };
   const double n256 = (width + 255) / 256, n128 = (width + 127) / 128;
   const double pair = 0.92 * rounds(tiles(2 * BM) * n256, sms / 2), wide = rounds(tiles(BM) * n256, sms), narrow = 0.75 * rounds(tiles(BM) * n128, sms);
   const bool two = pair <= wide && pair <= narrow, broad = two || wide <= narrow;
   const int bn = broad ? 256 : 128, span = two ? 2 * BM : BM;
-  const int finish = c.backward ? (c.pre ? F_SLOPE : F_BIAS) : c.epilogue == 1 ? (c.pre ? F_GELU_PRE : F_GELU) : c.epilogue == 2 ? F_RESIDUAL : F_BIAS;
   RowsLaunch l;
   l.p = RowsArgs{c.shape, width, sum, c.backward ? nullptr : c.bias, static_cast<bf16*>(c.y), c.ldy, static_cast<bf16*>(c.pre), c.ldp,
                  (width + bn - 1) / bn, c.dev_status};

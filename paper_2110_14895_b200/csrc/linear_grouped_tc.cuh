@@ -128,10 +128,18 @@ __device__ __forceinline__ void send_rows(const CUtensorMap* tm, bf16* out, int6
   __syncwarp();
 }
 
-// ---- host: maps of matrices in 128-byte-swizzled boxes of 64 columns by `box_rows` rows
+// ---- host
+// What is done with the sums: bias, GELU, GELU with its argument kept, a residual added, GELU's slope at what is read.
+enum Finish : int { F_BIAS = 0, F_GELU = 1, F_GELU_PRE = 2, F_RESIDUAL = 3, F_SLOPE = 4 };
+// maps of matrices in 128-byte-swizzled boxes of 64 columns by `box_rows` rows
 bool encode_rows(CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows);
 // the weights of all groups, [groups][rows][cols]
 bool encode_weights(CUtensorMap* tm, const void* base, int groups, int rows, int cols, int box_rows);
 
 }  // namespace grouped
+
+// few tiles with a long sum, shared by clusters (linear_grouped_few.cu)
+int grouped_few_split(const GroupedShape& shape, int width, int sum);
+cudaError_t launch_grouped_few_bf16(const GroupedCall& c, grouped::Finish finish, int split, cudaStream_t s);
+
 }  // namespace vit
