@@ -372,6 +372,8 @@ LAYERS = [
     ([256, 257, 31, 32, 33], 5, 5, 200, 328), ([64, 63, 65, 0, 15, 16, 17], 0, 0, 128, 256), ([1000], 0, 7, 192, 768), ([40] * 70, 3, 0, 48, 96),
     ([3000, 0, 500, 1], 0, 0, 256, 512), ([700, 900], 11, 0, 1024, 64), ([0, 0], 0, 4, 64, 64), ([1, 1, 1, 1], 0, 0, 640, 8),
     ([9000], 0, 0, 64, 128), ([2500, 2500, 2500], 1, 1, 512, 1288), ([6400], 0, 0, 1280, 1280),
+    # long sums with few tiles, forwards or backwards
+    ([1], 0, 0, 4096, 72), ([5, 0, 130, 1], 2, 3, 1544, 200), ([33], 0, 0, 64, 2056), ([1, 2, 300], 0, 1, 136, 1600), ([129], 0, 0, 1536, 1536),
 ]
 LAYER_CASES = pytest.mark.parametrize("lengths,before,behind,k,n", LAYERS, ids=lambda v: "%dx%d" % (len(v), max(v)) if isinstance(v, list) else str(v))
 
@@ -653,3 +655,238 @@ def test_groups_with_bad_offsets_are_skipped_and_reported(ctx, edges, dtype):
     vit.vit_op_linear_grouped_backward_weights(m.h, dt, none, 0, 64, 0, 72, dw.data_ptr(), db.data_ptr(), ws.data_ptr(), n)
     m.check()
     assert (dw == 0).all() and (db == 0).all()
+
+
+def test_grouped_refusals(ctx):
+    vit, m = ctx
+    rows, k, n, groups = 24, 64, 72, 3
+    z = lambda *shape, t=torch.bfloat16: torch.zeros(*shape, dtype=t, device="cuda")
+    x, out, res, pre, dx, w, dw = z(rows, k), z(rows, n), z(rows, n), z(rows, n), z(rows, k), z(groups, n, k), z(groups, n, k)
+    prek, bias, db = z(rows, k), z(groups, n, t=torch.float32), z(groups, n, t=torch.float32)
+    off = torch.tensor([0, 8, 8, 24], dtype=torch.int32, device="cuda")
+    P = lambda t: t.data_ptr()
+    shape = dict(groups=groups, rows=rows, in_features=k, out_features=n, offsets=P(off))
+    size = vit.vit_linear_grouped_backward_weights_bytes(0, vit.make_grouped_problem(**shape))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    forward = dict(h=m.h, dtype=0, x=P(x), ldx=k, w=P(w), bias=P(bias), epilogue=1, residual=0, ldr=0, out=P(out), ldo=n, pre=P(pre), ldp=n)
+    inputs = dict(h=m.h, dtype=0, dout=P(out), lddout=n, w=P(w), pre=P(prek), ldp=k, dx=P(dx), lddx=k)
+    weights = dict(h=m.h, dtype=0, x=P(x), ldx=k, dout=P(out), lddout=n, dw=P(dw), dbias=P(db), ws=P(ws), ws_bytes=size)
+    calls = ((vit.vit_op_linear_grouped, forward), (vit.vit_op_linear_grouped_backward_input, inputs), (vit.vit_op_linear_grouped_backward_weights, weights))
+
+    def call(f, arguments, problem={}, **changed):
+        f(**{**arguments, **changed, "problem": vit.make_grouped_problem(**{**shape, **problem})})
+
+    before = m.launches
+    for f, arguments in calls:
+        for problem in (dict(groups=0), dict(groups=-1), dict(rows=-1), dict(in_features=0), dict(in_features=60), dict(out_features=4),
+                        dict(out_features=76), dict(offsets=0), dict(offsets=P(off) + 2)):
+            _refused(vit, lambda: call(f, arguments, problem))
+        for problem in (dict(rows=2 ** 31 - 1000), dict(groups=2 ** 30, in_features=2 ** 20, out_features=2 ** 20), dict(groups=2 ** 30)):
+            _refused(vit, lambda: call(f, arguments, problem), vit.VIT_ERR_TOO_LARGE)
+        for bad in (dict(h=None), dict(dtype=2)):
+            _refused(vit, lambda: call(f, arguments, **bad))
+        _refused(vit, lambda: f(**{**arguments, "problem": None}))
+    for bad in (dict(x=0), dict(w=0), dict(out=0), dict(ldx=56), dict(ldo=76), dict(ldp=64), dict(epilogue=3), dict(epilogue=-1), dict(x=P(x) + 2),
+                dict(w=P(w) + 8), dict(bias=P(bias) + 4), dict(out=P(x)), dict(out=P(w)), dict(out=P(bias)), dict(out=P(off)), dict(pre=P(out)),
+                dict(pre=P(x)), dict(pre=P(out) + 16), dict(epilogue=2, pre=0), dict(epilogue=2, pre=0, residual=P(res), ldr=40),
+                dict(epilogue=2, pre=0, residual=P(out), ldr=80)):
+        _refused(vit, lambda: call(vit.vit_op_linear_grouped, forward, **bad))
+    for bad in (dict(dout=0), dict(w=0), dict(dx=0), dict(lddout=64), dict(lddx=60), dict(ldp=8), dict(dx=P(out)), dict(dx=P(w)), dict(dx=P(off)),
+                dict(dx=P(prek), lddx=72), dict(dx=P(prek) + 128), dict(dout=P(out) + 4)):
+        _refused(vit, lambda: call(vit.vit_op_linear_grouped_backward_input, inputs, **bad))
+    for bad in (dict(x=0), dict(dout=0), dict(dw=0), dict(ws=0), dict(ldx=8), dict(lddout=8), dict(dw=P(x)), dict(dw=P(out)), dict(dw=P(off)),
+                dict(dbias=P(dw)), dict(dbias=P(out)), dict(dbias=P(db) + 4), dict(ws=P(x)), dict(ws=P(dw)), dict(ws=P(ws) + 8), dict(ws=P(db))):
+        _refused(vit, lambda: call(vit.vit_op_linear_grouped_backward_weights, weights, **bad))
+    _refused(vit, lambda: call(vit.vit_op_linear_grouped_backward_weights, weights, ws_bytes=size - 1), vit.VIT_ERR_WORKSPACE)
+    assert m.launches == before
+    for f, arguments in calls:
+        call(f, arguments)
+    # what is not looked at may be anything
+    call(vit.vit_op_linear_grouped, forward, epilogue=0, residual=3, ldr=1, pre=5, ldp=1)
+    call(vit.vit_op_linear_grouped, forward, epilogue=2, residual=P(res), ldr=n, pre=7, ldp=3)
+    m.check()
+    assert m.launches == before + 5
+
+
+# ------------------------------------------------------------------------------------ as they are used
+class Mlp:
+    """The MLP half of a layer with experts, rows sorted by expert: x + fc2(gelu(fc1(norm(x)))), its gradients, clipped."""
+
+    NAMES = ("w1", "b1", "w2", "b2", "gain", "shift")
+
+    def __init__(self, vit, m, dtype, lengths, hidden, mlp, seed=0):
+        self.vit, self.m, self.dtype, self.lengths, self.h, self.f = vit, m, dtype, lengths, hidden, mlp
+        gen = _gen(seed)
+        groups, rows = len(lengths), sum(lengths)
+        self.rows, self.dt = rows, _dt(vit, dtype)
+        self.off = torch.tensor([0] + lengths, device="cuda").cumsum(0).to(torch.int32)
+        self.p1 = vit.make_grouped_problem(groups, rows, hidden, mlp, self.off.data_ptr())
+        self.p2 = vit.make_grouped_problem(groups, rows, mlp, hidden, self.off.data_ptr())
+        self.weights = dict(w1=_normal(gen, groups, mlp, hidden, scale=hidden ** -0.5, dtype=dtype), b1=_normal(gen, groups, mlp, scale=0.1),
+                            w2=_normal(gen, groups, hidden, mlp, scale=mlp ** -0.5, dtype=dtype), b2=_normal(gen, groups, hidden, scale=0.1),
+                            gain=1 + _normal(gen, hidden, scale=0.1), shift=_normal(gen, hidden, scale=0.1))
+        self.x, self.dy = _normal(gen, rows, hidden, dtype=dtype), _normal(gen, rows, hidden, scale=0.1, dtype=dtype)
+        e = lambda *shape, t=dtype: torch.empty(*shape, dtype=t, device="cuda")
+        self.norm, self.pre, self.hid, self.y, self.dpre, self.dnorm, self.dx = (e(rows, d) for d in (hidden, mlp, mlp, hidden, mlp, hidden, hidden))
+        self.stats, self.total = e(rows, 2, t=torch.float32), e(1, t=torch.float32)
+        self.grads = {k: torch.empty_like(v) for k, v in self.weights.items()}
+        self.clipped = {k: torch.empty_like(v) for k, v in self.weights.items()}
+        self.tensors = vit.make_tensors([(self.grads[k].data_ptr(), self.clipped[k].data_ptr(), self.grads[k].numel(), _dt(vit, self.grads[k].dtype))
+                                         for k in self.NAMES])
+        self.size = max(vit.vit_layernorm_backward_bytes(rows, hidden), vit.vit_grad_clip_bytes(len(self.NAMES)),
+                        *(vit.vit_linear_grouped_backward_weights_bytes(self.dt, p) for p in (self.p1, self.p2)))
+        self.ws = torch.empty(self.size, dtype=torch.uint8, device="cuda")
+
+    def step(self, bound, stream=0):
+        vit, h, dt, rows, H, F, w, g = self.vit, self.m.h, self.dt, self.rows, self.h, self.f, self.weights, self.grads
+        P = lambda t: t.data_ptr()
+        ws = (P(self.ws), self.size)
+        vit.vit_op_layernorm_forward(h, dt, rows, H, P(self.x), H, P(w["gain"]), P(w["shift"]), EPS, P(self.norm), H, P(self.stats), stream)
+        vit.vit_op_linear_grouped(h, dt, self.p1, P(self.norm), H, P(w["w1"]), P(w["b1"]), 1, 0, 0, P(self.hid), F, P(self.pre), F, stream)
+        vit.vit_op_linear_grouped(h, dt, self.p2, P(self.hid), F, P(w["w2"]), P(w["b2"]), 2, P(self.x), H, P(self.y), H, 0, 0, stream)
+        vit.vit_op_linear_grouped_backward_weights(h, dt, self.p2, P(self.hid), F, P(self.dy), H, P(g["w2"]), P(g["b2"]), *ws, stream)
+        vit.vit_op_linear_grouped_backward_input(h, dt, self.p2, P(self.dy), H, P(w["w2"]), P(self.pre), F, P(self.dpre), F, stream)
+        vit.vit_op_linear_grouped_backward_weights(h, dt, self.p1, P(self.norm), H, P(self.dpre), F, P(g["w1"]), P(g["b1"]), *ws, stream)
+        vit.vit_op_linear_grouped_backward_input(h, dt, self.p1, P(self.dpre), F, P(w["w1"]), 0, 0, P(self.dnorm), H, stream)
+        vit.vit_op_layernorm_backward(h, dt, rows, H, P(self.x), H, P(w["gain"]), P(self.stats), P(self.dnorm), H, P(self.dy), H, P(self.dx), H,
+                                      P(g["gain"]), P(g["shift"]), *ws, stream)
+        vit.vit_op_grad_clip(h, self.tensors, len(self.NAMES), bound, P(self.total), *ws, stream)
+
+    def results(self):
+        return [self.y, self.dx, self.total, *self.grads.values(), *self.clipped.values()]
+
+    def loss(self, x, w):
+        """In 64 bits; x and the weights as tensors that may ask for gradients."""
+        z = (x - x.mean(1, keepdim=True)) / (x.var(1, unbiased=False, keepdim=True) + EPS).sqrt() * w["gain"] + w["shift"]
+        ys = []
+        for g, rows in enumerate(z.split(self.lengths)):
+            ys.append(_gelu64(rows @ w["w1"][g].t() + w["b1"][g]) @ w["w2"][g].t() + w["b2"][g])
+        return x + torch.cat(ys)
+
+
+@BOTH
+def test_training_step_of_an_mlp_with_experts(ctx, dtype):
+    vit, m = ctx
+    mlp = Mlp(vit, m, dtype, [130, 0, 57, 300, 1], 192, 384)
+    mlp.step(0.5)
+    m.check()
+    x = mlp.x.double().requires_grad_()
+    w = {k: v.double().requires_grad_() for k, v in mlp.weights.items()}
+    y = mlp.loss(x, w)
+    want = dict(zip(("x",) + mlp.NAMES, torch.autograd.grad((y * mlp.dy.double()).sum(), [x] + [w[k] for k in mlp.NAMES])))
+    # Every tensor on the way is rounded once, by at most HALF of each value and so of its norm; products with matrices of random
+    # numbers carry such a part of the norm on as it is, give or take a few percent.  On the longest way (x, norm, argument, GELU,
+    # gradient of the argument, of the norm, result) there are six roundings; the sums in 32 bits add a few hundred steps.
+    part = lambda a, b: ((a.double() - b).norm() / b.norm()).item()
+    most = 6 * 1.1 * HALF[dtype] + 500 * STEP
+    assert part(mlp.y, y.detach()) <= most
+    assert part(mlp.dx, want["x"]) <= most
+    for k in mlp.NAMES:
+        assert part(mlp.grads[k], want[k]) <= most, k
+    _check_clip(list(mlp.grads.values()), 0.5, mlp.total, list(mlp.clipped.values()))
+    assert mlp.total.item() > 0.5                                                # the bound is at work
+    # along a direction, against differences of the 64-bit forward pass
+    gen = _gen(9)
+    by = {k: _normal(gen, *v.shape).double() * v.double().abs().mean() for k, v in [("x", mlp.x)] + list(mlp.weights.items())}
+    at = lambda e: (mlp.loss(mlp.x.double() + e * by["x"], {k: v.double() + e * by[k] for k, v in mlp.weights.items()}) * mlp.dy.double()).sum().item()
+    difference = (at(1e-5) - at(-1e-5)) / 2e-5
+    got = {**mlp.grads, "x": mlp.dx}
+    inner = sum((got[k].double() * by[k]).sum().item() for k in by)
+    size = math.sqrt(sum(got[k].double().norm().item() ** 2 for k in by)) * math.sqrt(sum(by[k].norm().item() ** 2 for k in by))
+    assert abs(inner - difference) <= most * size + 1e-6 * abs(difference)
+
+
+@BOTH
+def test_training_step_on_streams_and_in_graphs(ctx, dtype):
+    """Two loops at once, each with scratch of its own, eagerly on two streams and as graphs replayed with other inputs."""
+    vit, m = ctx
+    loops = [Mlp(vit, m, dtype, [200, 31, 0, 400], 128, 320, seed=1), Mlp(vit, m, dtype, [1500], 256, 512, seed=2)]
+    want = []
+    for loop in loops:
+        loop.step(0.3)
+        m.check()
+        want.append([t.clone() for t in loop.results()])
+    streams = [torch.cuda.Stream() for _ in loops]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for loop, stream in zip(loops, streams):
+            loop.step(0.3, stream.cuda_stream)
+    torch.cuda.synchronize()
+    m.check()
+    for loop, w in zip(loops, want):
+        assert all(torch.equal(a, b) for a, b in zip(loop.results(), w))
+    graphs = [torch.cuda.CUDAGraph() for _ in loops]
+    for loop, stream, graph in zip(loops, streams, graphs):
+        with torch.cuda.graph(graph, stream=stream):
+            loop.step(0.3, stream.cuda_stream)
+    for loop in loops:
+        for t in loop.results():
+            t.fill_(55.0)
+        loop.dy.mul_(2)
+        loop.x.neg_()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for stream, graph in zip(streams, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    m.check()
+    replayed = [[t.clone() for t in loop.results()] for loop in loops]
+    for loop, r in zip(loops, replayed):
+        loop.step(0.3)
+        m.check()
+        assert all(torch.equal(a, b) for a, b in zip(loop.results(), r))
+
+
+def test_rows_beyond_two_to_the_31_elements(ctx):
+    """The last rows of buffers whose offsets need more than 32 bits."""
+    vit, m = ctx
+    rows, ld, k, n, last = 70000, 32768, 64, 72, 300
+    a, b = (torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld) for _ in range(2))
+    gen = _gen(8)
+    a[-last:, :k] = _normal(gen, last, k, dtype=torch.bfloat16)
+    off = torch.tensor([0, 0, rows - last, rows], dtype=torch.int32, device="cuda")
+    off[1] = off[2]                                        # the first group has all other rows; the second none
+    l = Layer(vit, m, [1], 0, 0, k, n, torch.bfloat16)
+    small = a[-last:, :k].contiguous()
+    w = _normal(gen, 3, n, k, dtype=torch.bfloat16)
+    p = vit.make_grouped_problem(3, rows, k, n, off.data_ptr())
+    one = vit.make_grouped_problem(1, last, k, n, 0)
+    vit.vit_op_linear_grouped(m.h, 0, p, a.data_ptr(), ld, w.data_ptr(), 0, 0, 0, 0, b.data_ptr(), ld, 0, 0)
+    want = torch.empty(last, n, dtype=torch.bfloat16, device="cuda")
+    vit.vit_op_linear_grouped(m.h, 0, one, small.data_ptr(), k, w[2].data_ptr(), 0, 0, 0, 0, want.data_ptr(), n, 0, 0)
+    m.check()
+    assert torch.equal(b[-last:, :n], want)
+    dx = torch.empty(last, k, dtype=torch.bfloat16, device="cuda")
+    vit.vit_op_linear_grouped_backward_input(m.h, 0, one, want.data_ptr(), n, w[2].data_ptr(), 0, 0, dx.data_ptr(), k)
+    g, s = torch.ones(k, device="cuda"), torch.zeros(k, device="cuda")
+    size = vit.vit_linear_grouped_backward_weights_bytes(0, p)
+    ws, dw, dw1 = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty_like(w), torch.empty_like(w[:1])
+    off[1] = 0
+    off[2] = rows - last
+    off[0] = 0
+    a[:last, :k] = a[-last:, :k]
+    b[:last, :n] = b[-last:, :n]
+    off.copy_(torch.tensor([0, last, last, last], dtype=torch.int32))
+    vit.vit_op_linear_grouped_backward_weights(m.h, 0, p, a.data_ptr(), ld, b.data_ptr(), ld, dw.data_ptr(), 0, ws.data_ptr(), size)
+    off.copy_(torch.tensor([rows - last, rows, rows, rows], dtype=torch.int32))
+    dw2 = torch.empty_like(w)
+    vit.vit_op_linear_grouped_backward_weights(m.h, 0, p, a.data_ptr(), ld, b.data_ptr(), ld, dw2.data_ptr(), 0, ws.data_ptr(), size)
+    assert torch.equal(dw, dw2) and dw[0].abs().sum() > 0 and (dw[1:] == 0).all()
+    off.copy_(torch.tensor([rows, rows, rows - last, rows], dtype=torch.int32))       # (the second one is a bad one)
+    vit.vit_op_linear_grouped_backward_input(m.h, 0, p, b.data_ptr(), ld, w.data_ptr(), 0, 0, a.data_ptr(), ld)
+    with pytest.raises(vit.VitError):
+        m.check()
+    assert torch.equal(a[-last:, :k], dx)
+    stats, stats1 = torch.empty(rows, 2, device="cuda"), torch.empty(last, 2, device="cuda")
+    y1 = torch.empty(last, k, dtype=torch.bfloat16, device="cuda")
+    vit.vit_op_layernorm_forward(m.h, 0, last, k, a[-last:].data_ptr(), ld, g.data_ptr(), s.data_ptr(), EPS, y1.data_ptr(), k, stats1.data_ptr())
+    vit.vit_op_layernorm_forward(m.h, 0, rows, k, a.data_ptr(), ld, g.data_ptr(), s.data_ptr(), EPS, b.data_ptr(), ld, stats.data_ptr())
+    assert torch.equal(b[-last:, :k], y1) and torch.equal(stats[-last:], stats1)
+    m.check()
+    # and one tensor as long
+    a.fill_(0.5)
+    norm, out = _clip(vit, m, [a.view(-1)], 1.0, "same")
+    assert norm.item() == pytest.approx(0.5 * math.sqrt(rows * ld), rel=1e-6)
+    by = 1 / norm.item()
+    assert (a == torch.tensor(0.5 * by).to(torch.bfloat16).item()).all()
