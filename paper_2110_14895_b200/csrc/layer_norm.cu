@@ -393,9 +393,10 @@ cudaError_t launch_backward(BackwardArgs a, cudaStream_t s, int* blocks) {
   if (*blocks > LAYER_NORM_MAX_BLOCKS) *blocks = LAYER_NORM_MAX_BLOCKS;
   return launch_after(kernel, *blocks, WARPS * 32, smem, s, a);
 }
-// The sums of dg and db are what a thread needs registers for: with a warp to a row of 1024 columns 64, twelve warps fit an SM
-// and wait for one another's instructions (22 us at 12608 rows); two warps to a row leave room for twenty (xx us).  fp32 rows
-// are twice as long in the ring.
+// The sums of dg and db are what a thread needs registers for: a warp to a row of 1280 columns leaves room for eight warps an SM
+// (60.5 us at 32896 rows), two warps to a row for sixteen (58 us); at 1024 columns twelve and twenty (24.2, 23.9 us at 12608
+// rows).  Most of the rest are the start, the end and the second kernel: 12 us and 6.9 TB/s fit both.  fp32 rows are twice as
+// long in the ring.
 template <typename T>
 cudaError_t dispatch_backward(const BackwardArgs& a, cudaStream_t s, int* blocks) {
   constexpr bool F = sizeof(T) == 4;

@@ -9,7 +9,8 @@
 // The rows behind a group's end are the next group's: they are cleared in the last stage, in both operands (zero times a
 // value that is not a number would not be zero).  A warp of its own in each block sees the copies land, clears, and hands the
 // stage on to the warp that issues the products (the even block's, for both); it runs ahead of them, so that neither the
-// clearing nor the way from block to block holds them up (with both in the issuing warp's path: 241 us, now 2xx).
+// clearing nor the way from block to block holds them up (at 25216 rows of 16 groups 2 % of the time, with both
+// in the issuing warp's path; with a release at cluster scope in every stage twice the time).
 // Two more warps add up dout's columns for db from the same stages, where the tile is its row's first.
 // The units of work get equal stretches of it (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
 #include "linear_grouped.cuh"
@@ -314,7 +315,7 @@ template <> __device__ __forceinline__ void store4(bf16* to, float4 v) {
 }
 constexpr int JOIN_THREADS = 256;
 template <typename T, int ROWS, int COLS>
-__global__ void __launch_bounds__(JOIN_THREADS)
+__global__ void __launch_bounds__(JOIN_THREADS, 4)
 grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int tiles, int blocks, const int* __restrict__ table,
                     const float* __restrict__ part, const float* __restrict__ part_bias, T* __restrict__ dw, float* __restrict__ dbias) {
   constexpr bool WARPS = sizeof(T) == 2;                          // parts lie as the epilogue warps of the tensor-core kernel hold them
@@ -338,15 +339,25 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
   for (int i = 0; i < N; ++i) sum[i] = *reinterpret_cast<const float4*>(mine + ((int64_t)before * 2 + 1) * ROWS * COLS + 4 * JOIN_THREADS * i);
   const bool bias = dbias && k0 == 0 && piece == 0 && threadIdx.x < ROWS;
   float b = bias ? part_bias[((int64_t)before * 2 + 1) * ROWS + threadIdx.x] : 0.f;
-#pragma unroll 4
-  for (int who = block; who < blocks && table[who] < tile_end; ++who) {          // (some have no share: they are added as zeros)
-    const bool some = table[who + 1] > table[who];
+  // two parts at a time, all their values under way together
+  for (int first = block; first < blocks && table[first] < tile_end; first += 2) {
+    float4 v[2][N];
+    float c[2];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float4 v = some ? *reinterpret_cast<const float4*>(mine + (int64_t)who * 2 * ROWS * COLS + 4 * JOIN_THREADS * i) : make_float4(0.f, 0.f, 0.f, 0.f);
-      sum[i] = make_float4(sum[i].x + v.x, sum[i].y + v.y, sum[i].z + v.z, sum[i].w + v.w);
+    for (int k = 0; k < 2; ++k) {
+      const int who = first + k;
+      const bool some = who < blocks && table[who] < tile_end && table[who + 1] > table[who];          // (blocks without a share add zeros)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        v[k][i] = some ? *reinterpret_cast<const float4*>(mine + (int64_t)who * 2 * ROWS * COLS + 4 * JOIN_THREADS * i) : make_float4(0.f, 0.f, 0.f, 0.f);
+      c[k] = bias && some ? part_bias[(int64_t)who * 2 * ROWS + threadIdx.x] : 0.f;
     }
-    if (bias && some) b += part_bias[(int64_t)who * 2 * ROWS + threadIdx.x];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum[i] = make_float4(sum[i].x + v[k][i].x, sum[i].y + v[k][i].y, sum[i].z + v[k][i].z, sum[i].w + v[k][i].w);
+      b += c[k];
+    }
   }
   if (bias && n0 + (int)threadIdx.x < out) dbias[(int64_t)here.group * out + n0 + threadIdx.x] = b;
   if (WARPS) {
@@ -375,8 +386,9 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
 struct DwTiling { int rows, cols, tiles_in, tiles, blocks; bool cuts; };       // blocks: units of work, pairs where a tile has 256 rows
 DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   DwTiling t;
-  // a pair's tile costs 1.4 of a single block's half (measured at 1024 x 4096): not for layers that would leave it empty
-  const bool pair = act_bf16 && (out + 255) / 256 * 2.8 <= (out + 127) / 128 * 2.0;
+  // A pair's tile takes 0.87 of the time of its two halves from single blocks (180 against 207 us at 25216 rows of 16 groups,
+  // 1024 x 4096), and is wasted where it hangs over (1536 x 384: 57 against 50 us).
+  const bool pair = act_bf16 && (out + 255) / 256 * 1.74 <= (out + 127) / 128;
   t.rows = pair ? 256 : 128;
   t.cols = act_bf16 ? TN : 128;
   t.tiles_in = (in + t.cols - 1) / t.cols;
