@@ -47,7 +47,7 @@ enum {
   VIT_ERR_TOO_LARGE = -8,   /* problem exceeds the fixed scratch of an allocation-free entry point,
                                or the partitioner's tables do not fit in host memory */
   VIT_ERR_INFEASIBLE = -9,  /* the partitioner found no assignment that fits the devices' memory */
-  VIT_ERR_OFFSETS = -10     /* device status word: a packed sequence's offsets were out of order or range */
+  VIT_ERR_OFFSETS = -10     /* device status word: a packed sequence's or group's offsets were out of order or range */
 };
 
 enum { VIT_BF16 = 0, VIT_FP32 = 1 };
@@ -300,7 +300,7 @@ int vit_op_attention(vit_handle* h, int dtype, int images, int T, int heads, int
 /* ---- packed images: position rotation, query/key norm, attention and their gradients ---------
  * A batch of images of different sizes is one buffer of tokens, image after image.  These operations
  * serve such a layer between its QKV product and its output product, forwards and backwards.  The gradients of the
- * layer's other parts (linear products, LayerNorm, GELU) are not in this library, and the stage calls above do not use
+ * layer's other parts (linear products, LayerNorm, GELU) are further below, and the stage calls above do not use
  * these operations: a caller's own training or serving loop does.
  * Rows have strides of their own (`ld...`, in elements), so that queries, keys and values can be read
  * from, and their gradients written to, the column blocks of one [rows, (heads + 2 kv_heads) * d] buffer.
@@ -419,7 +419,8 @@ int vit_op_layernorm_backward(vit_handle* h, int dtype, int rows, int cols, cons
  * The rows of group g are offsets[g] ... offsets[g+1] - 1.  The offsets are read on the device.  A group whose offsets are
  * out of order or reach outside the rows is skipped, its rows (or weights' gradients) are left as they were, and
  * vit_check_status reports VIT_ERR_OFFSETS; the other groups are computed; where a step backwards makes two of them
- * overlap, what is written to the rows that they share is undefined.  Rows that no group covers are left as they were. */
+ * overlap, what is written to the rows that they share is undefined.  Rows that no group covers are left as they were.
+ * A problem whose tiles could not be counted in 32 bits, if every group had all rows, is refused (VIT_ERR_TOO_LARGE). */
 typedef struct vit_grouped_problem {
   int32_t groups;                     /* >= 1 */
   int32_t rows;                       /* of the activations; at most INT32_MAX - 1024 */

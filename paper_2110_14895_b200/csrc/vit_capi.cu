@@ -326,7 +326,7 @@ bool grouped_fits(const vit_grouped_problem* p) {
   return weights <= (int64_t)1 << 36 && p->groups <= INT64_MAX / 16 / weights && units <= INT32_MAX / 2 / ((widest + 63) / 64) &&
          units <= INT32_MAX / 2 / sums;
 }
-// whether an output lies over the offsets or any other operand
+// whether an output lies over the offsets
 bool over_offsets(const vit_grouped_problem* p, const Block& out) {
   return p->offsets && blocks_overlap(out, Block{p->offsets, 1, (int64_t)p->groups + 1, (int64_t)p->groups + 1, 4});
 }

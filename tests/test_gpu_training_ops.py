@@ -862,9 +862,6 @@ def test_rows_beyond_two_to_the_31_elements(ctx):
     g, s = torch.ones(k, device="cuda"), torch.zeros(k, device="cuda")
     size = vit.vit_linear_grouped_backward_weights_bytes(0, p)
     ws, dw, dw1 = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.empty_like(w), torch.empty_like(w[:1])
-    off[1] = 0
-    off[2] = rows - last
-    off[0] = 0
     a[:last, :k] = a[-last:, :k]
     b[:last, :n] = b[-last:, :n]
     off.copy_(torch.tensor([0, last, last, last], dtype=torch.int32))
