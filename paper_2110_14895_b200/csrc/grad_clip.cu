@@ -156,6 +156,12 @@ square_sum_kernel(const __grid_constant__ List<CAP> list, double* __restrict__ p
 template <int CAP>
 __global__ void __launch_bounds__(THREADS)
 clip_kernel(const __grid_constant__ List<CAP> list, const double* __restrict__ partial, int partials, float bound, float* norm) {
+  const int begin = share_begin(list.pieces, (int)blockIdx.x, (int)gridDim.x), end = share_begin(list.pieces, (int)blockIdx.x + 1, (int)gridDim.x);
+  int at = begin < end ? entry_of(list, end - 1) : 0;
+  // The first piece is fetched while the kernel before this one ends: that one, too, has only begun when nobody wrote the
+  // tensors any more, and does not write them itself.
+  float v[PER];
+  if (begin < end && list.e[at].dst) load_piece(list.e[at], (int64_t)(end - 1 - list.e[at].first_piece) * PIECE, v);
   ptx::grid_dependency_wait();
   double sum = 0.0;
   for (int i = threadIdx.x; i < partials; i += THREADS) sum += partial[i];
@@ -167,15 +173,12 @@ clip_kernel(const __grid_constant__ List<CAP> list, const double* __restrict__ p
   const float small = by64 < 0x1p-100 ? 0x1p-100f : 1.0f;
   if (by64 < 0x1p-100) by64 *= 0x1p100;
   const float by = (float)by64;
-  const int begin = share_begin(list.pieces, (int)blockIdx.x, (int)gridDim.x), end = share_begin(list.pieces, (int)blockIdx.x + 1, (int)gridDim.x);
-  int at = begin < end ? entry_of(list, end - 1) : 0;
   for (int piece = end - 1; piece >= begin; --piece) {
     while (list.e[at].first_piece > piece) --at;
     const Entry& e = list.e[at];
     if (!e.dst || (e.dst == e.src && by == 1.0f)) continue;
     const int64_t from = (int64_t)(piece - e.first_piece) * PIECE;
-    float v[PER];
-    load_piece(e, from, v);
+    if (piece != end - 1) load_piece(e, from, v);
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = v[i] * by * small;
     store_piece(e, from, v);

@@ -347,7 +347,7 @@ struct Span { uintptr_t begin, end; };
 int clip_list_status(const vit_tensor* t, int n, const void* norm, const void* ws, size_t ws_bytes) {
   std::vector<Span> reads, writes;
   reads.reserve((size_t)n);
-  writes.reserve((size_t)n + 2);
+  writes.reserve((size_t)n);
   auto add = [](std::vector<Span>& to, const void* p, size_t bytes) {
     if (p && bytes) to.push_back(Span{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + bytes});
   };
@@ -362,8 +362,16 @@ int clip_list_status(const vit_tensor* t, int n, const void* norm, const void* w
     if (t[i].dst != t[i].src) add(reads, t[i].src, bytes);
     add(writes, t[i].dst, bytes);
   }
-  add(writes, norm, sizeof(float));
-  add(writes, ws, ws_bytes);
+  std::vector<Span> own;                                                 // norm and scratch, against everything
+  add(own, norm, sizeof(float));
+  add(own, ws, ws_bytes);
+  const auto meet = [](const Span& a, const Span& b) { return a.begin < b.end && b.begin < a.end; };
+  for (size_t k = 0; k < own.size(); ++k) {
+    if (k == 1 && meet(own[0], own[1])) return VIT_ERR_INVALID_ARG;
+    for (const std::vector<Span>* v : {&reads, &writes})
+      for (const Span& s : *v)
+        if (meet(s, own[k])) return VIT_ERR_INVALID_ARG;
+  }
   const auto before = [](const Span& a, const Span& b) { return a.begin < b.begin; };
   for (std::vector<Span>* v : {&reads, &writes})                         // (views of one buffer come in order)
     if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
