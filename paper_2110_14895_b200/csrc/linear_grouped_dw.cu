@@ -11,7 +11,7 @@
 // stage on to the warp that issues the products (the even block's, for both); it runs ahead of them, so that neither the
 // clearing nor the way from block to block holds them up (at 25216 rows of 16 groups 2 % of the time, with both
 // in the issuing warp's path; with a release at cluster scope in every stage twice the time).
-// Two more warps add up dout's columns for db from the same stages, where the tile is its row's first.
+// Four more warps add up dout's columns for db from the same stages, where the tile is its row's first.
 // The units of work get equal shares of it (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
 // 25216 rows of 16 groups, 1024 x 4096: 185 us (tensor pipe active 66 %); one group of 8192 rows, 4096 x 4096: 190 us (1440
 // TFLOP/s); 8224 rows, 1280 x 1280: 39 us, of which 12 are products.
@@ -162,7 +162,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         __syncwarp();
         if (++buf == 2) { buf = 0; aphase ^= 1; }
       }
-      if (*abort_flag) drain_products(drain, lane);
+      if (*abort_flag) drain_products(drain);
     }
   } else if (warp == 2 + EPI_WARPS + SUM_WARPS) {
     // ---------------------------------------------------------------- stages that have landed are handed on
@@ -209,7 +209,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
           for (int h = 0; h < 2; ++h) {
             uint32_t r[32];
             tmem_ld32(taddr + 64 * cb + 32 * h, r);
-            tmem_ld_wait();
+            tmem_ld_wait_for(r);
             float2 v[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e)
@@ -227,7 +227,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         for (int q = 0; q < 4; ++q) {
           uint32_t r[32];
           tmem_ld32(taddr + 32 * q, r);
-          tmem_ld_wait();
+          tmem_ld_wait_for(r);
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             *reinterpret_cast<uint4*>(to + (q * 8 + e) * 128) = make_uint4(r[4 * e], r[4 * e + 1], r[4 * e + 2], r[4 * e + 3]);

@@ -132,7 +132,7 @@ grouped_few_kernel(const __grid_constant__ FewMaps m, const __grid_constant__ Fe
         for (int h = 0; h < 2; ++h) {
           uint32_t r[32];
           tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half + 32 * h), r);
-          tmem_ld_wait();
+          tmem_ld_wait_for(r);
           if (row < rows) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -197,7 +197,7 @@ grouped_few_kernel(const __grid_constant__ FewMaps m, const __grid_constant__ Fe
 
   if (*abort_flag) {
     if (warp == 0) drain_stages(full, STAGES, fills);
-    if (warp == 1) drain_products(drain, lane);
+    if (warp == 1) drain_products(drain);
   }
   __syncwarp();
   tc_fence_before();

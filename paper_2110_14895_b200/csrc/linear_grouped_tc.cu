@@ -166,7 +166,7 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
         __syncwarp();
         if (++buf == 2) { buf = 0; aphase ^= 1; }
       }
-      if (*abort_flag) drain_products(drain, lane);
+      if (*abort_flag) drain_products(drain);
     }
   } else {
     // ---------------------------------------------------------------- epilogue
@@ -209,7 +209,7 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
               for (int g = 0; g < 8; ++g)
                 b[g] = bias && c0 + 32 * h + 4 * g < p.width ? __ldg(reinterpret_cast<const float4*>(bias + 32 * h) + g) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            tmem_ld_wait();
+            tmem_ld_wait_for(r);
 #pragma unroll
             for (int g = 0; g < 8; ++g) {
               v[2 * g] = make_float2(__uint_as_float(r[4 * g]), __uint_as_float(r[4 * g + 1]));
@@ -268,8 +268,10 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
             put_half(v, piece, lane, h);
           }
           send_rows(&m.out, p.out, p.ldo, piece, row0, c0, rows, p.width, lane);
-        } else if (last && lane == 0) {
-          give_back<CTAS>(tempty + 8 * buf);
+        } else if (last) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) give_back<CTAS>(tempty + 8 * buf);
         }
       }
       if (!ok) break;

@@ -82,10 +82,10 @@ __device__ __forceinline__ void drain_stages(uint32_t full, int stages, long lon
   for (long long f = fills > stages ? fills - stages : 0; f < fills; ++f)
     mbar_wait_limit(full + 8 * (uint32_t)(f % stages), (uint32_t)((f / stages) & 1), &never, DRAIN_LIMIT_CYCLES);
 }
-// and the products issued so far are done before tensor memory is freed
-__device__ __forceinline__ void drain_products(uint32_t bar, int lane) {
+// and the products issued so far (by the thread that the hardware elects) are done before tensor memory is freed
+__device__ __forceinline__ void drain_products(uint32_t bar) {
   volatile int never = 0;
-  if (lane == 0) {
+  if (elect_one()) {
     umma_commit(bar);
     mbar_wait_limit(bar, 0, &never, DRAIN_LIMIT_CYCLES);
   }
