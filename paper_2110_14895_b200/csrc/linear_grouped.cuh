@@ -93,8 +93,8 @@ struct TileCount {
 // and last tile there may be parts; each part has one owner, and the parts are joined in the order of their rows.
 // Parts begin in the middle where that brings all blocks to the same rows modulo a share: at a time t of its share a block is
 // at unit t + k share of its tile, for some k.
-// Blocks at most; units of a share of the line at least (a part costs about as much as this many), unless there are fewer tiles
-// than blocks: a unit takes 0.3 us on the tensor cores, 5 us on the fp32 pipes.
+// Blocks at most; units of a share of the line at least, unless there are fewer tiles than blocks (grouped_dw_plan may ask for
+// more): a unit takes 0.3 us on the tensor cores, 5 us on the fp32 pipes, and a part of a tile 2 us and more.
 constexpr int DW_BLOCKS = 148, DW_BLOCKS_F32 = 296, DW_ROWS = 64, DW_LEAST = 8, DW_LEAST_F32 = 1;
 struct SumCount {
   int tiles;

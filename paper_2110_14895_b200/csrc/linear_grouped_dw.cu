@@ -18,6 +18,8 @@
 #include "linear_grouped.cuh"
 #include "linear_grouped_tc.cuh"
 
+#include <cmath>
+
 namespace vit {
 
 using namespace grouped;
@@ -32,7 +34,7 @@ template <int CTAS> struct DwCfg {
 
 struct DwArgs {
   GroupedShape shape;
-  int in, out, tiles_in, tiles, cuts;  // tiles of a group: ceil(out / (128 blocks)) x ceil(in / 256)
+  int in, out, tiles_in, tiles, least, cuts;  // tiles of a group: ceil(out / (128 blocks)) x ceil(in / 256)
   float* dbias;                    // [groups][out] or nullptr
   float* part_bias;                // [units][2][128 blocks]
   float* part;                     // [units][2][epilogue warps of the blocks][4][8][32][4]: parts of tiles, as the warps hold them
@@ -100,7 +102,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   grid_dependency_wait();
   grid_launch_dependents();
   const uint32_t tmem = *tmem_slot;
-  const Share share = find_share(p.shape, p.tiles, units, self, DW_LEAST, p.cuts, reinterpret_cast<int*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
+  const Share share = find_share(p.shape, p.tiles, units, self, p.least, p.cuts, reinterpret_cast<int*>(smem + STAGES * C::STAGE_BYTES) /* staging */,
                                  rank == 0 ? p.table : nullptr);
   __syncthreads();
   PartWalk work(p.shape, p.tiles, lane, share, self, units);
@@ -385,7 +387,7 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
   }
 }
 
-struct DwTiling { int rows, cols, tiles_in, tiles, blocks; bool cuts; };       // blocks: units of work, pairs where a tile has 256 rows
+struct DwTiling { int rows, cols, tiles_in, tiles, blocks, least; bool cuts; };       // blocks: units of work, pairs where a tile has 256 rows
 DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   DwTiling t;
   // A pair's tile takes 0.87 of the time of its two halves from single blocks (180 against 207 us at 25216 rows of 16 groups,
@@ -398,10 +400,14 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   t.tiles = (int)tiles;
   // as many as the rows can need: the kernels, which see the groups' lengths, may use fewer
   const int64_t units = tiles * ((int64_t)shape.rows / DW_ROWS + shape.groups), whole = tiles * shape.groups;
-  const int64_t least = act_bf16 ? DW_LEAST : DW_LEAST_F32, wanted = units / least > whole ? units / least : whole;
+  // A tile cut into n parts saves (1 - 1 / n) of its time, 0.3 (5) us a unit, and costs about 0.35 us a part when they are joined:
+  // shares of sqrt(1.2 (0.07) units of a tile) are the best (12608 rows, 768 x 192: 31 us with 8 units, 24 with 14).
+  const int root = (int)std::sqrt((double)(shape.rows / DW_ROWS));
+  t.least = act_bf16 ? (root > DW_LEAST ? root : DW_LEAST) : (root / 4 > DW_LEAST_F32 ? root / 4 : DW_LEAST_F32);
+  const int64_t least = t.least, wanted = units / least > whole ? units / least : whole;
   const int64_t most = pair ? DW_BLOCKS / 2 : act_bf16 ? DW_BLOCKS : DW_BLOCKS_F32;
   // few rows: no tile is worth a cut, and neither parts nor a second kernel are needed
-  t.cuts = shape.rows > least * DW_ROWS;
+  t.cuts = shape.rows > (act_bf16 ? DW_LEAST : DW_LEAST_F32) * DW_ROWS;
   t.blocks = (int)((t.cuts ? wanted : whole) < most ? (wanted < 1 ? 1 : t.cuts ? wanted : whole) : most);
   return t;
 }
@@ -416,7 +422,7 @@ size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int o
 GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16) {
   const DwTiling t = tiling_of(act_bf16, c.shape, c.in, c.out_features);
   float* part = c.partial + 64 * ((DW_TABLE + 63) / 64);                        // behind the table
-  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, t.cuts, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int*>(c.partial)};
+  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, t.least, t.cuts, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int*>(c.partial)};
 }
 
 template <int CTAS>
@@ -443,7 +449,7 @@ static cudaError_t launch_dw(const DwMaps& m, const DwArgs& p, int units, cudaSt
 cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, true);
   DwMaps m;
-  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.cuts, c.dbias, plan.part_bias, plan.part, plan.table, c.dev_status};
+  DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.least, plan.cuts, c.dbias, plan.part_bias, plan.part, plan.table, c.dev_status};
   // without rows nothing is read, and any map will do
   const int64_t rows = c.shape.rows > 0 ? c.shape.rows : 1;
   const void *dout = c.shape.rows > 0 ? c.dout : c.dw, *x = c.shape.rows > 0 ? c.x : c.dw;

@@ -189,7 +189,7 @@ grouped_rows_f32_kernel(const RowsArgs p) {
 
 struct DwArgs {
   GroupedShape shape;
-  int in, out, tiles_in, tiles, cuts;
+  int in, out, tiles_in, tiles, least, cuts;
   const float *x, *dout;
   int64_t ldx, lddout;
   float *dw, *dbias, *part, *part_bias;
@@ -205,7 +205,7 @@ grouped_dw_f32_kernel(const DwArgs p) {
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
-  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, DW_LEAST_F32, p.cuts, reinterpret_cast<int*>(&a[0][0][0]), p.table);
+  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, p.least, p.cuts, reinterpret_cast<int*>(&a[0][0][0]), p.table);
   __syncthreads();
   PartWalk work(p.shape, p.tiles, lane, share, (int)blockIdx.x, (int)gridDim.x);
   Part part;
@@ -309,7 +309,7 @@ cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s) {
 
 cudaError_t launch_grouped_dw_f32(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, false);
-  const DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.cuts, static_cast<const float*>(c.x), static_cast<const float*>(c.dout),
+  const DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.least, plan.cuts, static_cast<const float*>(c.x), static_cast<const float*>(c.dout),
                  c.ldx, c.lddout, static_cast<float*>(c.dw), c.dbias, plan.part, plan.part_bias, plan.table, c.dev_status};
   return launch_after(grouped_dw_f32_kernel, plan.blocks, p, s);
 }

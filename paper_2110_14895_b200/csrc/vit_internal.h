@@ -249,7 +249,7 @@ cudaError_t launch_grouped_rows_bf16(const GroupedCall& c, cudaStream_t s);
 cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s);
 // weight gradients: blocks share all work equally and leave the sums of cut tiles in `partial`, a second kernel joins them
 size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int out_features);
-struct GroupedDw { int rows, tiles_in, tiles, blocks; bool cuts; float *part, *part_bias; int* table; };        // [blocks][2] tiles and rows of them; shares
+struct GroupedDw { int rows, tiles_in, tiles, blocks, least; bool cuts; float *part, *part_bias; int* table; };        // [blocks][2] tiles and rows of them; shares
 GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16);
 cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s);
 cudaError_t launch_grouped_dw_f32(const GroupedCall& c, cudaStream_t s);
