@@ -11,7 +11,7 @@ LIB = os.path.join(PKG, "libvit_b200.so")
 SOURCES = ["vit_capi.cu", "kernels_simt.cu", "gemm_tcgen05.cu", "attention.cu", "attention_tc.cu", "partition.cu",
            "rope_norm.cu", "attention_packed.cu", "attention_packed_tc.cu",
            "attention_rows.cu", "layer_norm.cu", "grad_clip.cu",
-           "linear_grouped_tc.cu", "linear_grouped_dw.cu", "linear_grouped_few.cu", "linear_grouped_f32.cu"]
+           "linear_grouped_tc.cu", "linear_grouped_dw.cu", "linear_grouped_dw_few.cu", "linear_grouped_few.cu", "linear_grouped_f32.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "-Xcompiler", "-fPIC", "-Xptxas", "-v",

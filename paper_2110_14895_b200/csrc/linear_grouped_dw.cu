@@ -14,7 +14,7 @@
 // Four more warps add up dout's columns for db from the same stages, where the tile is its row's first.
 // The units of work get equal shares of it (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
 // 25216 rows of 16 groups, 1024 x 4096: 185 us (tensor pipe active 66 %); one group of 8192 rows, 4096 x 4096: 190 us (1440
-// TFLOP/s); 8224 rows, 1280 x 1280: 39 us, of which 12 are products.
+// TFLOP/s); 32896 rows, 1280 x 1280: 99 us.
 #include "linear_grouped.cuh"
 #include "linear_grouped_tc.cuh"
 
@@ -387,7 +387,7 @@ grouped_join_kernel(const GroupedShape shape, int in, int out, int tiles_in, int
   }
 }
 
-struct DwTiling { int rows, cols, tiles_in, tiles, blocks, least; bool cuts; };       // blocks: units of work, pairs where a tile has 256 rows
+struct DwTiling { int rows, cols, tiles_in, tiles, blocks, least, split; bool cuts; };       // blocks: units of work, pairs where a tile has 256 rows
 DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   DwTiling t;
   // A pair's tile takes 0.87 of the time of its two halves from single blocks (180 against 207 us at 25216 rows of 16 groups,
@@ -409,6 +409,18 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   // few rows: no tile is worth a cut, and neither parts nor a second kernel are needed
   t.cuts = shape.rows > (act_bf16 ? DW_LEAST : DW_LEAST_F32) * DW_ROWS;
   t.blocks = (int)((t.cuts ? wanted : whole) < most ? (wanted < 1 ? 1 : t.cuts ? wanted : whole) : most);
+  // One sum for few tiles: a cluster's two or four pairs to a tile need neither parts in memory nor the second kernel, 7 to 10 us,
+  // but leave pairs idle, 0.42 us for each unit that a pair has more than a share: even at 22 (577 rows, 1280 x 1280: 13 us, 21
+  // with shares; 6000 rows, 768 x 768: 24 and 27; 12608: 34 and 32).  Not every SM finds partners: 14 clusters of eight
+  // blocks run at once and 16 do not (2000 rows, 1024 x 1024: 29 us), of four 32 do.
+  t.split = 1;
+  if (t.cuts && pair && shape.groups == 1 && tiles <= 32) {
+    const int split = tiles <= 14 ? 4 : 2, sum = (shape.rows + DW_ROWS - 1) / DW_ROWS, even = (int)(sum * tiles / most);
+    if ((sum + split - 1) / split - (even > t.least ? even : t.least) <= 22) {
+      t.split = split;
+      t.cuts = false;
+    }
+  }
   return t;
 }
 
@@ -422,7 +434,7 @@ size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int o
 GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16) {
   const DwTiling t = tiling_of(act_bf16, c.shape, c.in, c.out_features);
   float* part = c.partial + 64 * ((DW_TABLE + 63) / 64);                        // behind the table
-  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, t.least, t.cuts, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int*>(c.partial)};
+  return GroupedDw{t.rows, t.tiles_in, t.tiles, t.blocks, t.least, t.split, t.cuts, part, part + (size_t)t.blocks * 2 * t.rows * t.cols, reinterpret_cast<int*>(c.partial)};
 }
 
 template <int CTAS>
@@ -448,6 +460,7 @@ static cudaError_t launch_dw(const DwMaps& m, const DwArgs& p, int units, cudaSt
 
 cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, true);
+  if (plan.split > 1) return launch_grouped_dw_few(c, plan, s);
   DwMaps m;
   DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.least, plan.cuts, c.dbias, plan.part_bias, plan.part, plan.table, c.dev_status};
   // without rows nothing is read, and any map will do

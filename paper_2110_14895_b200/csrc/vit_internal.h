@@ -226,7 +226,7 @@ int grad_clip_lists(int tensors);
 cudaError_t launch_grad_clip(const vit_tensor* tensors, int count, int index, bool clip, double* partial, int* partials, float bound,
                              float* norm, cudaStream_t s);
 
-// linear layers by group (linear_grouped_tc.cu, linear_grouped_dw.cu, linear_grouped_f32.cu)
+// linear layers by group (linear_grouped_tc.cu, linear_grouped_dw.cu, linear_grouped_dw_few.cu, linear_grouped_f32.cu)
 struct GroupedShape { int groups, rows; const int32_t* offsets; };      // offsets: nullptr for one group of all rows
 struct GroupedCall {
   GroupedShape shape;
@@ -249,9 +249,10 @@ cudaError_t launch_grouped_rows_bf16(const GroupedCall& c, cudaStream_t s);
 cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s);
 // weight gradients: blocks share all work equally and leave the sums of cut tiles in `partial`, a second kernel joins them
 size_t grouped_dw_floats(bool act_bf16, const GroupedShape& shape, int in, int out_features);
-struct GroupedDw { int rows, tiles_in, tiles, blocks, least; bool cuts; float *part, *part_bias; int* table; };        // [blocks][2] tiles and rows of them; shares
+struct GroupedDw { int rows, tiles_in, tiles, blocks, least, split; bool cuts; float *part, *part_bias; int* table; };        // [blocks][2] tiles and rows of them; shares
 GroupedDw grouped_dw_plan(const GroupedCall& c, bool act_bf16);
 cudaError_t launch_grouped_dw_bf16(const GroupedCall& c, cudaStream_t s);
+cudaError_t launch_grouped_dw_few(const GroupedCall& c, const GroupedDw& plan, cudaStream_t s);
 cudaError_t launch_grouped_dw_f32(const GroupedCall& c, cudaStream_t s);
 cudaError_t launch_grouped_join(const GroupedCall& c, bool act_bf16, cudaStream_t s);
 

@@ -534,6 +534,16 @@ def test_linear_grouped_weight_grads(ctx, lengths, before, behind, k, n, dtype):
     assert torch.equal(l.weight_grads(x, dout)[1], db)
 
 
+# one long sum of few tiles of 256 x 256 is shared by clusters: two and four pairs to a tile, tiles that hang over either edge, a
+# last unit of rows that is not full, pairs without rows, and more tiles or units than clusters take
+@pytest.mark.parametrize("length,before,behind,k,n", [
+    (577, 0, 0, 264, 512), (1091, 3, 70, 776, 520), (520, 0, 130, 1000, 1000), (2000, 0, 0, 512, 1792), (2000, 0, 0, 1032, 1024),
+    (64, 5, 900, 128, 1024), (1, 0, 600, 256, 512), (0, 300, 300, 256, 512), (6304, 1, 0, 1280, 1272), (1600, 0, 16, 2056, 1024),
+    (12608, 0, 0, 192, 768)])
+def test_weight_grads_of_one_group(ctx, length, before, behind, k, n):
+    test_linear_grouped_weight_grads(ctx, [length], before, behind, k, n, torch.bfloat16)
+
+
 @BOTH
 def test_linear_without_offsets_is_one_group(ctx, dtype):
     vit, m = ctx
