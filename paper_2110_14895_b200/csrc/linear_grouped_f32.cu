@@ -1,8 +1,9 @@
 // Linear layers by group in the fp32 mode, on the fp32 pipes: rows times their group's weights forwards and backwards, and the
-// weights' gradients.  Tiles of the result in registers, 16 of the summed index at a time through shared memory, the next 16
-// under way while these are multiplied; two products to an instruction (packed fp32).
-// 128 x 128 tiles where there are enough of them to go round, else 64 x 64, whose sums are shared by a cluster of blocks and
-// joined in its shared memory as long as blocks are left over.
+// weights' gradients.  Tiles of the result in registers, 16 of the summed index at a time through shared memory, the next
+// pieces under way while these are multiplied; two products to an instruction (packed fp32).
+// Tiles of 128 x 128 or 64 x 64, whose sums can be shared by a cluster of blocks and are joined in its shared memory (cycles_of).
+// 8224 rows, 1280 x 1280: 606 us (44 TFLOP/s), the fp32 pipe active 70 % of the time and issue limited by it; 577 rows of 4 groups,
+// 768 to 192: 14 us.  Weights' gradients of 25216 rows, 768 x 192: 215 us, the pipe active 75 %.
 #include "linear_grouped.cuh"
 
 namespace vit {
@@ -11,61 +12,104 @@ namespace {
 
 constexpr int KS = 16, THREADS = 256, WIDE = 128, SMALL = 64;
 
-// A T x 16 piece of an operand in registers: float4 i of a thread.  `base` is the operand's first value of the tile; valid: its
-// rows (or, ACROSS, columns) that exist; left: of the summed index.  ACROSS: the summed index runs over rows of memory.
-template <int T, bool ACROSS>
-__device__ __forceinline__ void fetch(float4 (&v)[T / 64], const float* base, int64_t ld, int valid, int left) {
-#pragma unroll
-  for (int i = 0; i < T / 64; ++i) {
-    const int at = (int)threadIdx.x + THREADS * i;
-    const int t = ACROSS ? at % (T / 4) * 4 : at / 4, k = ACROSS ? at / (T / 4) : at % 4 * 4;
-    v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (t < valid && k < left) v[i] = *reinterpret_cast<const float4*>(base + (ACROSS ? k * ld + t : t * ld + k));
-  }
+// T x 16 pieces of both operands, the summed index across rows, in a ring in shared memory.
+template <int T> struct Ring {
+  static constexpr int STAGES = T == WIDE ? 4 : 6, LD = T + 4, PIECE = KS * LD, BYTES = STAGES * 2 * PIECE * 4;
+};
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src, uint32_t src_bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
 }
+// A thread's copies of a piece.  `base` is the operand's first value of it; valid: the tile's rows (or, ACROSS, columns) that
+// exist; left: of the summed index; what does not exist is zero.  ACROSS: the summed index runs over rows of memory.  Else values
+// are copied one by one, by a warp 4 rows of 8, which meet all banks.
 template <int T, bool ACROSS>
-__device__ __forceinline__ void keep(const float4 (&v)[T / 64], float (*to)[T + 4]) {
+__device__ __forceinline__ void fetch(float* to, const float* base, int64_t ld, int valid, int left) {
+  const uint32_t piece = ptx::smem_u32(to);
+  if (ACROSS) {
 #pragma unroll
-  for (int i = 0; i < T / 64; ++i) {
-    const int at = (int)threadIdx.x + THREADS * i;
-    if (ACROSS) *reinterpret_cast<float4*>(&to[at / (T / 4)][at % (T / 4) * 4]) = v[i];
-    else {
-      const int t = at / 4, k = at % 4 * 4;
-      to[k][t] = v[i].x;
-      to[k + 1][t] = v[i].y;
-      to[k + 2][t] = v[i].z;
-      to[k + 3][t] = v[i].w;
+    for (int i = 0; i < T / 64; ++i) {
+      const int at = (int)threadIdx.x + THREADS * i, t = at % (T / 4) * 4, k = at / (T / 4);
+      const bool there = t < valid && k < left;
+      ptx::cp_async_16(piece + (uint32_t)(k * Ring<T>::LD + t) * 4, there ? base + (int64_t)k * ld + t : base, there ? 16u : 0u);
     }
+  } else {
+    const int t0 = (int)threadIdx.x / 8, k0 = (int)threadIdx.x % 8;
+#pragma unroll
+    for (int i = 0; i < T / 32; ++i)
+#pragma unroll
+      for (int j = 0; j < KS / 8; ++j) {
+        const int t = t0 + 32 * i, k = k0 + 8 * j;
+        const bool there = t < valid && k < left;
+        cp_async_4(piece + (uint32_t)(k * Ring<T>::LD + t) * 4, there ? base + (int64_t)t * ld + k : base, there ? 4u : 0u);
+      }
   }
 }
 
+// Where a thread's values of a tile lie.  A warp has 8 by 4 threads, and neighbouring lanes share columns: its reads of 16 bytes
+// are then served for half a warp at a time (64 x 64 tiles take 0.86 of the time of rows of 16 threads).
+__device__ __forceinline__ int thread_x() { return (threadIdx.x >> 5 & 1) * 8 + (threadIdx.x >> 1 & 7); }
+__device__ __forceinline__ int thread_y() { return (threadIdx.x >> 6) * 4 + (threadIdx.x >> 4 & 1) * 2 + (threadIdx.x & 1); }
 // A thread's values of a tile: rows 4 ty + r and T / 2 + 4 ty + r, columns alike (T = 128); 4 by 4 of them (T = 64).
 template <int T> struct Tile { float2 v[T / 16][T / 32]; };
 template <int T> __device__ __forceinline__ int part_at(int i, int t) { return T == WIDE ? (i / 4) * 64 + 4 * t + i % 4 : 4 * t + i; }
 
+// what the next of the summed index needs is read while this one's is multiplied
 template <int T>
 __device__ __forceinline__ void multiply(Tile<T>& acc, const float (*a)[T + 4], const float (*b)[T + 4]) {
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-#pragma unroll
-  for (int k = 0; k < KS; ++k) {
-    float x[T / 16];
-    float2 y[T / 32];
+  const int tx = thread_x(), ty = thread_y();
+  float4 x[2][T / 64], y[2][T / 64];
+  auto read = [&](int k) {
 #pragma unroll
     for (int h = 0; h < T / 64; ++h) {
-      const float4 f = *reinterpret_cast<const float4*>(&a[k][64 * h + 4 * ty]), g = *reinterpret_cast<const float4*>(&b[k][64 * h + 4 * tx]);
-      x[4 * h] = f.x; x[4 * h + 1] = f.y; x[4 * h + 2] = f.z; x[4 * h + 3] = f.w;
-      y[2 * h] = make_float2(g.x, g.y); y[2 * h + 1] = make_float2(g.z, g.w);
+      x[k & 1][h] = *reinterpret_cast<const float4*>(&a[k][64 * h + 4 * ty]);
+      y[k & 1][h] = *reinterpret_cast<const float4*>(&b[k][64 * h + 4 * tx]);
     }
+  };
+  read(0);
 #pragma unroll
-    for (int i = 0; i < T / 16; ++i)
+  for (int k = 0; k < KS; ++k) {
+    if (k + 1 < KS) read(k + 1);
 #pragma unroll
-      for (int j = 0; j < T / 32; ++j) acc.v[i][j] = __ffma2_rn(make_float2(x[i], x[i]), y[j], acc.v[i][j]);
+    for (int i = 0; i < T / 16; ++i) {
+      const float4 f = x[k & 1][i / 4];
+      const float v = i % 4 == 0 ? f.x : i % 4 == 1 ? f.y : i % 4 == 2 ? f.z : f.w;
+#pragma unroll
+      for (int h = 0; h < T / 64; ++h) {
+        acc.v[i][2 * h] = __ffma2_rn(make_float2(v, v), make_float2(y[k & 1][h].x, y[k & 1][h].y), acc.v[i][2 * h]);
+        acc.v[i][2 * h + 1] = __ffma2_rn(make_float2(v, v), make_float2(y[k & 1][h].z, y[k & 1][h].w), acc.v[i][2 * h + 1]);
+      }
+    }
+  }
+}
+
+// A tile's sum over `steps` pieces.  get(s, a, b): the copies of piece s; also(a): what else is done with it.
+template <int T, typename Get, typename Also>
+__device__ __forceinline__ void sum_pieces(Tile<T>& acc, float* ring, int steps, Get get, Also also) {
+  using R = Ring<T>;
+  __syncthreads();                                     // nobody reads the ring any more
+#pragma unroll
+  for (int s = 0; s < R::STAGES - 1; ++s) {
+    if (s < steps) get(s, ring + s * 2 * R::PIECE, ring + (s * 2 + 1) * R::PIECE);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  int now = 0, next = R::STAGES - 1;
+  for (int s = 0; s < steps; ++s) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(R::STAGES - 2) : "memory");
+    __syncthreads();                                   // all threads' copies have landed, and piece s - 1 has been multiplied
+    if (s + R::STAGES - 1 < steps) get(s + R::STAGES - 1, ring + next * 2 * R::PIECE, ring + (next * 2 + 1) * R::PIECE);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const auto a = reinterpret_cast<const float(*)[R::LD]>(ring + now * 2 * R::PIECE), b = a + KS;
+    multiply<T>(acc, a, b);
+    also(a);
+    if (++now == R::STAGES) now = 0;
+    if (++next == R::STAGES) next = 0;
   }
 }
 
 struct RowsArgs {
   GroupedShape shape;
   int width, sum, epilogue, tiles_n, split;
+  bool early;                          // the next kernel may be launched at once
   const float *x, *w, *bias, *residual;
   float *pre, *y;
   int64_t ldx, ldr, ldp, ldy;
@@ -105,22 +149,19 @@ __device__ __forceinline__ float4 read_cluster(const float* here, uint32_t rank)
   return v;
 }
 
-template <int T> union Stages {
-  struct { float a[2][KS][T + 4], b[2][KS][T + 4]; } s;
-  float sums[T == SMALL ? T : 1][T + 4];               // a block's part of a tile whose sums are shared
-};
-
 template <int T, bool BACKWARD>
 __global__ void __launch_bounds__(THREADS, T == WIDE ? 2 : 4)
 grouped_rows_f32_kernel(const RowsArgs p) {
-  __shared__ __align__(16) Stages<T> mem;
-  auto &a = mem.s.a, &b = mem.s.b;
-  const int lane = threadIdx.x & 31, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int split = T == SMALL ? p.split : 1, self = (int)blockIdx.x / split, units = (int)gridDim.x / split;
+  extern __shared__ __align__(16) float ring[];         // and a block's part of a tile whose sums are shared
+  const int lane = threadIdx.x & 31, tx = thread_x(), ty = thread_y();
+  const int split = p.split, self = (int)blockIdx.x / split, units = (int)gridDim.x / split;
   const uint32_t rank = blockIdx.x % split;            // in the cluster that shares a tile's sums
   const int share = (p.sum + KS * split - 1) / (KS * split) * KS, k_begin = (int)rank * share, k_end = min(p.sum, k_begin + share);
   ptx::grid_dependency_wait();
-  ptx::grid_launch_dependents();
+  // The next kernel's blocks take the places that are left: where there are some, or come one by one, the first to come would
+  // crowd on a few SMs (kernels of their kind one after the other: 2000 rows, 768 x 768, 84 us, 108 if launched at once; 5300
+  // rows, 576 x 520, 90 and 121).  Whole sums on all places are better off (4000 rows, 1024 x 4096: 759 us, 855 launched late).
+  if (p.early) ptx::grid_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
   GroupWalk<TileCount> walk(p.shape, TileCount{T, p.tiles_n}, lane);
   GroupAt at;
@@ -132,27 +173,13 @@ grouped_rows_f32_kernel(const RowsArgs p) {
     const float* w = p.w + (int64_t)at.group * p.width * p.sum + (BACKWARD ? (int64_t)col0 : (int64_t)col0 * p.sum);
     const int64_t ldw = BACKWARD ? p.width : p.sum;
     Tile<T> acc = {};
-    float4 va[T / 64], vb[T / 64];
-    auto get = [&](int k) {
-      fetch<T, false>(va, x + k, p.ldx, rows, k_end - k);
-      fetch<T, BACKWARD>(vb, w + (BACKWARD ? (int64_t)k * ldw : (int64_t)k), ldw, cols, k_end - k);
-    };
-    get(k_begin);
-    __syncthreads();                                    // the tile before has been multiplied
-    keep<T, false>(va, a[0]);
-    keep<T, BACKWARD>(vb, b[0]);
-    __syncthreads();
-    int now = 0;
-    for (int k = k_begin; k < k_end; k += KS, now ^= 1) {
-      const bool more = k + KS < k_end;
-      if (more) get(k + KS);
-      multiply<T>(acc, a[now], b[now]);
-      if (more) {
-        keep<T, false>(va, a[now ^ 1]);
-        keep<T, BACKWARD>(vb, b[now ^ 1]);
-      }
-      __syncthreads();
-    }
+    sum_pieces<T>(acc, ring, (k_end - k_begin + KS - 1) / KS,
+                  [&](int s, float* a, float* b) {
+                    const int k = k_begin + s * KS;
+                    fetch<T, false>(a, x + k, p.ldx, rows, k_end - k);
+                    fetch<T, BACKWARD>(b, w + (BACKWARD ? (int64_t)k * ldw : (int64_t)k), ldw, cols, k_end - k);
+                  },
+                  [](const float(*)[T + 4]) {});
     if (split == 1) {
 #pragma unroll
       for (int i = 0; i < T / 16; ++i) {
@@ -165,16 +192,21 @@ grouped_rows_f32_kernel(const RowsArgs p) {
             finish<BACKWARD>(p, at.group, row, c, make_float4(acc.v[i][2 * h].x, acc.v[i][2 * h].y, acc.v[i][2 * h + 1].x, acc.v[i][2 * h + 1].y));
         }
       }
-    } else if (T == SMALL) {
+    } else {
       // every block leaves its part where the others can read it, and finishes some of the rows
+      __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(&mem.sums[(4 * ty + i) % (T == SMALL ? T : 1)][4 * tx]) = make_float4(acc.v[i][0].x, acc.v[i][0].y, acc.v[i][1].x, acc.v[i][1].y);
+      for (int i = 0; i < T / 16; ++i)
+#pragma unroll
+        for (int h = 0; h < T / 64; ++h)
+          *reinterpret_cast<float4*>(&ring[part_at<T>(i, ty) * (T + 4) + 64 * h + 4 * tx]) =
+              make_float4(acc.v[i][2 * h].x, acc.v[i][2 * h].y, acc.v[i][2 * h + 1].x, acc.v[i][2 * h + 1].y);
       ptx::cluster_sync();
-      for (int i = threadIdx.x; i < T / split * 16; i += THREADS) {
-        const int r = (int)rank * (T / split) + i / 16, c = i % 16 * 4;
+      const int first = (int)rank * T / split, count = ((int)rank + 1) * T / split - first;
+      for (int i = threadIdx.x; i < count * (T / 4); i += THREADS) {
+        const int r = first + i / (T / 4), c = i % (T / 4) * 4;
         if (row0 + r >= at.end || col0 + c >= p.width) continue;
-        const float* from = &mem.sums[r % (T == SMALL ? T : 1)][c];
+        const float* from = &ring[r * (T + 4) + c];
         float4 sum = read_cluster(from, 0);
         for (int k = 1; k < split; ++k) {
           const float4 v = read_cluster(from, (uint32_t)k);
@@ -200,12 +232,12 @@ struct DwArgs {
 __global__ void __launch_bounds__(THREADS, 2)
 grouped_dw_f32_kernel(const DwArgs p) {
   constexpr int T = WIDE;
-  __shared__ __align__(16) float a[2][KS][T + 4], b[2][KS][T + 4];
-  const int lane = threadIdx.x & 31, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  extern __shared__ __align__(16) float ring[];
+  const int lane = threadIdx.x & 31, tx = thread_x(), ty = thread_y();
   ptx::grid_dependency_wait();
   ptx::grid_launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x < 32) report_bad_groups(p.shape, p.dev_status, lane);
-  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, p.least, p.cuts, reinterpret_cast<int*>(&a[0][0][0]), p.table);
+  const Share share = find_share(p.shape, p.tiles, (int)gridDim.x, (int)blockIdx.x, p.least, p.cuts, reinterpret_cast<int*>(ring), p.table);
   __syncthreads();
   PartWalk work(p.shape, p.tiles, lane, share, (int)blockIdx.x, (int)gridDim.x);
   Part part;
@@ -217,33 +249,19 @@ grouped_dw_f32_kernel(const DwArgs p) {
     Tile<T> acc = {};
     float bias = 0.f;
     const bool sums = p.dbias && k0 == 0 && threadIdx.x < T;
-    float4 va[2], vb[2];
-    fetch<T, true>(va, d, p.lddout, p.out - n0, rows);
-    fetch<T, true>(vb, x, p.ldx, p.in - k0, rows);
-    __syncthreads();
-    keep<T, true>(va, a[0]);
-    keep<T, true>(vb, b[0]);
-    __syncthreads();
-    int now = 0;
-    for (int r = 0; r < rows; r += KS, now ^= 1) {
-      const bool more = r + KS < rows;
-      if (more) {
-        fetch<T, true>(va, d + (int64_t)(r + KS) * p.lddout, p.lddout, p.out - n0, rows - r - KS);
-        fetch<T, true>(vb, x + (int64_t)(r + KS) * p.ldx, p.ldx, p.in - k0, rows - r - KS);
-      }
-      multiply<T>(acc, a[now], b[now]);
-      if (sums) {
-        float some = 0.f;
+    sum_pieces<T>(acc, ring, (rows + KS - 1) / KS,
+                  [&](int s, float* a, float* b) {
+                    const int r = s * KS;
+                    fetch<T, true>(a, d + (int64_t)r * p.lddout, p.lddout, p.out - n0, rows - r);
+                    fetch<T, true>(b, x + (int64_t)r * p.ldx, p.ldx, p.in - k0, rows - r);
+                  },
+                  [&](const float(*a)[T + 4]) {
+                    if (!sums) return;
+                    float some = 0.f;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) some += a[now][k][threadIdx.x];
-        bias += some;
-      }
-      if (more) {
-        keep<T, true>(va, a[now ^ 1]);
-        keep<T, true>(vb, b[now ^ 1]);
-      }
-      __syncthreads();
-    }
+                    for (int k = 0; k < KS; ++k) some += a[k][threadIdx.x];
+                    bias += some;
+                  });
     const bool whole = part.whole();
     const int64_t slot = (int64_t)blockIdx.x * 2 + part.slot();
 #pragma unroll
@@ -261,9 +279,11 @@ grouped_dw_f32_kernel(const DwArgs p) {
   }
 }
 
-template <typename Kernel, typename Args>
-cudaError_t launch_after(Kernel kernel, int grid, const Args& args, cudaStream_t s, int cluster = 1) {
+template <int T, typename Kernel, typename Args>
+cudaError_t launch_after(PerDeviceFlag& configured, Kernel kernel, int grid, const Args& args, cudaStream_t s, int cluster = 1) {
+  if (cudaError_t e = ensure_dynamic_smem(configured, kernel, Ring<T>::BYTES)) return e;
   cudaLaunchConfig_t cfg = {};
+  cfg.dynamicSmemBytes = Ring<T>::BYTES;
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(THREADS);
   cfg.stream = s;
@@ -289,29 +309,67 @@ cudaError_t launch_check_groups(const GroupedCall& c, cudaStream_t s) {
   return cudaGetLastError();
 }
 
+// Tiles at a time: two or four blocks to an SM; clusters do not find all places (71 of four and 33 of eight blocks of 128 x 128, 142
+// and 71 of 64 x 64, by the occupancy calculator).
+static int units_of(bool wide, int split, int sms) {
+  const int all = sms * (wide ? 2 : 4) / split;
+  return split < 4 ? all : split == 8 && wide ? all * 9 / 10 : all * 24 / 25;
+}
+// About what the products of rows take, in cycles.  A round of blocks takes, for 16 of the sum, `piece` with one to four of them
+// on an SM, and what starts and ends a tile, more so between rounds.  Measured with either tile and 1 to 8 blocks to a sum at 23
+// shapes: the choice is the best or within 7 % of it (577 rows, 768 x 768: 28 us with 128 x 128 tiles in eighths, 33 with 64 x 64;
+// 197 rows, 768 x 192: 9 us with 64 x 64 in eighths, 17 with 128 x 128; 8224 rows, 1280 x 1280: 606 us in halves, 652 whole).
+static double cycles_of(bool wide, int split, const GroupedShape& shape, int width, int sum, int sms) {
+  constexpr double PIECE[2][4] = {{1085., 1900., 2900., 3900.}, {2950., 5330., 0., 0.}};
+  const int t = wide ? WIDE : SMALL, places = wide ? 2 : 4;
+  // groups end somewhere in a tile, and those with rows have one
+  const int64_t some = shape.groups < shape.rows ? shape.groups : shape.rows, row_tiles = (2 * (int64_t)shape.rows + some * t) / (2 * t);
+  const int64_t down = some == 1 ? (shape.rows + t - 1) / t : row_tiles > some ? row_tiles : some, tiles = down * ((width + t - 1) / t);
+  const int64_t units = units_of(wide, split, sms), rounds = tiles / units, last = tiles - rounds * units;
+  const double pieces = (sum + KS * split - 1) / (KS * split);
+  const double end = wide ? (split == 1 ? 9000. : 11500.) : 5500. + 600. * split;
+  const double between = !wide ? end : split == 1 ? 12000. : split == 2 ? 15000. : split == 4 ? 28000. : 50000.;
+  double cycles = rounds * (pieces * PIECE[wide][places - 1] + between);
+  if (last == 0) return cycles - (rounds > 0 ? between - end : 0.);
+  // clusters do not spread evenly over the SMs by themselves
+  const int64_t blocks = last * split * (rounds == 0 && split > 1 ? 23 : 20) / 20, on_sm = (blocks + sms - 1) / sms;
+  return cycles + pieces * PIECE[wide][(on_sm < places ? on_sm : places) - 1] + end;
+}
 cudaError_t launch_grouped_rows_f32(const GroupedCall& c, cudaStream_t s) {
-  RowsArgs p{c.shape, c.backward ? c.in : c.out_features, c.backward ? c.out_features : c.in, c.epilogue, 0, 1, static_cast<const float*>(c.x),
+  RowsArgs p{c.shape, c.backward ? c.in : c.out_features, c.backward ? c.out_features : c.in, c.epilogue, 0, 1, false, static_cast<const float*>(c.x),
              static_cast<const float*>(c.w), c.bias, static_cast<const float*>(c.residual), static_cast<float*>(c.pre), static_cast<float*>(c.y),
              c.ldx, c.ldr, c.ldp, c.ldy, c.dev_status};
   const int sms = current_device_sm_count();
-  auto tiles = [&](int t) { return ((int64_t)c.shape.rows / t + c.shape.groups) * ((p.width + t - 1) / t); };
-  const bool wide = tiles(WIDE) >= 2 * (int64_t)sms;
-  const int t = wide ? WIDE : SMALL;
+  if (sms < 1) return cudaErrorInvalidDevice;
+  bool wide = false;
+  double best = 0.;
+  for (int t = SMALL; t <= WIDE; t += SMALL)
+    for (int split = 1; split <= 8 && (split == 1 || p.sum >= 2 * KS * split); split *= 2) {
+      const double cycles = cycles_of(t == WIDE, split, c.shape, p.width, p.sum, sms);
+      if (best > 0. && cycles >= best) continue;
+      best = cycles;
+      wide = t == WIDE;
+      p.split = split;
+    }
+  const int t = wide ? WIDE : SMALL, units = units_of(wide, p.split, sms);
   p.tiles_n = (p.width + t - 1) / t;
-  // at least 64 of a sum to a block, and no more blocks than run at once
-  if (!wide)
-    while (p.split < 8 && tiles(t) * p.split * 2 <= (int64_t)sms * 2 && p.sum >= 128 * p.split) p.split *= 2;
-  const int64_t most = (int64_t)sms * (wide ? 2 : 4);
-  const int grid = (int)(tiles(t) < most ? tiles(t) : most) * p.split;
-  if (c.backward) return wide ? launch_after(grouped_rows_f32_kernel<WIDE, true>, grid, p, s) : launch_after(grouped_rows_f32_kernel<SMALL, true>, grid, p, s, p.split);
-  return wide ? launch_after(grouped_rows_f32_kernel<WIDE, false>, grid, p, s) : launch_after(grouped_rows_f32_kernel<SMALL, false>, grid, p, s, p.split);
+  const int64_t most = ((int64_t)c.shape.rows / t + c.shape.groups) * p.tiles_n;      // tiles
+  p.early = wide && p.split == 1 && most >= units;
+  const int grid = (int)(most < units ? most : units) * p.split;
+  static PerDeviceFlag configured[4];
+  if (c.backward)
+    return wide ? launch_after<WIDE>(configured[0], grouped_rows_f32_kernel<WIDE, true>, grid, p, s, p.split)
+                : launch_after<SMALL>(configured[1], grouped_rows_f32_kernel<SMALL, true>, grid, p, s, p.split);
+  return wide ? launch_after<WIDE>(configured[2], grouped_rows_f32_kernel<WIDE, false>, grid, p, s, p.split)
+              : launch_after<SMALL>(configured[3], grouped_rows_f32_kernel<SMALL, false>, grid, p, s, p.split);
 }
 
 cudaError_t launch_grouped_dw_f32(const GroupedCall& c, cudaStream_t s) {
   const GroupedDw plan = grouped_dw_plan(c, false);
   const DwArgs p{c.shape, c.in, c.out_features, plan.tiles_in, plan.tiles, plan.least, plan.cuts, static_cast<const float*>(c.x), static_cast<const float*>(c.dout),
                  c.ldx, c.lddout, static_cast<float*>(c.dw), c.dbias, plan.part, plan.part_bias, plan.table, c.dev_status};
-  return launch_after(grouped_dw_f32_kernel, plan.blocks, p, s);
+  static PerDeviceFlag configured;
+  return launch_after<WIDE>(configured, grouped_dw_f32_kernel, plan.blocks, p, s);
 }
 
 }  // namespace vit

@@ -544,6 +544,16 @@ def test_weight_grads_of_one_group(ctx, length, before, behind, k, n):
     test_linear_grouped_weight_grads(ctx, [length], before, behind, k, n, torch.bfloat16)
 
 
+# either tile of the fp32 products of rows, whole and with its sum in halves, quarters and eighths, in one round and in several
+@pytest.mark.parametrize("lengths,before,behind,k,n", [
+    ([577], 0, 0, 768, 768), ([2000], 0, 0, 768, 768), ([333, 333, 334], 0, 7, 1000, 1000), ([33] * 30, 2, 0, 768, 768), ([25] * 8, 0, 0, 384, 1536),
+    ([481], 3, 9, 2952, 368), ([1325] * 4, 0, 0, 576, 520), ([1, 300, 0, 299], 0, 0, 136, 2056), ([4] * 16, 0, 0, 2048, 512), ([3152], 0, 0, 192, 192)],
+    ids=lambda v: "%dx%d" % (len(v), max(v)) if isinstance(v, list) else str(v))
+def test_linear_grouped_fp32_tiles(ctx, lengths, before, behind, k, n):
+    test_linear_grouped(ctx, lengths, before, behind, k, n, torch.float32)
+    test_linear_grouped_input_grad(ctx, lengths, before, behind, k, n, torch.float32)
+
+
 @BOTH
 def test_linear_without_offsets_is_one_group(ctx, dtype):
     vit, m = ctx
