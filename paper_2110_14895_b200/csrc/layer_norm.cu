@@ -213,8 +213,8 @@ layer_norm_backward_kernel(const BackwardArgs p) {
     for (int e = 0; e < 4; ++e) dg[i][e] = db[i][e] = make_float2(0.f, 0.f);
   const float inv = 1.0f / (float)p.cols;
   int64_t row = (int64_t)blockIdx.x * (WARPS / WPR) + warp / WPR;
+  // (the next kernel launched at once would crowd here: 3152 rows of 768, both kernels, 8.7 us for 7.9)
   ptx::grid_dependency_wait();
-  ptx::grid_launch_dependents();
   for (int s = 0; s < p.stages - 1; ++s) fetch(row + s * step, s);
   for (int i = 4 * threadIdx.x; i < p.cols; i += WARPS * 128) *reinterpret_cast<float4*>(gain + i) = *reinterpret_cast<const float4*>(p.gain + i);
   __syncthreads();
