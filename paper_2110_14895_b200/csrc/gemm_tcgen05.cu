@@ -251,7 +251,8 @@ linear_tc_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
       if (*abort_flag) {
         // products issued so far retire before tensor memory is freed
         volatile int never = 0;
-        umma_commit(smem_u32(drain_bar));
+        if (CTAS == 2) umma_commit_pair_here(smem_u32(drain_bar));
+        else umma_commit(smem_u32(drain_bar));
         mbar_wait_limit(smem_u32(drain_bar), 0, &never, DRAIN_LIMIT_CYCLES);
       }
     }

@@ -164,7 +164,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         __syncwarp();
         if (++buf == 2) { buf = 0; aphase ^= 1; }
       }
-      if (*abort_flag) drain_products(drain);
+      if (*abort_flag) drain_products<CTAS>(drain);
     }
   } else if (warp == 2 + EPI_WARPS + SUM_WARPS) {
     // ---------------------------------------------------------------- stages that have landed are handed on

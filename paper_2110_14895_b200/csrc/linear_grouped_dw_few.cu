@@ -261,7 +261,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
 
   if (*abort_flag) {
     if (warp == 0) drain_stages(full, STAGES, fills);
-    if (warp == 1 && rank == 0) drain_products(drain);
+    if (warp == 1 && rank == 0) drain_products<2>(drain);
     // the partner may be in a wait of its own that nothing will satisfy any more
     if (threadIdx.x == 0)
       asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_cta(smem_u32(const_cast<int*>(abort_flag)), place ^ 1u)), "r"(1) : "memory");

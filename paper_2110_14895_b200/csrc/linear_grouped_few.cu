@@ -197,7 +197,7 @@ grouped_few_kernel(const __grid_constant__ FewMaps m, const __grid_constant__ Fe
 
   if (*abort_flag) {
     if (warp == 0) drain_stages(full, STAGES, fills);
-    if (warp == 1) drain_products(drain);
+    if (warp == 1) drain_products<1>(drain);
   }
   __syncwarp();
   tc_fence_before();

@@ -166,7 +166,7 @@ grouped_rows_kernel(const __grid_constant__ RowsMaps m, const __grid_constant__ 
         __syncwarp();
         if (++buf == 2) { buf = 0; aphase ^= 1; }
       }
-      if (*abort_flag) drain_products(drain);
+      if (*abort_flag) drain_products<CTAS>(drain);
     }
   } else {
     // ---------------------------------------------------------------- epilogue

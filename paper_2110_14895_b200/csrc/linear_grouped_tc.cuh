@@ -82,11 +82,14 @@ __device__ __forceinline__ void drain_stages(uint32_t full, int stages, long lon
   for (long long f = fills > stages ? fills - stages : 0; f < fills; ++f)
     mbar_wait_limit(full + 8 * (uint32_t)(f % stages), (uint32_t)((f / stages) & 1), &never, DRAIN_LIMIT_CYCLES);
 }
-// and the products issued so far (by the thread that the hardware elects) are done before tensor memory is freed
+// and the products issued so far (by the thread that the hardware elects) are done before tensor memory is freed.  A commit
+// tracks the products of its own kind only: a pair's are committed as a pair's.
+template <int CTAS>
 __device__ __forceinline__ void drain_products(uint32_t bar) {
   volatile int never = 0;
   if (elect_one()) {
-    umma_commit(bar);
+    if (CTAS == 2) umma_commit_pair_here(bar);
+    else umma_commit(bar);
     mbar_wait_limit(bar, 0, &never, DRAIN_LIMIT_CYCLES);
   }
 }

@@ -1,0 +1,28 @@
+"""Rules of order that the kernels' sources have to keep and that no run shows when they are broken, checked in the text."""
+import pathlib
+import re
+
+import pytest
+
+SOURCES = sorted((pathlib.Path(__file__).parent.parent / "paper_2110_14895_b200" / "csrc").glob("*.cu*"))
+
+
+def _code(path):
+    return re.sub(r"//[^\n]*", "", path.read_text())
+
+
+def _statements(code, call):
+    """Everything from the end of the statement before to each call of a function by its name."""
+    return [re.split(r"[;{}]", code[:m.start()])[-1] for m in re.finditer(r"\b%s\(" % call, code)]
+
+
+@pytest.mark.parametrize("path", [p for p in SOURCES if re.search(r"umma_bf16_pair\(|product<", _code(p))], ids=lambda p: p.name)
+def test_products_of_pairs_are_committed_as_pairs(path):
+    """A commit of one block's kind need not cover the products of a pair: where those are issued it stands behind an `else`."""
+    if path.name == "sm100_ptx.cuh":
+        return                                             # (the definitions)
+    code = _code(path)
+    assert all(re.search(r"\belse\s*$", s) for s in _statements(code, "umma_commit"))
+    kinds = re.findall(r"\bdrain_products(?:<(\w+)>)?\(drain\)", code)
+    wanted = "2" if "umma_bf16_pair(" in code and "__global__" in code and "int CTAS" not in code else "CTAS"
+    assert all(k == wanted for k in kinds)
