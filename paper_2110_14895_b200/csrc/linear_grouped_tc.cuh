@@ -128,6 +128,7 @@ __device__ __forceinline__ void send_rows(const CUtensorMap* tm, bf16* out, int6
     read_chunk(w, piece, r, ck);
     if (c0 + 8 * ck < width) *reinterpret_cast<uint4*>(out + (int64_t)(row0 + r) * ld + c0 + 8 * ck) = make_uint4(w[0], w[1], w[2], w[3]);
   }
+  fence_proxy_async_smem();                                 // the next copy into the piece comes by TMA, behind these reads and writes
   __syncwarp();
 }
 

@@ -26,3 +26,21 @@ def test_products_of_pairs_are_committed_as_pairs(path):
     kinds = re.findall(r"\bdrain_products(?:<(\w+)>)?\(drain\)", code)
     wanted = "2" if "umma_bf16_pair(" in code and "__global__" in code and "int CTAS" not in code else "CTAS"
     assert all(k == wanted for k in kinds)
+
+
+def _function(code, name):
+    """The text of a function's body, without its braces."""
+    at = code.index("{", re.search(r"\b%s\([^;{]*\)\s*\{" % name, code).start())
+    depth, end = 1, at + 1
+    while depth:
+        depth += {"{": 1, "}": -1}.get(code[end], 0)
+        end += 1
+    return code[at + 1:end - 1]
+
+
+def test_pieces_sent_row_by_row_are_given_back_to_tma():
+    """A piece that ordinary stores have filled is the target of the next TMA load (residual, GELU's argument) also where it left by
+    ordinary loads: every lane has to order its accesses before the asynchronous ones, before one lane issues the copy."""
+    body = _function(_code(next(p for p in SOURCES if p.name == "linear_grouped_tc.cuh")), "send_rows")
+    rows = body[body.index("return;"):]
+    assert re.search(r"fence_proxy_async_smem\(\);\s*__syncwarp\(\);\s*$", rows)
