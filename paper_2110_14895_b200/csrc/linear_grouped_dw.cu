@@ -179,7 +179,8 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
             for (int i = rows * 8 + lane; i < (rows + 15) / 16 * 128; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + (uint32_t)(s * SLAB_BYTES + i * 16)), "r"(0u) : "memory");
           fence_proxy_async_smem();
-          if (CTAS == 2) fence_cluster();
+          __syncwarp();
+          if (CTAS == 2) fence_cluster();                // behind the other lanes' zeros
         }
         __syncwarp();
         if (lane == 0) {

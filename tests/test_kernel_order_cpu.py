@@ -44,3 +44,15 @@ def test_pieces_sent_row_by_row_are_given_back_to_tma():
     body = _function(_code(next(p for p in SOURCES if p.name == "linear_grouped_tc.cuh")), "send_rows")
     rows = body[body.index("return;"):]
     assert re.search(r"fence_proxy_async_smem\(\);\s*__syncwarp\(\);\s*$", rows)
+
+
+@pytest.mark.parametrize("name", ["linear_grouped_dw.cu", "linear_grouped_dw_few.cu"])
+def test_cleared_rows_are_ordered_before_their_stage_is_handed_on(name):
+    """All lanes write zeros and one hands the stage on to the other block: between the warp's meeting and that lane's arrival there
+    is a release at cluster scope, a fence or the arrival itself."""
+    code = _code(next(p for p in SOURCES if p.name == name))
+    behind = code[code.index('"r"(0u) : "memory");'):]
+    order = re.findall(r"fence_proxy_async_smem\(\)|__syncwarp\(\)|fence_cluster\(\)|hand_on\(|mbar_arrive_cluster\(", behind)
+    first = next(i for i, what in enumerate(order) if what in ("hand_on(", "mbar_arrive_cluster("))
+    assert order[:2] == ["fence_proxy_async_smem()", "__syncwarp()"]
+    assert order[first] == "mbar_arrive_cluster(" or "fence_cluster()" in order[2:first]
