@@ -7,11 +7,11 @@
 // slabs: shared memory then takes in and gives out 64 KB for 64 rows, in the 512 cycles of their products, where the 96 KB of
 // a single block's 128 x 256 are more than it can move.  Single blocks stay for narrow layers, where half a pair would idle.
 // The rows behind a group's end are the next group's: they are cleared in the last stage, in both operands (zero times a
-// value that is not a number would not be zero).  A warp of its own in each block sees the copies land, clears, and hands the
-// stage on to the warp that issues the products (the even block's, for both); it runs ahead of them, so that neither the
-// clearing nor the way from block to block holds them up (at 25216 rows of 16 groups 2 % of the time, with both
-// in the issuing warp's path; with a release at cluster scope in every stage twice the time).
-// Four more warps add up dout's columns for db from the same stages, where the tile is its row's first.
+// value that is not a number would not be zero).  A warp of its own in each block sees such a stage land, clears it and hands it on
+// to the warp that issues the products (the even block's, for both), with a release at cluster scope.  The copies of all other
+// stages are counted where the products wait: a release for every stage took twice the time.
+// Four more warps add up dout's columns for db from the same stages, where the tile is its row's first: in the even block beside the
+// products, in the odd one, where nothing but the products tells that the copies have landed, behind them.
 // The units of work get equal shares of it (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
 // 25216 rows of 16 groups, 1024 x 4096: 185 us (tensor pipe active 66 %); one group of 8192 rows, 4096 x 4096: 190 us (1440
 // TFLOP/s); 32896 rows, 1280 x 1280: 99 us.
@@ -50,13 +50,6 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* tm, uint32_t src
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 
-// The odd block of a pair hands a stage on.  What TMA wrote there is complete; a release at cluster scope would wait for about
-// a microsecond, so that it is left to the stages that this warp has written to itself.
-__device__ __forceinline__ void hand_on(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
-
 template <int CTAS>
 __global__ void __launch_bounds__(DW_THREADS, 1)
 grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwArgs p) {
@@ -66,9 +59,9 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t tiles = smem_u32(smem), staging = tiles + STAGES * C::STAGE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * C::STAGE_BYTES + C::STAGING_BYTES);
-  const uint32_t full = smem_u32(bars), ready = full + 8 * STAGES, empty = ready + 8 * STAGES, tfull = empty + 8 * STAGES, tempty = tfull + 16,
-                 drain = tempty + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 5);
+  const uint32_t landed = smem_u32(bars), ready = landed + 8 * STAGES, used = ready + 8 * STAGES, summed = used + 8 * STAGES,
+                 tfull = summed + 8 * STAGES, tempty = tfull + 16, drain = tempty + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * STAGES + 5);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
@@ -77,9 +70,10 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(full + 8 * i, 1);
+      mbar_init(landed + 8 * i, 1);
       mbar_init(ready + 8 * i, CTAS);                                   // a word of each block
-      mbar_init(empty + 8 * i, p.dbias ? 1 + SUM_WARPS : 1);
+      mbar_init(used + 8 * i, 1);                                       // by the products
+      mbar_init(summed + 8 * i, SUM_WARPS);                             // and, with biases, by the sums of columns
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(tfull + 8 * i, 1);
@@ -113,26 +107,32 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA producer
     long long fills = 0;
+    uint32_t tails = 0, turns = 0;
     bool ok = true;
     while (ok && work.next(part)) {
       const int n0 = part.tile / p.tiles_in * (BM * CTAS) + (int)rank * BM, k0 = part.tile % p.tiles_in * TN + (int)rank * (TN / CTAS);
       for (int kb = 0; kb < part.blocks(); ++kb) {
-        if (!warp_wait(empty + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
+        if (!warp_wait(used + 8 * stage, phase ^ 1, abort_flag) || (p.dbias && !warp_wait(summed + 8 * stage, phase ^ 1, abort_flag))) {
+          ok = false;
+          break;
+        }
         ++fills;
+        const int row = part.begin + part.unit(kb) * DW_ROWS;
+        const bool tail = has_tail(part.end - row);
+        tails = tail ? tails | 1u << stage : tails & ~(1u << stage);
+        turns ^= (tail ? 1u : 0u) << stage;
         if (lane == 0) {
-          const uint32_t sa = tiles + stage * C::STAGE_BYTES, fb = full + 8 * stage;
-          const int row = part.begin + part.unit(kb) * DW_ROWS;
-          mbar_arrive_expect_tx(fb, C::STAGE_BYTES);
+          const uint32_t sa = tiles + stage * C::STAGE_BYTES, to = announce<CTAS>(landed + 8 * stage, ready + 8 * stage, tail, rank, C::STAGE_BYTES);
 #pragma unroll
-          for (int s = 0; s < 2; ++s) tma_load_2d(sa + s * SLAB_BYTES, &m.dout, n0 + 64 * s, row, fb);
+          for (int s = 0; s < 2; ++s) load_2d<CTAS>(sa + s * SLAB_BYTES, &m.dout, n0 + 64 * s, row, to);
 #pragma unroll
-          for (int s = 0; s < C::B_SLABS; ++s) tma_load_2d(sa + C::A_BYTES + s * SLAB_BYTES, &m.x, k0 + 64 * s, row, fb);
+          for (int s = 0; s < C::B_SLABS; ++s) load_2d<CTAS>(sa + C::A_BYTES + s * SLAB_BYTES, &m.x, k0 + 64 * s, row, to);
         }
         __syncwarp();
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
     }
-    if (*abort_flag && lane == 0) drain_stages(full, STAGES, fills);
+    if (*abort_flag && lane == 0) drain_fills(landed, ready, STAGES, fills, tails, turns, rank == 0);
   } else if (warp == 1) {
     // ---------------------------------------------------------------- products
     if (rank == 0) {
@@ -146,15 +146,16 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         const uint32_t d = tmem + (uint32_t)(buf * TN);
         for (int kb = 0; kb < part.blocks(); ++kb) {
           if (!warp_wait(ready + 8 * stage, phase, abort_flag)) { ok = false; break; }
+          const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS, steps = (min(DW_ROWS, rows) + 15) / 16;
+          if (has_tail(rows)) see_cleared<CTAS>(ready + 8 * stage, phase);
           tc_fence_after();
           const uint32_t sa = uniform(tiles + stage * C::STAGE_BYTES);
-          const int steps = (min(DW_ROWS, part.end - part.begin - part.unit(kb) * DW_ROWS) + 15) / 16;
           const uint64_t ad = smem_desc(sa, SLAB_BYTES), bd = smem_desc(sa + C::A_BYTES, SLAB_BYTES);
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)                // 16 rows of 128 bytes
               if (k < steps) product<CTAS>(d, ad + (uint64_t)(128 * k), bd + (uint64_t)(128 * k), id, (kb > 0 || k > 0) ? 1u : 0u);
-            commit<CTAS>(empty + 8 * stage);
+            commit<CTAS>(used + 8 * stage);
           }
           __syncwarp();
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -167,27 +168,28 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
       if (*abort_flag) drain_products<CTAS>(drain);
     }
   } else if (warp == 2 + EPI_WARPS + SUM_WARPS) {
-    // ---------------------------------------------------------------- stages that have landed are handed on
+    // ---------------------------------------------------------------- the groups' last rows
+    uint32_t turns = 0;
     bool ok = true;
     while (ok && work.next(part)) {
       for (int kb = 0; kb < part.blocks(); ++kb) {
-        if (!warp_wait(full + 8 * stage, phase, abort_flag)) { ok = false; break; }
-        const int rows = min(DW_ROWS, part.end - part.begin - part.unit(kb) * DW_ROWS);
-        if (rows & 15) {                               // the group's last rows: the others of their 16 become zero
+        const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS;
+        if (has_tail(rows)) {                          // the others of their 16 become zero
+          if (!warp_wait(landed + 8 * stage, turns >> stage & 1, abort_flag)) { ok = false; break; }
+          turns ^= 1u << stage;
           const uint32_t sa = tiles + stage * C::STAGE_BYTES;
           for (int s = 0; s < 2 + C::B_SLABS; ++s)
             for (int i = rows * 8 + lane; i < (rows + 15) / 16 * 128; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + (uint32_t)(s * SLAB_BYTES + i * 16)), "r"(0u) : "memory");
           fence_proxy_async_smem();
           __syncwarp();
-          if (CTAS == 2) fence_cluster();                // behind the other lanes' zeros
+          if (lane == 0) {
+            if (CTAS == 2) mbar_arrive_cluster(map_to_cta(ready + 8 * stage, 0));
+            else mbar_arrive(ready + 8 * stage);
+          }
+          __syncwarp();
         }
-        __syncwarp();
-        if (lane == 0) {
-          if (CTAS == 2) hand_on(map_to_cta(ready + 8 * stage, 0));
-          else mbar_arrive(ready + 8 * stage);
-        }
-        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        if (++stage == STAGES) stage = 0;
       }
     }
   } else if (warp < 2 + EPI_WARPS) {
@@ -246,12 +248,13 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     // ---------------------------------------------------------------- sums of dout's columns
     // a warp has 32 columns; a lane 8 of them and every eighth row, such that eight lanes meet all banks
     const int sw = warp - 2 - EPI_WARPS, slab = sw >> 1, ck = (sw & 1) * 4 + (lane & 3), first = (lane >> 3) | (lane & 4);
+    const uint32_t there = rank == 0 ? ready : used;
     bool ok = true;
     while (ok && work.next(part)) {
       const bool mine = part.tile % p.tiles_in == 0;
       float2 sum[4] = {};
       for (int kb = 0; kb < part.blocks(); ++kb) {
-        if (!warp_wait(full + 8 * stage, phase, abort_flag)) { ok = false; break; }
+        if (!warp_wait(there + 8 * stage, phase, abort_flag)) { ok = false; break; }
         if (mine) {
           const uint32_t from = tiles + stage * C::STAGE_BYTES + slab * SLAB_BYTES;
           const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS;
@@ -270,7 +273,7 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
           for (int e = 0; e < 4; ++e) sum[e] = __fadd2_rn(sum[e], some[e]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(empty + 8 * stage);
+        if (lane == 0) mbar_arrive(summed + 8 * stage);
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
       if (!ok || !mine) continue;

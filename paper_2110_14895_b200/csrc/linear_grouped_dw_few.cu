@@ -44,11 +44,6 @@ __device__ __forceinline__ void commit_to(uint32_t bar, uint32_t even) {
       "h"((uint16_t)(3u << even))
       : "memory");
 }
-// (without a release, as in linear_grouped_dw.cu)
-__device__ __forceinline__ void hand_on(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ void fence_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
 __global__ void __launch_bounds__(THREADS, 1)
 grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant__ DwFewArgs p) {
@@ -56,8 +51,9 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t tiles = smem_u32(smem);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES);
-  const uint32_t full = smem_u32(bars), ready = full + 8 * STAGES, empty = ready + 8 * STAGES, done = empty + 8 * STAGES, drain = done + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 3 * STAGES + 2);
+  const uint32_t landed = smem_u32(bars), ready = landed + 8 * STAGES, used = ready + 8 * STAGES, summed = used + 8 * STAGES,
+                 done = summed + 8 * STAGES, drain = done + 8;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * STAGES + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const uint32_t bias_sums = tiles + STAGES * STAGE_BYTES + 512;                             // [128] floats
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -67,9 +63,10 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
   if (threadIdx.x == 0) {
     *abort_flag = 0;
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(full + 8 * i, 1);
+      mbar_init(landed + 8 * i, 1);
       mbar_init(ready + 8 * i, 2);
-      mbar_init(empty + 8 * i, p.dbias ? 1 + SUM_WARPS : 1);
+      mbar_init(used + 8 * i, 1);
+      mbar_init(summed + 8 * i, SUM_WARPS);
     }
     mbar_init(done, 1);
     mbar_init(drain, 1);
@@ -89,7 +86,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
 
   int begin, end;
   int stage = 0;
-  uint32_t phase = 0;
+  uint32_t phase = 0, tails = 0, turns = 0;
   long long fills = 0;
   if (group_rows(p.shape, 0, begin, end)) {
     const int n0 = tile / p.tiles_in * (2 * BM) + (int)rank * BM, kt = tile % p.tiles_in, k0 = kt * TN;
@@ -98,16 +95,18 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
     if (warp == 0) {
       // ---------------------------------------------------------------- TMA producer
       for (int kb = from; kb < to; ++kb) {
-        if (!warp_wait(empty + 8 * stage, phase ^ 1, abort_flag)) break;
+        if (!warp_wait(used + 8 * stage, phase ^ 1, abort_flag) || (p.dbias && !warp_wait(summed + 8 * stage, phase ^ 1, abort_flag))) break;
         ++fills;
+        const int row = begin + kb * DW_ROWS;
+        const bool tail = has_tail(end - row);
+        tails = tail ? tails | 1u << stage : tails & ~(1u << stage);
+        turns ^= (tail ? 1u : 0u) << stage;
         if (lane == 0) {
-          const uint32_t sa = tiles + stage * STAGE_BYTES, fb = full + 8 * stage;
-          const int row = begin + kb * DW_ROWS;
-          mbar_arrive_expect_tx(fb, STAGE_BYTES);
+          const uint32_t sa = tiles + stage * STAGE_BYTES, at = announce<2>(landed + 8 * stage, ready + 8 * stage, tail, place, STAGE_BYTES);
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
-            tma_load_2d(sa + s * SLAB_BYTES, &m.dout, n0 + 64 * s, row, fb);
-            tma_load_2d(sa + A_BYTES + s * SLAB_BYTES, &m.x, k0 + (int)rank * (TN / 2) + 64 * s, row, fb);
+            tma_load_2d_pair(sa + s * SLAB_BYTES, &m.dout, n0 + 64 * s, row, at);
+            tma_load_2d_pair(sa + A_BYTES + s * SLAB_BYTES, &m.x, k0 + (int)rank * (TN / 2) + 64 * s, row, at);
           }
         }
         __syncwarp();
@@ -119,6 +118,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
         constexpr uint32_t id = instr_desc(2 * BM, TN, true, true);
         for (int kb = from; kb < to; ++kb) {
           if (!warp_wait(ready + 8 * stage, phase, abort_flag)) break;
+          if (has_tail(rows - kb * DW_ROWS)) see_cleared<2>(ready + 8 * stage, phase);
           tc_fence_after();
           const uint32_t sa = uniform(tiles + stage * STAGE_BYTES);
           const int steps = (min(DW_ROWS, rows - kb * DW_ROWS) + 15) / 16;
@@ -127,7 +127,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
 #pragma unroll
             for (int k = 0; k < 4; ++k)
               if (k < steps) umma_bf16_pair(tmem, ad + (uint64_t)(128 * k), bd + (uint64_t)(128 * k), id, (kb > from || k > 0) ? 1u : 0u);
-            commit_to(empty + 8 * stage, even);
+            commit_to(used + 8 * stage, even);
           }
           __syncwarp();
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -136,30 +136,31 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
         __syncwarp();
       }
     } else if (warp == 2 + EPI_WARPS + SUM_WARPS) {
-      // ---------------------------------------------------------------- stages that have landed are handed on
+      // ---------------------------------------------------------------- the group's last rows
       for (int kb = from; kb < to; ++kb) {
-        if (!warp_wait(full + 8 * stage, phase, abort_flag)) break;
-        const int some = min(DW_ROWS, rows - kb * DW_ROWS);
-        if (some & 15) {                                 // the group's last rows: the others of their 16 become zero
+        const int some = rows - kb * DW_ROWS;
+        if (has_tail(some)) {                            // the others of their 16 become zero
+          if (!warp_wait(landed + 8 * stage, turns >> stage & 1, abort_flag)) break;
+          turns ^= 1u << stage;
           const uint32_t sa = tiles + stage * STAGE_BYTES;
           for (int s = 0; s < 4; ++s)
             for (int i = some * 8 + lane; i < (some + 15) / 16 * 128; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + (uint32_t)(s * SLAB_BYTES + i * 16)), "r"(0u) : "memory");
           fence_proxy_async_smem();
           __syncwarp();
-          fence_cluster();
+          if (lane == 0) mbar_arrive_cluster(map_to_cta(ready + 8 * stage, even));
+          __syncwarp();
         }
-        __syncwarp();
-        if (lane == 0) hand_on(map_to_cta(ready + 8 * stage, even));
-        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        if (++stage == STAGES) stage = 0;
       }
     } else if (warp >= 2 + EPI_WARPS && p.dbias) {
       // ---------------------------------------------------------------- sums of dout's columns
       // a warp has 32 columns; a lane 8 of them and every eighth row, such that eight lanes meet all banks
       const int sw = warp - 2 - EPI_WARPS, slab = sw >> 1, ck = (sw & 1) * 4 + (lane & 3), first = (lane >> 3) | (lane & 4);
+      const uint32_t there = rank == 0 ? ready : used;
       float2 sum[4] = {};
       for (int kb = from; kb < to; ++kb) {
-        if (!warp_wait(full + 8 * stage, phase, abort_flag)) break;
+        if (!warp_wait(there + 8 * stage, phase, abort_flag)) break;
         if (kt == 0) {
           const uint32_t slab_at = tiles + stage * STAGE_BYTES + slab * SLAB_BYTES;
           uint32_t w[8][4];
@@ -177,7 +178,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
           for (int e = 0; e < 4; ++e) sum[e] = __fadd2_rn(sum[e], some[e]);
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive(empty + 8 * stage);
+        if (lane == 0) mbar_arrive(summed + 8 * stage);
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
 #pragma unroll
@@ -260,7 +261,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
   }
 
   if (*abort_flag) {
-    if (warp == 0) drain_stages(full, STAGES, fills);
+    if (warp == 0) drain_fills(landed, ready, STAGES, fills, tails, turns, rank == 0);
     if (warp == 1 && rank == 0) drain_products<2>(drain);
     // the partner may be in a wait of its own that nothing will satisfy any more
     if (threadIdx.x == 0)

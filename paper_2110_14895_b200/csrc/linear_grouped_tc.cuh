@@ -1,7 +1,6 @@
 // Pieces of the tensor-core kernels of linear layers by group: tiles, descriptors, copies, products, the way out.
 #pragma once
-#include "vit_internal.h"
-#include "sm100_ptx.cuh"
+#include "linear_grouped.cuh"
 
 #include <cuda.h>
 
@@ -91,6 +90,37 @@ __device__ __forceinline__ void drain_products(uint32_t bar) {
     if (CTAS == 2) umma_commit_pair_here(bar);
     else umma_commit(bar);
     mbar_wait_limit(bar, 0, &never, DRAIN_LIMIT_CYCLES);
+  }
+}
+
+// The stages of the weights' gradients.  A stage's copies, in a pair those of both blocks, are counted on `ready` of the even block,
+// where the products wait.  A stage with a group's last rows, of which some have to be cleared first, comes to `landed` of its own
+// block, and the warp that clears arrives at `ready`.  `landed` has a turn of its own for every stage: a bit of `turns`.
+__device__ __forceinline__ bool has_tail(int rows) { return rows < DW_ROWS && (rows & 15); }         // rows: from the unit's first to the group's last
+// announces the bytes of a block's copies; the barrier to which they come
+template <int CTAS>
+__device__ __forceinline__ uint32_t announce(uint32_t landed, uint32_t ready, bool tail, uint32_t place, uint32_t bytes) {
+  if (CTAS == 1) {
+    mbar_arrive_expect_tx(tail ? landed : ready, bytes);
+    return tail ? landed : ready;
+  }
+  const uint32_t bar = tail ? map_to_cta(landed, place) : map_to_cta(ready, place & ~1u);
+  mbar_arrive_expect_tx_cluster(bar, bytes);
+  return bar;
+}
+// all of a stage's rows that were cleared, here or in the other block, are seen by the products behind this
+template <int CTAS>
+__device__ __forceinline__ void see_cleared(uint32_t ready, uint32_t phase) {
+  if (CTAS == 2) mbar_try_wait_cluster(ready, phase);
+}
+// After a wait gave up, as drain_stages: tails: the stages whose last fill had a tail.  The copies of an odd block's other stages are
+// counted in the even one, which it does not leave before.
+__device__ __forceinline__ void drain_fills(uint32_t landed, uint32_t ready, int stages, long long fills, uint32_t tails, uint32_t turns, bool even) {
+  volatile int never = 0;
+  for (long long f = fills > stages ? fills - stages : 0; f < fills; ++f) {
+    const uint32_t s = (uint32_t)(f % stages);
+    if (tails >> s & 1) mbar_wait_limit(landed + 8 * s, (turns >> s & 1) ^ 1, &never, DRAIN_LIMIT_CYCLES);
+    else if (even) mbar_wait_limit(ready + 8 * s, (uint32_t)((f / stages) & 1), &never, DRAIN_LIMIT_CYCLES);
   }
 }
 

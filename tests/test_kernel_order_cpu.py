@@ -56,3 +56,11 @@ def test_cleared_rows_are_ordered_before_their_stage_is_handed_on(name):
     first = next(i for i, what in enumerate(order) if what in ("hand_on(", "mbar_arrive_cluster("))
     assert order[:2] == ["fence_proxy_async_smem()", "__syncwarp()"]
     assert order[first] == "mbar_arrive_cluster(" or "fence_cluster()" in order[2:first]
+
+
+@pytest.mark.parametrize("path", SOURCES, ids=lambda p: p.name)
+def test_blocks_hand_nothing_on_without_a_release(path):
+    """What another block reads is ordered by a release, or counted by the copies themselves; an arrival that orders nothing may
+    announce bytes and no more."""
+    relaxed = re.findall(r"mbarrier\.arrive[.\w:]*\.relaxed[.\w:]*", _code(path))
+    assert all(".expect_tx." in r for r in relaxed)
