@@ -461,7 +461,7 @@ int vit_op_linear_grouped_backward_weights(vit_handle* h, int dtype, const vit_g
  * dst = src * min(1, max_norm / norm) for every tensor with a dst.  Sums are taken so that neither large nor small values
  * leave the range of 32 bits before the norm itself does.
  * (A norm beyond fp32 is written as infinity, and the tensors are scaled by what it is.)  An infinite value makes all dst
- * zero, and NaN in the infinite places; a value that is not a number makes all dst NaN.
+ * zero, and NaN in the infinite places, also where max_norm is infinite; a value that is not a number makes all dst NaN.
  *   tensors: HOST array of `count` entries, read before the call returns (a captured graph keeps what it said).
  *     dst == src scales in place (and writes nothing where the norm is within the bound); dst == NULL: the tensor only
  *     counts.  No dst may otherwise overlap a src, another dst, norm or ws.

@@ -168,9 +168,9 @@ clip_kernel(const __grid_constant__ List<CAP> list, const double* __restrict__ p
   for (int i = threadIdx.x; i < partials; i += THREADS) sum += partial[i];
   const double n = sqrt(block_sum(sum));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
-  // not a number: so is the factor.  Infinite: zero, and the infinite values themselves become not a number.  A factor that
+  // not a number: so is the factor.  Infinite: zero, for any bound, and the infinite values themselves become not a number.  A factor that
   // would lose bits below the normal numbers is applied in two steps, the second a power of two.
-  double by64 = n <= (double)bound ? 1.0 : (double)bound / n;
+  double by64 = isinf(n) ? 0.0 : n <= (double)bound ? 1.0 : (double)bound / n;
   const float small = by64 < 0x1p-100 ? 0x1p-100f : 1.0f;
   if (by64 < 0x1p-100) by64 *= 0x1p100;
   const float by = (float)by64;
