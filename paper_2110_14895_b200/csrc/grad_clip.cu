@@ -168,11 +168,10 @@ clip_kernel(const __grid_constant__ List<CAP> list, const double* __restrict__ p
   for (int i = threadIdx.x; i < partials; i += THREADS) sum += partial[i];
   const double n = sqrt(block_sum(sum));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
-  // not a number: so is the factor.  Infinite: zero, for any bound, and the infinite values themselves become not a number.  A factor that
-  // would lose bits below the normal numbers is applied in two steps, the second a power of two.
-  double by64 = isinf(n) ? 0.0 : n <= (double)bound ? 1.0 : (double)bound / n;
-  const float small = by64 < 0x1p-100 ? 0x1p-100f : 1.0f;
-  if (by64 < 0x1p-100) by64 *= 0x1p100;
+  // not a number: so is the factor.  Infinite: zero, for any bound, and the infinite values themselves become not a number.  A factor
+  // that would lose bits below the normal numbers of 32 bits, or has none left there, is applied in 64.
+  const double by64 = isinf(n) ? 0.0 : n <= (double)bound ? 1.0 : (double)bound / n;
+  const bool tiny = by64 > 0.0 && by64 < 0x1p-100;
   const float by = (float)by64;
   for (int piece = begin; piece < end; ++piece) {
     while (at + 1 < list.n && list.e[at + 1].first_piece <= piece) ++at;
@@ -180,8 +179,13 @@ clip_kernel(const __grid_constant__ List<CAP> list, const double* __restrict__ p
     if (!e.dst || (e.dst == e.src && by == 1.0f)) continue;
     const int64_t from = (int64_t)(piece - e.first_piece) * PIECE;
     if (piece != begin) load_piece(e, from, v);
+    if (tiny) {
 #pragma unroll
-    for (int i = 0; i < PER; ++i) v[i] = v[i] * by * small;
+      for (int i = 0; i < PER; ++i) v[i] = (float)((double)v[i] * by64);
+    } else {
+#pragma unroll
+      for (int i = 0; i < PER; ++i) v[i] *= by;
+    }
     store_piece(e, from, v);
   }
 }
