@@ -473,7 +473,7 @@ typedef struct vit_tensor {
   int32_t dtype;          /* VIT_BF16 or VIT_FP32, of src and dst */
 } vit_tensor;
 
-/* Bytes of scratch for vit_op_grad_clip with `count` tensors; 0 if count is negative or the lists are too many to count. */
+/* Bytes of scratch for vit_op_grad_clip with `count` tensors; 0 if count is negative. */
 size_t vit_grad_clip_bytes(int count);
 
 int vit_op_grad_clip(vit_handle* h, const vit_tensor* tensors, int count, float max_norm, float* norm, void* ws,

@@ -234,7 +234,7 @@ cudaError_t launch_list(const vit_tensor* t, int n, bool clip, double* partial, 
 
 }  // namespace
 
-int grad_clip_lists(int tensors) { return tensors <= MOST ? 1 : (tensors + MOST - 1) / MOST; }
+int grad_clip_lists(int tensors) { return tensors <= MOST ? 1 : (tensors - 1) / MOST + 1; }
 
 // list number `index` of the call's: its sum of squares (clip == false; *partials: how many parts it leaves) or its scaling
 cudaError_t launch_grad_clip(const vit_tensor* tensors, int count, int index, bool clip, double* partial, int* partials, float bound,
