@@ -48,3 +48,42 @@ def test_clip_of_huge_values_by_tiny_bounds(ctx, bound, size, dtype):
         # the norm's squares are added in 64 bits where they leave the range, and 16 at a time in 32 elsewhere: 12 steps; two roundings
         assert ((o.double() - want).abs() <= (HALF[dtype] + 14 * STEP) * want.abs() + 2.0 ** -133 * (1 if dtype == torch.bfloat16 else 2.0 ** -16)).all()
         assert (o != 0).all()
+
+
+
+# ------------------------------------------------------------------------------------ linear layers by group
+@BOTH
+def test_a_single_row_has_any_stride(ctx, dtype):
+    """With one row, or none, nothing lies a stride further on: strides beyond what any memory holds are as good as others."""
+    vit, m = ctx
+    k, n, far = 72, 136, 1 << 45
+    dt = _dt(vit, dtype)
+    l = Layer(vit, m, [1], 0, 0, k, n, dtype)
+    x, dout, residual, pre = l.some(k, k), l.some(n, n), l.some(n, n), l.some(k, k)
+    calls = lambda ld: [l_forward(1, ld), l_forward(2, ld), l_input(ld), *l_weights(ld)]
+
+    def l_forward(epilogue, ld):
+        out, kept = l.blank(n), l.blank(n)
+        vit.vit_op_linear_grouped(m.h, dt, l.problem, x.data_ptr(), ld or k, l.w.data_ptr(), 0, epilogue, residual.data_ptr(), ld or n, out.data_ptr(),
+                                  ld or n, kept.data_ptr(), ld or n)
+        return out
+
+    def l_input(ld):
+        dx = l.blank(k)
+        vit.vit_op_linear_grouped_backward_input(m.h, dt, l.problem, dout.data_ptr(), ld or n, l.w.data_ptr(), pre.data_ptr(), ld or k, dx.data_ptr(), ld or k)
+        return dx
+
+    def l_weights(ld, problem=None):
+        dw, db = torch.full_like(l.w, 77.0), torch.full((1, n), 77.0, device="cuda")
+        size = vit.vit_linear_grouped_backward_weights_bytes(dt, problem or l.problem)
+        ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+        vit.vit_op_linear_grouped_backward_weights(m.h, dt, problem or l.problem, x.data_ptr(), ld or k, dout.data_ptr(), ld or n, dw.data_ptr(),
+                                                   db.data_ptr(), ws.data_ptr(), size)
+        return dw, db
+
+    for a, b in zip(calls(0), calls(far)):
+        assert torch.equal(a, b)
+    m.check()
+    none = vit.make_grouped_problem(1, 0, k, n, 0)
+    assert all((t == 0).all() for t in l_weights(far, none))
+    m.check()
