@@ -87,3 +87,38 @@ def test_a_single_row_has_any_stride(ctx, dtype):
     none = vit.make_grouped_problem(1, 0, k, n, 0)
     assert all((t == 0).all() for t in l_weights(far, none))
     m.check()
+
+
+@pytest.mark.parametrize("far", [False, True])
+def test_gelu_and_its_slope_in_fp32(ctx, far):
+    """The error function and the exponential of the fp32 mode are CUDA's own, good to a few roundings; an approximation to 1e-7 of
+    one, as the bf16 mode uses, is not."""
+    vit, m = ctx
+    k, rows = 64, 300
+    l = Layer(vit, m, [rows], 0, 0, k, k, torch.float32)
+    l.w[0] = torch.eye(k, device="cuda")
+    v = _normal(l.gen, rows, k, scale=4.0 if far else 1.0)                       # products with ones and sums with zeros are exact
+    a = v.double()
+    # erfc is good to 4 steps (8 roundings); its argument u has two roundings, which count 2 u^2 + 1.2 times at most beyond u = 0 (u erfc'(u) / erfc(u),
+    # and less than u before); three products follow
+    u = a.abs() / math.sqrt(2)
+    erfc = 8 + 2 * (2 * u * u + 2) + 3
+    out = l.forward(v, None, 1, out=l.blank(k))
+    want = _gelu64(a)
+    assert ((out.double() - want).abs() <= erfc * STEP * want.abs() + 2.0 ** -140).all()
+    # the exponential is good to 2 steps, its argument a^2 / 2 has a rounding; the factors before it three, the sum one
+    dx = l.input_grad(torch.ones_like(v), v, l.blank(k))
+    phi = a.abs() * torch.exp(-0.5 * a * a) / math.sqrt(2 * math.pi)
+    want = _slope64(a)
+    tol = phi * (4 + 0.5 * a * a + 3) + 0.5 * torch.erfc(-a / math.sqrt(2)) * erfc + want.abs()
+    assert ((dx.double() - want).abs() <= STEP * tol + 2.0 ** -140).all()
+
+
+# ------------------------------------------------------------------------------------ layer norm
+# two rows to a warp from 32 to an SM on, in one to six pieces a lane (three in fp32), an odd row left over; the same with four warps to two rows
+@pytest.mark.parametrize("rows,cols", [(4737, 200), (4737, 384), (4739, 768), (4999, 1000), (4741, 1024), (4801, 1280), (4736, 1536), (4735, 768),
+                                       (5001, 1800), (4737, 2056), (4801, 4000)])
+@BOTH
+def test_layernorm_of_many_rows(ctx, rows, cols, dtype):
+    check_layernorm_forward(ctx, rows, cols, dtype)
+    check_layernorm_backward(ctx, rows, cols, True, dtype)
