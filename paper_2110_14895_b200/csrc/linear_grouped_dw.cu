@@ -8,10 +8,11 @@
 // a single block's 128 x 256 are more than it can move.  Single blocks stay for narrow layers, where half a pair would idle.
 // The rows behind a group's end are the next group's: they are cleared in the last stage, in both operands (zero times a
 // value that is not a number would not be zero).  A warp of its own in each block sees such a stage land, clears it and hands it on
-// to the warp that issues the products (the even block's, for both), with a release at cluster scope.  The copies of all other
-// stages are counted where the products wait: a release for every stage took twice the time.
-// Four more warps add up dout's columns for db from the same stages, where the tile is its row's first: in the even block beside the
-// products, in the odd one, where nothing but the products tells that the copies have landed, behind them.
+// to the warp that issues the products (the even block's, for both), from block to block with a release at cluster scope.  The
+// copies of all other stages are counted where the products wait (a release for every stage takes twice the time; all bytes of a
+// pair announced by its even block 3 % more).
+// Four more warps add up dout's columns for db from the same stages, where the tile is its row's first.  They read a stage behind its
+// products, which alone tell the odd block that its copies have landed, and only such a stage waits for them.
 // The units of work get equal shares of it (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
 // 25216 rows of 16 groups, 1024 x 4096: 185 us (tensor pipe active 66 %); one group of 8192 rows, 4096 x 4096: 190 us (1440
 // TFLOP/s); 32896 rows, 1280 x 1280: 99 us.
@@ -29,7 +30,7 @@ namespace {
 constexpr int TN = 256, EPI_WARPS = 8, SUM_WARPS = 4, DW_THREADS = 32 * (2 + EPI_WARPS + SUM_WARPS + 1);
 template <int CTAS> struct DwCfg {
   static constexpr int B_SLABS = 4 / CTAS, A_BYTES = 2 * SLAB_BYTES, STAGE_BYTES = A_BYTES + B_SLABS * SLAB_BYTES, STAGES = CTAS == 2 ? 6 : 4;
-  static constexpr int STAGING_BYTES = EPI_WARPS * 4096, SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 256;
+  static constexpr int STAGING_BYTES = EPI_WARPS * 4096, SMEM_BYTES = STAGES * STAGE_BYTES + STAGING_BYTES + 1024 + 384;
 };
 
 struct DwArgs {
@@ -59,9 +60,9 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t tiles = smem_u32(smem), staging = tiles + STAGES * C::STAGE_BYTES;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * C::STAGE_BYTES + C::STAGING_BYTES);
-  const uint32_t landed = smem_u32(bars), ready = landed + 8 * STAGES, used = ready + 8 * STAGES, summed = used + 8 * STAGES,
-                 tfull = summed + 8 * STAGES, tempty = tfull + 16, drain = tempty + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * STAGES + 5);
+  const uint32_t landed = smem_u32(bars), cleared = landed + 8 * STAGES, ready = cleared + 8 * STAGES, used = ready + 8 * STAGES, multiplied = used + 8 * STAGES,
+                 summed = multiplied + 8 * STAGES, tfull = summed + 8 * STAGES, tempty = tfull + 16, drain = tempty + 16;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 6 * STAGES + 5);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = CTAS == 2 ? cluster_ctarank() : 0u;
@@ -71,9 +72,11 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     *abort_flag = 0;
     for (int i = 0; i < STAGES; ++i) {
       mbar_init(landed + 8 * i, 1);
+      mbar_init(cleared + 8 * i, 1);
       mbar_init(ready + 8 * i, CTAS);                                   // a word of each block
       mbar_init(used + 8 * i, 1);                                       // by the products
-      mbar_init(summed + 8 * i, SUM_WARPS);                             // and, with biases, by the sums of columns
+      mbar_init(multiplied + 8 * i, 1);                                 // the same, where columns are summed
+      mbar_init(summed + 8 * i, SUM_WARPS);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(tfull + 8 * i, 1);
@@ -107,16 +110,20 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
   if (warp == 0) {
     // ---------------------------------------------------------------- TMA producer
     long long fills = 0;
-    uint32_t tails = 0, turns = 0;
+    uint32_t tails = 0, turns = 0, sums = 0, sum_turns = 0;             // (sums: the stages whose last fill has its columns summed)
     bool ok = true;
     while (ok && work.next(part)) {
+      const bool mine = p.dbias && part.tile % p.tiles_in == 0;
       const int n0 = part.tile / p.tiles_in * (BM * CTAS) + (int)rank * BM, k0 = part.tile % p.tiles_in * TN + (int)rank * (TN / CTAS);
       for (int kb = 0; kb < part.blocks(); ++kb) {
-        if (!warp_wait(used + 8 * stage, phase ^ 1, abort_flag) || (p.dbias && !warp_wait(summed + 8 * stage, phase ^ 1, abort_flag))) {
+        if (!warp_wait(used + 8 * stage, phase ^ 1, abort_flag) ||
+            ((sums >> stage & 1) && !warp_wait(summed + 8 * stage, (sum_turns >> stage & 1) ^ 1, abort_flag))) {
           ok = false;
           break;
         }
         ++fills;
+        sums = mine ? sums | 1u << stage : sums & ~(1u << stage);
+        sum_turns ^= (mine ? 1u : 0u) << stage;
         const int row = part.begin + part.unit(kb) * DW_ROWS;
         const bool tail = has_tail(part.end - row);
         tails = tail ? tails | 1u << stage : tails & ~(1u << stage);
@@ -144,18 +151,19 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         if (!warp_wait(tempty + 8 * buf, aphase ^ 1, abort_flag)) break;
         tc_fence_after();
         const uint32_t d = tmem + (uint32_t)(buf * TN);
+        const bool mine = p.dbias && part.tile % p.tiles_in == 0;
         for (int kb = 0; kb < part.blocks(); ++kb) {
           if (!warp_wait(ready + 8 * stage, phase, abort_flag)) { ok = false; break; }
-          const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS, steps = (min(DW_ROWS, rows) + 15) / 16;
-          if (has_tail(rows)) see_cleared<CTAS>(ready + 8 * stage, phase);
           tc_fence_after();
           const uint32_t sa = uniform(tiles + stage * C::STAGE_BYTES);
+          const int steps = (min(DW_ROWS, part.end - part.begin - part.unit(kb) * DW_ROWS) + 15) / 16;
           const uint64_t ad = smem_desc(sa, SLAB_BYTES), bd = smem_desc(sa + C::A_BYTES, SLAB_BYTES);
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)                // 16 rows of 128 bytes
               if (k < steps) product<CTAS>(d, ad + (uint64_t)(128 * k), bd + (uint64_t)(128 * k), id, (kb > 0 || k > 0) ? 1u : 0u);
             commit<CTAS>(used + 8 * stage);
+            if (mine) commit<CTAS>(multiplied + 8 * stage);
           }
           __syncwarp();
           if (++stage == STAGES) { stage = 0; phase ^= 1; }
@@ -176,18 +184,12 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
         const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS;
         if (has_tail(rows)) {                          // the others of their 16 become zero
           if (!warp_wait(landed + 8 * stage, turns >> stage & 1, abort_flag)) { ok = false; break; }
-          turns ^= 1u << stage;
           const uint32_t sa = tiles + stage * C::STAGE_BYTES;
           for (int s = 0; s < 2 + C::B_SLABS; ++s)
             for (int i = rows * 8 + lane; i < (rows + 15) / 16 * 128; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + (uint32_t)(s * SLAB_BYTES + i * 16)), "r"(0u) : "memory");
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            if (CTAS == 2) mbar_arrive_cluster(map_to_cta(ready + 8 * stage, 0));
-            else mbar_arrive(ready + 8 * stage);
-          }
-          __syncwarp();
+          if (!hand_on<CTAS>(ready + 8 * stage, cleared + 8 * stage, turns >> stage & 1, rank, lane, abort_flag)) { ok = false; break; }
+          turns ^= 1u << stage;
         }
         if (++stage == STAGES) stage = 0;
       }
@@ -248,35 +250,37 @@ grouped_dw_kernel(const __grid_constant__ DwMaps m, const __grid_constant__ DwAr
     // ---------------------------------------------------------------- sums of dout's columns
     // a warp has 32 columns; a lane 8 of them and every eighth row, such that eight lanes meet all banks
     const int sw = warp - 2 - EPI_WARPS, slab = sw >> 1, ck = (sw & 1) * 4 + (lane & 3), first = (lane >> 3) | (lane & 4);
-    const uint32_t there = rank == 0 ? ready : used;
+    uint32_t turns = 0;
     bool ok = true;
     while (ok && work.next(part)) {
-      const bool mine = part.tile % p.tiles_in == 0;
+      if (part.tile % p.tiles_in != 0) {
+        stage = (stage + part.blocks()) % STAGES;
+        continue;
+      }
       float2 sum[4] = {};
       for (int kb = 0; kb < part.blocks(); ++kb) {
-        if (!warp_wait(there + 8 * stage, phase, abort_flag)) { ok = false; break; }
-        if (mine) {
-          const uint32_t from = tiles + stage * C::STAGE_BYTES + slab * SLAB_BYTES;
-          const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS;
-          uint32_t w[8][4];
+        if (!warp_wait(multiplied + 8 * stage, turns >> stage & 1, abort_flag)) { ok = false; break; }
+        turns ^= 1u << stage;
+        const uint32_t from = tiles + stage * C::STAGE_BYTES + slab * SLAB_BYTES;
+        const int rows = part.end - part.begin - part.unit(kb) * DW_ROWS;
+        uint32_t w[8][4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) read_chunk(w[i], from, first + 8 * i, ck);
-          float2 some[4] = {};
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (first + 8 * i < rows) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                some[e] = __fadd2_rn(some[e], make_float2(__uint_as_float(w[i][e] << 16), __uint_as_float(w[i][e] & 0xffff0000u)));
-            }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[e] = __fadd2_rn(sum[e], some[e]);
-        }
+        for (int i = 0; i < 8; ++i) read_chunk(w[i], from, first + 8 * i, ck);
         __syncwarp();
-        if (lane == 0) mbar_arrive(summed + 8 * stage);
-        if (++stage == STAGES) { stage = 0; phase ^= 1; }
+        if (lane == 0) mbar_arrive(summed + 8 * stage);  // releases behind what has been read
+        float2 some[4] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (first + 8 * i < rows) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              some[e] = __fadd2_rn(some[e], make_float2(__uint_as_float(w[i][e] << 16), __uint_as_float(w[i][e] & 0xffff0000u)));
+          }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = __fadd2_rn(sum[e], some[e]);
+        if (++stage == STAGES) stage = 0;
       }
-      if (!ok || !mine) continue;
+      if (!ok) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll

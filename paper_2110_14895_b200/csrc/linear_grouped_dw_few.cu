@@ -51,9 +51,9 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   const uint32_t tiles = smem_u32(smem);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES);
-  const uint32_t landed = smem_u32(bars), ready = landed + 8 * STAGES, used = ready + 8 * STAGES, summed = used + 8 * STAGES,
+  const uint32_t landed = smem_u32(bars), cleared = landed + 8 * STAGES, ready = cleared + 8 * STAGES, used = ready + 8 * STAGES, summed = used + 8 * STAGES,
                  done = summed + 8 * STAGES, drain = done + 8;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * STAGES + 2);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 5 * STAGES + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const uint32_t bias_sums = tiles + STAGES * STAGE_BYTES + 512;                             // [128] floats
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -64,7 +64,8 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
     *abort_flag = 0;
     for (int i = 0; i < STAGES; ++i) {
       mbar_init(landed + 8 * i, 1);
-      mbar_init(ready + 8 * i, 2);
+      mbar_init(cleared + 8 * i, 1);
+      mbar_init(ready + 8 * i, 2);                                      // a word of each block
       mbar_init(used + 8 * i, 1);
       mbar_init(summed + 8 * i, SUM_WARPS);
     }
@@ -90,12 +91,13 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
   long long fills = 0;
   if (group_rows(p.shape, 0, begin, end)) {
     const int n0 = tile / p.tiles_in * (2 * BM) + (int)rank * BM, kt = tile % p.tiles_in, k0 = kt * TN;
+    const bool sums = p.dbias && kt == 0;                                                    // columns are summed, behind the products
     const int rows = end - begin, all = (rows + DW_ROWS - 1) / DW_ROWS, share = (all + p.split - 1) / p.split;
     const int from = min(all, pair * share), to = min(all, from + share);                    // of the tile's units of 64 rows
     if (warp == 0) {
       // ---------------------------------------------------------------- TMA producer
       for (int kb = from; kb < to; ++kb) {
-        if (!warp_wait(used + 8 * stage, phase ^ 1, abort_flag) || (p.dbias && !warp_wait(summed + 8 * stage, phase ^ 1, abort_flag))) break;
+        if (!warp_wait(used + 8 * stage, phase ^ 1, abort_flag) || (sums && !warp_wait(summed + 8 * stage, phase ^ 1, abort_flag))) break;
         ++fills;
         const int row = begin + kb * DW_ROWS;
         const bool tail = has_tail(end - row);
@@ -118,7 +120,6 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
         constexpr uint32_t id = instr_desc(2 * BM, TN, true, true);
         for (int kb = from; kb < to; ++kb) {
           if (!warp_wait(ready + 8 * stage, phase, abort_flag)) break;
-          if (has_tail(rows - kb * DW_ROWS)) see_cleared<2>(ready + 8 * stage, phase);
           tc_fence_after();
           const uint32_t sa = uniform(tiles + stage * STAGE_BYTES);
           const int steps = (min(DW_ROWS, rows - kb * DW_ROWS) + 15) / 16;
@@ -141,44 +142,38 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
         const int some = rows - kb * DW_ROWS;
         if (has_tail(some)) {                            // the others of their 16 become zero
           if (!warp_wait(landed + 8 * stage, turns >> stage & 1, abort_flag)) break;
-          turns ^= 1u << stage;
           const uint32_t sa = tiles + stage * STAGE_BYTES;
           for (int s = 0; s < 4; ++s)
             for (int i = some * 8 + lane; i < (some + 15) / 16 * 128; i += 32)
               asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + (uint32_t)(s * SLAB_BYTES + i * 16)), "r"(0u) : "memory");
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) mbar_arrive_cluster(map_to_cta(ready + 8 * stage, even));
-          __syncwarp();
+          if (!hand_on<2>(ready + 8 * stage, cleared + 8 * stage, turns >> stage & 1, place, lane, abort_flag)) break;
+          turns ^= 1u << stage;
         }
         if (++stage == STAGES) stage = 0;
       }
-    } else if (warp >= 2 + EPI_WARPS && p.dbias) {
+    } else if (warp >= 2 + EPI_WARPS && sums) {
       // ---------------------------------------------------------------- sums of dout's columns
       // a warp has 32 columns; a lane 8 of them and every eighth row, such that eight lanes meet all banks
       const int sw = warp - 2 - EPI_WARPS, slab = sw >> 1, ck = (sw & 1) * 4 + (lane & 3), first = (lane >> 3) | (lane & 4);
-      const uint32_t there = rank == 0 ? ready : used;
       float2 sum[4] = {};
       for (int kb = from; kb < to; ++kb) {
-        if (!warp_wait(there + 8 * stage, phase, abort_flag)) break;
-        if (kt == 0) {
-          const uint32_t slab_at = tiles + stage * STAGE_BYTES + slab * SLAB_BYTES;
-          uint32_t w[8][4];
+        if (!warp_wait(used + 8 * stage, phase, abort_flag)) break;
+        const uint32_t slab_at = tiles + stage * STAGE_BYTES + slab * SLAB_BYTES;
+        uint32_t w[8][4];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) read_chunk(w[i], slab_at, first + 8 * i, ck);
-          float2 some[4] = {};
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (first + 8 * i < rows - kb * DW_ROWS) {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                some[e] = __fadd2_rn(some[e], make_float2(__uint_as_float(w[i][e] << 16), __uint_as_float(w[i][e] & 0xffff0000u)));
-            }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[e] = __fadd2_rn(sum[e], some[e]);
-        }
+        for (int i = 0; i < 8; ++i) read_chunk(w[i], slab_at, first + 8 * i, ck);
         __syncwarp();
-        if (lane == 0) mbar_arrive(summed + 8 * stage);
+        if (lane == 0) mbar_arrive(summed + 8 * stage);  // releases behind what has been read
+        float2 some[4] = {};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (first + 8 * i < rows - kb * DW_ROWS) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              some[e] = __fadd2_rn(some[e], make_float2(__uint_as_float(w[i][e] << 16), __uint_as_float(w[i][e] & 0xffff0000u)));
+          }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] = __fadd2_rn(sum[e], some[e]);
         if (++stage == STAGES) { stage = 0; phase ^= 1; }
       }
 #pragma unroll

@@ -95,7 +95,8 @@ __device__ __forceinline__ void drain_products(uint32_t bar) {
 
 // The stages of the weights' gradients.  A stage's copies, in a pair those of both blocks, are counted on `ready` of the even block,
 // where the products wait.  A stage with a group's last rows, of which some have to be cleared first, comes to `landed` of its own
-// block, and the warp that clears arrives at `ready`.  `landed` has a turn of its own for every stage: a bit of `turns`.
+// block.  The warp that clears it there hands it on, the odd block's to the even one's, which waits at `cleared` and arrives for both.
+// `landed` and `cleared` have turns of their own for every stage: a bit of `turns`.
 __device__ __forceinline__ bool has_tail(int rows) { return rows < DW_ROWS && (rows & 15); }         // rows: from the unit's first to the group's last
 // announces the bytes of a block's copies; the barrier to which they come
 template <int CTAS>
@@ -104,14 +105,27 @@ __device__ __forceinline__ uint32_t announce(uint32_t landed, uint32_t ready, bo
     mbar_arrive_expect_tx(tail ? landed : ready, bytes);
     return tail ? landed : ready;
   }
-  const uint32_t bar = tail ? map_to_cta(landed, place) : map_to_cta(ready, place & ~1u);
-  mbar_arrive_expect_tx_cluster(bar, bytes);
-  return bar;
+  if (tail) mbar_arrive_expect_tx(landed, bytes);
+  else mbar_arrive_expect_tx_cluster(map_to_cta(ready, place & ~1u), bytes);
+  return tail ? map_to_cta(landed, place) : map_to_cta(ready, place & ~1u);
 }
-// all of a stage's rows that were cleared, here or in the other block, are seen by the products behind this
+// All lanes have written their zeros: a stage is handed on to the products.
 template <int CTAS>
-__device__ __forceinline__ void see_cleared(uint32_t ready, uint32_t phase) {
-  if (CTAS == 2) mbar_try_wait_cluster(ready, phase);
+__device__ __forceinline__ bool hand_on(uint32_t ready, uint32_t cleared, uint32_t turn, uint32_t place, int lane, volatile int* abort_flag) {
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (CTAS == 2 && (place & 1)) {
+    if (lane == 0) mbar_arrive_cluster(map_to_cta(cleared, place & ~1u));
+    __syncwarp();
+    return true;
+  }
+  if (CTAS == 2) {
+    if (!warp_wait(cleared, turn, abort_flag)) return false;
+    mbar_try_wait_cluster(cleared, turn);               // (it is complete) what the other block wrote before it arrived is acquired
+  }
+  if (lane < CTAS) mbar_arrive(ready);                  // a word of each block
+  __syncwarp();
+  return true;
 }
 // After a wait gave up, as drain_stages: tails: the stages whose last fill had a tail.  The copies of an odd block's other stages are
 // counted in the even one, which it does not leave before.

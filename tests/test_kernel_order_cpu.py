@@ -52,10 +52,12 @@ def test_cleared_rows_are_ordered_before_their_stage_is_handed_on(name):
     is a release at cluster scope, a fence or the arrival itself."""
     code = _code(next(p for p in SOURCES if p.name == name))
     behind = code[code.index('"r"(0u) : "memory");'):]
-    order = re.findall(r"fence_proxy_async_smem\(\)|__syncwarp\(\)|fence_cluster\(\)|hand_on\(|mbar_arrive_cluster\(", behind)
-    first = next(i for i, what in enumerate(order) if what in ("hand_on(", "mbar_arrive_cluster("))
-    assert order[:2] == ["fence_proxy_async_smem()", "__syncwarp()"]
-    assert order[first] == "mbar_arrive_cluster(" or "fence_cluster()" in order[2:first]
+    shared = _code(next(p for p in SOURCES if p.name == "linear_grouped_tc.cuh"))
+    assert "hand_on<" in behind[:300]
+    order = re.findall(r"fence_proxy_async_smem\(\)|__syncwarp\(\)|mbar_arrive_cluster\(|mbar_arrive\(", _function(shared, "hand_on"))
+    assert order[:3] == ["fence_proxy_async_smem()", "__syncwarp()", "mbar_arrive_cluster("]
+    # and the even block's warp acquires it at the scope at which it was released
+    assert re.search(r"warp_wait\(cleared.*mbar_try_wait_cluster\(cleared.*mbar_arrive\(ready\)", _function(shared, "hand_on"), re.S)
 
 
 @pytest.mark.parametrize("path", SOURCES, ids=lambda p: p.name)
