@@ -65,7 +65,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
     for (int i = 0; i < STAGES; ++i) {
       mbar_init(landed + 8 * i, 1);
       mbar_init(cleared + 8 * i, 1);
-      mbar_init(ready + 8 * i, 2);                                      // a word of each block
+      mbar_init(ready + 8 * i, 1);
       mbar_init(used + 8 * i, 1);
       mbar_init(summed + 8 * i, SUM_WARPS);
     }
@@ -103,7 +103,7 @@ grouped_dw_few_kernel(const __grid_constant__ DwFewMaps m, const __grid_constant
         const bool tail = has_tail(end - row);
         tails = tail ? tails | 1u << stage : tails & ~(1u << stage);
         turns ^= (tail ? 1u : 0u) << stage;
-        if (lane == 0) {
+        if (elect_one()) {
           const uint32_t sa = tiles + stage * STAGE_BYTES, at = announce<2>(landed + 8 * stage, ready + 8 * stage, tail, place, STAGE_BYTES);
 #pragma unroll
           for (int s = 0; s < 2; ++s) {

@@ -95,18 +95,15 @@ __device__ __forceinline__ void drain_products(uint32_t bar) {
 
 // The stages of the weights' gradients.  A stage's copies, in a pair those of both blocks, are counted on `ready` of the even block,
 // where the products wait.  A stage with a group's last rows, of which some have to be cleared first, comes to `landed` of its own
-// block.  The warp that clears it there hands it on, the odd block's to the even one's, which waits at `cleared` and arrives for both.
+// block.  The warp that clears it there arrives at `ready`, the odd block's by way of the even one's, which waits at `cleared`.
 // `landed` and `cleared` have turns of their own for every stage: a bit of `turns`.
 __device__ __forceinline__ bool has_tail(int rows) { return rows < DW_ROWS && (rows & 15); }         // rows: from the unit's first to the group's last
 // announces the bytes of a block's copies; the barrier to which they come
 template <int CTAS>
 __device__ __forceinline__ uint32_t announce(uint32_t landed, uint32_t ready, bool tail, uint32_t place, uint32_t bytes) {
-  if (CTAS == 1) {
-    mbar_arrive_expect_tx(tail ? landed : ready, bytes);
-    return tail ? landed : ready;
-  }
   if (tail) mbar_arrive_expect_tx(landed, bytes);
-  else mbar_arrive_expect_tx_cluster(map_to_cta(ready, place & ~1u), bytes);
+  else if (CTAS == 1 || !(place & 1)) mbar_arrive_expect_tx(ready, CTAS * bytes);
+  if (CTAS == 1) return tail ? landed : ready;
   return tail ? map_to_cta(landed, place) : map_to_cta(ready, place & ~1u);
 }
 // All lanes have written their zeros: a stage is handed on to the products.
@@ -123,7 +120,7 @@ __device__ __forceinline__ bool hand_on(uint32_t ready, uint32_t cleared, uint32
     if (!warp_wait(cleared, turn, abort_flag)) return false;
     mbar_try_wait_cluster(cleared, turn);               // (it is complete) what the other block wrote before it arrived is acquired
   }
-  if (lane < CTAS) mbar_arrive(ready);                  // a word of each block
+  if (lane == 0) mbar_arrive(ready);
   __syncwarp();
   return true;
 }
