@@ -4,7 +4,7 @@ import math
 import pytest
 
 torch = pytest.importorskip("torch")
-from test_gpu_training_ops import BOTH, EPS, HALF, STEP, Layer, _clip, _dt, _gelu64, _gen, _normal, _slope64, ctx  # noqa: E402,F401
+from test_gpu_training_ops import BOTH, EPS, HALF, STEP, Layer, _clip, _dt, _gelu64, _gen, _normal, _slope64, _sum_error, ctx  # noqa: E402,F401
 from test_gpu_training_ops import test_layernorm_backward as check_layernorm_backward, test_layernorm_forward as check_layernorm_forward  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -122,3 +122,48 @@ def test_gelu_and_its_slope_in_fp32(ctx, far):
 def test_layernorm_of_many_rows(ctx, rows, cols, dtype):
     check_layernorm_forward(ctx, rows, cols, dtype)
     check_layernorm_backward(ctx, rows, cols, True, dtype)
+
+
+# ------------------------------------------------------------------------------------ bad offsets where clusters share the sums
+@pytest.mark.parametrize("edges,rows,k,n", [([5, 3], 577, 1280, 1280), ([0, 578], 577, 1280, 1280), ([-1, 577], 577, 1280, 1024), ([0, 90, 60, 97], 97, 4096, 1544),
+                                            ([0, 2 ** 31 - 1, 5, 33], 33, 2048, 1536)], ids=lambda v: "-".join(map(str, v)) if isinstance(v, list) else str(v))
+@BOTH
+def test_bad_offsets_of_few_tiles(ctx, edges, rows, k, n, dtype):
+    """Long sums of few tiles, forwards, backwards and of the weights: bad groups are left as they were and reported, the others are right."""
+    vit, m = ctx
+    groups = len(edges) - 1
+    good = [g for g in range(groups) if 0 <= edges[g] <= edges[g + 1] <= rows]
+    dt = _dt(vit, dtype)
+    gen = _gen(rows + k)
+    x, dout = _normal(gen, rows, k, dtype=dtype), _normal(gen, rows, n, dtype=dtype)
+    w = _normal(gen, groups, n, k, scale=k ** -0.5, dtype=dtype)
+    off = torch.tensor(edges, dtype=torch.int32, device="cuda")
+    p = vit.make_grouped_problem(groups, rows, k, n, off.data_ptr())
+    out, dx = torch.full_like(dout, 77.0), torch.full_like(x, 77.0)
+    dw, db = torch.full_like(w, 777.0), torch.full((groups, n), 777.0, device="cuda")
+    size = vit.vit_linear_grouped_backward_weights_bytes(dt, p)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+    for call in (lambda: vit.vit_op_linear_grouped(m.h, dt, p, x.data_ptr(), k, w.data_ptr(), 0, 0, 0, 0, out.data_ptr(), n, 0, 0),
+                 lambda: vit.vit_op_linear_grouped_backward_input(m.h, dt, p, dout.data_ptr(), n, w.data_ptr(), 0, 0, dx.data_ptr(), k),
+                 lambda: vit.vit_op_linear_grouped_backward_weights(m.h, dt, p, x.data_ptr(), k, dout.data_ptr(), n, dw.data_ptr(), db.data_ptr(),
+                                                                    ws.data_ptr(), size)):
+        call()
+        with pytest.raises(vit.VitError) as e:
+            m.check()
+        assert e.value.status == vit.VIT_ERR_OFFSETS
+    owners = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    for g in good:
+        owners[edges[g]:edges[g + 1]] += 1
+    assert (out[owners == 0] == 77).all() and (dx[owners == 0] == 77).all()
+    for g in range(groups):
+        b, e = edges[g], edges[g + 1]
+        if g not in good:
+            assert (dw[g] == 777).all() and (db[g] == 777).all()
+            continue
+        own = (owners[b:e] == 1)[:, None]
+        xs, ds, wg = x[b:e].double(), dout[b:e].double(), w[g].double()
+        for got, want, terms, length in ((out[b:e], xs @ wg.t(), xs.abs() @ wg.abs().t(), k), (dx[b:e], ds @ wg, ds.abs() @ wg.abs(), n)):
+            assert (((got.double() - want).abs() <= HALF[dtype] * want.abs() + (_sum_error(length, dtype) + 8 * STEP) * terms) | ~own).all()
+        want, terms = ds.t() @ xs, ds.abs().t() @ xs.abs()
+        assert ((dw[g].double() - want).abs() <= HALF[dtype] * want.abs() + (_sum_error(e - b, dtype) + 8 * STEP) * terms).all()
+        assert ((db[g].double() - ds.sum(0)).abs() <= ((e - b) / 16 + 32) * STEP * ds.abs().sum(0)).all()
