@@ -395,8 +395,9 @@ cudaError_t launch_backward(BackwardArgs a, cudaStream_t s, int* blocks) {
 }
 // The sums of dg and db are what a thread needs registers for: a warp to a row of 1280 columns leaves room for eight warps an SM
 // (60.5 us at 32896 rows), two warps to a row for sixteen (58 us); at 1024 columns twelve and twenty (24.2, 23.9 us at 12608
-// rows).  Most of the rest are the start, the end and the second kernel: 12 us and 6.9 TB/s fit both.  fp32 rows are twice as
-// long in the ring.
+// rows; all with some of the inputs still in L2).  On inputs that L2 does not hold, bf16 and with the residual's gradient, calls take
+// 9 us for the start, the end and the second kernel, and their bytes at 6.6 TB/s: 3152 rows of 768 columns 11 us, 12608 of 768
+// 21, 12608 of 1024 25, 32896 of 1280 60.  fp32 rows are twice as long in the ring.
 template <typename T>
 cudaError_t dispatch_backward(const BackwardArgs& a, cudaStream_t s, int* blocks) {
   constexpr bool F = sizeof(T) == 4;

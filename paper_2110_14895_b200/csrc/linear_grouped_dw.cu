@@ -13,8 +13,8 @@
 // Four more warps add up dout's columns for db from the same stages, where the tile is its row's first.  They read a stage behind its
 // products, which alone tell the odd block that its copies have landed, and only such a stage waits for them.
 // The units of work get equal shares of it (linear_grouped.cuh), so that a single long sum with 25 tiles keeps all SMs busy.
-// 25216 rows of 16 groups, 1024 x 4096: 185 us (tensor pipe active 66 %); one group of 8192 rows, 4096 x 4096: 190 us (1440
-// TFLOP/s); 32896 rows, 1280 x 1280: 99 us.
+// 25216 rows of 16 groups, 1024 x 4096: 193 us (tensor pipe active 65 %), 182 without biases; one group of 8192 rows, 4096 x 4096:
+// 200 us (1370 TFLOP/s), 188 without; 32896 rows, 1280 x 1280: 100 us.
 #include "linear_grouped.cuh"
 #include "linear_grouped_tc.cuh"
 
@@ -417,9 +417,10 @@ DwTiling tiling_of(bool act_bf16, const GroupedShape& shape, int in, int out) {
   t.cuts = shape.rows > (act_bf16 ? DW_LEAST : DW_LEAST_F32) * DW_ROWS;
   t.blocks = (int)((t.cuts ? wanted : whole) < most ? (wanted < 1 ? 1 : t.cuts ? wanted : whole) : most);
   // One sum for few tiles: a cluster's two or four pairs to a tile need neither parts in memory nor the second kernel, 7 to 10 us,
-  // but leave pairs idle, 0.42 us for each unit that a pair has more than a share: even at 22 (577 rows, 1280 x 1280: 13 us, 21
-  // with shares; 6000 rows, 768 x 768: 24 and 27; 12608: 34 and 32).  Not every SM finds partners: 14 clusters of eight
-  // blocks run at once and 16 do not (2000 rows, 1024 x 1024: 29 us), of four 32 do.
+  // but leave pairs idle, 0.42 us for each unit that a pair has more than a share: even at 22, by the sum of both.  With clusters and
+  // with shares: 577 rows, 1280 x 1280: 14 and 20 us; 3152, 1024 x 2048: 22 and 29; 4000, 1536 x 1280: 25 and 31; 6000, 768 x 768: 24 and
+  // 27; 7000, 1280 x 1280: 34 and 37; 8224: 39 and 40; 9000: 43 and 42; 12608, 768 x 768: 33 and 32; 1091, 520 x 776: 19 and 19.  Not every
+  // SM finds partners: 14 clusters of eight blocks run at once and 16 do not (2000 rows, 1024 x 1024: 29 us), of four 32 do.
   t.split = 1;
   if (t.cuts && pair && shape.groups == 1 && tiles <= 32) {
     const int split = tiles <= 14 ? 4 : 2, sum = (shape.rows + DW_ROWS - 1) / DW_ROWS, even = (int)(sum * tiles / most);

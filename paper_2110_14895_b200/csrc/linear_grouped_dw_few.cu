@@ -4,8 +4,8 @@
 // Parts of tiles that go through memory cost 256 KB each way and a second kernel, 7 to 10 us in all; here the pairs leave their sums
 // where the operands were, and each block adds up an equal number of rows, in the order of the pairs.  The pairs of a cluster
 // have equal shares of the rows, and there is one tile to a cluster.
-// 577 rows, 1280 x 1280: 13 us, 21 by way of memory; 3152 rows, 1024 x 2048: 21 and 28; 8224 rows, 1280 x 1280: 38 and
-// 39 (a pair has 65 units there instead of 44, at the 0.4 us that they take on all SMs).
+// 577 rows, 1280 x 1280: 14 us, 20 by way of memory; 3152 rows, 1024 x 2048: 22 and 29; 8224 rows, 1280 x 1280: 39 and
+// 40 (a pair has 65 units there instead of 44, at the 0.4 us that they take on all SMs).
 //
 // Every wait on a barrier in memory is bounded; on expiry the block raises the device status word and goes on to the barriers of
 // the block and the cluster, which all threads reach the same number of times.

@@ -13,11 +13,12 @@
 // across rows (backwards, slabs of 64 columns in the other major order), through a map of three dimensions whose bounds make
 // what lies behind a group's weights zero and not the next group's values.
 //
-// Bound by power and by shared memory: a stage of a pair takes in and gives out 64 KB in the 512 cycles of its products, 125 of
-// the 128 bytes a cycle, and a tile's way out 64 KB twice more for each result.  25216 rows of 16 groups, 1024 -> 4096: 160 us
-// with a bias (1325 TFLOP/s; the plain product of vit_op_linear 167), 179 with GELU, 203 with its argument kept; the input
-// gradient of the layer behind it 165, 197 with GELU's slope.  Results sent straight from registers, rows of 32 bytes a
-// thread, took 215 us instead of 203.
+// Bound by shared memory and the way out: a stage of a pair takes in and gives out 64 KB in the 512 cycles of its products, 125 of
+// the 128 bytes a cycle, and a tile's way out 64 KB twice more for each result; with GELU's argument kept the accumulator and the
+// biases are read twice, and a warp's one piece is waited for between its results.  25216 rows of 16 groups, 1024 -> 4096: 156 us
+// with a bias (1360 TFLOP/s), 172 with GELU, 195 with its argument kept (tensor pipe active 70 %); the input gradient of the layer
+// behind it 160, 196 with GELU's slope (72 %); 4096 -> 1024 with a residual 161.  Results sent straight from registers, rows of 32
+// bytes a thread, took 215 us where these took 203.
 //
 // Every mbarrier wait is bounded; on expiry the block raises the device status word, lets the copies and products in flight
 // finish (bounded), frees tensor memory and leaves.
